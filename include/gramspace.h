@@ -81,7 +81,7 @@
 extern "C" {
 #endif
 
-#define GS_ABI_VERSION 2
+#define GS_ABI_VERSION 3
 
 typedef enum {
     GS_OK = 0,
@@ -517,6 +517,108 @@ typedef enum { GS_SOFT_AUTO = 0, GS_SOFT_GRAM = 1, GS_SOFT_COORDS = 2 } gs_soft_
 gs_status gs_soft_select(const gs_soft_group *groups, int ngroups, gs_dtype pt, gs_dtype tt,
                          gs_sim_mode mode, float scale, float beta, gs_soft_form form,
                          void *stream);
+
+/*
+ * gs_cross_attention -- attention of one sequence's heads to the states of
+ * another (an encoder's), the attention of Sec. 2.2 with vectors of its own per
+ * sequence in the codebook's place.  For sequence b, position i < qlen[b], head
+ * h, and the live states j (j < klen[b], mask[b, j] != 0):
+ *   S[j] = scale <Q[b, i, h], K[b, j, h / G]>,  G = Hq / Hkv
+ *   O[b, i, h] = sum_j softmax_j(S)[j] V[b, j, h / G]
+ *   lse[b, h, i] = log sum_j exp S[j]
+ * A row without a live state gives O = 0 and lse = -inf, and so do positions
+ * i >= qlen[b], so every element of O and lse is written.  Q at those
+ * positions, and K and V of states that are not live, contribute nothing
+ * whatever they hold, NaN and infinities included.
+ *
+ * gs_cross_attention_grad -- the gradients of sum(O .* dO) with respect to Q, K
+ * and V, given that call's O and lse:
+ *   P = exp(S - lse)     dS = P (dO V^T - rowsum(dO .* O))
+ *   dV = P^T dO     dQ = scale dS K     dK = scale dS^T Q
+ * summed in fp32, in a fixed order, over the heads that share K and V.  Rows of
+ * positions i >= qlen[b] and of states that are not live are written as zeros.
+ * Where K or V stand for several sequences (sb = 0) dK and dV are still those
+ * of each sequence.
+ *
+ *   B, Lq, Lk  sequences, positions and states (each >= 0)
+ *   Hq, Hkv    heads; Hkv divides Hq      Dh  values a head, 1 <= Dh <= 128
+ *   qlen,klen  int32[B] device, nullable (Lq, Lk); taken as 0 below 0 and as Lq
+ *              or Lk above
+ *   mask       B x Lk bytes, device, ldm >= Lk, nullable
+ *   scale      finite, not zero (1e-30 <= |scale| <= 1e30)
+ *   Q, O, dO, dQ   B x Lq x Hq x Dh, K, V, dK, dV   B x Lk x Hkv x Dh, all of
+ *              type t in {F32, BF16}: element (b, i, h, d) at
+ *              p[b sb + i sl + h sh + d], strides >= 0; elements of an output
+ *              at places of their own.  Rows that start on 16-byte boundaries
+ *              with Dh a multiple of 16 bytes are the fast case
+ *   lse        float B x Hq x Lq; out (nullable) and in
+ *   ws         device workspace of the size that the _workspace call gives
+ *              (0: none), 16-byte aligned, contents unspecified; calls that may
+ *              run at the same time need one each
+ * fp32 accumulation; probabilities and their gradients enter the second
+ * products in type t.  The byte ranges of outputs must overlap neither inputs
+ * nor each other.
+ */
+typedef struct { void *p; int64_t sb, sl, sh; } gs_seq;
+
+typedef struct {
+    int64_t B, Lq, Lk, Hq, Hkv, Dh;
+    const int32_t *qlen, *klen;
+    const uint8_t *mask; int64_t ldm;
+    double scale;
+    gs_seq Q, K, V, O;
+    float *lse;
+    gs_seq dO, dQ, dK, dV;      /* gs_cross_attention_grad alone */
+} gs_cross_attn;
+
+/* Bytes of workspace (0 also for sizes that the calls reject). */
+size_t gs_cross_attention_workspace(const gs_cross_attn *a, gs_dtype t);
+size_t gs_cross_attention_grad_workspace(const gs_cross_attn *a, gs_dtype t);
+
+gs_status gs_cross_attention(const gs_cross_attn *a, gs_dtype t, void *ws, size_t ws_bytes, void *stream);
+gs_status gs_cross_attention_grad(const gs_cross_attn *a, gs_dtype t, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * gs_sample -- an entry drawn from each row of scores (gs_similarity's S, or
+ * logits), where argmax would take the best.  For row b with the scores x_j:
+ *   1. entries in falling order of x_j, equal ones by index; entries of -inf
+ *      and NaN are left out
+ *   2. weights w_j = exp((x_j - max x) / temperature)
+ *   3. top_k: the first top_k entries (<= 0: all)
+ *   4. top_p: of these the shortest run from the first whose weight is at least
+ *      top_p of theirs all (>= 1, NaN: all; <= 0: the first)
+ *   5. min_p: of these the ones with w_j >= min_p (<= 0, NaN: all; above 1 is 1)
+ *   6. idx: the first entry, by index, at which the sum of the kept weights
+ *      exceeds u times their total (u below 0 or NaN counts as 0; from 1 on
+ *      the last entry is taken)
+ * A temperature that is not above 0 takes the first entry of the order (the
+ * argmax, lowest index on ties).  Scores of +inf share the weight equally.  A
+ * row with no entry gives idx = -1, prob = 0, kept = 0.
+ *
+ *   S      in   B x M, st in {F32, BF16}, lds >= M, 1 <= M < 2^31
+ *   u      in   float[B] random numbers, device
+ *   p           HOST, nullable (plain softmax): per-row parameters as device
+ *               arrays of B, or, where an array is null, one value for all
+ *   idx    out  int32[B]
+ *   prob   out  float[B], nullable: the drawn entry's share of the kept weight
+ *   kept   out  int32[B], nullable: entries kept
+ *   ws          device workspace of >= gs_sample_workspace(st, B, M) bytes
+ *               (0: none), 16-byte aligned, contents unspecified; calls that
+ *               may run at the same time need one each
+ * Weights are formed in fp64 and summed as whole multiples of 2^-s of the
+ * largest, s = min(52, 62 - ceil(log2 M)), an entry of any weight counting at
+ * least one: results do not depend on the order of a sum.
+ */
+typedef struct {
+    const float *temperature; const int32_t *top_k; const float *top_p; const float *min_p;
+    float temperature_all; int32_t top_k_all; float top_p_all; float min_p_all;
+} gs_sampling;
+
+size_t gs_sample_workspace(gs_dtype st, int64_t B, int64_t M);
+
+gs_status gs_sample(const void *S, gs_dtype st, int64_t B, int64_t M, int64_t lds, const float *u,
+                    const gs_sampling *p, int32_t *idx, float *prob, int32_t *kept,
+                    void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

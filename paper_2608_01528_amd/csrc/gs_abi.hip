@@ -2,10 +2,12 @@
 // reporting and dispatch to the kernels.  Every check runs on the host before
 // any HIP call, so a rejected call touches neither the device nor its outputs.
 #include <atomic>
+#include <cmath>
 #include <mutex>
 #include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
+#include <initializer_list>
 #include <string>
 #include <algorithm>
 #include <vector>
@@ -68,15 +70,21 @@ bool overlap(const Span &a, const Span &b) {
 }
 
 // Outputs must overlap neither inputs nor each other.
-gs_status check_overlaps(const std::vector<Span> &in, const std::vector<Span> &out) {
-    for (size_t a = 0; a < out.size(); ++a) {
-        for (const Span &i : in)
-            if (overlap(out[a], i)) return fail(GS_ERR_ARG, "output %s overlaps input %s", out[a].name, i.name);
-        for (size_t b = a + 1; b < out.size(); ++b)
+gs_status check_overlaps(const Span *in, size_t nin, const Span *out, size_t nout) {
+    for (size_t a = 0; a < nout; ++a) {
+        for (size_t i = 0; i < nin; ++i)
+            if (overlap(out[a], in[i])) return fail(GS_ERR_ARG, "output %s overlaps input %s", out[a].name, in[i].name);
+        for (size_t b = a + 1; b < nout; ++b)
             if (overlap(out[a], out[b]))
                 return fail(GS_ERR_ARG, "outputs %s and %s overlap", out[a].name, out[b].name);
     }
     return GS_OK;
+}
+gs_status check_overlaps(const std::vector<Span> &in, const std::vector<Span> &out) {
+    return check_overlaps(in.data(), in.size(), out.data(), out.size());
+}
+gs_status check_overlaps(std::initializer_list<Span> in, std::initializer_list<Span> out) {
+    return check_overlaps(in.begin(), in.size(), out.begin(), out.size());
 }
 
 gs_status check_aligned(const void *p, size_t es, const char *name) {
@@ -274,6 +282,103 @@ public:
 private:
     gs::CompressOverlap ov_{nullptr, nullptr, nullptr};
 };
+
+// Tensors of gs_cross_attention: n0 x n1 x n2 rows of Dh values.
+struct SeqShape { int64_t n[3]; int64_t dh; };
+
+Span seq_span(const gs_seq &q, const SeqShape &z, size_t es, const char *name) {
+    Span s;
+    s.name = name;
+    if (!q.p || !z.n[0] || !z.n[1] || !z.n[2]) return s;
+    s.lo = static_cast<const char *>(q.p);
+    s.hi = s.lo + ((z.n[0] - 1) * q.sb + (z.n[1] - 1) * q.sl + (z.n[2] - 1) * q.sh + z.dh) * (int64_t)es;
+    return s;
+}
+
+constexpr int64_t SEQ_MAX = (int64_t)1 << 31;       // sizes and rows below this
+constexpr int64_t STRIDE_MAX = (int64_t)1 << 40;    // (elements: byte offsets stay far inside 64 bits)
+
+gs_status check_seq(const char *fn, const char *name, const gs_seq &q, const SeqShape &z, gs_dtype t, bool out) {
+    const int64_t st[3] = {q.sb, q.sl, q.sh};
+    for (int64_t s : st)
+        if (s < 0 || s >= STRIDE_MAX) return fail(GS_ERR_SHAPE, "%s: stride of %s out of range", fn, name);
+    if (!z.n[0] || !z.n[1] || !z.n[2]) return GS_OK;
+    if (!q.p) return fail(GS_ERR_ARG, "%s: %s is null", fn, name);
+    GS_CHECK(check_aligned(q.p, esize(t), name));
+    if (!out) return GS_OK;
+    // rows of their own: from the smallest stride up, each spans the ones below
+    int64_t s[3], n[3];
+    int k = 0;
+    for (int i = 0; i < 3; ++i)
+        if (z.n[i] > 1) s[k] = st[i], n[k] = z.n[i], ++k;
+    for (int i = 0; i < k; ++i)
+        for (int j = i + 1; j < k; ++j)
+            if (s[j] < s[i]) std::swap(s[i], s[j]), std::swap(n[i], n[j]);
+    int64_t extent = z.dh;
+    for (int i = 0; i < k; ++i) {
+        if (s[i] < extent) return fail(GS_ERR_SHAPE, "%s: rows of %s overlap one another", fn, name);
+        extent += (n[i] - 1) * s[i];
+    }
+    return GS_OK;
+}
+
+// Sizes that the kernels count in 32 bits.
+bool attn_sizes(const gs_cross_attn *a) {
+    if (a->B < 0 || a->Lq < 0 || a->Lk < 0 || a->Hq < 1 || a->Hkv < 1 || a->Hq % a->Hkv != 0) return false;
+    if (a->Dh < 1 || a->Dh > CROSS_ATTN_MAX_DH) return false;
+    const int64_t most = SEQ_MAX - 256;
+    if (a->B >= most || a->Lq >= most || a->Lk >= most || a->Hq >= most) return false;
+    // B Hkv (work-groups) and Lq G (packed rows) first, so that no product overflows
+    if (a->B * a->Hkv >= most || a->Lq * (a->Hq / a->Hkv) >= most) return false;
+    const int64_t bh = a->B * a->Hkv ? a->B * a->Hkv : 1;
+    return a->Lq * (a->Hq / a->Hkv) < most / bh && a->Lk < most / bh;
+}
+
+gs_status check_attn(const char *fn, const gs_cross_attn *a, gs_dtype t, bool grad) {
+    if (!a) return fail(GS_ERR_ARG, "%s: the problem is null", fn);
+    if (!is_batch_type(t)) return fail(GS_ERR_DTYPE, "%s: tensors must be f32 or bf16", fn);
+    if (!attn_sizes(a))
+        return fail(GS_ERR_SHAPE, "%s: need B, Lq, Lk >= 0, Hkv >= 1 dividing Hq, 1 <= Dh <= %d, and B Hq Lq and B Hkv Lk below 2^31 - 256",
+                    fn, CROSS_ATTN_MAX_DH);
+    if (!(std::fabs(a->scale) >= 1e-30 && std::fabs(a->scale) <= 1e30))
+        return fail(GS_ERR_ARG, "%s: |scale| must be in [1e-30, 1e30]", fn);
+    const SeqShape q{{a->B, a->Lq, a->Hq}, a->Dh}, k{{a->B, a->Lk, a->Hkv}, a->Dh};
+    GS_CHECK(check_seq(fn, "Q", a->Q, q, t, false));
+    GS_CHECK(check_seq(fn, "K", a->K, k, t, false));
+    GS_CHECK(check_seq(fn, "V", a->V, k, t, false));
+    GS_CHECK(check_seq(fn, "O", a->O, q, t, !grad));
+    GS_CHECK(check_aligned(a->lse, 4, "lse"));
+    GS_CHECK(check_aligned(a->qlen, 4, "qlen"));
+    GS_CHECK(check_aligned(a->klen, 4, "klen"));
+    if (a->mask && a->ldm < a->Lk) return fail(GS_ERR_SHAPE, "%s: leading dimension of mask is smaller than Lk", fn);
+    if (grad) {
+        if (!a->lse && a->B && a->Lq) return fail(GS_ERR_ARG, "%s: lse is null", fn);
+        GS_CHECK(check_seq(fn, "dO", a->dO, q, t, false));
+        GS_CHECK(check_seq(fn, "dQ", a->dQ, q, t, true));
+        GS_CHECK(check_seq(fn, "dK", a->dK, k, t, true));
+        GS_CHECK(check_seq(fn, "dV", a->dV, k, t, true));
+    }
+    return GS_OK;
+}
+
+gs_status check_ws(const char *fn, const void *ws, size_t ws_bytes, size_t need) {
+    if (!need) return GS_OK;
+    if (!ws) return fail(GS_ERR_WORKSPACE, "%s: workspace is null", fn);
+    if ((reinterpret_cast<uintptr_t>(ws) & 15u) != 0) return fail(GS_ERR_ALIGN, "%s: workspace must be 16-byte aligned", fn);
+    if (ws_bytes < need) return fail(GS_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, need);
+    return GS_OK;
+}
+
+Span bytes_span(const void *p, size_t n, const char *name) { return span(p, 1, (int64_t)n, (int64_t)n, 1, name); }
+
+// 16-byte pieces everywhere: rows of the tensor start on 16-byte boundaries.
+bool vec_rows(const gs_seq &q, const SeqShape &z, gs_dtype t) {
+    const int64_t per = 16 / (int64_t)esize(t);
+    if (z.dh % per || (reinterpret_cast<uintptr_t>(q.p) & 15u)) return false;
+    return (z.n[0] <= 1 || q.sb % per == 0) && (z.n[1] <= 1 || q.sl % per == 0) && (z.n[2] <= 1 || q.sh % per == 0);
+}
+
+SeqStrides strides(const gs_seq &q) { return SeqStrides{q.sb, q.sl, q.sh}; }
 
 }  // namespace
 
@@ -761,6 +866,113 @@ gs_status gs_soft_select(const gs_soft_group *groups, int ngroups, gs_dtype pt, 
     if (tiles == 0) return ok();
     GS_CHECK(check_device());
     return launched(launch_soft_select(pt, tt, a, (hipStream_t)stream), "gs_soft_select");
+}
+
+size_t gs_cross_attention_workspace(const gs_cross_attn *a, gs_dtype t) {
+    if (!a || !is_batch_type(t) || !attn_sizes(a)) return 0;
+    return cross_attn_workspace(t, a->B, a->Lq, a->Lk, a->Hq, a->Hkv, a->Dh);
+}
+
+size_t gs_cross_attention_grad_workspace(const gs_cross_attn *a, gs_dtype t) {
+    if (!a || !is_batch_type(t) || !attn_sizes(a)) return 0;
+    return cross_attn_grad_workspace(a->B, a->Lq, a->Hq);
+}
+
+gs_status gs_cross_attention(const gs_cross_attn *p, gs_dtype t, void *ws, size_t ws_bytes, void *stream) {
+    const char *fn = "gs_cross_attention";
+    GS_CHECK(check_attn(fn, p, t, false));
+    const size_t es = esize(t), need = gs_cross_attention_workspace(p, t);
+    GS_CHECK(check_ws(fn, ws, ws_bytes, need));
+    const SeqShape q{{p->B, p->Lq, p->Hq}, p->Dh}, k{{p->B, p->Lk, p->Hkv}, p->Dh};
+    GS_CHECK(check_overlaps({seq_span(p->Q, q, es, "Q"), seq_span(p->K, k, es, "K"), seq_span(p->V, k, es, "V"),
+                             span(p->qlen, 1, p->B, p->B, 4, "qlen"), span(p->klen, 1, p->B, p->B, 4, "klen"),
+                             span(p->mask, p->B, p->Lk, p->ldm, 1, "mask")},
+                            {seq_span(p->O, q, es, "O"), span(p->lse, 1, p->B * p->Hq * p->Lq, 1, 4, "lse"),
+                             bytes_span(ws, need, "workspace")}));
+    if (p->B == 0 || p->Lq == 0) return ok();
+    GS_CHECK(check_device());
+    CrossAttnArgs a{};
+    a.Q = p->Q.p; a.K = p->K.p; a.V = p->V.p; a.O = p->O.p; a.lse = p->lse;
+    a.q = strides(p->Q); a.k = strides(p->K); a.v = strides(p->V); a.o = strides(p->O);
+    a.B = (int)p->B; a.Lq = (int)p->Lq; a.Lk = (int)p->Lk; a.Hq = (int)p->Hq; a.Hkv = (int)p->Hkv; a.Dh = (int)p->Dh;
+    a.G = a.Hq / a.Hkv;
+    a.qlen = p->qlen; a.klen = p->klen; a.mask = p->mask; a.mask_ld = p->ldm;
+    a.scale = (float)p->scale;
+    a.vec = vec_rows(p->Q, q, t) && vec_rows(p->K, k, t) && vec_rows(p->V, k, t) && vec_rows(p->O, q, t);
+    return launched(launch_cross_attn(t, a, ws, (hipStream_t)stream), fn);
+}
+
+gs_status gs_cross_attention_grad(const gs_cross_attn *p, gs_dtype t, void *ws, size_t ws_bytes, void *stream) {
+    const char *fn = "gs_cross_attention_grad";
+    GS_CHECK(check_attn(fn, p, t, true));
+    const size_t es = esize(t), need = gs_cross_attention_grad_workspace(p, t);
+    GS_CHECK(check_ws(fn, ws, ws_bytes, need));
+    const SeqShape q{{p->B, p->Lq, p->Hq}, p->Dh}, k{{p->B, p->Lk, p->Hkv}, p->Dh};
+    GS_CHECK(check_overlaps({seq_span(p->Q, q, es, "Q"), seq_span(p->K, k, es, "K"), seq_span(p->V, k, es, "V"),
+                             seq_span(p->O, q, es, "O"), seq_span(p->dO, q, es, "dO"),
+                             span(p->lse, 1, p->B * p->Hq * p->Lq, 1, 4, "lse"),
+                             span(p->qlen, 1, p->B, p->B, 4, "qlen"), span(p->klen, 1, p->B, p->B, 4, "klen"),
+                             span(p->mask, p->B, p->Lk, p->ldm, 1, "mask")},
+                            {seq_span(p->dQ, q, es, "dQ"), seq_span(p->dK, k, es, "dK"), seq_span(p->dV, k, es, "dV"),
+                             bytes_span(ws, need, "workspace")}));
+    if (p->B == 0 || (p->Lq == 0 && p->Lk == 0)) return ok();
+    GS_CHECK(check_device());
+    CrossAttnGradArgs a{};
+    a.Q = p->Q.p; a.K = p->K.p; a.V = p->V.p; a.O = p->O.p; a.dO = p->dO.p; a.lse = p->lse;
+    a.dQ = p->dQ.p; a.dK = p->dK.p; a.dV = p->dV.p;
+    a.q = strides(p->Q); a.k = strides(p->K); a.v = strides(p->V); a.o = strides(p->O);
+    a.d = strides(p->dO); a.dq = strides(p->dQ); a.dk = strides(p->dK); a.dv = strides(p->dV);
+    a.B = (int)p->B; a.Lq = (int)p->Lq; a.Lk = (int)p->Lk; a.Hq = (int)p->Hq; a.Hkv = (int)p->Hkv; a.Dh = (int)p->Dh;
+    a.G = a.Hq / a.Hkv;
+    a.qlen = p->qlen; a.klen = p->klen; a.mask = p->mask; a.mask_ld = p->ldm;
+    a.scale = (float)p->scale;
+    a.vec = vec_rows(p->Q, q, t) && vec_rows(p->K, k, t) && vec_rows(p->V, k, t) && vec_rows(p->O, q, t) &&
+            vec_rows(p->dO, q, t) && vec_rows(p->dQ, q, t) && vec_rows(p->dK, k, t) && vec_rows(p->dV, k, t);
+    return launched(launch_cross_attn_grad(t, a, ws, (hipStream_t)stream), fn);
+}
+
+size_t gs_sample_workspace(gs_dtype st, int64_t B, int64_t M) {
+    (void)st; (void)B; (void)M;
+    return 0;
+}
+
+gs_status gs_sample(const void *S, gs_dtype st, int64_t B, int64_t M, int64_t lds, const float *u,
+                    const gs_sampling *p, int32_t *idx, float *prob, int32_t *kept,
+                    void *ws, size_t ws_bytes, void *stream) {
+    const char *fn = "gs_sample";
+    if (!is_batch_type(st)) return fail(GS_ERR_DTYPE, "%s: scores must be f32 or bf16", fn);
+    if (B < 0 || B >= SEQ_MAX - 256 || M < 1 || M >= SEQ_MAX - 256)
+        return fail(GS_ERR_SHAPE, "%s: need 0 <= B and 1 <= M, both below 2^31 - 256", fn);
+    GS_CHECK(check_matrix(S, "S", B, M, lds, st, false));
+    if (lds >= STRIDE_MAX) return fail(GS_ERR_SHAPE, "%s: leading dimension of S out of range", fn);
+    if (B > 0 && !u) return fail(GS_ERR_ARG, "%s: u is null", fn);
+    if (B > 0 && !idx) return fail(GS_ERR_ARG, "%s: idx is null", fn);
+    const gs_sampling plain = {nullptr, nullptr, nullptr, nullptr, 1.f, 0, 1.f, 0.f};
+    const gs_sampling &q = p ? *p : plain;
+    GS_CHECK(check_aligned(u, 4, "u"));
+    GS_CHECK(check_aligned(q.temperature, 4, "temperature"));
+    GS_CHECK(check_aligned(q.top_k, 4, "top_k"));
+    GS_CHECK(check_aligned(q.top_p, 4, "top_p"));
+    GS_CHECK(check_aligned(q.min_p, 4, "min_p"));
+    GS_CHECK(check_aligned(idx, 4, "idx"));
+    GS_CHECK(check_aligned(prob, 4, "prob"));
+    GS_CHECK(check_aligned(kept, 4, "kept"));
+    const size_t need = gs_sample_workspace(st, B, M);
+    GS_CHECK(check_ws(fn, ws, ws_bytes, need));
+    GS_CHECK(check_overlaps({span(S, B, M, lds, esize(st), "S"), span(u, 1, B, B, 4, "u"),
+                             span(q.temperature, 1, B, B, 4, "temperature"), span(q.top_k, 1, B, B, 4, "top_k"),
+                             span(q.top_p, 1, B, B, 4, "top_p"), span(q.min_p, 1, B, B, 4, "min_p")},
+                            {span(idx, 1, B, B, 4, "idx"), span(prob, 1, B, B, 4, "prob"),
+                             span(kept, 1, B, B, 4, "kept"), bytes_span(ws, need, "workspace")}));
+    if (B == 0) return ok();
+    GS_CHECK(check_device());
+    SampleArgs a{};
+    a.S = S; a.lds = lds; a.B = B; a.M = M; a.u = u;
+    a.temperature = q.temperature; a.top_k = q.top_k; a.top_p = q.top_p; a.min_p = q.min_p;
+    a.temperature_all = q.temperature_all; a.top_k_all = q.top_k_all;
+    a.top_p_all = q.top_p_all; a.min_p_all = q.min_p_all;
+    a.idx = idx; a.prob = prob; a.kept = kept;
+    return launched(launch_sample(st, a, (hipStream_t)stream), fn);
 }
 
 }  // extern "C"

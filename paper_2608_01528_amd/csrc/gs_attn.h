@@ -1,0 +1,170 @@
+// Tiles shared by the cross-attention kernels (forward and gradient).
+//
+// A 32 x 32 score block is formed on the matrix cores with the side that a
+// wave keeps in registers (32 query rows, or 32 keys in the gradient of K and
+// V) as its columns: lane l holds column l % 32 and, of the block's rows,
+// 8 g + 4 (l / 32) + e in accumulator register 4 g + e (g, e = 0..3).  The
+// second product sums over those rows.  A contraction may take its terms in
+// any order as long as both operands agree, so the accumulator registers are
+// the second product's operand as they stand: register block PER s .. PER s +
+// PER - 1 is the fragment of step s, and col_frag reads the other operand in
+// the same order.  Scores never cross lanes, but for the two halves of a column.
+#pragma once
+
+#include "gs_internal.h"
+
+namespace gs {
+namespace attn {
+
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef float f4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u2v __attribute__((ext_vector_type(2)));
+typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
+typedef short s4v __attribute__((ext_vector_type(4)));
+#define GS_LDS __attribute__((address_space(3)))
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// Fragments: PER values a lane and step, 2 PER values of the contraction.
+template <typename T> struct Op;
+template <> struct Op<bf16_t> {
+    static constexpr int PER = 8;
+    typedef bf8v V;
+    static __device__ __forceinline__ f16v mma(V a, V b, f16v c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+    // registers PER s .. of an accumulator, rounded to bf16 (nearest even): the
+    // probabilities and their gradients enter the second product in the inputs'
+    // type, which costs each term half a step of that type, as the inputs' own
+    // rounding did
+    static __device__ __forceinline__ V pack(const f16v &p, int s) {
+        V r;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = (__bf16)p[8 * s + e];
+        return r;
+    }
+};
+template <> struct Op<float> {
+    static constexpr int PER = 4;
+    typedef f4v V;
+    static __device__ __forceinline__ f16v mma(V a, V b, f16v c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+    static __device__ __forceinline__ V pack(const f16v &p, int s) {
+        V r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = p[4 * s + e];
+        return r;
+    }
+};
+
+// A tile in LDS: rows of DP values, in 16-byte chunks.  Chunk c of row r lies
+// at position c ^ swizzle(r): eight consecutive rows put the same chunk on
+// eight different positions (row_frag reads one chunk of 32 rows), and four
+// consecutive rows put a pair of chunks on four different pairs (the transpose
+// reads of col_frag take 32 bytes of four rows).
+__device__ __forceinline__ int swizzle(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+template <typename T, int DP> __device__ __forceinline__ int place(int r, int c) {
+    return (r * (DP / Op<T>::PER) + (c ^ swizzle(r))) * 16;
+}
+
+// Operand whose rows are the tile's rows row0 + 0..31, step s of the
+// contraction over a row's values.
+template <typename T, int DP>
+__device__ __forceinline__ typename Op<T>::V row_frag(const char *tile, int row0, int s, int l) {
+    return *reinterpret_cast<const typename Op<T>::V *>(tile + place<T, DP>(row0 + (l & 31), 2 * s + (l >> 5)));
+}
+
+// Operand whose rows are the values 32 j + 0..31 of the tile's rows, step s of
+// the contraction over the rows row0 + 0..31 in accumulator order.
+template <typename T, int DP>
+__device__ __forceinline__ typename Op<T>::V col_frag(const char *tile, int row0, int s, int j, int l) {
+    if constexpr (sizeof(T) == 4) {
+        f4v r;
+        const int n = 32 * j + (l & 31), k = row0 + 8 * s + 4 * (l >> 5);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = *reinterpret_cast<const float *>(tile + place<T, DP>(k + e, n >> 2) + 4 * (n & 3));
+        return r;
+    } else {
+        // two transpose reads: 16 lanes read four rows of 16 values and each
+        // gets one value of the four rows
+        const int gq = l >> 4, a = l & 15;
+        const int n = 32 * j + 16 * (gq & 1) + 4 * (a & 3);
+        const int k = row0 + 16 * s + 4 * (gq >> 1) + (a >> 2);
+        const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GS_LDS s4v *)(tile + place<T, DP>(k, n >> 3) + 2 * (n & 7)));
+        const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GS_LDS s4v *)(tile + place<T, DP>(k + 8, n >> 3) + 2 * (n & 7)));
+        const s4v both[2] = {lo, hi};
+        return *reinterpret_cast<const bf8v *>(both);
+    }
+}
+
+// 16 bytes (PER values) of a row from value d on; zeros at and past dh.  vec:
+// rows start on 16-byte boundaries and dh is a multiple of PER.
+template <typename T> __device__ __forceinline__ u4v load_chunk(const T *row, int d, int dh, bool vec) {
+    u4v r = {0, 0, 0, 0};
+    if (vec) {
+        if (d < dh) r = *reinterpret_cast<const u4v *>(row + d);
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (d + e < dh) r[e] = __float_as_uint(row[d + e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (d + e < dh) r[e >> 1] |= (uint32_t)row[d + e].bits << (16 * (e & 1));
+    }
+    return r;
+}
+
+// Four consecutive values of a row, rounded to T once.
+template <typename T> __device__ __forceinline__ void store4(T *row, int d, int dh, bool vec, f4v v) {
+    if (vec) {
+        if (d >= dh) return;
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<f4v *>(row + d) = v;
+        } else {
+            u2v p;
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                p[e] = (uint32_t)f32_to_bf16(v[2 * e]) | (uint32_t)f32_to_bf16(v[2 * e + 1]) << 16;
+            *reinterpret_cast<u2v *>(row + d) = p;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (d + e < dh) st_f32<T>(row, d + e, v[e]);
+    }
+}
+
+__device__ __forceinline__ int clamped(const int32_t *len, int b, int most) {
+    if (!len) return most;
+    const int n = len[b];
+    return n < 0 ? 0 : (n > most ? most : n);
+}
+
+// Fragments of the side that stays in registers: row's values as the column
+// l % 32 of a product; a null row gives zeros.
+template <typename T, int DP>
+__device__ __forceinline__ void load_frags(typename Op<T>::V (&f)[DP / (2 * Op<T>::PER)], const T *row, int dh, bool vec, int l) {
+    constexpr int PER = Op<T>::PER;
+#pragma unroll
+    for (int s = 0; s < DP / (2 * PER); ++s) {
+        u4v v = {0, 0, 0, 0};
+        if (row) v = load_chunk<T>(row, PER * (2 * s + (l >> 5)), dh, vec);
+        f[s] = *reinterpret_cast<const typename Op<T>::V *>(&v);
+    }
+}
+
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+// Consecutive logical work-groups (which share what they read) on one XCD.
+__device__ __forceinline__ int64_t logical_group(int64_t total) {
+    const int64_t per = (total + 7) / 8;
+    return (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+}
+
+}  // namespace attn
+}  // namespace gs

@@ -229,6 +229,58 @@ struct SparseArgs {
 };
 hipError_t launch_sparse_prob2vec(gs_dtype tv, gs_dtype tt, const SparseArgs &a, hipStream_t s);
 
+// Cross attention (gs_xattn.hip) and its gradient (gs_xattn_grad.hip).
+constexpr int CROSS_ATTN_MAX_DH = 128;
+struct SeqStrides { int64_t b, l, h; };     // elements between sequences, positions, heads
+struct CrossAttnArgs {
+    const void *Q, *K, *V;
+    void *O;
+    float *lse;                         // B x Hq x Lq, nullable
+    SeqStrides q, k, v, o;
+    int B, Lq, Lk, Hq, Hkv, Dh, G;      // G = Hq / Hkv
+    const int32_t *qlen, *klen;         // B, nullable
+    const uint8_t *mask; int64_t mask_ld;   // B x Lk, nullable
+    float scale;
+    bool vec;                           // 16-byte aligned rows, Dh a whole number of 16-byte pieces
+    // set by launch_cross_attn
+    int rows, row_tiles, splits, split_keys;
+    int64_t groups;
+    float *part, *part_lse;             // parts of rows: B Hkv x rows x splits (x DP)
+};
+size_t cross_attn_workspace(gs_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh);
+hipError_t launch_cross_attn(gs_dtype t, CrossAttnArgs a, void *ws, hipStream_t s);
+struct CrossAttnGradArgs {
+    const void *Q, *K, *V, *O, *dO;
+    const float *lse;
+    void *dQ, *dK, *dV;
+    SeqStrides q, k, v, o, d, dq, dk, dv;
+    int B, Lq, Lk, Hq, Hkv, Dh, G;
+    const int32_t *qlen, *klen;
+    const uint8_t *mask; int64_t mask_ld;
+    float scale;
+    bool vec;
+    // set by launch_cross_attn_grad
+    int rows, row_tiles, key_tiles;
+    int64_t q_groups, k_groups;
+    float *D;                           // B x Hq x Lq: sum_d dO O
+};
+size_t cross_attn_grad_workspace(int64_t B, int64_t Lq, int64_t Hq);
+hipError_t launch_cross_attn_grad(gs_dtype t, CrossAttnGradArgs a, void *ws, hipStream_t s);
+
+// Sampling of entries from scores (gs_sample.hip).
+struct SampleArgs {
+    const void *S; int64_t lds;
+    int64_t B, M;
+    const float *u;
+    const float *temperature; const int32_t *top_k; const float *top_p, *min_p;     // B, nullable
+    float temperature_all; int32_t top_k_all; float top_p_all, min_p_all;           // where those are null
+    int32_t *idx;
+    float *prob;                        // nullable
+    int32_t *kept;                      // nullable
+    double unit;                        // set by launch_sample
+};
+hipError_t launch_sample(gs_dtype st, SampleArgs a, hipStream_t s);
+
 // Compression.
 size_t compress_workspace(int64_t M, int64_t D);
 // A second stream (non-blocking, default priority) on which compression runs

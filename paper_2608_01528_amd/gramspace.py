@@ -6,7 +6,8 @@ Two layers with the C names:
   pointers exactly as declared in the header.
 * `gs_compress`, `gs_compress_padded`, `gs_compress_partitioned`, `gs_compress_noalloc`, `gs_project`, `gs_prob2vec`, `gs_prob2vec_sparse`,
   `gs_similarity`,
-  `gs_attention`, `gs_similarity_attention`, `gs_reconstruct`, `gs_bind_coords`, `gs_soft_select` and `gs_bind_restored`
+  `gs_attention`, `gs_similarity_attention`, `gs_reconstruct`, `gs_bind_coords`, `gs_soft_select`, `gs_bind_restored`,
+  `gs_cross_attention`, `gs_cross_attention_grad` and `gs_sample`
   below take torch tensors on the current
   GPU, allocate the outputs with torch, and pass pointers, sizes and the
   current stream to the library.  They only marshal arguments: every step of
@@ -19,6 +20,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -101,6 +103,19 @@ _SIGS["gs_bind_coords"] = ([_vp, ctypes.c_int, _i64, _i64, _i64, _vp, _i64, _vp,
 
 _SIGS["gs_soft_select"] = ([ctypes.POINTER(SoftGroup), ctypes.c_int, ctypes.c_int, ctypes.c_int,
                             ctypes.c_int, ctypes.c_float, ctypes.c_float, ctypes.c_int, _vp], ctypes.c_int)
+
+# gs_cross_attn and gs_sampling are handed over as packed bytes (their fields
+# in order: 8-byte integers and pointers, one double; four pointers, then
+# float, int32, float, float)
+_SIGS["gs_cross_attention_workspace"] = ([_vp, ctypes.c_int], ctypes.c_size_t)
+_SIGS["gs_cross_attention_grad_workspace"] = ([_vp, ctypes.c_int], ctypes.c_size_t)
+_SIGS["gs_cross_attention"] = ([_vp, ctypes.c_int, _vp, ctypes.c_size_t, _vp], ctypes.c_int)
+_SIGS["gs_cross_attention_grad"] = ([_vp, ctypes.c_int, _vp, ctypes.c_size_t, _vp], ctypes.c_int)
+_SIGS["gs_sample_workspace"] = ([ctypes.c_int, _i64, _i64], ctypes.c_size_t)
+_SIGS["gs_sample"] = ([_vp, ctypes.c_int, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp],
+                      ctypes.c_int)
+_ATTN = struct.Struct("=6q3Qqd" + "Q3q" * 4 + "Q" + "Q3q" * 4)
+_SAMPLING = struct.Struct("=4Qfiff")
 
 
 def lib():
@@ -561,3 +576,168 @@ def gs_soft_select(groups, mode="cosine", scale: float = 1.0, beta: float = 1.0,
     arr, pt, tt = prepared if prepared is not None else soft_groups(groups)
     _check(lib().gs_soft_select(arr, len(arr), pt, tt, _mode(mode), float(scale), float(beta),
                                 _SOFT_FORMS[form], _stream()))
+
+
+# ------------------------------------------------ sequences and drawn entries
+
+def _here(t: torch.Tensor, name: str, dtype=None):
+    """A GPU tensor of the current device (the call goes to that device's
+    current stream)."""
+    if not t.is_cuda:
+        raise ValueError("%s must be on the GPU" % name)
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("%s must be on the current device" % name)
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError("%s must be %s, is %s" % (name, dtype, t.dtype))
+
+
+def _seq(t: torch.Tensor, name: str, shape, dtype):
+    """Address and strides of a 4-D tensor of the given shape and type."""
+    if t.shape != shape:
+        raise ValueError("%s must be %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    _here(t, name, dtype)
+    s = t.stride()
+    if s[3] != 1 and shape[3] > 1:
+        raise ValueError("%s must have values of a head side by side (unit last stride)" % name)
+    return t.data_ptr(), s[0], s[1], s[2]
+
+
+def _per_row(t, name: str, n: int, dtype):
+    """Address of a contiguous vector of n entries, 0 for None."""
+    if t is None:
+        return 0
+    _here(t, name, dtype)
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be contiguous with %d entries" % (name, n))
+    return t.data_ptr()
+
+
+def _workspace(need: int, given, device):
+    """(address, bytes, keeper) of a workspace of at least `need` bytes."""
+    if not need:
+        return None, 0, None
+    if given is None:
+        given = torch.empty(need, dtype=torch.uint8, device=device)
+    else:
+        _here(given, "workspace")
+        if not given.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+    return given.data_ptr(), given.numel() * given.element_size(), given
+
+
+_NO_SEQ = (0, 0, 0, 0)
+
+
+def _attn_problem(Q, K, V, O, lse, qlen, klen, mask, scale, grads=None):
+    """The packed gs_cross_attn and the element type."""
+    q, k = Q.shape, K.shape
+    if len(q) != 4 or len(k) != 4:
+        raise ValueError("Q must be (B, Lq, Hq, Dh), K and V (B, Lk, Hkv, Dh)")
+    B, Lq, Hq, Dh = q
+    Lk, Hkv = k[1], k[2]
+    if k[0] != B or k[3] != Dh:
+        raise ValueError("K must be (%d, Lk, Hkv, %d), got %s" % (B, Dh, tuple(k)))
+    dtype = Q.dtype
+    t = _DT.get(dtype)
+    if t is None:
+        raise ValueError("Q: unsupported dtype %s" % dtype)
+    ldm = Lk
+    mp = 0
+    if mask is not None:
+        if mask.dtype not in (torch.bool, torch.uint8):
+            raise ValueError("mask must be bool or uint8")
+        _here(mask, "mask")
+        if mask.shape != (B, Lk):
+            raise ValueError("mask must be (%d, %d), got %s" % (B, Lk, tuple(mask.shape)))
+        if (Lk > 1 and mask.stride(1) != 1) or (B > 1 and mask.stride(0) < Lk):
+            raise ValueError("mask must have rows of its own with unit column stride")
+        mp, ldm = mask.data_ptr(), max(mask.stride(0), Lk)
+    lp = 0
+    if lse is not None:
+        _here(lse, "lse", torch.float32)
+        if lse.shape != (B, Hq, Lq) or not lse.is_contiguous():
+            raise ValueError("lse must be contiguous (%d, %d, %d)" % (B, Hq, Lq))
+        lp = lse.data_ptr()
+    rest = _NO_SEQ * 4
+    if grads is not None:
+        dO, dQ, dK, dV = grads
+        rest = _seq(dO, "dO", q, dtype) + _seq(dQ, "dQ", q, dtype) + _seq(dK, "dK", k, dtype) + _seq(dV, "dV", k, dtype)
+    return _ATTN.pack(B, Lq, Lk, Hq, Hkv, Dh, _per_row(qlen, "qlen", B, torch.int32),
+                      _per_row(klen, "klen", B, torch.int32), mp, ldm, float(Dh ** -0.5 if scale is None else scale),
+                      *_seq(Q, "Q", q, dtype), *_seq(K, "K", k, dtype), *_seq(V, "V", k, dtype),
+                      *_seq(O, "O", q, dtype), lp, *rest), t
+
+
+def gs_cross_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, qlen=None, klen=None, mask=None,
+                       scale: float | None = None, lse: bool = False, out: torch.Tensor | None = None,
+                       lse_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """O = softmax(scale Q K^T) V, head by head, over each sequence's live
+    states: Q (B, Lq, Hq, Dh), K and V (B, Lk, Hkv, Dh) with Hkv dividing Hq;
+    qlen, klen (int32, B) lengths; mask (B, Lk) bool, False for states left
+    out; scale 1 / sqrt(Dh) by default.  Any strides but the last dimension's.
+    Returns O, or (O, lse) with lse (B, Hq, Lq) fp32."""
+    if out is None:
+        out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+    if lse_out is None and lse:
+        B, Lq, Hq = Q.shape[:3]
+        lse_out = torch.empty((B, Hq, Lq), dtype=torch.float32, device=Q.device)
+    p, t = _attn_problem(Q, K, V, out, lse_out, qlen, klen, mask, scale)
+    L = lib()
+    ws, n, _keep = _workspace(L.gs_cross_attention_workspace(p, t), workspace, Q.device)
+    _check(L.gs_cross_attention(p, t, ws, n, _stream()))
+    return (out, lse_out) if lse else out
+
+
+def gs_cross_attention_grad(dO: torch.Tensor, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.Tensor,
+                            lse: torch.Tensor, qlen=None, klen=None, mask=None, scale: float | None = None, out=None,
+                            workspace: torch.Tensor | None = None):
+    """Gradients (dQ, dK, dV) of sum(O * dO) for gs_cross_attention with the
+    same arguments, from its O and lse.  `out`: three tensors to write into.
+    K or V expanded over the batch get the gradients of each sequence."""
+    if out is None:
+        out = tuple(torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (Q, K, V))
+    dQ, dK, dV = out
+    p, t = _attn_problem(Q, K, V, O, lse, qlen, klen, mask, scale, (dO, dQ, dK, dV))
+    L = lib()
+    ws, n, _keep = _workspace(L.gs_cross_attention_grad_workspace(p, t), workspace, Q.device)
+    _check(L.gs_cross_attention_grad(p, t, ws, n, _stream()))
+    return dQ, dK, dV
+
+
+def gs_sample(S: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+              prob: bool = False, kept: bool = False, idx_out: torch.Tensor | None = None,
+              prob_out: torch.Tensor | None = None, kept_out: torch.Tensor | None = None,
+              workspace: torch.Tensor | None = None):
+    """One entry of each row of scores S (B x M), drawn by the random numbers u
+    (fp32, B, in [0, 1)) after temperature, top_k (0: all), top_p and min_p,
+    each one number for all rows or a tensor of B (fp32; top_k int32).
+    Returns idx (int32, B; -1 for a row of -inf), or a tuple with prob (fp32,
+    the entry's share of the kept weight) and kept (int32, entries kept) where
+    asked for."""
+    st, lds = _mat(S, "S")
+    _here(S, "S")
+    B, M = S.shape
+    if B > 1 and S.stride(0) < M:
+        raise ValueError("S must have rows of its own")
+    f32, i32, dev = torch.float32, torch.int32, S.device
+    at, one = [0, 0, 0, 0], [1.0, 0, 1.0, 0.0]
+    for i, (name, v, dt) in enumerate((("temperature", temperature, f32), ("top_k", top_k, i32),
+                                       ("top_p", top_p, f32), ("min_p", min_p, f32))):
+        if isinstance(v, torch.Tensor):
+            at[i] = _per_row(v, name, B, dt)
+        else:
+            one[i] = v
+    one[1] = min(max(int(one[1]), 0), 0x7fffffff)
+    idx = idx_out if idx_out is not None else torch.empty(B, dtype=i32, device=dev)
+    pr = (prob_out if prob_out is not None else torch.empty(B, dtype=f32, device=dev)) if prob else None
+    kp = (kept_out if kept_out is not None else torch.empty(B, dtype=i32, device=dev)) if kept else None
+    if u is None:
+        raise ValueError("u must be a tensor of random numbers")
+    L = lib()
+    ws, n, _keep = _workspace(L.gs_sample_workspace(st, B, M), workspace, dev)
+    _check(L.gs_sample(S.data_ptr(), st, B, M, lds, _per_row(u, "u", B, f32), _SAMPLING.pack(*at, *one),
+                       _per_row(idx, "idx_out", B, i32), _per_row(pr, "prob_out", B, f32) or None,
+                       _per_row(kp, "kept_out", B, i32) or None, ws, n, _stream()))
+    if not (prob or kept):
+        return idx
+    return (idx,) + ((pr,) if prob else ()) + ((kp,) if kept else ())

@@ -1,0 +1,259 @@
+"""Cross attention and its gradient on the GPU against 64 bits."""
+import math
+
+import pytest
+import torch
+
+import attn_util
+from paper_2608_01528_amd import gramspace as gs
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+INF, NAN = float("inf"), float("nan")
+
+
+def normal(seed, *shape, dtype=F32, factor=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * factor).to(dtype).cuda()
+
+
+def ints(*v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def problem(B, Lq, Lk, Hq, Hkv, Dh, dtype, seed=1, factor=1.0):
+    return (normal(seed, B, Lq, Hq, Dh, dtype=dtype, factor=factor), normal(seed + 1, B, Lk, Hkv, Dh, dtype=dtype, factor=factor),
+            normal(seed + 2, B, Lk, Hkv, Dh, dtype=dtype), normal(seed + 3, B, Lq, Hq, Dh, dtype=dtype))
+
+
+def whole(Q, K, V, dO, **kw):
+    """Forward and gradient; results by name."""
+    O, lse = gs.gs_cross_attention(Q, K, V, lse=True, **kw)
+    dQ, dK, dV = gs.gs_cross_attention_grad(dO, Q, K, V, O, lse, **kw)
+    return {"O": O, "lse": lse, "dQ": dQ, "dK": dK, "dV": dV}
+
+
+def agree(Q, K, V, dO, **kw):
+    got = whole(Q, K, V, dO, **kw)
+    ref = attn_util.reference(Q, K, V, dO=dO, **kw)
+    for n in got:
+        attn_util.check(got[n], ref, n)
+    return got
+
+
+SIZES = [
+    # B, Lq, Lk, Hq, Hkv, Dh
+    (1, 1, 1, 1, 1, 1),
+    (1, 1, 2, 1, 1, 64),
+    (2, 1, 61, 8, 8, 64),
+    (3, 1, 700, 8, 2, 128),     # one position: keys split over work-groups
+    (2, 2, 333, 6, 2, 80),
+    (1, 31, 64, 2, 2, 32),
+    (1, 32, 65, 2, 1, 64),
+    (2, 33, 63, 3, 3, 40),
+    (1, 128, 128, 4, 1, 128),
+    (2, 129, 257, 4, 2, 96),
+    (1, 200, 31, 5, 1, 127),    # rows that do not start on 16-byte boundaries
+    (1, 77, 129, 2, 2, 33),
+    (1, 3, 3000, 2, 1, 72),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("size", SIZES, ids=str)
+def test_sizes(size, dtype):
+    agree(*problem(*size, dtype))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("size", [(4, 70, 150, 4, 2, 64), (4, 1, 900, 8, 2, 128), (4, 9, 70, 3, 1, 50)], ids=str)
+def test_lengths_and_masks(size, dtype):
+    B, Lq, Lk = size[:3]
+    Q, K, V, dO = problem(*size, dtype)
+    g = torch.Generator().manual_seed(9)
+    mask = (torch.rand(B, Lk, generator=g) < 0.6).cuda()
+    mask[1] = False                                 # a sequence whose mask leaves nothing
+    mask[2, : min(Lk, 64)] = False                  # a whole tile of masked states
+    qlen, klen = ints(Lq, max(Lq - 3, 0), 1, Lq), ints(Lk, Lk, max(Lk - 5, 1), 0)
+    for kw in ({"mask": mask}, {"klen": klen}, {"qlen": qlen}, {"qlen": qlen, "klen": klen, "mask": mask},
+               {"mask": mask.to(torch.uint8) * 3}):
+        got = agree(Q, K, V, dO, **kw)
+        if "klen" in kw:
+            assert torch.equal(got["O"][3], torch.zeros_like(got["O"][3])) and (got["lse"][3] == -INF).all()
+    # lengths out of range are taken as the nearest one in it
+    far = agree(Q, K, V, dO, qlen=ints(Lq + 9, -3, 2 ** 31 - 1, Lq), klen=ints(-1, Lk + 1, 2 ** 31 - 1, -2 ** 31))
+    assert (far["lse"][0] == -INF).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("poison", [NAN, INF, -INF, "lowest"])
+def test_what_is_left_out_contributes_nothing(dtype, poison):
+    B, Lq, Lk, Hq, Hkv, Dh = 3, 40, 100, 4, 2, 64
+    if poison == "lowest":
+        poison = torch.finfo(dtype).min
+    Q, K, V, dO = problem(B, Lq, Lk, Hq, Hkv, Dh, dtype)
+    mask = (torch.arange(Lk, device="cuda")[None] % 3 != 1).repeat(B, 1)
+    qlen, klen = ints(40, 7, 0), ints(100, 50, 99)
+    kw = {"qlen": qlen, "klen": klen, "mask": mask}
+    clean = whole(Q, K, V, dO, **kw)
+    dead = ~mask | (torch.arange(Lk, device="cuda")[None] >= klen[:, None])
+    gone = torch.arange(Lq, device="cuda")[None] >= qlen[:, None]
+    K, V = (t.masked_fill(dead[:, :, None, None], poison) for t in (K, V))
+    Q, dO = (t.masked_fill(gone[:, :, None, None], poison) for t in (Q, dO))
+    got = whole(Q, K, V, dO, **kw)
+    for n in got:
+        assert torch.equal(got[n], clean[n]), n
+    for n in ("O", "dQ"):
+        assert (got[n][gone] == 0).all()
+    for n in ("dK", "dV"):
+        assert (got[n][dead] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_strides(dtype):
+    """Heads before positions, rows inside wider ones, values off 16-byte
+    boundaries, states shared by all sequences."""
+    B, Lq, Lk, Hq, Hkv, Dh = 2, 37, 90, 4, 2, 64
+    Q, K, V, dO = problem(B, Lq, Lk, Hq, Hkv, Dh, dtype)
+    plain = whole(Q, K, V, dO)
+
+    def heads_first(t):
+        return t.transpose(1, 2).contiguous().transpose(1, 2)
+
+    def inside(t, off):
+        wide = torch.full(t.shape[:3] + (t.shape[3] + 24,), NAN, dtype=dtype, device="cuda")
+        wide[..., off: off + t.shape[3]] = t
+        return wide[..., off: off + t.shape[3]]
+
+    for f in (heads_first, lambda t: inside(t, 8), lambda t: inside(t, 3)):
+        got = whole(f(Q), f(K), f(V), f(dO))
+        for n in plain:
+            assert torch.equal(got[n], plain[n]), n
+    outs = [f(torch.zeros_like(t)) for t, f in ((Q, heads_first), (K, lambda t: inside(t, 8)), (V, lambda t: inside(t, 5)))]
+    O, lse = gs.gs_cross_attention(Q, K, V, lse=True, out=inside(torch.zeros_like(Q), 8))
+    assert torch.equal(O, plain["O"])
+    for g, n in zip(gs.gs_cross_attention_grad(dO, Q, K, V, O, lse, out=outs), ("dQ", "dK", "dV")):
+        assert torch.equal(g, plain[n]), n
+    shared = [t[:1].expand(B, -1, -1, -1) for t in (K, V)]
+    agree(Q, *shared, dO)
+
+
+@pytest.mark.parametrize("size", [(2, 50, 100, 4, 2, 64), (3, 1, 2000, 4, 1, 72), (1, 20, 30, 2, 2, 33)], ids=str)
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_writes_its_outputs_and_nothing_else(size, dtype):
+    B, Lq, Lk, Hq, Hkv, Dh = size
+    Q, K, V, dO = problem(*size, dtype)
+    kw = {"qlen": ints(*[Lq - b for b in range(B)]), "klen": ints(*[Lk - b for b in range(B)])}
+    inputs = [t.clone() for t in (Q, K, V, dO)]
+
+    def framed(shape, dt):
+        n = math.prod(shape)
+        buf = torch.full((n + 512,), 77.0, dtype=dt, device="cuda")
+        return buf, buf[256: 256 + n].view(shape)
+
+    bufs = {n: framed(s, d) for n, s, d in (("O", Q.shape, dtype), ("lse", (B, Hq, Lq), F32), ("dQ", Q.shape, dtype),
+                                             ("dK", K.shape, dtype), ("dV", V.shape, dtype))}
+    gs.gs_cross_attention(Q, K, V, lse=True, out=bufs["O"][1], lse_out=bufs["lse"][1], **kw)
+    gs.gs_cross_attention_grad(dO, Q, K, V, bufs["O"][1], bufs["lse"][1], out=[bufs[n][1] for n in ("dQ", "dK", "dV")], **kw)
+    again = whole(Q, K, V, dO, **kw)
+    for n, (buf, view) in bufs.items():
+        assert (buf[:256] == 77).all() and (buf[-256:] == 77).all(), n
+        assert torch.equal(view, again[n]), n
+    for t, was in zip((Q, K, V, dO), inputs):
+        assert torch.equal(t, was)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_large_scores_and_scales(dtype):
+    """Scores of some hundreds: one state takes all the weight; negative scales."""
+    size = (1, 40, 130, 2, 2, 64)
+    Q, K, V, dO = problem(*size, dtype, factor=8.0)
+    for scale in (1.0, -0.7, 1e-6):
+        agree(Q, K, V, dO, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_gradient_against_differences(dtype):
+    """<gradient, E> against the central difference of sum(O dO) along E in 64
+    bits (step 1e-4: its own error is below 1e-6 of the terms)."""
+    Q, K, V, dO = problem(1, 9, 21, 4, 2, 24, dtype)
+    got = whole(Q, K, V, dO)
+    ref = attn_util.reference(Q, K, V, dO=dO)
+    d = dO.cpu().double()
+
+    def loss(q, k, v):
+        k, v = (t.repeat_interleave(2, dim=2) for t in (k, v))
+        S = torch.matmul(q.transpose(1, 2), k.permute(0, 2, 3, 1)) * 24 ** -0.5
+        return float((torch.matmul(torch.softmax(S, -1), v.transpose(1, 2)).transpose(1, 2) * d).sum())
+
+    at = [t.cpu().double() for t in (Q, K, V)]
+    for i, name in enumerate(("dQ", "dK", "dV")):
+        E = torch.randn(at[i].shape, generator=torch.Generator().manual_seed(i), dtype=torch.float64)
+        step = [[t + s * 1e-4 * E if x == i else t for x, t in enumerate(at)] for s in (1, -1)]
+        slope = (loss(*step[0]) - loss(*step[1])) / 2e-4
+        dot = got[name].cpu().double() * E
+        assert abs(float(dot.sum()) - slope) <= float((ref[name][1] * E.abs()).sum()) + 1e-6 * float(dot.abs().sum()), name
+
+
+def test_offsets_beyond_32_bits():
+    """States more than 2^31 bytes, and 2^31 elements, apart."""
+    Dh, far = 64, (1 << 30) + 64
+    Q = normal(1, 1, 2, 1, Dh, dtype=BF16)
+    dO = normal(4, 1, 2, 1, Dh, dtype=BF16)
+    room = torch.empty(3 * far, dtype=BF16, device="cuda")
+    K = room.as_strided((1, 3, 1, Dh), (0, far, Dh, 1))
+    V = room.as_strided((1, 3, 1, Dh), (0, far, Dh, 1), 4096)
+    K.copy_(normal(2, 1, 3, 1, Dh, dtype=BF16))
+    V.copy_(normal(3, 1, 3, 1, Dh, dtype=BF16))
+    agree(Q, K, V, dO)
+    packed = whole(Q, K.contiguous(), V.contiguous(), dO)
+    for n, t in whole(Q, K, V, dO).items():
+        assert torch.equal(t, packed[n]), n
+
+
+def test_empty_problems():
+    for B, Lq, Lk in ((0, 3, 4), (2, 0, 4), (2, 3, 0)):
+        Q, K, V, dO = problem(B, Lq, Lk, 2, 1, 64, BF16)
+        got = whole(Q, K, V, dO)
+        assert all((t == 0).all() for n, t in got.items() if n != "lse") and (got["lse"] == -INF).all()
+
+
+def test_on_another_stream_and_twice_at_once():
+    """Calls on two streams at the same time, each with its own workspace."""
+    Q, K, V, dO = problem(2, 1, 3000, 8, 2, 128, BF16)
+    Q2, K2, V2, dO2 = problem(2, 100, 300, 8, 2, 64, BF16, seed=11)
+    want, want2 = whole(Q, K, V, dO), whole(Q2, K2, V2, dO2)
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(s1):
+            got = whole(Q, K, V, dO)
+        with torch.cuda.stream(s2):
+            got2 = whole(Q2, K2, V2, dO2)
+        torch.cuda.synchronize()
+        for n in want:
+            assert torch.equal(got[n], want[n]) and torch.equal(got2[n], want2[n]), n
+
+
+def test_captured_and_replayed():
+    size = (2, 1, 1500, 8, 2, 64)
+    Q, K, V, dO = problem(*size, BF16)
+    klen = ints(1500, 700)
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        whole(Q, K, V, dO, klen=klen)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = whole(Q, K, V, dO, klen=klen)
+    for seed in (21, 31, 41):
+        for t, new in zip((Q, K, V, dO), problem(*size, BF16, seed=seed)):
+            t.copy_(new)
+        klen.copy_(ints(seed, 1500 - seed))
+        g.replay()
+        torch.cuda.synchronize()
+        eager = whole(Q, K, V, dO, klen=klen)
+        torch.cuda.synchronize()
+        for n in eager:
+            assert torch.equal(got[n], eager[n]), (seed, n)
