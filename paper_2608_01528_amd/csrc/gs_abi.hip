@@ -932,8 +932,8 @@ gs_status gs_cross_attention_grad(const gs_cross_attn *p, gs_dtype t, void *ws, 
 }
 
 size_t gs_sample_workspace(gs_dtype st, int64_t B, int64_t M) {
-    (void)st; (void)B; (void)M;
-    return 0;
+    if (!is_batch_type(st) || B < 1 || B >= SEQ_MAX - 256 || M < 1 || M >= SEQ_MAX - 256) return 0;
+    return sample_workspace(B, M);
 }
 
 gs_status gs_sample(const void *S, gs_dtype st, int64_t B, int64_t M, int64_t lds, const float *u,
@@ -972,7 +972,9 @@ gs_status gs_sample(const void *S, gs_dtype st, int64_t B, int64_t M, int64_t ld
     a.temperature_all = q.temperature_all; a.top_k_all = q.top_k_all;
     a.top_p_all = q.top_p_all; a.min_p_all = q.min_p_all;
     a.idx = idx; a.prob = prob; a.kept = kept;
-    return launched(launch_sample(st, a, (hipStream_t)stream), fn);
+    const size_t quad = 4 * esize(st);
+    a.vec = reinterpret_cast<uintptr_t>(S) % quad == 0 && (B == 1 || lds % 4 == 0);
+    return launched(launch_sample(st, a, ws, (hipStream_t)stream), fn);
 }
 
 }  // extern "C"

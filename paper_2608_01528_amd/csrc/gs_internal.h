@@ -277,9 +277,15 @@ struct SampleArgs {
     int32_t *idx;
     float *prob;                        // nullable
     int32_t *kept;                      // nullable
-    double unit;                        // set by launch_sample
+    bool vec;                           // rows start on boundaries of four entries
+    // set by launch_sample
+    int shift;
+    void *ws;
+    int64_t row0, row_bytes;
+    int chunks;
 };
-hipError_t launch_sample(gs_dtype st, SampleArgs a, hipStream_t s);
+size_t sample_workspace(int64_t B, int64_t M);
+hipError_t launch_sample(gs_dtype st, SampleArgs a, void *ws, hipStream_t s);
 
 // Compression.
 size_t compress_workspace(int64_t M, int64_t D);
