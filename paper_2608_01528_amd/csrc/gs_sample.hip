@@ -16,8 +16,12 @@
 //                       entries are in question, and these are ranked
 //   a work-group a row  up to 8192 entries, in registers: a histogram of the
 //                       scores below the largest finds the bin the run ends in
-//   work-groups a row   more entries: the same over chunks of 8192, in three
-//                       launches (largest score, histogram, entries of the bin)
+//   work-groups a row   more entries: the same over chunks of 8192, in four
+//                       launches (largest score, histogram, entries of the bin,
+//                       ranking and draw): a launch boundary hands a row's data
+//                       on faster than fences and counters did, which write the
+//                       caches back from every work-group (402 and 511 us for
+//                       the two launches they were in, against TIMES)
 #include "gs_internal.h"
 
 namespace gs {
@@ -86,6 +90,7 @@ struct Row {
         least = mp > 0.f ? fmin(1., (double)mp) : 0.;
         c = 1.4426950408889634074 / (double)temp;
     }
+    __device__ __forceinline__ bool keeps_all(int64_t M) const { return k >= M && p >= 1.; }
 };
 
 // The sum that the drawn entry's has to exceed.
@@ -124,29 +129,33 @@ __device__ __forceinline__ void load_keys(uint32_t *key, const T *row, int64_t j
 
 // ---------------------------------------------------------------- in a wave
 
-template <typename V, typename F> __device__ __forceinline__ V wave_reduce(V v, F f) {
-#pragma unroll
-    for (int x = 32; x; x >>= 1) v = f(v, (V)__shfl_xor(v, x));
-    return v;
+// Sums and maxima over a wave by moves between lanes within the vector unit:
+// within rows of 16 lanes by 1, 2, 4, 8, then from the rows before.  Lanes
+// without a source contribute 0.
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t moved(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
 }
-__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
-    return wave_reduce(v, [](uint64_t a, uint64_t b) { return a + b; });
+template <int CTRL, int ROWS> __device__ __forceinline__ uint64_t moved(uint64_t v) {
+    return (uint64_t)moved<CTRL, ROWS>((uint32_t)(v >> 32)) << 32 | moved<CTRL, ROWS>((uint32_t)v);
 }
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-    return wave_reduce(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+template <typename V, typename F> __device__ __forceinline__ V wave_scan(V v, F f) {
+    v = f(v, moved<0x111, 0xf>(v));
+    v = f(v, moved<0x112, 0xf>(v));
+    v = f(v, moved<0x114, 0xf>(v));
+    v = f(v, moved<0x118, 0xf>(v));
+    v = f(v, moved<0x142, 0xa>(v));     // lane 15 of the row before, into rows 1 and 3
+    return f(v, moved<0x143, 0xc>(v));  // lane 31, into rows 2 and 3
 }
+__device__ __forceinline__ uint64_t plus(uint64_t a, uint64_t b) { return a + b; }
 // sum over this and the lanes before it
-__device__ __forceinline__ uint64_t wave_upto(uint64_t v, int l) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint64_t y = __shfl_up(v, o);
-        if (l >= o) v += y;
-    }
-    return v;
-}
+__device__ __forceinline__ uint64_t wave_upto(uint64_t v) { return wave_scan(v, plus); }
 __device__ __forceinline__ uint64_t read_lane64(uint64_t v, int i) {
     const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)v, i), hi = __builtin_amdgcn_readlane((uint32_t)(v >> 32), i);
     return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ uint64_t wave_sum(uint64_t v) { return read_lane64(wave_upto(v), 63); }
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+    return __builtin_amdgcn_readlane(wave_scan(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; }), 63);
 }
 // Hand-over through LDS between the lanes of one wave.
 __device__ __forceinline__ void wave_sync() {
@@ -155,53 +164,89 @@ __device__ __forceinline__ void wave_sync() {
 }
 __device__ __forceinline__ int below(uint64_t ballot, int l) { return __popcll(ballot & (((uint64_t)1 << l) - 1)); }
 
-// Entries in rank order before this lane's, among the first n lanes (which
-// hold entries in index order): their number and mass.
-__device__ __forceinline__ void rank_lanes(uint32_t key, uint64_t mass, int n, int l, int &rank, uint64_t &before) {
-    rank = 0;
-    before = 0;
-    for (int i = 0; i < n; ++i) {
-        const uint32_t k = __builtin_amdgcn_readlane(key, i);
-        const uint64_t m = read_lane64(mass, i);
-        if (k > key || (k == key && i < l)) {
-            ++rank;
-            before += m;
+// Lists of up to 64 E entries in index order: lane l holds entries E l + e.
+// Entries in rank order before each of this lane's: their number and mass.
+template <int E>
+__device__ __forceinline__ void rank_lanes(const uint32_t (&key)[E], const uint64_t (&mass)[E], int n, int l, int (&rank)[E],
+                                           uint64_t (&before)[E]) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) rank[e] = 0, before[e] = 0;
+    for (int i = 0; i < n; i += E) {
+#pragma unroll
+        for (int f = 0; f < E; ++f) {
+            const uint32_t k = __builtin_amdgcn_readlane(key[f], i / E);
+            const uint64_t m = read_lane64(mass[f], i / E);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (k > key[e] || (k == key[e] && i + f < E * l + e)) {
+                    ++rank[e];
+                    before[e] += m;
+                }
         }
     }
 }
 
-// Draws from the entries that the first n lanes hold in index order (all
-// others of the row rank behind them and are not kept).
-__device__ __forceinline__ void draw_lanes(const SampleArgs &a, int64_t b, const Row &r, const Weigh &wt, uint32_t key,
-                                           int64_t j, int n, int l) {
-    const double w = key ? wt.weight(key) : 0.;
-    uint64_t mass = wt.mass_of(w);
-    bool keep = key != 0;
+// Draws from the n entries of a list (all others of the row rank behind them
+// and are not kept).
+template <int E>
+__device__ __forceinline__ void draw_lanes(const SampleArgs &a, int64_t b, const Row &r, const Weigh &wt,
+                                           const uint32_t (&key)[E], const int32_t (&j)[E], int n, int l) {
+    double w[E];
+    uint64_t mass[E];
+    bool keep[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        w[e] = key[e] ? wt.weight(key[e]) : 0.;
+        mass[e] = wt.mass_of(w[e]);
+        keep[e] = key[e] != 0;
+    }
     if (r.k < n || r.p < 1.) {
-        int rank;
-        uint64_t before;
-        rank_lanes(key, mass, n, l, rank, before);
-        keep = keep && rank < r.k;
+        int rank[E];
+        uint64_t before[E], sum = 0;
+        rank_lanes<E>(key, mass, n, l, rank, before);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            keep[e] = keep[e] && rank[e] < r.k;
+            if (keep[e]) sum += mass[e];
+        }
         if (r.p < 1.) {
-            const double goal = r.p * (double)wave_sum(keep ? mass : 0);
-            keep = keep && (rank == 0 || (double)before < goal);
+            const double goal = r.p * (double)wave_sum(sum);
+#pragma unroll
+            for (int e = 0; e < E; ++e) keep[e] = keep[e] && (rank[e] == 0 || (double)before[e] < goal);
         }
     }
-    keep = keep && w >= r.least;
-    if (!keep) mass = 0;
-    const int kept = __popcll(__ballot(keep));
-    const uint64_t upto = wave_upto(mass, l), total = read_lane64(upto, 63);
+    int kept = 0;
+    uint64_t mine = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        keep[e] = keep[e] && w[e] >= r.least;
+        if (!keep[e]) mass[e] = 0;
+        kept += __popcll(__ballot(keep[e]));
+        mine += mass[e];
+    }
+    const uint64_t upto = wave_upto(mine), total = read_lane64(upto, 63);
     const double goal = goal_of(a.u[b], total);
-    const uint64_t has = __ballot(mass != 0), past = __ballot(mass != 0 && (double)upto > goal);
+    const uint64_t has = __ballot(mine != 0), past = __ballot(mine != 0 && (double)upto > goal);
     const int at = past ? __ffsll((unsigned long long)past) - 1 : 63 - __clzll(has);
-    if (l == at) put(a, b, j, mass, total, kept);
+    if (l != at) return;
+    uint64_t sum = upto - mine, hw = 0;
+    int hit = -1;
+    bool done = false;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (!done && mass[e]) {
+            sum += mass[e];
+            hit = j[e], hw = mass[e];
+            done = (double)sum > goal;
+        }
+    put(a, b, hit, hw, total, kept);
 }
 
 // A wave a row.  Lane l holds the entries 64 V q + V l + c, q < Q, c < V.
 template <typename T, int V, int Q>
 __global__ void __launch_bounds__(256) sample_wave_kernel(SampleArgs a) {
     __shared__ double table[TABLE];
-    __shared__ uint2 list_of[4][64];
+    __shared__ uint2 list_of[4][128];
     const int t = threadIdx.x, l = t & 63, wv = __builtin_amdgcn_readfirstlane(t >> 6);
     fill_table(table, t);
     __syncthreads();
@@ -226,7 +271,8 @@ __global__ void __launch_bounds__(256) sample_wave_kernel(SampleArgs a) {
     const Row r(a, b);
     const Weigh wt{(double)value_of(top), r.c, a.shift, table};
     if constexpr (V == 1 && Q == 1) {
-        draw_lanes(a, b, r, wt, key[0][0], l, (int)M, l);
+        const int32_t j[1] = {l};
+        draw_lanes<1>(a, b, r, wt, key[0], j, (int)M, l);
         return;
     }
     auto count_from = [&](uint32_t c0) {
@@ -237,7 +283,7 @@ __global__ void __launch_bounds__(256) sample_wave_kernel(SampleArgs a) {
             for (int c = 0; c < V; ++c) n += __popcll(__ballot(key[q][c] >= c0));
         return n;
     };
-    // entries of [lo, hi] into the list, in index order; at most 64 of them
+    // entries of [lo, hi] into the list, in index order; at most 128 of them
     auto gather = [&](uint32_t lo, uint32_t hi) {
         int n = 0;
         wave_sync();
@@ -275,22 +321,41 @@ __global__ void __launch_bounds__(256) sample_wave_kernel(SampleArgs a) {
     if (n <= 64) {
         gather(cut, top);
         const uint2 e = l < n ? list[l] : make_uint2(0, 0);
-        draw_lanes(a, b, r, wt, e.x, e.y, n, l);
+        const uint32_t k[1] = {e.x};
+        const int32_t j[1] = {(int32_t)e.y};
+        draw_lanes<1>(a, b, r, wt, k, j, n, l);
         return;
     }
-    // more than 64 entries: of those equal to cut the first `ties` by index
+    if (n <= 128) {
+        gather(cut, top);
+        uint32_t k[2];
+        int32_t j[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint2 x = 2 * l + e < n ? list[2 * l + e] : make_uint2(0, 0);
+            k[e] = x.x, j[e] = (int32_t)x.y;
+        }
+        draw_lanes<2>(a, b, r, wt, k, j, n, l);
+        return;
+    }
+    // more than 128 entries: of those equal to cut the first `ties` by index
     int ties = n;
+    uint64_t mass[Q][V];
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int c = 0; c < V; ++c) {
+            const double w = key[q][c] >= cut && key[q][c] ? wt.weight(key[q][c]) : 0.;
+            mass[q][c] = wt.mass_of(w);
+        }
     if (n > r.k) ties = (int)r.k - (cut == top ? 0 : count_from(cut + 1));
     if (r.p < 1.) {
-        uint64_t mass[Q][V];
         uint64_t all = 0;
 #pragma unroll
         for (int q = 0; q < Q; ++q)
 #pragma unroll
-            for (int c = 0; c < V; ++c) {
-                mass[q][c] = wt.mass(key[q][c]);
+            for (int c = 0; c < V; ++c)
                 if (key[q][c] > cut) all += mass[q][c];
-            }
         const uint64_t one = wt.mass(cut), above_cut = wave_sum(all);
         const int equal = n - (cut == top ? 0 : count_from(cut + 1));
         if (ties > equal) ties = equal;     // (a cut of 1 that no entry has)
@@ -300,7 +365,7 @@ __global__ void __launch_bounds__(256) sample_wave_kernel(SampleArgs a) {
         uint64_t above = 0;
         int over = 0;                       // entries over hi
         int in = n;                         // entries of [lo, hi]
-        while (lo < hi && in > 64) {
+        while (lo < hi && in > 24) {
             const uint32_t mid = lo + (hi - lo) / 2 + 1;
             uint64_t s = 0;
 #pragma unroll
@@ -327,10 +392,12 @@ __global__ void __launch_bounds__(256) sample_wave_kernel(SampleArgs a) {
         if (in <= 64) {
             gather(lo, hi);
             const uint2 e = l < in ? list[l] : make_uint2(0, 0);
-            int rank;
-            uint64_t before;
-            rank_lanes(e.x, wt.mass(e.x), in, l, rank, before);
-            bool keep = e.x != 0 && ((rank == 0 && over == 0) || (double)(above + before) < goal);
+            int rank[1];
+            uint64_t before[1];
+            const uint32_t k[1] = {e.x};
+            const uint64_t m[1] = {wt.mass(e.x)};
+            rank_lanes<1>(k, m, in, l, rank, before);
+            bool keep = e.x != 0 && ((rank[0] == 0 && over == 0) || (double)(above + before[0]) < goal);
             if (e.x == cut) {               // top_k's ties
                 const uint64_t same = __ballot(keep && e.x == cut);
                 keep = keep && below(same, l) < ties;
@@ -353,6 +420,17 @@ __global__ void __launch_bounds__(256) sample_wave_kernel(SampleArgs a) {
             cut = lo;
         }
     }
+    // min_p: the smallest key that weighs enough (weights do not fall as keys rise)
+    uint32_t floor = 1;
+    if (r.least > 0.) {
+        uint32_t light = 0;
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+#pragma unroll
+            for (int c = 0; c < V; ++c)
+                if (key[q][c] >= cut && key[q][c] > light && wt.weight(key[q][c]) < r.least) light = key[q][c];
+        floor = wave_max(light) + 1;
+    }
     // the kept entries, block by block of 64 V: masses, and where the sum passes
     uint64_t part[Q];
     int kept = 0, seen = 0;
@@ -369,8 +447,7 @@ __global__ void __launch_bounds__(256) sample_wave_kernel(SampleArgs a) {
             const uint32_t x = key[q][c];
             if (!x || x < cut) continue;
             if (x == cut && at++ >= ties) continue;
-            const double w = wt.weight(x);
-            if (w >= r.least) use(c, wt.mass_of(w));
+            if (x >= floor) use(c, mass[q][c]);
         }
     };
     uint64_t total = 0;
@@ -394,7 +471,7 @@ __global__ void __launch_bounds__(256) sample_wave_kernel(SampleArgs a) {
             int tie = seen;
             uint64_t mine = 0;
             each(q, tie, [&](int, uint64_t w) { mine += w; });
-            const uint64_t upto = wave_upto(mine, l);
+            const uint64_t upto = wave_upto(mine);
             const uint64_t has = __ballot(mine != 0), past = __ballot(mine != 0 && (double)(base + upto) > goal);
             const int at = past ? __ffsll((unsigned long long)past) - 1 : 63 - __clzll(has);
             uint64_t sum = base + upto - mine, hw = 0;
@@ -423,6 +500,7 @@ __global__ void __launch_bounds__(256) sample_wave_kernel(SampleArgs a) {
 template <typename T, int P>
 __global__ void __launch_bounds__(64) sample_thread_kernel(SampleArgs a) {
     __shared__ double table[TABLE];
+    __shared__ uint64_t sorted[P][64];
     fill_table(table, threadIdx.x);
     __syncthreads();
     const int64_t b = (int64_t)blockIdx.x * 64 + threadIdx.x;
@@ -449,32 +527,47 @@ __global__ void __launch_bounds__(64) sample_thread_kernel(SampleArgs a) {
         mass[j] = wt.mass_of(w);
         if (w < r.least) light |= 1u << j;
     }
-    uint32_t keep = 0;
-    uint64_t all = 0;
+    uint32_t keep = ~0u;
+    if (r.k < M || r.p < 1.) {
+        // ranks by comparing every pair once; entries that cannot be drawn come last
+        int rank[P];
 #pragma unroll
-    for (int j = 0; j < P; ++j) {
-        int rank = 0;
-        if (r.k < M) {
+        for (int j = 0; j < P; ++j) rank[j] = P - 1 - j;
 #pragma unroll
-            for (int i = 0; i < P; ++i) rank += i < j ? key[i] >= key[j] : (i > j ? key[i] > key[j] : 0);
-        }
-        if (key[j] && rank < r.k) keep |= 1u << j, all += mass[j];
-    }
-    if (r.p < 1.) {
-        const double goal = r.p * (double)all;
-        uint32_t in = 0;
+        for (int j = 1; j < P; ++j)
 #pragma unroll
-        for (int j = 0; j < P; ++j) {
-            uint64_t before = 0;
-            bool first = true;
-#pragma unroll
-            for (int i = 0; i < P; ++i) {
-                if (i == j) continue;
-                if (i < j ? key[i] >= key[j] : key[i] > key[j]) before += mass[i], first = false;
+            for (int i = 0; i < j; ++i) {
+                const bool c = key[i] >= key[j];
+                rank[j] += c;
+                rank[i] -= c;
             }
-            if (first || (double)before < goal) in |= 1u << j;
+        // masses in rank order, a column of LDS a thread
+#pragma unroll
+        for (int j = 0; j < P; ++j) sorted[rank[j]][threadIdx.x] = mass[j];
+        const int most = r.k < P ? (int)r.k : P;
+        int end = most;
+        if (r.p < 1.) {
+            uint64_t all = 0, m = 0;
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+                if (i < most) all += sorted[i][threadIdx.x];
+            const double goal = r.p * (double)all;
+            end = 1;
+#pragma unroll
+            for (int i = 0; i < P - 1; ++i) {
+                m += sorted[i][threadIdx.x];
+                if (i + 1 < most && (double)m < goal) end = i + 2;
+            }
         }
-        keep &= in;
+        keep = 0;
+#pragma unroll
+        for (int j = 0; j < P; ++j)
+            if (key[j] && rank[j] < end) keep |= 1u << j;
+    } else {
+#pragma unroll
+        for (int j = 0; j < P; ++j)
+            if (!key[j]) keep &= ~(1u << j);
+        if (P < 32) keep &= (1u << (P & 31)) - 1;
     }
     keep &= ~light;
     uint64_t total = 0;
@@ -497,7 +590,7 @@ __global__ void __launch_bounds__(64) sample_thread_kernel(SampleArgs a) {
 
 // ---------------------------------------------------- work-groups of 256 a row
 
-constexpr int NT = 256, Q = 8, CHUNK = NT * 4 * Q, BINS = 2048, CAP = 1024;
+constexpr int NT = 256, Q = 8, CHUNK = NT * 4 * Q, BINS = 2048, CAP = 1024, MORE = 256;
 
 struct Block {
     uint64_t tmp[NT / 64];
@@ -518,7 +611,7 @@ struct Block {
     // sum over the threads before this one; *all: over all of them
     __device__ __forceinline__ uint64_t before(uint64_t v, uint64_t *all) {
         const int w = threadIdx.x >> 6;
-        const uint64_t x = wave_upto(v, threadIdx.x & 63);
+        const uint64_t x = wave_upto(v);
         __syncthreads();
         if ((threadIdx.x & 63) == 63) tmp[w] = x;
         __syncthreads();
@@ -575,8 +668,7 @@ struct Hist {
 // Workspace of a row that several work-groups share.
 struct RowSpace {
     Hist hist;
-    Plan plan;
-    uint32_t tickets[2], listed, pad;
+    uint32_t listed, pad;
     uint64_t list[CAP];
     // then chunks x { mass u64, count u32, top u32, low u32, pad u32 }
 };
@@ -596,6 +688,7 @@ struct Shared {
     uint32_t n, flag;
     uint64_t found, total, base;
     uint64_t part[NT / 64][Q];
+    uint64_t more[MORE];        // masses of listed entries by chunk
 };
 
 template <typename T> struct Chunk {
@@ -894,7 +987,7 @@ __device__ __forceinline__ void draw_chunk(Shared &sh, const SampleArgs &a, int6
 #pragma unroll
     for (int q = 0; q < Q; ++q)
         if (q == at_q) sum = mine[q];
-    const uint64_t upto = wave_upto(sum, l);
+    const uint64_t upto = wave_upto(sum);
     const uint64_t has = __ballot(sum != 0), past = __ballot(sum != 0 && (double)(at_base + upto) > goal);
     const int lane = past ? __ffsll((unsigned long long)past) - 1 : 63 - __clzll(has);
     if (l != lane) return;
@@ -978,18 +1071,6 @@ __device__ __forceinline__ RowSpace *row_space(const SampleArgs &a, int64_t slot
 }
 __device__ __forceinline__ ChunkSpace *chunk_space(RowSpace *rs) { return reinterpret_cast<ChunkSpace *>(rs + 1); }
 
-// True in the last of a row's work-groups to come here; what the others wrote
-// before is visible to it.
-__device__ __forceinline__ bool last_here(Shared &sh, uint32_t *ticket, int chunks) {
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) sh.flag = atomicAdd(ticket, 1u) + 1 == (uint32_t)chunks;
-    __syncthreads();
-    const bool last = sh.flag;
-    if (last) __threadfence();
-    return last;
-}
-
 // Launch 1: each chunk's largest and smallest score; the row's space cleared.
 template <typename T>
 __global__ void __launch_bounds__(NT) sample_top_kernel(SampleArgs a) {
@@ -998,7 +1079,7 @@ __global__ void __launch_bounds__(NT) sample_top_kernel(SampleArgs a) {
     const int64_t slot = blockIdx.x / a.chunks, b = a.row0 + slot;
     RowSpace *const rs = row_space(a, slot);
     for (int i = chunk * NT + t; i < BINS; i += a.chunks * NT) rs->hist.count[i] = 0, rs->hist.mass[i] = 0;
-    if (chunk == 0 && t < 3) (t < 2 ? rs->tickets[t] : rs->listed) = 0;
+    if (chunk == 0 && t == 0) rs->listed = 0;
     Chunk<T> ch;
     ch.load(a, b, chunk);
     uint32_t top = 0, low = 0;
@@ -1017,45 +1098,43 @@ __device__ __forceinline__ void row_range(Shared &sh, const SampleArgs &a, const
     low = ~sh.block.most(low);
 }
 
-// Draws once the end of the run is known: every chunk's mass is in cs.
+// Draws once the end of the run is known: every chunk's mass is in cs, but for
+// the masses `more` of listed entries.
 template <typename T>
-__device__ __forceinline__ void draw_row(Shared &sh, const SampleArgs &a, int64_t b, ChunkSpace *cs, const Row &r,
-                                         const Weigh &wt, End end, uint64_t more_mass, uint64_t more_count) {
+__device__ __forceinline__ void draw_row(Shared &sh, const SampleArgs &a, int64_t b, const ChunkSpace *cs, const Row &r,
+                                         const Weigh &wt, End end, uint64_t more_count) {
     const int t = threadIdx.x;
-    (void)more_mass;
-    // chunk sums in index order
-    uint64_t n = 0;
-    for (int i = t; i < a.chunks; i += NT) n += cs[i].count;
-    const uint64_t kept = sh.block.sum(n) + more_count;
-    uint64_t total = 0;
-    for (int i0 = 0; i0 < a.chunks; i0 += NT) total += sh.block.sum(i0 + t < a.chunks ? cs[i0 + t].mass : 0);
+    auto mass_of = [&](int i) { return i < a.chunks ? cs[i].mass + (i < MORE ? sh.more[i] : 0) : 0; };
+    uint64_t n = 0, m = 0;
+    for (int i = t; i < a.chunks; i += NT) n += cs[i].count, m += mass_of(i);
+    const uint64_t kept = sh.block.sum(n) + more_count, total = sh.block.sum(m);
     const double goal = goal_of(a.u[b], total);
+    // the chunk in which the sum passes, in index order; the last with a mass where none does
     if (t == 0) sh.found = ~0ull, sh.n = 0;
     __syncthreads();
     uint64_t base = 0;
     for (int i0 = 0; i0 < a.chunks; i0 += NT) {
-        const int i = i0 + t;
-        const uint64_t m = i < a.chunks ? cs[i].mass : 0;
+        const uint64_t c = mass_of(i0 + t);
         uint64_t all;
-        const uint64_t before = base + sh.block.before(m, &all);
-        if (m) {
-            atomicMax(&sh.n, (uint32_t)i);
-            if ((double)(before + m) > goal) atomicMin((unsigned long long *)&sh.found, (unsigned long long)i);
+        const uint64_t before = base + sh.block.before(c, &all);
+        if (c) {
+            atomicMax(&sh.n, (uint32_t)(i0 + t));
+            if ((double)(before + c) > goal) atomicMin((unsigned long long *)&sh.found, (unsigned long long)(i0 + t));
         }
         base += all;
     }
     __syncthreads();
     const int at = sh.found == ~0ull ? (int)sh.n : (int)sh.found;
     base = 0;
-    for (int i = t; i < at; i += NT) base += cs[i].mass;
+    for (int i = t; i < at; i += NT) base += mass_of(i);
     base = sh.block.sum(base);
     Chunk<T> ch;
     ch.load(a, b, at);
     draw_chunk(sh, a, b, ch, r, wt, end, base, total, kept, goal);
 }
 
-// Launch 2: the histogram, read off by the row's last work-group; rows without
-// top_k and top_p are drawn from here.
+// Launch 2: the histogram of the row; for rows without top_k and top_p the
+// chunk's mass.
 template <typename T>
 __global__ void __launch_bounds__(NT) sample_bins_kernel(SampleArgs a) {
     __shared__ Shared sh;
@@ -1069,18 +1148,13 @@ __global__ void __launch_bounds__(NT) sample_bins_kernel(SampleArgs a) {
     ch.load(a, b, chunk);
     uint32_t top, low;
     row_range(sh, a, cs, top, low);
-    if (!top) {
-        if (chunk == 0 && t == 0) put(a, b, -1, 0, 0, 0);
-        return;
-    }
+    if (!top) return;
     const Row r(a, b);
     const Weigh wt{(double)value_of(top), r.c, a.shift, sh.table};
-    if (r.k >= a.M && r.p >= 1.) {
+    if (r.keeps_all(a.M)) {
         uint64_t m, n;
         chunk_sums(sh, ch, r, wt, [](uint32_t, uint32_t) { return true; }, &m, &n);
         if (t == 0) cs[chunk].mass = m, cs[chunk].count = (uint32_t)n;
-        if (!last_here(sh, &rs->tickets[0], a.chunks)) return;
-        draw_row<T>(sh, a, b, cs, r, wt, End{1, 0xffffffffu}, 0, 0);
         return;
     }
     const Binning bins(value_of(top), value_of(low), r.temp);
@@ -1091,50 +1165,38 @@ __global__ void __launch_bounds__(NT) sample_bins_kernel(SampleArgs a) {
         atomicAdd(&rs->hist.count[i], sh.hist.count[i]);
         if (sh.hist.mass[i]) atomicAdd((unsigned long long *)&rs->hist.mass[i], (unsigned long long)sh.hist.mass[i]);
     }
-    if (!last_here(sh, &rs->tickets[0], a.chunks)) return;
-    for (int i = t; i < BINS; i += NT) sh.hist.count[i] = rs->hist.count[i], sh.hist.mass[i] = rs->hist.mass[i];
+}
+
+// What launches 3 and 4 begin with: the plan, read off the row's histogram by
+// each work-group for itself.
+__device__ __forceinline__ void row_plan(Shared &sh, const RowSpace *rs, const Row &r, int64_t M) {
+    for (int i = threadIdx.x; i < BINS; i += NT) sh.hist.count[i] = rs->hist.count[i], sh.hist.mass[i] = rs->hist.mass[i];
     __syncthreads();
-    make_plan(sh, r, a.M);
-    if (t == 0) rs->plan = sh.plan;
+    make_plan(sh, r, M);
 }
 
 // Launch 3: entries of the bins in question listed, the mass of those before
-// them summed; the row's last work-group ranks and draws.
+// them summed.
 template <typename T>
-__global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
+__global__ void __launch_bounds__(NT) sample_list_kernel(SampleArgs a) {
     __shared__ Shared sh;
     const int t = threadIdx.x, chunk = blockIdx.x % a.chunks;
     const int64_t slot = blockIdx.x / a.chunks, b = a.row0 + slot;
     RowSpace *const rs = row_space(a, slot);
     ChunkSpace *const cs = chunk_space(rs);
     const Row r(a, b);
-    if (r.k >= a.M && r.p >= 1.) return;
+    if (r.keeps_all(a.M)) return;
     fill_table(sh.table, t);
     Chunk<T> ch;
     ch.load(a, b, chunk);
     uint32_t top, low;
     row_range(sh, a, cs, top, low);
     if (!top) return;
+    row_plan(sh, rs, r, a.M);
+    const Plan p = sh.plan;
+    if (p.listed > CAP) return;
     const Weigh wt{(double)value_of(top), r.c, a.shift, sh.table};
     const Binning bins(value_of(top), value_of(low), r.temp);
-    if (t == 0) sh.plan = rs->plan;
-    __syncthreads();
-    const Plan p = sh.plan;
-    if (p.listed > CAP) {
-        // one work-group goes over the row
-        if (!last_here(sh, &rs->tickets[1], a.chunks)) return;
-        end_by_passes<T>(sh, a, b, r, wt, top);
-        const End end = sh.end;
-        for (int i = 0; i < a.chunks; ++i) {
-            ch.load(a, b, i);
-            uint64_t m, n;
-            chunk_sums(sh, ch, r, wt, [&](uint32_t x, uint32_t j) { return end.has(x, j); }, &m, &n);
-            if (t == 0) cs[i].mass = m, cs[i].count = (uint32_t)n;
-        }
-        __syncthreads();
-        draw_row<T>(sh, a, b, cs, r, wt, end, 0, 0);
-        return;
-    }
     ch.each([&](uint32_t x, int q, int c) {
         if (p.asks(bins.bin(x))) rs->list[atomicAdd(&rs->listed, 1u)] = (uint64_t)~x << 32 | ch.at(q, c);
     });
@@ -1142,27 +1204,71 @@ __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
     const int sure = p.sure();
     chunk_sums(sh, ch, r, wt, [&](uint32_t x, uint32_t) { return bins.bin(x) < sure; }, &m, &n);
     if (t == 0) cs[chunk].mass = m, cs[chunk].count = (uint32_t)n;
-    if (!last_here(sh, &rs->tickets[1], a.chunks)) return;
-    for (int i = t; i < (int)p.listed; i += NT) sh.list[i] = rs->list[i];
-    __syncthreads();
-    uint64_t count = 0;
+}
+
+// Launch 4, a work-group a row: the listed entries ranked, and the draw.
+template <typename T>
+__global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
+    __shared__ Shared sh;
+    const int t = threadIdx.x;
+    const int64_t slot = blockIdx.x, b = a.row0 + slot;
+    RowSpace *const rs = row_space(a, slot);
+    ChunkSpace *const cs = chunk_space(rs);
+    fill_table(sh.table, t);
+    for (int i = t; i < MORE; i += NT) sh.more[i] = 0;
+    uint32_t top, low;
+    row_range(sh, a, cs, top, low);
+    if (!top) {
+        if (t == 0) put(a, b, -1, 0, 0, 0);
+        return;
+    }
+    const Row r(a, b);
+    const Weigh wt{(double)value_of(top), r.c, a.shift, sh.table};
     End end{1, 0xffffffffu};
-    if (p.listed) {
+    if (r.keeps_all(a.M)) {
+        draw_row<T>(sh, a, b, cs, r, wt, end, 0);
+        return;
+    }
+    row_plan(sh, rs, r, a.M);
+    const Plan p = sh.plan;
+    uint64_t count = 0;
+    // (chunks past MORE: listed entries' masses would have no place)
+    if (p.listed > CAP || (p.listed && a.chunks > MORE)) {
+        if (p.listed > CAP) {
+            end_by_passes<T>(sh, a, b, r, wt, top);
+        } else {
+            for (int i = t; i < (int)p.listed; i += NT) sh.list[i] = rs->list[i];
+            __syncthreads();
+            rank_list(sh, r, wt, Binning(value_of(top), value_of(low), r.temp), (int)p.listed);
+        }
+        end = sh.end;
+        Chunk<T> ch;
+        for (int i = 0; i < a.chunks; ++i) {
+            ch.load(a, b, i);
+            uint64_t m, n;
+            chunk_sums(sh, ch, r, wt, [&](uint32_t x, uint32_t j) { return end.has(x, j); }, &m, &n);
+            if (t == 0) cs[i].mass = m, cs[i].count = (uint32_t)n;
+        }
+        __threadfence_block();
+        __syncthreads();
+    } else if (p.listed) {
+        const Binning bins(value_of(top), value_of(low), r.temp);
+        for (int i = t; i < (int)p.listed; i += NT) sh.list[i] = rs->list[i];
+        __syncthreads();
         rank_list(sh, r, wt, bins, (int)p.listed);
         end = sh.end;
+        const int sure = p.sure();
         for (int i = t; i < (int)sh.n; i += NT) {
             const uint32_t x = ~(uint32_t)(sh.list[i] >> 32), j = (uint32_t)sh.list[i];
             if (bins.bin(x) < sure) continue;
             const double w = wt.weight(x);
             if (w < r.least) continue;
             ++count;
-            atomicAdd((unsigned long long *)&cs[j / CHUNK].mass, (unsigned long long)wt.mass_of(w));
+            atomicAdd((unsigned long long *)&sh.more[j / CHUNK], (unsigned long long)wt.mass_of(w));
         }
         count = sh.block.sum(count);
-        __threadfence();
-        __syncthreads();
     }
-    draw_row<T>(sh, a, b, cs, r, wt, end, 0, count);
+    draw_row<T>(sh, a, b, cs, r, wt, end, count);
 }
 
 constexpr int64_t SLAB = 2048;      // rows of a large table in flight: their space is reused
@@ -1205,7 +1311,8 @@ template <typename T> hipError_t launch_typed(SampleArgs a, void *ws, hipStream_
         const dim3 grid((unsigned)(rows * a.chunks));
         sample_top_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
         sample_bins_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
-        if (!all) sample_draw_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
+        if (!all) sample_list_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
+        sample_draw_kernel<T><<<dim3((unsigned)rows), dim3(NT), 0, s>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
