@@ -61,14 +61,17 @@ template <> struct Op<float> {
     }
 };
 
-// A tile in LDS: rows of DP values, in 16-byte chunks.  Chunk c of row r lies
-// at position c ^ swizzle(r): eight consecutive rows put the same chunk on
-// eight different positions (row_frag reads one chunk of 32 rows), and four
-// consecutive rows put a pair of chunks on four different pairs (the transpose
-// reads of col_frag take 32 bytes of four rows).
-__device__ __forceinline__ int swizzle(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+// A tile in LDS: rows of DP values in 16-byte chunks, chunk c of row r at
+// position c ^ swizzle(r).  256 bytes of LDS (64 banks) are one row or several:
+// 16 consecutive rows put the same chunk on 16 different places of those
+// (row_frag reads one chunk of 32 rows), and four consecutive rows put four
+// consecutive chunks on 16 different ones (what 32 lanes of col_frag's
+// transpose reads take).
 template <typename T, int DP> __device__ __forceinline__ int place(int r, int c) {
-    return (r * (DP / Op<T>::PER) + (c ^ swizzle(r))) * 16;
+    constexpr int CPR = DP / Op<T>::PER;
+    static_assert(CPR == 8 || CPR == 16 || CPR == 32, "rows of 128, 256 or 512 bytes");
+    const int s = CPR == 8 ? ((r >> 1) & 1) << 2 | ((r >> 2) & 3) : (r & 3) << 2 | ((r >> 2) & 3);
+    return (r * CPR + (c ^ s)) * 16;
 }
 
 // Operand whose rows are the tile's rows row0 + 0..31, step s of the
@@ -128,8 +131,10 @@ template <typename T> __device__ __forceinline__ void store4(T *row, int d, int 
         } else {
             u2v p;
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-                p[e] = (uint32_t)f32_to_bf16(v[2 * e]) | (uint32_t)f32_to_bf16(v[2 * e + 1]) << 16;
+            for (int e = 0; e < 2; ++e) {
+                const __bf16 two[2] = {(__bf16)v[2 * e], (__bf16)v[2 * e + 1]};
+                p[e] = *reinterpret_cast<const uint32_t *>(two);
+            }
             *reinterpret_cast<u2v *>(row + d) = p;
         }
     } else {
@@ -157,6 +162,56 @@ __device__ __forceinline__ void load_frags(typename Op<T>::V (&f)[DP / (2 * Op<T
         f[s] = *reinterpret_cast<const typename Op<T>::V *>(&v);
     }
 }
+
+// The part of a tile that a thread carries from memory to LDS: rows r of T
+// values at base + r * stride; rows whose bit of `live` is off, and values at
+// and past dh, are zeros.  VEC: 16-byte pieces, read through a buffer
+// descriptor that returns zeros for the offset of a row that is off (base + BN
+// rows within 2^31 bytes).
+template <typename T, int DP, int BN, int NT, bool VEC> struct TileLoad {
+    static constexpr int PER = Op<T>::PER, CPR = DP / PER, N = BN * CPR / NT, RPI = NT / CPR;
+    static_assert(BN * CPR % NT == 0 && NT % CPR == 0, "whole chunks per thread");
+    u4v v[N];
+    __device__ __forceinline__ void fetch(const T *base, int64_t stride, uint64_t live, int dh, int t) {
+        const int c = t % CPR, r0 = t / CPR;
+        if constexpr (VEC) {
+            const uint32_t row = (uint32_t)stride * (uint32_t)sizeof(T);
+            const __amdgpu_buffer_rsrc_t rs =
+                __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(base), (short)0, 0x7fffffff, 0x00020000);
+            const uint32_t at = (uint32_t)r0 * row + 16 * c;
+            const uint64_t mine = c * PER < dh ? live >> r0 : 0;
+#pragma unroll
+            for (int q = 0; q < N; ++q)
+                v[q] = __builtin_amdgcn_raw_buffer_load_b128(
+                    rs, (int)((mine >> (q * RPI)) & 1 ? at + (uint32_t)(q * RPI) * row : 0x80000000u), 0, 0);
+        } else {
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                v[q] = u4v{0, 0, 0, 0};
+                if ((live >> (r0 + q * RPI)) & 1) v[q] = load_chunk<T>(base + (r0 + q * RPI) * stride, PER * c, dh, false);
+            }
+        }
+    }
+    __device__ __forceinline__ void stash(char *tile, int t) const {
+#pragma unroll
+        for (int q = 0; q < N; ++q) *reinterpret_cast<u4v *>(tile + place<T, DP>(t / CPR + q * RPI, t % CPR)) = v[q];
+    }
+};
+
+// A row's position and head: packed row m = position G + head within the group.
+struct RowOf {
+    int i, h;
+    __device__ __forceinline__ RowOf(int m, int hk, int G) : i(m / G), h(hk * G + m % G) {}
+};
+
+// Bit n: key j0 + n takes part (n < BN).
+template <int BN> __device__ __forceinline__ uint64_t live_keys(const uint8_t *mask, int j0, int kend, int l) {
+    const int j = j0 + l;
+    bool on = l < BN && j < kend;
+    if (on && mask) on = mask[j] != 0;
+    return __ballot(on);
+}
+template <int BN> constexpr uint64_t ALL_LIVE = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
 
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
 

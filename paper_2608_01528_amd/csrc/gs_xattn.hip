@@ -11,47 +11,16 @@ namespace gs {
 namespace {
 using namespace attn;
 
-// A row's position and head: packed row m = position G + head within the group.
-struct RowOf {
-    int i, h;
-    __device__ __forceinline__ RowOf(int m, int hk, int G) : i(m / G), h(hk * G + m % G) {}
-};
+// Waves a SIMD that registers are kept for: fp32 fragments take twice the
+// registers of bf16 ones, and those with 128 values, or of a single wave (which
+// carries whole tiles), would spill at two.
+template <typename T, int DP, int NW> constexpr int min_waves() { return sizeof(T) == 4 && (DP == 128 || NW == 1) ? 1 : 2; }
 
-template <typename T, int DP, int BN, int NT> struct TileLoad {
-    static constexpr int PER = Op<T>::PER, CPR = DP / PER, N = BN * CPR / NT;
-    static_assert(BN * CPR % NT == 0, "whole chunks per thread");
-    u4v v[N];
-    __device__ __forceinline__ void fetch(const T *base, int64_t stride, int j0, uint64_t live, int dh, bool vec, int t) {
-#pragma unroll
-        for (int q = 0; q < N; ++q) {
-            const int c = t + q * NT, r = c / CPR;
-            v[q] = u4v{0, 0, 0, 0};
-            if ((live >> r) & 1) v[q] = load_chunk<T>(base + (int64_t)(j0 + r) * stride, PER * (c % CPR), dh, vec);
-        }
-    }
-    __device__ __forceinline__ void stash(char *tile, int t) const {
-#pragma unroll
-        for (int q = 0; q < N; ++q) {
-            const int c = t + q * NT;
-            *reinterpret_cast<u4v *>(tile + place<T, DP>(c / CPR, c % CPR)) = v[q];
-        }
-    }
-};
-
-// Bit n: key j0 + n takes part (n < BN).
-template <int BN>
-__device__ __forceinline__ uint64_t live_keys(const uint8_t *mask, int j0, int kend, int l) {
-    const int j = j0 + l;
-    bool on = l < BN && j < kend;
-    if (on && mask) on = mask[j] != 0;
-    return __ballot(on);
-}
-
-template <typename T, int DP, int NW, int BN>
-__global__ void __launch_bounds__(64 * NW) xattn_kernel(CrossAttnArgs a) {
+template <typename T, int DP, int NW, int BN, bool VEC>
+__global__ void __launch_bounds__(64 * NW, (min_waves<T, DP, NW>())) xattn_kernel(CrossAttnArgs a) {
     constexpr int PER = Op<T>::PER, NS = DP / (2 * PER), NJ = DP / 32, NT = 64 * NW;
-    __shared__ __attribute__((aligned(16))) char lds[2 * BN * DP * sizeof(T)];
-    char *const kt = lds, *const vt = lds + BN * DP * sizeof(T);
+    constexpr int TILE = BN * DP * sizeof(T);
+    __shared__ __attribute__((aligned(16))) char lds[4 * TILE];     // two of K, two of V
     const int t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
     const int64_t L = logical_group(a.groups);
     if (L >= a.groups) return;
@@ -74,7 +43,7 @@ __global__ void __launch_bounds__(64 * NW) xattn_kernel(CrossAttnArgs a) {
     if ((rt * 32 * NW) / a.G >= ql) kend = 0;           // no row of the tile is there
 
     typename Op<T>::V q[NS];
-    load_frags<T, DP>(q, on ? static_cast<const T *>(a.Q) + b * a.q.b + row.i * a.q.l + row.h * a.q.h : nullptr, a.Dh, a.vec, l);
+    load_frags<T, DP>(q, on ? static_cast<const T *>(a.Q) + b * a.q.b + row.i * a.q.l + row.h * a.q.h : nullptr, a.Dh, VEC, l);
     // scores in units of log 2; a negative scale turns the queries round, so
     // that the largest product is the largest score
     const float c = fabsf(a.scale) * LOG2E;
@@ -91,24 +60,26 @@ __global__ void __launch_bounds__(64 * NW) xattn_kernel(CrossAttnArgs a) {
     for (int j = 0; j < NJ; ++j) o[j] = f16v{0};
     float mx = -INFINITY, sum = 0.f;
 
-    TileLoad<T, DP, BN, NT> kr, vr;
-    uint64_t live = 0;
+    TileLoad<T, DP, BN, NT, VEC> kr, vr;
+    uint64_t live = 0, next_live = 0;
+    auto fetch = [&](int j, uint64_t on) {
+        kr.fetch(K + (int64_t)j * a.k.l, a.k.l, on, a.Dh, t);
+        vr.fetch(V + (int64_t)j * a.v.l, a.v.l, on, a.Dh, t);
+    };
+    char *kt = lds, *vt = lds + TILE;       // the tile in use; the next goes 2 TILE on, or back
+    int other = 2 * TILE;
     if (j0 < kend) {
         live = live_keys<BN>(mask, j0, kend, l);
-        kr.fetch(K, a.k.l, j0, live, a.Dh, a.vec, t);
-        vr.fetch(V, a.v.l, j0, live, a.Dh, a.vec, t);
-    }
-    for (; j0 < kend; j0 += BN) {
-        __syncthreads();
+        fetch(j0, live);
         kr.stash(kt, t);
         vr.stash(vt, t);
-        __syncthreads();
-        const uint64_t now = live;
         if (j0 + BN < kend) {
-            live = live_keys<BN>(mask, j0 + BN, kend, l);
-            kr.fetch(K, a.k.l, j0 + BN, live, a.Dh, a.vec, t);
-            vr.fetch(V, a.v.l, j0 + BN, live, a.Dh, a.vec, t);
+            next_live = live_keys<BN>(mask, j0 + BN, kend, l);
+            fetch(j0 + BN, next_live);
         }
+    }
+    for (; j0 < kend; j0 += BN) {
+        lds_barrier();
         f16v p[BN / 32];
 #pragma unroll
         for (int n = 0; n < BN / 32; ++n) {
@@ -116,10 +87,10 @@ __global__ void __launch_bounds__(64 * NW) xattn_kernel(CrossAttnArgs a) {
 #pragma unroll
             for (int s = 0; s < NS; ++s) p[n] = Op<T>::mma(row_frag<T, DP>(kt, 32 * n, s, l), q[s], p[n]);
         }
-        if (now != (BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1)) {
+        if (live != ALL_LIVE<BN>) {
 #pragma unroll
             for (int n = 0; n < BN / 32; ++n) {
-                const uint32_t bits = (uint32_t)(now >> (32 * n)) >> (4 * (l >> 5));
+                const uint32_t bits = (uint32_t)(live >> (32 * n)) >> (4 * (l >> 5));
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (!((bits >> (8 * (r / 4) + r % 4)) & 1)) p[n][r] = -INFINITY;
@@ -131,10 +102,18 @@ __global__ void __launch_bounds__(64 * NW) xattn_kernel(CrossAttnArgs a) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, p[n][r]);
         top = fmaxf(top, other_half(top)) * c;          // -inf * 0 is NaN: c is not 0 (see the entry point)
-        const float next = fmaxf(mx, top);
-        const float ref = next == -INFINITY ? 0.f : next;
-        const float turn = __builtin_amdgcn_exp2f(mx - ref);
-        mx = next;
+        // The reference that exponents are taken from follows the maximum only
+        // when that has risen by 2^8: sums and probabilities up to 2^8 times
+        // larger cost no precision, and the weighted sum is rarely rescaled.
+        if (__any(top > mx + 8.f)) {
+            const float next = fmaxf(mx, top);
+            const float turn = __builtin_amdgcn_exp2f(mx - (next == -INFINITY ? 0.f : next));
+            mx = next;
+            sum *= turn;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) o[j] *= turn;
+        }
+        const float ref = mx == -INFINITY ? 0.f : mx;
         float part = 0.f;
 #pragma unroll
         for (int n = 0; n < BN / 32; ++n)
@@ -143,9 +122,7 @@ __global__ void __launch_bounds__(64 * NW) xattn_kernel(CrossAttnArgs a) {
                 p[n][r] = __builtin_amdgcn_exp2f(fmaf(p[n][r], c, -ref));
                 part += p[n][r];
             }
-        sum = fmaf(sum, turn, part);
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) o[j] *= turn;
+        sum += part;
 #pragma unroll
         for (int n = 0; n < BN / 32; ++n)
 #pragma unroll
@@ -154,6 +131,18 @@ __global__ void __launch_bounds__(64 * NW) xattn_kernel(CrossAttnArgs a) {
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) o[j] = Op<T>::mma(col_frag<T, DP>(vt, 32 * n, s, j, l), pf, o[j]);
             }
+        kt += other;
+        vt += other;
+        other = -other;
+        live = next_live;
+        if (j0 + BN < kend) {
+            kr.stash(kt, t);
+            vr.stash(vt, t);
+            if (j0 + 2 * BN < kend) {
+                next_live = live_keys<BN>(mask, j0 + 2 * BN, kend, l);
+                fetch(j0 + 2 * BN, next_live);
+            }
+        }
     }
     sum += other_half(sum);
     if (!in) return;
@@ -182,46 +171,48 @@ __global__ void __launch_bounds__(64 * NW) xattn_kernel(CrossAttnArgs a) {
             f4v v;
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = on ? o[j][4 * g + e] * inv : 0.f;
-            store4<T>(out, 32 * j + 8 * g + 4 * (l >> 5), a.Dh, a.vec, v);
+            store4<T>(out, 32 * j + 8 * g + 4 * (l >> 5), a.Dh, VEC, v);
         }
     if (a.lse && l < 32) a.lse[((int64_t)b * a.Hq + row.h) * a.Lq + row.i] = lse;
 }
 
-// Joins the parts of a row: O = sum_s exp(lse_s - lse) O_s, one wave a row.
+// Joins the parts of a row: O = sum_s exp(lse_s - lse) O_s, DP / 4 lanes a row.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256) xattn_join_kernel(CrossAttnArgs a) {
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int l = threadIdx.x & 63;
+    constexpr int LANES = DP / 4;
+    const int64_t at = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const int d = 4 * (threadIdx.x % LANES);
     if (at >= (int64_t)a.B * a.Hkv * a.rows) return;
     const int bh = (int)(at / a.rows), m = (int)(at % a.rows);
     const int b = bh / a.Hkv;
     const RowOf row(m, bh % a.Hkv, a.G);
     const bool on = row.i < clamped(a.qlen, b, a.Lq);
     const float *const pl = a.part_lse + at * a.splits;
-    float top = -INFINITY;
-    for (int s = l; s < a.splits; s += 64) top = fmaxf(top, pl[s]);
-#pragma unroll
-    for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    const float *const po = a.part + at * a.splits * DP + d;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll 8
+    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, pl[s]);
     const float ref = top == -INFINITY ? 0.f : top;
-    constexpr int PL = DP / 64;
-    float sum = 0.f, o[PL] = {};
+    f4v o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
     for (int s = 0; s < a.splits; ++s) {
         const float e = __builtin_amdgcn_exp2f((pl[s] - ref) * LOG2E);
         sum += e;
-#pragma unroll
-        for (int k = 0; k < PL; ++k) o[k] = fmaf(e, a.part[(at * a.splits + s) * DP + l + 64 * k], o[k]);
+        o += e * *reinterpret_cast<const f4v *>(po + s * DP);
     }
     const float inv = on && sum != 0.f ? 1.f / sum : 0.f;
-    T *const out = static_cast<T *>(a.O) + b * a.o.b + row.i * a.o.l + row.h * a.o.h;
+    f4v v;
 #pragma unroll
-    for (int k = 0; k < PL; ++k)
-        if (l + 64 * k < a.Dh) st_f32<T>(out, l + 64 * k, on ? o[k] * inv : 0.f);
-    if (a.lse && l == 0)
+    for (int e = 0; e < 4; ++e) v[e] = on ? o[e] * inv : 0.f;
+    store4<T>(static_cast<T *>(a.O) + b * a.o.b + row.i * a.o.l + row.h * a.o.h, d, a.Dh, a.vec, v);
+    if (a.lse && d == 0)
         a.lse[((int64_t)b * a.Hq + row.h) * a.Lq + row.i] =
             on && sum != 0.f ? ref + __builtin_amdgcn_logf(sum) * LN2 : -INFINITY;
 }
 
-constexpr int tile_keys(gs_dtype t) { return t == GS_F32 ? 32 : 64; }
+// Keys a tile: 16 KB each of K and V at 128 values for work-groups of four
+// waves; half of that for single waves, of which more share a CU.
+constexpr int tile_keys(gs_dtype t, int waves) { return t == GS_F32 || waves == 1 ? 32 : 64; }
 
 // How the rows and keys are dealt out: waves of a work-group, parts of the keys.
 struct Plan {
@@ -233,10 +224,10 @@ Plan plan_for(gs_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t
     p.dp = Dh <= 64 ? 64 : 128;
     p.waves = rows <= 32 ? 1 : 4;
     p.row_tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
-    const int64_t groups = B * Hkv * p.row_tiles, tile = tile_keys(t);
-    const int64_t want = (p.waves == 1 ? 1024 : 512) / (groups > 0 ? groups : 1);
+    const int64_t groups = B * Hkv * p.row_tiles, tile = tile_keys(t, p.waves);
+    const int64_t want = (p.waves == 1 ? 2048 : 512) / (groups > 0 ? groups : 1);
     int64_t per = (Lk + (want > 1 ? want : 1) - 1) / (want > 1 ? want : 1);
-    if (per < 4 * tile) per = 4 * tile;
+    if (per < 128) per = 128;
     per = (per + tile - 1) / tile * tile;
     p.split_keys = (int)per;
     p.splits = (int)((Lk + per - 1) / per);
@@ -244,20 +235,21 @@ Plan plan_for(gs_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t
     return p;
 }
 
-template <typename T, int DP, int NW, int BN>
+template <typename T, int DP, int NW, int BN, bool VEC>
 hipError_t launch_rows(const CrossAttnArgs &a, hipStream_t s) {
-    xattn_kernel<T, DP, NW, BN><<<dim3((unsigned)((a.groups + 7) / 8 * 8)), dim3(64 * NW), 0, s>>>(a);
+    xattn_kernel<T, DP, NW, BN, VEC><<<dim3((unsigned)((a.groups + 7) / 8 * 8)), dim3(64 * NW), 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
-    const int64_t rows = (int64_t)a.B * a.Hkv * a.rows;
-    xattn_join_kernel<T, DP><<<dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s>>>(a);
+    const int64_t rows = (int64_t)a.B * a.Hkv * a.rows, per = 256 / (DP / 4);
+    xattn_join_kernel<T, DP><<<dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
 
-template <typename T, int BN>
+template <typename T, bool VEC>
 hipError_t launch_typed(const CrossAttnArgs &a, int dp, int waves, hipStream_t s) {
-    if (dp == 64) return waves == 1 ? launch_rows<T, 64, 1, BN>(a, s) : launch_rows<T, 64, 4, BN>(a, s);
-    return waves == 1 ? launch_rows<T, 128, 1, BN>(a, s) : launch_rows<T, 128, 4, BN>(a, s);
+    constexpr int BN = sizeof(T) == 4 ? 32 : 64;
+    if (dp == 64) return waves == 1 ? launch_rows<T, 64, 1, 32, VEC>(a, s) : launch_rows<T, 64, 4, BN, VEC>(a, s);
+    return waves == 1 ? launch_rows<T, 128, 1, 32, VEC>(a, s) : launch_rows<T, 128, 4, BN, VEC>(a, s);
 }
 
 }  // namespace
@@ -277,8 +269,10 @@ hipError_t launch_cross_attn(gs_dtype t, CrossAttnArgs a, void *ws, hipStream_t 
     a.groups = (int64_t)a.B * a.Hkv * p.row_tiles * p.splits;
     a.part = static_cast<float *>(ws);
     a.part_lse = a.part + (int64_t)a.B * a.Hkv * a.rows * p.splits * p.dp;
-    if (t == GS_F32) return launch_typed<float, 32>(a, p.dp, p.waves, s);
-    return launch_typed<bf16_t, 64>(a, p.dp, p.waves, s);
+    // tiles are read with 32-bit offsets: rows of a tile within 2^31 bytes
+    a.vec = a.vec && a.k.l < ATTN_VEC_STRIDE && a.v.l < ATTN_VEC_STRIDE;
+    if (t == GS_F32) return a.vec ? launch_typed<float, true>(a, p.dp, p.waves, s) : launch_typed<float, false>(a, p.dp, p.waves, s);
+    return a.vec ? launch_typed<bf16_t, true>(a, p.dp, p.waves, s) : launch_typed<bf16_t, false>(a, p.dp, p.waves, s);
 }
 
 }  // namespace gs

@@ -2,58 +2,70 @@
 // D_i = sum_d dO_id O_id:
 //   dV = P^T dO     dP = dO V^T     dS = P (dP - D)
 //   dQ = scale dS K                 dK = scale dS^T Q
-// Two passes form P again instead of storing it: one over the keys for each
-// block of query rows (dQ, and D on the way), one over the query rows for each
-// block of keys (dK and dV).  A joint pass would save two of the seven
+// A first pass forms D.  Two passes then form P again instead of storing it:
+// one over the keys for each block of query rows (dQ), one over the query rows
+// for each block of keys (dK and dV).  A joint pass would save two of the seven
 // products, but one of its gradients would have to be summed across
-// work-groups, in an order that changes from run to run; here every sum has a
-// fixed order.
+// work-groups in an order that changes from run to run; here every sum has a
+// fixed order.  Where there are few blocks, the range that a block runs over is
+// split into parts whose sums a last pass adds up.
 #include "gs_attn.h"
 
 namespace gs {
 namespace {
 using namespace attn;
 
-struct RowOf {
-    int i, h;
-    __device__ __forceinline__ RowOf(int m, int hk, int G) : i(m / G), h(hk * G + m % G) {}
-};
+// D: a row in DP / 8 lanes.
+template <typename T, int DP, bool VEC>
+__global__ void __launch_bounds__(256) xattn_rows_kernel(CrossAttnGradArgs a) {
+    constexpr int PER = Op<T>::PER, LANES = DP / PER;
+    const int64_t at = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    if (at >= (int64_t)a.B * a.Hq * a.Lq) return;       // (whole rows: LANES divides 64)
+    const int c = threadIdx.x % LANES;
+    const int i = (int)(at % a.Lq), h = (int)(at / a.Lq % a.Hq), b = (int)(at / a.Lq / a.Hq);
+    float D = 0.f;
+    if (i < clamped(a.qlen, b, a.Lq)) {
+        const u4v o = load_chunk<T>(static_cast<const T *>(a.O) + b * a.o.b + i * a.o.l + h * a.o.h, PER * c, a.Dh, VEC);
+        const u4v d = load_chunk<T>(static_cast<const T *>(a.dO) + b * a.d.b + i * a.d.l + h * a.d.h, PER * c, a.Dh, VEC);
+        const typename Op<T>::V x = *reinterpret_cast<const typename Op<T>::V *>(&o);
+        const typename Op<T>::V y = *reinterpret_cast<const typename Op<T>::V *>(&d);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) D = fmaf((float)x[e], (float)y[e], D);
+    }
+#pragma unroll
+    for (int x = LANES / 2; x; x /= 2) D += __shfl_xor(D, x);
+    if (c == 0) a.D[at] = D;
+}
 
 // 32 query rows a wave as columns, keys streamed through LDS.
-template <typename T, int DP, int BN>
-__global__ void __launch_bounds__(256) xattn_dq_kernel(CrossAttnGradArgs a) {
-    constexpr int PER = Op<T>::PER, NS = DP / (2 * PER), NJ = DP / 32, CPR = DP / PER;
-    __shared__ __attribute__((aligned(16))) char lds[2 * BN * DP * sizeof(T)];
-    char *const kt = lds, *const vt = lds + BN * DP * sizeof(T);
+template <typename T, int DP, int BN, bool VEC>
+__global__ void __launch_bounds__(256, (sizeof(T) == 4 && DP == 128 ? 1 : 2)) xattn_dq_kernel(CrossAttnGradArgs a) {
+    constexpr int PER = Op<T>::PER, NS = DP / (2 * PER), NJ = DP / 32, TILE = BN * DP * sizeof(T);
+    __shared__ __attribute__((aligned(16))) char lds[4 * TILE];
     const int t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
     const int64_t L = logical_group(a.q_groups);
     if (L >= a.q_groups) return;
-    const int rt = (int)(L % a.row_tiles), bh = (int)(L / a.row_tiles);
+    const int rt = (int)(L % a.row_tiles);
+    const int64_t rest = L / a.row_tiles;
+    const int sp = (int)(rest % a.q_parts), bh = (int)(rest / a.q_parts);
     const int b = bh / a.Hkv, hk = bh % a.Hkv;
     const int ql = clamped(a.qlen, b, a.Lq), kl = clamped(a.klen, b, a.Lk);
     const int m = rt * 128 + 32 * w + (l & 31);
     const bool in = m < a.rows;
     const RowOf row(in ? m : 0, hk, a.G);
     const bool on = in && row.i < ql;
-    const int kend = rt * 128 / a.G >= ql ? 0 : kl;
+    int j0 = sp * a.q_step, kend = j0 + a.q_step < kl ? j0 + a.q_step : kl;
+    if (rt * 128 / a.G >= ql) kend = 0;
 
     typename Op<T>::V q[NS], d[NS];
+    load_frags<T, DP>(q, on ? static_cast<const T *>(a.Q) + b * a.q.b + row.i * a.q.l + row.h * a.q.h : nullptr, a.Dh, VEC, l);
+    load_frags<T, DP>(d, on ? static_cast<const T *>(a.dO) + b * a.d.b + row.i * a.d.l + row.h * a.d.h : nullptr, a.Dh, VEC, l);
     float D = 0.f, lse2 = INFINITY;     // exp2(s - inf) = 0: rows that are not there, rows without a live key
-    const int64_t at = ((int64_t)b * a.Hq + row.h) * a.Lq + row.i;
-    {
-        load_frags<T, DP>(q, on ? static_cast<const T *>(a.O) + b * a.o.b + row.i * a.o.l + row.h * a.o.h : nullptr, a.Dh, a.vec, l);
-        load_frags<T, DP>(d, on ? static_cast<const T *>(a.dO) + b * a.d.b + row.i * a.d.l + row.h * a.d.h : nullptr, a.Dh, a.vec, l);
-#pragma unroll
-        for (int s = 0; s < NS; ++s)
-#pragma unroll
-            for (int e = 0; e < PER; ++e) D = fmaf((float)q[s][e], (float)d[s][e], D);
-        D += other_half(D);
-        load_frags<T, DP>(q, on ? static_cast<const T *>(a.Q) + b * a.q.b + row.i * a.q.l + row.h * a.q.h : nullptr, a.Dh, a.vec, l);
-        if (on) {
-            lse2 = a.lse[at] * LOG2E;
-            if (lse2 == -INFINITY) lse2 = INFINITY;
-        }
-        if (in && l < 32) a.D[at] = D;
+    if (on) {
+        const int64_t at = ((int64_t)b * a.Hq + row.h) * a.Lq + row.i;
+        D = a.D[at];
+        lse2 = a.lse[at] * LOG2E;
+        if (lse2 == -INFINITY) lse2 = INFINITY;
     }
     const float c = a.scale * LOG2E;
     const T *const K = static_cast<const T *>(a.K) + b * a.k.b + hk * a.k.h;
@@ -63,25 +75,26 @@ __global__ void __launch_bounds__(256) xattn_dq_kernel(CrossAttnGradArgs a) {
     f16v o[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) o[j] = f16v{0};
-    for (int j0 = 0; j0 < kend; j0 += BN) {
-        __syncthreads();
-        // (dead keys are zeros: their scores are 0 here, and a factor of a row
-        // of K in dQ is 0 whatever dS is, as long as that is finite)
-        for (int x = t; x < BN * CPR; x += 256) {
-            const int r = x / CPR, j = j0 + r;
-            const bool ok = j < kend && (!mask || mask[j]);
-            u4v kv = {0, 0, 0, 0}, vv = {0, 0, 0, 0};
-            if (ok) {
-                kv = load_chunk<T>(K + (int64_t)j * a.k.l, PER * (x % CPR), a.Dh, a.vec);
-                vv = load_chunk<T>(V + (int64_t)j * a.v.l, PER * (x % CPR), a.Dh, a.vec);
-            }
-            *reinterpret_cast<u4v *>(kt + place<T, DP>(r, x % CPR)) = kv;
-            *reinterpret_cast<u4v *>(vt + place<T, DP>(r, x % CPR)) = vv;
+    TileLoad<T, DP, BN, 256, VEC> kr, vr;
+    uint64_t live = 0, next_live = 0;
+    auto fetch = [&](int j, uint64_t alive) {
+        kr.fetch(K + (int64_t)j * a.k.l, a.k.l, alive, a.Dh, t);
+        vr.fetch(V + (int64_t)j * a.v.l, a.v.l, alive, a.Dh, t);
+    };
+    char *kt = lds, *vt = lds + TILE;
+    int other = 2 * TILE;
+    if (j0 < kend) {
+        live = live_keys<BN>(mask, j0, kend, l);
+        fetch(j0, live);
+        kr.stash(kt, t);
+        vr.stash(vt, t);
+        if (j0 + BN < kend) {
+            next_live = live_keys<BN>(mask, j0 + BN, kend, l);
+            fetch(j0 + BN, next_live);
         }
-        bool alive = l < BN && j0 + l < kend;
-        if (alive && mask) alive = mask[j0 + l] != 0;
-        const uint64_t live = __ballot(alive);
-        __syncthreads();
+    }
+    for (; j0 < kend; j0 += BN) {
+        lds_barrier();
 #pragma unroll
         for (int n = 0; n < BN / 32; ++n) {
             f16v p = {0}, g = {0};
@@ -89,11 +102,14 @@ __global__ void __launch_bounds__(256) xattn_dq_kernel(CrossAttnGradArgs a) {
             for (int s = 0; s < NS; ++s) p = Op<T>::mma(row_frag<T, DP>(kt, 32 * n, s, l), q[s], p);
 #pragma unroll
             for (int s = 0; s < NS; ++s) g = Op<T>::mma(row_frag<T, DP>(vt, 32 * n, s, l), d[s], g);
-            const uint32_t bits = (uint32_t)(live >> (32 * n)) >> (4 * (l >> 5));
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(p[r], c, -lse2));
-                p[r] = (bits >> (8 * (r / 4) + r % 4)) & 1 ? e * (g[r] - D) : 0.f;
+            for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], c, -lse2)) * (g[r] - D);
+            if (live != ALL_LIVE<BN>) {
+                // (dead keys are zeros in LDS: their score is 0, not minus infinity)
+                const uint32_t bits = (uint32_t)(live >> (32 * n)) >> (4 * (l >> 5));
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (!((bits >> (8 * (r / 4) + r % 4)) & 1)) p[r] = 0.f;
             }
 #pragma unroll
             for (int s = 0; s < 16 / PER; ++s) {
@@ -102,141 +118,281 @@ __global__ void __launch_bounds__(256) xattn_dq_kernel(CrossAttnGradArgs a) {
                 for (int j = 0; j < NJ; ++j) o[j] = Op<T>::mma(col_frag<T, DP>(kt, 32 * n, s, j, l), pf, o[j]);
             }
         }
+        kt += other;
+        vt += other;
+        other = -other;
+        live = next_live;
+        if (j0 + BN < kend) {
+            kr.stash(kt, t);
+            vr.stash(vt, t);
+            if (j0 + 2 * BN < kend) {
+                next_live = live_keys<BN>(mask, j0 + 2 * BN, kend, l);
+                fetch(j0 + 2 * BN, next_live);
+            }
+        }
     }
     if (!in) return;
+    float *const part = a.q_parts > 1 ? a.dq_part + (((int64_t)sp * a.B * a.Hkv + bh) * a.rows + m) * DP : nullptr;
     T *const out = static_cast<T *>(a.dQ) + b * a.dq.b + row.i * a.dq.l + row.h * a.dq.h;
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             f4v v;
+            const int at = 32 * j + 8 * g + 4 * (l >> 5);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = on ? o[j][4 * g + e] * a.scale : 0.f;
-            store4<T>(out, 32 * j + 8 * g + 4 * (l >> 5), a.Dh, a.vec, v);
+            if (part) *reinterpret_cast<f4v *>(part + at) = v;
+            else store4<T>(out, at, a.Dh, VEC, v);
         }
 }
 
-// 32 keys a wave as columns, query rows (of all heads that share the keys)
-// streamed through LDS.
-template <typename T, int DP>
-__global__ void __launch_bounds__(256, 1) xattn_dkv_kernel(CrossAttnGradArgs a) {
-    constexpr int PER = Op<T>::PER, NS = DP / (2 * PER), NJ = DP / 32, CPR = DP / PER, BM = 32;
-    __shared__ __attribute__((aligned(16))) char lds[2 * BM * DP * sizeof(T)];
-    __shared__ __attribute__((aligned(16))) float stat[2 * BM];
-    char *const qt = lds, *const dt = lds + BM * DP * sizeof(T);
+// 32 keys a wave as columns, query rows streamed through LDS: the positions of
+// one head after those of another, for all heads that share the keys.
+template <typename T, int DP, bool VEC>
+__global__ void __launch_bounds__(256, (DP == 128 ? 1 : 2)) xattn_dkv_kernel(CrossAttnGradArgs a) {
+    constexpr int PER = Op<T>::PER, NS = DP / (2 * PER), NJ = DP / 32, BM = 32, TILE = BM * DP * sizeof(T);
+    __shared__ __attribute__((aligned(16))) char lds[4 * TILE];
+    __shared__ __attribute__((aligned(16))) float stat[4 * BM];
     const int t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
     const int64_t L = logical_group(a.k_groups);
     if (L >= a.k_groups) return;
-    const int kt = (int)(L % a.key_tiles), bh = (int)(L / a.key_tiles);
+    const int kt = (int)(L % a.key_tiles);
+    const int64_t rest = L / a.key_tiles;
+    const int sp = (int)(rest % a.k_parts), bh = (int)(rest / a.k_parts);
     const int b = bh / a.Hkv, hk = bh % a.Hkv;
     const int ql = clamped(a.qlen, b, a.Lq), kl = clamped(a.klen, b, a.Lk);
     const int j = kt * 128 + 32 * w + (l & 31);         // this lane's key
     const bool in = j < a.Lk;
     bool on = j < kl;
     if (on && a.mask) on = a.mask[b * a.mask_ld + j] != 0;
-    const int rows = kt * 128 < kl ? ql * a.G : 0;
+
+    // tiles of 32 positions, `tiles` a head; this part's run of them
+    const int tiles = kt * 128 < kl ? (ql + BM - 1) / BM : 0;
+    const int64_t total = (int64_t)tiles * a.G;
+    int64_t n = total * sp / a.k_parts;
+    const int64_t end = total * (sp + 1) / a.k_parts;
+    int g = tiles ? (int)(n / tiles) : 0, x = tiles ? (int)(n % tiles) : 0;     // head and tile of the next fetch
 
     typename Op<T>::V k[NS], v[NS];
-    load_frags<T, DP>(k, on ? static_cast<const T *>(a.K) + b * a.k.b + j * a.k.l + hk * a.k.h : nullptr, a.Dh, a.vec, l);
-    load_frags<T, DP>(v, on ? static_cast<const T *>(a.V) + b * a.v.b + j * a.v.l + hk * a.v.h : nullptr, a.Dh, a.vec, l);
+    load_frags<T, DP>(k, on ? static_cast<const T *>(a.K) + b * a.k.b + j * a.k.l + hk * a.k.h : nullptr, a.Dh, VEC, l);
+    load_frags<T, DP>(v, on ? static_cast<const T *>(a.V) + b * a.v.b + j * a.v.l + hk * a.v.h : nullptr, a.Dh, VEC, l);
     const float c = a.scale * LOG2E;
     f16v dk[NJ], dv[NJ];
 #pragma unroll
-    for (int n = 0; n < NJ; ++n) dk[n] = f16v{0}, dv[n] = f16v{0};
-    for (int m0 = 0; m0 < rows; m0 += BM) {
-        __syncthreads();
-        for (int x = t; x < BM * CPR; x += 256) {
-            const int r = x / CPR, m = m0 + r;
-            u4v qv = {0, 0, 0, 0}, ov = {0, 0, 0, 0};
-            if (m < rows) {
-                const RowOf row(m, hk, a.G);
-                qv = load_chunk<T>(static_cast<const T *>(a.Q) + b * a.q.b + row.i * a.q.l + row.h * a.q.h, PER * (x % CPR), a.Dh, a.vec);
-                ov = load_chunk<T>(static_cast<const T *>(a.dO) + b * a.d.b + row.i * a.d.l + row.h * a.d.h, PER * (x % CPR), a.Dh, a.vec);
+    for (int y = 0; y < NJ; ++y) dk[y] = f16v{0}, dv[y] = f16v{0};
+
+    TileLoad<T, DP, BM, 256, VEC> qr, dr;
+    float st = 0.f;
+    auto fetch = [&]() {
+        const int i0 = x * BM, h = hk * a.G + g;
+        const uint64_t alive = ql - i0 >= BM ? ALL_LIVE<BM> : (1ull << (ql - i0)) - 1;
+        qr.fetch(static_cast<const T *>(a.Q) + b * a.q.b + (int64_t)i0 * a.q.l + h * a.q.h, a.q.l, alive, a.Dh, t);
+        dr.fetch(static_cast<const T *>(a.dO) + b * a.d.b + (int64_t)i0 * a.d.l + h * a.d.h, a.d.l, alive, a.Dh, t);
+        if (t < 2 * BM) {
+            // -lse (in units of log 2) and D of the rows; minus infinity, so that exp2 gives 0, for rows that
+            // are not there and rows without a live key
+            const int i = i0 + (t & (BM - 1));
+            st = t < BM ? -INFINITY : 0.f;
+            if (i < ql) {
+                const int64_t at = ((int64_t)b * a.Hq + h) * a.Lq + i;
+                st = t < BM ? -LOG2E * a.lse[at] : a.D[at];
+                if (st == INFINITY) st = -INFINITY;
             }
-            *reinterpret_cast<u4v *>(qt + place<T, DP>(r, x % CPR)) = qv;
-            *reinterpret_cast<u4v *>(dt + place<T, DP>(r, x % CPR)) = ov;
         }
-        if (t < BM) {
-            float lse2 = INFINITY, D = 0.f;
-            if (m0 + t < rows) {
-                const RowOf row(m0 + t, hk, a.G);
-                const int64_t at = ((int64_t)b * a.Hq + row.h) * a.Lq + row.i;
-                lse2 = a.lse[at] * LOG2E;
-                if (lse2 == -INFINITY) lse2 = INFINITY;
-                D = a.D[at];
-            }
-            stat[t] = lse2;
-            stat[BM + t] = D;
-        }
-        __syncthreads();
-        f16v p = {0}, g = {0};
+        if (++x == tiles) x = 0, ++g;
+    };
+    char *qt = lds, *dt = lds + TILE;
+    float *ss = stat;
+    int other = 2 * TILE, other_s = 2 * BM;
+    auto stash = [&]() {
+        qr.stash(qt, t);
+        dr.stash(dt, t);
+        if (t < 2 * BM) ss[t] = st;
+    };
+    if (n < end) {
+        fetch();
+        stash();
+        if (n + 1 < end) fetch();
+    }
+    for (; n < end; ++n) {
+        lds_barrier();
+        f16v p = {0}, s = {0};
 #pragma unroll
-        for (int s = 0; s < NS; ++s) p = Op<T>::mma(row_frag<T, DP>(qt, 0, s, l), k[s], p);
+        for (int y = 0; y < NS; ++y) p = Op<T>::mma(row_frag<T, DP>(qt, 0, y, l), k[y], p);
 #pragma unroll
-        for (int s = 0; s < NS; ++s) g = Op<T>::mma(row_frag<T, DP>(dt, 0, s, l), v[s], g);
+        for (int y = 0; y < NS; ++y) s = Op<T>::mma(row_frag<T, DP>(dt, 0, y, l), v[y], s);
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const f4v lse2 = *reinterpret_cast<const f4v *>(stat + 8 * x + 4 * (l >> 5));
-            const f4v D = *reinterpret_cast<const f4v *>(stat + BM + 8 * x + 4 * (l >> 5));
+        for (int y = 0; y < 4; ++y) {
+            const f4v lse2 = *reinterpret_cast<const f4v *>(ss + 8 * y + 4 * (l >> 5));
+            const f4v D = *reinterpret_cast<const f4v *>(ss + BM + 8 * y + 4 * (l >> 5));
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int r = 4 * x + e;
-                p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], c, -lse2[e]));
-                g[r] = p[r] * (g[r] - D[e]);
+                const int r = 4 * y + e;
+                p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], c, lse2[e]));
+                s[r] = p[r] * (s[r] - D[e]);
             }
         }
 #pragma unroll
-        for (int s = 0; s < 16 / PER; ++s) {
-            const typename Op<T>::V pf = Op<T>::pack(p, s), gf = Op<T>::pack(g, s);
+        for (int y = 0; y < 16 / PER; ++y) {
+            const typename Op<T>::V pf = Op<T>::pack(p, y), sf = Op<T>::pack(s, y);
 #pragma unroll
-            for (int n = 0; n < NJ; ++n) dv[n] = Op<T>::mma(col_frag<T, DP>(dt, 0, s, n, l), pf, dv[n]);
+            for (int z = 0; z < NJ; ++z) dv[z] = Op<T>::mma(col_frag<T, DP>(dt, 0, y, z, l), pf, dv[z]);
 #pragma unroll
-            for (int n = 0; n < NJ; ++n) dk[n] = Op<T>::mma(col_frag<T, DP>(qt, 0, s, n, l), gf, dk[n]);
+            for (int z = 0; z < NJ; ++z) dk[z] = Op<T>::mma(col_frag<T, DP>(qt, 0, y, z, l), sf, dk[z]);
+        }
+        qt += other;
+        dt += other;
+        ss += other_s;
+        other = -other;
+        other_s = -other_s;
+        if (n + 1 < end) {
+            stash();
+            if (n + 2 < end) fetch();
         }
     }
     if (!in) return;
+    const int64_t keys = (int64_t)a.B * a.Hkv * a.Lk;
+    float *const part = a.k_parts > 1 ? a.dkv_part + (2 * sp * keys + (int64_t)bh * a.Lk + j) * DP : nullptr;
     T *const ok = static_cast<T *>(a.dK) + b * a.dk.b + j * a.dk.l + hk * a.dk.h;
     T *const ov = static_cast<T *>(a.dV) + b * a.dv.b + j * a.dv.l + hk * a.dv.h;
 #pragma unroll
-    for (int n = 0; n < NJ; ++n)
+    for (int z = 0; z < NJ; ++z)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
+        for (int y = 0; y < 4; ++y) {
             f4v kv, vv;
+            const int at = 32 * z + 8 * y + 4 * (l >> 5);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                kv[e] = on ? dk[n][4 * x + e] * a.scale : 0.f;
-                vv[e] = on ? dv[n][4 * x + e] : 0.f;
+                kv[e] = on ? dk[z][4 * y + e] * a.scale : 0.f;
+                vv[e] = on ? dv[z][4 * y + e] : 0.f;
             }
-            store4<T>(ok, 32 * n + 8 * x + 4 * (l >> 5), a.Dh, a.vec, kv);
-            store4<T>(ov, 32 * n + 8 * x + 4 * (l >> 5), a.Dh, a.vec, vv);
+            if (part) {
+                *reinterpret_cast<f4v *>(part + at) = kv;
+                *reinterpret_cast<f4v *>(part + keys * DP + at) = vv;
+            } else {
+                store4<T>(ok, at, a.Dh, VEC, kv);
+                store4<T>(ov, at, a.Dh, VEC, vv);
+            }
         }
 }
 
-template <typename T, int DP, int BN>
-hipError_t launch_sized(const CrossAttnGradArgs &a, hipStream_t s) {
-    if (a.q_groups) {
-        xattn_dq_kernel<T, DP, BN><<<dim3((unsigned)((a.q_groups + 7) / 8 * 8)), dim3(256), 0, s>>>(a);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
+// Adds up the parts of a row, DP / 4 lanes a row: rows of dQ first, then those
+// of dK and of dV.
+template <typename T, int DP, bool VEC>
+__global__ void __launch_bounds__(256) xattn_parts_kernel(CrossAttnGradArgs a) {
+    constexpr int LANES = DP / 4;
+    const int d = 4 * (threadIdx.x % LANES);
+    int64_t at = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const int64_t qrows = (int64_t)a.B * a.Hkv * a.rows, keys = (int64_t)a.B * a.Hkv * a.Lk;
+    const float *p;
+    T *out;
+    int parts;
+    int64_t step;
+    if (at < a.join_q) {
+        p = a.dq_part + at * DP;
+        parts = a.q_parts;
+        step = qrows * DP;
+        const int bh = (int)(at / a.rows);
+        const RowOf row((int)(at % a.rows), bh % a.Hkv, a.G);
+        out = static_cast<T *>(a.dQ) + bh / a.Hkv * a.dq.b + row.i * a.dq.l + row.h * a.dq.h;
+    } else {
+        at -= a.join_q;
+        if (at >= a.join_k) return;
+        p = a.dkv_part + at * DP;
+        parts = a.k_parts;
+        step = 2 * keys * DP;
+        const bool is_v = at >= keys;
+        if (is_v) at -= keys;
+        const int bh = (int)(at / a.Lk), j = (int)(at % a.Lk);
+        const SeqStrides z = is_v ? a.dv : a.dk;
+        out = static_cast<T *>(is_v ? a.dV : a.dK) + bh / a.Hkv * z.b + j * z.l + bh % a.Hkv * z.h;
     }
-    if (!a.k_groups) return hipSuccess;
-    xattn_dkv_kernel<T, DP><<<dim3((unsigned)((a.k_groups + 7) / 8 * 8)), dim3(256), 0, s>>>(a);
-    return hipGetLastError();
+    f4v v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < parts; ++s) v += *reinterpret_cast<const f4v *>(p + s * step + d);
+    store4<T>(out, d, a.Dh, VEC, v);
 }
+
+// Parts that bring the work-groups to two a CU, as far as parts of a useful
+// length (128 keys, 4 tiles of 32 query rows) go.
+struct Plan {
+    int dp, q_parts, q_step, k_parts;
+};
+Plan plan_for(int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh) {
+    Plan p{};
+    p.dp = Dh <= 64 ? 64 : 128;
+    const int64_t G = Hq / Hkv, most = 512;
+    const int64_t q_groups = B * Hkv * ((Lq * G + 127) / 128), k_groups = B * Hkv * ((Lk + 127) / 128);
+    auto parts = [&](int64_t groups, int64_t useful) {
+        int64_t n = groups ? most / groups : 1;
+        n = n < useful ? n : useful;
+        return (int)(n > 1 ? n : 1);
+    };
+    int n = parts(q_groups, Lk / 128);
+    const int64_t step = ((Lk + n - 1) / n + 63) / 64 * 64;
+    p.q_step = (int)(step ? step : 64);
+    p.q_parts = Lk ? (int)((Lk + step - 1) / step) : 1;
+    p.k_parts = parts(k_groups, (Lq + 31) / 32 * G / 4);
+    return p;
+}
+
+template <typename T, int DP, int BN, bool VEC>
+hipError_t launch_sized(const CrossAttnGradArgs &a, hipStream_t s) {
+    const auto grid = [](int64_t n, int64_t per) { return dim3((unsigned)((n + per - 1) / per)); };
+    hipError_t e = hipSuccess;
+    if (a.q_groups) {
+        xattn_rows_kernel<T, DP, VEC><<<grid((int64_t)a.B * a.Hq * a.Lq, 256 / (DP / Op<T>::PER)), dim3(256), 0, s>>>(a);
+        xattn_dq_kernel<T, DP, BN, VEC><<<dim3((unsigned)((a.q_groups + 7) / 8 * 8)), dim3(256), 0, s>>>(a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (a.k_groups) {
+        xattn_dkv_kernel<T, DP, VEC><<<dim3((unsigned)((a.k_groups + 7) / 8 * 8)), dim3(256), 0, s>>>(a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (a.join_q + a.join_k) {
+        xattn_parts_kernel<T, DP, VEC><<<grid(a.join_q + a.join_k, 256 / (DP / 4)), dim3(256), 0, s>>>(a);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+template <typename T, int BN> hipError_t launch_typed(const CrossAttnGradArgs &a, int dp, hipStream_t s) {
+    if (dp == 64) return a.vec ? launch_sized<T, 64, BN, true>(a, s) : launch_sized<T, 64, BN, false>(a, s);
+    return a.vec ? launch_sized<T, 128, BN, true>(a, s) : launch_sized<T, 128, BN, false>(a, s);
+}
+
+int64_t align4(int64_t n) { return (n + 3) / 4 * 4; }     // (16-byte rows of parts behind D)
 
 }  // namespace
 
-size_t cross_attn_grad_workspace(int64_t B, int64_t Lq, int64_t Hq) { return (size_t)(B * Lq * Hq) * 4; }
+size_t cross_attn_grad_workspace(int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh) {
+    const Plan p = plan_for(B, Lq, Lk, Hq, Hkv, Dh);
+    size_t n = (size_t)align4(B * Lq * Hq);
+    if (p.q_parts > 1) n += (size_t)(B * Lq * Hq) * p.q_parts * p.dp;
+    if (p.k_parts > 1) n += (size_t)(B * Lk * Hkv) * 2 * p.k_parts * p.dp;
+    return n * 4;
+}
 
 hipError_t launch_cross_attn_grad(gs_dtype t, CrossAttnGradArgs a, void *ws, hipStream_t s) {
+    const Plan p = plan_for(a.B, a.Lq, a.Lk, a.Hq, a.Hkv, a.Dh);
     a.rows = a.Lq * a.G;
     a.row_tiles = (int)(((int64_t)a.rows + 127) / 128);
     a.key_tiles = (int)(((int64_t)a.Lk + 127) / 128);
-    a.q_groups = (int64_t)a.B * a.Hkv * a.row_tiles;
-    a.k_groups = (int64_t)a.B * a.Hkv * a.key_tiles;
+    a.q_parts = p.q_parts;
+    a.q_step = p.q_step;
+    a.k_parts = p.k_parts;
+    a.q_groups = (int64_t)a.B * a.Hkv * a.row_tiles * p.q_parts;
+    a.k_groups = (int64_t)a.B * a.Hkv * a.key_tiles * p.k_parts;
+    const int64_t qrows = (int64_t)a.B * a.Hq * a.Lq, keys = (int64_t)a.B * a.Hkv * a.Lk;
+    a.join_q = p.q_parts > 1 ? qrows : 0;
+    a.join_k = p.k_parts > 1 ? 2 * keys : 0;
     a.D = static_cast<float *>(ws);
-    if (t == GS_F32) return a.Dh <= 64 ? launch_sized<float, 64, 32>(a, s) : launch_sized<float, 128, 32>(a, s);
-    return a.Dh <= 64 ? launch_sized<bf16_t, 64, 64>(a, s) : launch_sized<bf16_t, 128, 64>(a, s);
+    a.dq_part = a.D + align4(qrows);
+    a.dkv_part = a.dq_part + a.join_q * p.q_parts * p.dp;
+    // tiles are read with 32-bit offsets: rows of a tile within 2^31 bytes
+    for (const SeqStrides *x : {&a.q, &a.k, &a.v, &a.d}) a.vec = a.vec && x->l < ATTN_VEC_STRIDE;
+    return t == GS_F32 ? launch_typed<float, 32>(a, p.dp, s) : launch_typed<bf16_t, 64>(a, p.dp, s);
 }
 
 }  // namespace gs
