@@ -198,6 +198,45 @@ template <typename T, int DP, int BN, int NT, bool VEC> struct TileLoad {
     }
 };
 
+// The same tile brought straight to LDS, a piece of 16 bytes a lane: nothing is
+// held in registers on the way.  The loads are written as assembly so that the
+// compiler does not wait for them before unrelated LDS reads (it cannot tell
+// the buffers apart); wait_tiles orders them.  Rows past the last one are read
+// as that one (what is made of them has weight 0); pieces at and past dh are out
+// of the resource's range and leave the zeros that clear_lds has put there, or
+// zeros.
+typedef int i4v __attribute__((ext_vector_type(4)));
+template <typename T, int DP, int BN, int NT> struct TileDma {
+    static constexpr int PER = Op<T>::PER, CPR = DP / PER, N = BN * CPR / NT;
+    static_assert(BN * CPR % NT == 0, "whole pieces per thread");
+    static __device__ __forceinline__ void issue(const T *base, int64_t stride, int last, int dh, const char *tile, int t) {
+        const uint64_t a = reinterpret_cast<uint64_t>(base);
+        i4v rs;
+        rs[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)a);
+        rs[1] = __builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xffffu));
+        rs[2] = 0x7fffffff;
+        rs[3] = 0x00020000;
+        const uint32_t row = (uint32_t)stride * (uint32_t)sizeof(T);
+        const int w = __builtin_amdgcn_readfirstlane(t >> 6);
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            const int r = (q * NT + t) / CPR, pos = (q * NT + t) % CPR;
+            const int c = place<T, DP>(r, pos) / 16 - r * CPR;      // the piece that lies there
+            const uint32_t off = c * PER < dh ? (uint32_t)(r < last ? r : last) * row + 16 * c : 0x80000000u;
+            const int m0v = __builtin_amdgcn_readfirstlane((int)(size_t)(const GS_LDS char *)tile + (q * NT + 64 * w) * 16);
+            asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds"
+                         :
+                         : "v"(off), "s"(m0v), "s"(rs)
+                         : "memory", "m0");
+        }
+    }
+};
+template <int NT> __device__ __forceinline__ void clear_lds(char *p, int bytes, int t) {
+    for (int i = 16 * t; i < bytes; i += 16 * NT) *reinterpret_cast<u4v *>(p + i) = u4v{0, 0, 0, 0};
+}
+// All of this wave's loads have landed (vmcnt 0).
+__device__ __forceinline__ void wait_tiles() { __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8)); }
+
 // A row's position and head: packed row m = position G + head within the group.
 struct RowOf {
     int i, h;

@@ -232,6 +232,7 @@ hipError_t launch_sparse_prob2vec(gs_dtype tv, gs_dtype tt, const SparseArgs &a,
 // Cross attention (gs_xattn.hip) and its gradient (gs_xattn_grad.hip).
 constexpr int CROSS_ATTN_MAX_DH = 128;
 constexpr int64_t ATTN_VEC_STRIDE = (int64_t)1 << 22;    // elements: 64 rows of up to 4 bytes each within 2^30 bytes
+typedef float f2v __attribute__((ext_vector_type(2)));
 struct SeqStrides { int64_t b, l, h; };     // elements between sequences, positions, heads
 struct CrossAttnArgs {
     const void *Q, *K, *V;
@@ -265,7 +266,7 @@ struct CrossAttnGradArgs {
     int q_parts, q_step, k_parts;       // parts of the keys (dQ) and of the query rows (dK, dV)
     int64_t q_groups, k_groups;
     int64_t join_q, join_k;             // rows to add up: of dQ, and of dK and dV
-    float *D;                           // B x Hq x Lq: sum_d dO O
+    f2v *stat;                          // B x Hq x Lq: -lse / ln 2, sum_d dO O
     float *dq_part, *dkv_part;
 };
 size_t cross_attn_grad_workspace(int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh);

@@ -15,7 +15,9 @@ namespace gs {
 namespace {
 using namespace attn;
 
-// D: a row in DP / 8 lanes.
+// What the passes need of a row: D, and -lse in units of log 2, the constant of
+// the exponent; minus infinity, so that exp2 gives 0, for rows that are not
+// there and rows without a live key.  A row in DP / PER lanes.
 template <typename T, int DP, bool VEC>
 __global__ void __launch_bounds__(256) xattn_rows_kernel(CrossAttnGradArgs a) {
     constexpr int PER = Op<T>::PER, LANES = DP / PER;
@@ -34,7 +36,10 @@ __global__ void __launch_bounds__(256) xattn_rows_kernel(CrossAttnGradArgs a) {
     }
 #pragma unroll
     for (int x = LANES / 2; x; x /= 2) D += __shfl_xor(D, x);
-    if (c == 0) a.D[at] = D;
+    if (c) return;
+    float e = -LOG2E * a.lse[at];
+    if (!(i < clamped(a.qlen, b, a.Lq)) || e == INFINITY) e = -INFINITY;
+    a.stat[at] = f2v{e, D};
 }
 
 // 32 query rows a wave as columns, keys streamed through LDS.
@@ -60,13 +65,7 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DP == 128 ? 1 : 2)) xa
     typename Op<T>::V q[NS], d[NS];
     load_frags<T, DP>(q, on ? static_cast<const T *>(a.Q) + b * a.q.b + row.i * a.q.l + row.h * a.q.h : nullptr, a.Dh, VEC, l);
     load_frags<T, DP>(d, on ? static_cast<const T *>(a.dO) + b * a.d.b + row.i * a.d.l + row.h * a.d.h : nullptr, a.Dh, VEC, l);
-    float D = 0.f, lse2 = INFINITY;     // exp2(s - inf) = 0: rows that are not there, rows without a live key
-    if (on) {
-        const int64_t at = ((int64_t)b * a.Hq + row.h) * a.Lq + row.i;
-        D = a.D[at];
-        lse2 = a.lse[at] * LOG2E;
-        if (lse2 == -INFINITY) lse2 = INFINITY;
-    }
+    const f2v st = on ? a.stat[((int64_t)b * a.Hq + row.h) * a.Lq + row.i] : f2v{-INFINITY, 0.f};
     const float c = a.scale * LOG2E;
     const T *const K = static_cast<const T *>(a.K) + b * a.k.b + hk * a.k.h;
     const T *const V = static_cast<const T *>(a.V) + b * a.v.b + hk * a.v.h;
@@ -95,7 +94,7 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DP == 128 ? 1 : 2)) xa
     }
     for (; j0 < kend; j0 += BN) {
         lds_barrier();
-#pragma unroll
+#pragma unroll 1
         for (int n = 0; n < BN / 32; ++n) {
             f16v p = {0}, g = {0};
 #pragma unroll
@@ -103,7 +102,7 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DP == 128 ? 1 : 2)) xa
 #pragma unroll
             for (int s = 0; s < NS; ++s) g = Op<T>::mma(row_frag<T, DP>(vt, 32 * n, s, l), d[s], g);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], c, -lse2)) * (g[r] - D);
+            for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], c, st[0])) * (g[r] - st[1]);
             if (live != ALL_LIVE<BN>) {
                 // (dead keys are zeros in LDS: their score is 0, not minus infinity)
                 const uint32_t bits = (uint32_t)(live >> (32 * n)) >> (4 * (l >> 5));
@@ -149,11 +148,17 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DP == 128 ? 1 : 2)) xa
 
 // 32 keys a wave as columns, query rows streamed through LDS: the positions of
 // one head after those of another, for all heads that share the keys.
+// The keys' rows of V stay in registers, and so do those of K where two waves
+// a SIMD then still fit (256 registers each); bf16 rows of 128 values leave K
+// in LDS, fp32 ones run one wave a SIMD (one wave a SIMD for bf16: 443 us for
+// train_large's 16 x 2048 x 2048 x 4, against TIMEDKV).
 template <typename T, int DP, bool VEC>
-__global__ void __launch_bounds__(256, (DP == 128 ? 1 : 2)) xattn_dkv_kernel(CrossAttnGradArgs a) {
+__global__ void __launch_bounds__(256, (sizeof(T) == 4 && DP == 128 ? 1 : 2)) xattn_dkv_kernel(CrossAttnGradArgs a) {
     constexpr int PER = Op<T>::PER, NS = DP / (2 * PER), NJ = DP / 32, BM = 32, TILE = BM * DP * sizeof(T);
-    __shared__ __attribute__((aligned(16))) char lds[4 * TILE];
-    __shared__ __attribute__((aligned(16))) float stat[4 * BM];
+    constexpr bool KEEP_K = !(sizeof(T) == 2 && DP == 128);
+    __shared__ __attribute__((aligned(16))) char lds[4 * TILE + (KEEP_K ? 0 : 128 * DP * sizeof(T))];
+    __shared__ __attribute__((aligned(16))) f2v stat[2 * BM];
+    char *const keys_lds = lds + 4 * TILE;
     const int t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
     const int64_t L = logical_group(a.k_groups);
     if (L >= a.k_groups) return;
@@ -169,68 +174,80 @@ __global__ void __launch_bounds__(256, (DP == 128 ? 1 : 2)) xattn_dkv_kernel(Cro
 
     // tiles of 32 positions, `tiles` a head; this part's run of them
     const int tiles = kt * 128 < kl ? (ql + BM - 1) / BM : 0;
+    // (below 2^31, as B Hq Lq is; divided once, kept in scalar registers)
     const int64_t total = (int64_t)tiles * a.G;
-    int64_t n = total * sp / a.k_parts;
-    const int64_t end = total * (sp + 1) / a.k_parts;
-    int g = tiles ? (int)(n / tiles) : 0, x = tiles ? (int)(n % tiles) : 0;     // head and tile of the next fetch
+    int n = __builtin_amdgcn_readfirstlane((int)(total * sp / a.k_parts));
+    const int end = __builtin_amdgcn_readfirstlane((int)(total * (sp + 1) / a.k_parts));
+    int g = __builtin_amdgcn_readfirstlane(tiles ? n / tiles : 0), x = n - g * tiles;     // head and tile of the next fetch
 
     typename Op<T>::V k[NS], v[NS];
     load_frags<T, DP>(k, on ? static_cast<const T *>(a.K) + b * a.k.b + j * a.k.l + hk * a.k.h : nullptr, a.Dh, VEC, l);
+    if constexpr (!KEEP_K) {    // (read back by the wave that writes them)
+#pragma unroll
+        for (int y = 0; y < NS; ++y)
+            *reinterpret_cast<typename Op<T>::V *>(keys_lds + place<T, DP>(32 * w + (l & 31), 2 * y + (l >> 5))) = k[y];
+    }
     load_frags<T, DP>(v, on ? static_cast<const T *>(a.V) + b * a.v.b + j * a.v.l + hk * a.v.h : nullptr, a.Dh, VEC, l);
     const float c = a.scale * LOG2E;
     f16v dk[NJ], dv[NJ];
 #pragma unroll
     for (int y = 0; y < NJ; ++y) dk[y] = f16v{0}, dv[y] = f16v{0};
 
-    TileLoad<T, DP, BM, 256, VEC> qr, dr;
-    float st = 0.f;
-    auto fetch = [&]() {
+    // VEC: tiles go straight to LDS, the next while one is used; otherwise
+    // through registers, each when it is needed
+    TileLoad<T, DP, BM, 256, false> qr, dr;
+    f2v st = {0.f, 0.f};
+    char *qt = lds, *dt = lds + TILE;
+    f2v *ss = stat;
+    int other = 2 * TILE, other_s = BM;
+    auto fetch = [&](char *to) {
         const int i0 = x * BM, h = hk * a.G + g;
-        const uint64_t alive = ql - i0 >= BM ? ALL_LIVE<BM> : (1ull << (ql - i0)) - 1;
-        qr.fetch(static_cast<const T *>(a.Q) + b * a.q.b + (int64_t)i0 * a.q.l + h * a.q.h, a.q.l, alive, a.Dh, t);
-        dr.fetch(static_cast<const T *>(a.dO) + b * a.d.b + (int64_t)i0 * a.d.l + h * a.d.h, a.d.l, alive, a.Dh, t);
-        if (t < 2 * BM) {
-            // -lse (in units of log 2) and D of the rows; minus infinity, so that exp2 gives 0, for rows that
-            // are not there and rows without a live key
-            const int i = i0 + (t & (BM - 1));
-            st = t < BM ? -INFINITY : 0.f;
-            if (i < ql) {
-                const int64_t at = ((int64_t)b * a.Hq + h) * a.Lq + i;
-                st = t < BM ? -LOG2E * a.lse[at] : a.D[at];
-                if (st == INFINITY) st = -INFINITY;
-            }
+        const T *const Q = static_cast<const T *>(a.Q) + b * a.q.b + (int64_t)i0 * a.q.l + h * a.q.h;
+        const T *const O = static_cast<const T *>(a.dO) + b * a.d.b + (int64_t)i0 * a.d.l + h * a.d.h;
+        if constexpr (VEC) {
+            TileDma<T, DP, BM, 256>::issue(Q, a.q.l, ql - 1 - i0, a.Dh, to, t);
+            TileDma<T, DP, BM, 256>::issue(O, a.d.l, ql - 1 - i0, a.Dh, to + TILE, t);
+        } else {
+            const uint64_t alive = ql - i0 >= BM ? ALL_LIVE<BM> : (1ull << (ql - i0)) - 1;
+            qr.fetch(Q, a.q.l, alive, a.Dh, t);
+            dr.fetch(O, a.d.l, alive, a.Dh, t);
         }
+        if (t < BM) st = i0 + t < ql ? (a.stat + ((int64_t)b * a.Hq + h) * a.Lq + i0)[t] : f2v{-INFINITY, 0.f};
         if (++x == tiles) x = 0, ++g;
     };
-    char *qt = lds, *dt = lds + TILE;
-    float *ss = stat;
-    int other = 2 * TILE, other_s = 2 * BM;
-    auto stash = [&]() {
-        qr.stash(qt, t);
-        dr.stash(dt, t);
-        if (t < 2 * BM) ss[t] = st;
-    };
-    if (n < end) {
-        fetch();
-        stash();
-        if (n + 1 < end) fetch();
+    if constexpr (VEC) {
+        clear_lds<256>(lds, 4 * TILE, t);
+        lds_barrier();
+        if (n < end) fetch(qt);
     }
     for (; n < end; ++n) {
+        if constexpr (VEC) {
+            wait_tiles();
+        } else {
+            fetch(qt);
+            qr.stash(qt, t);
+            dr.stash(dt, t);
+        }
+        if (t < BM) ss[t] = st;
         lds_barrier();
+        if (VEC && n + 1 < end) fetch(qt + other);
         f16v p = {0}, s = {0};
 #pragma unroll
-        for (int y = 0; y < NS; ++y) p = Op<T>::mma(row_frag<T, DP>(qt, 0, y, l), k[y], p);
+        for (int y = 0; y < NS; ++y) {
+            const typename Op<T>::V ky = KEEP_K ? k[y] : row_frag<T, DP>(keys_lds, 32 * w, y, l);
+            p = Op<T>::mma(row_frag<T, DP>(qt, 0, y, l), ky, p);
+        }
 #pragma unroll
         for (int y = 0; y < NS; ++y) s = Op<T>::mma(row_frag<T, DP>(dt, 0, y, l), v[y], s);
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
-            const f4v lse2 = *reinterpret_cast<const f4v *>(ss + 8 * y + 4 * (l >> 5));
-            const f4v D = *reinterpret_cast<const f4v *>(ss + BM + 8 * y + 4 * (l >> 5));
+            const f4v *const sy = reinterpret_cast<const f4v *>(ss + 8 * y + 4 * (l >> 5));
+            const f4v two[2] = {sy[0], sy[1]};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int r = 4 * y + e;
-                p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], c, lse2[e]));
-                s[r] = p[r] * (s[r] - D[e]);
+                p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], c, two[e / 2][2 * (e % 2)]));
+                s[r] = p[r] * (s[r] - two[e / 2][2 * (e % 2) + 1]);
             }
         }
 #pragma unroll
@@ -246,10 +263,6 @@ __global__ void __launch_bounds__(256, (DP == 128 ? 1 : 2)) xattn_dkv_kernel(Cro
         ss += other_s;
         other = -other;
         other_s = -other_s;
-        if (n + 1 < end) {
-            stash();
-            if (n + 2 < end) fetch();
-        }
     }
     if (!in) return;
     const int64_t keys = (int64_t)a.B * a.Hkv * a.Lk;
@@ -362,13 +375,13 @@ template <typename T, int BN> hipError_t launch_typed(const CrossAttnGradArgs &a
     return a.vec ? launch_sized<T, 128, BN, true>(a, s) : launch_sized<T, 128, BN, false>(a, s);
 }
 
-int64_t align4(int64_t n) { return (n + 3) / 4 * 4; }     // (16-byte rows of parts behind D)
+int64_t align4(int64_t n) { return (n + 3) / 4 * 4; }     // (16-byte rows of parts behind the rows' constants)
 
 }  // namespace
 
 size_t cross_attn_grad_workspace(int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh) {
     const Plan p = plan_for(B, Lq, Lk, Hq, Hkv, Dh);
-    size_t n = (size_t)align4(B * Lq * Hq);
+    size_t n = (size_t)align4(2 * B * Lq * Hq);
     if (p.q_parts > 1) n += (size_t)(B * Lq * Hq) * p.q_parts * p.dp;
     if (p.k_parts > 1) n += (size_t)(B * Lk * Hkv) * 2 * p.k_parts * p.dp;
     return n * 4;
@@ -387,8 +400,8 @@ hipError_t launch_cross_attn_grad(gs_dtype t, CrossAttnGradArgs a, void *ws, hip
     const int64_t qrows = (int64_t)a.B * a.Hq * a.Lq, keys = (int64_t)a.B * a.Hkv * a.Lk;
     a.join_q = p.q_parts > 1 ? qrows : 0;
     a.join_k = p.k_parts > 1 ? 2 * keys : 0;
-    a.D = static_cast<float *>(ws);
-    a.dq_part = a.D + align4(qrows);
+    a.stat = static_cast<f2v *>(ws);
+    a.dq_part = static_cast<float *>(ws) + align4(2 * qrows);
     a.dkv_part = a.dq_part + a.join_q * p.q_parts * p.dp;
     // tiles are read with 32-bit offsets: rows of a tile within 2^31 bytes
     for (const SeqStrides *x : {&a.q, &a.k, &a.v, &a.d}) a.vec = a.vec && x->l < ATTN_VEC_STRIDE;
