@@ -606,7 +606,7 @@ gs_status gs_cross_attention_grad(const gs_cross_attn *a, gs_dtype t, void *ws, 
  *               (0: none), 16-byte aligned, contents unspecified; calls that
  *               may run at the same time need one each
  * Weights are formed in fp64 and summed as whole multiples of 2^-s of the
- * largest, s = min(52, 62 - ceil(log2 M)), an entry of any weight counting at
+ * largest, s = min(51, 62 - ceil(log2 M)), an entry of any weight counting at
  * least one: results do not depend on the order of a sum.
  */
 typedef struct {

@@ -16,12 +16,13 @@
 //                       entries are in question, and these are ranked
 //   a work-group a row  up to 8192 entries, in registers: a histogram of the
 //                       scores below the largest finds the bin the run ends in
-//   work-groups a row   more entries: the same over chunks of 8192, in four
-//                       launches (largest score, histogram, entries of the bin,
-//                       ranking and draw): a launch boundary hands a row's data
-//                       on faster than fences and counters did, which write the
-//                       caches back from every work-group (402 and 511 us for
-//                       the two launches they were in, against TIMES)
+//   work-groups a row   more entries: the same over chunks of 8192, in five
+//                       launches (largest score, histogram, where the run ends,
+//                       entries in question, ranking and draw).  A launch
+//                       boundary hands a row's data on faster than fences and
+//                       counters did, which write caches back from every
+//                       work-group: 200 rows of 128001 took 402 and 511 us in
+//                       the launches that had them, 97 and 128 without
 #include "gs_internal.h"
 
 namespace gs {
@@ -37,6 +38,7 @@ __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+constexpr uint32_t LOWEST = 0x00800000u;     // key of the lowest finite score
 __device__ __forceinline__ float value_of(uint32_t key) {
     return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
@@ -47,27 +49,42 @@ __device__ __forceinline__ void fill_table(double *table, int t) {
     if (t < TABLE) table[t] = exp2((double)t / TABLE);
 }
 
-// Weight of an entry, exp((x - max) / temperature): 2^y with y in 64ths taken
-// from the table and the rest, |t| <= ln 2 / 128, by its series up to t^4 (the
-// next term is below 4e-14 of the weight).
+// Weight of an entry, exp((x - max) / temperature) = 2^(y / 64): the whole part
+// of y from the table and the exponent, the rest, |f| <= 1/2, by its series up
+// to f^4 (the next term is below 4e-14 of the weight).  Whole parts and
+// multiples are taken by adding a power of two whose last place is the unit
+// (no conversions between fp64 and integers).
 struct Weigh {
-    double m, c;                // largest score; log2(e) / temperature
-    int shift;                  // a mass of 2^shift is the largest weight
+    double m, c;                // largest score; 64 log2(e) / temperature
+    int shift;                  // a mass of 2^shift (at most 2^51) is the largest weight
     const double *table;
+    // an infinite largest score leaves weight to its equals alone
+    __device__ __forceinline__ Weigh(uint32_t top, double c64, int s, const double *t)
+        : m(fmin((double)value_of(top), 1e300)), c(c64), shift(s), table(t) {}
+    __device__ __forceinline__ double scaled(uint32_t key) const { return fmin(((double)value_of(key) - m) * c, 0.); }
+    __device__ __forceinline__ double part(double y, int &n) const {     // 2^(y / 64) = part 2^n
+        const double z = y + 6755399441055744.;                         // 1.5 2^52
+        const int whole = (int)(uint32_t)__double_as_longlong(z);
+        const double f = y - (z - 6755399441055744.);
+        constexpr double L = 0.693147180559945309417 / TABLE;
+        n = whole >> 6;
+        return fma(fma(fma(fma(f, L * L * L * L / 24, L * L * L / 6), f, L * L / 2), f, L), f, 1.) * table[whole & (TABLE - 1)];
+    }
     __device__ __forceinline__ double weight(uint32_t key) const {
-        const double x = value_of(key);
-        if (x == m) return 1.;
-        const double y = fmax((x - m) * c, -1100.);     // (2^-1100 is zero)
-        const double n = rint(y * TABLE);
-        const double t = fma(n, -1. / TABLE, y) * 0.693147180559945309417;
-        const int i = (int)n;
-        const double s = fma(fma(fma(fma(t, 1. / 24, 1. / 6), t, 0.5), t, 1.), t, 1.);
-        return ldexp(s * table[i & (TABLE - 1)], i >> 6);
+        int n;
+        const double w = part(fmax(scaled(key), -1100. * TABLE), n);
+        return ldexp(w, n);
     }
-    __device__ __forceinline__ uint64_t mass_of(double w) const {
-        return w > 0. ? (uint64_t)fmax(1., rint(ldexp(w, shift))) : 0;
+    // The weight in whole multiples of 2^-shift, at least one (zero only below
+    // the smallest fp64 number); weights below 2^-70 all round to that one.
+    __device__ __forceinline__ uint64_t mass(uint32_t key) const {
+        const double y = scaled(key);
+        int n;
+        const double w = part(fmax(y, -70. * TABLE), n);
+        const double v = __longlong_as_double(__double_as_longlong(w) + (int64_t)(n + shift) * (1ll << 52));
+        const uint64_t r = (uint64_t)__double_as_longlong(v + 4503599627370496.) & 0xfffffffffffffull;      // 2^52
+        return r ? r : (y > -1074. * TABLE ? 1 : 0);
     }
-    __device__ __forceinline__ uint64_t mass(uint32_t key) const { return key ? mass_of(weight(key)) : 0; }
 };
 
 // A row's parameters, brought into range.
@@ -75,7 +92,7 @@ struct Row {
     int64_t k;                  // entries kept by rank, M: all
     double p;                   // share of the weight kept, >= 1: all
     double least;               // smallest weight kept
-    double c;                   // log2(e) / temperature
+    double c;                   // 64 log2(e) / temperature
     float temp;
     __device__ __forceinline__ Row(const SampleArgs &a, int64_t b) {
         temp = a.temperature ? a.temperature[b] : a.temperature_all;
@@ -88,9 +105,10 @@ struct Row {
         }
         p = tp < 1.f ? (tp > 0.f ? (double)tp : 0.) : 1.;
         least = mp > 0.f ? fmin(1., (double)mp) : 0.;
-        c = 1.4426950408889634074 / (double)temp;
+        c = fmax(TABLE * 1.4426950408889634074 / (double)temp, 1e-290);     // (infinite temperature: all weights 1)
     }
     __device__ __forceinline__ bool keeps_all(int64_t M) const { return k >= M && p >= 1.; }
+    __device__ __forceinline__ bool takes_first() const { return k == 1; }
 };
 
 // The sum that the drawn entry's has to exceed.
@@ -114,16 +132,21 @@ template <> struct Quad<bf16_t> {
     }
 };
 
-// Keys of V consecutive entries from j on (0 past the row's end).
-template <typename T, int V>
-__device__ __forceinline__ void load_keys(uint32_t *key, const T *row, int64_t j, int64_t M, bool vec) {
-    if (V == 4 && vec && j + 4 <= M) {
+// Entries are dealt out by places: place 0 is the last one at or before a row's
+// start that lies on a boundary of four entries, so that quads of places load
+// as one piece whatever the row's alignment; index = place - skew.
+template <typename T> __device__ __forceinline__ int skew_of(const T *row) {
+    return (int)(reinterpret_cast<uintptr_t>(row) / sizeof(T) & 3);
+}
+// Keys of the V entries from index j on (0 outside the row).
+template <typename T, int V> __device__ __forceinline__ void load_keys(uint32_t *key, const T *row, int32_t j, uint32_t M) {
+    if (V == 4 && (uint32_t)j < M && (uint32_t)(j + 3) < M) {
         const f4v x = Quad<T>::load(row + j);
 #pragma unroll
         for (int c = 0; c < V; ++c) key[c] = key_of(x[c]);
     } else {
 #pragma unroll
-        for (int c = 0; c < V; ++c) key[c] = j + c < M ? key_of(ld_f32<T>(row, j + c)) : 0;
+        for (int c = 0; c < V; ++c) key[c] = (uint32_t)(j + c) < M ? key_of(ld_f32<T>(row, j + c)) : 0;
     }
 }
 
@@ -164,62 +187,117 @@ __device__ __forceinline__ void wave_sync() {
 }
 __device__ __forceinline__ int below(uint64_t ballot, int l) { return __popcll(ballot & (((uint64_t)1 << l) - 1)); }
 
-// Lists of up to 64 E entries in index order: lane l holds entries E l + e.
-// Entries in rank order before each of this lane's: their number and mass.
-template <int E>
-__device__ __forceinline__ void rank_lanes(const uint32_t (&key)[E], const uint64_t (&mass)[E], int n, int l, int (&rank)[E],
-                                           uint64_t (&before)[E]) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) rank[e] = 0, before[e] = 0;
-    for (int i = 0; i < n; i += E) {
-#pragma unroll
-        for (int f = 0; f < E; ++f) {
-            const uint32_t k = __builtin_amdgcn_readlane(key[f], i / E);
-            const uint64_t m = read_lane64(mass[f], i / E);
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (k > key[e] || (k == key[e] && i + f < E * l + e)) {
-                    ++rank[e];
-                    before[e] += m;
-                }
-        }
+// The smallest key in [lo, hi] with `has`, which holds for hi and, with a key,
+// for all larger ones: 64 candidates a step.
+template <typename F> __device__ __forceinline__ uint32_t least_key(uint32_t lo, uint32_t hi, int l, F has) {
+    while (lo < hi) {
+        const uint32_t step = (hi - lo + 63) / 64;
+        const uint64_t at = (uint64_t)lo + (uint64_t)l * step;
+        const uint64_t on = __ballot(at >= hi || has((uint32_t)at));
+        const int first = on ? __ffsll((unsigned long long)on) - 1 : 64;    // (64 steps reach hi)
+        const uint64_t next = (uint64_t)lo + (uint64_t)first * step;
+        if (first) lo = lo + (uint32_t)((first - 1) * (uint64_t)step) + 1;
+        else return lo;
+        hi = next < hi ? (uint32_t)next : hi;
     }
+    return hi;
 }
 
-// Draws from the n entries of a list (all others of the row rank behind them
-// and are not kept).
+// Draws from the n <= 64 E entries of a list in index order, E l + e in lane l
+// (all others of the row rank behind them and are not kept).  top_k and top_p
+// end the run of kept entries after the first `ties`, by index, of those equal
+// to `cut`, found by halving the range of keys.
 template <int E>
-__device__ __forceinline__ void draw_lanes(const SampleArgs &a, int64_t b, const Row &r, const Weigh &wt,
+__device__ __forceinline__ void draw_lanes(const SampleArgs &a, int64_t b, const Row &r, const Weigh &wt, uint32_t top,
                                            const uint32_t (&key)[E], const int32_t (&j)[E], int n, int l) {
-    double w[E];
+    auto count_from = [&](uint32_t c) {
+        int m = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) m += __popcll(__ballot(key[e] >= c));
+        return m;
+    };
     uint64_t mass[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) mass[e] = key[e] ? wt.mass(key[e]) : 0;
+    uint32_t cut = 1;
+    int ties = n;
+    if (n > r.k) {
+        uint32_t lo = 1, hi = top;
+        int m = n;
+        while (lo < hi && m != (int)r.k) {
+            const uint32_t mid = lo + (hi - lo) / 2 + 1;
+            const int x = count_from(mid);
+            if (x >= (int)r.k) lo = mid, m = x;
+            else hi = mid - 1;
+        }
+        cut = lo;
+        if (m > r.k) ties = (int)r.k - (cut == top ? 0 : count_from(cut + 1));
+    }
     bool keep[E];
+    auto cut_ties = [&](uint32_t c, int most) {     // keep[] without the ties past `most`
+        int at = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        w[e] = key[e] ? wt.weight(key[e]) : 0.;
-        mass[e] = wt.mass_of(w[e]);
-        keep[e] = key[e] != 0;
-    }
-    if (r.k < n || r.p < 1.) {
-        int rank[E];
-        uint64_t before[E], sum = 0;
-        rank_lanes<E>(key, mass, n, l, rank, before);
+        for (int e = 0; e < E; ++e) at += below(__ballot(keep[e] && key[e] == c), l);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            keep[e] = keep[e] && rank[e] < r.k;
-            if (keep[e]) sum += mass[e];
+        for (int e = 0; e < E; ++e)
+            if (keep[e] && key[e] == c) keep[e] = at++ < most;
+    };
+#pragma unroll
+    for (int e = 0; e < E; ++e) keep[e] = key[e] >= cut;
+    if (ties < n) cut_ties(cut, ties);
+    if (r.p < 1.) {
+        uint64_t sum = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum += keep[e] ? mass[e] : 0;
+        const double goal = r.p * (double)wave_sum(sum);
+        // the smallest key over which less than the goal lies: its entries, or some of them, end the run
+        uint32_t lo = cut, hi = top;
+        uint64_t above = 0;                         // mass over hi
+        int in = 0, over = 0;                       // entries of [lo, hi], and over hi
+#pragma unroll
+        for (int e = 0; e < E; ++e) in += __popcll(__ballot(keep[e]));
+        while (lo < hi && in > 1) {
+            const uint32_t mid = lo + (hi - lo) / 2 + 1;
+            uint64_t m = 0;
+            int x = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const bool on = keep[e] && key[e] >= mid;
+                m += on ? mass[e] : 0;
+                x += __popcll(__ballot(on));
+            }
+            m = wave_sum(m);
+            if (x > 0 && (double)m >= goal) {
+                lo = mid;
+                in = x - over;
+            } else {
+                hi = mid - 1;
+                above = m;
+                in -= x - over;
+                over = x;
+            }
         }
-        if (r.p < 1.) {
-            const double goal = r.p * (double)wave_sum(sum);
+        // [lo, hi] holds entries of one key at most: it is theirs
+        uint32_t found = 0;
 #pragma unroll
-            for (int e = 0; e < E; ++e) keep[e] = keep[e] && (rank[e] == 0 || (double)before[e] < goal);
-        }
+        for (int e = 0; e < E; ++e)
+            if (keep[e] && key[e] >= lo && key[e] <= hi) found = key[e];
+        found = wave_max(found);
+        if (!found) found = lo;
+        const uint64_t one = wt.mass(found);
+        // as many of them as reach the goal, one at least
+        double need = one ? ceil((goal - (double)above) / (double)one) : 1.;
+        need = need < 1. ? 1. : need;
+#pragma unroll
+        for (int e = 0; e < E; ++e) keep[e] = keep[e] && key[e] >= found;
+        if (need < (double)n) cut_ties(found, (int)need);
     }
+    const uint32_t floor = r.least > 0. ? least_key(LOWEST, top, l, [&](uint32_t k) { return wt.weight(k) >= r.least; }) : 1;
     int kept = 0;
     uint64_t mine = 0;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        keep[e] = keep[e] && w[e] >= r.least;
+        keep[e] = keep[e] && key[e] >= floor;
         if (!keep[e]) mass[e] = 0;
         kept += __popcll(__ballot(keep[e]));
         mine += mass[e];
@@ -242,255 +320,111 @@ __device__ __forceinline__ void draw_lanes(const SampleArgs &a, int64_t b, const
     put(a, b, hit, hw, total, kept);
 }
 
-// A wave a row.  Lane l holds the entries 64 V q + V l + c, q < Q, c < V.
-template <typename T, int V, int Q>
+// A wave a row of up to 64 E places (E a multiple of 4, or 1).  The entries are
+// loaded in pieces of four a lane and handed over to lie E side by side in a
+// lane, so that lanes are in index order; what top_k leaves, if it fits, moves
+// on to lists of one or two entries a lane.
+template <typename T, int E>
 __global__ void __launch_bounds__(256) sample_wave_kernel(SampleArgs a) {
+    constexpr int V = E < 4 ? 1 : 4, Q = E / V, STEP = E + 1;       // (an odd step: 64 lanes on different banks)
     __shared__ double table[TABLE];
-    __shared__ uint2 list_of[4][128];
+    __shared__ uint32_t rows[4][E == 1 ? 1 : 64 * STEP];
     const int t = threadIdx.x, l = t & 63, wv = __builtin_amdgcn_readfirstlane(t >> 6);
     fill_table(table, t);
     __syncthreads();
     const int64_t b = (int64_t)blockIdx.x * 4 + wv;
     if (b >= a.B) return;
-    uint2 *const list = list_of[wv];
-    const int64_t M = a.M;
+    uint32_t *const lds = rows[wv];
     const T *const row = static_cast<const T *>(a.S) + b * a.lds;
-    uint32_t key[Q][V];
-    uint32_t top = 0;
+    const int skew = E == 1 ? 0 : skew_of(row);
+    uint32_t key[E], top = 0;
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
-        load_keys<T, V>(key[q], row, (64 * q + l) * V, M, a.vec);
+    for (int q = 0; q < Q; ++q) load_keys<T, V>(key + V * q, row, (64 * q + l) * V - skew, (uint32_t)a.M);
 #pragma unroll
-        for (int c = 0; c < V; ++c) top = max(top, key[q][c]);
-    }
+    for (int e = 0; e < E; ++e) top = max(top, key[e]);
     top = wave_max(top);
     if (!top) {
         if (l == 0) put(a, b, -1, 0, 0, 0);
         return;
     }
-    const Row r(a, b);
-    const Weigh wt{(double)value_of(top), r.c, a.shift, table};
-    if constexpr (V == 1 && Q == 1) {
-        const int32_t j[1] = {l};
-        draw_lanes<1>(a, b, r, wt, key[0], j, (int)M, l);
-        return;
-    }
-    auto count_from = [&](uint32_t c0) {
-        int n = 0;
+    if constexpr (E > 1) {
+        // place p = E x + y of lane x lies at STEP x + y
 #pragma unroll
         for (int q = 0; q < Q; ++q)
-#pragma unroll
-            for (int c = 0; c < V; ++c) n += __popcll(__ballot(key[q][c] >= c0));
-        return n;
-    };
-    // entries of [lo, hi] into the list, in index order; at most 128 of them
-    auto gather = [&](uint32_t lo, uint32_t hi) {
-        int n = 0;
-        wave_sync();
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            int at = n;
 #pragma unroll
             for (int c = 0; c < V; ++c) {
-                const uint64_t on = __ballot(key[q][c] >= lo && key[q][c] <= hi);
-                at += below(on, l);
-                n += __popcll(on);
+                const int p = (64 * q + l) * V + c;
+                lds[p / E * STEP + p % E] = key[V * q + c];
             }
-#pragma unroll
-            for (int c = 0; c < V; ++c)
-                if (key[q][c] >= lo && key[q][c] <= hi) list[at++] = make_uint2(key[q][c], (64 * q + l) * V + c);
-        }
         wave_sync();
-        return n;
-    };
-
-    // top_k: the largest cut with at least k entries from it on (cut is a key
-    // that entries have, or all the entries above cut - 1 are exactly k)
-    uint32_t cut = 1;
-    int n = count_from(1);
-    if (n > r.k) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) key[e] = lds[STEP * l + e];
+        wave_sync();
+    }
+    const Row r(a, b);
+    const Weigh wt(top, r.c, a.shift, table);
+    if constexpr (E > 2) {
+        // top_k's halving on whole rows, from the 64th largest or lower on: the least of the lanes' largest
+        uint32_t best = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) best = max(best, key[e]);
+        auto count_from = [&](uint32_t c) {
+            int m = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) m += __popcll(__ballot(key[e] >= c));
+            return m;
+        };
         uint32_t lo = 1, hi = top;
-        while (lo < hi && n != (int)r.k) {
-            const uint32_t mid = lo + (hi - lo) / 2 + 1;
-            const int m = count_from(mid);
-            if (m >= (int)r.k) lo = mid, n = m;
-            else hi = mid - 1;
+        int n = count_from(1);
+        if (n > r.k) {
+            if (r.k <= 64) {
+                lo = max(1u, ~wave_max(~best));
+                n = count_from(lo);
+            }
+            while (r.k <= 128 && lo < hi && n > 128) {
+                const uint32_t mid = lo + (hi - lo) / 2 + 1;
+                const int m = count_from(mid);
+                if (m >= (int)r.k) lo = mid, n = m;
+                else hi = mid - 1;
+            }
         }
-        cut = lo;
-    }
-    if (n <= 64) {
-        gather(cut, top);
-        const uint2 e = l < n ? list[l] : make_uint2(0, 0);
-        const uint32_t k[1] = {e.x};
-        const int32_t j[1] = {(int32_t)e.y};
-        draw_lanes<1>(a, b, r, wt, k, j, n, l);
-        return;
-    }
-    if (n <= 128) {
-        gather(cut, top);
-        uint32_t k[2];
-        int32_t j[2];
+        if (n <= 128) {
+            // entries from lo on, in index order: 16 bits of place are enough
+            int at = 0;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint2 x = 2 * l + e < n ? list[2 * l + e] : make_uint2(0, 0);
-            k[e] = x.x, j[e] = (int32_t)x.y;
-        }
-        draw_lanes<2>(a, b, r, wt, k, j, n, l);
-        return;
-    }
-    // more than 128 entries: of those equal to cut the first `ties` by index
-    int ties = n;
-    uint64_t mass[Q][V];
+            for (int e = 0; e < E; ++e) at += below(__ballot(key[e] >= lo), l);
 #pragma unroll
-    for (int q = 0; q < Q; ++q)
-#pragma unroll
-        for (int c = 0; c < V; ++c) {
-            const double w = key[q][c] >= cut && key[q][c] ? wt.weight(key[q][c]) : 0.;
-            mass[q][c] = wt.mass_of(w);
-        }
-    if (n > r.k) ties = (int)r.k - (cut == top ? 0 : count_from(cut + 1));
-    if (r.p < 1.) {
-        uint64_t all = 0;
-#pragma unroll
-        for (int q = 0; q < Q; ++q)
-#pragma unroll
-            for (int c = 0; c < V; ++c)
-                if (key[q][c] > cut) all += mass[q][c];
-        const uint64_t one = wt.mass(cut), above_cut = wave_sum(all);
-        const int equal = n - (cut == top ? 0 : count_from(cut + 1));
-        if (ties > equal) ties = equal;     // (a cut of 1 that no entry has)
-        const double goal = r.p * (double)(above_cut + (uint64_t)ties * one);
-        // the run ends among the keys of [lo, hi]; `above`: the mass over hi
-        uint32_t lo = cut, hi = top;
-        uint64_t above = 0;
-        int over = 0;                       // entries over hi
-        int in = n;                         // entries of [lo, hi]
-        while (lo < hi && in > 24) {
-            const uint32_t mid = lo + (hi - lo) / 2 + 1;
-            uint64_t s = 0;
-#pragma unroll
-            for (int q = 0; q < Q; ++q)
-#pragma unroll
-                for (int c = 0; c < V; ++c)
-                    if (key[q][c] >= mid) s += mass[q][c];
-            s = wave_sum(s);
-            const int m = count_from(mid);
-            if ((double)s >= goal && m > 0) {
-                lo = mid;
-                in = m - over;
+            for (int e = 0; e < E; ++e)
+                if (key[e] >= lo) {
+                    lds[at] = key[e];
+                    lds[128 + at++] = E * l + e - skew;
+                }
+            wave_sync();
+            if (n <= 64) {
+                const uint32_t k[1] = {l < n ? lds[l] : 0};
+                const int32_t j[1] = {l < n ? (int32_t)lds[128 + l] : 0};
+                draw_lanes<1>(a, b, r, wt, top, k, j, n, l);
             } else {
-                hi = mid - 1;
-                above = s;
-                in -= m - over;
-                over = m;
+                uint32_t k[2];
+                int32_t j[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const bool in = 2 * l + e < n;
+                    k[e] = in ? lds[2 * l + e] : 0;
+                    j[e] = in ? (int32_t)lds[128 + 2 * l + e] : 0;
+                }
+                draw_lanes<2>(a, b, r, wt, top, k, j, n, l);
             }
-        }
-        if (lo > cut) {
-            cut = lo;
-            ties = n;
-        }
-        if (in <= 64) {
-            gather(lo, hi);
-            const uint2 e = l < in ? list[l] : make_uint2(0, 0);
-            int rank[1];
-            uint64_t before[1];
-            const uint32_t k[1] = {e.x};
-            const uint64_t m[1] = {wt.mass(e.x)};
-            rank_lanes<1>(k, m, in, l, rank, before);
-            bool keep = e.x != 0 && ((rank[0] == 0 && over == 0) || (double)(above + before[0]) < goal);
-            if (e.x == cut) {               // top_k's ties
-                const uint64_t same = __ballot(keep && e.x == cut);
-                keep = keep && below(same, l) < ties;
-            }
-            // the last one kept ends the run; if none is, all of it is over hi
-            const uint64_t kb = __ballot(keep);
-            if (!kb) {
-                cut = hi == top ? top : hi + 1;
-                ties = n;
-            } else {
-                cut = ~wave_max(keep ? ~e.x : 0);
-                ties = __popcll(__ballot(keep && e.x == cut));
-            }
-        } else {                            // equal entries alone
-            const uint64_t w1 = wt.mass(lo);
-            double need = w1 ? ceil((goal - (double)above) / (double)w1) : 1.;
-            if (over == 0 && need < 1.) need = 1.;
-            if (need < 0.) need = 0.;
-            if (need < (double)ties) ties = (int)need;
-            cut = lo;
+            return;
         }
     }
-    // min_p: the smallest key that weighs enough (weights do not fall as keys rise)
-    uint32_t floor = 1;
-    if (r.least > 0.) {
-        uint32_t light = 0;
+    int32_t j[E];
 #pragma unroll
-        for (int q = 0; q < Q; ++q)
+    for (int e = 0; e < E; ++e) j[e] = E * l + e - skew;
+    int n = 0;
 #pragma unroll
-            for (int c = 0; c < V; ++c)
-                if (key[q][c] >= cut && key[q][c] > light && wt.weight(key[q][c]) < r.least) light = key[q][c];
-        floor = wave_max(light) + 1;
-    }
-    // the kept entries, block by block of 64 V: masses, and where the sum passes
-    uint64_t part[Q];
-    int kept = 0, seen = 0;
-    auto each = [&](int q, int &tie, auto use) {
-        int at = tie;
-#pragma unroll
-        for (int c = 0; c < V; ++c) {
-            const uint64_t on = __ballot(key[q][c] == cut);
-            at += below(on, l);
-            tie += __popcll(on);
-        }
-#pragma unroll
-        for (int c = 0; c < V; ++c) {
-            const uint32_t x = key[q][c];
-            if (!x || x < cut) continue;
-            if (x == cut && at++ >= ties) continue;
-            if (x >= floor) use(c, mass[q][c]);
-        }
-    };
-    uint64_t total = 0;
-#pragma unroll
-    for (int q = 0; q < Q; ++q) {
-        uint64_t s = 0;
-        each(q, seen, [&](int, uint64_t w) { s += w, ++kept; });
-        part[q] = wave_sum(s);
-        total += part[q];
-    }
-    kept = (int)wave_sum(kept);
-    const double goal = goal_of(a.u[b], total);
-    uint64_t base = 0;
-    seen = 0;
-    bool done = false;
-#pragma unroll
-    for (int q = 0; q < Q; ++q) {
-        const bool last = base + part[q] == total && part[q];
-        if (!done && part[q] && ((double)(base + part[q]) > goal || last)) {
-            done = true;
-            int tie = seen;
-            uint64_t mine = 0;
-            each(q, tie, [&](int, uint64_t w) { mine += w; });
-            const uint64_t upto = wave_upto(mine);
-            const uint64_t has = __ballot(mine != 0), past = __ballot(mine != 0 && (double)(base + upto) > goal);
-            const int at = past ? __ffsll((unsigned long long)past) - 1 : 63 - __clzll(has);
-            uint64_t sum = base + upto - mine, hw = 0;
-            int hit = -1, end = -1;
-            uint64_t ew = 0;
-            tie = seen;
-            each(q, tie, [&](int c, uint64_t w) {
-                if (!w) return;
-                sum += w;
-                end = c, ew = w;
-                if (hit < 0 && (double)sum > goal) hit = c, hw = w;
-            });
-            if (hit < 0) hit = end, hw = ew;
-            if (l == at) put(a, b, (64 * q + l) * V + hit, hw, total, kept);
-        }
-        base += part[q];
-#pragma unroll
-        for (int c = 0; c < V; ++c) seen += __popcll(__ballot(key[q][c] == cut));
-    }
+    for (int e = 0; e < E; ++e) n += __popcll(__ballot(key[e] != 0));
+    draw_lanes<E>(a, b, r, wt, top, key, j, n, l);
 }
 
 // ------------------------------------------------------------- a thread a row
@@ -518,14 +452,13 @@ __global__ void __launch_bounds__(64) sample_thread_kernel(SampleArgs a) {
         return;
     }
     const Row r(a, b);
-    const Weigh wt{(double)value_of(top), r.c, a.shift, table};
+    const Weigh wt(top, r.c, a.shift, table);
     uint64_t mass[P];
     uint32_t light = 0;                     // entries below min_p
 #pragma unroll
     for (int j = 0; j < P; ++j) {
-        const double w = key[j] ? wt.weight(key[j]) : 0.;
-        mass[j] = wt.mass_of(w);
-        if (w < r.least) light |= 1u << j;
+        mass[j] = key[j] ? wt.mass(key[j]) : 0;
+        if (r.least > 0. && key[j] && wt.weight(key[j]) < r.least) light |= 1u << j;
     }
     uint32_t keep = ~0u;
     if (r.k < M || r.p < 1.) {
@@ -590,7 +523,8 @@ __global__ void __launch_bounds__(64) sample_thread_kernel(SampleArgs a) {
 
 // ---------------------------------------------------- work-groups of 256 a row
 
-constexpr int NT = 256, Q = 8, CHUNK = NT * 4 * Q, BINS = 2048, CAP = 1024, MORE = 256;
+constexpr int NT = 256, Q = 8, CHUNK = NT * 4 * Q, BINS = 2048, CAP = 1024;
+constexpr uint32_t LAST = 0x7fffffff;       // an index behind every entry
 
 struct Block {
     uint64_t tmp[NT / 64];
@@ -630,8 +564,8 @@ struct Block {
 // above e^-32) if that is less; the last one takes the rest.
 struct Binning {
     float m, scale;
-    __device__ __forceinline__ Binning(float top, float low, float temp) : m(top) {
-        const float range = fminf(top - low, 32.f * temp);
+    __device__ __forceinline__ Binning(uint32_t top, uint32_t low, float temp) : m(value_of(top)) {
+        const float range = fminf(m - value_of(low), 32.f * temp);
         scale = (float)BINS / range;
     }
     __device__ __forceinline__ int bin(uint32_t key) const {
@@ -642,16 +576,18 @@ struct Binning {
     }
 };
 
-// Where the run of kept entries ends, as far as the histogram tells: bins below
-// `sure` are kept; the entries of the bins lo..hi (top_p), and of bin bk
-// (top_k), have to be ranked.
+// Where the run of kept entries ends, as far as the histogram tells.  Keys from
+// `sure` on are kept; those of [p_lo, p_hi] (the bins top_p may end in) and of
+// [k_lo, k_hi] (the bin top_k ends in) have to be ranked.  An empty range asks
+// for nothing.
 struct Plan {
-    int lo, hi, bk;             // bk = BINS: top_k keeps all; lo..hi empty: top_p does
-    uint64_t mass_lo, mass_k, all;      // mass below bin lo / below bk; mass of all entries
-    uint32_t count_lo, count_k;         // entries below bin lo / below bk
+    uint32_t sure, p_lo, p_hi, k_lo, k_hi;
     uint32_t listed;            // entries to rank
-    __device__ __forceinline__ int sure() const { return lo <= hi ? lo : bk; }
-    __device__ __forceinline__ bool asks(int bin) const { return (bin >= lo && bin <= hi) || bin == bk; }
+    uint64_t mass_p, mass_k, all;       // mass over p_hi, over k_hi, of all entries
+    uint64_t count_k;                   // entries over k_hi
+    __device__ __forceinline__ bool in_p(uint32_t x) const { return x >= p_lo && x <= p_hi; }
+    __device__ __forceinline__ bool in_k(uint32_t x) const { return x >= k_lo && x <= k_hi; }
+    __device__ __forceinline__ bool asks(uint32_t x) const { return in_p(x) || in_k(x); }
 };
 
 // The end of the run: entries over `key`, and those equal to it up to index j.
@@ -659,18 +595,19 @@ struct End {
     uint32_t key, j;
     __device__ __forceinline__ bool has(uint32_t x, uint32_t i) const { return x > key || (x == key && x && i <= j); }
 };
+constexpr End NO_END = {1, LAST};
 
 struct Hist {
     uint32_t count[BINS];
     uint64_t mass[BINS];
 };
 
-// Workspace of a row that several work-groups share.
+// Workspace of a row that several work-groups share; chunks x ChunkSpace follow.
 struct RowSpace {
     Hist hist;
-    uint32_t listed, pad;
+    Plan plan;
+    uint32_t listed, floor;     // entries listed; the smallest key that min_p keeps
     uint64_t list[CAP];
-    // then chunks x { mass u64, count u32, top u32, low u32, pad u32 }
 };
 struct ChunkSpace {
     uint64_t mass;
@@ -685,21 +622,20 @@ struct Shared {
     uint64_t list[CAP];
     Plan plan;
     End end;
-    uint32_t n, flag;
-    uint64_t found, total, base;
-    uint64_t part[NT / 64][Q];
-    uint64_t more[MORE];        // masses of listed entries by chunk
+    uint32_t n, bins[4], floor;
+    uint64_t base;
+    uint64_t part[NT / 64 * Q];
 };
 
 template <typename T> struct Chunk {
     uint32_t key[Q][4];
-    uint32_t j0;
-    __device__ __forceinline__ uint32_t at(int q, int c) const { return j0 + (NT * q + threadIdx.x) * 4 + c; }
+    int32_t j0;                 // index of the first place
+    __device__ __forceinline__ uint32_t at(int q, int c) const { return (uint32_t)(j0 + (int)(NT * q + threadIdx.x) * 4 + c); }
     __device__ __forceinline__ void load(const SampleArgs &a, int64_t b, int chunk) {
-        j0 = (uint32_t)chunk * CHUNK;
         const T *const row = static_cast<const T *>(a.S) + b * a.lds;
+        j0 = (int32_t)((uint32_t)chunk * CHUNK - (uint32_t)skew_of(row));
 #pragma unroll
-        for (int q = 0; q < Q; ++q) load_keys<T, 4>(key[q], row, at(q, 0), a.M, a.vec);
+        for (int q = 0; q < Q; ++q) load_keys<T, 4>(key[q], row, (int32_t)at(q, 0), (uint32_t)a.M);
     }
     template <typename F> __device__ __forceinline__ void each(F f) const {
 #pragma unroll
@@ -708,69 +644,96 @@ template <typename T> struct Chunk {
             for (int c = 0; c < 4; ++c)
                 if (key[q][c]) f(key[q][c], q, c);
     }
+    // largest key, and the complement of the smallest, of this thread's entries
+    __device__ __forceinline__ void range(uint32_t &top, uint32_t &low) const {
+        top = 0, low = 0;
+        each([&](uint32_t x, int, int) { top = max(top, x), low = max(low, ~x); });
+    }
 };
 
 __device__ __forceinline__ void clear(Hist &h) {
     for (int i = threadIdx.x; i < BINS; i += NT) h.count[i] = 0, h.mass[i] = 0;
 }
 
-// Reads the plan off the histogram (masses are there if top_p or min_p asks).
-__device__ __forceinline__ void make_plan(Shared &sh, const Row &r, int64_t M) {
+// The smallest key that min_p keeps.
+__device__ __forceinline__ uint32_t floor_of(const Row &r, const Weigh &wt, uint32_t top) {
+    if (!(r.least > 0.)) return 1;
+    return least_key(LOWEST, top, threadIdx.x & 63, [&](uint32_t k) { return wt.weight(k) >= r.least; });
+}
+
+// Reads the plan off the histogram (which holds counts where top_k asks, masses
+// where top_p does).
+__device__ __forceinline__ void make_plan(Shared &sh, const Row &r, const Binning &bins, uint32_t top) {
     constexpr int PER = BINS / NT;
-    const int t = threadIdx.x, i0 = t * PER;
+    const int t = threadIdx.x, w = t >> 6, l = t & 63, i0 = t * PER;
     Hist &h = sh.hist;
-    uint64_t n = 0, w = 0, all_n, all_w;
-    for (int i = i0; i < i0 + PER; ++i) n += h.count[i], w += h.mass[i];
-    const uint64_t n0 = sh.block.before(n, &all_n), w0 = sh.block.before(w, &all_w);
-    if (t == 0) {
-        sh.plan = Plan{1, 0, BINS, 0, 0, all_w, 0, 0, 0};
-    }
+    uint64_t n = 0, m = 0, all_n, all_m;
+    for (int i = i0; i < i0 + PER; ++i) n += h.count[i], m += h.mass[i];
+    const uint64_t n0 = sh.block.before(n, &all_n), m0 = sh.block.before(m, &all_m);
+    // bins 0: top_k's; 1, 2: the first and last that top_p may end in; BINS: none
+    if (t < 4) sh.bins[t] = BINS;
+    if (t == 0) sh.plan = Plan{1, 1, 0, 1, 0, 0, 0, 0, all_m, 0};
     __syncthreads();
     const bool by_k = (uint64_t)r.k < all_n, by_p = r.p < 1.;
     if (by_k) {
-        uint64_t c = n0, m = w0;
+        uint64_t c = n0, x = m0;
         for (int i = i0; i < i0 + PER; ++i) {
             if (c < (uint64_t)r.k && c + h.count[i] >= (uint64_t)r.k) {
-                sh.plan.bk = i;
-                sh.plan.count_k = (uint32_t)c;
-                sh.plan.mass_k = m;
+                sh.bins[0] = i;
+                sh.plan.count_k = c;
+                sh.plan.mass_k = x;
             }
-            c += h.count[i], m += h.mass[i];
+            c += h.count[i], x += h.mass[i];
         }
     }
     __syncthreads();
     if (by_p) {
-        // top_k leaves between mass_k and mass_k + the mass of bin bk
-        const double least = r.p * (double)(by_k ? sh.plan.mass_k : all_w);
-        const double most = r.p * (double)(by_k ? sh.plan.mass_k + h.mass[sh.plan.bk] : all_w);
-        uint64_t c = n0, m = w0;
+        // top_k leaves between mass_k and mass_k + the mass of its bin
+        const double least = r.p * (double)(by_k ? sh.plan.mass_k : all_m);
+        const double most = r.p * (double)(by_k ? sh.plan.mass_k + h.mass[sh.bins[0]] : all_m);
+        uint64_t x = m0;
         for (int i = i0; i < i0 + PER; ++i) {
-            const uint64_t m1 = m + h.mass[i];
-            if (h.count[i]) {
-                // the first bin whose sum reaches: (an empty row has been dealt with)
-                const bool start = c == 0;
-                if ((start || (double)m < least) && (double)m1 >= least) {
-                    sh.plan.lo = i;
-                    sh.plan.count_lo = (uint32_t)c;
-                    sh.plan.mass_lo = m;
+            const uint64_t y = x + h.mass[i];
+            if (y > x) {        // the first bin whose sum reaches (the largest score's, if that is no more than 0)
+                if ((x == 0 || (double)x < least) && (double)y >= least) {
+                    sh.bins[1] = i;
+                    sh.plan.mass_p = x;
                 }
-                if ((start || (double)m < most) && (double)m1 >= most) sh.plan.hi = i;
+                if ((x == 0 || (double)x < most) && (double)y >= most) sh.bins[2] = i;
             }
-            c += h.count[i], m = m1;
+            x = y;
         }
     }
     __syncthreads();
-    uint64_t ask = 0;
-    for (int i = i0; i < i0 + PER; ++i)
-        if (sh.plan.asks(i)) ask += h.count[i];
-    ask = sh.block.sum(ask);
-    if (t == 0) sh.plan.listed = (uint32_t)ask;
+    // the keys at the bins' edges, one a wave: the smallest key of a bin or of a smaller one
+    const int k = (int)sh.bins[0], p1 = (int)sh.bins[1], p2 = (int)sh.bins[2];
+    const int edge = w == 0 ? k : (w == 1 ? k - 1 : (w == 2 ? p2 : p1 - 1));
+    const bool ask = w < 2 ? k < BINS : p1 < BINS;
+    uint32_t key = 0;
+    if (ask) key = edge < 0 ? top + 1 : least_key(LOWEST, top, l, [&](uint32_t x) { return bins.bin(x) <= edge; });
+    if (l == 0 && ask) {
+        if (w == 0) sh.plan.k_lo = key;
+        if (w == 1) sh.plan.k_hi = key - 1;
+        if (w == 2) sh.plan.p_lo = key;
+        if (w == 3) sh.plan.p_hi = key - 1;
+    }
+    uint64_t listed = 0;
+    if (by_k) {
+        for (int i = i0; i < i0 + PER; ++i)
+            if (i == k || (i >= p1 && i <= p2)) listed += h.count[i];
+    }
+    listed = sh.block.sum(listed);
+    if (t == 0) {
+        Plan &p = sh.plan;
+        p.sure = p1 < BINS ? p.p_hi + 1 : (k < BINS ? p.k_hi + 1 : 1);
+        p.listed = (uint32_t)(listed < CAP + 1 ? listed : CAP + 1);     // (without top_k: counted as they are listed)
+    }
     __syncthreads();
 }
 
-// Ranks the listed entries (at most CAP, in sh.list as ~key, index) and finds
-// the end of the run.
-__device__ __forceinline__ void rank_list(Shared &sh, const Row &r, const Weigh &wt, const Binning &bins, int n) {
+// Ranks the listed entries (n <= CAP, in sh.list as ~key, index) and finds the
+// end of the run.
+__device__ __forceinline__ void rank_list(Shared &sh, const Row &r, const Weigh &wt, int n) {
     const int t = threadIdx.x;
     int size = 64;
     while (size < n) size *= 2;
@@ -786,55 +749,49 @@ __device__ __forceinline__ void rank_list(Shared &sh, const Row &r, const Weigh 
             __syncthreads();
         }
     constexpr int PER = CAP / NT;
-    const Plan &p = sh.plan;
+    const Plan p = sh.plan;
     uint32_t key[PER];
     uint64_t mass[PER], of_k = 0, of_p = 0, all;
-    int bin[PER], first_k = 0;
+    int first_k = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int x = t * PER + i;
         key[i] = x < n ? ~(uint32_t)(sh.list[x] >> 32) : 0;
-        bin[i] = key[i] ? bins.bin(key[i]) : -1;
-        mass[i] = wt.mass(key[i]);
-        if (key[i] && bin[i] >= p.lo && bin[i] <= p.hi) of_p += mass[i];
-        if (key[i] && bin[i] < p.bk) ++first_k;
+        mass[i] = key[i] && r.p < 1. ? wt.mass(key[i]) : 0;
+        if (p.in_p(key[i])) of_p += mass[i];
+        if (key[i] && !(p.k_lo <= p.k_hi && key[i] <= p.k_hi)) ++first_k;
     }
-    // listed entries below bin bk come first
+    // listed entries over top_k's bin come first
     const int start_k = (int)sh.block.sum(first_k);
     uint32_t keep = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int x = t * PER + i;
         if (!key[i]) continue;
-        if (bin[i] < p.bk || (uint64_t)(x - start_k) + p.count_k < (uint64_t)r.k) {
+        if (!p.in_k(key[i]) || (uint64_t)(t * PER + i - start_k) + p.count_k < (uint64_t)r.k) {
             keep |= 1u << i;
-            if (bin[i] == p.bk) of_k += mass[i];
+            if (p.in_k(key[i])) of_k += mass[i];
         }
     }
     if (r.p < 1.) {
         of_k = sh.block.sum(of_k);
-        const double goal = r.p * (double)(p.bk < BINS ? p.mass_k + of_k : p.all);
-        uint64_t m = p.mass_lo + sh.block.before(of_p, &all);
+        const double goal = r.p * (double)(p.k_lo <= p.k_hi ? p.mass_k + of_k : p.all);
+        const uint64_t of = sh.block.before(of_p, &all);
+        uint64_t m = p.mass_p + of;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             if (!key[i]) continue;
-            const bool in = bin[i] >= p.lo && bin[i] <= p.hi;
-            const bool first = t == 0 && i == 0 && p.count_lo == 0;
-            if (!in || !(first || (double)m < goal)) keep &= ~(1u << i);
-            if (in) m += mass[i];
+            if (!p.in_p(key[i]) || !(m == 0 || (double)m < goal)) keep &= ~(1u << i);
+            if (p.in_p(key[i])) m += mass[i];
         }
     }
-    // the last one kept (its rank + 1; none: everything below bin `sure`)
+    // the last one kept (its place + 1)
     uint32_t last = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i)
         if ((keep >> i) & 1) last = t * PER + i + 1;
     last = sh.block.most(last);
     if (t == 0) {
-        if (last) {
-            sh.end.key = ~(uint32_t)(sh.list[last - 1] >> 32);
-            sh.end.j = (uint32_t)sh.list[last - 1];
-        }
+        sh.end = last ? End{~(uint32_t)(sh.list[last - 1] >> 32), (uint32_t)sh.list[last - 1]} : End{p.sure, LAST};
         sh.n = last;
     }
     __syncthreads();
@@ -855,9 +812,9 @@ __device__ __forceinline__ void end_by_passes(Shared &sh, const SampleArgs &a, i
         }
     };
     // the largest key from which on at least `goal` (entries, or mass) lies, not
-    // below `floor`; *above: what lies over it
-    auto find = [&](uint32_t floor, double goal, bool by_mass, uint64_t *above) {
-        uint32_t lo = floor, hi = top;
+    // below `from`; *above: what lies over it
+    auto find = [&](uint32_t from, double goal, bool by_mass, uint64_t *above) {
+        uint32_t lo = from, hi = top;
         *above = 0;
         while (lo < hi) {
             const uint64_t step = ((uint64_t)hi - lo + BINS) / BINS;
@@ -909,14 +866,14 @@ __device__ __forceinline__ void end_by_passes(Shared &sh, const SampleArgs &a, i
         const double goal = r.p * (double)all_mass;
         const uint32_t at = find(cut, goal, true, &above);
         if (at > cut) cut = at, ties = (uint64_t)a.M;
-        const uint64_t one = wt.mass(cut);
+        const uint64_t one = cut > 1 ? wt.mass(cut) : 0;
         double n = one ? ceil((goal - (double)above) / (double)one) : 1.;
         if (n < 1.) n = 1.;
         if (n < (double)ties) ties = (uint64_t)n;
     }
     // index of the last tie kept
     uint64_t seen = 0;
-    if (t == 0) sh.end = End{cut, 0xffffffffu};
+    if (t == 0) sh.end = End{cut, LAST};
     __syncthreads();
     if (ties < (uint64_t)a.M) {
         for (int64_t j0 = 0; j0 < a.M && seen < ties; j0 += NT) {
@@ -931,32 +888,27 @@ __device__ __forceinline__ void end_by_passes(Shared &sh, const SampleArgs &a, i
     __syncthreads();
 }
 
-// Mass and number of a chunk's kept entries.
+// Mass and number of the entries of a chunk that `has` keeps.
 template <typename T, typename F>
-__device__ __forceinline__ void chunk_sums(Shared &sh, const Chunk<T> &ch, const Row &r, const Weigh &wt, F has,
-                                           uint64_t *mass, uint64_t *count) {
+__device__ __forceinline__ void chunk_sums(Block &block, const Chunk<T> &ch, const Weigh &wt, F has, uint64_t *mass,
+                                           uint64_t *count) {
     uint64_t m = 0, n = 0;
     ch.each([&](uint32_t x, int q, int c) {
-        if (!has(x, ch.at(q, c))) return;
-        const double w = wt.weight(x);
-        if (w >= r.least) m += wt.mass_of(w), ++n;
+        if (has(x, ch.at(q, c))) m += wt.mass(x), ++n;
     });
-    *mass = sh.block.sum(m);
-    *count = sh.block.sum(n);
+    *mass = block.sum(m);
+    *count = block.sum(n);
 }
 
 // Draws from a chunk: `base` is the mass of the chunks before it, and the sum
 // passes the goal in it (or it is the last with a mass).
 template <typename T>
-__device__ __forceinline__ void draw_chunk(Shared &sh, const SampleArgs &a, int64_t b, const Chunk<T> &ch, const Row &r,
-                                           const Weigh &wt, End end, uint64_t base, uint64_t total, uint64_t kept,
-                                           double goal) {
+__device__ __forceinline__ void draw_chunk(Shared &sh, const SampleArgs &a, int64_t b, const Chunk<T> &ch, const Weigh &wt,
+                                           End end, uint32_t floor, uint64_t base, uint64_t total, uint64_t kept, double goal) {
     const int t = threadIdx.x, l = t & 63, w = t >> 6;
     auto mass_at = [&](int q, int c) -> uint64_t {
         const uint32_t x = ch.key[q][c];
-        if (!x || !end.has(x, ch.at(q, c))) return 0;
-        const double v = wt.weight(x);
-        return v >= r.least ? wt.mass_of(v) : 0;
+        return x && x >= floor && end.has(x, ch.at(q, c)) ? wt.mass(x) : 0;
     };
     uint64_t mine[Q];
 #pragma unroll
@@ -965,24 +917,17 @@ __device__ __forceinline__ void draw_chunk(Shared &sh, const SampleArgs &a, int6
 #pragma unroll
         for (int c = 0; c < 4; ++c) mine[q] += mass_at(q, c);
         const uint64_t s = wave_sum(mine[q]);
-        if (l == 0) sh.part[w][q] = s;
+        if (l == 0) sh.part[q * (NT / 64) + w] = s;
     }
-    if (t == 0) sh.found = ~0ull, sh.base = 0;
     __syncthreads();
-    // the wave and block of 256 entries in which the sum passes, in index order
-    uint64_t run = base;
-    int at_q = -1, at_w = -1, end_q = -1, end_w = -1;
-    uint64_t at_base = 0, end_base = 0;
-    for (int q = 0; q < Q; ++q)
-        for (int v = 0; v < NT / 64; ++v) {
-            const uint64_t s = sh.part[v][q];
-            if (!s) continue;
-            end_q = q, end_w = v, end_base = run;
-            if (at_q < 0 && (double)(run + s) > goal) at_q = q, at_w = v, at_base = run;
-            run += s;
-        }
-    if (at_q < 0) at_q = end_q, at_w = end_w, at_base = end_base;
-    if (w != at_w) return;
+    // the block of 256 places in which the sum passes, in index order
+    const uint64_t part = l < NT / 64 * Q ? sh.part[l] : 0;
+    const uint64_t sums = base + wave_upto(part);
+    const uint64_t some = __ballot(part != 0), over = __ballot(part != 0 && (double)sums > goal);
+    const int at = over ? __ffsll((unsigned long long)over) - 1 : 63 - __clzll(some);
+    const int at_q = at / (NT / 64);
+    if (w != at % (NT / 64)) return;
+    const uint64_t at_base = read_lane64(sums - part, at);
     uint64_t sum = 0;
 #pragma unroll
     for (int q = 0; q < Q; ++q)
@@ -1009,17 +954,29 @@ __device__ __forceinline__ void draw_chunk(Shared &sh, const SampleArgs &a, int6
     put(a, b, hit, hw, total, kept);
 }
 
+// The first of the largest entries, which temperature 0 and top_k 1 take.
 template <typename T>
-__device__ __forceinline__ void count_bins(Shared &sh, const Chunk<T> &ch, const Row &r, const Weigh &wt, const Binning &bins) {
+__device__ __forceinline__ void draw_first(Shared &sh, const SampleArgs &a, int64_t b, const Chunk<T> &ch, uint32_t top) {
+    uint32_t mine = 0;          // complement of the index: the largest is the first
+    ch.each([&](uint32_t x, int q, int c) {
+        if (x == top) mine = max(mine, ~ch.at(q, c));
+    });
+    mine = sh.block.most(mine);
+    if (threadIdx.x == 0) put(a, b, (int32_t)~mine, 1, 1, 1);
+}
+
+template <typename T>
+__device__ __forceinline__ void count_bins(Hist &h, const Chunk<T> &ch, const Row &r, const Weigh &wt, const Binning &bins,
+                                           bool by_k) {
     const bool by_p = r.p < 1.;
     ch.each([&](uint32_t x, int, int) {
         const int i = bins.bin(x);
-        atomicAdd(&sh.hist.count[i], 1u);
-        if (by_p) atomicAdd((unsigned long long *)&sh.hist.mass[i], (unsigned long long)wt.mass(x));
+        if (by_k) atomicAdd(&h.count[i], 1u);
+        if (by_p) atomicAdd((unsigned long long *)&h.mass[i], (unsigned long long)wt.mass(x));
     });
 }
 
-// A work-group a row, up to CHUNK entries.
+// A work-group a row, up to CHUNK places.
 template <typename T>
 __global__ void __launch_bounds__(NT) sample_group_kernel(SampleArgs a) {
     __shared__ Shared sh;
@@ -1029,8 +986,8 @@ __global__ void __launch_bounds__(NT) sample_group_kernel(SampleArgs a) {
     clear(sh.hist);
     Chunk<T> ch;
     ch.load(a, b, 0);
-    uint32_t top = 0, low = 0;
-    ch.each([&](uint32_t x, int, int) { top = max(top, x), low = max(low, ~x); });
+    uint32_t top, low;
+    ch.range(top, low);
     top = sh.block.most(top);
     low = ~sh.block.most(low);
     if (!top) {
@@ -1038,32 +995,42 @@ __global__ void __launch_bounds__(NT) sample_group_kernel(SampleArgs a) {
         return;
     }
     const Row r(a, b);
-    const Weigh wt{(double)value_of(top), r.c, a.shift, sh.table};
-    End end{1, 0xffffffffu};
-    if (r.k < a.M || r.p < 1.) {
-        const Binning bins(value_of(top), value_of(low), r.temp);
-        count_bins(sh, ch, r, wt, bins);
+    if (r.takes_first()) {
+        draw_first(sh, a, b, ch, top);
+        return;
+    }
+    const Weigh wt(top, r.c, a.shift, sh.table);
+    End end = NO_END;
+    if (!r.keeps_all(a.M)) {
+        const Binning bins(top, low, r.temp);
+        count_bins(sh.hist, ch, r, wt, bins, r.k < a.M);
+        if (t == 0) sh.n = 0;
         __syncthreads();
-        make_plan(sh, r, a.M);
+        make_plan(sh, r, bins, top);
         const Plan p = sh.plan;
-        if (p.listed > CAP) {
-            end_by_passes<T>(sh, a, b, r, wt, top);
-            end = sh.end;
-        } else if (p.lo <= p.hi || p.bk < BINS) {
-            if (t == 0) sh.n = 0;
-            __syncthreads();
+        uint32_t listed = p.listed;
+        if (listed <= CAP) {
             ch.each([&](uint32_t x, int q, int c) {
-                if (p.asks(bins.bin(x))) sh.list[atomicAdd(&sh.n, 1u)] = (uint64_t)~x << 32 | ch.at(q, c);
+                if (!p.asks(x)) return;
+                const uint32_t at = atomicAdd(&sh.n, 1u);
+                if (at < CAP) sh.list[at] = (uint64_t)~x << 32 | ch.at(q, c);
             });
             __syncthreads();
-            rank_list(sh, r, wt, bins, (int)p.listed);
+            listed = sh.n;
+            __syncthreads();
+        }
+        if (listed > CAP) {
+            end_by_passes<T>(sh, a, b, r, wt, top);
             end = sh.end;
-            if (!sh.n) end = End{0xffffffffu, 0};       // (not reached: the run ends in a listed bin)
+        } else if (listed) {
+            rank_list(sh, r, wt, (int)listed);
+            end = sh.end;
         }
     }
+    const uint32_t floor = floor_of(r, wt, top);
     uint64_t total, kept;
-    chunk_sums(sh, ch, r, wt, [&](uint32_t x, uint32_t j) { return end.has(x, j); }, &total, &kept);
-    draw_chunk(sh, a, b, ch, r, wt, end, 0, total, kept, goal_of(a.u[b], total));
+    chunk_sums(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); }, &total, &kept);
+    draw_chunk(sh, a, b, ch, wt, end, floor, 0, total, kept, goal_of(a.u[b], total));
 }
 
 __device__ __forceinline__ RowSpace *row_space(const SampleArgs &a, int64_t slot) {
@@ -1082,131 +1049,143 @@ __global__ void __launch_bounds__(NT) sample_top_kernel(SampleArgs a) {
     if (chunk == 0 && t == 0) rs->listed = 0;
     Chunk<T> ch;
     ch.load(a, b, chunk);
-    uint32_t top = 0, low = 0;
-    ch.each([&](uint32_t x, int, int) { top = max(top, x), low = max(low, ~x); });
+    uint32_t top, low;
+    ch.range(top, low);
     top = block.most(top);
     low = ~block.most(low);
     if (t == 0) chunk_space(rs)[chunk].top = top, chunk_space(rs)[chunk].low = low;
 }
 
 // The row's largest and smallest key from the chunks' ones.
-__device__ __forceinline__ void row_range(Shared &sh, const SampleArgs &a, const ChunkSpace *cs, uint32_t &top, uint32_t &low) {
+__device__ __forceinline__ void row_range(Block &block, const SampleArgs &a, const ChunkSpace *cs, uint32_t &top, uint32_t &low) {
     top = 0;
     low = 0;
     for (int i = threadIdx.x; i < a.chunks; i += NT) top = max(top, cs[i].top), low = max(low, ~cs[i].low);
-    top = sh.block.most(top);
-    low = ~sh.block.most(low);
-}
-
-// Draws once the end of the run is known: every chunk's mass is in cs, but for
-// the masses `more` of listed entries.
-template <typename T>
-__device__ __forceinline__ void draw_row(Shared &sh, const SampleArgs &a, int64_t b, const ChunkSpace *cs, const Row &r,
-                                         const Weigh &wt, End end, uint64_t more_count) {
-    const int t = threadIdx.x;
-    auto mass_of = [&](int i) { return i < a.chunks ? cs[i].mass + (i < MORE ? sh.more[i] : 0) : 0; };
-    uint64_t n = 0, m = 0;
-    for (int i = t; i < a.chunks; i += NT) n += cs[i].count, m += mass_of(i);
-    const uint64_t kept = sh.block.sum(n) + more_count, total = sh.block.sum(m);
-    const double goal = goal_of(a.u[b], total);
-    // the chunk in which the sum passes, in index order; the last with a mass where none does
-    if (t == 0) sh.found = ~0ull, sh.n = 0;
-    __syncthreads();
-    uint64_t base = 0;
-    for (int i0 = 0; i0 < a.chunks; i0 += NT) {
-        const uint64_t c = mass_of(i0 + t);
-        uint64_t all;
-        const uint64_t before = base + sh.block.before(c, &all);
-        if (c) {
-            atomicMax(&sh.n, (uint32_t)(i0 + t));
-            if ((double)(before + c) > goal) atomicMin((unsigned long long *)&sh.found, (unsigned long long)(i0 + t));
-        }
-        base += all;
-    }
-    __syncthreads();
-    const int at = sh.found == ~0ull ? (int)sh.n : (int)sh.found;
-    base = 0;
-    for (int i = t; i < at; i += NT) base += mass_of(i);
-    base = sh.block.sum(base);
-    Chunk<T> ch;
-    ch.load(a, b, at);
-    draw_chunk(sh, a, b, ch, r, wt, end, base, total, kept, goal);
+    top = block.most(top);
+    low = ~block.most(low);
 }
 
 // Launch 2: the histogram of the row; for rows without top_k and top_p the
 // chunk's mass.
 template <typename T>
 __global__ void __launch_bounds__(NT) sample_bins_kernel(SampleArgs a) {
-    __shared__ Shared sh;
+    __shared__ Block block;
+    __shared__ double table[TABLE];
+    __shared__ Hist hist;
     const int t = threadIdx.x, chunk = blockIdx.x % a.chunks;
     const int64_t slot = blockIdx.x / a.chunks, b = a.row0 + slot;
+    const Row r(a, b);
+    if (r.takes_first()) return;
     RowSpace *const rs = row_space(a, slot);
     ChunkSpace *const cs = chunk_space(rs);
-    fill_table(sh.table, t);
-    clear(sh.hist);
     Chunk<T> ch;
     ch.load(a, b, chunk);
+    fill_table(table, t);
+    clear(hist);
     uint32_t top, low;
-    row_range(sh, a, cs, top, low);
+    row_range(block, a, cs, top, low);
     if (!top) return;
-    const Row r(a, b);
-    const Weigh wt{(double)value_of(top), r.c, a.shift, sh.table};
+    const Weigh wt(top, r.c, a.shift, table);
     if (r.keeps_all(a.M)) {
+        const uint32_t floor = floor_of(r, wt, top);
         uint64_t m, n;
-        chunk_sums(sh, ch, r, wt, [](uint32_t, uint32_t) { return true; }, &m, &n);
+        chunk_sums(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= floor; }, &m, &n);
         if (t == 0) cs[chunk].mass = m, cs[chunk].count = (uint32_t)n;
         return;
     }
-    const Binning bins(value_of(top), value_of(low), r.temp);
-    count_bins(sh, ch, r, wt, bins);
+    const bool by_k = r.k < a.M;
+    count_bins(hist, ch, r, wt, Binning(top, low, r.temp), by_k);
     __syncthreads();
     for (int i = t; i < BINS; i += NT) {
-        if (!sh.hist.count[i]) continue;
-        atomicAdd(&rs->hist.count[i], sh.hist.count[i]);
-        if (sh.hist.mass[i]) atomicAdd((unsigned long long *)&rs->hist.mass[i], (unsigned long long)sh.hist.mass[i]);
+        if (by_k && hist.count[i]) atomicAdd(&rs->hist.count[i], hist.count[i]);
+        if (hist.mass[i]) atomicAdd((unsigned long long *)&rs->hist.mass[i], (unsigned long long)hist.mass[i]);
     }
 }
 
-// What launches 3 and 4 begin with: the plan, read off the row's histogram by
-// each work-group for itself.
-__device__ __forceinline__ void row_plan(Shared &sh, const RowSpace *rs, const Row &r, int64_t M) {
-    for (int i = threadIdx.x; i < BINS; i += NT) sh.hist.count[i] = rs->hist.count[i], sh.hist.mass[i] = rs->hist.mass[i];
-    __syncthreads();
-    make_plan(sh, r, M);
+// Launch 3, a work-group a row: the plan.
+__global__ void __launch_bounds__(NT) sample_plan_kernel(SampleArgs a) {
+    __shared__ Shared sh;
+    const int t = threadIdx.x;
+    const int64_t slot = blockIdx.x, b = a.row0 + slot;
+    const Row r(a, b);
+    if (r.takes_first() || r.keeps_all(a.M)) return;
+    RowSpace *const rs = row_space(a, slot);
+    for (int i = t; i < BINS; i += NT) sh.hist.count[i] = rs->hist.count[i], sh.hist.mass[i] = rs->hist.mass[i];
+    fill_table(sh.table, t);
+    uint32_t top, low;
+    row_range(sh.block, a, chunk_space(rs), top, low);
+    if (!top) return;
+    make_plan(sh, r, Binning(top, low, r.temp), top);
+    const uint32_t floor = floor_of(r, Weigh(top, r.c, a.shift, sh.table), top);
+    if (t == 0) rs->plan = sh.plan, rs->floor = floor;
 }
 
-// Launch 3: entries of the bins in question listed, the mass of those before
-// them summed.
+// Launch 4: the entries in question listed, the mass of those before them
+// summed.
 template <typename T>
 __global__ void __launch_bounds__(NT) sample_list_kernel(SampleArgs a) {
-    __shared__ Shared sh;
+    __shared__ Block block;
+    __shared__ double table[TABLE];
     const int t = threadIdx.x, chunk = blockIdx.x % a.chunks;
     const int64_t slot = blockIdx.x / a.chunks, b = a.row0 + slot;
+    const Row r(a, b);
+    if (r.takes_first() || r.keeps_all(a.M)) return;
     RowSpace *const rs = row_space(a, slot);
     ChunkSpace *const cs = chunk_space(rs);
-    const Row r(a, b);
-    if (r.keeps_all(a.M)) return;
-    fill_table(sh.table, t);
     Chunk<T> ch;
     ch.load(a, b, chunk);
+    fill_table(table, t);
     uint32_t top, low;
-    row_range(sh, a, cs, top, low);
+    row_range(block, a, cs, top, low);
     if (!top) return;
-    row_plan(sh, rs, r, a.M);
-    const Plan p = sh.plan;
+    const Plan p = rs->plan;
     if (p.listed > CAP) return;
-    const Weigh wt{(double)value_of(top), r.c, a.shift, sh.table};
-    const Binning bins(value_of(top), value_of(low), r.temp);
+    const Weigh wt(top, r.c, a.shift, table);
+    const uint32_t from = max(p.sure, rs->floor);
     ch.each([&](uint32_t x, int q, int c) {
-        if (p.asks(bins.bin(x))) rs->list[atomicAdd(&rs->listed, 1u)] = (uint64_t)~x << 32 | ch.at(q, c);
+        if (!p.asks(x)) return;
+        const uint32_t at = atomicAdd(&rs->listed, 1u);
+        if (at < CAP) rs->list[at] = (uint64_t)~x << 32 | ch.at(q, c);
     });
     uint64_t m, n;
-    const int sure = p.sure();
-    chunk_sums(sh, ch, r, wt, [&](uint32_t x, uint32_t) { return bins.bin(x) < sure; }, &m, &n);
+    chunk_sums(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= from; }, &m, &n);
     if (t == 0) cs[chunk].mass = m, cs[chunk].count = (uint32_t)n;
 }
 
-// Launch 4, a work-group a row: the listed entries ranked, and the draw.
+// Draws once every chunk's mass is in cs.
+template <typename T>
+__device__ __forceinline__ void draw_row(Shared &sh, const SampleArgs &a, int64_t b, const ChunkSpace *cs, const Weigh &wt,
+                                         End end, uint32_t floor) {
+    const int t = threadIdx.x;
+    uint64_t kept = 0, total = 0;
+    for (int i = t; i < a.chunks; i += NT) kept += cs[i].count, total += cs[i].mass;
+    kept = sh.block.sum(kept);
+    total = sh.block.sum(total);
+    const double goal = goal_of(a.u[b], total);
+    // the chunk in which the sum passes, in index order; the last with a mass where none does
+    uint64_t run = 0;
+    if (t == 0) sh.n = 0;
+    __syncthreads();
+    for (int i0 = 0; i0 < a.chunks; i0 += NT) {
+        const int i = i0 + t;
+        const uint64_t c = i < a.chunks ? cs[i].mass : 0;
+        uint64_t all;
+        const uint64_t before = run + sh.block.before(c, &all);
+        // (a chunk is the one if the sum before it has not passed and it has a mass: the last such)
+        if (c && !((double)before > goal)) atomicMax(&sh.n, (uint32_t)i + 1);
+        run += all;
+    }
+    __syncthreads();
+    const int at = (int)sh.n - 1;
+    uint64_t base = 0;
+    for (int i = t; i < at; i += NT) base += cs[i].mass;
+    base = sh.block.sum(base);
+    Chunk<T> ch;
+    ch.load(a, b, at);
+    draw_chunk(sh, a, b, ch, wt, end, floor, base, total, kept, goal);
+}
+
+// Launch 5, a work-group a row: the listed entries ranked, and the draw.
 template <typename T>
 __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
     __shared__ Shared sh;
@@ -1215,69 +1194,70 @@ __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
     RowSpace *const rs = row_space(a, slot);
     ChunkSpace *const cs = chunk_space(rs);
     fill_table(sh.table, t);
-    for (int i = t; i < MORE; i += NT) sh.more[i] = 0;
     uint32_t top, low;
-    row_range(sh, a, cs, top, low);
+    row_range(sh.block, a, cs, top, low);
     if (!top) {
         if (t == 0) put(a, b, -1, 0, 0, 0);
         return;
     }
     const Row r(a, b);
-    const Weigh wt{(double)value_of(top), r.c, a.shift, sh.table};
-    End end{1, 0xffffffffu};
-    if (r.keeps_all(a.M)) {
-        draw_row<T>(sh, a, b, cs, r, wt, end, 0);
+    if (r.takes_first()) {
+        uint32_t first = 0;     // complement of the first chunk that has it
+        for (int i = t; i < a.chunks; i += NT)
+            if (cs[i].top == top) first = max(first, ~(uint32_t)i);
+        Chunk<T> ch;
+        ch.load(a, b, (int)~sh.block.most(first));
+        draw_first(sh, a, b, ch, top);
         return;
     }
-    row_plan(sh, rs, r, a.M);
+    const Weigh wt(top, r.c, a.shift, sh.table);
+    if (r.keeps_all(a.M)) {
+        draw_row<T>(sh, a, b, cs, wt, NO_END, floor_of(r, wt, top));
+        return;
+    }
+    if (t == 0) sh.plan = rs->plan;
+    __syncthreads();
     const Plan p = sh.plan;
-    uint64_t count = 0;
-    // (chunks past MORE: listed entries' masses would have no place)
-    if (p.listed > CAP || (p.listed && a.chunks > MORE)) {
-        if (p.listed > CAP) {
-            end_by_passes<T>(sh, a, b, r, wt, top);
-        } else {
-            for (int i = t; i < (int)p.listed; i += NT) sh.list[i] = rs->list[i];
-            __syncthreads();
-            rank_list(sh, r, wt, Binning(value_of(top), value_of(low), r.temp), (int)p.listed);
-        }
+    const uint32_t floor = rs->floor, listed = p.listed > CAP ? p.listed : rs->listed;
+    End end = NO_END;
+    if (listed > CAP) {
+        end_by_passes<T>(sh, a, b, r, wt, top);
         end = sh.end;
         Chunk<T> ch;
         for (int i = 0; i < a.chunks; ++i) {
             ch.load(a, b, i);
             uint64_t m, n;
-            chunk_sums(sh, ch, r, wt, [&](uint32_t x, uint32_t j) { return end.has(x, j); }, &m, &n);
+            chunk_sums(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); }, &m, &n);
             if (t == 0) cs[i].mass = m, cs[i].count = (uint32_t)n;
         }
-        __threadfence_block();
+    } else if (listed) {
+        for (int i = t; i < (int)listed; i += NT) sh.list[i] = rs->list[i];
         __syncthreads();
-    } else if (p.listed) {
-        const Binning bins(value_of(top), value_of(low), r.temp);
-        for (int i = t; i < (int)p.listed; i += NT) sh.list[i] = rs->list[i];
-        __syncthreads();
-        rank_list(sh, r, wt, bins, (int)p.listed);
+        rank_list(sh, r, wt, (int)listed);
         end = sh.end;
-        const int sure = p.sure();
+        // their masses to their chunks' (exact sums: the order is of no account)
+        const int skew = skew_of(static_cast<const T *>(a.S) + b * a.lds);
         for (int i = t; i < (int)sh.n; i += NT) {
             const uint32_t x = ~(uint32_t)(sh.list[i] >> 32), j = (uint32_t)sh.list[i];
-            if (bins.bin(x) < sure) continue;
-            const double w = wt.weight(x);
-            if (w < r.least) continue;
-            ++count;
-            atomicAdd((unsigned long long *)&sh.more[j / CHUNK], (unsigned long long)wt.mass_of(w));
+            if (x >= p.sure || x < floor) continue;
+            ChunkSpace &c = cs[(j + skew) / CHUNK];
+            atomicAdd((unsigned long long *)&c.mass, (unsigned long long)wt.mass(x));
+            atomicAdd(&c.count, 1u);
         }
-        count = sh.block.sum(count);
+        __threadfence();
     }
-    draw_row<T>(sh, a, b, cs, r, wt, end, count);
+    __syncthreads();
+    __threadfence();
+    draw_row<T>(sh, a, b, cs, wt, end, floor);
 }
 
 constexpr int64_t SLAB = 2048;      // rows of a large table in flight: their space is reused
 
 size_t row_bytes(int64_t chunks) { return sizeof(RowSpace) + (size_t)chunks * sizeof(ChunkSpace); }
-int64_t chunks_of(int64_t M) { return (M + CHUNK - 1) / CHUNK; }
+int64_t chunks_of(int64_t M) { return (M + 3 + CHUNK - 1) / CHUNK; }     // (a row's places: its entries and up to 3 before)
 
-template <typename T, int V, int Q> hipError_t launch_wave(const SampleArgs &a, hipStream_t s) {
-    sample_wave_kernel<T, V, Q><<<dim3((unsigned)((a.B + 3) / 4)), dim3(256), 0, s>>>(a);
+template <typename T, int E> hipError_t launch_wave(const SampleArgs &a, hipStream_t s) {
+    sample_wave_kernel<T, E><<<dim3((unsigned)((a.B + 3) / 4)), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename T, int P> hipError_t launch_thread(const SampleArgs &a, hipStream_t s) {
@@ -1291,28 +1271,31 @@ template <typename T> hipError_t launch_typed(SampleArgs a, void *ws, hipStream_
         if (a.M <= 16) return launch_thread<T, 16>(a, s);
         return a.M <= 24 ? launch_thread<T, 24>(a, s) : launch_thread<T, 32>(a, s);
     }
-    if (a.M <= 64) return launch_wave<T, 1, 1>(a, s);
-    if (a.M <= 256) return launch_wave<T, 4, 1>(a, s);
-    if (a.M <= 512) return launch_wave<T, 4, 2>(a, s);
-    if (a.M <= 1024) return launch_wave<T, 4, 4>(a, s);
-    if (a.M <= 2048) return launch_wave<T, 4, 8>(a, s);
-    if (a.M <= CHUNK) {
+    if (a.M <= 64) return launch_wave<T, 1>(a, s);
+    const int64_t places = a.vec ? a.M : a.M + 3;
+    if (places <= 256) return launch_wave<T, 4>(a, s);
+    if (places <= 512) return launch_wave<T, 8>(a, s);
+    if (places <= 1024) return launch_wave<T, 16>(a, s);
+    if (places <= 2048) return launch_wave<T, 32>(a, s);
+    if (a.M + 3 <= CHUNK) {
         sample_group_kernel<T><<<dim3((unsigned)a.B), dim3(NT), 0, s>>>(a);
         return hipGetLastError();
     }
     a.chunks = (int)chunks_of(a.M);
     a.row_bytes = row_bytes(a.chunks);
     a.ws = ws;
-    // one value for all rows that keeps everything: no row comes to the third launch
-    const bool all = !a.top_k && !a.top_p && !a.temperature && a.temperature_all > 0.f &&
-                     (a.top_k_all <= 0 || a.top_k_all >= a.M) && !(a.top_p_all < 1.f);
+    // no row with a run to end: launches 3 and 4 have nothing to do
+    const bool all = !a.top_k && !a.top_p && (a.top_k_all <= 1 || a.top_k_all >= a.M) && !(a.top_p_all < 1.f);
     for (a.row0 = 0; a.row0 < a.B; a.row0 += SLAB) {
         const int64_t rows = a.B - a.row0 < SLAB ? a.B - a.row0 : SLAB;
-        const dim3 grid((unsigned)(rows * a.chunks));
+        const dim3 grid((unsigned)(rows * a.chunks)), one((unsigned)rows);
         sample_top_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
         sample_bins_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
-        if (!all) sample_list_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
-        sample_draw_kernel<T><<<dim3((unsigned)rows), dim3(NT), 0, s>>>(a);
+        if (!all) {
+            sample_plan_kernel<<<one, dim3(NT), 0, s>>>(a);
+            sample_list_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
+        }
+        sample_draw_kernel<T><<<one, dim3(NT), 0, s>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -1322,14 +1305,14 @@ template <typename T> hipError_t launch_typed(SampleArgs a, void *ws, hipStream_
 }  // namespace
 
 size_t sample_workspace(int64_t B, int64_t M) {
-    if (M <= CHUNK) return 0;
+    if (M + 3 <= CHUNK) return 0;
     return (size_t)(B < SLAB ? B : SLAB) * row_bytes(chunks_of(M));
 }
 
 hipError_t launch_sample(gs_dtype st, SampleArgs a, void *ws, hipStream_t s) {
     int bits = 0;
     while (((int64_t)1 << bits) < a.M) ++bits;
-    a.shift = 62 - bits < 52 ? 62 - bits : 52;
+    a.shift = 62 - bits < 51 ? 62 - bits : 51;
     return st == GS_F32 ? launch_typed<float>(a, ws, s) : launch_typed<bf16_t>(a, ws, s);
 }
 

@@ -328,25 +328,28 @@ __global__ void __launch_bounds__(256) xattn_parts_kernel(CrossAttnGradArgs a) {
 }
 
 // Parts that bring the work-groups to two a CU, as far as parts of a useful
-// length (128 keys, 4 tiles of 32 query rows) go.
+// length (64 keys, 2 tiles of 32 query rows) go: each part costs a write and a
+// read of fp32 rows.  Work-groups of two waves instead, so that fewer parts
+// do, were slower: dK and dV of train_ragged 55 us in 2 parts of 64-key
+// work-groups, 39 in 3 of 128-key ones.
 struct Plan {
     int dp, q_parts, q_step, k_parts;
 };
 Plan plan_for(int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh) {
     Plan p{};
     p.dp = Dh <= 64 ? 64 : 128;
-    const int64_t G = Hq / Hkv, most = 512;
-    const int64_t q_groups = B * Hkv * ((Lq * G + 127) / 128), k_groups = B * Hkv * ((Lk + 127) / 128);
-    auto parts = [&](int64_t groups, int64_t useful) {
-        int64_t n = groups ? most / groups : 1;
+    const int64_t G = Hq / Hkv;
+    auto parts = [&](int64_t rows, int64_t useful) {
+        const int64_t groups = B * Hkv * ((rows + 127) / 128);
+        int64_t n = groups ? 512 / groups : 1;
         n = n < useful ? n : useful;
         return (int)(n > 1 ? n : 1);
     };
-    int n = parts(q_groups, Lk / 128);
+    const int n = parts(Lq * G, Lk / 64);
     const int64_t step = ((Lk + n - 1) / n + 63) / 64 * 64;
     p.q_step = (int)(step ? step : 64);
     p.q_parts = Lk ? (int)((Lk + step - 1) / step) : 1;
-    p.k_parts = parts(k_groups, (Lq + 31) / 32 * G / 4);
+    p.k_parts = parts(Lk, (Lq + 31) / 32 * G / 2);
     return p;
 }
 
