@@ -523,7 +523,9 @@ __global__ void __launch_bounds__(64) sample_thread_kernel(SampleArgs a) {
 
 // ---------------------------------------------------- work-groups of 256 a row
 
-constexpr int NT = 256, Q = 8, CHUNK = NT * 4 * Q, BINS = 2048, CAP = 1024;
+// A chunk is PARTS parts of 256 places (four a lane of one wave), in index
+// order; PARTS_HERE: parts of a row whose masses fit a work-group's LDS.
+constexpr int NT = 256, Q = 8, PARTS = NT / 64 * Q, CHUNK = 256 * PARTS, BINS = 2048, CAP = 1024, PARTS_HERE = 1024;
 constexpr uint32_t LAST = 0x7fffffff;       // an index behind every entry
 
 struct Block {
@@ -607,10 +609,11 @@ struct RowSpace {
     Hist hist;
     Plan plan;
     uint32_t listed, floor;     // entries listed; the smallest key that min_p keeps
+    uint32_t top, pad;          // the largest key
     uint64_t list[CAP];
 };
 struct ChunkSpace {
-    uint64_t mass;
+    uint64_t mass[PARTS];       // of the entries that are surely kept, by parts
     uint32_t count, top, low, pad;
 };
 
@@ -622,9 +625,9 @@ struct Shared {
     uint64_t list[CAP];
     Plan plan;
     End end;
-    uint32_t n, bins[4], floor;
-    uint64_t base;
-    uint64_t part[NT / 64 * Q];
+    uint32_t n, bins[4];
+    uint64_t base, wave[2][NT / 64];
+    uint64_t mass[PARTS_HERE];  // masses of a row's parts
 };
 
 template <typename T> struct Chunk {
@@ -731,77 +734,93 @@ __device__ __forceinline__ void make_plan(Shared &sh, const Row &r, const Binnin
     __syncthreads();
 }
 
-// Ranks the listed entries (n <= CAP, in sh.list as ~key, index) and finds the
-// end of the run.
-__device__ __forceinline__ void rank_list(Shared &sh, const Row &r, const Weigh &wt, int n) {
-    const int t = threadIdx.x;
-    int size = 64;
-    while (size < n) size *= 2;
-    for (int i = n + t; i < size; i += NT) sh.list[i] = ~0ull;
-    __syncthreads();
-    for (int k = 2; k <= size; k *= 2)
-        for (int d = k / 2; d; d /= 2) {
-            for (int i = t; i < size / 2; i += NT) {
-                const int x = (i / d) * 2 * d + i % d, y = x + d;
-                const uint64_t u = sh.list[x], v = sh.list[y];
-                if ((u > v) == ((x & k) == 0)) sh.list[x] = v, sh.list[y] = u;
-            }
-            __syncthreads();
-        }
-    constexpr int PER = CAP / NT;
-    const Plan p = sh.plan;
-    uint32_t key[PER];
-    uint64_t mass[PER], of_k = 0, of_p = 0, all;
-    int first_k = 0;
+// Entries of a work-group, CAP / NT a thread in any order, key 0 for none.
+struct Listed {
+    static constexpr int PER = CAP / NT;
+    uint32_t key[PER], j[PER];
+    uint64_t mass[PER];
+    int turn = 0;               // (two sets of partial sums: one barrier a sum)
+    // sums over the entries that `on` takes, of 1 or of their masses
+    template <typename F> __device__ __forceinline__ uint64_t sum(Shared &sh, bool by_mass, F on) {
+        uint64_t v = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int x = t * PER + i;
-        key[i] = x < n ? ~(uint32_t)(sh.list[x] >> 32) : 0;
-        mass[i] = key[i] && r.p < 1. ? wt.mass(key[i]) : 0;
-        if (p.in_p(key[i])) of_p += mass[i];
-        if (key[i] && !(p.k_lo <= p.k_hi && key[i] <= p.k_hi)) ++first_k;
+        for (int i = 0; i < PER; ++i)
+            if (key[i] && on(i)) v += by_mass ? mass[i] : 1;
+        v = wave_sum(v);
+        uint64_t *const to = sh.wave[turn];
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0) to[threadIdx.x >> 6] = v;
+        __syncthreads();
+        return to[0] + to[1] + to[2] + to[3];
     }
-    // listed entries over top_k's bin come first
-    const int start_k = (int)sh.block.sum(first_k);
-    uint32_t keep = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        if (!key[i]) continue;
-        if (!p.in_k(key[i]) || (uint64_t)(t * PER + i - start_k) + p.count_k < (uint64_t)r.k) {
-            keep |= 1u << i;
-            if (p.in_k(key[i])) of_k += mass[i];
+    // The end of the run of entries in rank order that has n of them (by_mass:
+    // that reaches the mass n), among the keys of [lo, most] and with the sum
+    // `above` before them.  The run is known to end there.
+    __device__ __forceinline__ End run(Shared &sh, uint32_t lo, uint32_t most, bool by_mass, double n, uint64_t above) {
+        uint32_t hi = most;
+        uint64_t over = above;          // the sum over hi
+        while (lo < hi) {
+            const uint32_t mid = lo + (hi - lo) / 2 + 1;
+            const uint64_t x = above + sum(sh, by_mass, [&](int i) { return key[i] >= mid && key[i] <= most; });
+            if (x > above && (double)x >= n) lo = mid;
+            else hi = mid - 1, over = x;
         }
+        // ends among the entries equal to lo: after as many of them as are needed
+        const uint64_t same = sum(sh, false, [&](int i) { return key[i] == lo; });
+        uint64_t one = 0;
+        if (by_mass) {
+            const uint64_t all = sum(sh, true, [&](int i) { return key[i] == lo; });
+            one = same ? all / same : 0;
+        }
+        double need = by_mass ? (one ? ceil((n - (double)over) / (double)one) : 1.) : n - (double)over;
+        if (need < 1.) need = 1.;
+        if (need >= (double)same) return End{lo, LAST};
+        uint32_t a = 0, b = LAST;       // the smallest index with `need` of them up to it
+        while (a < b) {
+            const uint32_t mid = a + (b - a) / 2;
+            if ((double)sum(sh, false, [&](int i) { return key[i] == lo && j[i] <= mid; }) >= need) b = mid;
+            else a = mid + 1;
+        }
+        return End{lo, a};
+    }
+};
+
+// The end of the run from the listed entries (n <= CAP, in sh.list as key and
+// index): top_k's, then top_p's within it.
+__device__ __forceinline__ End end_of_list(Shared &sh, const Row &r, const Weigh &wt, int n) {
+    const Plan p = sh.plan;
+    Listed e;
+#pragma unroll
+    for (int i = 0; i < Listed::PER; ++i) {
+        const int x = i * NT + threadIdx.x;
+        const uint64_t v = x < n ? sh.list[x] : 0;
+        e.key[i] = (uint32_t)(v >> 32);
+        e.j[i] = (uint32_t)v;
+        e.mass[i] = e.key[i] && r.p < 1. ? wt.mass(e.key[i]) : 0;
+    }
+    End end = NO_END;
+    uint64_t all = p.all;
+    if (p.k_lo <= p.k_hi) {
+        end = e.run(sh, p.k_lo, p.k_hi, false, (double)r.k, p.count_k);
+        all = p.mass_k + e.sum(sh, true, [&](int i) { return p.in_k(e.key[i]) && end.has(e.key[i], e.j[i]); });
     }
     if (r.p < 1.) {
-        of_k = sh.block.sum(of_k);
-        const double goal = r.p * (double)(p.k_lo <= p.k_hi ? p.mass_k + of_k : p.all);
-        const uint64_t of = sh.block.before(of_p, &all);
-        uint64_t m = p.mass_p + of;
+        // entries that top_k leaves out weigh nothing
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            if (!key[i]) continue;
-            if (!p.in_p(key[i]) || !(m == 0 || (double)m < goal)) keep &= ~(1u << i);
-            if (p.in_p(key[i])) m += mass[i];
-        }
+        for (int i = 0; i < Listed::PER; ++i)
+            if (!p.in_p(e.key[i]) || !end.has(e.key[i], e.j[i])) e.key[i] = 0;
+        const uint32_t lo = p.k_lo <= p.k_hi && end.key > p.p_lo ? end.key : p.p_lo;
+        const End ends = e.run(sh, lo, p.p_hi, true, r.p * (double)all, p.mass_p);
+        if (ends.key > end.key || (ends.key == end.key && ends.j < end.j)) end = ends;
     }
-    // the last one kept (its place + 1)
-    uint32_t last = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-        if ((keep >> i) & 1) last = t * PER + i + 1;
-    last = sh.block.most(last);
-    if (t == 0) {
-        sh.end = last ? End{~(uint32_t)(sh.list[last - 1] >> 32), (uint32_t)sh.list[last - 1]} : End{p.sure, LAST};
-        sh.n = last;
-    }
-    __syncthreads();
+    return end;
 }
 
 // The end of the run for rows whose bins hold too many entries: the range of
 // keys in question is divided by 2048 until it is one key, by whole passes over
 // the row.
 template <typename T>
-__device__ __forceinline__ void end_by_passes(Shared &sh, const SampleArgs &a, int64_t b, const Row &r, const Weigh &wt,
+__device__ __forceinline__ End end_by_passes(Shared &sh, const SampleArgs &a, int64_t b, const Row &r, const Weigh &wt,
                                               uint32_t top) {
     const int t = threadIdx.x;
     const T *const row = static_cast<const T *>(a.S) + b * a.lds;
@@ -886,71 +905,83 @@ __device__ __forceinline__ void end_by_passes(Shared &sh, const SampleArgs &a, i
         }
     }
     __syncthreads();
+    return sh.end;
 }
 
-// Mass and number of the entries of a chunk that `has` keeps.
+// Masses, by parts, and number of the entries of a chunk that `has` keeps.
 template <typename T, typename F>
-__device__ __forceinline__ void chunk_sums(Block &block, const Chunk<T> &ch, const Weigh &wt, F has, uint64_t *mass,
-                                           uint64_t *count) {
-    uint64_t m = 0, n = 0;
-    ch.each([&](uint32_t x, int q, int c) {
-        if (has(x, ch.at(q, c))) m += wt.mass(x), ++n;
-    });
-    *mass = block.sum(m);
-    *count = block.sum(n);
-}
-
-// Draws from a chunk: `base` is the mass of the chunks before it, and the sum
-// passes the goal in it (or it is the last with a mass).
-template <typename T>
-__device__ __forceinline__ void draw_chunk(Shared &sh, const SampleArgs &a, int64_t b, const Chunk<T> &ch, const Weigh &wt,
-                                           End end, uint32_t floor, uint64_t base, uint64_t total, uint64_t kept, double goal) {
+__device__ __forceinline__ uint64_t chunk_parts(Block &block, const Chunk<T> &ch, const Weigh &wt, F has, uint64_t *mass) {
     const int t = threadIdx.x, l = t & 63, w = t >> 6;
-    auto mass_at = [&](int q, int c) -> uint64_t {
-        const uint32_t x = ch.key[q][c];
-        return x && x >= floor && end.has(x, ch.at(q, c)) ? wt.mass(x) : 0;
-    };
-    uint64_t mine[Q];
+    uint64_t n = 0;
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-        mine[q] = 0;
+        uint64_t m = 0;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) mine[q] += mass_at(q, c);
-        const uint64_t s = wave_sum(mine[q]);
-        if (l == 0) sh.part[q * (NT / 64) + w] = s;
+        for (int c = 0; c < 4; ++c) {
+            const uint32_t x = ch.key[q][c];
+            if (x && has(x, ch.at(q, c))) m += wt.mass(x), ++n;
+        }
+        m = wave_sum(m);
+        if (l == 0) mass[q * (NT / 64) + w] = m;
+    }
+    return block.sum(n);
+}
+
+// Draws from a row of whose `parts` parts `mass_of` tells the masses.
+template <typename T, typename F>
+__device__ __forceinline__ void draw_parts(Shared &sh, const SampleArgs &a, int64_t b, const Weigh &wt, End end,
+                                           uint32_t floor, uint64_t kept, int parts, F mass_of) {
+    const int t = threadIdx.x, l = t & 63;
+    const float u = a.u[b];
+    uint64_t total = 0;
+    for (int i = t; i < parts; i += NT) total += mass_of(i);
+    total = sh.block.sum(total);
+    const double goal = goal_of(u, total);
+    // the part in which the sum passes the goal, in index order: the last one
+    // with a mass before which it has not (that is also right where it never does)
+    if (t == 0) sh.n = 0;
+    __syncthreads();
+    uint64_t run = 0;
+    for (int i0 = 0; i0 < parts; i0 += NT) {
+        const int i = i0 + t;
+        const uint64_t m = i < parts ? mass_of(i) : 0;
+        uint64_t all;
+        const uint64_t before = run + sh.block.before(m, &all);
+        if (m && !((double)before > goal)) atomicMax(&sh.n, (uint32_t)i + 1);
+        run += all;
     }
     __syncthreads();
-    // the block of 256 places in which the sum passes, in index order
-    const uint64_t part = l < NT / 64 * Q ? sh.part[l] : 0;
-    const uint64_t sums = base + wave_upto(part);
-    const uint64_t some = __ballot(part != 0), over = __ballot(part != 0 && (double)sums > goal);
-    const int at = over ? __ffsll((unsigned long long)over) - 1 : 63 - __clzll(some);
-    const int at_q = at / (NT / 64);
-    if (w != at % (NT / 64)) return;
-    const uint64_t at_base = read_lane64(sums - part, at);
-    uint64_t sum = 0;
+    const int at = (int)sh.n - 1;
+    // what lies before it, again in a fixed order
+    uint64_t base = 0;
+    for (int i = t; i < at; i += NT) base += mass_of(i);
+    base = sh.block.sum(base);
+    if (t >= 64) return;
+    const T *const row = static_cast<const T *>(a.S) + b * a.lds;
+    const int32_t j = (int32_t)((uint32_t)at * 256 + 4 * l - (uint32_t)skew_of(row));
+    uint32_t key[4];
+    uint64_t mass[4], mine = 0;
+    load_keys<T, 4>(key, row, j, (uint32_t)a.M);
 #pragma unroll
-    for (int q = 0; q < Q; ++q)
-        if (q == at_q) sum = mine[q];
-    const uint64_t upto = wave_upto(sum);
-    const uint64_t has = __ballot(sum != 0), past = __ballot(sum != 0 && (double)(at_base + upto) > goal);
+    for (int c = 0; c < 4; ++c) {
+        const bool on = key[c] && key[c] >= floor && end.has(key[c], (uint32_t)(j + c));
+        mass[c] = on ? wt.mass(key[c]) : 0;
+        mine += mass[c];
+    }
+    const uint64_t upto = wave_upto(mine);
+    const uint64_t has = __ballot(mine != 0), past = __ballot(mine != 0 && (double)(base + upto) > goal);
     const int lane = past ? __ffsll((unsigned long long)past) - 1 : 63 - __clzll(has);
     if (l != lane) return;
-    uint64_t s = at_base + upto - sum, hw = 0;
-    int64_t hit = -1;
+    uint64_t s = base + upto - mine, hw = 0;
+    int32_t hit = -1;
+    bool done = false;
 #pragma unroll
-    for (int q = 0; q < Q; ++q)
-        if (q == at_q) {
-            bool done = false;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const uint64_t m = mass_at(q, c);
-                if (done || !m) continue;
-                s += m;
-                hit = ch.at(q, c), hw = m;
-                done = (double)s > goal;
-            }
-        }
+    for (int c = 0; c < 4; ++c) {
+        if (done || !mass[c]) continue;
+        s += mass[c];
+        hit = j + c, hw = mass[c];
+        done = (double)s > goal;
+    }
     put(a, b, hit, hw, total, kept);
 }
 
@@ -1013,24 +1044,19 @@ __global__ void __launch_bounds__(NT) sample_group_kernel(SampleArgs a) {
             ch.each([&](uint32_t x, int q, int c) {
                 if (!p.asks(x)) return;
                 const uint32_t at = atomicAdd(&sh.n, 1u);
-                if (at < CAP) sh.list[at] = (uint64_t)~x << 32 | ch.at(q, c);
+                if (at < CAP) sh.list[at] = (uint64_t)x << 32 | ch.at(q, c);
             });
             __syncthreads();
             listed = sh.n;
             __syncthreads();
         }
-        if (listed > CAP) {
-            end_by_passes<T>(sh, a, b, r, wt, top);
-            end = sh.end;
-        } else if (listed) {
-            rank_list(sh, r, wt, (int)listed);
-            end = sh.end;
-        }
+        if (listed > CAP) end = end_by_passes<T>(sh, a, b, r, wt, top);
+        else if (listed) end = end_of_list(sh, r, wt, (int)listed);
     }
     const uint32_t floor = floor_of(r, wt, top);
-    uint64_t total, kept;
-    chunk_sums(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); }, &total, &kept);
-    draw_chunk(sh, a, b, ch, wt, end, floor, 0, total, kept, goal_of(a.u[b], total));
+    const uint64_t kept =
+        chunk_parts(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); }, sh.mass);
+    draw_parts<T>(sh, a, b, wt, end, floor, kept, PARTS, [&](int i) { return sh.mass[i]; });
 }
 
 __device__ __forceinline__ RowSpace *row_space(const SampleArgs &a, int64_t slot) {
@@ -1088,9 +1114,8 @@ __global__ void __launch_bounds__(NT) sample_bins_kernel(SampleArgs a) {
     const Weigh wt(top, r.c, a.shift, table);
     if (r.keeps_all(a.M)) {
         const uint32_t floor = floor_of(r, wt, top);
-        uint64_t m, n;
-        chunk_sums(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= floor; }, &m, &n);
-        if (t == 0) cs[chunk].mass = m, cs[chunk].count = (uint32_t)n;
+        const uint64_t n = chunk_parts(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= floor; }, cs[chunk].mass);
+        if (t == 0) cs[chunk].count = (uint32_t)n;
         return;
     }
     const bool by_k = r.k < a.M;
@@ -1114,10 +1139,13 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(SampleArgs a) {
     fill_table(sh.table, t);
     uint32_t top, low;
     row_range(sh.block, a, chunk_space(rs), top, low);
-    if (!top) return;
+    if (!top) {
+        if (t == 0) rs->top = 0;
+        return;
+    }
     make_plan(sh, r, Binning(top, low, r.temp), top);
     const uint32_t floor = floor_of(r, Weigh(top, r.c, a.shift, sh.table), top);
-    if (t == 0) rs->plan = sh.plan, rs->floor = floor;
+    if (t == 0) rs->plan = sh.plan, rs->floor = floor, rs->top = top;
 }
 
 // Launch 4: the entries in question listed, the mass of those before them
@@ -1135,8 +1163,8 @@ __global__ void __launch_bounds__(NT) sample_list_kernel(SampleArgs a) {
     Chunk<T> ch;
     ch.load(a, b, chunk);
     fill_table(table, t);
-    uint32_t top, low;
-    row_range(block, a, cs, top, low);
+    __syncthreads();
+    const uint32_t top = rs->top;
     if (!top) return;
     const Plan p = rs->plan;
     if (p.listed > CAP) return;
@@ -1145,44 +1173,10 @@ __global__ void __launch_bounds__(NT) sample_list_kernel(SampleArgs a) {
     ch.each([&](uint32_t x, int q, int c) {
         if (!p.asks(x)) return;
         const uint32_t at = atomicAdd(&rs->listed, 1u);
-        if (at < CAP) rs->list[at] = (uint64_t)~x << 32 | ch.at(q, c);
+        if (at < CAP) rs->list[at] = (uint64_t)x << 32 | ch.at(q, c);
     });
-    uint64_t m, n;
-    chunk_sums(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= from; }, &m, &n);
-    if (t == 0) cs[chunk].mass = m, cs[chunk].count = (uint32_t)n;
-}
-
-// Draws once every chunk's mass is in cs.
-template <typename T>
-__device__ __forceinline__ void draw_row(Shared &sh, const SampleArgs &a, int64_t b, const ChunkSpace *cs, const Weigh &wt,
-                                         End end, uint32_t floor) {
-    const int t = threadIdx.x;
-    uint64_t kept = 0, total = 0;
-    for (int i = t; i < a.chunks; i += NT) kept += cs[i].count, total += cs[i].mass;
-    kept = sh.block.sum(kept);
-    total = sh.block.sum(total);
-    const double goal = goal_of(a.u[b], total);
-    // the chunk in which the sum passes, in index order; the last with a mass where none does
-    uint64_t run = 0;
-    if (t == 0) sh.n = 0;
-    __syncthreads();
-    for (int i0 = 0; i0 < a.chunks; i0 += NT) {
-        const int i = i0 + t;
-        const uint64_t c = i < a.chunks ? cs[i].mass : 0;
-        uint64_t all;
-        const uint64_t before = run + sh.block.before(c, &all);
-        // (a chunk is the one if the sum before it has not passed and it has a mass: the last such)
-        if (c && !((double)before > goal)) atomicMax(&sh.n, (uint32_t)i + 1);
-        run += all;
-    }
-    __syncthreads();
-    const int at = (int)sh.n - 1;
-    uint64_t base = 0;
-    for (int i = t; i < at; i += NT) base += cs[i].mass;
-    base = sh.block.sum(base);
-    Chunk<T> ch;
-    ch.load(a, b, at);
-    draw_chunk(sh, a, b, ch, wt, end, floor, base, total, kept, goal);
+    const uint64_t n = chunk_parts(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= from; }, cs[chunk].mass);
+    if (t == 0) cs[chunk].count = (uint32_t)n;
 }
 
 // Launch 5, a work-group a row: the listed entries ranked, and the draw.
@@ -1211,44 +1205,57 @@ __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
         return;
     }
     const Weigh wt(top, r.c, a.shift, sh.table);
-    if (r.keeps_all(a.M)) {
-        draw_row<T>(sh, a, b, cs, wt, NO_END, floor_of(r, wt, top));
-        return;
-    }
-    if (t == 0) sh.plan = rs->plan;
-    __syncthreads();
-    const Plan p = sh.plan;
-    const uint32_t floor = rs->floor, listed = p.listed > CAP ? p.listed : rs->listed;
+    const int parts = a.chunks * PARTS;
+    const bool here = parts <= PARTS_HERE;
     End end = NO_END;
-    if (listed > CAP) {
-        end_by_passes<T>(sh, a, b, r, wt, top);
-        end = sh.end;
+    uint32_t floor;
+    bool again = false;
+    uint64_t more = 0;
+    if (here)
+        for (int i = t; i < parts; i += NT) sh.mass[i] = cs[i / PARTS].mass[i % PARTS];
+    if (r.keeps_all(a.M)) {
+        floor = floor_of(r, wt, top);
+    } else {
+        if (t == 0) sh.plan = rs->plan;
+        __syncthreads();
+        const Plan p = sh.plan;
+        const uint32_t listed = p.listed > CAP ? p.listed : rs->listed;
+        floor = rs->floor;
+        if (listed > CAP) {
+            end = end_by_passes<T>(sh, a, b, r, wt, top);
+            again = true;
+        } else if (listed) {
+            for (int i = t; i < (int)listed; i += NT) sh.list[i] = rs->list[i];
+            __syncthreads();
+            end = end_of_list(sh, r, wt, (int)listed);
+            again = !here;
+            if (here) {
+                // their masses to their parts' (exact sums: the order is of no account)
+                const int skew = skew_of(static_cast<const T *>(a.S) + b * a.lds);
+                for (int i = t; i < (int)listed; i += NT) {
+                    const uint32_t x = (uint32_t)(sh.list[i] >> 32), j = (uint32_t)sh.list[i];
+                    if (x >= p.sure || x < floor || !end.has(x, j)) continue;
+                    ++more;
+                    atomicAdd((unsigned long long *)&sh.mass[(j + skew) / 256], (unsigned long long)wt.mass(x));
+                }
+            }
+        }
+    }
+    if (again) {
+        // the whole row once more, now that the end of the run is known
         Chunk<T> ch;
         for (int i = 0; i < a.chunks; ++i) {
             ch.load(a, b, i);
-            uint64_t m, n;
-            chunk_sums(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); }, &m, &n);
-            if (t == 0) cs[i].mass = m, cs[i].count = (uint32_t)n;
+            const uint64_t n = chunk_parts(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); },
+                                           here ? sh.mass + i * PARTS : cs[i].mass);
+            if (t == 0) cs[i].count = (uint32_t)n;
         }
-    } else if (listed) {
-        for (int i = t; i < (int)listed; i += NT) sh.list[i] = rs->list[i];
-        __syncthreads();
-        rank_list(sh, r, wt, (int)listed);
-        end = sh.end;
-        // their masses to their chunks' (exact sums: the order is of no account)
-        const int skew = skew_of(static_cast<const T *>(a.S) + b * a.lds);
-        for (int i = t; i < (int)sh.n; i += NT) {
-            const uint32_t x = ~(uint32_t)(sh.list[i] >> 32), j = (uint32_t)sh.list[i];
-            if (x >= p.sure || x < floor) continue;
-            ChunkSpace &c = cs[(j + skew) / CHUNK];
-            atomicAdd((unsigned long long *)&c.mass, (unsigned long long)wt.mass(x));
-            atomicAdd(&c.count, 1u);
-        }
-        __threadfence();
     }
     __syncthreads();
-    __threadfence();
-    draw_row<T>(sh, a, b, cs, wt, end, floor);
+    for (int i = t; i < a.chunks; i += NT) more += cs[i].count;
+    const uint64_t kept = sh.block.sum(more);
+    if (here) draw_parts<T>(sh, a, b, wt, end, floor, kept, parts, [&](int i) { return sh.mass[i]; });
+    else draw_parts<T>(sh, a, b, wt, end, floor, kept, parts, [&](int i) { return cs[i / PARTS].mass[i % PARTS]; });
 }
 
 constexpr int64_t SLAB = 2048;      // rows of a large table in flight: their space is reused
