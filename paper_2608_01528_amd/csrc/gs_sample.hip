@@ -325,7 +325,7 @@ __device__ __forceinline__ void draw_lanes(const SampleArgs &a, int64_t b, const
 // lane, so that lanes are in index order; what top_k leaves, if it fits, moves
 // on to lists of one or two entries a lane.
 template <typename T, int E>
-__global__ void __launch_bounds__(256) sample_wave_kernel(SampleArgs a) {
+__global__ void __launch_bounds__(256, 4) sample_wave_kernel(SampleArgs a) {
     constexpr int V = E < 4 ? 1 : 4, Q = E / V, STEP = E + 1;       // (an odd step: 64 lanes on different banks)
     __shared__ double table[TABLE];
     __shared__ uint32_t rows[4][E == 1 ? 1 : 64 * STEP];
@@ -762,6 +762,7 @@ struct Listed {
         while (lo < hi) {
             const uint32_t mid = lo + (hi - lo) / 2 + 1;
             const uint64_t x = above + sum(sh, by_mass, [&](int i) { return key[i] >= mid && key[i] <= most; });
+            if (!by_mass && (double)x == n) return End{mid, LAST};
             if (x > above && (double)x >= n) lo = mid;
             else hi = mid - 1, over = x;
         }
