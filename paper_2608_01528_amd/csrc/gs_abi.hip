@@ -875,7 +875,7 @@ size_t gs_cross_attention_workspace(const gs_cross_attn *a, gs_dtype t) {
 
 size_t gs_cross_attention_grad_workspace(const gs_cross_attn *a, gs_dtype t) {
     if (!a || !is_batch_type(t) || !attn_sizes(a)) return 0;
-    return cross_attn_grad_workspace(a->B, a->Lq, a->Lk, a->Hq, a->Hkv, a->Dh);
+    return cross_attn_grad_workspace(t, a->B, a->Lq, a->Lk, a->Hq, a->Hkv, a->Dh);
 }
 
 gs_status gs_cross_attention(const gs_cross_attn *p, gs_dtype t, void *ws, size_t ws_bytes, void *stream) {

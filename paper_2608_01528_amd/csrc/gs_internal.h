@@ -269,7 +269,7 @@ struct CrossAttnGradArgs {
     f2v *stat;                          // B x Hq x Lq: -lse / ln 2, sum_d dO O
     float *dq_part, *dkv_part;
 };
-size_t cross_attn_grad_workspace(int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh);
+size_t cross_attn_grad_workspace(gs_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh);
 hipError_t launch_cross_attn_grad(gs_dtype t, CrossAttnGradArgs a, void *ws, hipStream_t s);
 
 // Sampling of entries from scores (gs_sample.hip).

@@ -14,7 +14,7 @@
 //   a wave a row        up to 2048 entries, in registers: the end of the run is
 //                       found by halving the range of keys until at most 64
 //                       entries are in question, and these are ranked
-//   a work-group a row  up to 8192 entries, in registers: a histogram of the
+//   a work-group a row  up to 8189 entries, in registers: a histogram of the
 //                       scores below the largest finds the bin the run ends in
 //   work-groups a row   more entries: the same over chunks of 8192, in five
 //                       launches (largest score, histogram, where the run ends,
@@ -521,31 +521,41 @@ __global__ void __launch_bounds__(64) sample_thread_kernel(SampleArgs a) {
     put(a, b, hit, hw, total, __popc(keep));
 }
 
-// ---------------------------------------------------- work-groups of 256 a row
+// --------------------------------------------------------- work-groups a row
 
-// A chunk is PARTS parts of 256 places (four a lane of one wave), in index
-// order; PARTS_HERE: parts of a row whose masses fit a work-group's LDS.
+// What the threads hold, 32 places each, is a chunk: PARTS parts of 256 places
+// (four a lane of one wave), in index order.  PARTS_HERE: parts of a row whose
+// masses fit a work-group's LDS.
 constexpr int NT = 256, Q = 8, PARTS = NT / 64 * Q, CHUNK = 256 * PARTS, BINS = 2048, CAP = 1024, PARTS_HERE = 1024;
 constexpr uint32_t LAST = 0x7fffffff;       // an index behind every entry
 
 struct Block {
     uint64_t tmp[NT / 64];
+    __device__ __forceinline__ uint64_t all() const {
+        uint64_t v = 0;
+#pragma unroll
+        for (int i = 0; i < NT / 64; ++i) v += tmp[i];
+        return v;
+    }
     __device__ __forceinline__ uint64_t sum(uint64_t v) {
         v = wave_sum(v);
         __syncthreads();
         if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
         __syncthreads();
-        return tmp[0] + tmp[1] + tmp[2] + tmp[3];
+        return all();
     }
     __device__ __forceinline__ uint32_t most(uint32_t v) {
         v = wave_max(v);
         __syncthreads();
         if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
         __syncthreads();
-        return (uint32_t)max(max(tmp[0], tmp[1]), max(tmp[2], tmp[3]));
+        uint64_t m = tmp[0];
+#pragma unroll
+        for (int i = 1; i < NT / 64; ++i) m = max(m, tmp[i]);
+        return (uint32_t)m;
     }
-    // sum over the threads before this one; *all: over all of them
-    __device__ __forceinline__ uint64_t before(uint64_t v, uint64_t *all) {
+    // sum over the threads before this one; *sum_all: over all of them
+    __device__ __forceinline__ uint64_t before(uint64_t v, uint64_t *sum_all) {
         const int w = threadIdx.x >> 6;
         const uint64_t x = wave_upto(v);
         __syncthreads();
@@ -555,7 +565,7 @@ struct Block {
 #pragma unroll
         for (int i = 0; i < NT / 64; ++i)
             if (i < w) base += tmp[i];
-        *all = tmp[0] + tmp[1] + tmp[2] + tmp[3];
+        *sum_all = all();
         return base + x - v;
     }
 };
@@ -599,10 +609,14 @@ struct End {
 };
 constexpr End NO_END = {1, LAST};
 
+// Bin i lies in slot(i): a thread reads eight bins in a row, and 64 threads then
+// read 64 slots in a row.
 struct Hist {
     uint32_t count[BINS];
     uint64_t mass[BINS];
 };
+__device__ __forceinline__ int slot(int i) { return (i & 7) * (BINS / 8) + (i >> 3); }
+static_assert(BINS == 8 * NT, "eight bins a thread");
 
 // Workspace of a row that several work-groups share; chunks x ChunkSpace follow.
 struct RowSpace {
@@ -671,7 +685,7 @@ __device__ __forceinline__ void make_plan(Shared &sh, const Row &r, const Binnin
     const int t = threadIdx.x, w = t >> 6, l = t & 63, i0 = t * PER;
     Hist &h = sh.hist;
     uint64_t n = 0, m = 0, all_n, all_m;
-    for (int i = i0; i < i0 + PER; ++i) n += h.count[i], m += h.mass[i];
+    for (int i = i0; i < i0 + PER; ++i) n += h.count[slot(i)], m += h.mass[slot(i)];
     const uint64_t n0 = sh.block.before(n, &all_n), m0 = sh.block.before(m, &all_m);
     // bins 0: top_k's; 1, 2: the first and last that top_p may end in; BINS: none
     if (t < 4) sh.bins[t] = BINS;
@@ -681,22 +695,22 @@ __device__ __forceinline__ void make_plan(Shared &sh, const Row &r, const Binnin
     if (by_k) {
         uint64_t c = n0, x = m0;
         for (int i = i0; i < i0 + PER; ++i) {
-            if (c < (uint64_t)r.k && c + h.count[i] >= (uint64_t)r.k) {
+            if (c < (uint64_t)r.k && c + h.count[slot(i)] >= (uint64_t)r.k) {
                 sh.bins[0] = i;
                 sh.plan.count_k = c;
                 sh.plan.mass_k = x;
             }
-            c += h.count[i], x += h.mass[i];
+            c += h.count[slot(i)], x += h.mass[slot(i)];
         }
     }
     __syncthreads();
     if (by_p) {
         // top_k leaves between mass_k and mass_k + the mass of its bin
         const double least = r.p * (double)(by_k ? sh.plan.mass_k : all_m);
-        const double most = r.p * (double)(by_k ? sh.plan.mass_k + h.mass[sh.bins[0]] : all_m);
+        const double most = r.p * (double)(by_k ? sh.plan.mass_k + h.mass[slot(sh.bins[0])] : all_m);
         uint64_t x = m0;
         for (int i = i0; i < i0 + PER; ++i) {
-            const uint64_t y = x + h.mass[i];
+            const uint64_t y = x + h.mass[slot(i)];
             if (y > x) {        // the first bin whose sum reaches (the largest score's, if that is no more than 0)
                 if ((x == 0 || (double)x < least) && (double)y >= least) {
                     sh.bins[1] = i;
@@ -723,7 +737,7 @@ __device__ __forceinline__ void make_plan(Shared &sh, const Row &r, const Binnin
     uint64_t listed = 0;
     if (by_k) {
         for (int i = i0; i < i0 + PER; ++i)
-            if (i == k || (i >= p1 && i <= p2)) listed += h.count[i];
+            if (i == k || (i >= p1 && i <= p2)) listed += h.count[slot(i)];
     }
     listed = sh.block.sum(listed);
     if (t == 0) {
@@ -751,7 +765,10 @@ struct Listed {
         turn ^= 1;
         if ((threadIdx.x & 63) == 0) to[threadIdx.x >> 6] = v;
         __syncthreads();
-        return to[0] + to[1] + to[2] + to[3];
+        uint64_t all = 0;
+#pragma unroll
+        for (int i = 0; i < NT / 64; ++i) all += to[i];
+        return all;
     }
     // The end of the run of entries in rank order that has n of them (by_mass:
     // that reaches the mass n), among the keys of [lo, most] and with the sum
@@ -842,16 +859,19 @@ __device__ __forceinline__ End end_by_passes(Shared &sh, const SampleArgs &a, in
             __syncthreads();
             pass([&](uint32_t x, int64_t) {
                 if (x >= lo && x <= hi)
-                    atomicAdd((unsigned long long *)&sh.hist.mass[(hi - x) / step], by_mass ? (unsigned long long)wt.mass(x) : 1ull);
+                    atomicAdd((unsigned long long *)&sh.hist.mass[slot((int)((hi - x) / step))], by_mass ? (unsigned long long)wt.mass(x) : 1ull);
             });
             __syncthreads();
-            if (t == 0) {
-                uint64_t m = *above;
-                int i = 0;
-                const int last = (int)((hi - lo) / step);
-                while (i < last && !((double)(m + sh.hist.mass[i]) >= goal && m + sh.hist.mass[i])) m += sh.hist.mass[i++];
-                sh.n = i;
-                sh.base = m;
+            // the bin in which the sum comes to the goal; the last one if it does not
+            const int end = (int)((hi - lo) / step);
+            auto there = [&](uint64_t m) { return m && (double)m >= goal; };
+            uint64_t m = 0, all;
+            for (int i = 8 * t; i < 8 * t + 8; ++i) m += sh.hist.mass[slot(i)];
+            m = *above + sh.block.before(m, &all);
+            for (int i = 8 * t; i < 8 * t + 8; ++i) {
+                const uint64_t next = m + sh.hist.mass[slot(i)];
+                if (!there(m) && (there(next) || (i == end && !there(*above + all)))) sh.n = i, sh.base = m;
+                m = next;
             }
             __syncthreads();
             const uint32_t i = sh.n;
@@ -1002,15 +1022,15 @@ __device__ __forceinline__ void count_bins(Hist &h, const Chunk<T> &ch, const Ro
                                            bool by_k) {
     const bool by_p = r.p < 1.;
     ch.each([&](uint32_t x, int, int) {
-        const int i = bins.bin(x);
+        const int i = slot(bins.bin(x));
         if (by_k) atomicAdd(&h.count[i], 1u);
         if (by_p) atomicAdd((unsigned long long *)&h.mass[i], (unsigned long long)wt.mass(x));
     });
 }
 
-// A work-group a row, up to CHUNK places.
+// A work-group a row, up to a chunk of places.
 template <typename T>
-__global__ void __launch_bounds__(NT) sample_group_kernel(SampleArgs a) {
+__global__ void __launch_bounds__(NT, 3) sample_group_kernel(SampleArgs a) {
     __shared__ Shared sh;
     const int t = threadIdx.x;
     const int64_t b = blockIdx.x;

@@ -215,6 +215,11 @@ __global__ void __launch_bounds__(256) xattn_join_kernel(CrossAttnArgs a) {
 constexpr int tile_keys(gs_dtype t, int waves) { return t == GS_F32 || waves == 1 ? 32 : 64; }
 
 // How the rows and keys are dealt out: waves of a work-group, parts of the keys.
+// Up to 32 rows (a few positions) go to single waves, eight a CU in all if
+// there are keys enough; more rows to work-groups of four, two a CU.  A part is
+// at least 128 keys in bf16 and, as products take eight times as long there,
+// 32 (one tile) in fp32 (4 sequences of 4 x 240, 4 heads of 96 values over one:
+// 13 us, 31 in parts of 128).
 struct Plan {
     int waves, splits, split_keys, row_tiles, dp;
 };
@@ -224,10 +229,10 @@ Plan plan_for(gs_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t
     p.dp = Dh <= 64 ? 64 : 128;
     p.waves = rows <= 32 ? 1 : 4;
     p.row_tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
-    const int64_t groups = B * Hkv * p.row_tiles, tile = tile_keys(t, p.waves);
+    const int64_t groups = B * Hkv * p.row_tiles, tile = tile_keys(t, p.waves), least = t == GS_F32 ? 32 : 128;
     const int64_t want = (p.waves == 1 ? 2048 : 512) / (groups > 0 ? groups : 1);
     int64_t per = (Lk + (want > 1 ? want : 1) - 1) / (want > 1 ? want : 1);
-    if (per < 128) per = 128;
+    if (per < least) per = least;
     per = (per + tile - 1) / tile * tile;
     p.split_keys = (int)per;
     p.splits = (int)((Lk + per - 1) / per);

@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DP == 128 ? 1 : 2)) xa
     typename Op<T>::V q[NS], d[NS];
     load_frags<T, DP>(q, on ? static_cast<const T *>(a.Q) + b * a.q.b + row.i * a.q.l + row.h * a.q.h : nullptr, a.Dh, VEC, l);
     load_frags<T, DP>(d, on ? static_cast<const T *>(a.dO) + b * a.d.b + row.i * a.d.l + row.h * a.d.h : nullptr, a.Dh, VEC, l);
-    const f2v st = on ? a.stat[((int64_t)b * a.Hq + row.h) * a.Lq + row.i] : f2v{-INFINITY, 0.f};
+    f2v st = on ? a.stat[((int64_t)b * a.Hq + row.h) * a.Lq + row.i] : f2v{-INFINITY, 0.f};
     const float c = a.scale * LOG2E;
     const T *const K = static_cast<const T *>(a.K) + b * a.k.b + hk * a.k.h;
     const T *const V = static_cast<const T *>(a.V) + b * a.v.b + hk * a.v.h;
@@ -91,6 +91,26 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DP == 128 ? 1 : 2)) xa
             next_live = live_keys<BN>(mask, j0 + BN, kend, l);
             fetch(j0 + BN, next_live);
         }
+    }
+    if (kl <= BN && j0 < kend) {
+        // Few keys: D as the sum of P dP over the tile, in fp32.  sum_d dO O has
+        // the rounding of O in it, which is small beside dP only where O is an
+        // average over many rows of V.
+        float D = 0.f;
+        lds_barrier();
+#pragma unroll 1
+        for (int n = 0; n < BN / 32; ++n) {
+            f16v p = {0}, g = {0};
+#pragma unroll
+            for (int s = 0; s < NS; ++s) p = Op<T>::mma(row_frag<T, DP>(kt, 32 * n, s, l), q[s], p);
+#pragma unroll
+            for (int s = 0; s < NS; ++s) g = Op<T>::mma(row_frag<T, DP>(vt, 32 * n, s, l), d[s], g);
+            // (a dead key's row of V is zeros, and so is its g)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) D = fmaf(__builtin_amdgcn_exp2f(fmaf(p[r], c, st[0])), g[r], D);
+        }
+        st[1] = D + other_half(D);
+        if (on && l < 32) a.stat[((int64_t)b * a.Hq + row.h) * a.Lq + row.i] = st;
     }
     for (; j0 < kend; j0 += BN) {
         lds_barrier();
@@ -328,28 +348,31 @@ __global__ void __launch_bounds__(256) xattn_parts_kernel(CrossAttnGradArgs a) {
 }
 
 // Parts that bring the work-groups to two a CU, as far as parts of a useful
-// length (64 keys, 2 tiles of 32 query rows) go: each part costs a write and a
-// read of fp32 rows.  Work-groups of two waves instead, so that fewer parts
-// do, were slower: dK and dV of train_ragged 55 us in 2 parts of 64-key
-// work-groups, 39 in 3 of 128-key ones.
+// length go: each costs a write and a read of fp32 rows.  For bf16 that is 64
+// keys or 2 tiles of 32 query rows; for fp32, whose products take eight times
+// as long, half of it (dQ of 29 sequences of 23 x 563, 3 heads of 72 values over
+// one: 27 us in parts of 64 keys, 40 in parts of 128).  Work-groups of two waves instead, so that fewer parts do, were
+// slower: dK and dV of train_ragged 55 us in 2 parts of 64-key work-groups, 39
+// in 3 of 128-key ones.
 struct Plan {
     int dp, q_parts, q_step, k_parts;
 };
-Plan plan_for(int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh) {
+Plan plan_for(gs_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh) {
     Plan p{};
     p.dp = Dh <= 64 ? 64 : 128;
-    const int64_t G = Hq / Hkv;
-    auto parts = [&](int64_t rows, int64_t useful) {
+    const int64_t G = Hq / Hkv, least = t == GS_F32 ? 1 : 2;
+    auto parts = [&](int64_t rows, int64_t most, int64_t useful) {
         const int64_t groups = B * Hkv * ((rows + 127) / 128);
-        int64_t n = groups ? 512 / groups : 1;
+        int64_t n = groups ? most / groups : 1;
         n = n < useful ? n : useful;
         return (int)(n > 1 ? n : 1);
     };
-    const int n = parts(Lq * G, Lk / 64);
-    const int64_t step = ((Lk + n - 1) / n + 63) / 64 * 64;
-    p.q_step = (int)(step ? step : 64);
+    const int n = parts(Lq * G, 512, Lk / (32 * least));
+    const int64_t unit = 32 * least, step = ((Lk + n - 1) / n + unit - 1) / unit * unit;
+    p.q_step = (int)(step ? step : unit);
     p.q_parts = Lk ? (int)((Lk + step - 1) / step) : 1;
-    p.k_parts = parts(Lk, (Lq + 31) / 32 * G / 2);
+    // (fp32 work-groups of 128 values run one a CU)
+    p.k_parts = parts(Lk, t == GS_F32 && p.dp == 128 ? 256 : 512, (Lq + 31) / 32 * G / least);
     return p;
 }
 
@@ -382,8 +405,8 @@ int64_t align4(int64_t n) { return (n + 3) / 4 * 4; }     // (16-byte rows of pa
 
 }  // namespace
 
-size_t cross_attn_grad_workspace(int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh) {
-    const Plan p = plan_for(B, Lq, Lk, Hq, Hkv, Dh);
+size_t cross_attn_grad_workspace(gs_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh) {
+    const Plan p = plan_for(t, B, Lq, Lk, Hq, Hkv, Dh);
     size_t n = (size_t)align4(2 * B * Lq * Hq);
     if (p.q_parts > 1) n += (size_t)(B * Lq * Hq) * p.q_parts * p.dp;
     if (p.k_parts > 1) n += (size_t)(B * Lk * Hkv) * 2 * p.k_parts * p.dp;
@@ -391,7 +414,7 @@ size_t cross_attn_grad_workspace(int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, 
 }
 
 hipError_t launch_cross_attn_grad(gs_dtype t, CrossAttnGradArgs a, void *ws, hipStream_t s) {
-    const Plan p = plan_for(a.B, a.Lq, a.Lk, a.Hq, a.Hkv, a.Dh);
+    const Plan p = plan_for(t, a.B, a.Lq, a.Lk, a.Hq, a.Hkv, a.Dh);
     a.rows = a.Lq * a.G;
     a.row_tiles = (int)(((int64_t)a.rows + 127) / 128);
     a.key_tiles = (int)(((int64_t)a.Lk + 127) / 128);

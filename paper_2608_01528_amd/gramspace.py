@@ -677,10 +677,10 @@ def gs_cross_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, qlen=N
     out; scale 1 / sqrt(Dh) by default.  Any strides but the last dimension's.
     Returns O, or (O, lse) with lse (B, Hq, Lq) fp32."""
     if out is None:
-        out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        out = Q.new_empty(Q.shape)
     if lse_out is None and lse:
         B, Lq, Hq = Q.shape[:3]
-        lse_out = torch.empty((B, Hq, Lq), dtype=torch.float32, device=Q.device)
+        lse_out = Q.new_empty((B, Hq, Lq), dtype=torch.float32)
     p, t = _attn_problem(Q, K, V, out, lse_out, qlen, klen, mask, scale)
     L = lib()
     ws, n, _keep = _workspace(L.gs_cross_attention_workspace(p, t), workspace, Q.device)
@@ -695,7 +695,7 @@ def gs_cross_attention_grad(dO: torch.Tensor, Q: torch.Tensor, K: torch.Tensor, 
     same arguments, from its O and lse.  `out`: three tensors to write into.
     K or V expanded over the batch get the gradients of each sequence."""
     if out is None:
-        out = tuple(torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (Q, K, V))
+        out = tuple(x.new_empty(x.shape) for x in (Q, K, V))
     dQ, dK, dV = out
     p, t = _attn_problem(Q, K, V, O, lse, qlen, klen, mask, scale, (dO, dQ, dK, dV))
     L = lib()
