@@ -672,6 +672,24 @@ __device__ __forceinline__ void clear(Hist &h) {
     for (int i = threadIdx.x; i < BINS; i += NT) h.count[i] = 0, h.mass[i] = 0;
 }
 
+// Lists the entries that the plan asks for, CAP of them at most, in any order.
+template <typename T>
+__device__ __forceinline__ void list_asked(const Chunk<T> &ch, const Plan &p, uint32_t *count, uint64_t *list) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        bool ask[4], any = false;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) any |= ask[c] = p.asks(ch.key[q][c]);       // (no range has key 0)
+        if (!any) continue;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if (!ask[c]) continue;
+            const uint32_t at = atomicAdd(count, 1u);
+            if (at < CAP) list[at] = (uint64_t)ch.key[q][c] << 32 | ch.at(q, c);
+        }
+    }
+}
+
 // The smallest key that min_p keeps.
 __device__ __forceinline__ uint32_t floor_of(const Row &r, const Weigh &wt, uint32_t top) {
     if (!(r.least > 0.)) return 1;
@@ -803,9 +821,42 @@ struct Listed {
     }
 };
 
+// The same for up to 64 entries, by every wave for itself: an entry a lane,
+// compared with all of them.
+__device__ __forceinline__ End end_of_short_list(const Shared &sh, const Row &r, const Weigh &wt, int n) {
+    const Plan &p = sh.plan;
+    const int l = threadIdx.x & 63;
+    const uint64_t v = l < n ? sh.list[l] : 0;
+    const uint32_t key = (uint32_t)(v >> 32), j = (uint32_t)v;
+    const bool in_k = key && p.in_k(key), in_p = key && p.in_p(key);
+    const uint64_t mass = key && r.p < 1. ? wt.mass(key) : 0, mass_p = in_p ? mass : 0;
+    const uint64_t ks = __ballot(in_k);
+    uint64_t before_p = 0;
+    int rank = 0, rank_k = 0;
+    for (int i = 0; i < n; ++i) {
+        const uint32_t k = __builtin_amdgcn_readlane(key, i), ji = __builtin_amdgcn_readlane(j, i);
+        const uint64_t m = read_lane64(mass_p, i);
+        const bool first = k > key || (k == key && ji < j);
+        rank += first;
+        rank_k += first && ((ks >> i) & 1);
+        before_p += first ? m : 0;
+    }
+    bool keep = key && (!in_k || (uint64_t)rank_k + p.count_k < (uint64_t)r.k);
+    if (r.p < 1.) {
+        const uint64_t all = p.k_lo <= p.k_hi ? p.mass_k + wave_sum(keep && in_k ? mass : 0) : p.all;
+        const uint64_t before = p.mass_p + before_p;
+        keep = keep && in_p && (before == 0 || (double)before < r.p * (double)all);
+    }
+    // the last one kept (one is: the run ends among these)
+    const uint32_t last = wave_max(keep ? rank + 1 : 0);
+    const int at = __ffsll((unsigned long long)__ballot(keep && rank + 1 == (int)last)) - 1;
+    return End{(uint32_t)__builtin_amdgcn_readlane(key, at < 0 ? 0 : at), (uint32_t)__builtin_amdgcn_readlane(j, at < 0 ? 0 : at)};
+}
+
 // The end of the run from the listed entries (n <= CAP, in sh.list as key and
 // index): top_k's, then top_p's within it.
 __device__ __forceinline__ End end_of_list(Shared &sh, const Row &r, const Weigh &wt, int n) {
+    if (n <= 64) return end_of_short_list(sh, r, wt, n);
     const Plan p = sh.plan;
     Listed e;
 #pragma unroll
@@ -930,7 +981,10 @@ __device__ __forceinline__ End end_by_passes(Shared &sh, const SampleArgs &a, in
 }
 
 // Masses, by parts, and number of the entries of a chunk that `has` keeps.
-template <typename T, typename F>
+// MOST of them: masses are formed for all, without branches, several side by
+// side; otherwise for those kept, where a wave has any (the nucleus of 200 rows
+// of 128001: 39 us for their list launch, 54 with all masses).
+template <bool MOST, typename T, typename F>
 __device__ __forceinline__ uint64_t chunk_parts(Block &block, const Chunk<T> &ch, const Weigh &wt, F has, uint64_t *mass) {
     const int t = threadIdx.x, l = t & 63, w = t >> 6;
     uint64_t n = 0;
@@ -940,7 +994,15 @@ __device__ __forceinline__ uint64_t chunk_parts(Block &block, const Chunk<T> &ch
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             const uint32_t x = ch.key[q][c];
-            if (x && has(x, ch.at(q, c))) m += wt.mass(x), ++n;
+            const bool on = x && has(x, ch.at(q, c));
+            if constexpr (MOST) {
+                const uint64_t one = wt.mass(x);
+                m += on ? one : 0;
+                n += on;
+            } else if (on) {
+                m += wt.mass(x);
+                ++n;
+            }
         }
         m = wave_sum(m);
         if (l == 0) mass[q * (NT / 64) + w] = m;
@@ -1021,11 +1083,22 @@ template <typename T>
 __device__ __forceinline__ void count_bins(Hist &h, const Chunk<T> &ch, const Row &r, const Weigh &wt, const Binning &bins,
                                            bool by_k) {
     const bool by_p = r.p < 1.;
-    ch.each([&](uint32_t x, int, int) {
-        const int i = slot(bins.bin(x));
-        if (by_k) atomicAdd(&h.count[i], 1u);
-        if (by_p) atomicAdd((unsigned long long *)&h.mass[i], (unsigned long long)wt.mass(x));
-    });
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        uint64_t mass[4];
+        int at[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            at[c] = slot(bins.bin(ch.key[q][c]));
+            mass[c] = by_p ? wt.mass(ch.key[q][c]) : 0;
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if (!ch.key[q][c]) continue;
+            if (by_k) atomicAdd(&h.count[at[c]], 1u);
+            if (by_p) atomicAdd((unsigned long long *)&h.mass[at[c]], (unsigned long long)mass[c]);
+        }
+    }
 }
 
 // A work-group a row, up to a chunk of places.
@@ -1062,11 +1135,7 @@ __global__ void __launch_bounds__(NT, 3) sample_group_kernel(SampleArgs a) {
         const Plan p = sh.plan;
         uint32_t listed = p.listed;
         if (listed <= CAP) {
-            ch.each([&](uint32_t x, int q, int c) {
-                if (!p.asks(x)) return;
-                const uint32_t at = atomicAdd(&sh.n, 1u);
-                if (at < CAP) sh.list[at] = (uint64_t)x << 32 | ch.at(q, c);
-            });
+            list_asked(ch, p, &sh.n, sh.list);
             __syncthreads();
             listed = sh.n;
             __syncthreads();
@@ -1076,7 +1145,7 @@ __global__ void __launch_bounds__(NT, 3) sample_group_kernel(SampleArgs a) {
     }
     const uint32_t floor = floor_of(r, wt, top);
     const uint64_t kept =
-        chunk_parts(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); }, sh.mass);
+        chunk_parts<true>(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); }, sh.mass);
     draw_parts<T>(sh, a, b, wt, end, floor, kept, PARTS, [&](int i) { return sh.mass[i]; });
 }
 
@@ -1135,7 +1204,7 @@ __global__ void __launch_bounds__(NT) sample_bins_kernel(SampleArgs a) {
     const Weigh wt(top, r.c, a.shift, table);
     if (r.keeps_all(a.M)) {
         const uint32_t floor = floor_of(r, wt, top);
-        const uint64_t n = chunk_parts(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= floor; }, cs[chunk].mass);
+        const uint64_t n = chunk_parts<true>(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= floor; }, cs[chunk].mass);
         if (t == 0) cs[chunk].count = (uint32_t)n;
         return;
     }
@@ -1191,12 +1260,8 @@ __global__ void __launch_bounds__(NT) sample_list_kernel(SampleArgs a) {
     if (p.listed > CAP) return;
     const Weigh wt(top, r.c, a.shift, table);
     const uint32_t from = max(p.sure, rs->floor);
-    ch.each([&](uint32_t x, int q, int c) {
-        if (!p.asks(x)) return;
-        const uint32_t at = atomicAdd(&rs->listed, 1u);
-        if (at < CAP) rs->list[at] = (uint64_t)x << 32 | ch.at(q, c);
-    });
-    const uint64_t n = chunk_parts(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= from; }, cs[chunk].mass);
+    list_asked(ch, p, &rs->listed, rs->list);
+    const uint64_t n = chunk_parts<false>(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= from; }, cs[chunk].mass);
     if (t == 0) cs[chunk].count = (uint32_t)n;
 }
 
@@ -1267,7 +1332,7 @@ __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
         Chunk<T> ch;
         for (int i = 0; i < a.chunks; ++i) {
             ch.load(a, b, i);
-            const uint64_t n = chunk_parts(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); },
+            const uint64_t n = chunk_parts<false>(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); },
                                            here ? sh.mass + i * PARTS : cs[i].mass);
             if (t == 0) cs[i].count = (uint32_t)n;
         }
