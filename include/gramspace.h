@@ -540,7 +540,8 @@ gs_status gs_soft_select(const gs_soft_group *groups, int ngroups, gs_dtype pt, 
  * Where K or V stand for several sequences (sb = 0) dK and dV are still those
  * of each sequence.
  *
- *   B, Lq, Lk  sequences, positions and states (each >= 0)
+ *   B, Lq, Lk  sequences, positions and states (each >= 0); B Hkv below 2^23,
+ *              B Hq Lq and B Hkv Lk below 2^31 - 256
  *   Hq, Hkv    heads; Hkv divides Hq      Dh  values a head, 1 <= Dh <= 128
  *   qlen,klen  int32[B] device, nullable (Lq, Lk); taken as 0 below 0 and as Lq
  *              or Lk above

@@ -296,6 +296,7 @@ Span seq_span(const gs_seq &q, const SeqShape &z, size_t es, const char *name) {
 }
 
 constexpr int64_t SEQ_MAX = (int64_t)1 << 31;       // sizes and rows below this
+constexpr int64_t ATTN_MAX_GROUPS = (int64_t)1 << 23;
 constexpr int64_t STRIDE_MAX = (int64_t)1 << 40;    // (elements: byte offsets stay far inside 64 bits)
 
 gs_status check_seq(const char *fn, const char *name, const gs_seq &q, const SeqShape &z, gs_dtype t, bool out) {
@@ -330,6 +331,7 @@ bool attn_sizes(const gs_cross_attn *a) {
     if (a->B >= most || a->Lq >= most || a->Lk >= most || a->Hq >= most) return false;
     // B Hkv (work-groups) and Lq G (packed rows) first, so that no product overflows
     if (a->B * a->Hkv >= most || a->Lq * (a->Hq / a->Hkv) >= most) return false;
+    if (a->B * a->Hkv >= ATTN_MAX_GROUPS) return false;      // (work-groups of 256 threads, counted in 32 bits)
     const int64_t bh = a->B * a->Hkv ? a->B * a->Hkv : 1;
     return a->Lq * (a->Hq / a->Hkv) < most / bh && a->Lk < most / bh;
 }
@@ -338,7 +340,7 @@ gs_status check_attn(const char *fn, const gs_cross_attn *a, gs_dtype t, bool gr
     if (!a) return fail(GS_ERR_ARG, "%s: the problem is null", fn);
     if (!is_batch_type(t)) return fail(GS_ERR_DTYPE, "%s: tensors must be f32 or bf16", fn);
     if (!attn_sizes(a))
-        return fail(GS_ERR_SHAPE, "%s: need B, Lq, Lk >= 0, Hkv >= 1 dividing Hq, 1 <= Dh <= %d, and B Hq Lq and B Hkv Lk below 2^31 - 256",
+        return fail(GS_ERR_SHAPE, "%s: need B, Lq, Lk >= 0, Hkv >= 1 dividing Hq, 1 <= Dh <= %d, B Hkv below 2^23, and B Hq Lq and B Hkv Lk below 2^31 - 256",
                     fn, CROSS_ATTN_MAX_DH);
     if (!(std::fabs(a->scale) >= 1e-30 && std::fabs(a->scale) <= 1e30))
         return fail(GS_ERR_ARG, "%s: |scale| must be in [1e-30, 1e30]", fn);

@@ -286,7 +286,7 @@ struct SampleArgs {
     // set by launch_sample
     int shift;
     void *ws;
-    int64_t row0, row_bytes;
+    int64_t row0, row1, row_bytes;
     int chunks;
 };
 size_t sample_workspace(int64_t B, int64_t M);

@@ -10,10 +10,9 @@
 // What is kept is a run of the entries in rank order (falling scores, equal
 // ones by index), thinned by min_p from its end: top_k and top_p each end it
 // after some entry.  No row is sorted.  Forms by the size of a row:
-//   a thread a row      up to 32 entries, many rows: every pair compared
+//   a thread a row      up to 32 entries: every pair compared
 //   a wave a row        up to 2048 entries, in registers: the end of the run is
-//                       found by halving the range of keys until at most 64
-//                       entries are in question, and these are ranked
+//                       found by halving the range of keys
 //   a work-group a row  up to 8189 entries, in registers: a histogram of the
 //                       scores below the largest finds the bin the run ends in
 //   work-groups a row   more entries: the same over chunks of 8192, in five
@@ -332,8 +331,8 @@ __global__ void __launch_bounds__(256, 4) sample_wave_kernel(SampleArgs a) {
     const int t = threadIdx.x, l = t & 63, wv = __builtin_amdgcn_readfirstlane(t >> 6);
     fill_table(table, t);
     __syncthreads();
-    const int64_t b = (int64_t)blockIdx.x * 4 + wv;
-    if (b >= a.B) return;
+    const int64_t b = a.row0 + (int64_t)blockIdx.x * 4 + wv;
+    if (b >= a.row1) return;
     uint32_t *const lds = rows[wv];
     const T *const row = static_cast<const T *>(a.S) + b * a.lds;
     const int skew = E == 1 ? 0 : skew_of(row);
@@ -437,8 +436,8 @@ __global__ void __launch_bounds__(64) sample_thread_kernel(SampleArgs a) {
     __shared__ uint64_t sorted[P][64];
     fill_table(table, threadIdx.x);
     __syncthreads();
-    const int64_t b = (int64_t)blockIdx.x * 64 + threadIdx.x;
-    if (b >= a.B) return;
+    const int64_t b = a.row0 + (int64_t)blockIdx.x * 64 + threadIdx.x;
+    if (b >= a.row1) return;
     const T *const row = static_cast<const T *>(a.S) + b * a.lds;
     const int M = (int)a.M;
     uint32_t key[P], top = 0;
@@ -1106,7 +1105,7 @@ template <typename T>
 __global__ void __launch_bounds__(NT, 3) sample_group_kernel(SampleArgs a) {
     __shared__ Shared sh;
     const int t = threadIdx.x;
-    const int64_t b = blockIdx.x;
+    const int64_t b = a.row0 + blockIdx.x;
     fill_table(sh.table, t);
     clear(sh.hist);
     Chunk<T> ch;
@@ -1344,51 +1343,70 @@ __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
     else draw_parts<T>(sh, a, b, wt, end, floor, kept, parts, [&](int i) { return cs[i / PARTS].mass[i % PARTS]; });
 }
 
-constexpr int64_t SLAB = 2048;      // rows of a large table in flight: their space is reused
+// Rows a launch: the space of rows that several work-groups share is reused, and
+// the threads of a launch are counted in 32 bits.
+constexpr int64_t SHARED_ROWS = 2048, ROWS = (int64_t)1 << 22;
 
 size_t row_bytes(int64_t chunks) { return sizeof(RowSpace) + (size_t)chunks * sizeof(ChunkSpace); }
 int64_t chunks_of(int64_t M) { return (M + 3 + CHUNK - 1) / CHUNK; }     // (a row's places: its entries and up to 3 before)
 
-template <typename T, int E> hipError_t launch_wave(const SampleArgs &a, hipStream_t s) {
-    sample_wave_kernel<T, E><<<dim3((unsigned)((a.B + 3) / 4)), dim3(256), 0, s>>>(a);
-    return hipGetLastError();
+template <typename T, int E> void launch_wave(const SampleArgs &a, int64_t rows, hipStream_t s) {
+    sample_wave_kernel<T, E><<<dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s>>>(a);
 }
-template <typename T, int P> hipError_t launch_thread(const SampleArgs &a, hipStream_t s) {
-    sample_thread_kernel<T, P><<<dim3((unsigned)((a.B + 63) / 64)), dim3(64), 0, s>>>(a);
-    return hipGetLastError();
+template <typename T, int P> void launch_thread(const SampleArgs &a, int64_t rows, hipStream_t s) {
+    sample_thread_kernel<T, P><<<dim3((unsigned)((rows + 63) / 64)), dim3(64), 0, s>>>(a);
+}
+
+// A thread a row or a wave a row, up to 32 entries (top_k 5 and top_p, fp32, in
+// us, thread and wave):
+//   5 entries   512 rows 5.6, 7.2;   65536 rows 7.8, 72
+//   12 entries  2048 rows 8.9, 8.1;  4096 rows 8.9, 9.9;    65536 rows 9.5, 66
+//   22 entries  8192 rows 13.4, 11.7;  16384 rows 13.5, 18.8;  65536 rows 14.3, 59
+//   32 entries  8192 rows 18.3, 11.7;  16384 rows 18.5, 18.9;  65536 rows 21.6, 59
+bool thread_a_row(int64_t M, int64_t B) { return M <= 8 || (M <= 32 && B >= (M <= 16 ? 4096 : (M <= 24 ? 12288 : 16384))); }
+
+// Rows row0 .. row1 - 1.  A wave a row while its lanes hold the row (2045
+// entries, top_k 50 and top_p, one row: 12 us, a work-group 24; 2000 rows: 17,
+// 83), a work-group while it does (8000 entries, one row: 26 us, shared by
+// work-groups 39; 2000 rows: 93, 147).
+template <typename T> void launch_rows(const SampleArgs &a, hipStream_t s) {
+    const int64_t rows = a.row1 - a.row0, places = a.vec ? a.M : a.M + 3;
+    if (thread_a_row(a.M, a.B)) {
+        if (a.M <= 8) return launch_thread<T, 8>(a, rows, s);
+        if (a.M <= 16) return launch_thread<T, 16>(a, rows, s);
+        return a.M <= 24 ? launch_thread<T, 24>(a, rows, s) : launch_thread<T, 32>(a, rows, s);
+    }
+    if (a.M <= 64) return launch_wave<T, 1>(a, rows, s);
+    if (places <= 256) return launch_wave<T, 4>(a, rows, s);
+    if (places <= 512) return launch_wave<T, 8>(a, rows, s);
+    if (places <= 1024) return launch_wave<T, 16>(a, rows, s);
+    if (places <= 2048) return launch_wave<T, 32>(a, rows, s);
+    if (a.M + 3 <= CHUNK) {
+        sample_group_kernel<T><<<dim3((unsigned)rows), dim3(NT), 0, s>>>(a);
+        return;
+    }
+    // no row with a run to end: launches 3 and 4 have nothing to do
+    const bool all = !a.top_k && !a.top_p && (a.top_k_all <= 1 || a.top_k_all >= a.M) && !(a.top_p_all < 1.f);
+    const dim3 grid((unsigned)(rows * a.chunks)), one((unsigned)rows);
+    sample_top_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
+    sample_bins_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
+    if (!all) {
+        sample_plan_kernel<<<one, dim3(NT), 0, s>>>(a);
+        sample_list_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
+    }
+    sample_draw_kernel<T><<<one, dim3(NT), 0, s>>>(a);
 }
 
 template <typename T> hipError_t launch_typed(SampleArgs a, void *ws, hipStream_t s) {
-    if (a.M <= 32 && a.B >= 4096) {
-        if (a.M <= 8) return launch_thread<T, 8>(a, s);
-        if (a.M <= 16) return launch_thread<T, 16>(a, s);
-        return a.M <= 24 ? launch_thread<T, 24>(a, s) : launch_thread<T, 32>(a, s);
-    }
-    if (a.M <= 64) return launch_wave<T, 1>(a, s);
-    const int64_t places = a.vec ? a.M : a.M + 3;
-    if (places <= 256) return launch_wave<T, 4>(a, s);
-    if (places <= 512) return launch_wave<T, 8>(a, s);
-    if (places <= 1024) return launch_wave<T, 16>(a, s);
-    if (places <= 2048) return launch_wave<T, 32>(a, s);
-    if (a.M + 3 <= CHUNK) {
-        sample_group_kernel<T><<<dim3((unsigned)a.B), dim3(NT), 0, s>>>(a);
-        return hipGetLastError();
-    }
+    const bool shared = a.M + 3 > CHUNK;
     a.chunks = (int)chunks_of(a.M);
     a.row_bytes = row_bytes(a.chunks);
     a.ws = ws;
-    // no row with a run to end: launches 3 and 4 have nothing to do
-    const bool all = !a.top_k && !a.top_p && (a.top_k_all <= 1 || a.top_k_all >= a.M) && !(a.top_p_all < 1.f);
-    for (a.row0 = 0; a.row0 < a.B; a.row0 += SLAB) {
-        const int64_t rows = a.B - a.row0 < SLAB ? a.B - a.row0 : SLAB;
-        const dim3 grid((unsigned)(rows * a.chunks)), one((unsigned)rows);
-        sample_top_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
-        sample_bins_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
-        if (!all) {
-            sample_plan_kernel<<<one, dim3(NT), 0, s>>>(a);
-            sample_list_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
-        }
-        sample_draw_kernel<T><<<one, dim3(NT), 0, s>>>(a);
+    int64_t most = shared ? SHARED_ROWS : ROWS;
+    if (shared && most > ROWS / a.chunks) most = ROWS / a.chunks;
+    for (a.row0 = 0; a.row0 < a.B; a.row0 = a.row1) {
+        a.row1 = a.row0 + most < a.B ? a.row0 + most : a.B;
+        launch_rows<T>(a, s);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -1399,7 +1417,7 @@ template <typename T> hipError_t launch_typed(SampleArgs a, void *ws, hipStream_
 
 size_t sample_workspace(int64_t B, int64_t M) {
     if (M + 3 <= CHUNK) return 0;
-    return (size_t)(B < SLAB ? B : SLAB) * row_bytes(chunks_of(M));
+    return (size_t)(B < SHARED_ROWS ? B : SHARED_ROWS) * row_bytes(chunks_of(M));
 }
 
 hipError_t launch_sample(gs_dtype st, SampleArgs a, void *ws, hipStream_t s) {

@@ -20,26 +20,28 @@ using namespace attn;
 // there and rows without a live key.  A row in DP / PER lanes.
 template <typename T, int DP, bool VEC>
 __global__ void __launch_bounds__(256) xattn_rows_kernel(CrossAttnGradArgs a) {
-    constexpr int PER = Op<T>::PER, LANES = DP / PER;
-    const int64_t at = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-    if (at >= (int64_t)a.B * a.Hq * a.Lq) return;       // (whole rows: LANES divides 64)
+    constexpr int PER = Op<T>::PER, LANES = DP / PER, ROWS = 256 / LANES;      // (LANES divides 64)
     const int c = threadIdx.x % LANES;
-    const int i = (int)(at % a.Lq), h = (int)(at / a.Lq % a.Hq), b = (int)(at / a.Lq / a.Hq);
-    float D = 0.f;
-    if (i < clamped(a.qlen, b, a.Lq)) {
-        const u4v o = load_chunk<T>(static_cast<const T *>(a.O) + b * a.o.b + i * a.o.l + h * a.o.h, PER * c, a.Dh, VEC);
-        const u4v d = load_chunk<T>(static_cast<const T *>(a.dO) + b * a.d.b + i * a.d.l + h * a.d.h, PER * c, a.Dh, VEC);
-        const typename Op<T>::V x = *reinterpret_cast<const typename Op<T>::V *>(&o);
-        const typename Op<T>::V y = *reinterpret_cast<const typename Op<T>::V *>(&d);
+    const int64_t rows = (int64_t)a.B * a.Hq * a.Lq;
+    for (int64_t at = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; at < rows; at += (int64_t)gridDim.x * ROWS) {
+        const int i = (int)(at % a.Lq), h = (int)(at / a.Lq % a.Hq), b = (int)(at / a.Lq / a.Hq);
+        const bool on = i < clamped(a.qlen, b, a.Lq);
+        float D = 0.f;
+        if (on) {
+            const u4v o = load_chunk<T>(static_cast<const T *>(a.O) + b * a.o.b + i * a.o.l + h * a.o.h, PER * c, a.Dh, VEC);
+            const u4v d = load_chunk<T>(static_cast<const T *>(a.dO) + b * a.d.b + i * a.d.l + h * a.d.h, PER * c, a.Dh, VEC);
+            const typename Op<T>::V x = *reinterpret_cast<const typename Op<T>::V *>(&o);
+            const typename Op<T>::V y = *reinterpret_cast<const typename Op<T>::V *>(&d);
 #pragma unroll
-        for (int e = 0; e < PER; ++e) D = fmaf((float)x[e], (float)y[e], D);
+            for (int e = 0; e < PER; ++e) D = fmaf((float)x[e], (float)y[e], D);
+        }
+#pragma unroll
+        for (int x = LANES / 2; x; x /= 2) D += __shfl_xor(D, x);
+        if (c) continue;
+        float e = -LOG2E * a.lse[at];
+        if (!on || e == INFINITY) e = -INFINITY;
+        a.stat[at] = f2v{e, D};
     }
-#pragma unroll
-    for (int x = LANES / 2; x; x /= 2) D += __shfl_xor(D, x);
-    if (c) return;
-    float e = -LOG2E * a.lse[at];
-    if (!(i < clamped(a.qlen, b, a.Lq)) || e == INFINITY) e = -INFINITY;
-    a.stat[at] = f2v{e, D};
 }
 
 // 32 query rows a wave as columns, keys streamed through LDS.
@@ -170,8 +172,9 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DP == 128 ? 1 : 2)) xa
 // one head after those of another, for all heads that share the keys.
 // The keys' rows of V stay in registers, and so do those of K where two waves
 // a SIMD then still fit (256 registers each); bf16 rows of 128 values leave K
-// in LDS, fp32 ones run one wave a SIMD (one wave a SIMD for bf16: 443 us for
-// train_large's 16 x 2048 x 2048 x 4, against TIMEDKV).
+// in LDS, fp32 ones run one wave a SIMD.  (4 x 16 heads of 2048 x 2048, bf16: one
+// wave a SIMD 443 us; two, with tiles through registers, which spill, 430; two,
+// tiles straight to LDS, 348.)
 template <typename T, int DP, bool VEC>
 __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DP == 128 ? 1 : 2)) xattn_dkv_kernel(CrossAttnGradArgs a) {
     constexpr int PER = Op<T>::PER, NS = DP / (2 * PER), NJ = DP / 32, BM = 32, TILE = BM * DP * sizeof(T);
@@ -381,7 +384,9 @@ hipError_t launch_sized(const CrossAttnGradArgs &a, hipStream_t s) {
     const auto grid = [](int64_t n, int64_t per) { return dim3((unsigned)((n + per - 1) / per)); };
     hipError_t e = hipSuccess;
     if (a.q_groups) {
-        xattn_rows_kernel<T, DP, VEC><<<grid((int64_t)a.B * a.Hq * a.Lq, 256 / (DP / Op<T>::PER)), dim3(256), 0, s>>>(a);
+        // (threads of a launch are counted in 32 bits: the rows of very large problems go round)
+        const int64_t rows = (int64_t)a.B * a.Hq * a.Lq, most = (int64_t)1 << 24;
+        xattn_rows_kernel<T, DP, VEC><<<grid(rows < most ? rows : most, 256 / (DP / Op<T>::PER)), dim3(256), 0, s>>>(a);
         xattn_dq_kernel<T, DP, BN, VEC><<<dim3((unsigned)((a.q_groups + 7) / 8 * 8)), dim3(256), 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }

@@ -79,6 +79,7 @@ def test_nothing_to_do(L):
 @pytest.mark.parametrize("change", [
     {"B": -1}, {"Lq": -1}, {"Lk": -2}, {"Hq": 0}, {"Hkv": 0}, {"Hq": 3}, {"Dh": 0}, {"Dh": 129}, {"B": 1 << 31},
     {"Lq": 1 << 62}, {"Lk": 1 << 40}, {"B": 1 << 20, "Lq": 1 << 20}, {"Hq": 1 << 30, "Hkv": 1 << 30, "B": 1 << 30},
+    {"B": 1 << 22, "Lq": 1, "Lk": 1},
     {"Q": (0x10000000, -64, 256, 64)}, {"K": (0x11000000, 1 << 50, 128, 64)},
     {"mask": 0x80000000, "ldm": 4},
 ], ids=str)

@@ -257,3 +257,52 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         for n in eager:
             assert torch.equal(got[n], eager[n]), (seed, n)
+
+
+@pytest.mark.parametrize("seed", range(10))
+def test_drawn_problems(seed):
+    """Sizes, lengths, masks, types and layouts drawn from a seed."""
+    import random
+    rng = random.Random(seed)
+    dtype = rng.choice([BF16, F32])
+    Hkv, G = rng.choice([1, 2, 3]), rng.choice([1, 2, 5])
+    size = (rng.randint(1, 4), rng.choice([1, 2, 7, 33, 130]), rng.randint(1, 400), Hkv * G, Hkv, rng.randint(1, 128))
+    B, Lq, Lk = size[:3]
+    Q, K, V, dO = problem(*size, dtype, seed=100 + seed)
+    if rng.random() < 0.5:
+        K, V = (t.transpose(1, 2).contiguous().transpose(1, 2) for t in (K, V))
+    kw = {"scale": rng.choice([None, 0.5, -0.2])}
+    if rng.random() < 0.6:
+        kw["klen"] = ints(*[rng.randint(0, Lk) for _ in range(B)])
+    if rng.random() < 0.4:
+        kw["qlen"] = ints(*[rng.randint(0, Lq) for _ in range(B)])
+    if rng.random() < 0.4:
+        kw["mask"] = torch.tensor([[rng.random() < 0.7 for _ in range(Lk)] for _ in range(B)], device="cuda")
+    agree(Q, K, V, dO, **kw)
+
+
+def test_outputs_and_workspaces_of_the_caller():
+    Q, K, V, dO = problem(2, 1, 2000, 8, 2, 128, BF16)
+    O, lse = gs.gs_cross_attention(Q, K, V, lse=True)
+    assert torch.equal(gs.gs_cross_attention(Q, K, V), O)           # without the statistics
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    out, stats = torch.empty_like(Q), torch.empty_like(lse)
+    got = gs.gs_cross_attention(Q, K, V, lse=True, out=out, lse_out=stats, workspace=ws)
+    assert got[0] is out and got[1] is stats and torch.equal(out, O) and torch.equal(stats, lse)
+    want = gs.gs_cross_attention_grad(dO, Q, K, V, O, lse)
+    for a, b in zip(gs.gs_cross_attention_grad(dO, Q, K, V, O, lse, workspace=ws), want):
+        assert torch.equal(a, b)
+    with pytest.raises(gs.GramSpaceError, match="workspace"):
+        gs.gs_cross_attention(Q, K, V, workspace=ws[:16])
+    with pytest.raises(gs.GramSpaceError, match="workspace"):
+        gs.gs_cross_attention_grad(dO, Q, K, V, O, lse, workspace=ws[:16])
+
+
+def test_gradient_of_a_row_with_one_state_vanishes():
+    """With one live state the probability is 1 and dS = dP - D is 0: within the
+    rounding of two fp32 sums of the same products in different orders."""
+    for dtype in (BF16, F32):
+        Q, K, V, dO = problem(1, 40, 1, 2, 1, 64, dtype)
+        got = whole(Q, K, V, dO)
+        bound = 64 * 2.0 ** -23 * float((dO.float().abs().sum(-1).max() * V.float().abs().max() * K.float().abs().max()))
+        assert float(got["dQ"].float().abs().max()) <= bound

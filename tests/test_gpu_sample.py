@@ -258,3 +258,59 @@ def test_states_to_entries():
     assert (kept[: 2 * Lq] >= 1).all() and (lse[2] == -INF).all()
     # the sequence without states has equal scores (0) everywhere: nine tenths of the entries are kept
     assert (kept[2 * Lq:] == 87).all() and torch.allclose(prob[2 * Lq:], torch.full((Lq,), 1 / 87.0, device="cuda"))
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_drawn_settings(seed):
+    """Sizes, types, spreads, ties and parameters drawn from a seed."""
+    import random
+    rng = random.Random(seed)
+    M = int(round(2 ** rng.uniform(0, 17)))
+    B = rng.randint(1, 12)
+    S, u = scores(B, M, seed=50 + seed, dtype=rng.choice([torch.float32, torch.bfloat16]),
+                  spread=rng.choice([0.01, 1.0, 3.0, 20.0]), out=rng.choice([0.0, 0.3, 0.95]))
+    if rng.random() < 0.3:
+        S = torch.round(S)
+    for _ in range(6):
+        p = {}
+        if rng.random() < 0.7:
+            p["temperature"] = rng.choice([0.3, 0.8, 1.0, 4.0])
+        if rng.random() < 0.5:
+            p["top_k"] = rng.choice([1, 3, 40, 70, 130, 1000, M])
+        if rng.random() < 0.6:
+            p["top_p"] = rng.choice([0.01, 0.5, 0.9, 0.999])
+        if rng.random() < 0.4:
+            p["min_p"] = rng.choice([1e-30, 1e-3, 0.2, 0.9])
+        agree(S, u, **p)
+
+
+def test_more_rows_than_a_launch_takes():
+    """Rows beyond the 2^22 of one launch, and beyond the 2048 that share a
+    workspace, are drawn like any others."""
+    for B, M, at in ((2 ** 22 + 5, 33, [0, 2 ** 22 - 1, 2 ** 22, 2 ** 22 + 4]), (2 ** 22 + 70, 3, [2 ** 22 + 69]),
+                     (2048 + 3, 9000, [0, 2047, 2048, 2050])):
+        g = torch.Generator(device="cuda").manual_seed(1)
+        S = torch.randn(B, M, generator=g, device="cuda", dtype=torch.bfloat16)
+        u = torch.rand(B, generator=g, device="cuda")
+        p = {"top_k": 7, "top_p": 0.9}
+        idx = gs.gs_sample(S, u, **p)
+        pick = torch.tensor(at, device="cuda")
+        assert torch.equal(idx[pick], gs.gs_sample(S[pick].contiguous(), u[pick].contiguous(), **p))
+        assert int(idx.min()) >= 0 and int(idx.max()) < M
+
+
+def test_outputs_and_workspaces_of_the_caller():
+    S, u = scores(3, 50000)
+    want = gs.gs_sample(S, u, top_p=0.9)
+    ws = torch.empty(8 << 20, dtype=torch.uint8, device="cuda")
+    ws.fill_(255)
+    out = torch.empty(3, dtype=torch.int32, device="cuda")
+    assert gs.gs_sample(S, u, top_p=0.9, idx_out=out, workspace=ws) is out and torch.equal(out, want)
+    with pytest.raises(gs.GramSpaceError, match="workspace"):
+        gs.gs_sample(S, u, top_p=0.9, workspace=ws[:1024])
+    with pytest.raises(ValueError):
+        gs.gs_sample(S, u[:2])
+    with pytest.raises(ValueError):
+        gs.gs_sample(S, u, top_k=torch.ones(3, device="cuda"))
+    with pytest.raises(ValueError):
+        gs.gs_sample(S, u.cpu())
