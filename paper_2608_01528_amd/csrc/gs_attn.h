@@ -61,6 +61,11 @@ template <> struct Op<float> {
     }
 };
 
+// Heads of Dh values are computed with as DC = 64, 96 or 128 of them (zeros behind
+// the last) and lie in LDS, and in parts of rows, as DP = 64 or 128.
+constexpr int padded(int dc) { return dc <= 64 ? 64 : 128; }
+inline int computed(int64_t dh) { return dh <= 64 ? 64 : (dh <= 96 ? 96 : 128); }
+
 // A tile in LDS: rows of DP values in 16-byte chunks, chunk c of row r at
 // position c ^ swizzle(r).  256 bytes of LDS (64 banks) are one row or several:
 // 16 consecutive rows put the same chunk on 16 different places of those
@@ -152,11 +157,11 @@ __device__ __forceinline__ int clamped(const int32_t *len, int b, int most) {
 
 // Fragments of the side that stays in registers: row's values as the column
 // l % 32 of a product; a null row gives zeros.
-template <typename T, int DP>
-__device__ __forceinline__ void load_frags(typename Op<T>::V (&f)[DP / (2 * Op<T>::PER)], const T *row, int dh, bool vec, int l) {
+template <typename T, int DC>
+__device__ __forceinline__ void load_frags(typename Op<T>::V (&f)[DC / (2 * Op<T>::PER)], const T *row, int dh, bool vec, int l) {
     constexpr int PER = Op<T>::PER;
 #pragma unroll
-    for (int s = 0; s < DP / (2 * PER); ++s) {
+    for (int s = 0; s < DC / (2 * PER); ++s) {
         u4v v = {0, 0, 0, 0};
         if (row) v = load_chunk<T>(row, PER * (2 * s + (l >> 5)), dh, vec);
         f[s] = *reinterpret_cast<const typename Op<T>::V *>(&v);

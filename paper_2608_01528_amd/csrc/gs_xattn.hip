@@ -12,13 +12,13 @@ namespace {
 using namespace attn;
 
 // Waves a SIMD that registers are kept for: fp32 fragments take twice the
-// registers of bf16 ones, and those with 128 values, or of a single wave (which
+// registers of bf16 ones, and those with more than 64 values, or of a single wave (which
 // carries whole tiles), would spill at two.
-template <typename T, int DP, int NW> constexpr int min_waves() { return sizeof(T) == 4 && (DP == 128 || NW == 1) ? 1 : 2; }
+template <typename T, int DC, int NW> constexpr int min_waves() { return sizeof(T) == 4 && (DC > 64 || NW == 1) ? 1 : 2; }
 
-template <typename T, int DP, int NW, int BN, bool VEC>
-__global__ void __launch_bounds__(64 * NW, (min_waves<T, DP, NW>())) xattn_kernel(CrossAttnArgs a) {
-    constexpr int PER = Op<T>::PER, NS = DP / (2 * PER), NJ = DP / 32, NT = 64 * NW;
+template <typename T, int DC, int NW, int BN, bool VEC>
+__global__ void __launch_bounds__(64 * NW, (min_waves<T, DC, NW>())) xattn_kernel(CrossAttnArgs a) {
+    constexpr int DP = padded(DC), PER = Op<T>::PER, NS = DC / (2 * PER), NJ = DC / 32, NT = 64 * NW;
     constexpr int TILE = BN * DP * sizeof(T);
     __shared__ __attribute__((aligned(16))) char lds[4 * TILE];     // two of K, two of V
     const int t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, DP, NW>())) xattn_kerne
     if ((rt * 32 * NW) / a.G >= ql) kend = 0;           // no row of the tile is there
 
     typename Op<T>::V q[NS];
-    load_frags<T, DP>(q, on ? static_cast<const T *>(a.Q) + b * a.q.b + row.i * a.q.l + row.h * a.q.h : nullptr, a.Dh, VEC, l);
+    load_frags<T, DC>(q, on ? static_cast<const T *>(a.Q) + b * a.q.b + row.i * a.q.l + row.h * a.q.h : nullptr, a.Dh, VEC, l);
     // scores in units of log 2; a negative scale turns the queries round, so
     // that the largest product is the largest score
     const float c = fabsf(a.scale) * LOG2E;
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(256) xattn_join_kernel(CrossAttnArgs a) {
     constexpr int LANES = DP / 4;
     const int64_t at = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
     const int d = 4 * (threadIdx.x % LANES);
-    if (at >= (int64_t)a.B * a.Hkv * a.rows) return;
+    if (at >= (int64_t)a.B * a.Hkv * a.rows || d >= a.Dh) return;
     const int bh = (int)(at / a.rows), m = (int)(at % a.rows);
     const int b = bh / a.Hkv;
     const RowOf row(m, bh % a.Hkv, a.G);
@@ -226,7 +226,7 @@ struct Plan {
 Plan plan_for(gs_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh) {
     Plan p{};
     const int64_t rows = Lq * (Hq / Hkv);
-    p.dp = Dh <= 64 ? 64 : 128;
+    p.dp = padded(computed(Dh));
     p.waves = rows <= 32 ? 1 : 4;
     p.row_tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
     const int64_t groups = B * Hkv * p.row_tiles, tile = tile_keys(t, p.waves), least = t == GS_F32 ? 32 : 128;
@@ -240,9 +240,10 @@ Plan plan_for(gs_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t
     return p;
 }
 
-template <typename T, int DP, int NW, int BN, bool VEC>
+template <typename T, int DC, int NW, int BN, bool VEC>
 hipError_t launch_rows(const CrossAttnArgs &a, hipStream_t s) {
-    xattn_kernel<T, DP, NW, BN, VEC><<<dim3((unsigned)((a.groups + 7) / 8 * 8)), dim3(64 * NW), 0, s>>>(a);
+    constexpr int DP = padded(DC);
+    xattn_kernel<T, DC, NW, BN, VEC><<<dim3((unsigned)((a.groups + 7) / 8 * 8)), dim3(64 * NW), 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t rows = (int64_t)a.B * a.Hkv * a.rows, per = 256 / (DP / 4);
@@ -250,11 +251,13 @@ hipError_t launch_rows(const CrossAttnArgs &a, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <typename T, bool VEC>
-hipError_t launch_typed(const CrossAttnArgs &a, int dp, int waves, hipStream_t s) {
-    constexpr int BN = sizeof(T) == 4 ? 32 : 64;
-    if (dp == 64) return waves == 1 ? launch_rows<T, 64, 1, 32, VEC>(a, s) : launch_rows<T, 64, 4, BN, VEC>(a, s);
-    return waves == 1 ? launch_rows<T, 128, 1, 32, VEC>(a, s) : launch_rows<T, 128, 4, BN, VEC>(a, s);
+template <typename T, int DC, bool VEC> hipError_t launch_waves(const CrossAttnArgs &a, int waves, hipStream_t s) {
+    return waves == 1 ? launch_rows<T, DC, 1, 32, VEC>(a, s) : launch_rows<T, DC, 4, sizeof(T) == 4 ? 32 : 64, VEC>(a, s);
+}
+template <typename T, bool VEC> hipError_t launch_typed(const CrossAttnArgs &a, int waves, hipStream_t s) {
+    const int dc = computed(a.Dh);
+    if (dc == 64) return launch_waves<T, 64, VEC>(a, waves, s);
+    return dc == 96 ? launch_waves<T, 96, VEC>(a, waves, s) : launch_waves<T, 128, VEC>(a, waves, s);
 }
 
 }  // namespace
@@ -276,8 +279,8 @@ hipError_t launch_cross_attn(gs_dtype t, CrossAttnArgs a, void *ws, hipStream_t 
     a.part_lse = a.part + (int64_t)a.B * a.Hkv * a.rows * p.splits * p.dp;
     // tiles are read with 32-bit offsets: rows of a tile within 2^31 bytes
     a.vec = a.vec && a.k.l < ATTN_VEC_STRIDE && a.v.l < ATTN_VEC_STRIDE;
-    if (t == GS_F32) return a.vec ? launch_typed<float, true>(a, p.dp, p.waves, s) : launch_typed<float, false>(a, p.dp, p.waves, s);
-    return a.vec ? launch_typed<bf16_t, true>(a, p.dp, p.waves, s) : launch_typed<bf16_t, false>(a, p.dp, p.waves, s);
+    if (t == GS_F32) return a.vec ? launch_typed<float, true>(a, p.waves, s) : launch_typed<float, false>(a, p.waves, s);
+    return a.vec ? launch_typed<bf16_t, true>(a, p.waves, s) : launch_typed<bf16_t, false>(a, p.waves, s);
 }
 
 }  // namespace gs

@@ -45,9 +45,9 @@ __global__ void __launch_bounds__(256) xattn_rows_kernel(CrossAttnGradArgs a) {
 }
 
 // 32 query rows a wave as columns, keys streamed through LDS.
-template <typename T, int DP, int BN, bool VEC>
-__global__ void __launch_bounds__(256, (sizeof(T) == 4 && DP == 128 ? 1 : 2)) xattn_dq_kernel(CrossAttnGradArgs a) {
-    constexpr int PER = Op<T>::PER, NS = DP / (2 * PER), NJ = DP / 32, TILE = BN * DP * sizeof(T);
+template <typename T, int DC, int BN, bool VEC>
+__global__ void __launch_bounds__(256, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xattn_dq_kernel(CrossAttnGradArgs a) {
+    constexpr int DP = padded(DC), PER = Op<T>::PER, NS = DC / (2 * PER), NJ = DC / 32, TILE = BN * DP * sizeof(T);
     __shared__ __attribute__((aligned(16))) char lds[4 * TILE];
     const int t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
     const int64_t L = logical_group(a.q_groups);
@@ -65,8 +65,8 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DP == 128 ? 1 : 2)) xa
     if (rt * 128 / a.G >= ql) kend = 0;
 
     typename Op<T>::V q[NS], d[NS];
-    load_frags<T, DP>(q, on ? static_cast<const T *>(a.Q) + b * a.q.b + row.i * a.q.l + row.h * a.q.h : nullptr, a.Dh, VEC, l);
-    load_frags<T, DP>(d, on ? static_cast<const T *>(a.dO) + b * a.d.b + row.i * a.d.l + row.h * a.d.h : nullptr, a.Dh, VEC, l);
+    load_frags<T, DC>(q, on ? static_cast<const T *>(a.Q) + b * a.q.b + row.i * a.q.l + row.h * a.q.h : nullptr, a.Dh, VEC, l);
+    load_frags<T, DC>(d, on ? static_cast<const T *>(a.dO) + b * a.d.b + row.i * a.d.l + row.h * a.d.h : nullptr, a.Dh, VEC, l);
     f2v st = on ? a.stat[((int64_t)b * a.Hq + row.h) * a.Lq + row.i] : f2v{-INFINITY, 0.f};
     const float c = a.scale * LOG2E;
     const T *const K = static_cast<const T *>(a.K) + b * a.k.b + hk * a.k.h;
@@ -175,10 +175,10 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DP == 128 ? 1 : 2)) xa
 // in LDS, fp32 ones run one wave a SIMD.  (4 x 16 heads of 2048 x 2048, bf16: one
 // wave a SIMD 443 us; two, with tiles through registers, which spill, 430; two,
 // tiles straight to LDS, 348.)
-template <typename T, int DP, bool VEC>
-__global__ void __launch_bounds__(256, (sizeof(T) == 4 && DP == 128 ? 1 : 2)) xattn_dkv_kernel(CrossAttnGradArgs a) {
-    constexpr int PER = Op<T>::PER, NS = DP / (2 * PER), NJ = DP / 32, BM = 32, TILE = BM * DP * sizeof(T);
-    constexpr bool KEEP_K = !(sizeof(T) == 2 && DP == 128);
+template <typename T, int DC, bool VEC>
+__global__ void __launch_bounds__(256, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xattn_dkv_kernel(CrossAttnGradArgs a) {
+    constexpr int DP = padded(DC), PER = Op<T>::PER, NS = DC / (2 * PER), NJ = DC / 32, BM = 32, TILE = BM * DP * sizeof(T);
+    constexpr bool KEEP_K = !(sizeof(T) == 2 && DC == 128);
     __shared__ __attribute__((aligned(16))) char lds[4 * TILE + (KEEP_K ? 0 : 128 * DP * sizeof(T))];
     __shared__ __attribute__((aligned(16))) f2v stat[2 * BM];
     char *const keys_lds = lds + 4 * TILE;
@@ -204,13 +204,13 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DP == 128 ? 1 : 2)) xa
     int g = __builtin_amdgcn_readfirstlane(tiles ? n / tiles : 0), x = n - g * tiles;     // head and tile of the next fetch
 
     typename Op<T>::V k[NS], v[NS];
-    load_frags<T, DP>(k, on ? static_cast<const T *>(a.K) + b * a.k.b + j * a.k.l + hk * a.k.h : nullptr, a.Dh, VEC, l);
+    load_frags<T, DC>(k, on ? static_cast<const T *>(a.K) + b * a.k.b + j * a.k.l + hk * a.k.h : nullptr, a.Dh, VEC, l);
     if constexpr (!KEEP_K) {    // (read back by the wave that writes them)
 #pragma unroll
         for (int y = 0; y < NS; ++y)
             *reinterpret_cast<typename Op<T>::V *>(keys_lds + place<T, DP>(32 * w + (l & 31), 2 * y + (l >> 5))) = k[y];
     }
-    load_frags<T, DP>(v, on ? static_cast<const T *>(a.V) + b * a.v.b + j * a.v.l + hk * a.v.h : nullptr, a.Dh, VEC, l);
+    load_frags<T, DC>(v, on ? static_cast<const T *>(a.V) + b * a.v.b + j * a.v.l + hk * a.v.h : nullptr, a.Dh, VEC, l);
     const float c = a.scale * LOG2E;
     f16v dk[NJ], dv[NJ];
 #pragma unroll
@@ -321,6 +321,7 @@ __global__ void __launch_bounds__(256) xattn_parts_kernel(CrossAttnGradArgs a) {
     const int d = 4 * (threadIdx.x % LANES);
     int64_t at = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
     const int64_t qrows = (int64_t)a.B * a.Hkv * a.rows, keys = (int64_t)a.B * a.Hkv * a.Lk;
+    if (d >= a.Dh) return;
     const float *p;
     T *out;
     int parts;
@@ -362,7 +363,7 @@ struct Plan {
 };
 Plan plan_for(gs_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh) {
     Plan p{};
-    p.dp = Dh <= 64 ? 64 : 128;
+    p.dp = padded(computed(Dh));
     const int64_t G = Hq / Hkv, least = t == GS_F32 ? 1 : 2;
     auto parts = [&](int64_t rows, int64_t most, int64_t useful) {
         const int64_t groups = B * Hkv * ((rows + 127) / 128);
@@ -379,19 +380,19 @@ Plan plan_for(gs_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t
     return p;
 }
 
-template <typename T, int DP, int BN, bool VEC>
-hipError_t launch_sized(const CrossAttnGradArgs &a, hipStream_t s) {
+template <typename T, int DC, bool VEC> hipError_t launch_sized(const CrossAttnGradArgs &a, hipStream_t s) {
+    constexpr int DP = padded(DC), BN = sizeof(T) == 4 ? 32 : 64;
     const auto grid = [](int64_t n, int64_t per) { return dim3((unsigned)((n + per - 1) / per)); };
     hipError_t e = hipSuccess;
     if (a.q_groups) {
         // (threads of a launch are counted in 32 bits: the rows of very large problems go round)
         const int64_t rows = (int64_t)a.B * a.Hq * a.Lq, most = (int64_t)1 << 24;
         xattn_rows_kernel<T, DP, VEC><<<grid(rows < most ? rows : most, 256 / (DP / Op<T>::PER)), dim3(256), 0, s>>>(a);
-        xattn_dq_kernel<T, DP, BN, VEC><<<dim3((unsigned)((a.q_groups + 7) / 8 * 8)), dim3(256), 0, s>>>(a);
+        xattn_dq_kernel<T, DC, BN, VEC><<<dim3((unsigned)((a.q_groups + 7) / 8 * 8)), dim3(256), 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (a.k_groups) {
-        xattn_dkv_kernel<T, DP, VEC><<<dim3((unsigned)((a.k_groups + 7) / 8 * 8)), dim3(256), 0, s>>>(a);
+        xattn_dkv_kernel<T, DC, VEC><<<dim3((unsigned)((a.k_groups + 7) / 8 * 8)), dim3(256), 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (a.join_q + a.join_k) {
@@ -401,9 +402,10 @@ hipError_t launch_sized(const CrossAttnGradArgs &a, hipStream_t s) {
     return e;
 }
 
-template <typename T, int BN> hipError_t launch_typed(const CrossAttnGradArgs &a, int dp, hipStream_t s) {
-    if (dp == 64) return a.vec ? launch_sized<T, 64, BN, true>(a, s) : launch_sized<T, 64, BN, false>(a, s);
-    return a.vec ? launch_sized<T, 128, BN, true>(a, s) : launch_sized<T, 128, BN, false>(a, s);
+template <typename T, bool VEC> hipError_t launch_typed(const CrossAttnGradArgs &a, hipStream_t s) {
+    const int dc = computed(a.Dh);
+    if (dc == 64) return launch_sized<T, 64, VEC>(a, s);
+    return dc == 96 ? launch_sized<T, 96, VEC>(a, s) : launch_sized<T, 128, VEC>(a, s);
 }
 
 int64_t align4(int64_t n) { return (n + 3) / 4 * 4; }     // (16-byte rows of parts behind the rows' constants)
@@ -436,7 +438,8 @@ hipError_t launch_cross_attn_grad(gs_dtype t, CrossAttnGradArgs a, void *ws, hip
     a.dkv_part = a.dq_part + a.join_q * p.q_parts * p.dp;
     // tiles are read with 32-bit offsets: rows of a tile within 2^31 bytes
     for (const SeqStrides *x : {&a.q, &a.k, &a.v, &a.d}) a.vec = a.vec && x->l < ATTN_VEC_STRIDE;
-    return t == GS_F32 ? launch_typed<float, 32>(a, p.dp, s) : launch_typed<bf16_t, 64>(a, p.dp, s);
+    if (t == GS_F32) return a.vec ? launch_typed<float, true>(a, s) : launch_typed<float, false>(a, s);
+    return a.vec ? launch_typed<bf16_t, true>(a, s) : launch_typed<bf16_t, false>(a, s);
 }
 
 }  // namespace gs
