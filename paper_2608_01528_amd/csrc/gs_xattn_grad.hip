@@ -107,9 +107,12 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xatt
             for (int s = 0; s < NS; ++s) p = Op<T>::mma(row_frag<T, DP>(kt, 32 * n, s, l), q[s], p);
 #pragma unroll
             for (int s = 0; s < NS; ++s) g = Op<T>::mma(row_frag<T, DP>(vt, 32 * n, s, l), d[s], g);
-            // (a dead key's row of V is zeros, and so is its g)
+            // (a dead key's score is 0 here, which a row of very negative scores
+            // makes an infinite probability)
+            const uint32_t bits = (uint32_t)(live >> (32 * n)) >> (4 * (l >> 5));
 #pragma unroll
-            for (int r = 0; r < 16; ++r) D = fmaf(__builtin_amdgcn_exp2f(fmaf(p[r], c, st[0])), g[r], D);
+            for (int r = 0; r < 16; ++r)
+                D += (bits >> (8 * (r / 4) + r % 4)) & 1 ? __builtin_amdgcn_exp2f(fmaf(p[r], c, st[0])) * g[r] : 0.f;
         }
         st[1] = D + other_half(D);
         if (on && l < 32) a.stat[((int64_t)b * a.Hq + row.h) * a.Lq + row.i] = st;

@@ -174,6 +174,19 @@ def test_large_scores_and_scales(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("Lk", [1, 3, 30, 45, 64, 150])
+def test_scores_far_below_zero(Lk, dtype):
+    """Every score some hundreds below 0, the score that a left-out state's zeros
+    would have: exp(0 - lse) is infinite."""
+    Q, K, V, dO = problem(2, 40, Lk, 4, 2, 64, dtype)
+    Q, K = Q.abs() * 2, -K.abs() * 2
+    agree(Q, K, V, dO, scale=1.5)
+    if Lk > 1:
+        mask = (torch.arange(Lk, device="cuda")[None] % 3 != 1).repeat(2, 1)
+        agree(Q, K, V, dO, scale=1.5, klen=ints(Lk, Lk - 1), mask=mask)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 def test_gradient_against_differences(dtype):
     """<gradient, E> against the central difference of sum(O dO) along E in 64
     bits (step 1e-4: its own error is below 1e-6 of the terms)."""
