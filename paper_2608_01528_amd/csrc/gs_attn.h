@@ -66,6 +66,35 @@ template <> struct Op<float> {
 constexpr int padded(int dc) { return dc <= 64 ? 64 : 128; }
 inline int computed(int64_t dh) { return dh <= 64 ? 64 : (dh <= 96 ? 96 : 128); }
 
+// How blocks of 128 rows (or keys), each of which runs over `pieces` tiles of the
+// other side, are dealt out: to work-groups of four waves or of eight, whose two
+// halves share the tiles, and every block's tiles to `parts` work-groups, whose
+// results another launch adds up.
+struct Deal {
+    int waves, parts;
+};
+// The deal that should take least time.  piece_us: a tile's time in a work-group
+// of four waves that shares its CU with another one (alone, it takes 0.65 of
+// that; eight waves take two tiles in that time); a work-group takes about 3 us
+// besides.  `single`: one work-group of four waves a CU.  part_us: the time to
+// write and read one part of every block.
+inline Deal deal_out(int64_t blocks, int64_t pieces, bool single, double piece_us, double part_us) {
+    Deal best = {4, 1};
+    double least = 1e300;
+    for (int64_t n = 1; n <= pieces && n <= 256 && (n == 1 || blocks * n <= 4096); n += n < 8 ? 1 : n / 4) {
+        const int64_t groups = blocks * n;
+        const double len = (double)((pieces + n - 1) / n), more = n > 1 ? 4. + (double)n * part_us : 0.;
+        const double last = groups % 512 == 0 ? 0. : (groups % 512 <= 256 ? 0.65 : 1.);
+        const double rounds = single ? (double)((groups + 255) / 256) : (double)(groups / 512) + last;
+        const double four = rounds * (len * piece_us + 3.) + more;
+        if (four < least) least = four, best = {4, (int)n};
+        if (single || pieces < 2) continue;
+        const double eight = (double)((groups + 255) / 256) * (ceil(len / 2.) * piece_us + 3.5) + more;
+        if (eight < least) least = eight, best = {8, (int)n};
+    }
+    return best;
+}
+
 // A tile in LDS: rows of DP values in 16-byte chunks, chunk c of row r at
 // position c ^ swizzle(r).  256 bytes of LDS (64 banks) are one row or several:
 // 16 consecutive rows put the same chunk on 16 different places of those
@@ -242,19 +271,37 @@ template <int NT> __device__ __forceinline__ void clear_lds(char *p, int bytes, 
 // All of this wave's loads have landed (vmcnt 0).
 __device__ __forceinline__ void wait_tiles() { __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8)); }
 
+// Waits until matrix products have written their results (19 cycles at most).
+// hipcc counts these waits itself, but where a branch lies between the products
+// and the end of their loop it can (ROCm 7.2) count the longer way round the
+// branch for both, and sums are read before they are written.  It did so in one
+// instance, which calls this; a test looks at the code of all of them.
+template <int N> __device__ __forceinline__ void products_done(f16v (&o)[N]) {
+    static_assert(N == 2, "the results are named one by one");
+    asm volatile("s_nop 15\n\ts_nop 3" : "+v"(o[0]), "+v"(o[1]));
+}
+
 // A row's position and head: packed row m = position G + head within the group.
 struct RowOf {
     int i, h;
     __device__ __forceinline__ RowOf(int m, int hk, int G) : i(m / G), h(hk * G + m % G) {}
 };
 
-// Bit n: key j0 + n takes part (n < BN).
-template <int BN> __device__ __forceinline__ uint64_t live_keys(const uint8_t *mask, int j0, int kend, int l) {
-    const int j = j0 + l;
-    bool on = l < BN && j < kend;
-    if (on && mask) on = mask[j] != 0;
-    return __ballot(on);
-}
+// Which keys of a tile take part.  The mask's bytes are asked for a tile before
+// they are needed: the loads of K and V are issued by them, and would wait for
+// them otherwise.
+template <int BN> struct LiveKeys {
+    const uint8_t *mask;
+    int kend, l;
+    uint8_t byte;
+    __device__ __forceinline__ bool there(int j0) const { return l < BN && j0 + l < kend; }
+    __device__ __forceinline__ void ahead(int j0) {
+        byte = 1;
+        if (mask && there(j0)) byte = mask[j0 + l];
+    }
+    // bit n: key j0 + n takes part (of the tile last asked for)
+    __device__ __forceinline__ uint64_t take(int j0) const { return __ballot(there(j0) && byte != 0); }
+};
 template <int BN> constexpr uint64_t ALL_LIVE = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
 
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }

@@ -16,12 +16,13 @@ using namespace attn;
 // carries whole tiles), would spill at two.
 template <typename T, int DC, int NW> constexpr int min_waves() { return sizeof(T) == 4 && (DC > 64 || NW == 1) ? 1 : 2; }
 
-template <typename T, int DC, int NW, int BN, bool VEC>
-__global__ void __launch_bounds__(64 * NW, (min_waves<T, DC, NW>())) xattn_kernel(CrossAttnArgs a) {
+template <typename T, int DC, int NW, int GR, int BN, bool VEC>
+__global__ void __launch_bounds__(64 * NW * GR, (min_waves<T, DC, NW>())) xattn_kernel(CrossAttnArgs a) {
     constexpr int DP = padded(DC), PER = Op<T>::PER, NS = DC / (2 * PER), NJ = DC / 32, NT = 64 * NW;
-    constexpr int TILE = BN * DP * sizeof(T);
-    __shared__ __attribute__((aligned(16))) char lds[4 * TILE];     // two of K, two of V
-    const int t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+    constexpr int TILE = BN * DP * sizeof(T), STEP = GR * BN;
+    __shared__ __attribute__((aligned(16))) char lds[GR * 4 * TILE];        // two of K, two of V for each group
+    const int t = threadIdx.x % NT, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int group = GR > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0, mine = group * BN;
     const int64_t L = logical_group(a.groups);
     if (L >= a.groups) return;
     const int rt = (int)(L % a.row_tiles);
@@ -53,7 +54,7 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, DC, NW>())) xattn_kerne
     }
     const T *const K = static_cast<const T *>(a.K) + b * a.k.b + hk * a.k.h;
     const T *const V = static_cast<const T *>(a.V) + b * a.v.b + hk * a.v.h;
-    const uint8_t *const mask = a.mask ? a.mask + b * a.mask_ld : nullptr;
+    LiveKeys<BN> keys{a.mask ? a.mask + b * a.mask_ld : nullptr, kend, l, 0};
 
     f16v o[NJ];
 #pragma unroll
@@ -66,19 +67,22 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, DC, NW>())) xattn_kerne
         kr.fetch(K + (int64_t)j * a.k.l, a.k.l, on, a.Dh, t);
         vr.fetch(V + (int64_t)j * a.v.l, a.v.l, on, a.Dh, t);
     };
-    char *kt = lds, *vt = lds + TILE;       // the tile in use; the next goes 2 TILE on, or back
+    char *kt = lds + group * 4 * TILE, *vt = kt + TILE;       // the tile in use; the next goes 2 TILE on, or back
     int other = 2 * TILE;
     if (j0 < kend) {
-        live = live_keys<BN>(mask, j0, kend, l);
-        fetch(j0, live);
+        keys.ahead(j0 + mine);
+        live = keys.take(j0 + mine);
+        keys.ahead(j0 + STEP + mine);
+        fetch(j0 + mine, live);
         kr.stash(kt, t);
         vr.stash(vt, t);
-        if (j0 + BN < kend) {
-            next_live = live_keys<BN>(mask, j0 + BN, kend, l);
-            fetch(j0 + BN, next_live);
+        if (j0 + STEP < kend) {
+            next_live = keys.take(j0 + STEP + mine);
+            keys.ahead(j0 + 2 * STEP + mine);
+            fetch(j0 + STEP + mine, next_live);
         }
     }
-    for (; j0 < kend; j0 += BN) {
+    for (; j0 < kend; j0 += STEP) {
         lds_barrier();
         f16v p[BN / 32];
 #pragma unroll
@@ -135,16 +139,45 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, DC, NW>())) xattn_kerne
         vt += other;
         other = -other;
         live = next_live;
-        if (j0 + BN < kend) {
+        if (j0 + STEP < kend) {
             kr.stash(kt, t);
             vr.stash(vt, t);
-            if (j0 + 2 * BN < kend) {
-                next_live = live_keys<BN>(mask, j0 + 2 * BN, kend, l);
-                fetch(j0 + 2 * BN, next_live);
+            if (j0 + 2 * STEP < kend) {
+                next_live = keys.take(j0 + 2 * STEP + mine);
+                keys.ahead(j0 + 3 * STEP + mine);
+                fetch(j0 + 2 * STEP + mine, next_live);
             }
         }
     }
     sum += other_half(sum);
+    if constexpr (GR == 2) {        // the second group's share, through LDS
+        f4v *const share = reinterpret_cast<f4v *>(lds) + w * NJ * 256 + l;
+        f2v *const state = reinterpret_cast<f2v *>(lds + NW * NJ * 4096) + 64 * w + l;
+        __syncthreads();
+        if (group) {
+            *state = f2v{mx, sum};
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    share[64 * (4 * j + g)] = f4v{o[j][4 * g], o[j][4 * g + 1], o[j][4 * g + 2], o[j][4 * g + 3]};
+        }
+        __syncthreads();
+        if (group) return;
+        const f2v theirs = *state;
+        const float next = fmaxf(mx, theirs[0]), ref = next == -INFINITY ? 0.f : next;
+        const float x = __builtin_amdgcn_exp2f(mx - ref), y = __builtin_amdgcn_exp2f(theirs[0] - ref);
+        mx = next;
+        sum = sum * x + theirs[1] * y;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f4v v = share[64 * (4 * j + g)];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[j][4 * g + e] = o[j][4 * g + e] * x + v[e] * y;
+            }
+    }
     if (!in) return;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const float lse = on && sum != 0.f ? (mx + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
@@ -214,36 +247,47 @@ __global__ void __launch_bounds__(256) xattn_join_kernel(CrossAttnArgs a) {
 // waves; half of that for single waves, of which more share a CU.
 constexpr int tile_keys(gs_dtype t, int waves) { return t == GS_F32 || waves == 1 ? 32 : 64; }
 
-// How the rows and keys are dealt out: waves of a work-group, parts of the keys.
-// Up to 32 rows (a few positions) go to single waves, eight a CU in all if
-// there are keys enough; more rows to work-groups of four, two a CU.  A part is
-// at least 128 keys in bf16 and, as products take eight times as long there,
-// 32 (one tile) in fp32 (4 sequences of 4 x 240, 4 heads of 96 values over one:
-// 13 us, 31 in parts of 128).
+// How the rows and keys are dealt out.  Up to 32 rows (a few positions) go to
+// single waves, eight a CU in all if there are keys enough, in parts of at least
+// 128 keys in bf16 and, as products take eight times as long there, 32 (one tile)
+// in fp32 (4 sequences of 4 x 240, 4 heads of 96 values over one: 13 us, 31 in
+// parts of 128).  More rows go to work-groups of four or eight waves.
 struct Plan {
     int waves, splits, split_keys, row_tiles, dp;
 };
 Plan plan_for(gs_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh) {
     Plan p{};
     const int64_t rows = Lq * (Hq / Hkv);
-    p.dp = padded(computed(Dh));
-    p.waves = rows <= 32 ? 1 : 4;
-    p.row_tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
-    const int64_t groups = B * Hkv * p.row_tiles, tile = tile_keys(t, p.waves), least = t == GS_F32 ? 32 : 128;
-    const int64_t want = (p.waves == 1 ? 2048 : 512) / (groups > 0 ? groups : 1);
-    int64_t per = (Lk + (want > 1 ? want : 1) - 1) / (want > 1 ? want : 1);
-    if (per < least) per = least;
+    const int dc = computed(Dh);
+    const bool few = rows <= 32;
+    p.dp = padded(dc);
+    p.row_tiles = (int)((rows + (few ? 31 : 127)) / (few ? 32 : 128));
+    const int64_t blocks = B * Hkv * p.row_tiles, tile = tile_keys(t, few ? 1 : 4);
+    int64_t per;
+    if (few) {
+        p.waves = 1;
+        const int64_t least = t == GS_F32 ? 32 : 128, want = 2048 / (blocks > 0 ? blocks : 1);
+        per = (Lk + (want > 1 ? want : 1) - 1) / (want > 1 ? want : 1);
+        if (per < least) per = least;
+    } else {
+        // (us a tile, measured: bf16 2.7 for heads of 128, 1.4 for 64; fp32 6.0 and 5.8)
+        const bool single = t == GS_F32 && dc > 64;
+        const double us = t == GS_F32 ? (single ? 0.047 * dc : 5.8) : 0.021 * dc;
+        const Deal d = deal_out(blocks, (Lk + tile - 1) / tile, single, us, (double)(B * Hkv * rows) * (p.dp * 8) / 4.5e6);
+        p.waves = d.waves;
+        per = (Lk + d.parts - 1) / d.parts;
+    }
     per = (per + tile - 1) / tile * tile;
     p.split_keys = (int)per;
-    p.splits = (int)((Lk + per - 1) / per);
+    p.splits = per ? (int)((Lk + per - 1) / per) : 1;
     if (p.splits < 1) p.splits = 1;
     return p;
 }
 
-template <typename T, int DC, int NW, int BN, bool VEC>
+template <typename T, int DC, int NW, int GR, bool VEC>
 hipError_t launch_rows(const CrossAttnArgs &a, hipStream_t s) {
-    constexpr int DP = padded(DC);
-    xattn_kernel<T, DC, NW, BN, VEC><<<dim3((unsigned)((a.groups + 7) / 8 * 8)), dim3(64 * NW), 0, s>>>(a);
+    constexpr int DP = padded(DC), BN = tile_keys(sizeof(T) == 4 ? GS_F32 : GS_BF16, NW);
+    xattn_kernel<T, DC, NW, GR, BN, VEC><<<dim3((unsigned)((a.groups + 7) / 8 * 8)), dim3(64 * NW * GR), 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t rows = (int64_t)a.B * a.Hkv * a.rows, per = 256 / (DP / 4);
@@ -251,13 +295,16 @@ hipError_t launch_rows(const CrossAttnArgs &a, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <typename T, int DC, bool VEC> hipError_t launch_waves(const CrossAttnArgs &a, int waves, hipStream_t s) {
-    return waves == 1 ? launch_rows<T, DC, 1, 32, VEC>(a, s) : launch_rows<T, DC, 4, sizeof(T) == 4 ? 32 : 64, VEC>(a, s);
+template <typename T, int DC, bool VEC> hipError_t launch_waves(const CrossAttnArgs &a, const Plan &p, hipStream_t s) {
+    if (p.waves == 1) return launch_rows<T, DC, 1, 1, VEC>(a, s);
+    if constexpr (sizeof(T) == 2 || DC == 64)
+        if (p.waves == 8) return launch_rows<T, DC, 4, 2, VEC>(a, s);
+    return launch_rows<T, DC, 4, 1, VEC>(a, s);
 }
-template <typename T, bool VEC> hipError_t launch_typed(const CrossAttnArgs &a, int waves, hipStream_t s) {
+template <typename T, bool VEC> hipError_t launch_typed(const CrossAttnArgs &a, const Plan &p, hipStream_t s) {
     const int dc = computed(a.Dh);
-    if (dc == 64) return launch_waves<T, 64, VEC>(a, waves, s);
-    return dc == 96 ? launch_waves<T, 96, VEC>(a, waves, s) : launch_waves<T, 128, VEC>(a, waves, s);
+    if (dc == 64) return launch_waves<T, 64, VEC>(a, p, s);
+    return dc == 96 ? launch_waves<T, 96, VEC>(a, p, s) : launch_waves<T, 128, VEC>(a, p, s);
 }
 
 }  // namespace
@@ -279,8 +326,8 @@ hipError_t launch_cross_attn(gs_dtype t, CrossAttnArgs a, void *ws, hipStream_t 
     a.part_lse = a.part + (int64_t)a.B * a.Hkv * a.rows * p.splits * p.dp;
     // tiles are read with 32-bit offsets: rows of a tile within 2^31 bytes
     a.vec = a.vec && a.k.l < ATTN_VEC_STRIDE && a.v.l < ATTN_VEC_STRIDE;
-    if (t == GS_F32) return a.vec ? launch_typed<float, true>(a, p.waves, s) : launch_typed<float, false>(a, p.waves, s);
-    return a.vec ? launch_typed<bf16_t, true>(a, p.waves, s) : launch_typed<bf16_t, false>(a, p.waves, s);
+    if (t == GS_F32) return a.vec ? launch_typed<float, true>(a, p, s) : launch_typed<float, false>(a, p, s);
+    return a.vec ? launch_typed<bf16_t, true>(a, p, s) : launch_typed<bf16_t, false>(a, p, s);
 }
 
 }  // namespace gs

@@ -44,12 +44,39 @@ __global__ void __launch_bounds__(256) xattn_rows_kernel(CrossAttnGradArgs a) {
     }
 }
 
+// Adds the sums of a work-group's second four waves to those of its first four;
+// true for the second, which have no more to do.
+template <int N> __device__ __forceinline__ bool add_groups(f16v (&o)[N], char *lds, int group, int w, int l) {
+    f4v *const share = reinterpret_cast<f4v *>(lds) + w * N * 256 + l;
+    __syncthreads();
+    if (group) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                share[64 * (4 * j + g)] = f4v{o[j][4 * g], o[j][4 * g + 1], o[j][4 * g + 2], o[j][4 * g + 3]};
+    }
+    __syncthreads();
+    if (group) return true;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f4v v = share[64 * (4 * j + g)];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[j][4 * g + e] += v[e];
+        }
+    return false;
+}
+
 // 32 query rows a wave as columns, keys streamed through LDS.
-template <typename T, int DC, int BN, bool VEC>
-__global__ void __launch_bounds__(256, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xattn_dq_kernel(CrossAttnGradArgs a) {
+template <typename T, int DC, int GR, int BN, bool VEC>
+__global__ void __launch_bounds__(256 * GR, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xattn_dq_kernel(CrossAttnGradArgs a) {
     constexpr int DP = padded(DC), PER = Op<T>::PER, NS = DC / (2 * PER), NJ = DC / 32, TILE = BN * DP * sizeof(T);
-    __shared__ __attribute__((aligned(16))) char lds[4 * TILE];
-    const int t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+    constexpr int STEP = GR * BN;
+    __shared__ __attribute__((aligned(16))) char lds[GR * 4 * TILE];
+    const int t = threadIdx.x % 256, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int group = GR > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 256) : 0, mine = group * BN;
     const int64_t L = logical_group(a.q_groups);
     if (L >= a.q_groups) return;
     const int rt = (int)(L % a.row_tiles);
@@ -71,7 +98,7 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xatt
     const float c = a.scale * LOG2E;
     const T *const K = static_cast<const T *>(a.K) + b * a.k.b + hk * a.k.h;
     const T *const V = static_cast<const T *>(a.V) + b * a.v.b + hk * a.v.h;
-    const uint8_t *const mask = a.mask ? a.mask + b * a.mask_ld : nullptr;
+    LiveKeys<BN> keys{a.mask ? a.mask + b * a.mask_ld : nullptr, kend, l, 0};
 
     f16v o[NJ];
 #pragma unroll
@@ -82,16 +109,19 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xatt
         kr.fetch(K + (int64_t)j * a.k.l, a.k.l, alive, a.Dh, t);
         vr.fetch(V + (int64_t)j * a.v.l, a.v.l, alive, a.Dh, t);
     };
-    char *kt = lds, *vt = lds + TILE;
+    char *kt = lds + group * 4 * TILE, *vt = kt + TILE;
     int other = 2 * TILE;
     if (j0 < kend) {
-        live = live_keys<BN>(mask, j0, kend, l);
-        fetch(j0, live);
+        keys.ahead(j0 + mine);
+        live = keys.take(j0 + mine);
+        keys.ahead(j0 + STEP + mine);
+        fetch(j0 + mine, live);
         kr.stash(kt, t);
         vr.stash(vt, t);
-        if (j0 + BN < kend) {
-            next_live = live_keys<BN>(mask, j0 + BN, kend, l);
-            fetch(j0 + BN, next_live);
+        if (j0 + STEP < kend) {
+            next_live = keys.take(j0 + STEP + mine);
+            keys.ahead(j0 + 2 * STEP + mine);
+            fetch(j0 + STEP + mine, next_live);
         }
     }
     if (kl <= BN && j0 < kend) {
@@ -115,9 +145,9 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xatt
                 D += (bits >> (8 * (r / 4) + r % 4)) & 1 ? __builtin_amdgcn_exp2f(fmaf(p[r], c, st[0])) * g[r] : 0.f;
         }
         st[1] = D + other_half(D);
-        if (on && l < 32) a.stat[((int64_t)b * a.Hq + row.h) * a.Lq + row.i] = st;
+        if (on && l < 32 && !group) a.stat[((int64_t)b * a.Hq + row.h) * a.Lq + row.i] = st;
     }
-    for (; j0 < kend; j0 += BN) {
+    for (; j0 < kend; j0 += STEP) {
         lds_barrier();
 #pragma unroll 1
         for (int n = 0; n < BN / 32; ++n) {
@@ -142,18 +172,23 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xatt
                 for (int j = 0; j < NJ; ++j) o[j] = Op<T>::mma(col_frag<T, DP>(kt, 32 * n, s, j, l), pf, o[j]);
             }
         }
+        if constexpr (sizeof(T) == 4 && GR == 2) products_done(o);
         kt += other;
         vt += other;
         other = -other;
         live = next_live;
-        if (j0 + BN < kend) {
+        if (j0 + STEP < kend) {
             kr.stash(kt, t);
             vr.stash(vt, t);
-            if (j0 + 2 * BN < kend) {
-                next_live = live_keys<BN>(mask, j0 + 2 * BN, kend, l);
-                fetch(j0 + 2 * BN, next_live);
+            if (j0 + 2 * STEP < kend) {
+                next_live = keys.take(j0 + 2 * STEP + mine);
+                keys.ahead(j0 + 3 * STEP + mine);
+                fetch(j0 + 2 * STEP + mine, next_live);
             }
         }
+    }
+    if constexpr (GR == 2) {
+        if (add_groups<NJ>(o, lds, group, w, l)) return;
     }
     if (!in) return;
     float *const part = a.q_parts > 1 ? a.dq_part + (((int64_t)sp * a.B * a.Hkv + bh) * a.rows + m) * DP : nullptr;
@@ -178,14 +213,15 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xatt
 // in LDS, fp32 ones run one wave a SIMD.  (4 x 16 heads of 2048 x 2048, bf16: one
 // wave a SIMD 443 us; two, with tiles through registers, which spill, 430; two,
 // tiles straight to LDS, 348.)
-template <typename T, int DC, bool VEC>
-__global__ void __launch_bounds__(256, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xattn_dkv_kernel(CrossAttnGradArgs a) {
+template <typename T, int DC, int GR, bool VEC>
+__global__ void __launch_bounds__(256 * GR, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xattn_dkv_kernel(CrossAttnGradArgs a) {
     constexpr int DP = padded(DC), PER = Op<T>::PER, NS = DC / (2 * PER), NJ = DC / 32, BM = 32, TILE = BM * DP * sizeof(T);
     constexpr bool KEEP_K = !(sizeof(T) == 2 && DC == 128);
-    __shared__ __attribute__((aligned(16))) char lds[4 * TILE + (KEEP_K ? 0 : 128 * DP * sizeof(T))];
-    __shared__ __attribute__((aligned(16))) f2v stat[2 * BM];
-    char *const keys_lds = lds + 4 * TILE;
-    const int t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+    __shared__ __attribute__((aligned(16))) char lds[GR * 4 * TILE + (KEEP_K ? 0 : GR * 128 * DP * sizeof(T))];
+    __shared__ __attribute__((aligned(16))) f2v stat[GR * 2 * BM];
+    const int t = threadIdx.x % 256, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int group = GR > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 256) : 0;
+    char *const own = lds + group * 4 * TILE, *const keys_lds = lds + GR * 4 * TILE + group * 128 * DP * sizeof(T);
     const int64_t L = logical_group(a.k_groups);
     if (L >= a.k_groups) return;
     const int kt = (int)(L % a.key_tiles);
@@ -198,12 +234,14 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xatt
     bool on = j < kl;
     if (on && a.mask) on = a.mask[b * a.mask_ld + j] != 0;
 
-    // tiles of 32 positions, `tiles` a head; this part's run of them
+    // tiles of 32 positions, `tiles` a head; this part's run of them, which the
+    // groups of four waves take in turn
     const int tiles = kt * 128 < kl ? (ql + BM - 1) / BM : 0;
     // (below 2^31, as B Hq Lq is; divided once, kept in scalar registers)
     const int64_t total = (int64_t)tiles * a.G;
-    int n = __builtin_amdgcn_readfirstlane((int)(total * sp / a.k_parts));
+    const int first = __builtin_amdgcn_readfirstlane((int)(total * sp / a.k_parts));
     const int end = __builtin_amdgcn_readfirstlane((int)(total * (sp + 1) / a.k_parts));
+    int n = first + group;
     int g = __builtin_amdgcn_readfirstlane(tiles ? n / tiles : 0), x = n - g * tiles;     // head and tile of the next fetch
 
     typename Op<T>::V k[NS], v[NS];
@@ -222,9 +260,9 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xatt
     // VEC: tiles go straight to LDS, the next while one is used; otherwise
     // through registers, each when it is needed
     TileLoad<T, DP, BM, 256, false> qr, dr;
-    f2v st = {0.f, 0.f};
-    char *qt = lds, *dt = lds + TILE;
-    f2v *ss = stat;
+    f2v st = {-INFINITY, 0.f};
+    char *qt = own, *dt = own + TILE;
+    f2v *ss = stat + group * 2 * BM;
     int other = 2 * TILE, other_s = BM;
     auto fetch = [&](char *to) {
         const int i0 = x * BM, h = hk * a.G + g;
@@ -239,24 +277,28 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xatt
             dr.fetch(O, a.d.l, alive, a.Dh, t);
         }
         if (t < BM) st = i0 + t < ql ? (a.stat + ((int64_t)b * a.Hq + h) * a.Lq + i0)[t] : f2v{-INFINITY, 0.f};
-        if (++x == tiles) x = 0, ++g;
+        for (x += GR; x >= tiles; x -= tiles) ++g;
     };
-    if constexpr (VEC) {
-        clear_lds<256>(lds, 4 * TILE, t);
-        lds_barrier();
-        if (n < end) fetch(qt);
-    }
-    for (; n < end; ++n) {
+    clear_lds<256>(own, 4 * TILE, t);
+    lds_barrier();
+    if (VEC && n < end) fetch(qt);
+    for (int n0 = first; n0 < end; n0 += GR, n += GR) {
         if constexpr (VEC) {
             wait_tiles();
-        } else {
+        } else if (n < end) {
             fetch(qt);
             qr.stash(qt, t);
             dr.stash(dt, t);
         }
         if (t < BM) ss[t] = st;
         lds_barrier();
-        if (VEC && n + 1 < end) fetch(qt + other);
+        if (n + GR < end) {
+            if constexpr (VEC) fetch(qt + other);
+        } else if (GR > 1) {
+            // No tile is left for the next turn, if there is one (of the other
+            // group): this one goes over what it has once more, at weight 0.
+            st = f2v{-INFINITY, 0.f};
+        }
         f16v p = {0}, s = {0};
 #pragma unroll
         for (int y = 0; y < NS; ++y) {
@@ -289,6 +331,10 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 && DC > 64 ? 1 : 2)) xatt
         ss += other_s;
         other = -other;
         other_s = -other_s;
+    }
+    if constexpr (GR == 2) {
+        add_groups<NJ>(dk, lds, group, w, l);
+        if (add_groups<NJ>(dv, lds, group, w, l)) return;
     }
     if (!in) return;
     const int64_t keys = (int64_t)a.B * a.Hkv * a.Lk;
@@ -354,48 +400,49 @@ __global__ void __launch_bounds__(256) xattn_parts_kernel(CrossAttnGradArgs a) {
     store4<T>(out, d, a.Dh, VEC, v);
 }
 
-// Parts that bring the work-groups to two a CU, as far as parts of a useful
-// length go: each costs a write and a read of fp32 rows.  For bf16 that is 64
-// keys or 2 tiles of 32 query rows; for fp32, whose products take eight times
-// as long, half of it (dQ of 29 sequences of 23 x 563, 3 heads of 72 values over
-// one: 27 us in parts of 64 keys, 40 in parts of 128).  Work-groups of two waves instead, so that fewer parts do, were
-// slower: dK and dV of train_ragged 55 us in 2 parts of 64-key work-groups, 39
-// in 3 of 128-key ones.
 struct Plan {
-    int dp, q_parts, q_step, k_parts;
+    int dp, q_waves, q_parts, q_step, k_waves, k_parts;
 };
 Plan plan_for(gs_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t Hq, int64_t Hkv, int64_t Dh) {
     Plan p{};
-    p.dp = padded(computed(Dh));
-    const int64_t G = Hq / Hkv, least = t == GS_F32 ? 1 : 2;
-    auto parts = [&](int64_t rows, int64_t most, int64_t useful) {
-        const int64_t groups = B * Hkv * ((rows + 127) / 128);
-        int64_t n = groups ? most / groups : 1;
-        n = n < useful ? n : useful;
-        return (int)(n > 1 ? n : 1);
-    };
-    const int n = parts(Lq * G, 512, Lk / (32 * least));
-    const int64_t unit = 32 * least, step = ((Lk + n - 1) / n + unit - 1) / unit * unit;
+    const int dc = computed(Dh);
+    const int64_t G = Hq / Hkv, unit = t == GS_F32 ? 32 : 64;
+    const bool single = t == GS_F32 && dc > 64;
+    p.dp = padded(dc);
+    // us a tile, measured: dQ, 64 or 32 keys: bf16 3.4 for heads of 128, 1.9 for
+    // 64; fp32 9.3 and 7.9.  dK and dV, 32 query rows: 2.7, 1.5; 12.5, 10.
+    const double dq_us = t == GS_F32 ? (single ? 0.073 * dc : 7.9) : 0.027 * dc;
+    const double dkv_us = t == GS_F32 ? (single ? 0.098 * dc : 10.) : 0.021 * dc;
+    const double row_us = (double)(p.dp * 8) / 4.5e6;
+    const Deal q = deal_out(B * Hkv * ((Lq * G + 127) / 128), (Lk + unit - 1) / unit, single, dq_us, (double)(B * Hq * Lq) * row_us);
+    const Deal k = deal_out(B * Hkv * ((Lk + 127) / 128), (Lq + 31) / 32 * G, single, dkv_us, (double)(B * Hkv * Lk) * 2 * row_us);
+    const int64_t step = ((Lk + q.parts - 1) / q.parts + unit - 1) / unit * unit;
+    p.q_waves = q.waves;
     p.q_step = (int)(step ? step : unit);
     p.q_parts = Lk ? (int)((Lk + step - 1) / step) : 1;
-    // (fp32 work-groups of 128 values run one a CU)
-    p.k_parts = parts(Lk, t == GS_F32 && p.dp == 128 ? 256 : 512, (Lq + 31) / 32 * G / least);
+    p.k_waves = k.waves;
+    p.k_parts = k.parts;
     return p;
 }
 
-template <typename T, int DC, bool VEC> hipError_t launch_sized(const CrossAttnGradArgs &a, hipStream_t s) {
+template <typename T, int DC, bool VEC> hipError_t launch_sized(const CrossAttnGradArgs &a, const Plan &p, hipStream_t s) {
     constexpr int DP = padded(DC), BN = sizeof(T) == 4 ? 32 : 64;
+    constexpr bool EIGHT = sizeof(T) == 2 || DC == 64;
     const auto grid = [](int64_t n, int64_t per) { return dim3((unsigned)((n + per - 1) / per)); };
     hipError_t e = hipSuccess;
     if (a.q_groups) {
         // (threads of a launch are counted in 32 bits: the rows of very large problems go round)
         const int64_t rows = (int64_t)a.B * a.Hq * a.Lq, most = (int64_t)1 << 24;
         xattn_rows_kernel<T, DP, VEC><<<grid(rows < most ? rows : most, 256 / (DP / Op<T>::PER)), dim3(256), 0, s>>>(a);
-        xattn_dq_kernel<T, DC, BN, VEC><<<dim3((unsigned)((a.q_groups + 7) / 8 * 8)), dim3(256), 0, s>>>(a);
+        const dim3 groups((unsigned)((a.q_groups + 7) / 8 * 8));
+        if (EIGHT && p.q_waves == 8) xattn_dq_kernel<T, DC, EIGHT ? 2 : 1, BN, VEC><<<groups, dim3(512), 0, s>>>(a);
+        else xattn_dq_kernel<T, DC, 1, BN, VEC><<<groups, dim3(256), 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (a.k_groups) {
-        xattn_dkv_kernel<T, DC, VEC><<<dim3((unsigned)((a.k_groups + 7) / 8 * 8)), dim3(256), 0, s>>>(a);
+        const dim3 groups((unsigned)((a.k_groups + 7) / 8 * 8));
+        if (EIGHT && p.k_waves == 8) xattn_dkv_kernel<T, DC, EIGHT ? 2 : 1, VEC><<<groups, dim3(512), 0, s>>>(a);
+        else xattn_dkv_kernel<T, DC, 1, VEC><<<groups, dim3(256), 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (a.join_q + a.join_k) {
@@ -405,10 +452,10 @@ template <typename T, int DC, bool VEC> hipError_t launch_sized(const CrossAttnG
     return e;
 }
 
-template <typename T, bool VEC> hipError_t launch_typed(const CrossAttnGradArgs &a, hipStream_t s) {
+template <typename T, bool VEC> hipError_t launch_typed(const CrossAttnGradArgs &a, const Plan &p, hipStream_t s) {
     const int dc = computed(a.Dh);
-    if (dc == 64) return launch_sized<T, 64, VEC>(a, s);
-    return dc == 96 ? launch_sized<T, 96, VEC>(a, s) : launch_sized<T, 128, VEC>(a, s);
+    if (dc == 64) return launch_sized<T, 64, VEC>(a, p, s);
+    return dc == 96 ? launch_sized<T, 96, VEC>(a, p, s) : launch_sized<T, 128, VEC>(a, p, s);
 }
 
 int64_t align4(int64_t n) { return (n + 3) / 4 * 4; }     // (16-byte rows of parts behind the rows' constants)
@@ -441,8 +488,8 @@ hipError_t launch_cross_attn_grad(gs_dtype t, CrossAttnGradArgs a, void *ws, hip
     a.dkv_part = a.dq_part + a.join_q * p.q_parts * p.dp;
     // tiles are read with 32-bit offsets: rows of a tile within 2^31 bytes
     for (const SeqStrides *x : {&a.q, &a.k, &a.v, &a.d}) a.vec = a.vec && x->l < ATTN_VEC_STRIDE;
-    if (t == GS_F32) return a.vec ? launch_typed<float, true>(a, s) : launch_typed<float, false>(a, s);
-    return a.vec ? launch_typed<bf16_t, true>(a, s) : launch_typed<bf16_t, false>(a, s);
+    if (t == GS_F32) return a.vec ? launch_typed<float, true>(a, p, s) : launch_typed<float, false>(a, p, s);
+    return a.vec ? launch_typed<bf16_t, true>(a, p, s) : launch_typed<bf16_t, false>(a, p, s);
 }
 
 }  // namespace gs

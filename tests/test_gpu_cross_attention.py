@@ -67,6 +67,17 @@ def test_sizes(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("Dh", [48, 63, 80, 95, 128, 126])
+def test_many_sequences(Dh, dtype):
+    """More heads and sequences than there are CUs: no long axis is split."""
+    B, Lq, Lk = 33, 34, 131
+    Q, K, V, dO = problem(B, Lq, Lk, 16, 8, Dh, dtype)
+    klen = torch.tensor([(37 * b) % (Lk + 1) for b in range(B)], dtype=torch.int32, device="cuda")
+    mask = (torch.arange(Lk, device="cuda")[None] % 7 != torch.arange(B, device="cuda")[:, None] % 7)
+    agree(Q, K, V, dO, klen=klen, mask=mask)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("size", [(4, 70, 150, 4, 2, 64), (4, 1, 900, 8, 2, 128), (4, 9, 70, 3, 1, 50)], ids=str)
 def test_lengths_and_masks(size, dtype):
     B, Lq, Lk = size[:3]
