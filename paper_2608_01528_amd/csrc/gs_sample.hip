@@ -122,10 +122,13 @@ __device__ __forceinline__ void put(const SampleArgs &a, int64_t b, int64_t j, u
 }
 
 template <typename T> struct Quad;
-template <> struct Quad<float> { static __device__ __forceinline__ f4v load(const float *p) { return *reinterpret_cast<const f4v *>(p); } };
+template <> struct Quad<float> {
+    typedef f4v Raw;
+    static __device__ __forceinline__ f4v scores(Raw r) { return r; }
+};
 template <> struct Quad<bf16_t> {
-    static __device__ __forceinline__ f4v load(const bf16_t *p) {
-        const u2v r = *reinterpret_cast<const u2v *>(p);
+    typedef u2v Raw;
+    static __device__ __forceinline__ f4v scores(Raw r) {
         return f4v{__uint_as_float(r[0] << 16), __uint_as_float(r[0] & 0xffff0000u), __uint_as_float(r[1] << 16),
                    __uint_as_float(r[1] & 0xffff0000u)};
     }
@@ -137,17 +140,26 @@ template <> struct Quad<bf16_t> {
 template <typename T> __device__ __forceinline__ int skew_of(const T *row) {
     return (int)(reinterpret_cast<uintptr_t>(row) / sizeof(T) & 3);
 }
-// Keys of the V entries from index j on (0 outside the row).
-template <typename T, int V> __device__ __forceinline__ void load_keys(uint32_t *key, const T *row, int32_t j, uint32_t M) {
-    if (V == 4 && (uint32_t)j < M && (uint32_t)(j + 3) < M) {
-        const f4v x = Quad<T>::load(row + j);
-#pragma unroll
-        for (int c = 0; c < V; ++c) key[c] = key_of(x[c]);
-    } else {
-#pragma unroll
-        for (int c = 0; c < V; ++c) key[c] = (uint32_t)(j + c) < M ? key_of(ld_f32<T>(row, j + c)) : 0;
+// Keys of the four entries from index j on (0 outside the row).  The load and
+// what is made of it are apart, so that a thread asks for several pieces before
+// it waits for the first.
+template <typename T> struct Piece {
+    typename Quad<T>::Raw raw;
+    bool whole;
+    __device__ __forceinline__ void ask(const T *row, int32_t j, uint32_t M) {
+        whole = (uint32_t)j < M && (uint32_t)(j + 3) < M;
+        raw = {};
+        if (whole) raw = *reinterpret_cast<const typename Quad<T>::Raw *>(row + j);
     }
-}
+    __device__ __forceinline__ void keys(uint32_t *key, const T *row, int32_t j, uint32_t M) const {
+        const f4v x = Quad<T>::scores(raw);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) key[c] = key_of(x[c]);
+        if (whole) return;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) key[c] = (uint32_t)(j + c) < M ? key_of(ld_f32<T>(row, j + c)) : 0;
+    }
+};
 
 // ---------------------------------------------------------------- in a wave
 
@@ -337,8 +349,17 @@ __global__ void __launch_bounds__(256, 4) sample_wave_kernel(SampleArgs a) {
     const T *const row = static_cast<const T *>(a.S) + b * a.lds;
     const int skew = E == 1 ? 0 : skew_of(row);
     uint32_t key[E], top = 0;
+    Piece<T> piece[V == 4 ? Q : 1];
 #pragma unroll
-    for (int q = 0; q < Q; ++q) load_keys<T, V>(key + V * q, row, (64 * q + l) * V - skew, (uint32_t)a.M);
+    for (int q = 0; q < Q; ++q) {
+        const int32_t j = (64 * q + l) * V - skew;
+        if constexpr (V == 1) key[q] = (uint32_t)j < (uint32_t)a.M ? key_of(ld_f32<T>(row, j)) : 0;
+        else piece[q].ask(row, j, (uint32_t)a.M);
+    }
+    if constexpr (V == 4) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) piece[q].keys(key + V * q, row, (64 * q + l) * V - skew, (uint32_t)a.M);
+    }
 #pragma unroll
     for (int e = 0; e < E; ++e) top = max(top, key[e]);
     top = wave_max(top);
@@ -572,18 +593,24 @@ struct Block {
 // Bins of the scores below the largest: a rank-preserving map, so that a run of
 // the first entries is some whole bins and a part of the next.  The bins cover
 // the row's range, or the 32 temperatures below the largest score (weights
-// above e^-32) if that is less; the last one takes the rest.
+// above e^-32) if that is less, down to the smallest key that min_p keeps; the
+// last one takes the rest.  (Where a run ends among entries that min_p takes
+// away is of no account; only with both top_k and top_p is the one's end there
+// needed for the other's.)
 struct Binning {
+    uint32_t floor;
     float m, scale;
-    __device__ __forceinline__ Binning(uint32_t top, uint32_t low, float temp) : m(value_of(top)) {
-        const float range = fminf(m - value_of(low), 32.f * temp);
+    __device__ __forceinline__ Binning(uint32_t top, uint32_t low, const Row &r, int64_t M, uint32_t least)
+        : floor(r.k < M && r.p < 1. ? 0 : least), m(value_of(top)) {
+        const float range = fminf(m - value_of(max(low, floor)), 32.f * r.temp);
         scale = (float)BINS / range;
     }
     __device__ __forceinline__ int bin(uint32_t key) const {
+        if (key < floor) return BINS - 1;
         const float x = value_of(key);
         if (x == m) return 0;
         const float at = (m - x) * scale;
-        return at < (float)(BINS - 1) ? (int)at : BINS - 1;     // (NaN and infinities: the last)
+        return at < (float)(BINS - 2) ? (int)at : BINS - 2;     // (NaN and infinities: the last but one)
     }
 };
 
@@ -622,11 +649,13 @@ struct RowSpace {
     Hist hist;
     Plan plan;
     uint32_t listed, floor;     // entries listed; the smallest key that min_p keeps
-    uint32_t top, pad;          // the largest key
+    uint32_t top;               // the largest key
+    uint32_t done;              // drawn from already
     uint64_t list[CAP];
 };
 struct ChunkSpace {
     uint64_t mass[PARTS];       // of the entries that are surely kept, by parts
+    uint32_t most[PARTS];       // each part's largest key
     uint32_t count, top, low, pad;
 };
 
@@ -650,8 +679,11 @@ template <typename T> struct Chunk {
     __device__ __forceinline__ void load(const SampleArgs &a, int64_t b, int chunk) {
         const T *const row = static_cast<const T *>(a.S) + b * a.lds;
         j0 = (int32_t)((uint32_t)chunk * CHUNK - (uint32_t)skew_of(row));
+        Piece<T> piece[Q];
 #pragma unroll
-        for (int q = 0; q < Q; ++q) load_keys<T, 4>(key[q], row, (int32_t)at(q, 0), (uint32_t)a.M);
+        for (int q = 0; q < Q; ++q) piece[q].ask(row, (int32_t)at(q, 0), (uint32_t)a.M);
+#pragma unroll
+        for (int q = 0; q < Q; ++q) piece[q].keys(key[q], row, (int32_t)at(q, 0), (uint32_t)a.M);
     }
     template <typename F> __device__ __forceinline__ void each(F f) const {
 #pragma unroll
@@ -659,6 +691,24 @@ template <typename T> struct Chunk {
 #pragma unroll
             for (int c = 0; c < 4; ++c)
                 if (key[q][c]) f(key[q][c], q, c);
+    }
+    // the same without the parts whose largest key is below `from`
+    __device__ __forceinline__ void load_from(const SampleArgs &a, int64_t b, int chunk, const uint32_t *most, uint32_t from) {
+        const T *const row = static_cast<const T *>(a.S) + b * a.lds;
+        j0 = (int32_t)((uint32_t)chunk * CHUNK - (uint32_t)skew_of(row));
+        Piece<T> piece[Q];
+        uint32_t largest[Q];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) largest[q] = most[q * (NT / 64) + (threadIdx.x >> 6)];
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+            if (largest[q] >= from) piece[q].ask(row, (int32_t)at(q, 0), (uint32_t)a.M);
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) key[q][c] = 0;
+            if (largest[q] >= from) piece[q].keys(key[q], row, (int32_t)at(q, 0), (uint32_t)a.M);
+        }
     }
     // largest key, and the complement of the smallest, of this thread's entries
     __device__ __forceinline__ void range(uint32_t &top, uint32_t &low) const {
@@ -697,7 +747,7 @@ __device__ __forceinline__ uint32_t floor_of(const Row &r, const Weigh &wt, uint
 
 // Reads the plan off the histogram (which holds counts where top_k asks, masses
 // where top_p does).
-__device__ __forceinline__ void make_plan(Shared &sh, const Row &r, const Binning &bins, uint32_t top) {
+__device__ __forceinline__ void make_plan(Shared &sh, const Row &r, const Binning &bins, uint32_t top, uint32_t floor) {
     constexpr int PER = BINS / NT;
     const int t = threadIdx.x, w = t >> 6, l = t & 63, i0 = t * PER;
     Hist &h = sh.hist;
@@ -761,6 +811,10 @@ __device__ __forceinline__ void make_plan(Shared &sh, const Row &r, const Binnin
         Plan &p = sh.plan;
         p.sure = p1 < BINS ? p.p_hi + 1 : (k < BINS ? p.k_hi + 1 : 1);
         p.listed = (uint32_t)(listed < CAP + 1 ? listed : CAP + 1);     // (without top_k: counted as they are listed)
+        if (floor > p.p_hi && floor > p.k_hi) {       // min_p takes away all that is in question
+            p.p_lo = p.k_lo = 1, p.p_hi = p.k_hi = 0;
+            p.listed = 0;
+        }
     }
     __syncthreads();
 }
@@ -852,10 +906,48 @@ __device__ __forceinline__ End end_of_short_list(const Shared &sh, const Row &r,
     return End{(uint32_t)__builtin_amdgcn_readlane(key, at < 0 ? 0 : at), (uint32_t)__builtin_amdgcn_readlane(j, at < 0 ? 0 : at)};
 }
 
+// The same for up to 256 entries, one a thread; the masses in the place of the
+// histogram's.  (More are searched by halving the range of keys, a sum over the
+// work-group a step: some 10 us, where 256 comparisons take 3.)
+__device__ __forceinline__ End end_of_ranked_list(Shared &sh, const Row &r, const Weigh &wt, int n) {
+    const Plan &p = sh.plan;
+    const int t = threadIdx.x;
+    const uint64_t v = t < n ? sh.list[t] : 0, mine = v ^ 0xffffffffu;      // in rank order: larger keys, then smaller indices
+    const uint32_t key = (uint32_t)(v >> 32);
+    const bool in_k = key && p.in_k(key), in_p = key && p.in_p(key);
+    const uint64_t mass = key && r.p < 1. ? wt.mass(key) : 0;
+    sh.hist.mass[t] = in_p ? mass : 0;
+    __syncthreads();
+    uint64_t before_p = 0;
+    int rank = 0, rank_k = 0;
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+        const uint64_t o = sh.list[i] ^ 0xffffffffu;
+        const bool first = o > mine;
+        rank += first;
+        rank_k += first && p.in_k((uint32_t)(o >> 32));
+        const uint64_t m = sh.hist.mass[i];
+        before_p += first ? m : 0;
+    }
+    bool keep = key && (!in_k || (uint64_t)rank_k + p.count_k < (uint64_t)r.k);
+    if (r.p < 1.) {
+        const uint64_t kept = sh.block.sum(keep && in_k ? mass : 0);
+        const uint64_t all = p.k_lo <= p.k_hi ? p.mass_k + kept : p.all;
+        const uint64_t before = p.mass_p + before_p;
+        keep = keep && in_p && (before == 0 || (double)before < r.p * (double)all);
+    }
+    // the last one kept (one is: the run ends among these)
+    const uint32_t last = sh.block.most(keep ? rank + 1 : 0);
+    if (keep && rank + 1 == (int)last) sh.end = End{key, (uint32_t)v};
+    __syncthreads();
+    return sh.end;
+}
+
 // The end of the run from the listed entries (n <= CAP, in sh.list as key and
 // index): top_k's, then top_p's within it.
 __device__ __forceinline__ End end_of_list(Shared &sh, const Row &r, const Weigh &wt, int n) {
     if (n <= 64) return end_of_short_list(sh, r, wt, n);
+    if (n <= NT) return end_of_ranked_list(sh, r, wt, n);
     const Plan p = sh.plan;
     Listed e;
 #pragma unroll
@@ -886,16 +978,22 @@ __device__ __forceinline__ End end_of_list(Shared &sh, const Row &r, const Weigh
 
 // The end of the run for rows whose bins hold too many entries: the range of
 // keys in question is divided by 2048 until it is one key, by whole passes over
-// the row.
+// the row, or over the parts of it that reach `least`, the entries below which
+// are known to lie behind the end (cs: the row's chunks, null if it is one).
 template <typename T>
 __device__ __forceinline__ End end_by_passes(Shared &sh, const SampleArgs &a, int64_t b, const Row &r, const Weigh &wt,
-                                              uint32_t top) {
+                                              uint32_t top, const ChunkSpace *cs, uint32_t least) {
     const int t = threadIdx.x;
-    const T *const row = static_cast<const T *>(a.S) + b * a.lds;
+    auto load = [&](Chunk<T> &ch, int c, uint32_t from) {
+        if (cs) ch.load_from(a, b, c, cs[c].most, from);
+        else ch.load(a, b, c);
+    };
     auto pass = [&](auto f) {
-        for (int64_t j = t; j < a.M; j += NT) {
-            const uint32_t x = key_of(ld_f32<T>(row, j));
-            if (x) f(x, j);
+        Chunk<T> ch;
+#pragma unroll 1
+        for (int c = 0; c < a.chunks; ++c) {
+            load(ch, c, least);
+            ch.each([&](uint32_t x, int, int) { f(x); });
         }
     };
     // the largest key from which on at least `goal` (entries, or mass) lies, not
@@ -907,7 +1005,7 @@ __device__ __forceinline__ End end_by_passes(Shared &sh, const SampleArgs &a, in
             const uint64_t step = ((uint64_t)hi - lo + BINS) / BINS;
             clear(sh.hist);
             __syncthreads();
-            pass([&](uint32_t x, int64_t) {
+            pass([&](uint32_t x) {
                 if (x >= lo && x <= hi)
                     atomicAdd((unsigned long long *)&sh.hist.mass[slot((int)((hi - x) / step))], by_mass ? (unsigned long long)wt.mass(x) : 1ull);
             });
@@ -936,7 +1034,7 @@ __device__ __forceinline__ End end_by_passes(Shared &sh, const SampleArgs &a, in
     };
     auto count_mass = [&](uint32_t from, uint64_t *m) {         // entries and mass of keys >= from
         uint64_t n = 0, w = 0;
-        pass([&](uint32_t x, int64_t) {
+        pass([&](uint32_t x) {
             if (x >= from) ++n, w += wt.mass(x);
         });
         *m = sh.block.sum(w);
@@ -961,19 +1059,31 @@ __device__ __forceinline__ End end_by_passes(Shared &sh, const SampleArgs &a, in
         if (n < 1.) n = 1.;
         if (n < (double)ties) ties = (uint64_t)n;
     }
-    // index of the last tie kept
-    uint64_t seen = 0;
+    // index of the last tie kept: the chunk that has it, then the place in it
     if (t == 0) sh.end = End{cut, LAST};
-    __syncthreads();
-    if (ties < (uint64_t)a.M) {
-        for (int64_t j0 = 0; j0 < a.M && seen < ties; j0 += NT) {
-            const int64_t j = j0 + t;
-            const bool is = j < a.M && key_of(ld_f32<T>(row, j)) == cut;
-            uint64_t all;
-            const uint64_t before = seen + sh.block.before(is, &all);
-            if (is && before + 1 == ties) sh.end.j = (uint32_t)j;
+    uint64_t seen = 0;
+    Chunk<T> ch;
+#pragma unroll 1
+    for (int c = 0; c < a.chunks && ties < (uint64_t)a.M; ++c) {
+        load(ch, c, cut);
+        uint64_t here = 0;
+        ch.each([&](uint32_t x, int, int) { here += x == cut; });
+        here = sh.block.sum(here);
+        seen += here;
+        if (seen < ties) continue;
+        seen -= here;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            uint64_t mine = 0, all;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mine += ch.key[q][e] == cut;
+            uint64_t at = seen + sh.block.before(mine, &all);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (ch.key[q][e] == cut && ++at == ties) sh.end.j = ch.at(q, e);
             seen += all;
         }
+        break;
     }
     __syncthreads();
     return sh.end;
@@ -1043,7 +1153,9 @@ __device__ __forceinline__ void draw_parts(Shared &sh, const SampleArgs &a, int6
     const int32_t j = (int32_t)((uint32_t)at * 256 + 4 * l - (uint32_t)skew_of(row));
     uint32_t key[4];
     uint64_t mass[4], mine = 0;
-    load_keys<T, 4>(key, row, j, (uint32_t)a.M);
+    Piece<T> piece;
+    piece.ask(row, j, (uint32_t)a.M);
+    piece.keys(key, row, j, (uint32_t)a.M);
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
         const bool on = key[c] && key[c] >= floor && end.has(key[c], (uint32_t)(j + c));
@@ -1082,21 +1194,33 @@ template <typename T>
 __device__ __forceinline__ void count_bins(Hist &h, const Chunk<T> &ch, const Row &r, const Weigh &wt, const Binning &bins,
                                            bool by_k) {
     const bool by_p = r.p < 1.;
+    uint32_t rest_n = 0;        // of the last bin, which many entries may share
+    uint64_t rest = 0;
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
         uint64_t mass[4];
         int at[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            at[c] = slot(bins.bin(ch.key[q][c]));
+            at[c] = bins.bin(ch.key[q][c]);
             mass[c] = by_p ? wt.mass(ch.key[q][c]) : 0;
         }
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             if (!ch.key[q][c]) continue;
-            if (by_k) atomicAdd(&h.count[at[c]], 1u);
-            if (by_p) atomicAdd((unsigned long long *)&h.mass[at[c]], (unsigned long long)mass[c]);
+            if (at[c] == BINS - 1) {
+                ++rest_n, rest += mass[c];
+                continue;
+            }
+            if (by_k) atomicAdd(&h.count[slot(at[c])], 1u);
+            if (by_p) atomicAdd((unsigned long long *)&h.mass[slot(at[c])], (unsigned long long)mass[c]);
         }
+    }
+    rest_n = (uint32_t)wave_sum(rest_n);
+    rest = wave_sum(rest);
+    if ((threadIdx.x & 63) == 0 && rest_n) {
+        if (by_k) atomicAdd(&h.count[slot(BINS - 1)], rest_n);
+        if (by_p) atomicAdd((unsigned long long *)&h.mass[slot(BINS - 1)], (unsigned long long)rest);
     }
 }
 
@@ -1124,13 +1248,14 @@ __global__ void __launch_bounds__(NT, 3) sample_group_kernel(SampleArgs a) {
         return;
     }
     const Weigh wt(top, r.c, a.shift, sh.table);
+    const uint32_t floor = floor_of(r, wt, top);
     End end = NO_END;
     if (!r.keeps_all(a.M)) {
-        const Binning bins(top, low, r.temp);
+        const Binning bins(top, low, r, a.M, floor);
         count_bins(sh.hist, ch, r, wt, bins, r.k < a.M);
         if (t == 0) sh.n = 0;
         __syncthreads();
-        make_plan(sh, r, bins, top);
+        make_plan(sh, r, bins, top, floor);
         const Plan p = sh.plan;
         uint32_t listed = p.listed;
         if (listed <= CAP) {
@@ -1139,10 +1264,9 @@ __global__ void __launch_bounds__(NT, 3) sample_group_kernel(SampleArgs a) {
             listed = sh.n;
             __syncthreads();
         }
-        if (listed > CAP) end = end_by_passes<T>(sh, a, b, r, wt, top);
+        if (listed > CAP) end = end_by_passes<T>(sh, a, b, r, wt, top, nullptr, 1);
         else if (listed) end = end_of_list(sh, r, wt, (int)listed);
     }
-    const uint32_t floor = floor_of(r, wt, top);
     const uint64_t kept =
         chunk_parts<true>(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); }, sh.mass);
     draw_parts<T>(sh, a, b, wt, end, floor, kept, PARTS, [&](int i) { return sh.mass[i]; });
@@ -1161,14 +1285,23 @@ __global__ void __launch_bounds__(NT) sample_top_kernel(SampleArgs a) {
     const int64_t slot = blockIdx.x / a.chunks, b = a.row0 + slot;
     RowSpace *const rs = row_space(a, slot);
     for (int i = chunk * NT + t; i < BINS; i += a.chunks * NT) rs->hist.count[i] = 0, rs->hist.mass[i] = 0;
-    if (chunk == 0 && t == 0) rs->listed = 0;
+    if (chunk == 0 && t == 0) rs->listed = 0, rs->done = 0;
     Chunk<T> ch;
     ch.load(a, b, chunk);
+    ChunkSpace &cs = chunk_space(rs)[chunk];
     uint32_t top, low;
     ch.range(top, low);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        uint32_t x = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x = max(x, ch.key[q][c]);
+        x = wave_max(x);
+        if ((t & 63) == 0) cs.most[q * (NT / 64) + (t >> 6)] = x;
+    }
     top = block.most(top);
     low = ~block.most(low);
-    if (t == 0) chunk_space(rs)[chunk].top = top, chunk_space(rs)[chunk].low = low;
+    if (t == 0) cs.top = top, cs.low = low;
 }
 
 // The row's largest and smallest key from the chunks' ones.
@@ -1178,6 +1311,132 @@ __device__ __forceinline__ void row_range(Block &block, const SampleArgs &a, con
     for (int i = threadIdx.x; i < a.chunks; i += NT) top = max(top, cs[i].top), low = max(low, ~cs[i].low);
     top = block.most(top);
     low = ~block.most(low);
+}
+
+// Rows of which top_k keeps a few, a work-group a row: a key that the largest
+// ones of k parts reach has k entries from it on, so that only parts that reach
+// it can hold kept entries, and few others do.  Those entries are listed, ranked
+// and drawn from at once.  A row with more than CAP of them (few parts that hold
+// all that counts, or many equal scores) is left to the other launches, or, ONLY
+// where there are none, ranked by passes over it.
+template <typename T, bool ONLY>
+__global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a) {
+    __shared__ Shared sh;
+    const int t = threadIdx.x, l = t & 63;
+    const int64_t slot = blockIdx.x, b = a.row0 + slot;
+    const Row r(a, b);
+    const int parts = a.chunks * PARTS;
+    if (!ONLY && (r.takes_first() || r.k > parts / 2)) return;
+    RowSpace *const rs = row_space(a, slot);
+    const ChunkSpace *const cs = chunk_space(rs);
+    constexpr int PER = PARTS_HERE / NT;
+    uint32_t *const ids = sh.hist.count;
+    uint32_t most[PER], top = 0;
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+        const int i = NT * x + t;
+        most[x] = i < parts ? cs[i / PARTS].most[i % PARTS] : 0;
+        top = max(top, most[x]);
+    }
+    fill_table(sh.table, t);
+    if (t == 0) sh.bins[0] = sh.bins[1] = 0;
+    top = sh.block.most(top);
+    if (!top) {
+        if (ONLY && t == 0) put(a, b, -1, 0, 0, 0);
+        return;
+    }
+    // a key that k parts reach, within 2^-16 of the largest such (1 if there are
+    // fewer parts with entries): by halving
+    uint32_t from = 1;
+    for (uint32_t hi = top, step = 0; step < 16 && from < hi; ++step) {
+        const uint32_t mid = hi - (hi - from) / 2;
+        uint32_t n = 0;
+#pragma unroll
+        for (int x = 0; x < PER; ++x) n += __popcll(__ballot(most[x] >= mid));
+        uint64_t *const to = sh.wave[step & 1];
+        if (l == 0) to[t >> 6] = n;
+        __syncthreads();
+        uint64_t all = 0;
+#pragma unroll
+        for (int i = 0; i < NT / 64; ++i) all += to[i];
+        if (all >= (uint64_t)r.k) from = mid;
+        else hi = mid - 1;
+    }
+#pragma unroll
+    for (int x = 0; x < PER; ++x)
+        if (most[x] >= from) ids[atomicAdd(&sh.bins[0], 1u)] = NT * x + t;
+    __syncthreads();
+    const int listed_parts = (int)sh.bins[0];
+    const T *const row = static_cast<const T *>(a.S) + b * a.lds;
+    const int skew = skew_of(row);
+    constexpr int U = 8;
+    for (int i0 = t >> 6; i0 < listed_parts; i0 += U * (NT / 64)) {
+        Piece<T> piece[U];
+        int32_t j[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {       // (behind the last: the last once more, not used)
+            j[u] = (int32_t)(ids[min(i0 + u * (NT / 64), listed_parts - 1)] * 256 + 4 * l) - skew;
+            piece[u].ask(row, j[u], (uint32_t)a.M);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i0 + u * (NT / 64) >= listed_parts) continue;
+            uint32_t key[4];
+            piece[u].keys(key, row, j[u], (uint32_t)a.M);
+            uint64_t on[4];
+            uint32_t n = 0;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) on[c] = __ballot(key[c] >= from), n += __popcll(on[c]);
+            uint32_t at = l == 0 ? atomicAdd(&sh.bins[1], n) : 0;
+            at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const uint32_t to = at + __builtin_amdgcn_mbcnt_hi((uint32_t)(on[c] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)on[c], 0));
+                if (key[c] >= from && to < CAP) sh.list[to] = (uint64_t)key[c] << 32 | (uint32_t)(j[u] + c);
+                at += __popcll(on[c]);
+            }
+        }
+    }
+    __syncthreads();
+    const int n = (int)sh.bins[1];
+    if (n > CAP && !ONLY) return;
+    const Weigh wt(top, r.c, a.shift, sh.table);
+    const uint32_t floor = max(floor_of(r, wt, top), from);
+    if (n > CAP) {
+        const End end = end_by_passes<T>(sh, a, b, r, wt, top, cs, from);
+        uint64_t kept = 0;
+        Chunk<T> ch;
+#pragma unroll 1
+        for (int i = 0; i < a.chunks; ++i) {
+            ch.load_from(a, b, i, cs[i].most, floor);
+            kept += chunk_parts<false>(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); },
+                                       sh.mass + i * PARTS);
+        }
+        draw_parts<T>(sh, a, b, wt, end, floor, kept, parts, [&](int i) { return sh.mass[i]; });
+        return;
+    }
+    const bool by_k = n > (int)r.k;
+    uint64_t all = 0;
+    if (!by_k && r.p < 1.) {
+        for (int i = t; i < n; i += NT) all += wt.mass((uint32_t)(sh.list[i] >> 32));
+        all = sh.block.sum(all);
+    }
+    // everything listed is in question
+    if (t == 0) sh.plan = Plan{top + 1, from, top, by_k ? from : 1, by_k ? top : 0, (uint32_t)n, 0, 0, all, 0};
+    for (int i = t; i < parts; i += NT) sh.mass[i] = 0;
+    __syncthreads();
+    End end = NO_END;
+    if (by_k || r.p < 1.) end = end_of_list(sh, r, wt, n);
+    uint64_t kept = 0;
+    for (int i = t; i < n; i += NT) {
+        const uint32_t x = (uint32_t)(sh.list[i] >> 32), at = (uint32_t)sh.list[i];
+        if (x < floor || !end.has(x, at)) continue;
+        ++kept;
+        atomicAdd((unsigned long long *)&sh.mass[(at + skew) / 256], (unsigned long long)wt.mass(x));
+    }
+    if (!ONLY && t == 0) rs->done = 1;
+    kept = sh.block.sum(kept);
+    draw_parts<T>(sh, a, b, wt, end, floor, kept, parts, [&](int i) { return sh.mass[i]; });
 }
 
 // Launch 2: the histogram of the row; for rows without top_k and top_p the
@@ -1192,6 +1451,7 @@ __global__ void __launch_bounds__(NT) sample_bins_kernel(SampleArgs a) {
     const Row r(a, b);
     if (r.takes_first()) return;
     RowSpace *const rs = row_space(a, slot);
+    if (rs->done) return;
     ChunkSpace *const cs = chunk_space(rs);
     Chunk<T> ch;
     ch.load(a, b, chunk);
@@ -1201,14 +1461,14 @@ __global__ void __launch_bounds__(NT) sample_bins_kernel(SampleArgs a) {
     row_range(block, a, cs, top, low);
     if (!top) return;
     const Weigh wt(top, r.c, a.shift, table);
+    const uint32_t floor = floor_of(r, wt, top);
     if (r.keeps_all(a.M)) {
-        const uint32_t floor = floor_of(r, wt, top);
         const uint64_t n = chunk_parts<true>(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= floor; }, cs[chunk].mass);
         if (t == 0) cs[chunk].count = (uint32_t)n;
         return;
     }
     const bool by_k = r.k < a.M;
-    count_bins(hist, ch, r, wt, Binning(top, low, r.temp), by_k);
+    count_bins(hist, ch, r, wt, Binning(top, low, r, a.M, floor), by_k);
     __syncthreads();
     for (int i = t; i < BINS; i += NT) {
         if (by_k && hist.count[i]) atomicAdd(&rs->hist.count[i], hist.count[i]);
@@ -1224,6 +1484,7 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(SampleArgs a) {
     const Row r(a, b);
     if (r.takes_first() || r.keeps_all(a.M)) return;
     RowSpace *const rs = row_space(a, slot);
+    if (rs->done) return;
     for (int i = t; i < BINS; i += NT) sh.hist.count[i] = rs->hist.count[i], sh.hist.mass[i] = rs->hist.mass[i];
     fill_table(sh.table, t);
     uint32_t top, low;
@@ -1232,8 +1493,8 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(SampleArgs a) {
         if (t == 0) rs->top = 0;
         return;
     }
-    make_plan(sh, r, Binning(top, low, r.temp), top);
     const uint32_t floor = floor_of(r, Weigh(top, r.c, a.shift, sh.table), top);
+    make_plan(sh, r, Binning(top, low, r, a.M, floor), top, floor);
     if (t == 0) rs->plan = sh.plan, rs->floor = floor, rs->top = top;
 }
 
@@ -1248,17 +1509,21 @@ __global__ void __launch_bounds__(NT) sample_list_kernel(SampleArgs a) {
     const Row r(a, b);
     if (r.takes_first() || r.keeps_all(a.M)) return;
     RowSpace *const rs = row_space(a, slot);
+    if (rs->done) return;
     ChunkSpace *const cs = chunk_space(rs);
-    Chunk<T> ch;
-    ch.load(a, b, chunk);
-    fill_table(table, t);
-    __syncthreads();
     const uint32_t top = rs->top;
     if (!top) return;
     const Plan p = rs->plan;
     if (p.listed > CAP) return;
-    const Weigh wt(top, r.c, a.shift, table);
     const uint32_t from = max(p.sure, rs->floor);
+    uint32_t least = from;
+    if (p.p_lo <= p.p_hi) least = min(least, p.p_lo);
+    if (p.k_lo <= p.k_hi) least = min(least, p.k_lo);
+    Chunk<T> ch;
+    ch.load_from(a, b, chunk, cs[chunk].most, least);
+    fill_table(table, t);
+    __syncthreads();
+    const Weigh wt(top, r.c, a.shift, table);
     list_asked(ch, p, &rs->listed, rs->list);
     const uint64_t n = chunk_parts<false>(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= from; }, cs[chunk].mass);
     if (t == 0) cs[chunk].count = (uint32_t)n;
@@ -1271,6 +1536,7 @@ __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
     const int t = threadIdx.x;
     const int64_t slot = blockIdx.x, b = a.row0 + slot;
     RowSpace *const rs = row_space(a, slot);
+    if (rs->done) return;
     ChunkSpace *const cs = chunk_space(rs);
     fill_table(sh.table, t);
     uint32_t top, low;
@@ -1307,7 +1573,7 @@ __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
         const uint32_t listed = p.listed > CAP ? p.listed : rs->listed;
         floor = rs->floor;
         if (listed > CAP) {
-            end = end_by_passes<T>(sh, a, b, r, wt, top);
+            end = end_by_passes<T>(sh, a, b, r, wt, top, cs, 1);
             again = true;
         } else if (listed) {
             for (int i = t; i < (int)listed; i += NT) sh.list[i] = rs->list[i];
@@ -1330,7 +1596,7 @@ __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
         // the whole row once more, now that the end of the run is known
         Chunk<T> ch;
         for (int i = 0; i < a.chunks; ++i) {
-            ch.load(a, b, i);
+            ch.load_from(a, b, i, cs[i].most, floor);
             const uint64_t n = chunk_parts<false>(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); },
                                            here ? sh.mass + i * PARTS : cs[i].mass);
             if (t == 0) cs[i].count = (uint32_t)n;
@@ -1389,6 +1655,15 @@ template <typename T> void launch_rows(const SampleArgs &a, hipStream_t s) {
     const bool all = !a.top_k && !a.top_p && (a.top_k_all <= 1 || a.top_k_all >= a.M) && !(a.top_p_all < 1.f);
     const dim3 grid((unsigned)(rows * a.chunks)), one((unsigned)rows);
     sample_top_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
+    const int parts = a.chunks * PARTS;
+    if (parts <= PARTS_HERE) {
+        const bool first = !a.temperature && !(a.temperature_all > 0.f);
+        if (first || (!a.top_k && a.top_k_all >= 1 && a.top_k_all <= parts / 2)) {
+            sample_pick_kernel<T, true><<<one, dim3(NT), 0, s>>>(a);
+            return;
+        }
+        if (a.top_k && parts >= 256) sample_pick_kernel<T, false><<<one, dim3(NT), 0, s>>>(a);
+    }
     sample_bins_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
     if (!all) {
         sample_plan_kernel<<<one, dim3(NT), 0, s>>>(a);

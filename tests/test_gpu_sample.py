@@ -115,6 +115,26 @@ def test_equal_scores(M):
             agree(S, u, **p)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("M", [8190, 9001, 40000])
+def test_where_the_large_scores_lie(M, dtype):
+    """Sorted rows (all that counts side by side), rows of which only a few
+    neighbours, or a few far from each other, can be drawn, and rows whose
+    largest scores are masked by the type's lowest value elsewhere."""
+    S, u = scores(6, M, seed=M, out=0.0)
+    S[0] = S[0].sort().values
+    S[1] = S[1].sort(descending=True).values
+    S[2, 20:] = -INF
+    S[3, torch.arange(M, device="cuda") % 1500 != 7] = -INF
+    S[4, 300:] = torch.finfo(dtype).min
+    S[5, : M - 900] = -60.0
+    S = S.to(dtype)
+    for p in ({"top_k": 3}, {"top_k": 12, "top_p": 0.7}, {"top_k": 30}, {"top_k": 30, "top_p": 0.9, "min_p": 0.01}, {"top_k": 2, "min_p": 0.9},
+              {"top_p": 0.9, "min_p": 0.05}, {"top_p": 0.2, "min_p": 0.001}, {"top_k": 500, "min_p": 0.2},
+              {"top_k": 500, "top_p": 0.95, "min_p": 0.2}, {"top_k": 4000, "top_p": 0.999, "min_p": 0.01}):
+        agree(S, u, **p)
+
+
 @pytest.mark.parametrize("M", [4, 70, 3000, 30000])
 def test_rows_with_little_in_them(M):
     S = torch.full((9, M), -INF)
