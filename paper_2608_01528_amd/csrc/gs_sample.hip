@@ -16,12 +16,25 @@
 //   a work-group a row  up to 8189 entries, in registers: a histogram of the
 //                       scores below the largest finds the bin the run ends in
 //   work-groups a row   more entries: the same over chunks of 8192, in five
-//                       launches (largest score, histogram, where the run ends,
+//                       launches (largest scores, histogram, where the run ends,
 //                       entries in question, ranking and draw).  A launch
 //                       boundary hands a row's data on faster than fences and
 //                       counters did, which write caches back from every
 //                       work-group: 200 rows of 128001 took 402 and 511 us in
 //                       the launches that had them, 97 and 128 without
+//   the same, few kept  where top_k keeps up to half as many entries as the row
+//                       has parts of 256: a second launch reads the parts whose
+//                       largest scores reach k parts' ones, and draws.  Where
+//                       each row has a top_k of its own the other launches
+//                       follow for the rest, from 256 parts on (131072 entries,
+//                       one row, top_k 50: 24 us for all rows alike, 31 for each
+//                       its own, 38 without; 32000: 24, 33 and 37, but 70 with a
+//                       row among them that keeps more, 44 without)
+//
+// Few rows are bound by the launches and the latency within them (4 us a
+// launch that does nothing), many by the fp64 work of the weights: some 40
+// instructions an entry, 25.6 million of which take 30 us of 53 in the histogram
+// launch for 200 rows of 128001; the scores alone would be read in 11.
 #include "gs_internal.h"
 
 namespace gs {
@@ -1656,7 +1669,7 @@ template <typename T> void launch_rows(const SampleArgs &a, hipStream_t s) {
     const dim3 grid((unsigned)(rows * a.chunks)), one((unsigned)rows);
     sample_top_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
     const int parts = a.chunks * PARTS;
-    if (parts <= PARTS_HERE) {
+    if (parts <= PARTS_HERE) {      // (the sums of more do not fit: see the head for both sides' times)
         const bool first = !a.temperature && !(a.temperature_all > 0.f);
         if (first || (!a.top_k && a.top_k_all >= 1 && a.top_k_all <= parts / 2)) {
             sample_pick_kernel<T, true><<<one, dim3(NT), 0, s>>>(a);
