@@ -541,7 +541,8 @@ gs_status gs_soft_select(const gs_soft_group *groups, int ngroups, gs_dtype pt, 
  * of each sequence.
  *
  *   B, Lq, Lk  sequences, positions and states (each >= 0); B Hkv below 2^23,
- *              B Hq Lq and B Hkv Lk below 2^31 - 256
+ *              B Hq Lq and B Hkv Lk below 2^31 - 256, and fewer than 2^24 - 8
+ *              blocks of 128: B Hkv ceil(Lq G / 128), B Hkv ceil(Lk / 128)
  *   Hq, Hkv    heads; Hkv divides Hq      Dh  values a head, 1 <= Dh <= 128
  *   qlen,klen  int32[B] device, nullable (Lq, Lk); taken as 0 below 0 and as Lq
  *              or Lk above
@@ -550,7 +551,7 @@ gs_status gs_soft_select(const gs_soft_group *groups, int ngroups, gs_dtype pt, 
  *   Q, O, dO, dQ   B x Lq x Hq x Dh, K, V, dK, dV   B x Lk x Hkv x Dh, all of
  *              type t in {F32, BF16}: element (b, i, h, d) at
  *              p[b sb + i sl + h sh + d], strides >= 0; elements of an output
- *              at places of their own.  Rows that start on 16-byte boundaries
+ *              at places of their own, none 2^46 or more from the first.  Rows that start on 16-byte boundaries
  *              with Dh a multiple of 16 bytes are the fast case
  *   lse        float B x Hq x Lq; out (nullable) and in
  *   ws         device workspace of the size that the _workspace call gives

@@ -296,8 +296,12 @@ Span seq_span(const gs_seq &q, const SeqShape &z, size_t es, const char *name) {
 }
 
 constexpr int64_t SEQ_MAX = (int64_t)1 << 31;       // sizes and rows below this
-constexpr int64_t ATTN_MAX_GROUPS = (int64_t)1 << 23;
-constexpr int64_t STRIDE_MAX = (int64_t)1 << 40;    // (elements: byte offsets stay far inside 64 bits)
+constexpr int64_t ATTN_MAX_GROUPS = (int64_t)1 << 23, ATTN_MAX_BLOCKS = ((int64_t)1 << 24) - 8;
+constexpr int64_t STRIDE_MAX = (int64_t)1 << 40;
+constexpr int64_t REACH_MAX = (int64_t)1 << 46;     // elements from a tensor's first to its last (no memory reaches as far)
+
+// The last of n0 rows, ld apart, of n elements lies within reach.
+bool within_reach(int64_t n0, int64_t ld, int64_t n) { return (__int128)(n0 > 0 ? n0 - 1 : 0) * ld + n < REACH_MAX; }
 
 gs_status check_seq(const char *fn, const char *name, const gs_seq &q, const SeqShape &z, gs_dtype t, bool out) {
     const int64_t st[3] = {q.sb, q.sl, q.sh};
@@ -305,6 +309,9 @@ gs_status check_seq(const char *fn, const char *name, const gs_seq &q, const Seq
         if (s < 0 || s >= STRIDE_MAX) return fail(GS_ERR_SHAPE, "%s: stride of %s out of range", fn, name);
     if (!z.n[0] || !z.n[1] || !z.n[2]) return GS_OK;
     if (!q.p) return fail(GS_ERR_ARG, "%s: %s is null", fn, name);
+    __int128 reach = z.dh;
+    for (int i = 0; i < 3; ++i) reach += (__int128)(z.n[i] - 1) * st[i];
+    if (reach >= REACH_MAX) return fail(GS_ERR_SHAPE, "%s: %s reaches too far", fn, name);
     GS_CHECK(check_aligned(q.p, esize(t), name));
     if (!out) return GS_OK;
     // rows of their own: from the smallest stride up, each spans the ones below
@@ -332,15 +339,16 @@ bool attn_sizes(const gs_cross_attn *a) {
     // B Hkv (work-groups) and Lq G (packed rows) first, so that no product overflows
     if (a->B * a->Hkv >= most || a->Lq * (a->Hq / a->Hkv) >= most) return false;
     if (a->B * a->Hkv >= ATTN_MAX_GROUPS) return false;      // (work-groups of 256 threads, counted in 32 bits)
-    const int64_t bh = a->B * a->Hkv ? a->B * a->Hkv : 1;
-    return a->Lq * (a->Hq / a->Hkv) < most / bh && a->Lk < most / bh;
+    const int64_t bh = a->B * a->Hkv ? a->B * a->Hkv : 1, rows = a->Lq * (a->Hq / a->Hkv);
+    if (rows >= most / bh || a->Lk >= most / bh) return false;
+    return bh * ((rows + 127) / 128) < ATTN_MAX_BLOCKS && bh * ((a->Lk + 127) / 128) < ATTN_MAX_BLOCKS;
 }
 
 gs_status check_attn(const char *fn, const gs_cross_attn *a, gs_dtype t, bool grad) {
     if (!a) return fail(GS_ERR_ARG, "%s: the problem is null", fn);
     if (!is_batch_type(t)) return fail(GS_ERR_DTYPE, "%s: tensors must be f32 or bf16", fn);
     if (!attn_sizes(a))
-        return fail(GS_ERR_SHAPE, "%s: need B, Lq, Lk >= 0, Hkv >= 1 dividing Hq, 1 <= Dh <= %d, B Hkv below 2^23, and B Hq Lq and B Hkv Lk below 2^31 - 256",
+        return fail(GS_ERR_SHAPE, "%s: need B, Lq, Lk >= 0, Hkv >= 1 dividing Hq, 1 <= Dh <= %d, B Hkv below 2^23, B Hq Lq and B Hkv Lk below 2^31 - 256, and of both less than 2^24 - 8 blocks of 128",
                     fn, CROSS_ATTN_MAX_DH);
     if (!(std::fabs(a->scale) >= 1e-30 && std::fabs(a->scale) <= 1e30))
         return fail(GS_ERR_ARG, "%s: |scale| must be in [1e-30, 1e30]", fn);
@@ -353,6 +361,7 @@ gs_status check_attn(const char *fn, const gs_cross_attn *a, gs_dtype t, bool gr
     GS_CHECK(check_aligned(a->qlen, 4, "qlen"));
     GS_CHECK(check_aligned(a->klen, 4, "klen"));
     if (a->mask && a->ldm < a->Lk) return fail(GS_ERR_SHAPE, "%s: leading dimension of mask is smaller than Lk", fn);
+    if (a->mask && !within_reach(a->B, a->ldm, a->Lk)) return fail(GS_ERR_SHAPE, "%s: mask reaches too far", fn);
     if (grad) {
         if (!a->lse && a->B && a->Lq) return fail(GS_ERR_ARG, "%s: lse is null", fn);
         GS_CHECK(check_seq(fn, "dO", a->dO, q, t, false));
@@ -946,7 +955,7 @@ gs_status gs_sample(const void *S, gs_dtype st, int64_t B, int64_t M, int64_t ld
     if (B < 0 || B >= SEQ_MAX - 256 || M < 1 || M >= SEQ_MAX - 256)
         return fail(GS_ERR_SHAPE, "%s: need 0 <= B and 1 <= M, both below 2^31 - 256", fn);
     GS_CHECK(check_matrix(S, "S", B, M, lds, st, false));
-    if (lds >= STRIDE_MAX) return fail(GS_ERR_SHAPE, "%s: leading dimension of S out of range", fn);
+    if (!within_reach(B, lds, M)) return fail(GS_ERR_SHAPE, "%s: leading dimension of S out of range", fn);
     if (B > 0 && !u) return fail(GS_ERR_ARG, "%s: u is null", fn);
     if (B > 0 && !idx) return fail(GS_ERR_ARG, "%s: idx is null", fn);
     const gs_sampling plain = {nullptr, nullptr, nullptr, nullptr, 1.f, 0, 1.f, 0.f};

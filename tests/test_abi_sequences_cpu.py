@@ -91,6 +91,21 @@ def test_shapes_refused(L, change):
         assert L.gs_cross_attention_grad_workspace(p.pack(), gs.GS_BF16) == 0
 
 
+@pytest.mark.parametrize("change", [
+    {"B": 256, "K": (0x11000000, 1 << 39, 128, 64)},            # the last sequence beyond any memory
+    {"mask": 0x80000000, "ldm": 1 << 60}, {"mask": 0x80000000, "ldm": (1 << 63) - 1},
+    {"B": (1 << 23) - 1, "Hq": 1, "Hkv": 1, "Lq": 200},         # 2^24 work-groups
+    {"B": (1 << 23) - 1, "Hq": 1, "Hkv": 1, "Lk": 200},
+], ids=str)
+def test_reach_and_work_groups_refused(L, change):
+    assert both(L, Problem(**change)) == (gs.GS_ERR_SHAPE,) * 2, say(L)
+
+
+def test_reach_of_scores_refused(L):
+    for B, lds in ((1 << 30, 1 << 39), (3, 1 << 62)):
+        assert L.gs_sample(0x1000, gs.GS_F32, B, 5, lds, 0x2000, None, 0x3000, None, None, None, 0, None) == gs.GS_ERR_SHAPE
+
+
 @pytest.mark.parametrize("scale", [0.0, float("nan"), float("inf"), -float("inf"), 1e-31, 1e31])
 def test_scales_refused(L, scale):
     assert both(L, Problem(scale=scale)) == (gs.GS_ERR_ARG,) * 2 and "scale" in say(L)
