@@ -2,9 +2,9 @@
 // D_i = sum_d dO_id O_id:
 //   dV = P^T dO     dP = dO V^T     dS = P (dP - D)
 //   dQ = scale dS K                 dK = scale dS^T Q
-// A first pass forms D.  Two passes then form P again instead of storing it:
-// one over the keys for each block of query rows (dQ), one over the query rows
-// for each block of keys (dK and dV).  A joint pass would save two of the seven
+// Two passes form P again instead of storing it: one over the keys for each
+// block of query rows (D and dQ), one over the query rows for each block of keys
+// (dK and dV).  A joint pass would save two of the seven
 // products, but one of its gradients would have to be summed across
 // work-groups in an order that changes from run to run; here every sum has a
 // fixed order.  Where there are few blocks, two halves of a work-group share
@@ -20,35 +20,6 @@
 namespace gs {
 namespace {
 using namespace attn;
-
-// What the passes need of a row: D, and -lse in units of log 2, the constant of
-// the exponent; minus infinity, so that exp2 gives 0, for rows that are not
-// there and rows without a live key.  A row in DP / PER lanes.
-template <typename T, int DP, bool VEC>
-__global__ void __launch_bounds__(256) xattn_rows_kernel(CrossAttnGradArgs a) {
-    constexpr int PER = Op<T>::PER, LANES = DP / PER, ROWS = 256 / LANES;      // (LANES divides 64)
-    const int c = threadIdx.x % LANES;
-    const int64_t rows = (int64_t)a.B * a.Hq * a.Lq;
-    for (int64_t at = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; at < rows; at += (int64_t)gridDim.x * ROWS) {
-        const int i = (int)(at % a.Lq), h = (int)(at / a.Lq % a.Hq), b = (int)(at / a.Lq / a.Hq);
-        const bool on = i < clamped(a.qlen, b, a.Lq);
-        float D = 0.f;
-        if (on) {
-            const u4v o = load_chunk<T>(static_cast<const T *>(a.O) + b * a.o.b + i * a.o.l + h * a.o.h, PER * c, a.Dh, VEC);
-            const u4v d = load_chunk<T>(static_cast<const T *>(a.dO) + b * a.d.b + i * a.d.l + h * a.d.h, PER * c, a.Dh, VEC);
-            const typename Op<T>::V x = *reinterpret_cast<const typename Op<T>::V *>(&o);
-            const typename Op<T>::V y = *reinterpret_cast<const typename Op<T>::V *>(&d);
-#pragma unroll
-            for (int e = 0; e < PER; ++e) D = fmaf((float)x[e], (float)y[e], D);
-        }
-#pragma unroll
-        for (int x = LANES / 2; x; x /= 2) D += __shfl_xor(D, x);
-        if (c) continue;
-        float e = -LOG2E * a.lse[at];
-        if (!on || e == INFINITY) e = -INFINITY;
-        a.stat[at] = f2v{e, D};
-    }
-}
 
 // Adds the sums of a work-group's second four waves to those of its first four;
 // true for the second, which have no more to do.
@@ -101,7 +72,23 @@ __global__ void __launch_bounds__(256 * GR, (sizeof(T) == 4 && DC > 64 ? 1 : 2))
     typename Op<T>::V q[NS], d[NS];
     load_frags<T, DC>(q, on ? static_cast<const T *>(a.Q) + b * a.q.b + row.i * a.q.l + row.h * a.q.h : nullptr, a.Dh, VEC, l);
     load_frags<T, DC>(d, on ? static_cast<const T *>(a.dO) + b * a.d.b + row.i * a.d.l + row.h * a.d.h : nullptr, a.Dh, VEC, l);
-    f2v st = on ? a.stat[((int64_t)b * a.Hq + row.h) * a.Lq + row.i] : f2v{-INFINITY, 0.f};
+    // What both passes need of a row: -lse in units of log 2, the constant of the
+    // exponent (minus infinity, so that exp2 gives 0, for rows that are not there
+    // and rows without a live key), and D.
+    const int64_t at_row = ((int64_t)b * a.Hq + row.h) * a.Lq + row.i;
+    f2v st = {-INFINITY, 0.f};
+    {
+        typename Op<T>::V y[NS];
+        load_frags<T, DC>(y, on ? static_cast<const T *>(a.O) + b * a.o.b + row.i * a.o.l + row.h * a.o.h : nullptr, a.Dh, VEC, l);
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int e = 0; e < PER; ++e) st[1] = fmaf((float)d[s][e], (float)y[s][e], st[1]);
+        st[1] += other_half(st[1]);
+        if (on) st[0] = -LOG2E * a.lse[at_row];
+        if (st[0] == INFINITY) st[0] = -INFINITY;
+        if (on && l < 32 && !group && sp == 0) a.stat[at_row] = st;
+    }
     const float c = a.scale * LOG2E;
     const T *const K = static_cast<const T *>(a.K) + b * a.k.b + hk * a.k.h;
     const T *const V = static_cast<const T *>(a.V) + b * a.v.b + hk * a.v.h;
@@ -152,7 +139,7 @@ __global__ void __launch_bounds__(256 * GR, (sizeof(T) == 4 && DC > 64 ? 1 : 2))
                 D += (bits >> (8 * (r / 4) + r % 4)) & 1 ? __builtin_amdgcn_exp2f(fmaf(p[r], c, st[0])) * g[r] : 0.f;
         }
         st[1] = D + other_half(D);
-        if (on && l < 32 && !group) a.stat[((int64_t)b * a.Hq + row.h) * a.Lq + row.i] = st;
+        if (on && l < 32 && !group) a.stat[at_row] = st;
     }
     for (; j0 < kend; j0 += STEP) {
         lds_barrier();
@@ -438,9 +425,6 @@ template <typename T, int DC, bool VEC> hipError_t launch_sized(const CrossAttnG
     const auto grid = [](int64_t n, int64_t per) { return dim3((unsigned)((n + per - 1) / per)); };
     hipError_t e = hipSuccess;
     if (a.q_groups) {
-        // (threads of a launch are counted in 32 bits: the rows of very large problems go round)
-        const int64_t rows = (int64_t)a.B * a.Hq * a.Lq, most = (int64_t)1 << 24;
-        xattn_rows_kernel<T, DP, VEC><<<grid(rows < most ? rows : most, 256 / (DP / Op<T>::PER)), dim3(256), 0, s>>>(a);
         const dim3 groups((unsigned)((a.q_groups + 7) / 8 * 8));
         if (EIGHT && p.q_waves == 8) xattn_dq_kernel<T, DC, EIGHT ? 2 : 1, BN, VEC><<<groups, dim3(512), 0, s>>>(a);
         else xattn_dq_kernel<T, DC, 1, BN, VEC><<<groups, dim3(256), 0, s>>>(a);
