@@ -233,7 +233,7 @@ template <typename F> __device__ __forceinline__ uint32_t least_key(uint32_t lo,
 // to `cut`, found by halving the range of keys.
 template <int E>
 __device__ __forceinline__ void draw_lanes(const SampleArgs &a, int64_t b, const Row &r, const Weigh &wt, uint32_t top,
-                                           const uint32_t (&key)[E], const int32_t (&j)[E], int n, int l) {
+                                           const uint32_t (&key)[E], const int32_t (&j)[E], int n, uint32_t *lds, int l) {
     auto count_from = [&](uint32_t c) {
         int m = 0;
 #pragma unroll
@@ -280,7 +280,19 @@ __device__ __forceinline__ void draw_lanes(const SampleArgs &a, int64_t b, const
         int in = 0, over = 0;                       // entries of [lo, hi], and over hi
 #pragma unroll
         for (int e = 0; e < E; ++e) in += __popcll(__ballot(keep[e]));
-        while (lo < hi && in > 1) {
+        // (m, x: mass and number of the entries from mid on)
+        auto halved = [&](uint32_t mid, uint64_t m, int x) {
+            if (x > 0 && (double)m >= goal) {
+                lo = mid;
+                in = x - over;
+            } else {
+                hi = mid - 1;
+                above = m;
+                in -= x - over;
+                over = x;
+            }
+        };
+        while (lo < hi && in > (E > 2 ? 64 : 1)) {
             const uint32_t mid = lo + (hi - lo) / 2 + 1;
             uint64_t m = 0;
             int x = 0;
@@ -290,15 +302,25 @@ __device__ __forceinline__ void draw_lanes(const SampleArgs &a, int64_t b, const
                 m += on ? mass[e] : 0;
                 x += __popcll(__ballot(on));
             }
-            m = wave_sum(m);
-            if (x > 0 && (double)m >= goal) {
-                lo = mid;
-                in = x - over;
-            } else {
-                hi = mid - 1;
-                above = m;
-                in -= x - over;
-                over = x;
+            halved(mid, wave_sum(m), x);
+        }
+        if (E > 2 && lo < hi && in > 1) {
+            // the entries still in question, one a lane
+            int at = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) at += below(__ballot(keep[e] && key[e] >= lo && key[e] <= hi), l);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (keep[e] && key[e] >= lo && key[e] <= hi) lds[at++] = key[e];
+            wave_sync();
+            const uint32_t k = l < in ? lds[l] : 0;
+            wave_sync();
+            const uint64_t one = k ? wt.mass(k) : 0, before = above;
+            const int ahead = over;
+            while (lo < hi && in > 1) {
+                const uint32_t mid = lo + (hi - lo) / 2 + 1;
+                const bool on = k >= mid;
+                halved(mid, before + wave_sum(on ? one : 0), ahead + __popcll(__ballot(on)));
             }
         }
         // [lo, hi] holds entries of one key at most: it is theirs
@@ -436,7 +458,7 @@ __global__ void __launch_bounds__(256, 4) sample_wave_kernel(SampleArgs a) {
             if (n <= 64) {
                 const uint32_t k[1] = {l < n ? lds[l] : 0};
                 const int32_t j[1] = {l < n ? (int32_t)lds[128 + l] : 0};
-                draw_lanes<1>(a, b, r, wt, top, k, j, n, l);
+                draw_lanes<1>(a, b, r, wt, top, k, j, n, lds, l);
             } else {
                 uint32_t k[2];
                 int32_t j[2];
@@ -446,7 +468,7 @@ __global__ void __launch_bounds__(256, 4) sample_wave_kernel(SampleArgs a) {
                     k[e] = in ? lds[2 * l + e] : 0;
                     j[e] = in ? (int32_t)lds[128 + 2 * l + e] : 0;
                 }
-                draw_lanes<2>(a, b, r, wt, top, k, j, n, l);
+                draw_lanes<2>(a, b, r, wt, top, k, j, n, lds, l);
             }
             return;
         }
@@ -457,7 +479,7 @@ __global__ void __launch_bounds__(256, 4) sample_wave_kernel(SampleArgs a) {
     int n = 0;
 #pragma unroll
     for (int e = 0; e < E; ++e) n += __popcll(__ballot(key[e] != 0));
-    draw_lanes<E>(a, b, r, wt, top, key, j, n, l);
+    draw_lanes<E>(a, b, r, wt, top, key, j, n, lds, l);
 }
 
 // ------------------------------------------------------------- a thread a row
@@ -837,6 +859,7 @@ struct Listed {
     static constexpr int PER = CAP / NT;
     uint32_t key[PER], j[PER];
     uint64_t mass[PER];
+    uint32_t places;            // indices lie below this
     int turn = 0;               // (two sets of partial sums: one barrier a sum)
     // sums over the entries that `on` takes, of 1 or of their masses
     template <typename F> __device__ __forceinline__ uint64_t sum(Shared &sh, bool by_mass, F on) {
@@ -877,7 +900,7 @@ struct Listed {
         double need = by_mass ? (one ? ceil((n - (double)over) / (double)one) : 1.) : n - (double)over;
         if (need < 1.) need = 1.;
         if (need >= (double)same) return End{lo, LAST};
-        uint32_t a = 0, b = LAST;       // the smallest index with `need` of them up to it
+        uint32_t a = 0, b = places - 1;     // the smallest index with `need` of them up to it
         while (a < b) {
             const uint32_t mid = a + (b - a) / 2;
             if ((double)sum(sh, false, [&](int i) { return key[i] == lo && j[i] <= mid; }) >= need) b = mid;
@@ -958,11 +981,12 @@ __device__ __forceinline__ End end_of_ranked_list(Shared &sh, const Row &r, cons
 
 // The end of the run from the listed entries (n <= CAP, in sh.list as key and
 // index): top_k's, then top_p's within it.
-__device__ __forceinline__ End end_of_list(Shared &sh, const Row &r, const Weigh &wt, int n) {
+__device__ __forceinline__ End end_of_list(Shared &sh, const Row &r, const Weigh &wt, int n, uint32_t places) {
     if (n <= 64) return end_of_short_list(sh, r, wt, n);
     if (n <= NT) return end_of_ranked_list(sh, r, wt, n);
     const Plan p = sh.plan;
     Listed e;
+    e.places = places;
 #pragma unroll
     for (int i = 0; i < Listed::PER; ++i) {
         const int x = i * NT + threadIdx.x;
@@ -1278,7 +1302,7 @@ __global__ void __launch_bounds__(NT, 3) sample_group_kernel(SampleArgs a) {
             __syncthreads();
         }
         if (listed > CAP) end = end_by_passes<T>(sh, a, b, r, wt, top, nullptr, 1);
-        else if (listed) end = end_of_list(sh, r, wt, (int)listed);
+        else if (listed) end = end_of_list(sh, r, wt, (int)listed, (uint32_t)a.M);
     }
     const uint64_t kept =
         chunk_parts<true>(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); }, sh.mass);
@@ -1439,7 +1463,7 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a) {
     for (int i = t; i < parts; i += NT) sh.mass[i] = 0;
     __syncthreads();
     End end = NO_END;
-    if (by_k || r.p < 1.) end = end_of_list(sh, r, wt, n);
+    if (by_k || r.p < 1.) end = end_of_list(sh, r, wt, n, (uint32_t)a.M);
     uint64_t kept = 0;
     for (int i = t; i < n; i += NT) {
         const uint32_t x = (uint32_t)(sh.list[i] >> 32), at = (uint32_t)sh.list[i];
@@ -1591,7 +1615,7 @@ __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
         } else if (listed) {
             for (int i = t; i < (int)listed; i += NT) sh.list[i] = rs->list[i];
             __syncthreads();
-            end = end_of_list(sh, r, wt, (int)listed);
+            end = end_of_list(sh, r, wt, (int)listed, (uint32_t)a.M);
             again = !here;
             if (here) {
                 // their masses to their parts' (exact sums: the order is of no account)
