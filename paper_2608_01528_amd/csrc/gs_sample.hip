@@ -1329,7 +1329,7 @@ __global__ void __launch_bounds__(NT) sample_top_kernel(SampleArgs a) {
     uint32_t top, low;
     ch.range(top, low);
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
+    for (int q = 0; q < Q && a.most; ++q) {
         uint32_t x = 0;
 #pragma unroll
         for (int c = 0; c < 4; ++c) x = max(x, ch.key[q][c]);
@@ -1672,7 +1672,7 @@ bool thread_a_row(int64_t M, int64_t B) { return M <= 8 || (M <= 32 && B >= (M <
 // entries, top_k 50 and top_p, one row: 12 us, a work-group 24; 2000 rows: 17,
 // 83), a work-group while it does (8000 entries, one row: 26 us, shared by
 // work-groups 39; 2000 rows: 93, 147).
-template <typename T> void launch_rows(const SampleArgs &a, hipStream_t s) {
+template <typename T> void launch_rows(SampleArgs a, hipStream_t s) {
     const int64_t rows = a.row1 - a.row0, places = a.vec ? a.M : a.M + 3;
     if (thread_a_row(a.M, a.B)) {
         if (a.M <= 8) return launch_thread<T, 8>(a, rows, s);
@@ -1691,16 +1691,18 @@ template <typename T> void launch_rows(const SampleArgs &a, hipStream_t s) {
     // no row with a run to end: launches 3 and 4 have nothing to do
     const bool all = !a.top_k && !a.top_p && (a.top_k_all <= 1 || a.top_k_all >= a.M) && !(a.top_p_all < 1.f);
     const dim3 grid((unsigned)(rows * a.chunks)), one((unsigned)rows);
-    sample_top_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
+    // one top_k for all rows, and a small one (temperature 0: one entry), in rows
+    // whose parts' sums fit: see the head for both sides' times
     const int parts = a.chunks * PARTS;
-    if (parts <= PARTS_HERE) {      // (the sums of more do not fit: see the head for both sides' times)
-        const bool first = !a.temperature && !(a.temperature_all > 0.f);
-        if (first || (!a.top_k && a.top_k_all >= 1 && a.top_k_all <= parts / 2)) {
-            sample_pick_kernel<T, true><<<one, dim3(NT), 0, s>>>(a);
-            return;
-        }
-        if (a.top_k && parts >= 256) sample_pick_kernel<T, false><<<one, dim3(NT), 0, s>>>(a);
+    const bool fits = parts <= PARTS_HERE, first = !a.temperature && !(a.temperature_all > 0.f);
+    const bool few = fits && (first || (!a.top_k && a.top_k_all >= 1 && a.top_k_all <= parts / 2));
+    a.most = few || !all;
+    sample_top_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
+    if (few) {
+        sample_pick_kernel<T, true><<<one, dim3(NT), 0, s>>>(a);
+        return;
     }
+    if (fits && a.top_k && parts >= 256) sample_pick_kernel<T, false><<<one, dim3(NT), 0, s>>>(a);
     sample_bins_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
     if (!all) {
         sample_plan_kernel<<<one, dim3(NT), 0, s>>>(a);

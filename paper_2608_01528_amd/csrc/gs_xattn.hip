@@ -14,8 +14,9 @@
 // two tiles side by side in one wave needed registers that cost more, 1.34 ms).
 // One position: bound by HBM (64 sequences of up to 4000 states, 32 heads over
 // 8 of 128 values: 601 MB in 135 us, 4.45 TB/s, where a large copy reaches
-// 4.77).  fp32 products take eight times as long as bf16 ones; 61 % of their
-// peak at 1024 x 1024 of 64 values, 59 % of 128.
+// 4.77).  fp32 products take eight times as long as bf16 ones: 61 % of the
+// library's rate at 1024 x 1024 of 64 values (the matrix cores are busy 67 % of
+// the cycles), 59 % of 128.
 #include "gs_attn.h"
 
 namespace gs {
@@ -264,7 +265,9 @@ constexpr int tile_keys(gs_dtype t, int waves) { return t == GS_F32 || waves == 
 // single waves, eight a CU in all if there are keys enough, in parts of at least
 // 128 keys in bf16 and, as products take eight times as long there, 32 (one tile)
 // in fp32 (4 sequences of 4 x 240, 4 heads of 96 values over one: 13 us, 31 in
-// parts of 128).  More rows go to work-groups of four or eight waves.
+// parts of 128).  More rows go to work-groups of four or eight waves (33
+// sequences of 19 x 3741, 2 heads of 72 values over one: bf16 22 us, 28 in single
+// waves; fp32 81 and 110).
 struct Plan {
     int waves, splits, split_keys, row_tiles, dp;
 };

@@ -12,9 +12,10 @@
 // last pass adds up.
 //
 // Bound by the matrix cores, the exponentials and the LDS reads between their
-// products: 4 x 16 heads of 2048 x 2048, 128 values, bf16: dQ 217 us (three
-// products, 950 TF/s), dK and dV 340 (four, 810 TF/s); fp32, 8 x 4 heads of
-// 1024 x 1024, 64 values: dQ 126 us (102 TF/s of 152), dK and dV 163 (105).
+// products: 4 x 16 heads of 2048 x 2048, 128 values, bf16: dQ 225 us (three
+// products, 920 TF/s), dK and dV 340 (four, 810 TF/s); fp32, 8 x 4 heads of
+// 1024 x 1024, 64 values: dQ 126 us (102 TF/s of 152; the matrix cores are busy
+// 75 % of its cycles), dK and dV 163 (105; 80 %).
 #include "gs_attn.h"
 
 namespace gs {

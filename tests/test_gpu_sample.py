@@ -93,6 +93,16 @@ def test_language_sized_tables(M, dtype):
         agree(S, u, **p)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_rows_beyond_a_million_bytes(dtype):
+    """More parts of 256 entries than one work-group holds sums of."""
+    S, u = scores(2, 300001, seed=3, dtype=dtype)
+    for p in ({}, {"temperature": 0.0}, {"top_k": 1}, {"top_k": 50}, {"top_k": 50, "top_p": 0.9}, {"top_p": 0.9}, {"top_p": 0.9, "min_p": 0.05},
+              {"min_p": 0.01}, {"top_k": torch.tensor([1, 60], dtype=torch.int32, device="cuda")},
+              {"temperature": torch.tensor([0.0, 1.5], device="cuda"), "top_k": 20}):
+        agree(S, u, **p)
+
+
 @pytest.mark.parametrize("M", [5, 40, 300, 3000, 40000])
 def test_parameters_of_each_row(M):
     B = 33
