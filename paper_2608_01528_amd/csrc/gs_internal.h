@@ -288,7 +288,7 @@ struct SampleArgs {
     void *ws;
     int64_t row0, row1, row_bytes;
     int chunks;
-    bool most;                          // the parts' largest keys are read by later launches
+    bool most, picked;                  // the parts' largest keys are read by later launches; a launch draws from some rows early
 };
 size_t sample_workspace(int64_t B, int64_t M);
 hipError_t launch_sample(gs_dtype st, SampleArgs a, void *ws, hipStream_t s);

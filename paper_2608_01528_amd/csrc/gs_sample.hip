@@ -698,7 +698,7 @@ struct ChunkSpace {
 struct Shared {
     Block block;
     double table[TABLE];
-    Hist hist;
+    alignas(16) Hist hist;
     uint64_t list[CAP];
     Plan plan;
     End end;
@@ -942,8 +942,9 @@ __device__ __forceinline__ End end_of_short_list(const Shared &sh, const Row &r,
     return End{(uint32_t)__builtin_amdgcn_readlane(key, at < 0 ? 0 : at), (uint32_t)__builtin_amdgcn_readlane(j, at < 0 ? 0 : at)};
 }
 
-// The same for up to 256 entries, one a thread; the masses in the place of the
-// histogram's.  (More are searched by halving the range of keys, a sum over the
+typedef uint64_t u8v __attribute__((ext_vector_type(2)));
+
+// The same for up to 256 entries, one a thread, in the place of the histogram.  (More are searched by halving the range of keys, a sum over the
 // work-group a step: some 10 us, where 256 comparisons take 3.)
 __device__ __forceinline__ End end_of_ranked_list(Shared &sh, const Row &r, const Weigh &wt, int n) {
     const Plan &p = sh.plan;
@@ -952,18 +953,20 @@ __device__ __forceinline__ End end_of_ranked_list(Shared &sh, const Row &r, cons
     const uint32_t key = (uint32_t)(v >> 32);
     const bool in_k = key && p.in_k(key), in_p = key && p.in_p(key);
     const uint64_t mass = key && r.p < 1. ? wt.mass(key) : 0;
-    sh.hist.mass[t] = in_p ? mass : 0;
+    // order and mass side by side; nothing behind the last entry
+    u8v *const pairs = reinterpret_cast<u8v *>(sh.hist.mass);
+    pairs[t] = t < n ? u8v{mine, in_p ? mass : 0} : u8v{0, 0};
     __syncthreads();
+    const uint64_t k_lo = (uint64_t)p.k_lo << 32, k_hi = (uint64_t)p.k_hi << 32 | LAST | 0x80000000u;
     uint64_t before_p = 0;
     int rank = 0, rank_k = 0;
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-        const uint64_t o = sh.list[i] ^ 0xffffffffu;
-        const bool first = o > mine;
+#pragma unroll 8
+    for (int i = 0; i < (n + 7) / 8 * 8; ++i) {
+        const u8v o = pairs[i];
+        const bool first = o[0] > mine;
         rank += first;
-        rank_k += first && p.in_k((uint32_t)(o >> 32));
-        const uint64_t m = sh.hist.mass[i];
-        before_p += first ? m : 0;
+        rank_k += first && o[0] >= k_lo && o[0] <= k_hi;
+        before_p += first ? o[1] : 0;
     }
     bool keep = key && (!in_k || (uint64_t)rank_k + p.count_k < (uint64_t)r.k);
     if (r.p < 1.) {
@@ -1488,7 +1491,7 @@ __global__ void __launch_bounds__(NT) sample_bins_kernel(SampleArgs a) {
     const Row r(a, b);
     if (r.takes_first()) return;
     RowSpace *const rs = row_space(a, slot);
-    if (rs->done) return;
+    if (a.picked && rs->done) return;
     ChunkSpace *const cs = chunk_space(rs);
     Chunk<T> ch;
     ch.load(a, b, chunk);
@@ -1521,7 +1524,7 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(SampleArgs a) {
     const Row r(a, b);
     if (r.takes_first() || r.keeps_all(a.M)) return;
     RowSpace *const rs = row_space(a, slot);
-    if (rs->done) return;
+    if (a.picked && rs->done) return;
     for (int i = t; i < BINS; i += NT) sh.hist.count[i] = rs->hist.count[i], sh.hist.mass[i] = rs->hist.mass[i];
     fill_table(sh.table, t);
     uint32_t top, low;
@@ -1546,7 +1549,7 @@ __global__ void __launch_bounds__(NT) sample_list_kernel(SampleArgs a) {
     const Row r(a, b);
     if (r.takes_first() || r.keeps_all(a.M)) return;
     RowSpace *const rs = row_space(a, slot);
-    if (rs->done) return;
+    if (a.picked && rs->done) return;
     ChunkSpace *const cs = chunk_space(rs);
     const uint32_t top = rs->top;
     if (!top) return;
@@ -1573,8 +1576,16 @@ __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
     const int t = threadIdx.x;
     const int64_t slot = blockIdx.x, b = a.row0 + slot;
     RowSpace *const rs = row_space(a, slot);
-    if (rs->done) return;
+    if (a.picked && rs->done) return;
     ChunkSpace *const cs = chunk_space(rs);
+    // asked for at once, whether the row needs it or not
+    const Row r(a, b);
+    const uint32_t planned = rs->plan.listed, sure = rs->plan.sure, in_question = rs->listed, least = rs->floor;
+    const uint64_t entry = rs->list[t];
+    const int parts = a.chunks * PARTS;
+    const bool here = parts <= PARTS_HERE;
+    if (here)
+        for (int i = t; i < parts; i += NT) sh.mass[i] = cs[i / PARTS].mass[i % PARTS];
     fill_table(sh.table, t);
     uint32_t top, low;
     row_range(sh.block, a, cs, top, low);
@@ -1582,7 +1593,6 @@ __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
         if (t == 0) put(a, b, -1, 0, 0, 0);
         return;
     }
-    const Row r(a, b);
     if (r.takes_first()) {
         uint32_t first = 0;     // complement of the first chunk that has it
         for (int i = t; i < a.chunks; i += NT)
@@ -1593,27 +1603,22 @@ __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
         return;
     }
     const Weigh wt(top, r.c, a.shift, sh.table);
-    const int parts = a.chunks * PARTS;
-    const bool here = parts <= PARTS_HERE;
     End end = NO_END;
     uint32_t floor;
     bool again = false;
     uint64_t more = 0;
-    if (here)
-        for (int i = t; i < parts; i += NT) sh.mass[i] = cs[i / PARTS].mass[i % PARTS];
     if (r.keeps_all(a.M)) {
         floor = floor_of(r, wt, top);
     } else {
         if (t == 0) sh.plan = rs->plan;
-        __syncthreads();
-        const Plan p = sh.plan;
-        const uint32_t listed = p.listed > CAP ? p.listed : rs->listed;
-        floor = rs->floor;
+        const uint32_t listed = planned > CAP ? planned : in_question;
+        floor = least;
         if (listed > CAP) {
             end = end_by_passes<T>(sh, a, b, r, wt, top, cs, 1);
             again = true;
         } else if (listed) {
-            for (int i = t; i < (int)listed; i += NT) sh.list[i] = rs->list[i];
+            sh.list[t] = entry;
+            for (int i = NT + t; i < (int)listed; i += NT) sh.list[i] = rs->list[i];
             __syncthreads();
             end = end_of_list(sh, r, wt, (int)listed, (uint32_t)a.M);
             again = !here;
@@ -1622,7 +1627,7 @@ __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
                 const int skew = skew_of(static_cast<const T *>(a.S) + b * a.lds);
                 for (int i = t; i < (int)listed; i += NT) {
                     const uint32_t x = (uint32_t)(sh.list[i] >> 32), j = (uint32_t)sh.list[i];
-                    if (x >= p.sure || x < floor || !end.has(x, j)) continue;
+                    if (x >= sure || x < floor || !end.has(x, j)) continue;
                     ++more;
                     atomicAdd((unsigned long long *)&sh.mass[(j + skew) / 256], (unsigned long long)wt.mass(x));
                 }
@@ -1702,7 +1707,8 @@ template <typename T> void launch_rows(SampleArgs a, hipStream_t s) {
         sample_pick_kernel<T, true><<<one, dim3(NT), 0, s>>>(a);
         return;
     }
-    if (fits && a.top_k && parts >= 256) sample_pick_kernel<T, false><<<one, dim3(NT), 0, s>>>(a);
+    a.picked = fits && a.top_k && parts >= 256;
+    if (a.picked) sample_pick_kernel<T, false><<<one, dim3(NT), 0, s>>>(a);
     sample_bins_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
     if (!all) {
         sample_plan_kernel<<<one, dim3(NT), 0, s>>>(a);
