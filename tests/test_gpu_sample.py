@@ -112,6 +112,28 @@ def test_parameters_of_each_row(M):
           top_p=(torch.rand(B, generator=g) * 1.1).cuda(), min_p=(torch.rand(B, generator=g) * 0.2).cuda())
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("M", [65536, 100003])
+def test_parameters_of_each_long_row(M, dtype):
+    """Rows that keep one entry, a few, many and all side by side; among them
+    rows without an entry, with fewer than top_k, sorted, and of equal scores."""
+    B = 24
+    S, u = scores(B, M, seed=M, dtype=dtype)
+    S[3] = -INF
+    S[5, 9:] = -INF
+    S[7] = S[7].sort().values
+    S[11] = 1.25
+    S[13, 5000:] = torch.finfo(dtype).min
+    k = torch.tensor([1, 2, 3, 5, 20, 50, 64, 70, 100, 130, 300, 40], dtype=torch.int32).repeat(2).cuda()
+    k[15], k[17], k[20] = 0, M, M // 2
+    T = torch.full((B,), 0.9, device="cuda")
+    T[8] = 0.0
+    p = torch.where(torch.arange(B, device="cuda") % 3 == 0, 1.0, 0.85)
+    agree(S, u, top_k=k)
+    agree(S, u, temperature=T, top_k=k, top_p=p)
+    agree(S, u, temperature=T, top_k=k, top_p=p, min_p=torch.rand(B, generator=torch.Generator().manual_seed(1)).cuda() * 0.1)
+
+
 @pytest.mark.parametrize("M", [3, 22, 64, 500, 2048, 9000, 70000])
 def test_equal_scores(M):
     """Ties by index: all equal, few different values, and the two zeros."""
