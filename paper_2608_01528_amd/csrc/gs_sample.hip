@@ -728,13 +728,16 @@ template <typename T> struct Chunk {
                 if (key[q][c]) f(key[q][c], q, c);
     }
     // the same without the parts whose largest key is below `from`
-    __device__ __forceinline__ void load_from(const SampleArgs &a, int64_t b, int chunk, const uint32_t *most, uint32_t from) {
+    __device__ __forceinline__ void load_from(const SampleArgs &a, int64_t b, int chunk, const ChunkSpace &cs, uint32_t from) {
+        uint32_t largest[Q];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) largest[q] = cs.most[q * (NT / 64) + (threadIdx.x >> 6)];
+        load_from(a, b, chunk, largest, from);
+    }
+    __device__ __forceinline__ void load_from(const SampleArgs &a, int64_t b, int chunk, const uint32_t (&largest)[Q], uint32_t from) {
         const T *const row = static_cast<const T *>(a.S) + b * a.lds;
         j0 = (int32_t)((uint32_t)chunk * CHUNK - (uint32_t)skew_of(row));
         Piece<T> piece[Q];
-        uint32_t largest[Q];
-#pragma unroll
-        for (int q = 0; q < Q; ++q) largest[q] = most[q * (NT / 64) + (threadIdx.x >> 6)];
 #pragma unroll
         for (int q = 0; q < Q; ++q)
             if (largest[q] >= from) piece[q].ask(row, (int32_t)at(q, 0), (uint32_t)a.M);
@@ -1025,7 +1028,7 @@ __device__ __forceinline__ End end_by_passes(Shared &sh, const SampleArgs &a, in
                                               uint32_t top, const ChunkSpace *cs, uint32_t least) {
     const int t = threadIdx.x;
     auto load = [&](Chunk<T> &ch, int c, uint32_t from) {
-        if (cs) ch.load_from(a, b, c, cs[c].most, from);
+        if (cs) ch.load_from(a, b, c, cs[c], from);
         else ch.load(a, b, c);
     };
     auto pass = [&](auto f) {
@@ -1153,7 +1156,7 @@ __device__ __forceinline__ uint64_t chunk_parts(Block &block, const Chunk<T> &ch
                 ++n;
             }
         }
-        m = wave_sum(m);
+        if (MOST || __ballot(m != 0)) m = wave_sum(m);
         if (l == 0) mass[q * (NT / 64) + w] = m;
     }
     return block.sum(n);
@@ -1448,7 +1451,7 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a) {
         Chunk<T> ch;
 #pragma unroll 1
         for (int i = 0; i < a.chunks; ++i) {
-            ch.load_from(a, b, i, cs[i].most, floor);
+            ch.load_from(a, b, i, cs[i], floor);
             kept += chunk_parts<false>(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); },
                                        sh.mass + i * PARTS);
         }
@@ -1550,23 +1553,26 @@ __global__ void __launch_bounds__(NT) sample_list_kernel(SampleArgs a) {
     if (r.takes_first() || r.keeps_all(a.M)) return;
     RowSpace *const rs = row_space(a, slot);
     if (a.picked && rs->done) return;
-    ChunkSpace *const cs = chunk_space(rs);
-    const uint32_t top = rs->top;
-    if (!top) return;
+    ChunkSpace &cs = chunk_space(rs)[chunk];
+    // asked for at once
+    uint32_t largest[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) largest[q] = cs.most[q * (NT / 64) + (t >> 6)];
+    const uint32_t top = rs->top, floor = rs->floor;
     const Plan p = rs->plan;
-    if (p.listed > CAP) return;
-    const uint32_t from = max(p.sure, rs->floor);
+    if (!top || p.listed > CAP) return;
+    const uint32_t from = max(p.sure, floor);
     uint32_t least = from;
     if (p.p_lo <= p.p_hi) least = min(least, p.p_lo);
     if (p.k_lo <= p.k_hi) least = min(least, p.k_lo);
     Chunk<T> ch;
-    ch.load_from(a, b, chunk, cs[chunk].most, least);
+    ch.load_from(a, b, chunk, largest, least);
     fill_table(table, t);
     __syncthreads();
     const Weigh wt(top, r.c, a.shift, table);
     list_asked(ch, p, &rs->listed, rs->list);
-    const uint64_t n = chunk_parts<false>(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= from; }, cs[chunk].mass);
-    if (t == 0) cs[chunk].count = (uint32_t)n;
+    const uint64_t n = chunk_parts<false>(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= from; }, cs.mass);
+    if (t == 0) cs.count = (uint32_t)n;
 }
 
 // Launch 5, a work-group a row: the listed entries ranked, and the draw.
@@ -1638,7 +1644,7 @@ __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
         // the whole row once more, now that the end of the run is known
         Chunk<T> ch;
         for (int i = 0; i < a.chunks; ++i) {
-            ch.load_from(a, b, i, cs[i].most, floor);
+            ch.load_from(a, b, i, cs[i], floor);
             const uint64_t n = chunk_parts<false>(sh.block, ch, wt, [&](uint32_t x, uint32_t j) { return x >= floor && end.has(x, j); },
                                            here ? sh.mass + i * PARTS : cs[i].mass);
             if (t == 0) cs[i].count = (uint32_t)n;
