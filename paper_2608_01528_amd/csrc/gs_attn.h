@@ -77,7 +77,11 @@ struct Deal {
 // of four waves that shares its CU with another one (alone, it takes 0.65 of
 // that; eight waves take two tiles in that time); a work-group takes about 3 us
 // besides.  `single`: one work-group of four waves a CU.  part_us: the time to
-// write and read one part of every block.
+// write and read one part of every block.  (Ten problems, both types, heads of 64
+// to 128 values, in 1 to 16 parts with four and with eight waves: the deal was
+// within 6 % of the best one in each, forward and gradient; where a block alone
+// fills the CUs, two parts cost 1.3 to 1.8 times one, and 3 x 600 x 600, 6 heads
+// of 128, fp32, 103 us in one part, 67 in the six dealt.)
 inline Deal deal_out(int64_t blocks, int64_t pieces, bool single, double piece_us, double part_us) {
     Deal best = {4, 1};
     double least = 1e300;
