@@ -509,11 +509,12 @@ __global__ void __launch_bounds__(64) sample_thread_kernel(SampleArgs a) {
     const Row r(a, b);
     const Weigh wt(top, r.c, a.shift, table);
     uint64_t mass[P];
-    uint32_t light = 0;                     // entries below min_p
+    uint32_t light = 0;                     // entries below min_p, told by their exponents
+    const double limit = r.least > 0. ? log2(r.least) * TABLE : -INFINITY;
 #pragma unroll
     for (int j = 0; j < P; ++j) {
         mass[j] = key[j] ? wt.mass(key[j]) : 0;
-        if (r.least > 0. && key[j] && wt.weight(key[j]) < r.least) light |= 1u << j;
+        if (key[j] && wt.scaled(key[j]) < limit) light |= 1u << j;
     }
     uint32_t keep = ~0u;
     if (r.k < M || r.p < 1.) {
