@@ -510,7 +510,8 @@ __global__ void __launch_bounds__(64) sample_thread_kernel(SampleArgs a) {
     const Weigh wt(top, r.c, a.shift, table);
     uint64_t mass[P];
     uint32_t light = 0;                     // entries below min_p, told by their exponents
-    const double limit = r.least > 0. ? log2(r.least) * TABLE : -INFINITY;
+    // (a weight within 2^-54 of 1 is 1: 64 log2(e) 2^-54 below the exponent 0)
+    const double limit = r.least > 0. ? log2(r.least) * TABLE - 5.2e-15 : -INFINITY;
 #pragma unroll
     for (int j = 0; j < P; ++j) {
         mass[j] = key[j] ? wt.mass(key[j]) : 0;

@@ -167,6 +167,14 @@ def test_where_the_large_scores_lie(M, dtype):
         agree(S, u, **p)
 
 
+@pytest.mark.parametrize("M", [5, 14, 22, 31, 64, 500, 2048, 9000, 70000])
+def test_temperatures_that_make_all_weights_one(M):
+    S, u = scores(5000 if M == 14 else 7, M, seed=M)
+    for T in (1e30, INF):
+        for p in ({"min_p": 1.0}, {"min_p": 0.5, "top_k": 3}, {"top_p": 0.5}):
+            agree(S, u, temperature=T, **p)
+
+
 @pytest.mark.parametrize("M", [4, 70, 3000, 30000])
 def test_rows_with_little_in_them(M):
     S = torch.full((9, M), -INF)
