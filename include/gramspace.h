@@ -607,9 +607,12 @@ gs_status gs_cross_attention_grad(const gs_cross_attn *a, gs_dtype t, void *ws, 
  *   ws          device workspace of >= gs_sample_workspace(st, B, M) bytes
  *               (0: none), 16-byte aligned, contents unspecified; calls that
  *               may run at the same time need one each
- * Weights are formed in fp64 and summed as whole multiples of 2^-s of the
- * largest, s = min(51, 62 - ceil(log2 M)), an entry of any weight counting at
- * least one: results do not depend on the order of a sum.
+ * Weights are formed in fp64 (4e-14 of each) and summed as whole multiples of a
+ * unit, an entry of any weight counting at least one: results do not depend on
+ * the order of a sum.  Up to 2^18 entries the unit is 2^-s of the largest weight,
+ * s = min(51, 62 - ceil(log2 M)): a sum is off by less than M 2^-s, at most 2^-26,
+ * of it.  Longer rows take their unit from their total: a sum is off by less than
+ * M 2^-60 of the weight of all entries.
  */
 typedef struct {
     const float *temperature; const int32_t *top_k; const float *top_p; const float *min_p;

@@ -1,11 +1,15 @@
 // An entry drawn from a row of scores: temperature, top-k, top-p, min-p, and a
 // given random number.
 //
-// Everything that decides is exact or in 64 bits.  Scores are ranked by an
-// order-preserving integer key; weights are formed in fp64 and held as whole
-// multiples of 2^-shift of the largest one, so their sums are integer sums: the
-// same in any order, whatever the split of a row over threads, and atomic sums
-// are as good as ordered ones.
+// Scores are ranked exactly, by an order-preserving integer key.  Weights are
+// formed in fp64 and held as whole multiples, at least one, of 2^-shift of the
+// largest one, so their sums are integer sums: the same in any order, whatever
+// the split of a row over threads, and atomic sums are as good as ordered ones.
+// Up to LONG_ROW entries the shift goes by the row's length: a sum is off by less
+// than M 2^-shift <= 2^-26 of the largest weight.  For longer rows that grows as
+// M^2 (a tail of no weight would come to a quarter of the largest entry at 2^30),
+// and the shift is taken from the row's total, which two more launches find: a
+// sum is off by less than M 2^-60 of the total.
 //
 // What is kept is a run of the entries in rank order (falling scores, equal
 // ones by index), thinned by min_p from its end: top_k and top_p each end it
@@ -17,7 +21,8 @@
 //                       scores below the largest finds the bin the run ends in
 //   work-groups a row   more entries: the same over chunks of 8192, in five
 //                       launches (largest scores, histogram, where the run ends,
-//                       entries in question, ranking and draw).  A launch
+//                       entries in question, ranking and draw; the two for the
+//                       total after the first).  A launch
 //                       boundary hands a row's data on faster than fences and
 //                       counters did, which write caches back from every
 //                       work-group: 200 rows of 128001 took 402 and 511 us in
@@ -66,12 +71,13 @@ __device__ __forceinline__ void fill_table(double *table, int t) {
 // to f^4 (the next term is below 4e-14 of the weight).  Whole parts and
 // multiples are taken by adding a power of two whose last place is the unit
 // (no conversions between fp64 and integers).
-struct Weigh {
+// LONG: rows of more than LONG_ROW entries.
+template <bool LONG> struct WeighOf {
     double m, c;                // largest score; 64 log2(e) / temperature
-    int shift;                  // a mass of 2^shift (at most 2^51) is the largest weight
+    int shift;                  // a mass of 2^shift (at most 2^51; LONG: 2^61) is the largest weight
     const double *table;
     // an infinite largest score leaves weight to its equals alone
-    __device__ __forceinline__ Weigh(uint32_t top, double c64, int s, const double *t)
+    __device__ __forceinline__ WeighOf(uint32_t top, double c64, int s, const double *t)
         : m(fmin((double)value_of(top), 1e300)), c(c64), shift(s), table(t) {}
     __device__ __forceinline__ double scaled(uint32_t key) const { return fmin(((double)value_of(key) - m) * c, 0.); }
     __device__ __forceinline__ double part(double y, int &n) const {     // 2^(y / 64) = part 2^n
@@ -94,10 +100,13 @@ struct Weigh {
         int n;
         const double w = part(fmax(y, -70. * TABLE), n);
         const double v = __longlong_as_double(__double_as_longlong(w) + (int64_t)(n + shift) * (1ll << 52));
-        const uint64_t r = (uint64_t)__double_as_longlong(v + 4503599627370496.) & 0xfffffffffffffull;      // 2^52
+        const uint64_t r = LONG ? (uint64_t)(v + 0.5)
+                                : (uint64_t)__double_as_longlong(v + 4503599627370496.) & 0xfffffffffffffull;   // 2^52
         return r ? r : (y > -1074. * TABLE ? 1 : 0);
     }
 };
+typedef WeighOf<false> Weigh;
+constexpr int64_t LONG_ROW = (int64_t)1 << 18;
 
 // A row's parameters, brought into range.
 struct Row {
@@ -686,8 +695,9 @@ struct RowSpace {
     Hist hist;
     Plan plan;
     uint32_t listed, floor;     // entries listed; the smallest key that min_p keeps
-    uint32_t top;               // the largest key
-    uint32_t done;              // drawn from already
+    uint32_t top, low;          // the largest key and (long rows) the smallest
+    uint64_t total;             // long rows: the sum of all masses at the shift that goes by the length
+    uint32_t done, pad;         // drawn from already
     uint64_t list[CAP];
 };
 struct ChunkSpace {
@@ -780,7 +790,7 @@ __device__ __forceinline__ void list_asked(const Chunk<T> &ch, const Plan &p, ui
 }
 
 // The smallest key that min_p keeps.
-__device__ __forceinline__ uint32_t floor_of(const Row &r, const Weigh &wt, uint32_t top) {
+template <typename W> __device__ __forceinline__ uint32_t floor_of(const Row &r, const W &wt, uint32_t top) {
     if (!(r.least > 0.)) return 1;
     return least_key(LOWEST, top, threadIdx.x & 63, [&](uint32_t k) { return wt.weight(k) >= r.least; });
 }
@@ -917,7 +927,7 @@ struct Listed {
 
 // The same for up to 64 entries, by every wave for itself: an entry a lane,
 // compared with all of them.
-__device__ __forceinline__ End end_of_short_list(const Shared &sh, const Row &r, const Weigh &wt, int n) {
+template <typename W> __device__ __forceinline__ End end_of_short_list(const Shared &sh, const Row &r, const W &wt, int n) {
     const Plan &p = sh.plan;
     const int l = threadIdx.x & 63;
     const uint64_t v = l < n ? sh.list[l] : 0;
@@ -949,9 +959,10 @@ __device__ __forceinline__ End end_of_short_list(const Shared &sh, const Row &r,
 
 typedef uint64_t u8v __attribute__((ext_vector_type(2)));
 
-// The same for up to 256 entries, one a thread, in the place of the histogram.  (More are searched by halving the range of keys, a sum over the
-// work-group a step: some 10 us, where 256 comparisons take 3.)
-__device__ __forceinline__ End end_of_ranked_list(Shared &sh, const Row &r, const Weigh &wt, int n) {
+// The same for up to 256 entries, one a thread, in the place of the histogram.
+// (More are searched by halving the range of keys, a sum over the work-group a
+// step: some 10 us, where 256 comparisons take 3.)
+template <typename W> __device__ __forceinline__ End end_of_ranked_list(Shared &sh, const Row &r, const W &wt, int n) {
     const Plan &p = sh.plan;
     const int t = threadIdx.x;
     const uint64_t v = t < n ? sh.list[t] : 0, mine = v ^ 0xffffffffu;      // in rank order: larger keys, then smaller indices
@@ -989,7 +1000,8 @@ __device__ __forceinline__ End end_of_ranked_list(Shared &sh, const Row &r, cons
 
 // The end of the run from the listed entries (n <= CAP, in sh.list as key and
 // index): top_k's, then top_p's within it.
-__device__ __forceinline__ End end_of_list(Shared &sh, const Row &r, const Weigh &wt, int n, uint32_t places) {
+template <typename W>
+__device__ __forceinline__ End end_of_list(Shared &sh, const Row &r, const W &wt, int n, uint32_t places) {
     if (n <= 64) return end_of_short_list(sh, r, wt, n);
     if (n <= NT) return end_of_ranked_list(sh, r, wt, n);
     const Plan p = sh.plan;
@@ -1025,8 +1037,8 @@ __device__ __forceinline__ End end_of_list(Shared &sh, const Row &r, const Weigh
 // keys in question is divided by 2048 until it is one key, by whole passes over
 // the row, or over the parts of it that reach `least`, the entries below which
 // are known to lie behind the end (cs: the row's chunks, null if it is one).
-template <typename T>
-__device__ __forceinline__ End end_by_passes(Shared &sh, const SampleArgs &a, int64_t b, const Row &r, const Weigh &wt,
+template <typename T, typename W>
+__device__ __forceinline__ End end_by_passes(Shared &sh, const SampleArgs &a, int64_t b, const Row &r, const W &wt,
                                               uint32_t top, const ChunkSpace *cs, uint32_t least) {
     const int t = threadIdx.x;
     auto load = [&](Chunk<T> &ch, int c, uint32_t from) {
@@ -1138,8 +1150,8 @@ __device__ __forceinline__ End end_by_passes(Shared &sh, const SampleArgs &a, in
 // MOST of them: masses are formed for all, without branches, several side by
 // side; otherwise for those kept, where a wave has any (the nucleus of 200 rows
 // of 128001: 39 us for their list launch, 54 with all masses).
-template <bool MOST, typename T, typename F>
-__device__ __forceinline__ uint64_t chunk_parts(Block &block, const Chunk<T> &ch, const Weigh &wt, F has, uint64_t *mass) {
+template <bool MOST, typename T, typename W, typename F>
+__device__ __forceinline__ uint64_t chunk_parts(Block &block, const Chunk<T> &ch, const W &wt, F has, uint64_t *mass) {
     const int t = threadIdx.x, l = t & 63, w = t >> 6;
     uint64_t n = 0;
 #pragma unroll
@@ -1165,8 +1177,8 @@ __device__ __forceinline__ uint64_t chunk_parts(Block &block, const Chunk<T> &ch
 }
 
 // Draws from a row of whose `parts` parts `mass_of` tells the masses.
-template <typename T, typename F>
-__device__ __forceinline__ void draw_parts(Shared &sh, const SampleArgs &a, int64_t b, const Weigh &wt, End end,
+template <typename T, typename W, typename F>
+__device__ __forceinline__ void draw_parts(Shared &sh, const SampleArgs &a, int64_t b, const W &wt, End end,
                                            uint32_t floor, uint64_t kept, int parts, F mass_of) {
     const int t = threadIdx.x, l = t & 63;
     const float u = a.u[b];
@@ -1235,8 +1247,8 @@ __device__ __forceinline__ void draw_first(Shared &sh, const SampleArgs &a, int6
     if (threadIdx.x == 0) put(a, b, (int32_t)~mine, 1, 1, 1);
 }
 
-template <typename T>
-__device__ __forceinline__ void count_bins(Hist &h, const Chunk<T> &ch, const Row &r, const Weigh &wt, const Binning &bins,
+template <typename T, typename W>
+__device__ __forceinline__ void count_bins(Hist &h, const Chunk<T> &ch, const Row &r, const W &wt, const Binning &bins,
                                            bool by_k) {
     const bool by_p = r.p < 1.;
     uint32_t rest_n = 0;        // of the last bin, which many entries may share
@@ -1330,7 +1342,7 @@ __global__ void __launch_bounds__(NT) sample_top_kernel(SampleArgs a) {
     const int64_t slot = blockIdx.x / a.chunks, b = a.row0 + slot;
     RowSpace *const rs = row_space(a, slot);
     for (int i = chunk * NT + t; i < BINS; i += a.chunks * NT) rs->hist.count[i] = 0, rs->hist.mass[i] = 0;
-    if (chunk == 0 && t == 0) rs->listed = 0, rs->done = 0;
+    if (chunk == 0 && t == 0) rs->listed = 0, rs->done = 0, rs->total = 0;
     Chunk<T> ch;
     ch.load(a, b, chunk);
     ChunkSpace &cs = chunk_space(rs)[chunk];
@@ -1356,6 +1368,47 @@ __device__ __forceinline__ void row_range(Block &block, const SampleArgs &a, con
     for (int i = threadIdx.x; i < a.chunks; i += NT) top = max(top, cs[i].top), low = max(low, ~cs[i].low);
     top = block.most(top);
     low = ~block.most(low);
+}
+
+// Long rows, after launch 1: their range, a work-group a row (that every chunk of
+// the launches that follow reads the ranges of all of them costs more than the
+// row's scores from some 2^26 entries on) ...
+__global__ void __launch_bounds__(NT) sample_range_kernel(SampleArgs a) {
+    __shared__ Block block;
+    RowSpace *const rs = row_space(a, blockIdx.x);
+    uint32_t top, low;
+    row_range(block, a, chunk_space(rs), top, low);
+    if (threadIdx.x == 0) rs->top = top, rs->low = low;
+}
+// ... and their total, at the shift that goes by the length.
+template <typename T>
+__global__ void __launch_bounds__(NT) sample_total_kernel(SampleArgs a) {
+    __shared__ Block block;
+    __shared__ double table[TABLE];
+    const int t = threadIdx.x, chunk = blockIdx.x % a.chunks;
+    const int64_t slot = blockIdx.x / a.chunks, b = a.row0 + slot;
+    const Row r(a, b);
+    if (r.takes_first()) return;
+    RowSpace *const rs = row_space(a, slot);
+    const uint32_t top = rs->top;
+    if (!top) return;
+    Chunk<T> ch;
+    ch.load(a, b, chunk);
+    fill_table(table, t);
+    __syncthreads();
+    const Weigh wt(top, r.c, a.shift, table);
+    uint64_t m = 0;
+    ch.each([&](uint32_t x, int, int) { m += wt.mass(x); });
+    m = block.sum(m);
+    if (t == 0) atomicAdd((unsigned long long *)&rs->total, (unsigned long long)m);
+}
+// With total < 2^e at the shift s a row's weight is below 3/2 2^(e - s) of its
+// largest one (no mass is less than 2/3 of its weight), so that its masses at the
+// shift s + 62 - e sum up to less than 3/2 2^62 + M; and as rounding up to one adds
+// at most M 2^-s <= 1, that is to say the largest weight at most, to the total, a
+// unit of that shift is below 2^-60 of the row's weight.
+template <bool LONG> __device__ __forceinline__ int shift_of(const SampleArgs &a, const RowSpace *rs) {
+    return LONG ? a.shift + __clzll((long long)rs->total) - 2 : a.shift;
 }
 
 // Rows of which top_k keeps a few, a work-group a row: a key that the largest
@@ -1486,7 +1539,7 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a) {
 
 // Launch 2: the histogram of the row; for rows without top_k and top_p the
 // chunk's mass.
-template <typename T>
+template <typename T, bool LONG>
 __global__ void __launch_bounds__(NT) sample_bins_kernel(SampleArgs a) {
     __shared__ Block block;
     __shared__ double table[TABLE];
@@ -1503,9 +1556,14 @@ __global__ void __launch_bounds__(NT) sample_bins_kernel(SampleArgs a) {
     fill_table(table, t);
     clear(hist);
     uint32_t top, low;
-    row_range(block, a, cs, top, low);
+    if constexpr (LONG) {
+        top = rs->top, low = rs->low;
+        __syncthreads();
+    } else {
+        row_range(block, a, cs, top, low);
+    }
     if (!top) return;
-    const Weigh wt(top, r.c, a.shift, table);
+    const WeighOf<LONG> wt(top, r.c, shift_of<LONG>(a, rs), table);
     const uint32_t floor = floor_of(r, wt, top);
     if (r.keeps_all(a.M)) {
         const uint64_t n = chunk_parts<true>(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= floor; }, cs[chunk].mass);
@@ -1545,7 +1603,7 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(SampleArgs a) {
 
 // Launch 4: the entries in question listed, the mass of those before them
 // summed.
-template <typename T>
+template <typename T, bool LONG>
 __global__ void __launch_bounds__(NT) sample_list_kernel(SampleArgs a) {
     __shared__ Block block;
     __shared__ double table[TABLE];
@@ -1571,14 +1629,14 @@ __global__ void __launch_bounds__(NT) sample_list_kernel(SampleArgs a) {
     ch.load_from(a, b, chunk, largest, least);
     fill_table(table, t);
     __syncthreads();
-    const Weigh wt(top, r.c, a.shift, table);
+    const WeighOf<LONG> wt(top, r.c, shift_of<LONG>(a, rs), table);
     list_asked(ch, p, &rs->listed, rs->list);
     const uint64_t n = chunk_parts<false>(block, ch, wt, [&](uint32_t x, uint32_t) { return x >= from; }, cs.mass);
     if (t == 0) cs.count = (uint32_t)n;
 }
 
 // Launch 5, a work-group a row: the listed entries ranked, and the draw.
-template <typename T>
+template <typename T, bool LONG>
 __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
     __shared__ Shared sh;
     const int t = threadIdx.x;
@@ -1610,7 +1668,7 @@ __global__ void __launch_bounds__(NT) sample_draw_kernel(SampleArgs a) {
         draw_first(sh, a, b, ch, top);
         return;
     }
-    const Weigh wt(top, r.c, a.shift, sh.table);
+    const WeighOf<LONG> wt(top, r.c, shift_of<LONG>(a, rs), sh.table);
     End end = NO_END;
     uint32_t floor;
     bool again = false;
@@ -1681,6 +1739,16 @@ template <typename T, int P> void launch_thread(const SampleArgs &a, int64_t row
 //   32 entries  8192 rows 18.3, 11.7;  16384 rows 18.5, 18.9;  65536 rows 21.6, 59
 bool thread_a_row(int64_t M, int64_t B) { return M <= 8 || (M <= 32 && B >= (M <= 16 ? 4096 : (M <= 24 ? 12288 : 16384))); }
 
+// Launches 2 to 5 (3 and 4 have nothing to do if `all` rows have no run to end).
+template <typename T, bool LONG> void launch_shared(const SampleArgs &a, dim3 grid, dim3 one, bool all, hipStream_t s) {
+    sample_bins_kernel<T, LONG><<<grid, dim3(NT), 0, s>>>(a);
+    if (!all) {
+        sample_plan_kernel<<<one, dim3(NT), 0, s>>>(a);
+        sample_list_kernel<T, LONG><<<grid, dim3(NT), 0, s>>>(a);
+    }
+    sample_draw_kernel<T, LONG><<<one, dim3(NT), 0, s>>>(a);
+}
+
 // Rows row0 .. row1 - 1.  A wave a row while its lanes hold the row (2045
 // entries, top_k 50 and top_p, one row: 12 us, a work-group 24; 2000 rows: 17,
 // 83), a work-group while it does (8000 entries, one row: 26 us, shared by
@@ -1701,7 +1769,7 @@ template <typename T> void launch_rows(SampleArgs a, hipStream_t s) {
         sample_group_kernel<T><<<dim3((unsigned)rows), dim3(NT), 0, s>>>(a);
         return;
     }
-    // no row with a run to end: launches 3 and 4 have nothing to do
+    // no row with a run to end
     const bool all = !a.top_k && !a.top_p && (a.top_k_all <= 1 || a.top_k_all >= a.M) && !(a.top_p_all < 1.f);
     const dim3 grid((unsigned)(rows * a.chunks)), one((unsigned)rows);
     // one top_k for all rows, and a small one (temperature 0: one entry), in rows
@@ -1717,12 +1785,13 @@ template <typename T> void launch_rows(SampleArgs a, hipStream_t s) {
     }
     a.picked = fits && a.top_k && parts >= 256;
     if (a.picked) sample_pick_kernel<T, false><<<one, dim3(NT), 0, s>>>(a);
-    sample_bins_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
-    if (!all) {
-        sample_plan_kernel<<<one, dim3(NT), 0, s>>>(a);
-        sample_list_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
+    if (a.M > LONG_ROW) {
+        sample_range_kernel<<<one, dim3(NT), 0, s>>>(a);
+        sample_total_kernel<T><<<grid, dim3(NT), 0, s>>>(a);
+        launch_shared<T, true>(a, grid, one, all, s);
+    } else {
+        launch_shared<T, false>(a, grid, one, all, s);
     }
-    sample_draw_kernel<T><<<one, dim3(NT), 0, s>>>(a);
 }
 
 template <typename T> hipError_t launch_typed(SampleArgs a, void *ws, hipStream_t s) {

@@ -1,0 +1,167 @@
+"""Rows of scores far longer than a language's table: one entry at 0, every
+other one at -x, so that the weights and their sums are known in closed form,
+and drawn rows against the definition in 64 bits.
+
+With W = 1 + (M - 1) e^-x the first entry's share is 1 / W.  Sums are off by
+M 2^-60 W at most (2^-30 of W for the longest row here), weights by 4e-14 of
+themselves; a share's own rounding is 2^-24 of it."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_01528_amd import gramspace as gs
+from test_gpu_sample import agree, scores
+
+pytestmark = pytest.mark.gpu
+
+INF = float("inf")
+
+
+def rows(M, at, below, dtype=torch.bfloat16):
+    S = torch.empty(len(below), M, dtype=dtype, device="cuda")
+    for b, x in enumerate(below):
+        S[b] = -x
+        S[b, at] = 0.0
+    return S
+
+
+def fp32(*v):
+    return torch.tensor(v, dtype=torch.float32, device="cuda")
+
+
+LENGTHS = [(1 << 18) + 1, (1 << 20) - 3, 1 << 24, (1 << 27) + 5]
+
+
+@pytest.mark.parametrize("M", LENGTHS)
+def test_tails_weigh_what_their_entries_do(M):
+    """Tails of no weight, of about half the largest entry's, and of more."""
+    at, below = M // 3, [100.0, 18.0, 20.0, 9.5]
+    S = rows(M, at, below)
+    for form in ({}, {"min_p": 1e-30}):
+        for u in (0.0001, 0.31, 0.97):
+            idx, prob, kept = (t.tolist() for t in gs.gs_sample(S, fp32(*[u] * 4), prob=True, kept=True, **form))
+            u32 = float(np.float32(u))
+            for b, x in enumerate(below):
+                least = form.get("min_p", 0.0)
+                w = math.exp(-x)
+                if w < least:
+                    w = 0.0
+                W = 1.0 + (M - 1) * w
+                assert kept[b] == (M if w else 1), (x, u)
+                # entries before `at` weigh at * w
+                before = at * w
+                goal = u32 * W
+                if goal < before:
+                    want, share = goal / w, w / W
+                elif goal < before + 1.0:
+                    want, share = at, 1.0 / W
+                else:
+                    want, share = at + (goal - before - 1.0) / w, w / W
+                # the sums' error and the weights', counted in entries of the tail; one for the border itself
+                slack = 1.0 + (0.0 if not w else W * (M * 2.0 ** -60 + 1e-13) / w)
+                near = min(abs(goal - before), abs(goal - before - 1.0)) <= 1e-9 * W
+                assert near or abs(idx[b] - want) <= slack, (x, u, idx[b], want, slack)
+                assert near or abs(prob[b] - share) <= 2.0 ** -23 * share, (x, u, prob[b], share)
+
+
+@pytest.mark.parametrize("M", LENGTHS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_one_entry_has_the_nucleus(M, dtype):
+    """A tail below 1e-34 of the largest entry's weight: the entry alone has
+    any top_p."""
+    at = M - 2
+    S = rows(M, at, [100.0, 100.0], dtype)
+    u = fp32(0.5, 1.0 - 2.0 ** -24)
+    for p in (0.5, 0.999, 1.0 - 2.0 ** -24):
+        idx, prob, kept = gs.gs_sample(S, u, top_p=p, prob=True, kept=True)
+        assert idx.tolist() == [at, at] and kept.tolist() == [1, 1] and prob.tolist() == [1.0, 1.0], p
+    idx, prob, kept = gs.gs_sample(S, u, prob=True, kept=True)
+    assert idx.tolist() == [at, at] and kept.tolist() == [M, M] and prob.tolist() == [1.0, 1.0]
+
+
+def test_a_run_that_ends_in_the_tail():
+    """top_p among equal entries of small weight: as many as it takes, by index."""
+    M, x, p = 1 << 24, 16.0, 0.75
+    S = rows(M, 77, [x])
+    w = math.exp(-x)
+    W = 1.0 + (M - 1) * w
+    idx, prob, kept = gs.gs_sample(S, fp32(0.0), top_p=p, prob=True, kept=True)
+    want = 1 + math.ceil((p * W - 1.0) / w)
+    slack = 1.0 + W * (M * 2.0 ** -60 + 1e-13) / w
+    assert abs(int(kept) - want) <= slack and int(idx) == 0
+    share = w / (1.0 + (want - 1) * w)
+    assert abs(float(prob) - share) <= (2.0 ** -23 + 2 * slack / want) * share
+
+
+def test_a_thousand_million_entries():
+    """The largest entry's share where the others weigh nothing, and a half."""
+    M = 1 << 30
+    for x in (100.0, 20.75):
+        S = rows(M, M - 7, [x])
+        W = 1.0 + (M - 1) * math.exp(-x)
+        idx, prob, kept = gs.gs_sample(S, fp32(1.0 - 0.5 / W), prob=True, kept=True)
+        assert int(idx) == M - 7 and int(kept) == M and abs(float(prob) * W - 1.0) <= 2.0 ** -23
+        del S
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("M", [262144, 262145, 700001])
+def test_drawn_rows(M, dtype):
+    """Rows on either side of the length from which on a row has a unit of its own."""
+    S, u = scores(4, M, seed=M, dtype=dtype)
+    S[1, M // 2:] = -INF
+    S[2, 3] = INF
+    for p in ({}, {"temperature": 0.4, "top_p": 0.9}, {"top_k": 70, "top_p": 0.8}, {"min_p": 0.01}, {"top_p": 0.999, "min_p": 1e-6},
+              {"temperature": fp32(0.0, 1e30, 0.7, 2.0), "top_k": torch.tensor([5, 0, 300, 1], dtype=torch.int32, device="cuda")}):
+        agree(S, u, **p)
+
+
+def test_long_rows_with_nothing_or_little_in_them():
+    M = 300007
+    S = torch.full((5, M), -INF, device="cuda")
+    S[1, M - 1] = -3.0
+    S[2] = float("nan")
+    S[3] = torch.finfo(torch.float32).min
+    S[4, 5], S[4, M - 3] = INF, INF
+    u = fp32(0.3, 0.3, 0.3, 0.3, 0.7)
+    for p in ({}, {"top_p": 0.9}, {"top_k": 2}, {"min_p": 0.5}, {"temperature": 0.0}):
+        idx = agree(S, u, **p)
+        assert idx[0] == -1 and idx[1] == M - 1 and idx[2] == -1
+
+
+@pytest.mark.parametrize("off", [0, 1, 3])
+def test_a_row_gives_the_same_wherever_it_lies(off):
+    """The unit of a row's masses does not depend on how the row is split."""
+    M = 300001
+    S, u = scores(3, M, seed=9)
+    p = {"top_p": 0.97, "temperature": 1.2}
+    want = gs.gs_sample(S, u, prob=True, kept=True, **p)
+    wide = torch.full((3, M + 7), INF, device="cuda")
+    view = wide[:, off: off + M]
+    view.copy_(S)
+    for g, w in zip(gs.gs_sample(view, u, prob=True, kept=True, **p), want):
+        assert torch.equal(g, w)
+
+
+def test_captured_long_rows():
+    M = 400000
+    S, u = scores(2, M, seed=6)
+    p = {"top_p": 0.9, "temperature": 0.8}
+    call = lambda: gs.gs_sample(S, u, prob=True, kept=True, **p)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = call()
+    for seed in (7, 8, 9):
+        X, v = scores(2, M, seed=seed, spread=float(seed))
+        S.copy_(X)
+        u.copy_(v)
+        g.replay()
+        torch.cuda.synchronize()
+        want = call()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b), seed
