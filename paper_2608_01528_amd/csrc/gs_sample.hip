@@ -40,6 +40,8 @@
 // launch that does nothing), many by the fp64 work of the weights: some 40
 // instructions an entry, 25.6 million of which take 30 us of 53 in the histogram
 // launch for 200 rows of 128001; the scores alone would be read in 11.
+#include <algorithm>
+
 #include "gs_internal.h"
 
 namespace gs {
@@ -1723,6 +1725,7 @@ constexpr int64_t SHARED_ROWS = 2048, ROWS = (int64_t)1 << 22;
 
 size_t row_bytes(int64_t chunks) { return sizeof(RowSpace) + (size_t)chunks * sizeof(ChunkSpace); }
 int64_t chunks_of(int64_t M) { return (M + 3 + CHUNK - 1) / CHUNK; }     // (a row's places: its entries and up to 3 before)
+int64_t shared_rows(int64_t M) { return std::min(SHARED_ROWS, ROWS / chunks_of(M)); }
 
 template <typename T, int E> void launch_wave(const SampleArgs &a, int64_t rows, hipStream_t s) {
     sample_wave_kernel<T, E><<<dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s>>>(a);
@@ -1799,8 +1802,7 @@ template <typename T> hipError_t launch_typed(SampleArgs a, void *ws, hipStream_
     a.chunks = (int)chunks_of(a.M);
     a.row_bytes = row_bytes(a.chunks);
     a.ws = ws;
-    int64_t most = shared ? SHARED_ROWS : ROWS;
-    if (shared && most > ROWS / a.chunks) most = ROWS / a.chunks;
+    const int64_t most = shared ? shared_rows(a.M) : ROWS;
     for (a.row0 = 0; a.row0 < a.B; a.row0 = a.row1) {
         a.row1 = a.row0 + most < a.B ? a.row0 + most : a.B;
         launch_rows<T>(a, s);
@@ -1814,7 +1816,7 @@ template <typename T> hipError_t launch_typed(SampleArgs a, void *ws, hipStream_
 
 size_t sample_workspace(int64_t B, int64_t M) {
     if (M + 3 <= CHUNK) return 0;
-    return (size_t)(B < SHARED_ROWS ? B : SHARED_ROWS) * row_bytes(chunks_of(M));
+    return (size_t)std::min(B, shared_rows(M)) * row_bytes(chunks_of(M));
 }
 
 hipError_t launch_sample(gs_dtype st, SampleArgs a, void *ws, hipStream_t s) {
