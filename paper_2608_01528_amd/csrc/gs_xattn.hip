@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(64 * NW * GR, (min_waves<T, DC, NW>())) xattn_
     int j0 = 0, kend = kl;
     if (a.splits > 1) {
         j0 = sp * a.split_keys;
-        kend = j0 + a.split_keys < kl ? j0 + a.split_keys : kl;
+        if (kl - j0 > a.split_keys) kend = j0 + a.split_keys;       // (the last part's end may lie beyond 2^31)
     }
     if ((rt * 32 * NW) / a.G >= ql) kend = 0;           // no row of the tile is there
 

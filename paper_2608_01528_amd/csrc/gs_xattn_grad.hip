@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(256 * GR, (sizeof(T) == 4 && DC > 64 ? 1 : 2))
     const bool in = m < a.rows;
     const RowOf row(in ? m : 0, hk, a.G);
     const bool on = in && row.i < ql;
-    int j0 = sp * a.q_step, kend = j0 + a.q_step < kl ? j0 + a.q_step : kl;
+    int j0 = sp * a.q_step, kend = kl - j0 > a.q_step ? j0 + a.q_step : kl;      // (the last part's end may lie beyond 2^31)
     if (rt * 128 / a.G >= ql) kend = 0;
 
     typename Op<T>::V q[NS], d[NS];
