@@ -535,6 +535,10 @@ gs_status gs_soft_select(const gs_soft_group *groups, int ngroups, gs_dtype pt, 
  * and V, given that call's O and lse:
  *   P = exp(S - lse)     dS = P (dO V^T - rowsum(dO .* O))
  *   dV = P^T dO     dQ = scale dS K     dK = scale dS^T Q
+ * The row sum takes O as it is given, so dS holds up to half a step of t of
+ * rowsum(|dO .* O|), which shows where one of many live states has nearly all the
+ * weight; sequences with at most 64 live states (fp32: 32), by length or by mask,
+ * take the sum of P .* (dO V^T) in fp32 instead.  Gradients are
  * summed in fp32, in a fixed order, over the heads that share K and V.  Rows of
  * positions i >= qlen[b] and of states that are not live are written as zeros.
  * Where K or V stand for several sequences (sb = 0) dK and dV are still those

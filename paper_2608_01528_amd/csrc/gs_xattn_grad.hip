@@ -78,6 +78,17 @@ __global__ void __launch_bounds__(256 * GR, (sizeof(T) == 4 && DC > 64 ? 1 : 2))
     // and rows without a live key), and D.
     const int64_t at_row = ((int64_t)b * a.Hq + row.h) * a.Lq + row.i;
     f2v st = {-INFINITY, 0.f};
+    // States that the sequence has, as far as `few` asks.
+    const uint8_t *const mask = a.mask ? a.mask + b * a.mask_ld : nullptr;
+    int states = kl;
+    if (mask && kl > BN) {
+        states = 0;
+        for (int j = 0; j < kl && states <= BN; j += 128) {
+            const bool x = j + l < kl && mask[j + l], y = kl - j > 64 + l && mask[j + 64 + l];
+            states += __popcll(__ballot(x)) + __popcll(__ballot(y));
+        }
+    }
+    const bool few = states <= BN && j0 < kend;
     {
         typename Op<T>::V y[NS];
         load_frags<T, DC>(y, on ? static_cast<const T *>(a.O) + b * a.o.b + row.i * a.o.l + row.h * a.o.h : nullptr, a.Dh, VEC, l);
@@ -88,12 +99,11 @@ __global__ void __launch_bounds__(256 * GR, (sizeof(T) == 4 && DC > 64 ? 1 : 2))
         st[1] += other_half(st[1]);
         if (on) st[0] = -LOG2E * a.lse[at_row];
         if (st[0] == INFINITY) st[0] = -INFINITY;
-        if (on && l < 32 && !group && sp == 0) a.stat[at_row] = st;
     }
     const float c = a.scale * LOG2E;
     const T *const K = static_cast<const T *>(a.K) + b * a.k.b + hk * a.k.h;
     const T *const V = static_cast<const T *>(a.V) + b * a.v.b + hk * a.v.h;
-    LiveKeys<BN> keys{a.mask ? a.mask + b * a.mask_ld : nullptr, kend, l, 0};
+    LiveKeys<BN> keys{mask, kend, l, 0};
 
     f16v o[NJ];
 #pragma unroll
@@ -106,6 +116,43 @@ __global__ void __launch_bounds__(256 * GR, (sizeof(T) == 4 && DC > 64 ? 1 : 2))
     };
     char *kt = lds + group * 4 * TILE, *vt = kt + TILE;
     int other = 2 * TILE;
+    if (few) {
+        // A tile's worth of states at most: D as the sum of P dP over them, in
+        // fp32.  sum_d dO O has the rounding of O in it (half a step of T, 2^-8 in
+        // bf16, of sum_d |dO O| at most), which dP - D keeps, and which is small
+        // beside dP only where O is an average over many rows of V.  Every
+        // work-group of the row and each of its groups goes over all of them.
+        float D = 0.f;
+        LiveKeys<BN> all{mask, kl, l, 0};
+#pragma unroll 1
+        for (int j = 0; j < kl; j += BN) {
+            all.ahead(j);
+            live = all.take(j);
+            if (!live) continue;
+            lds_barrier();
+            fetch(j, live);
+            kr.stash(kt, t);
+            vr.stash(vt, t);
+            lds_barrier();
+#pragma unroll 1
+            for (int n = 0; n < BN / 32; ++n) {
+                f16v p = {0}, g = {0};
+#pragma unroll
+                for (int s = 0; s < NS; ++s) p = Op<T>::mma(row_frag<T, DP>(kt, 32 * n, s, l), q[s], p);
+#pragma unroll
+                for (int s = 0; s < NS; ++s) g = Op<T>::mma(row_frag<T, DP>(vt, 32 * n, s, l), d[s], g);
+                // (a dead key's score is 0 here, which a row of very negative scores
+                // makes an infinite probability)
+                const uint32_t bits = (uint32_t)(live >> (32 * n)) >> (4 * (l >> 5));
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    D += (bits >> (8 * (r / 4) + r % 4)) & 1 ? __builtin_amdgcn_exp2f(fmaf(p[r], c, st[0])) * g[r] : 0.f;
+            }
+        }
+        st[1] = D + other_half(D);
+        lds_barrier();
+    }
+    if (on && l < 32 && !group && sp == 0) a.stat[at_row] = st;
     if (j0 < kend) {
         keys.ahead(j0 + mine);
         live = keys.take(j0 + mine);
@@ -118,29 +165,6 @@ __global__ void __launch_bounds__(256 * GR, (sizeof(T) == 4 && DC > 64 ? 1 : 2))
             keys.ahead(j0 + 2 * STEP + mine);
             fetch(j0 + STEP + mine, next_live);
         }
-    }
-    if (kl <= BN && j0 < kend) {
-        // Few keys: D as the sum of P dP over the tile, in fp32.  sum_d dO O has
-        // the rounding of O in it, which is small beside dP only where O is an
-        // average over many rows of V.
-        float D = 0.f;
-        lds_barrier();
-#pragma unroll 1
-        for (int n = 0; n < BN / 32; ++n) {
-            f16v p = {0}, g = {0};
-#pragma unroll
-            for (int s = 0; s < NS; ++s) p = Op<T>::mma(row_frag<T, DP>(kt, 32 * n, s, l), q[s], p);
-#pragma unroll
-            for (int s = 0; s < NS; ++s) g = Op<T>::mma(row_frag<T, DP>(vt, 32 * n, s, l), d[s], g);
-            // (a dead key's score is 0 here, which a row of very negative scores
-            // makes an infinite probability)
-            const uint32_t bits = (uint32_t)(live >> (32 * n)) >> (4 * (l >> 5));
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                D += (bits >> (8 * (r / 4) + r % 4)) & 1 ? __builtin_amdgcn_exp2f(fmaf(p[r], c, st[0])) * g[r] : 0.f;
-        }
-        st[1] = D + other_half(D);
-        if (on && l < 32 && !group) a.stat[at_row] = st;
     }
     for (; j0 < kend; j0 += STEP) {
         lds_barrier();
