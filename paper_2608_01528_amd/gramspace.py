@@ -713,7 +713,7 @@ def gs_sample(S: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=
     each one number for all rows or a tensor of B (fp32; top_k int32).
     Returns idx (int32, B; -1 for a row of -inf), or a tuple with prob (fp32,
     the entry's share of the kept weight) and kept (int32, entries kept) where
-    asked for."""
+    asked for; outputs that are given are written in any case."""
     st, lds = _mat(S, "S")
     _here(S, "S")
     B, M = S.shape
@@ -729,8 +729,8 @@ def gs_sample(S: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=
             one[i] = v
     one[1] = min(max(int(one[1]), 0), 0x7fffffff)
     idx = idx_out if idx_out is not None else torch.empty(B, dtype=i32, device=dev)
-    pr = (prob_out if prob_out is not None else torch.empty(B, dtype=f32, device=dev)) if prob else None
-    kp = (kept_out if kept_out is not None else torch.empty(B, dtype=i32, device=dev)) if kept else None
+    pr = torch.empty(B, dtype=f32, device=dev) if prob and prob_out is None else prob_out
+    kp = torch.empty(B, dtype=i32, device=dev) if kept and kept_out is None else kept_out
     if u is None:
         raise ValueError("u must be a tensor of random numbers")
     L = lib()

@@ -1,0 +1,26 @@
+"""Arguments of the sequence operators' binding: outputs that are given are
+written."""
+import pytest
+import torch
+
+from paper_2608_01528_amd import gramspace as gs
+
+pytestmark = pytest.mark.gpu
+
+
+def test_outputs_that_are_given_are_written():
+    S, u = torch.randn(9, 70, device="cuda"), torch.rand(9, device="cuda")
+    idx, prob, kept = gs.gs_sample(S, u, top_k=5, prob=True, kept=True)
+    p, k = torch.full((9,), 7.0, device="cuda"), torch.full((9,), 7, dtype=torch.int32, device="cuda")
+    got = gs.gs_sample(S, u, top_k=5, prob_out=p, kept_out=k)
+    assert isinstance(got, torch.Tensor) and torch.equal(got, idx)
+    assert torch.equal(p, prob) and torch.equal(k, kept)
+    p.fill_(7.0)
+    got = gs.gs_sample(S, u, top_k=5, kept=True, prob_out=p)
+    assert len(got) == 2 and torch.equal(got[1], kept) and torch.equal(p, prob)
+    with pytest.raises(ValueError, match="prob_out"):
+        gs.gs_sample(S, u, prob_out=p[:5])
+    Q, K = torch.randn(2, 3, 2, 64, device="cuda"), torch.randn(2, 5, 1, 64, device="cuda")
+    O, lse = gs.gs_cross_attention(Q, K, K, lse=True)
+    stats = torch.zeros_like(lse)
+    assert torch.equal(gs.gs_cross_attention(Q, K, K, lse_out=stats), O) and torch.equal(stats, lse)
