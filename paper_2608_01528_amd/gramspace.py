@@ -733,9 +733,13 @@ def gs_sample(S: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=
     kp = torch.empty(B, dtype=i32, device=dev) if kept and kept_out is None else kept_out
     if u is None:
         raise ValueError("u must be a tensor of random numbers")
+    try:
+        given = _SAMPLING.pack(*at, *one)
+    except OverflowError:       # a number beyond fp32 is infinite
+        given = _SAMPLING.pack(*at, *(v if i == 1 else ctypes.c_float(v).value for i, v in enumerate(one)))
     L = lib()
     ws, n, _keep = _workspace(L.gs_sample_workspace(st, B, M), workspace, dev)
-    _check(L.gs_sample(S.data_ptr(), st, B, M, lds, _per_row(u, "u", B, f32), _SAMPLING.pack(*at, *one),
+    _check(L.gs_sample(S.data_ptr(), st, B, M, lds, _per_row(u, "u", B, f32), given,
                        _per_row(idx, "idx_out", B, i32), _per_row(pr, "prob_out", B, f32) or None,
                        _per_row(kp, "kept_out", B, i32) or None, ws, n, _stream()))
     if not (prob or kept):

@@ -1,5 +1,5 @@
 """Arguments of the sequence operators' binding: outputs that are given are
-written."""
+written, numbers beyond fp32 are taken as infinite."""
 import pytest
 import torch
 
@@ -24,3 +24,12 @@ def test_outputs_that_are_given_are_written():
     O, lse = gs.gs_cross_attention(Q, K, K, lse=True)
     stats = torch.zeros_like(lse)
     assert torch.equal(gs.gs_cross_attention(Q, K, K, lse_out=stats), O) and torch.equal(stats, lse)
+
+
+def test_numbers_beyond_fp32():
+    S, u = torch.randn(6, 40, device="cuda"), torch.rand(6, device="cuda")
+    inf = float("inf")
+    for far, near in (({"temperature": 1e300}, {"temperature": inf}), ({"temperature": -1e300}, {"temperature": 0.0}),
+                      ({"top_p": 1e200}, {}), ({"min_p": 1e39}, {"min_p": 1.0}), ({"top_k": 1 << 40}, {}), ({"temperature": 2}, {"temperature": 2.0})):
+        for a, b in zip(gs.gs_sample(S, u, prob=True, kept=True, **far), gs.gs_sample(S, u, prob=True, kept=True, **near)):
+            assert torch.equal(a, b), far
