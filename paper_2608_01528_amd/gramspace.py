@@ -663,7 +663,7 @@ def _attn_problem(Q, K, V, O, lse, qlen, klen, mask, scale, grads=None):
         dO, dQ, dK, dV = grads
         rest = _seq(dO, "dO", q, dtype) + _seq(dQ, "dQ", q, dtype) + _seq(dK, "dK", k, dtype) + _seq(dV, "dV", k, dtype)
     return _ATTN.pack(B, Lq, Lk, Hq, Hkv, Dh, _per_row(qlen, "qlen", B, torch.int32),
-                      _per_row(klen, "klen", B, torch.int32), mp, ldm, float(Dh ** -0.5 if scale is None else scale),
+                      _per_row(klen, "klen", B, torch.int32), mp, ldm, float(max(Dh, 1) ** -0.5 if scale is None else scale),
                       *_seq(Q, "Q", q, dtype), *_seq(K, "K", k, dtype), *_seq(V, "V", k, dtype),
                       *_seq(O, "O", q, dtype), lp, *rest), t
 

@@ -1,5 +1,6 @@
 """Arguments of the sequence operators' binding: outputs that are given are
-written, numbers beyond fp32 are taken as infinite."""
+written, numbers beyond fp32 are taken as infinite, heads of no values are
+refused by the library."""
 import pytest
 import torch
 
@@ -33,3 +34,11 @@ def test_numbers_beyond_fp32():
                       ({"top_p": 1e200}, {}), ({"min_p": 1e39}, {"min_p": 1.0}), ({"top_k": 1 << 40}, {}), ({"temperature": 2}, {"temperature": 2.0})):
         for a, b in zip(gs.gs_sample(S, u, prob=True, kept=True, **far), gs.gs_sample(S, u, prob=True, kept=True, **near)):
             assert torch.equal(a, b), far
+
+
+def test_heads_of_no_values_are_refused():
+    Q, K = torch.empty(2, 3, 2, 0, device="cuda"), torch.empty(2, 5, 1, 0, device="cuda")
+    with pytest.raises(gs.GramSpaceError, match="Dh"):
+        gs.gs_cross_attention(Q, K, K)
+    with pytest.raises(gs.GramSpaceError, match="Dh"):
+        gs.gs_cross_attention_grad(Q, Q, K, K, Q, torch.empty(2, 2, 3, device="cuda"))
