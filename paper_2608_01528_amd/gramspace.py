@@ -675,7 +675,9 @@ def gs_cross_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, qlen=N
     states: Q (B, Lq, Hq, Dh), K and V (B, Lk, Hkv, Dh) with Hkv dividing Hq;
     qlen, klen (int32, B) lengths; mask (B, Lk) bool, False for states left
     out; scale 1 / sqrt(Dh) by default.  Any strides but the last dimension's.
-    Returns O, or (O, lse) with lse (B, Hq, Lq) fp32."""
+    Returns O, or (O, lse) with lse (B, Hq, Lq) fp32; lse_out is written in any
+    case.  As with all calls here the results are no part of torch's graph: the
+    gradients are gs_cross_attention_grad's."""
     if out is None:
         out = Q.new_empty(Q.shape)
     if lse_out is None and lse:
