@@ -9,7 +9,8 @@
 // than M 2^-shift <= 2^-26 of the largest weight.  For longer rows that grows as
 // M^2 (a tail of no weight would come to a quarter of the largest entry at 2^30),
 // and the shift is taken from the row's total, which two more launches find: a
-// sum is off by less than M 2^-60 of the total.
+// sum is off by less than M 2^-60 of the total (8 rows of 262145: 42 us, 30 with
+// the shift by length; with top_p 313 and 295).
 //
 // What is kept is a run of the entries in rank order (falling scores, equal
 // ones by index), thinned by min_p from its end: top_k and top_p each end it

@@ -14,9 +14,9 @@
 // two tiles side by side in one wave needed registers that cost more, 1.34 ms).
 // One position: bound by HBM (64 sequences of up to 4000 states, 32 heads over
 // 8 of 128 values: 601 MB in 135 us, 4.45 TB/s, where a large copy reaches
-// 4.77).  fp32 products take eight times as long as bf16 ones: 61 % of the
-// library's rate at 1024 x 1024 of 64 values (the matrix cores are busy 67 % of
-// the cycles), 59 % of 128.
+// 4.77).  fp32 products take eight times as long as bf16 ones: 62 % of the
+// library's rate at 1024 x 1024 of 64 values (the matrix cores are busy 69 % of
+// the cycles) and of 128 (67 %).
 #include "gs_attn.h"
 
 namespace gs {

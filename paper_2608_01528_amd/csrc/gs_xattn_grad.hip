@@ -14,8 +14,8 @@
 // Bound by the matrix cores, the exponentials and the LDS reads between their
 // products: 4 x 16 heads of 2048 x 2048, 128 values, bf16: dQ 225 us (three
 // products, 920 TF/s), dK and dV 340 (four, 810 TF/s); fp32, 8 x 4 heads of
-// 1024 x 1024, 64 values: dQ 126 us (102 TF/s of 152; the matrix cores are busy
-// 75 % of its cycles), dK and dV 163 (105; 80 %).
+// 1024 x 1024, 64 values: dQ 125 us (103 TF/s of 152; the matrix cores are busy
+// 75 % of its cycles), dK and dV 160 (107; 79 %).
 #include "gs_attn.h"
 
 namespace gs {
@@ -78,7 +78,8 @@ __global__ void __launch_bounds__(256 * GR, (sizeof(T) == 4 && DC > 64 ? 1 : 2))
     // and rows without a live key), and D.
     const int64_t at_row = ((int64_t)b * a.Hq + row.h) * a.Lq + row.i;
     f2v st = {-INFINITY, 0.f};
-    // States that the sequence has, as far as `few` asks.
+    // Live states of the sequence, as far as `few` asks (the first 128 mask bytes
+    // come with the rows above them: no time that shows).
     const uint8_t *const mask = a.mask ? a.mask + b * a.mask_ld : nullptr;
     int states = kl;
     if (mask && kl > BN) {
