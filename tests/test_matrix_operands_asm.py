@@ -71,16 +71,27 @@ def test_the_check_sees_an_early_operand():
     assert early_products(first + chain + apart + end) == (3, [])
 
 
-@pytest.mark.parametrize("source", ["gs_xattn.hip", "gs_xattn_grad.hip"])
-def test_operands_wait_for_the_products(source, tmp_path):
+SOURCES = ["gs_xattn.hip", "gs_xattn_grad.hip"]
+
+
+@pytest.fixture(scope="module")
+def assembly(tmp_path_factory):
+    """The sources' gfx950 assembly, compiled side by side."""
     if not (os.path.exists(B.HIPCC) or shutil.which(B.HIPCC)):
         pytest.skip("hipcc not available")
-    out = str(tmp_path / "code.s")
-    r = subprocess.run([B.HIPCC] + B.FLAGS + ["--cuda-device-only", "-S", "-o", out, os.path.join(B.CSRC, source)],
-                       capture_output=True, text=True)
-    assert r.returncode == 0, r.stderr[-2000:]
+    room = tmp_path_factory.mktemp("asm")
+    runs = [subprocess.Popen([B.HIPCC] + B.FLAGS + ["--cuda-device-only", "-S", "-o", str(room / s), os.path.join(B.CSRC, s)],
+                             stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True) for s in SOURCES]
+    for r in runs:
+        _, err = r.communicate()
+        assert r.returncode == 0, err[-2000:]
+    return {s: (room / s).read_text() for s in SOURCES}
+
+
+@pytest.mark.parametrize("source", SOURCES)
+def test_operands_wait_for_the_products(source, assembly):
     total = 0
-    for name, body in re.findall(r"^(_Z\S*kernel\S*):[^\n]*\n(.*?)^\s*\.section", open(out).read(), re.S | re.M):
+    for name, body in re.findall(r"^(_Z\S*kernel\S*):[^\n]*\n(.*?)^\s*\.section", assembly[source], re.S | re.M):
         products, found = early_products(body)
         assert not found, (name, found[0])
         total += products
