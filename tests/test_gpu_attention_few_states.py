@@ -92,3 +92,26 @@ def test_on_either_side_of_few(dtype):
         again = whole(Q, K, V, dO, mask=mask, **kw)
         for n in first:
             assert torch.equal(first[n], again[n]), n
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_captured_with_masks_that_change(dtype):
+    """A captured step replayed with few live states, none, and many."""
+    B, Lq, Lk = 2, 40, 400
+    Q, K, V, dO = problem(B, Lq, Lk, 4, 2, 64, dtype)
+    mask = torch.ones(B, Lk, dtype=torch.bool, device="cuda")
+    whole(Q, K, V, dO, mask=mask)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = whole(Q, K, V, dO, mask=mask)
+    for every in (200, 1, 13, 1000, 7, 3):
+        mask.copy_((torch.arange(Lk, device="cuda")[None] % every == 2 % every).repeat(B, 1))
+        if every == 1000:
+            mask[1] = False
+        g.replay()
+        torch.cuda.synchronize()
+        eager = agree(Q, K, V, dO, mask=mask)
+        torch.cuda.synchronize()
+        for n in eager:
+            assert torch.equal(got[n], eager[n]), (every, n)

@@ -165,3 +165,34 @@ def test_captured_long_rows():
         torch.cuda.synchronize()
         for a, b in zip(got, want):
             assert torch.equal(a, b), seed
+
+
+def test_more_long_rows_than_a_launch_takes():
+    """Rows beyond the 2048 that share a workspace, each with a total of its own."""
+    B, M = 2051, (1 << 18) + 1
+    g = torch.Generator(device="cuda").manual_seed(1)
+    S = torch.randn(B, M, generator=g, device="cuda", dtype=torch.bfloat16)
+    S *= torch.linspace(0.1, 6.0, B, device="cuda")[:, None]
+    u = torch.rand(B, generator=g, device="cuda")
+    for p in ({}, {"top_k": 7, "top_p": 0.9}):
+        got = gs.gs_sample(S, u, prob=True, kept=True, **p)
+        pick = torch.tensor([0, 1, 2047, 2048, 2050], device="cuda")
+        for a, b in zip(got, gs.gs_sample(S[pick].contiguous(), u[pick].contiguous(), prob=True, kept=True, **p)):
+            assert torch.equal(a[pick], b)
+
+
+def test_two_calls_at_once():
+    S, u = scores(3, 300001, seed=2)
+    X, v = scores(2, 700003, seed=3, dtype=torch.bfloat16)
+    p, q = {"top_p": 0.9, "min_p": 0.001}, {"temperature": 3.0}
+    want, other = gs.gs_sample(S, u, prob=True, kept=True, **p), gs.gs_sample(X, v, prob=True, kept=True, **q)
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(s1):
+            a = gs.gs_sample(S, u, prob=True, kept=True, **p)
+        with torch.cuda.stream(s2):
+            b = gs.gs_sample(X, v, prob=True, kept=True, **q)
+        torch.cuda.synchronize()
+        for x, y in zip(a + b, want + other):
+            assert torch.equal(x, y)
