@@ -269,7 +269,7 @@ def _run_own(s):
         return {"Kc": s["Kc"], "Vc": s["Vc"]}
     if c["kind"] == "verify":
         accepted, entry, entries = gs.gs_verify(s["P"], s["drafted"], s["u"], s["v"], s["qoff"], Q=s["Q"],
-                                                max_new=s["max_new"], entries=True)
+                                                entries=True)
         return {"accepted": accepted, "entry": entry, "entries": entries}
     O, lse = gs.gs_paged_attention(s["Q"], s["Kc"], s["Vc"], s["table"], s["klen"], qoff=s["qoff"],
                                    max_new=s["max_new"], max_len=s["max_len"], window=c["window"], sinks=c["sinks"],
