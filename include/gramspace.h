@@ -629,6 +629,192 @@ gs_status gs_sample(const void *S, gs_dtype st, int64_t B, int64_t M, int64_t ld
                     const gs_sampling *p, int32_t *idx, float *prob, int32_t *kept,
                     void *ws, size_t ws_bytes, void *stream);
 
+/*
+ * Serving out of a paged cache.  The states (keys and values) of many requests
+ * lie in one cache of `pages` pages of `page` positions, in pages from anywhere.
+ * Row b of a table (int32, B x width) names the pages of request b in order, so
+ * that its state j lies in page table[b, j / page] at place j % page, and in slot
+ * table[b, j / page] page + j % page of the cache.  A step adds new positions to
+ * requests: rows qoff[b] .. qoff[b + 1] - 1 of its tensors (qoff int32[B + 1],
+ * nondecreasing) belong to request b.  One step is gs_paged_plan, gs_paged_store
+ * of the new keys and values, gs_paged_attention, and, where entries were
+ * drafted, gs_verify.  All lengths, tables and offsets stay in device memory, so
+ * a captured step can be replayed.
+ *
+ * gs_paged_plan -- pages and slots of a step.  With len = length[b] and
+ * up(x) = ceil(x / page):
+ *   1. add[b] < 0 takes positions back (drafts refused, a request that ended:
+ *      any number from its length on): length_out = max(len + add, 0), and the
+ *      pages table[b, up(length_out) .. up(len) - 1] go to the end of the free
+ *      list, requests in order.
+ *   2. add[b] > 0 asks for positions: up(len + add) - up(len) pages, taken from
+ *      the end of the free list, one after the other, requests in order, into
+ *      table[b, up(len) ..].  A request is served if its table has room
+ *      (up(len + add) <= width; len + add below 2^31), its rows end within `rows`,
+ *      and it needs no page or no more are wanted up to and with it, by all that
+ *      pass the first two conditions, than are free.  Others get nothing: length_out = len, added 0,
+ *      slots -1.
+ *   qoff[0] = 0, qoff[b + 1] = qoff[b] + max(add[b], 0), served or not (2^31 - 1
+ *   where it would pass that)
+ *   slots[qoff[b] + i] = slot of position len + i of a served request; -1 in the
+ *   rows of other ones and behind the last request's.  (-1 too where the table
+ *   holds a negative page.)
+ *
+ *   B, page    requests >= 0, positions a page >= 1
+ *   rows       rows that the step has room for, >= 0 (all sizes below 2^31 - 256)
+ *   length,add int32[B] device, in; lengths below 0 count as 0, above width page
+ *              as width page
+ *   length_out int32[B], out; may be `length`
+ *   table      int32 B x width, ldt >= width >= 0, in and out: only entries of
+ *              pages taken are written
+ *   free_pages int32[capacity], in and out: *nfree page numbers (device, clamped
+ *              to 0 .. capacity); what would be put behind `capacity` is dropped
+ *   nfree_out  int32[1] out; may be nfree
+ *   qoff       int32[B + 1] out     slots int64[rows] out
+ *   added      int32[B] out: positions added
+ *   ws         device workspace of gs_paged_plan_workspace(B) bytes, 16-byte
+ *              aligned; calls that may run at the same time need one each
+ * All integer arithmetic: results do not depend on the schedule.
+ */
+typedef struct {
+    int64_t B, page, rows;
+    const int32_t *length, *add;
+    int32_t *length_out;
+    int32_t *table; int64_t width, ldt;
+    int32_t *free_pages; int64_t capacity;
+    const int32_t *nfree;
+    int32_t *nfree_out;
+    int32_t *qoff;
+    int64_t *slots;
+    int32_t *added;
+} gs_paged_step;
+
+size_t gs_paged_plan_workspace(int64_t B);
+
+gs_status gs_paged_plan(const gs_paged_step *p, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * gs_paged_store -- keys and values of a step's rows into their slots of the
+ * cache: Kc[slots[n] / page, slots[n] % page, h, d] = K[n, h, d], and V alike,
+ * rounded to the cache's type (nearest even).  Rows whose slot lies outside
+ * [0, pages page) are left out.  Slots of different rows are different; where two
+ * rows name the same slot, which of their values it holds is not defined, element
+ * by element.
+ *
+ *   N, Hkv, Dh   rows >= 0, heads and values a head >= 1, N Hkv ceil(Dh / 8) below
+ *                2^32 - 2048
+ *   pages, page  of the cache, >= 0 and >= 1
+ *   slots        int64[N] device
+ *   K, V    in   element (n, h, d) at p[n sl + h sh + d], type t in {F32, BF16}
+ *                (sb is not used)
+ *   Kc, Vc  out  element (page g, place i, h, d) at p[g sb + i sl + h sh + d],
+ *                type ct in {F32, BF16}; elements at places of their own
+ * Strides as for gs_cross_attention.  Nothing but the named slots is written.
+ */
+typedef struct {
+    int64_t N, Hkv, Dh, pages, page;
+    const int64_t *slots;
+    gs_seq K, V, Kc, Vc;
+} gs_paged_rows;
+
+gs_status gs_paged_store(const gs_paged_rows *p, gs_dtype t, gs_dtype ct, void *stream);
+
+/*
+ * gs_paged_attention -- attention of a step's new positions to all that their
+ * requests have in the cache, the new ones' own states among it (store them
+ * first).  Request b with klen[b] states and n = qoff[b + 1] - qoff[b] rows: row
+ * qoff[b] + i stands at position p = klen[b] - n + i and sees the states j <= p
+ * with, if window > 0, j > p - window or j < sinks.  For head h, G = Hq / Hkv:
+ *   S[j] = scale <Q[row, h], K[j, h / G]>
+ *   O[row, h] = sum_j softmax_j(S)[j] V[j, h / G]
+ *   lse[row, h] = log sum_j exp S[j]
+ * A row that sees no state gives O = 0 and lse = -inf.  States that a row does
+ * not see contribute nothing to it whatever they hold, NaN and infinities
+ * included; neither do states whose page number lies outside [0, pages) (they
+ * count as not there).  Pages of which no row sees a state are not read, and may
+ * have been given to others.  Rows of no request, and rows of a request behind
+ * its first Lq, are left as they are.
+ *
+ *   B, N       requests and rows >= 0       Lq   most rows of a request, >= 0
+ *   Lk         most states of a request, 0 <= Lk <= width page: klen counts as 0
+ *              below 0 and as Lk above
+ *   Hq, Hkv    heads; Hkv divides Hq        Dh   values a head, 1 <= Dh <= 128
+ *   N Hq below 2^30, B Hkv below 2^22, Hq below 2^16, B Hq Lq below 2^24 - 8 where
+ *   Lq G <= 32; Lq, Lk, pages, page, width below 2^31 - 256
+ *   table      int32 B x width device, ldt >= width       klen int32[B] device
+ *   qoff       int32[B + 1] device, clamped to 0 .. N; null: N = B, a row each
+ *   window     0: all states; sinks >= 0 (no effect without a window)
+ *   scale      finite, not zero (1e-30 <= |scale| <= 1e30)
+ *   Q, O       N x Hq x Dh at p[n sl + h sh + d] (sb is not used); K, V the cache,
+ *              pages x page x Hkv x Dh at p[g sb + i sl + h sh + d]; all of type t
+ *              in {F32, BF16}, strides as for gs_cross_attention.  Rows that start
+ *              on 16-byte boundaries with Dh a multiple of 16 bytes are the fast case
+ *   lse        float N x Hq out, nullable
+ *   ws         device workspace of gs_paged_attention_workspace(p, t) bytes,
+ *              16-byte aligned; calls that may run at the same time need one each
+ * fp32 accumulation; probabilities enter the second product in type t.  Work is
+ * shared out by the lengths that the device holds, in parts whose results are
+ * added in a fixed order: the same call gives the same bits.
+ */
+typedef struct {
+    int64_t B, N, Lq, Lk, Hq, Hkv, Dh;
+    int64_t pages, page, width, ldt;
+    const int32_t *table, *klen, *qoff;
+    int64_t window, sinks;
+    double scale;
+    gs_seq Q, K, V, O;
+    float *lse;
+} gs_paged_attn;
+
+size_t gs_paged_attention_workspace(const gs_paged_attn *p, gs_dtype t);
+
+gs_status gs_paged_attention(const gs_paged_attn *p, gs_dtype t, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * gs_verify -- drafted entries taken or refused by the probabilities p that the
+ * model gives at their places (speculative sampling: what is left has the
+ * model's own distribution).  Request b has the rows qoff[b] .. qoff[b + 1] - 1:
+ * row i's entry drafted[row] is the one drafted to follow it, the last row has
+ * none.  With x = drafted[row], and q the drafting model's probabilities:
+ *   1. a row's draft is taken if u[row] q(x) < p(x) and all before it were
+ *   2. accepted[b]: drafts taken
+ *   3. entry[b]: drawn at the first row whose draft was not taken, from the
+ *      weights max(p - q, 0), or, where these are all 0, from p; drawn from p at
+ *      the last row if all were taken.  It is the first entry, by index, at which
+ *      the sum of the weights exceeds v[b] times their total (from v = 1 on the
+ *      last one of any weight); -1 where p has no weight
+ *   4. entries[row]: the drafts taken, then entry[b], then -1
+ * Values of P and Q that are negative, infinite or NaN count as 0, and so do u and
+ * v below 0 or NaN.  A draft outside [0, M) has p = q = 0.  Rows of P and Q are
+ * taken as they are (their sums need not be 1).  A request without rows gives
+ * accepted 0 and entry -1.
+ *
+ *   P      in   N x M, pt in {F32, BF16}, ldp >= M, 1 <= M < 2^31 - 256, B and
+ *               B ceil(M / 4096) below 2^24 - 8
+ *   Q      in   N x M, type pt, ldq >= M (last rows of requests are not read);
+ *               null: drafts were certain, q = 1 at the draft
+ *   drafted     int32[N], u float[N], v float[B], qoff int32[B + 1] device (clamped
+ *               to 0 .. N)
+ *   accepted, entry   int32[B] out;  entries int32[N] out, nullable (rows of no
+ *               request are left as they are)
+ *   ws          device workspace of gs_verify_workspace(B, M) bytes (0: none),
+ *               16-byte aligned; calls that may run at the same time need one each
+ * Comparisons, weights and sums are fp64, summed in a fixed order.
+ */
+typedef struct {
+    int64_t B, N, M;
+    const void *P; int64_t ldp;
+    const void *Q; int64_t ldq;
+    const int32_t *drafted;
+    const float *u, *v;
+    const int32_t *qoff;
+    int32_t *accepted, *entry, *entries;
+} gs_drafts;
+
+size_t gs_verify_workspace(int64_t B, int64_t M);
+
+gs_status gs_verify(const gs_drafts *p, gs_dtype pt, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -391,6 +391,37 @@ bool vec_rows(const gs_seq &q, const SeqShape &z, gs_dtype t) {
 
 SeqStrides strides(const gs_seq &q) { return SeqStrides{q.sb, q.sl, q.sh}; }
 
+// Rows of a step and a paged cache, as tensors of the kind above.
+SeqShape row_shape(int64_t N, int64_t H, int64_t dh) { return SeqShape{{1, N, H}, dh}; }
+gs_seq rows_of(const gs_seq &q) { return gs_seq{q.p, 0, q.sl, q.sh}; }
+bool counts(std::initializer_list<int64_t> v) {
+    for (int64_t x : v)
+        if (x < 0 || x >= SEQ_MAX - 256) return false;
+    return true;
+}
+
+// Sizes that the kernels of gs_paged_attention count in 32 bits.
+bool paged_sizes(const gs_paged_attn *a) {
+    if (!counts({a->B, a->N, a->Lq, a->Lk, a->pages, a->page, a->width}) || a->page < 1) return false;
+    if (a->Hq < 1 || a->Hq >= (1 << 16) || a->Hkv < 1 || a->Hq % a->Hkv || a->Dh < 1 || a->Dh > CROSS_ATTN_MAX_DH) return false;
+    if (a->N * a->Hq >= ((int64_t)1 << 30) || a->B * a->Hkv >= ((int64_t)1 << 22)) return false;
+    const int64_t rows = a->Lq * (a->Hq / a->Hkv);
+    if (rows <= 32 && a->B * a->Hkv * rows >= ATTN_MAX_BLOCKS) return false;
+    return a->Lk <= (__int128)a->width * a->page && a->window >= 0 && a->sinks >= 0;
+}
+
+PagedAttnArgs paged_args(const gs_paged_attn *p) {
+    PagedAttnArgs a{};
+    a.B = (int)p->B; a.N = (int)p->N; a.Lq = (int)std::min(p->Lq, p->N); a.Lk = (int)p->Lk;
+    a.Hq = (int)p->Hq; a.Hkv = (int)p->Hkv; a.Dh = (int)p->Dh; a.G = a.Hq / a.Hkv;
+    a.pages = (int)p->pages; a.page = (int)p->page;
+    // a window that leaves nothing out is none
+    a.window = p->window < p->Lk ? (int)p->window : 0;
+    a.sinks = (int)std::min(p->sinks, p->Lk);
+    a.ldt = p->ldt;
+    return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -986,6 +1017,161 @@ gs_status gs_sample(const void *S, gs_dtype st, int64_t B, int64_t M, int64_t ld
     const size_t quad = 4 * esize(st);
     a.vec = reinterpret_cast<uintptr_t>(S) % quad == 0 && (B == 1 || lds % 4 == 0);
     return launched(launch_sample(st, a, ws, (hipStream_t)stream), fn);
+}
+
+size_t gs_paged_plan_workspace(int64_t B) { return counts({B}) ? paged_plan_workspace(B) : 0; }
+
+gs_status gs_paged_plan(const gs_paged_step *p, void *ws, size_t ws_bytes, void *stream) {
+    const char *fn = "gs_paged_plan";
+    if (!p) return fail(GS_ERR_ARG, "%s: the step is null", fn);
+    if (!counts({p->B, p->page, p->rows, p->width, p->capacity}) || p->page < 1)
+        return fail(GS_ERR_SHAPE, "%s: need B, rows, width, capacity >= 0 and page >= 1, all below 2^31 - 256", fn);
+    if (p->ldt < p->width || !within_reach(p->B, p->ldt, p->width))
+        return fail(GS_ERR_SHAPE, "%s: leading dimension of the table out of range", fn);
+    const struct { const void *p; size_t es; bool needed; const char *name; } each[] = {
+        {p->length, 4, p->B > 0, "length"}, {p->add, 4, p->B > 0, "add"}, {p->length_out, 4, p->B > 0, "length_out"},
+        {p->table, 4, p->B > 0 && p->width > 0, "table"}, {p->free_pages, 4, p->capacity > 0, "free_pages"},
+        {p->nfree, 4, true, "nfree"}, {p->nfree_out, 4, true, "nfree_out"}, {p->qoff, 4, true, "qoff"},
+        {p->slots, 8, p->rows > 0, "slots"}, {p->added, 4, p->B > 0, "added"}};
+    for (const auto &e : each) {
+        if (!e.p && e.needed) return fail(GS_ERR_ARG, "%s: %s is null", fn, e.name);
+        GS_CHECK(check_aligned(e.p, e.es, e.name));
+    }
+    const size_t need = paged_plan_workspace(p->B);
+    GS_CHECK(check_ws(fn, ws, ws_bytes, need));
+    // length_out and nfree_out may be the inputs themselves
+    const bool same = p->length_out == p->length, same_n = p->nfree_out == p->nfree;
+    GS_CHECK(check_overlaps({same ? Span{} : span(p->length, 1, p->B, p->B, 4, "length"), span(p->add, 1, p->B, p->B, 4, "add"),
+                             same_n ? Span{} : span(p->nfree, 1, 1, 1, 4, "nfree")},
+                            {span(p->length_out, 1, p->B, p->B, 4, "length_out"), span(p->table, p->B, p->width, p->ldt, 4, "table"),
+                             span(p->free_pages, 1, p->capacity, p->capacity, 4, "free_pages"),
+                             span(p->nfree_out, 1, 1, 1, 4, "nfree_out"), span(p->qoff, 1, p->B + 1, p->B + 1, 4, "qoff"),
+                             span(p->slots, 1, p->rows, p->rows, 8, "slots"), span(p->added, 1, p->B, p->B, 4, "added"),
+                             bytes_span(ws, need, "workspace")}));
+    GS_CHECK(check_device());
+    PagedPlanArgs a{};
+    a.B = p->B; a.page = p->page; a.rows = p->rows; a.width = p->width; a.ldt = p->ldt; a.capacity = p->capacity;
+    a.most_length = std::min((int64_t)0x7fffffff, p->width * p->page);
+    a.length = p->length; a.add = p->add; a.length_out = p->length_out; a.table = p->table; a.free_pages = p->free_pages;
+    a.nfree = p->nfree; a.nfree_out = p->nfree_out; a.qoff = p->qoff; a.slots = p->slots; a.added = p->added;
+    return launched(launch_paged_plan(a, ws, (hipStream_t)stream), fn);
+}
+
+gs_status gs_paged_store(const gs_paged_rows *p, gs_dtype t, gs_dtype ct, void *stream) {
+    const char *fn = "gs_paged_store";
+    if (!p) return fail(GS_ERR_ARG, "%s: the rows are null", fn);
+    if (!is_batch_type(t) || !is_batch_type(ct)) return fail(GS_ERR_DTYPE, "%s: rows and cache must be f32 or bf16", fn);
+    if (!counts({p->N, p->Hkv, p->Dh, p->pages, p->page}) || p->Hkv < 1 || p->Dh < 1 || p->page < 1)
+        return fail(GS_ERR_SHAPE, "%s: need N, pages >= 0 and Hkv, Dh, page >= 1, all below 2^31 - 256", fn);
+    if ((__int128)p->N * p->Hkv * ((p->Dh + 7) / 8) >= ((int64_t)1 << 32) - 2048)
+        return fail(GS_ERR_SHAPE, "%s: N Hkv ceil(Dh / 8) must be below 2^32 - 2048", fn);
+    const SeqShape x = row_shape(p->N, p->Hkv, p->Dh), c{{p->pages, p->page, p->Hkv}, p->Dh};
+    const gs_seq K = rows_of(p->K), V = rows_of(p->V);
+    GS_CHECK(check_seq(fn, "K", K, x, t, false));
+    GS_CHECK(check_seq(fn, "V", V, x, t, false));
+    GS_CHECK(check_seq(fn, "Kc", p->Kc, c, ct, true));
+    GS_CHECK(check_seq(fn, "Vc", p->Vc, c, ct, true));
+    if (!p->slots && p->N) return fail(GS_ERR_ARG, "%s: slots is null", fn);
+    GS_CHECK(check_aligned(p->slots, 8, "slots"));
+    GS_CHECK(check_overlaps({seq_span(K, x, esize(t), "K"), seq_span(V, x, esize(t), "V"), span(p->slots, 1, p->N, p->N, 8, "slots")},
+                            {seq_span(p->Kc, c, esize(ct), "Kc"), seq_span(p->Vc, c, esize(ct), "Vc")}));
+    if (p->N == 0 || p->pages == 0) return ok();
+    GS_CHECK(check_device());
+    PagedStoreArgs a{};
+    a.K = K.p; a.V = V.p; a.Kc = p->Kc.p; a.Vc = p->Vc.p; a.slots = p->slots;
+    a.k = strides(K); a.v = strides(V); a.kc = strides(p->Kc); a.vc = strides(p->Vc);
+    a.N = p->N; a.pages = p->pages; a.page = p->page; a.Hkv = (int)p->Hkv; a.Dh = (int)p->Dh;
+    a.vec_in = p->Dh % 8 == 0 && vec_rows(K, x, t) && vec_rows(V, x, t);
+    a.vec_out = p->Dh % 8 == 0 && vec_rows(p->Kc, c, ct) && vec_rows(p->Vc, c, ct);
+    return launched(launch_paged_store(t, ct, a, (hipStream_t)stream), fn);
+}
+
+size_t gs_paged_attention_workspace(const gs_paged_attn *p, gs_dtype t) {
+    if (!p || !is_batch_type(t) || !paged_sizes(p) || !p->B || !p->N || !p->Lq) return 0;
+    return paged_attn_workspace(t, paged_args(p));
+}
+
+gs_status gs_paged_attention(const gs_paged_attn *p, gs_dtype t, void *ws, size_t ws_bytes, void *stream) {
+    const char *fn = "gs_paged_attention";
+    if (!p) return fail(GS_ERR_ARG, "%s: the problem is null", fn);
+    if (!is_batch_type(t)) return fail(GS_ERR_DTYPE, "%s: tensors must be f32 or bf16", fn);
+    if (!paged_sizes(p))
+        return fail(GS_ERR_SHAPE, "%s: need B, N, Lq, window, sinks >= 0, Hkv >= 1 dividing Hq, 1 <= Dh <= %d, page >= 1, 0 <= Lk <= width page, and sizes within the limits",
+                    fn, CROSS_ATTN_MAX_DH);
+    if (!p->qoff && p->N != p->B) return fail(GS_ERR_SHAPE, "%s: without qoff every request has one row (N = B)", fn);
+    if (!(std::fabs(p->scale) >= 1e-30 && std::fabs(p->scale) <= 1e30))
+        return fail(GS_ERR_ARG, "%s: |scale| must be in [1e-30, 1e30]", fn);
+    const SeqShape q = row_shape(p->N, p->Hq, p->Dh), c{{p->pages, p->page, p->Hkv}, p->Dh};
+    const gs_seq Q = rows_of(p->Q), O = rows_of(p->O);
+    GS_CHECK(check_seq(fn, "Q", Q, q, t, false));
+    GS_CHECK(check_seq(fn, "K", p->K, c, t, false));
+    GS_CHECK(check_seq(fn, "V", p->V, c, t, false));
+    GS_CHECK(check_seq(fn, "O", O, q, t, true));
+    if (p->ldt < p->width || !within_reach(p->B, p->ldt, p->width))
+        return fail(GS_ERR_SHAPE, "%s: leading dimension of the table out of range", fn);
+    if (p->B && p->N && !p->klen) return fail(GS_ERR_ARG, "%s: klen is null", fn);
+    if (p->B && p->N && p->Lk && !p->table) return fail(GS_ERR_ARG, "%s: table is null", fn);
+    GS_CHECK(check_aligned(p->table, 4, "table"));
+    GS_CHECK(check_aligned(p->klen, 4, "klen"));
+    GS_CHECK(check_aligned(p->qoff, 4, "qoff"));
+    GS_CHECK(check_aligned(p->lse, 4, "lse"));
+    const size_t es = esize(t), need = gs_paged_attention_workspace(p, t);
+    GS_CHECK(check_ws(fn, ws, ws_bytes, need));
+    GS_CHECK(check_overlaps({seq_span(Q, q, es, "Q"), seq_span(p->K, c, es, "K"), seq_span(p->V, c, es, "V"),
+                             span(p->table, p->B, p->width, p->ldt, 4, "table"), span(p->klen, 1, p->B, p->B, 4, "klen"),
+                             span(p->qoff, 1, p->B + 1, p->B + 1, 4, "qoff")},
+                            {seq_span(O, q, es, "O"), span(p->lse, 1, p->N * p->Hq, 1, 4, "lse"), bytes_span(ws, need, "workspace")}));
+    if (!p->B || !p->N || !p->Lq) return ok();
+    GS_CHECK(check_device());
+    PagedAttnArgs a = paged_args(p);
+    a.Q = Q.p; a.K = p->K.p; a.V = p->V.p; a.O = O.p; a.lse = p->lse;
+    a.q = strides(Q); a.k = strides(p->K); a.v = strides(p->V); a.o = strides(O);
+    a.table = p->table; a.klen = p->klen; a.qoff = p->qoff;
+    a.scale = (float)p->scale;
+    a.vec = vec_rows(Q, q, t) && vec_rows(p->K, c, t) && vec_rows(p->V, c, t) && vec_rows(O, q, t);
+    return launched(launch_paged_attn(t, a, ws, (hipStream_t)stream), fn);
+}
+
+size_t gs_verify_workspace(int64_t B, int64_t M) {
+    if (!counts({B, M}) || B < 1 || M < 1 || verify_groups(B, M) >= ATTN_MAX_BLOCKS) return 0;
+    return verify_workspace(B, M);
+}
+
+gs_status gs_verify(const gs_drafts *p, gs_dtype pt, void *ws, size_t ws_bytes, void *stream) {
+    const char *fn = "gs_verify";
+    if (!p) return fail(GS_ERR_ARG, "%s: the drafts are null", fn);
+    if (!is_batch_type(pt)) return fail(GS_ERR_DTYPE, "%s: probabilities must be f32 or bf16", fn);
+    if (!counts({p->B, p->N, p->M}) || p->M < 1 || p->B >= ATTN_MAX_BLOCKS || verify_groups(p->B, p->M) >= ATTN_MAX_BLOCKS)
+        return fail(GS_ERR_SHAPE, "%s: need B, N >= 0 and M >= 1, below 2^31 - 256, B and B ceil(M / 4096) below 2^24 - 8", fn);
+    GS_CHECK(check_matrix(p->P, "P", p->N, p->M, p->ldp, pt, false));
+    GS_CHECK(check_matrix(p->Q, "Q", p->N, p->M, p->ldq, pt, true));
+    if ((p->P && !within_reach(p->N, p->ldp, p->M)) || (p->Q && !within_reach(p->N, p->ldq, p->M)))
+        return fail(GS_ERR_SHAPE, "%s: leading dimension out of range", fn);
+    const struct { const void *p; bool needed; const char *name; } each[] = {
+        {p->drafted, p->N > 0, "drafted"}, {p->u, p->N > 0, "u"}, {p->v, p->B > 0, "v"}, {p->qoff, p->B > 0, "qoff"},
+        {p->accepted, p->B > 0, "accepted"}, {p->entry, p->B > 0, "entry"}, {p->entries, false, "entries"}};
+    for (const auto &e : each) {
+        if (!e.p && e.needed) return fail(GS_ERR_ARG, "%s: %s is null", fn, e.name);
+        GS_CHECK(check_aligned(e.p, 4, e.name));
+    }
+    const size_t need = gs_verify_workspace(p->B, p->M);
+    GS_CHECK(check_ws(fn, ws, ws_bytes, need));
+    const size_t es = esize(pt);
+    GS_CHECK(check_overlaps({span(p->P, p->N, p->M, p->ldp, es, "P"), span(p->Q, p->N, p->M, p->ldq, es, "Q"),
+                             span(p->drafted, 1, p->N, p->N, 4, "drafted"), span(p->u, 1, p->N, p->N, 4, "u"),
+                             span(p->v, 1, p->B, p->B, 4, "v"), span(p->qoff, 1, p->B + 1, p->B + 1, 4, "qoff")},
+                            {span(p->accepted, 1, p->B, p->B, 4, "accepted"), span(p->entry, 1, p->B, p->B, 4, "entry"),
+                             span(p->entries, 1, p->N, p->N, 4, "entries"), bytes_span(ws, need, "workspace")}));
+    if (p->B == 0) return ok();
+    GS_CHECK(check_device());
+    VerifyArgs a{};
+    a.B = p->B; a.N = p->N; a.M = p->M; a.P = p->P; a.ldp = p->ldp; a.Q = p->Q; a.ldq = p->ldq;
+    a.drafted = p->drafted; a.u = p->u; a.v = p->v; a.qoff = p->qoff;
+    a.accepted = p->accepted; a.entry = p->entry; a.entries = p->entries;
+    const int64_t per = 16 / (int64_t)es;
+    a.vec_p = reinterpret_cast<uintptr_t>(p->P) % 16 == 0 && (p->N <= 1 || p->ldp % per == 0);
+    a.vec_q = reinterpret_cast<uintptr_t>(p->Q) % 16 == 0 && (p->N <= 1 || p->ldq % per == 0);
+    return launched(launch_verify(pt, a, ws, (hipStream_t)stream), fn);
 }
 
 }  // extern "C"

@@ -293,6 +293,81 @@ struct SampleArgs {
 size_t sample_workspace(int64_t B, int64_t M);
 hipError_t launch_sample(gs_dtype st, SampleArgs a, void *ws, hipStream_t s);
 
+// A paged cache: pages and slots of a step, its states (gs_paged.hip), its
+// attention (gs_paged_attn.hip).
+constexpr int64_t PLAN_ONE_PAGES = (int64_t)1 << 17;    // table entries up to which one work-group moves pages
+struct PagedPlanHead { int32_t nfree, back, taken, avail; };
+struct PagedPlanArgs {
+    int64_t B, page, rows, width, ldt, capacity;
+    int64_t most_length;                // min(width page, 2^31 - 1)
+    const int32_t *length, *add;
+    int32_t *length_out, *table, *free_pages;
+    const int32_t *nfree;
+    int32_t *nfree_out, *qoff;
+    int64_t *slots;
+    int32_t *added;
+    // set by launch_paged_plan
+    PagedPlanHead *head;
+    int32_t *sums;
+};
+size_t paged_plan_workspace(int64_t B);
+hipError_t launch_paged_plan(PagedPlanArgs a, void *ws, hipStream_t s);
+struct PagedStoreArgs {
+    const void *K, *V;
+    void *Kc, *Vc;
+    const int64_t *slots;
+    SeqStrides k, v, kc, vc;
+    int64_t N, pages, page;
+    int Hkv, Dh;
+    bool vec_in, vec_out;               // 16-byte pieces of rows, Dh a multiple of 8
+    // set by launch_paged_store
+    int head_pieces;
+    int64_t pieces;
+};
+hipError_t launch_paged_store(gs_dtype t, gs_dtype ct, PagedStoreArgs a, hipStream_t s);
+struct PagedItem { int32_t b, tile, x0, x1, slot; };        // key tiles x0 .. x1 - 1 of a block of rows; slot -1: all of them
+struct PagedJoin { int32_t b, tile, slot, parts; };
+struct PagedAttnHead { int32_t items, joins; };
+struct PagedAttnArgs {
+    const void *Q, *K, *V;
+    void *O;
+    float *lse;                         // N x Hq, nullable
+    SeqStrides q, k, v, o;
+    int B, N, Lq, Lk, Hq, Hkv, Dh, G;
+    int pages, page, window, sinks;
+    int64_t ldt;
+    const int32_t *table, *klen, *qoff; // qoff nullable
+    float scale;
+    bool vec;
+    // set by launch_paged_attn
+    uint32_t page_magic; int page_shift;    // j / page = (j page_magic) >> 32 >> page_shift
+    int rows, blocks, waves, least;         // packed rows of a part; blocks of rows; work-groups that share the work; fewest tiles of a part
+    PagedAttnHead *head;
+    PagedItem *items;
+    PagedJoin *joins;
+    float *part, *part_lse;
+};
+size_t paged_attn_workspace(gs_dtype t, const PagedAttnArgs &a);
+hipError_t launch_paged_attn(gs_dtype t, PagedAttnArgs a, void *ws, hipStream_t s);
+
+// Drafted entries (gs_verify.hip).
+struct VerifyArgs {
+    int64_t B, N, M;
+    const void *P; int64_t ldp;
+    const void *Q; int64_t ldq;         // nullable
+    const int32_t *drafted;
+    const float *u, *v;
+    const int32_t *qoff;
+    int32_t *accepted, *entry, *entries;
+    bool vec_p, vec_q;                  // rows start on 16-byte boundaries
+    // set by launch_verify
+    int64_t parts;
+    double *sums;                       // B x parts x 2
+};
+int64_t verify_groups(int64_t B, int64_t M);
+size_t verify_workspace(int64_t B, int64_t M);
+hipError_t launch_verify(gs_dtype pt, VerifyArgs a, void *ws, hipStream_t s);
+
 // Compression.
 size_t compress_workspace(int64_t M, int64_t D);
 // A second stream (non-blocking, default priority) on which compression runs

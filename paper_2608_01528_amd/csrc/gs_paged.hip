@@ -1,0 +1,272 @@
+// A paged cache's bookkeeping: pages and slots of a step (gs_paged_plan) and the
+// states of its rows written into them (gs_paged_store).
+//
+// Plan.  Everything follows from prefix sums over the requests: of the pages
+// given back, of the pages wanted and of the new rows.  One work-group forms
+// them; then each page moved and each slot is found on its own, by a binary
+// search of its index in those sums.  A page taken in this step may have been
+// given back in this step: it is then read from the table of the request that
+// gave it (which the step does not write), not from the free list, so that no
+// part waits for another.
+#include "gs_scan.h"
+
+namespace gs {
+namespace {
+
+constexpr int SCAN = 1024;          // requests a round of the scan, and threads of its work-group
+constexpr int STAGED = 2048;        // requests whose sums are searched in LDS
+constexpr int ONE_ROWS = 4096;      // rows up to which the scan's work-group fills in everything itself
+
+typedef PagedPlanHead PlanHead;
+
+// Pages of x positions (both below 2^31).
+__device__ __forceinline__ int64_t up(int64_t x, int64_t page) {
+    return x ? (int64_t)(((uint32_t)x - 1u) / (uint32_t)page + 1u) : 0;
+}
+
+// Sums over the requests as a step leaves them (B + 1 entries where there is a
+// total).  left: positions before the new ones, or -1 - that where the request
+// asked and got nothing.
+struct PlanSums {
+    const int32_t *left, *back, *take, *qoff;
+};
+
+__device__ __forceinline__ int32_t below(int64_t x, int64_t most) { return (int32_t)(x < most ? x : most); }
+
+// The sums, written to `left`, `back`, `take`, `rows_at` (nullable, as qoff) and the
+// outputs qoff, length_out, added and nfree_out.
+__device__ void plan_sums(const PagedPlanArgs &a, int32_t *left, int32_t *back, int32_t *take, int32_t *rows_at,
+                          PlanHead *head) {
+    __shared__ int64_t room[4][SCAN / 64];
+    __shared__ unsigned long long first_short;
+    const int t = threadIdx.x;
+    const int64_t page = a.page, most = a.most_length;      // min(width page, 2^31 - 1)
+    const int64_t nfree = min((int64_t)max(*a.nfree, 0), a.capacity), space = a.capacity - nfree;
+    int64_t len = 0, add = 0;
+    auto load = [&](int64_t b) {
+        len = add = 0;
+        if (b < a.B) {
+            len = a.length[b];
+            add = a.add[b];
+            len = len < 0 ? 0 : (len > most ? most : len);
+        }
+    };
+    if (t == 0) first_short = ~0ull;
+    int64_t given = 0;
+    int turn = 0;
+    for (int64_t b0 = 0; b0 < a.B; b0 += SCAN) {
+        const int64_t b = b0 + t;
+        load(b);
+        const int64_t rest = add < 0 ? max(len + add, (int64_t)0) : len;
+        int64_t total;
+        const int64_t at = group_scan(up(len, page) - up(rest, page), room[turn], &total);
+        turn ^= 1;
+        if (b < a.B) back[b] = below(given + at, space);
+        given += total;
+    }
+    const int64_t returned = min(given, space), avail = nfree + returned;
+    int64_t rows = 0, wanted = 0, taken = 0;
+    if (a.B == 0) __syncthreads();      // (nfree has been read by all before it may be written)
+    for (int64_t b0 = 0; b0 < a.B; b0 += SCAN) {
+        const int64_t b = b0 + t;
+        if (a.B > SCAN) load(b);
+        const int64_t n = max(add, (int64_t)0), rest = add < 0 ? max(len + add, (int64_t)0) : len;
+        int64_t row_total, want_total;
+        const int64_t row = rows + group_scan(n, room[turn], &row_total);
+        const bool fits = n > 0 && len + n <= most && row + n <= a.rows;
+        const int64_t need = fits ? up(len + n, page) - up(len, page) : 0;
+        const int64_t want = wanted + group_scan(need, room[2 + turn], &want_total);
+        turn ^= 1;
+        const bool served = fits && (need == 0 || want + need <= avail);
+        if (fits && !served) atomicMin(&first_short, (unsigned long long)want);
+        rows += row_total;
+        wanted += want_total;
+        __syncthreads();
+        // what was taken before the first request that found too few
+        taken = first_short != ~0ull ? (int64_t)first_short : wanted;
+        if (b < a.B) {
+            take[b] = (int32_t)min(want, taken);
+            left[b] = (int32_t)(n > 0 && !served ? -1 - rest : rest);
+            a.length_out[b] = (int32_t)(served ? len + n : rest);
+            a.added[b] = (int32_t)(served ? n : 0);
+            a.qoff[b] = below(row, 0x7fffffff);
+            if (rows_at) rows_at[b] = below(row, 0x7fffffff);
+        }
+    }
+    if (t == 0) {
+        back[a.B] = (int32_t)returned;
+        take[a.B] = (int32_t)taken;
+        a.qoff[a.B] = below(rows, 0x7fffffff);
+        if (rows_at) rows_at[a.B] = below(rows, 0x7fffffff);
+        *a.nfree_out = (int32_t)(avail - taken);
+        *head = PlanHead{(int32_t)nfree, (int32_t)returned, (int32_t)taken, (int32_t)avail};
+    }
+}
+
+// The last b with sums[b] <= i (sums[0] = 0, sums[B] > i).
+__device__ __forceinline__ int64_t owner(const int32_t *sums, int64_t B, int64_t i) {
+    int64_t lo = 0, hi = B;
+    while (hi - lo > 1) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (sums[mid] <= i) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Pages and slots number `first`, first + step, ...
+__device__ void plan_fill(const PagedPlanArgs &a, const PlanSums &z, const PlanHead &head, int64_t first, int64_t step) {
+    const int64_t B = a.B, page = a.page;
+    auto returned = [&](int64_t i) {
+        const int64_t b = owner(z.back, B, i);
+        return a.table[b * a.ldt + up(z.left[b], page) + (i - z.back[b])];
+    };
+    // the i-th page taken comes from the end of the free ones and the returned
+    // ones behind them
+    auto fresh = [&](int64_t i) {
+        const int64_t at = (int64_t)head.avail - 1 - i;
+        return at < head.nfree ? a.free_pages[at] : returned(at - head.nfree);
+    };
+    for (int64_t i = first; i < head.back; i += step) a.free_pages[(int64_t)head.nfree + i] = returned(i);
+    for (int64_t i = first; i < head.taken; i += step) {
+        const int64_t b = owner(z.take, B, i);
+        a.table[b * a.ldt + up(z.left[b], page) + (i - z.take[b])] = fresh(i);
+    }
+    const int64_t rows = B ? z.qoff[B] : 0;
+    for (int64_t r = first; r < a.rows; r += step) {
+        int64_t slot = -1;
+        if (r < rows) {
+            const int64_t b = owner(z.qoff, B, r), left = z.left[b];
+            if (left >= 0) {
+                const int64_t at = left + (r - z.qoff[b]), held = up(left, page), g = (uint32_t)at / (uint32_t)page;
+                const int64_t id = g < held ? a.table[b * a.ldt + g] : fresh(z.take[b] + (g - held));
+                if (id >= 0) slot = id * page + (at - g * page);
+            }
+        }
+        a.slots[r] = slot;
+    }
+}
+
+// The whole step in one work-group.  free_pages and table entries that are read
+// are not those that are written, but for the free list's returned part, which is
+// read from the tables.
+__global__ void __launch_bounds__(SCAN) plan_kernel(PagedPlanArgs a) {
+    __shared__ int32_t left[SCAN], back[SCAN + 1], take[SCAN + 1], rows_at[SCAN + 1];
+    __shared__ PlanHead head;
+    plan_sums(a, left, back, take, rows_at, &head);
+    __syncthreads();
+    plan_fill(a, PlanSums{left, back, take, rows_at}, head, threadIdx.x, SCAN);
+}
+
+__global__ void __launch_bounds__(SCAN) plan_sums_kernel(PagedPlanArgs a) {
+    int32_t *const at = a.sums;
+    plan_sums(a, at, at + a.B, at + 2 * a.B + 1, nullptr, a.head);
+}
+
+__global__ void __launch_bounds__(256) plan_fill_kernel(PagedPlanArgs a) {
+    __shared__ int32_t staged[4 * STAGED + 3];
+    const int B = (int)a.B;
+    PlanSums z{a.sums, a.sums + a.B, a.sums + 2 * a.B + 1, a.qoff};
+    if (a.B <= STAGED) {
+        for (int i = threadIdx.x; i < 3 * B + 2; i += 256) staged[i] = a.sums[i];
+        for (int i = threadIdx.x; i < B + 1; i += 256) staged[3 * B + 2 + i] = a.qoff[i];
+        __syncthreads();
+        z = PlanSums{staged, staged + B, staged + 2 * B + 1, staged + 3 * B + 2};
+    }
+    plan_fill(a, z, *a.head, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
+}
+
+// ---------------------------------------------------------------- rows
+
+// Eight values of a row from d on.
+template <typename T> __device__ __forceinline__ void read8(float (&v)[8], const T *row, int d, int dh, bool vec) {
+    typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+    if (vec) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const u4v x = *reinterpret_cast<const u4v *>(row + d + 4 * q);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[4 * q + e] = __uint_as_float(x[e]);
+            }
+        } else {
+            const u4v x = *reinterpret_cast<const u4v *>(row + d);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = bf16_to_f32((uint16_t)(x[e / 2] >> (16 * (e & 1))));
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = d + e < dh ? ld_f32<T>(row, d + e) : 0.f;
+    }
+}
+template <typename T> __device__ __forceinline__ void write8(const float (&v)[8], T *row, int d, int dh, bool vec) {
+    typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+    if (vec) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                u4v x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = __float_as_uint(v[4 * q + e]);
+                *reinterpret_cast<u4v *>(row + d + 4 * q) = x;
+            }
+        } else {
+            u4v x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = f32_to_bf16(v[2 * e]) | (uint32_t)f32_to_bf16(v[2 * e + 1]) << 16;
+            *reinterpret_cast<u4v *>(row + d) = x;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (d + e < dh) st_f32<T>(row, d + e, v[e]);
+    }
+}
+
+// A thread moves eight values of K and of V.
+template <typename T, typename C> __global__ void __launch_bounds__(256) store_kernel(PagedStoreArgs a) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.N * a.pieces) return;
+    const int64_t n = i / a.pieces;
+    const int rest = (int)(i % a.pieces), h = rest / a.head_pieces, d = 8 * (rest % a.head_pieces);
+    const int64_t slot = a.slots[n];
+    if (slot < 0 || slot >= a.pages * a.page) return;
+    const int64_t g = slot / a.page, at = slot % a.page;
+    float k[8], v[8];
+    read8<T>(k, static_cast<const T *>(a.K) + n * a.k.l + h * a.k.h, d, a.Dh, a.vec_in);
+    read8<T>(v, static_cast<const T *>(a.V) + n * a.v.l + h * a.v.h, d, a.Dh, a.vec_in);
+    write8<C>(k, static_cast<C *>(a.Kc) + g * a.kc.b + at * a.kc.l + h * a.kc.h, d, a.Dh, a.vec_out);
+    write8<C>(v, static_cast<C *>(a.Vc) + g * a.vc.b + at * a.vc.l + h * a.vc.h, d, a.Dh, a.vec_out);
+}
+
+}  // namespace
+
+size_t paged_plan_workspace(int64_t B) { return (sizeof(PlanHead) + 4 * (size_t)(3 * B + 2) + 15) / 16 * 16; }
+
+hipError_t launch_paged_plan(PagedPlanArgs a, void *ws, hipStream_t s) {
+    a.head = static_cast<PlanHead *>(ws);
+    a.sums = reinterpret_cast<int32_t *>(a.head + 1);
+    if (a.B <= SCAN && a.rows <= ONE_ROWS && a.B * a.width <= PLAN_ONE_PAGES) {
+        plan_kernel<<<dim3(1), dim3(SCAN), 0, s>>>(a);
+        return hipGetLastError();
+    }
+    plan_sums_kernel<<<dim3(1), dim3(SCAN), 0, s>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t groups = (a.rows + 1023) / 1024, most = 1024;
+    plan_fill_kernel<<<dim3((unsigned)(groups < 64 ? 64 : (groups < most ? groups : most))), dim3(256), 0, s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_store(gs_dtype t, gs_dtype ct, PagedStoreArgs a, hipStream_t s) {
+    a.head_pieces = (a.Dh + 7) / 8;
+    a.pieces = (int64_t)a.Hkv * a.head_pieces;
+    const dim3 grid((unsigned)((a.N * a.pieces + 255) / 256)), group(256);
+    if (t == GS_F32 && ct == GS_F32) store_kernel<float, float><<<grid, group, 0, s>>>(a);
+    else if (t == GS_F32) store_kernel<float, bf16_t><<<grid, group, 0, s>>>(a);
+    else if (ct == GS_F32) store_kernel<bf16_t, float><<<grid, group, 0, s>>>(a);
+    else store_kernel<bf16_t, bf16_t><<<grid, group, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace gs

@@ -1,0 +1,710 @@
+// Attention of a step's rows to their requests' states in a paged cache.
+//
+// The pass over the states is that of gs_xattn.hip: blocks of 32 rows a wave (the
+// rows of the heads that share a key and value head side by side), tiles of keys
+// and values through LDS, scores with the keys as rows, a running maximum and
+// sum.  What differs is where a tile's rows lie (each state's page is looked up,
+// a tile or two before its values are asked for) and what a row sees (states up
+// to its own position, from its window's start on, and the first few).
+//
+// How the work is shared out follows the lengths in device memory.  Requests of
+// few rows (up to 32 a key and value head: tokens, drafts): all tiles of all
+// requests and heads lie in one line, of which every wave takes an equal part
+// (few_kernel); a request cut by part ends is put together by few_join_kernel.
+// More rows (prompts): a launch lists the blocks of 128 rows, longest first, cut
+// where they are longer than a work-group's share (plan_kernel), and what was cut
+// is put together by many_join_kernel.
+#include "gs_attn.h"
+#include "gs_scan.h"
+
+namespace gs {
+namespace {
+using namespace attn;
+
+// ------------------------------------------------------------ what is seen
+
+// Rows of request b: qoff clamped to the tensors' rows; `n` of them count for
+// positions, the first `count` are computed.
+struct Rows {
+    int first, n, count, kl;
+    __device__ __forceinline__ Rows(const PagedAttnArgs &a, int b) {
+        kl = clamped(a.klen, b, a.Lk);
+        if (!a.qoff) {
+            first = b;
+            n = 1;
+        } else {
+            first = clamped(a.qoff, b, a.N);
+            n = clamped(a.qoff, b + 1, a.N) - first;
+        }
+        if (n < 0) n = 0;
+        count = n < a.Lq ? n : a.Lq;
+    }
+};
+
+// States that rows i0 .. i1 of a request see: [0, sink) and [lo, hi), and the
+// tiles of BN that hold them.
+template <int BN> struct View {
+    int hi, lo, sink, sink_tiles, first_tile, tiles;
+    __device__ __forceinline__ View(const PagedAttnArgs &a, const Rows &r, int i0, int i1) {
+        const int pmin = r.kl - r.n + i0, pmax = r.kl - r.n + i1;
+        hi = pmax < 0 ? 0 : pmax + 1;
+        lo = a.window && pmin >= a.window ? pmin - a.window + 1 : 0;
+        sink = a.sinks < lo ? a.sinks : lo;
+        sink_tiles = (sink + BN - 1) / BN;
+        first_tile = lo / BN;
+        if (first_tile < sink_tiles) first_tile = sink_tiles;
+        const int end = (hi + BN - 1) / BN;
+        tiles = sink_tiles + (end > first_tile ? end - first_tile : 0);
+    }
+    __device__ __forceinline__ int start(int x) const { return (x < sink_tiles ? x : first_tile + (x - sink_tiles)) * BN; }
+    __device__ __forceinline__ bool holds(int j) const { return j < hi && (j < sink || j >= lo); }
+};
+
+// Bits 0 .. n - 1.
+__device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0 : (n >= 64 ? ~0ull : (1ull << n) - 1); }
+
+// ------------------------------------------------------------ tiles from pages
+
+// Where the keys of a tile lie: lane l knows key j0 + l.  Keys that are not
+// there stand for page 0, place 0, which is in memory, and do not take part.
+template <int BN> struct Places {
+    const int32_t *table;       // the request's
+    int l;
+    int32_t id;
+    int j;
+    bool there;
+    __device__ __forceinline__ int page_of(const PagedAttnArgs &a) const {
+        return a.page_magic ? (int)(__umulhi((uint32_t)j, a.page_magic) >> a.page_shift) : j;
+    }
+    // asks for the page of this lane's key of the tile at j0
+    __device__ __forceinline__ void ahead(const PagedAttnArgs &a, const View<BN> &v, int j0) {
+        j = j0 + l;
+        there = l < BN && v.holds(j);
+        id = -1;
+        if (there) id = table[page_of(a)];
+    }
+    // Lanes' pages and places in them, and the keys that are there (of the tile
+    // last asked for).
+    __device__ __forceinline__ uint64_t take(const PagedAttnArgs &a, int32_t *page, int32_t *at) const {
+        const bool on = there && id >= 0 && id < a.pages;
+        *page = on ? id : 0;
+        *at = on ? j - page_of(a) * a.page : 0;
+        return __ballot(on);
+    }
+};
+
+// A thread's part of a tile of K or V on its way to LDS (as TileLoad, rows from
+// pages).  Rows that are not live hold page 0's values until `clean`.
+template <typename T, int DP, int BN, int NT, bool VEC> struct PagedLoad {
+    static constexpr int PER = Op<T>::PER, CPR = DP / PER, N = BN * CPR / NT, RPI = NT / CPR;
+    static_assert(BN * CPR % NT == 0 && NT % CPR == 0, "whole chunks per thread");
+    u4v v[N];
+    __device__ __forceinline__ void fetch(const T *cache, const SeqStrides &s, int32_t page, int32_t at, bool any, int dh, int t) {
+        const int c = t % CPR, r0 = t / CPR;
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            const int32_t g = __shfl(page, r0 + q * RPI), i = __shfl(at, r0 + q * RPI);
+            v[q] = u4v{0, 0, 0, 0};
+            if (any && c * PER < dh) v[q] = load_chunk<T>(cache + g * s.b + i * s.l, PER * c, dh, VEC);
+        }
+    }
+    __device__ __forceinline__ void stash(char *tile, int t) const {
+#pragma unroll
+        for (int q = 0; q < N; ++q) *reinterpret_cast<u4v *>(tile + place<T, DP>(t / CPR + q * RPI, t % CPR)) = v[q];
+    }
+    // zeros in the rows that are not live
+    __device__ __forceinline__ void clean(uint64_t live, int t) {
+#pragma unroll
+        for (int q = 0; q < N; ++q)
+            if (!((live >> (t / CPR + q * RPI)) & 1)) v[q] = u4v{0, 0, 0, 0};
+    }
+    // zeros in place of values that are not finite; their rows marked in *rows (the
+    // wave's own, in LDS)
+    __device__ __forceinline__ void finite(unsigned long long *rows, int t) {
+        *rows = 0;
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            bool bad = false;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t x = v[q][e];
+                if constexpr (sizeof(T) == 4) {
+                    const bool b = (x & 0x7f800000u) == 0x7f800000u;
+                    if (b) v[q][e] = 0;
+                    bad |= b;
+                } else {
+                    const bool lo = (x & 0x7f80u) == 0x7f80u, hi = (x & 0x7f800000u) == 0x7f800000u;
+                    v[q][e] = (lo ? 0 : x & 0xffffu) | (hi ? 0 : x & 0xffff0000u);
+                    bad |= lo || hi;
+                }
+            }
+            if (bad) atomicOr(rows, 1ull << (t / CPR + q * RPI));
+        }
+    }
+};
+
+// o += the values of a state's row that are not finite.
+template <typename T, int NJ> __device__ __forceinline__ void add_not_finite(f16v (&o)[NJ], const T *row, int dh, int l) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int d = 32 * j + 8 * (e / 4) + 4 * (l >> 5) + e % 4;
+            const float x = d < dh ? ld_f32<T>(row, d) : 0.f;
+            if (!(fabsf(x) < INFINITY)) o[j][e] += x;
+        }
+        asm volatile("" ::: "memory");      // (few registers matter more than time here)
+    }
+}
+
+// ------------------------------------------------------------ the pass
+
+// A block of 32 NW packed rows from m0 on of request b's head group hk against its
+// tiles x0 .. x1 - 1.  Writes O and lse, or, with `part`, the rows' results of
+// these tiles there.
+template <typename T, int DC, int NW, int BN, bool VEC>
+__device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, unsigned long long *marks, int b, int hk, const Rows &r, int m0, int x0, int x1,
+                                     float *part, float *part_lse) {
+    constexpr int DP = padded(DC), PER = Op<T>::PER, NS = DC / (2 * PER), NJ = DC / 32, NT = 64 * NW;
+    constexpr int TILE = BN * DP * sizeof(T);
+    const int t = threadIdx.x % NT, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int all = r.count * a.G, mw = m0 + 32 * w, m = mw + (l & 31);
+    const bool on = m < all, wave_on = mw < all;
+    const RowOf row(on ? m : 0, hk, a.G);
+    const int64_t at = r.first + row.i;
+    const int i0 = m0 / a.G, i1 = (m0 + 32 * NW < all ? m0 + 32 * NW - 1 : all - 1) / a.G;
+    const View<BN> view(a, r, i0, i1);
+    // positions: this lane's row's, and the first and last of the wave's rows
+    const int p0 = r.kl - r.n, pos = p0 + row.i;
+    const int pmin = p0 + mw / a.G, pmax = p0 + (mw + 32 < all ? mw + 31 : all - 1) / a.G;
+
+    typename Op<T>::V q[NS];
+    load_frags<T, DC>(q, on ? static_cast<const T *>(a.Q) + at * a.q.l + row.h * a.q.h : nullptr, a.Dh, VEC, l);
+    const float c = fabsf(a.scale) * LOG2E;
+    if (a.scale < 0) {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) q[s] = -q[s];
+    }
+    const T *const K = static_cast<const T *>(a.K) + hk * a.k.h;
+    const T *const V = static_cast<const T *>(a.V) + hk * a.v.h;
+    Places<BN> keys{a.table + b * a.ldt, l, -1, 0, false};
+
+    f16v o[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) o[j] = f16v{0};
+    float mx = -INFINITY, sum = 0.f;
+
+    PagedLoad<T, DP, BN, NT, VEC> kr, vr;
+    uint64_t live = 0, next_live = 0;
+    auto fetch = [&]() {
+        int32_t page, place;
+        const uint64_t on = keys.take(a, &page, &place);
+        kr.fetch(K, a.k, page, place, on != 0, a.Dh, t);
+        vr.fetch(V, a.v, page, place, on != 0, a.Dh, t);
+        return on;
+    };
+    // all keys of the tile at j0 are there, and seen by rows at positions from p to q
+    auto seen_by = [&](uint64_t on, int j0, int p, int q) {
+        return on == ALL_LIVE<BN> && p >= j0 + BN - 1 && (!a.window || (int64_t)q - a.window < j0 || j0 + BN <= a.sinks);
+    };
+    // Rows of the block see different states of the tile: a product takes 0 inf and 0
+    // NaN for NaN, so that values which are not finite are kept out of it.
+    auto differ = [&](uint64_t on, int j0) { return i0 != i1 && !seen_by(on, j0, p0 + i0, p0 + i1); };
+    auto stash = [&](char *kt, int buffer, uint64_t on, int j0) {
+        if (on != ALL_LIVE<BN>) vr.clean(on, t);
+        if (differ(on, j0)) vr.finite(marks + NW * buffer + w, t);
+        kr.stash(kt, t);
+        vr.stash(kt + TILE, t);
+    };
+    int buffer = 0;             // the tile in use: K, then V
+    if (x0 < x1) {
+        keys.ahead(a, view, view.start(x0));
+        live = fetch();
+        if (x0 + 1 < x1) keys.ahead(a, view, view.start(x0 + 1));
+        stash(lds, 0, live, view.start(x0));
+        if (x0 + 1 < x1) {
+            next_live = fetch();
+            if (x0 + 2 < x1) keys.ahead(a, view, view.start(x0 + 2));
+        }
+    }
+    for (int x = x0; x < x1; ++x) {
+        const int j0 = view.start(x);
+        const char *const kt = lds + buffer * 2 * TILE, *const vt = kt + TILE;
+        lds_barrier();
+        if (wave_on) {
+            f16v p[BN / 32];
+#pragma unroll
+            for (int n = 0; n < BN / 32; ++n) {
+                p[n] = f16v{0};
+#pragma unroll
+                for (int s = 0; s < NS; ++s) p[n] = Op<T>::mma(row_frag<T, DP>(kt, 32 * n, s, l), q[s], p[n]);
+            }
+            uint64_t seen = ~0ull;
+            if (!seen_by(live, j0, pmin, pmax)) {
+                seen = low_bits(pos + 1 - j0);
+                if (a.window) seen &= ~low_bits((pos >= a.window ? pos - a.window + 1 : 0) - j0) | low_bits(a.sinks - j0);
+                seen &= live;
+#pragma unroll
+                for (int n = 0; n < BN / 32; ++n) {
+                    const uint32_t bits = (uint32_t)(seen >> (32 * n)) >> (4 * (l >> 5));
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (!((bits >> (8 * (e / 4) + e % 4)) & 1)) p[n][e] = -INFINITY;
+                }
+            }
+            float top = p[0][0];
+#pragma unroll
+            for (int n = 0; n < BN / 32; ++n)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, p[n][e]);
+            top = fmaxf(top, other_half(top)) * c;
+            // (the reference of the exponents follows the maximum in steps of 2^8)
+            if (__any(top > mx + 8.f)) {
+                const float next = fmaxf(mx, top);
+                const float turn = __builtin_amdgcn_exp2f(mx - (next == -INFINITY ? 0.f : next));
+                mx = next;
+                sum *= turn;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) o[j] *= turn;
+            }
+            const float ref = mx == -INFINITY ? 0.f : mx;
+            float more = 0.f;
+#pragma unroll
+            for (int n = 0; n < BN / 32; ++n)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    p[n][e] = __builtin_amdgcn_exp2f(fmaf(p[n][e], c, -ref));
+                    more += p[n][e];
+                }
+            sum += more;
+#pragma unroll
+            for (int n = 0; n < BN / 32; ++n)
+#pragma unroll
+                for (int s = 0; s < 16 / PER; ++s) {
+                    const typename Op<T>::V pf = Op<T>::pack(p[n], s);
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) o[j] = Op<T>::mma(col_frag<T, DP>(vt, 32 * n, s, j, l), pf, o[j]);
+                }
+            if (differ(live, j0)) {
+                unsigned long long rest = 0;
+#pragma unroll
+                for (int v = 0; v < NW; ++v) rest |= marks[NW * buffer + v];
+                for (; rest; rest &= rest - 1) {
+                    const int k = __ffsll(rest) - 1, j = j0 + k, g = j / a.page;
+                    const T *const from = V + keys.table[g] * a.v.b + (j - g * a.page) * a.v.l;
+                    if ((seen >> k) & 1) add_not_finite<T, NJ>(o, from, a.Dh, l);
+                }
+            }
+        }
+        buffer ^= 1;
+        live = next_live;
+        if (x + 1 < x1) {
+            stash(lds + buffer * 2 * TILE, buffer, live, view.start(x + 1));
+            if (x + 2 < x1) {
+                next_live = fetch();
+                if (x + 3 < x1) keys.ahead(a, view, view.start(x + 3));
+            }
+        }
+    }
+    sum += other_half(sum);
+    if (!on) return;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float lse = sum != 0.f ? (mx + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
+    if (part) {
+        float *const po = part + (int64_t)(m - m0) * DP;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                f4v v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = o[j][4 * g + e] * inv;
+                *reinterpret_cast<f4v *>(po + 32 * j + 8 * g + 4 * (l >> 5)) = v;
+            }
+        if (l < 32) part_lse[m - m0] = lse;
+        return;
+    }
+    T *const out = static_cast<T *>(a.O) + at * a.o.l + row.h * a.o.h;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            f4v v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = o[j][4 * g + e] * inv;
+            store4<T>(out, 32 * j + 8 * g + 4 * (l >> 5), a.Dh, VEC, v);
+        }
+    if (a.lse && l < 32) a.lse[at * a.Hq + row.h] = lse;
+}
+
+// Waves a SIMD that registers are kept for (as gs_xattn.hip).
+template <typename T, int DC, int NW> constexpr int min_waves() { return sizeof(T) == 4 && (DC > 64 || NW == 1) ? 1 : 2; }
+
+// ------------------------------------------------------------ few rows
+
+// Tiles of request b; one where there are rows, but no states.
+template <int BN> __device__ __forceinline__ int few_tiles(const PagedAttnArgs &a, int b) {
+    const Rows r(a, b);
+    if (!r.count) return 0;
+    const View<BN> v(a, r, 0, r.count - 1);
+    return v.tiles > 1 ? v.tiles : 1;
+}
+
+// A place in the line of all (request, head, tile): requests in order, each
+// request's heads one after the other.  Found by a wave: `total` tiles of a head
+// over all requests, the request that holds unit u, and the tiles of a head of
+// those before it.
+template <int BN> struct Line {
+    int64_t total, before;
+    int b;
+    template <typename F> __device__ __forceinline__ void find(const PagedAttnArgs &a, F unit) {
+        const int l = threadIdx.x & 63;
+        int s = 0, e = a.B;
+        before = 0;
+        bool first = true;
+        int64_t u = 0;
+        do {
+            const int per = (e - s + 63) / 64;
+            const int from = s + l * per, to = from + per < e ? from + per : e;
+            int64_t mine = 0;
+#pragma unroll 4
+            for (int i = from; i < to; ++i) mine += few_tiles<BN>(a, i);
+            int64_t sums = mine;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int64_t x = __shfl_up((long long)sums, d);
+                if (l >= d) sums += x;
+            }
+            if (first) {
+                total = __shfl((long long)sums, 63);
+                u = unit(total);
+                first = false;
+            }
+            const uint64_t past = __ballot((before + sums) * a.Hkv > u);
+            if (!past) {        // behind the end
+                b = a.B;
+                return;
+            }
+            const int at = __ffsll((unsigned long long)past) - 1;
+            before += __shfl((long long)(sums - mine), at);
+            s += at * per;
+            e = s + per < e ? s + per : e;
+        } while (e - s > 1);
+        b = s;
+    }
+};
+
+__device__ __forceinline__ int64_t few_share(const PagedAttnArgs &a, int64_t total) {
+    const int64_t per = (total * a.Hkv + a.waves - 1) / a.waves;
+    return per < a.least ? a.least : per;
+}
+
+template <typename T, int DC, int BN, bool VEC>
+__global__ void __launch_bounds__(64, (min_waves<T, DC, 1>())) few_kernel(PagedAttnArgs a) {
+    constexpr int DP = padded(DC);
+    __shared__ __attribute__((aligned(16))) char lds[4 * BN * DP * sizeof(T)];
+    __shared__ unsigned long long marks[2];
+    const int64_t wave = blockIdx.x;
+    int64_t share = 0;
+    Line<BN> line;
+    line.find(a, [&](int64_t total) {
+        share = few_share(a, total);
+        return wave * share;
+    });
+    const int64_t begin = wave * share, units = line.total * a.Hkv;
+    const int64_t end = begin + share < units ? begin + share : units;
+    int b = __builtin_amdgcn_readfirstlane(line.b);
+    int64_t u = begin, before = line.before;
+    while (u < end && b < a.B) {
+        const Rows r(a, b);
+        const int tiles = few_tiles<BN>(a, b);
+        if (tiles) {
+            const int64_t off = u - before * a.Hkv;
+            const int hk = (int)(off / tiles), x0 = (int)(off % tiles);
+            const int x1 = end - u < tiles - x0 ? x0 + (int)(end - u) : tiles;
+            const View<BN> v(a, r, 0, r.count - 1);
+            float *part = nullptr, *part_lse = nullptr;
+            if (x1 - x0 < tiles) {
+                const int64_t slot = 2 * wave + (u - x0 > begin);
+                part = a.part + slot * a.rows * DP;
+                part_lse = a.part_lse + slot * a.rows;
+            }
+            pass<T, DC, 1, BN, VEC>(a, lds, marks, b, hk, r, 0, x0, x1 < v.tiles ? x1 : v.tiles, part, part_lse);
+            u += x1 - x0;
+            if (hk + 1 < a.Hkv || x1 < tiles) continue;
+        }
+        before += tiles;
+        ++b;
+    }
+}
+
+// Puts together a row of a request and head that part ends cut: a work-group a
+// row, parts shared out to its lanes' groups.
+template <typename T, int DP, int BN> __global__ void __launch_bounds__(256) few_join_kernel(PagedAttnArgs a) {
+    constexpr int LANES = DP / 4, GROUPS = 256 / LANES;
+    __shared__ int64_t counts[2][4];
+    __shared__ f4v sums[GROUPS][LANES];
+    __shared__ float weights[GROUPS], tops[4];
+    const int t = threadIdx.x, l = t & 63, w = t >> 6;
+    const int m = blockIdx.x % a.rows, hk = blockIdx.x / a.rows % a.Hkv, b = blockIdx.x / a.rows / a.Hkv;
+    const Rows r(a, b);
+    if (m >= r.count * a.G) return;
+    int64_t total = 0, before = 0;
+    for (int i = t; i < a.B; i += 256) {
+        const int n = few_tiles<BN>(a, i);
+        total += n;
+        if (i < b) before += n;
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        total += __shfl_xor((long long)total, d);
+        before += __shfl_xor((long long)before, d);
+    }
+    if (l == 0) counts[0][w] = total, counts[1][w] = before;
+    __syncthreads();
+    total = counts[0][0] + counts[0][1] + counts[0][2] + counts[0][3];
+    before = counts[1][0] + counts[1][1] + counts[1][2] + counts[1][3];
+    const int tiles = few_tiles<BN>(a, b);
+    const int64_t share = few_share(a, total), u0 = before * a.Hkv + (int64_t)hk * tiles;
+    const int64_t w0 = u0 / share, w1 = (u0 + tiles - 1) / share;
+    if (w0 == w1) return;
+    auto slot = [&](int64_t i) { return 2 * i + (u0 > i * share); };
+    float top = -INFINITY;
+    for (int64_t i = w0 + t; i <= w1; i += 256) top = fmaxf(top, a.part_lse[slot(i) * a.rows + m]);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if (l == 0) tops[w] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    const float ref = top == -INFINITY ? 0.f : top;
+    const int g = t / LANES, d = t % LANES;
+    f4v o = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+#pragma unroll 4
+    for (int64_t i = w0 + g; i <= w1; i += GROUPS) {
+        const int64_t at = slot(i) * a.rows + m;
+        const float e = __builtin_amdgcn_exp2f((a.part_lse[at] - ref) * LOG2E);
+        sum += e;
+        o += e * *reinterpret_cast<const f4v *>(a.part + at * DP + 4 * d);
+    }
+    sums[g][d] = o;
+    if (d == 0) weights[g] = sum;
+    __syncthreads();
+    if (g) return;
+    for (int i = 1; i < GROUPS; ++i) o += sums[i][d], sum += weights[i];
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    const RowOf row(m, hk, a.G);
+    const int64_t at = r.first + row.i;
+    if (4 * d < a.Dh) store4<T>(static_cast<T *>(a.O) + at * a.o.l + row.h * a.o.h, 4 * d, a.Dh, a.vec, o * inv);
+    if (a.lse && d == 0) a.lse[at * a.Hq + row.h] = sum != 0.f ? ref + __builtin_amdgcn_logf(sum) * LN2 : -INFINITY;
+}
+
+// ------------------------------------------------------------ many rows
+
+constexpr int BLOCK = 128;      // packed rows of a work-group of four waves
+
+// Requests' blocks lie in a line with a place for each: request b's from
+// floor(qoff[b] G / BLOCK) + b on, which leaves room for all of them.
+__device__ __forceinline__ int block_start(const PagedAttnArgs &a, int b) {
+    return (a.qoff ? clamped(a.qoff, b, a.N) : b) * a.G / BLOCK + b;
+}
+
+// Lists the work: blocks from the last one down (later rows of a prompt see more),
+// those of more than a share of the tiles in equal parts.
+template <int BN> __global__ void __launch_bounds__(1024) plan_kernel(PagedAttnArgs a) {
+    __shared__ int64_t room[4][16];
+    const int t = threadIdx.x;
+    auto tiles_of = [&](int i, int *b, int *tile) {
+        *b = 0, *tile = 0;
+        if (i >= a.blocks || a.B == 0) return 0;
+        int lo = 0, hi = a.B;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (block_start(a, mid) <= i) lo = mid;
+            else hi = mid;
+        }
+        const Rows r(a, lo);
+        const int k = i - block_start(a, lo), all = r.count * a.G;
+        if (k < 0 || k * BLOCK >= all) return 0;
+        *b = lo, *tile = k;
+        const View<BN> v(a, r, k * BLOCK / a.G, ((k + 1) * BLOCK < all ? (k + 1) * BLOCK - 1 : all - 1) / a.G);
+        return v.tiles > 1 ? v.tiles : 1;
+    };
+    int b, tile;
+    int64_t mine = 0, total;
+    for (int i = t; i < a.blocks; i += 1024) mine += tiles_of(i, &b, &tile);
+    (void)group_scan(mine, room[3], &total);
+    total = (total * a.Hkv + a.waves - 1) / a.waves;
+    const int share = total < a.least ? a.least : (int)(total < 0x40000000 ? total : 0x40000000);
+    int items = 0, slots = 0, joins = 0;
+    for (int i0 = 0; i0 < a.blocks; i0 += 1024) {
+        const int n = tiles_of(i0 + t < a.blocks ? a.blocks - 1 - (i0 + t) : a.blocks, &b, &tile);
+        const int parts = n > share ? (n - 1) / share + 1 : (n ? 1 : 0);
+        // (the next round's first scan waits for all to have read this one's last)
+        int64_t all;
+        const int item = items + (int)group_scan(parts, room[0], &all);
+        items += (int)all;
+        const int slot = slots + (int)group_scan(parts > 1 ? parts : 0, room[1], &all);
+        slots += (int)all;
+        const int join = joins + (int)group_scan(parts > 1, room[2], &all);
+        joins += (int)all;
+        for (int k = 0; k < parts; ++k)
+            a.items[item + k] = PagedItem{b, tile, (int32_t)((int64_t)n * k / parts), (int32_t)((int64_t)n * (k + 1) / parts),
+                                          parts > 1 ? slot + k : -1};
+        if (parts > 1) a.joins[join] = PagedJoin{b, tile, slot, parts};
+    }
+    if (t == 0) *a.head = PagedAttnHead{items, joins};
+}
+
+template <typename T, int DC, int BN, bool VEC>
+__global__ void __launch_bounds__(256, (min_waves<T, DC, 4>())) many_kernel(PagedAttnArgs a) {
+    constexpr int DP = padded(DC);
+    __shared__ __attribute__((aligned(16))) char lds[4 * BN * DP * sizeof(T)];
+    __shared__ unsigned long long marks[8];
+    const int item = blockIdx.x / a.Hkv, hk = blockIdx.x % a.Hkv;
+    if (item >= a.head->items) return;
+    const PagedItem p = a.items[item];
+    const Rows r(a, p.b);
+    const int m0 = p.tile * BLOCK, all = r.count * a.G;
+    const View<BN> v(a, r, m0 / a.G, (m0 + BLOCK < all ? m0 + BLOCK - 1 : all - 1) / a.G);
+    float *part = nullptr, *part_lse = nullptr;
+    if (p.slot >= 0) {
+        const int64_t slot = (int64_t)p.slot * a.Hkv + hk;
+        part = a.part + slot * BLOCK * DP;
+        part_lse = a.part_lse + slot * BLOCK;
+    }
+    pass<T, DC, 4, BN, VEC>(a, lds, marks, p.b, hk, r, m0, p.x0, p.x1 < v.tiles ? p.x1 : v.tiles, part, part_lse);
+}
+
+// Rows of blocks that were cut, DP / 4 lanes a row.
+template <typename T, int DP> __global__ void __launch_bounds__(256) many_join_kernel(PagedAttnArgs a) {
+    constexpr int LANES = DP / 4, PER = 256 / LANES, PIECES = BLOCK / PER;
+    const int join = blockIdx.x / (a.Hkv * PIECES), hk = blockIdx.x / PIECES % a.Hkv;
+    if (join >= a.head->joins) return;
+    const PagedJoin p = a.joins[join];
+    const int k = blockIdx.x % PIECES * PER + threadIdx.x / LANES, d = 4 * (threadIdx.x % LANES);
+    const Rows r(a, p.b);
+    const int m = p.tile * BLOCK + k;
+    if (m >= r.count * a.G || d >= a.Dh) return;
+    const float *const pl = a.part_lse + ((int64_t)p.slot * a.Hkv + hk) * BLOCK + k;
+    const float *const po = a.part + (((int64_t)p.slot * a.Hkv + hk) * BLOCK + k) * DP + d;
+    const int64_t step = (int64_t)a.Hkv * BLOCK;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll 8
+    for (int s = 0; s < p.parts; ++s) top = fmaxf(top, pl[s * step]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    f4v o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int s = 0; s < p.parts; ++s) {
+        const float e = __builtin_amdgcn_exp2f((pl[s * step] - ref) * LOG2E);
+        sum += e;
+        o += e * *reinterpret_cast<const f4v *>(po + s * step * DP);
+    }
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    const RowOf row(m, hk, a.G);
+    const int64_t at = r.first + row.i;
+    store4<T>(static_cast<T *>(a.O) + at * a.o.l + row.h * a.o.h, d, a.Dh, a.vec, o * inv);
+    if (a.lse && d == 0) a.lse[at * a.Hq + row.h] = sum != 0.f ? ref + __builtin_amdgcn_logf(sum) * LN2 : -INFINITY;
+}
+
+// ------------------------------------------------------------ dispatch
+
+constexpr int FEW = 32;         // packed rows up to which waves work alone
+
+constexpr int tile_keys(gs_dtype t, bool few) { return t == GS_F32 || few ? 32 : 64; }
+
+// Sizes of the workspace's parts, by sizes that the host knows.
+struct Layout {
+    bool few;
+    int waves, least, rows;
+    int64_t blocks, items, joins, slots;
+    int dp;
+    size_t list, bytes;
+};
+Layout layout(gs_dtype t, const PagedAttnArgs &a) {
+    Layout z{};
+    const int dc = computed(a.Dh);
+    const int64_t rows = (int64_t)a.Lq * a.G;
+    z.dp = padded(dc);
+    z.few = rows <= FEW;
+    if (z.few) {
+        // as many waves as the CUs hold at once, by their tiles' 160 KB
+        const int held = 163840 / (4 * tile_keys(t, true) * z.dp * (t == GS_F32 ? 4 : 2));
+        z.rows = (int)rows;
+        z.least = 4;
+        const int64_t most = ((int64_t)(a.Lk + 31) / 32 + 1) * a.B * a.Hkv / z.least + 1;
+        z.waves = (int)(most < 256 * held ? most : 256 * held);
+        z.slots = 2 * (int64_t)z.waves;
+    } else {
+        const int64_t most = t == GS_F32 && dc > 64 ? 256 : 512;
+        z.rows = BLOCK;
+        z.least = 8;
+        z.waves = (int)most;
+        z.blocks = (int64_t)a.N * a.G / BLOCK + a.B;
+        // a share is at least total Hkv / waves: blocks cut into parts have at most
+        // waves / Hkv + 1 shares in all, and less than two parts a share
+        z.slots = 2 * (most / a.Hkv + 1);
+        z.items = z.blocks + z.slots;
+        z.joins = z.slots / 2 + 1;
+        z.slots *= a.Hkv;
+    }
+    z.list = sizeof(PagedAttnHead) + (size_t)z.items * sizeof(PagedItem) + (size_t)z.joins * sizeof(PagedJoin);
+    z.list = (z.list + 15) / 16 * 16;
+    z.bytes = z.list + (size_t)z.slots * z.rows * (z.dp + 1) * 4;
+    return z;
+}
+
+template <typename T, int DC, bool VEC> hipError_t launch_sized(const PagedAttnArgs &a, const Layout &z, hipStream_t s) {
+    constexpr int DP = padded(DC);
+    constexpr gs_dtype t = sizeof(T) == 4 ? GS_F32 : GS_BF16;
+    if (z.few) {
+        constexpr int BN = tile_keys(t, true);
+        few_kernel<T, DC, BN, VEC><<<dim3((unsigned)z.waves), dim3(64), 0, s>>>(a);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess || z.waves == 1) return e;
+        few_join_kernel<T, DP, BN><<<dim3((unsigned)(a.B * a.Hkv * a.rows)), dim3(256), 0, s>>>(a);
+        return hipGetLastError();
+    }
+    constexpr int BN = tile_keys(t, false);
+    plan_kernel<BN><<<dim3(1), dim3(1024), 0, s>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    many_kernel<T, DC, BN, VEC><<<dim3((unsigned)(z.items * a.Hkv)), dim3(256), 0, s>>>(a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    many_join_kernel<T, DP><<<dim3((unsigned)(z.joins * a.Hkv * (BLOCK * DP / 1024))), dim3(256), 0, s>>>(a);
+    return hipGetLastError();
+}
+template <typename T, bool VEC> hipError_t launch_typed(const PagedAttnArgs &a, const Layout &z, hipStream_t s) {
+    const int dc = computed(a.Dh);
+    if (dc == 64) return launch_sized<T, 64, VEC>(a, z, s);
+    return dc == 96 ? launch_sized<T, 96, VEC>(a, z, s) : launch_sized<T, 128, VEC>(a, z, s);
+}
+
+}  // namespace
+
+size_t paged_attn_workspace(gs_dtype t, const PagedAttnArgs &a) { return layout(t, a).bytes; }
+
+hipError_t launch_paged_attn(gs_dtype t, PagedAttnArgs a, void *ws, hipStream_t s) {
+    const Layout z = layout(t, a);
+    a.rows = z.rows;
+    a.blocks = (int)z.blocks;
+    a.waves = z.waves;
+    a.least = z.least;
+    a.head = static_cast<PagedAttnHead *>(ws);
+    a.items = reinterpret_cast<PagedItem *>(a.head + 1);
+    a.joins = reinterpret_cast<PagedJoin *>(a.items + z.items);
+    a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + z.list);
+    a.part_lse = a.part + z.slots * z.rows * z.dp;
+    // j / page for j below 2^31: with 2^s >= page > 2^(s - 1) and m = ceil(2^(31 + s) / page)
+    // < 2^32, floor(j m / 2^(31 + s)) is it (m page exceeds 2^(31 + s) by less than page <= 2^s)
+    int shift = 0;
+    while (((int64_t)1 << shift) < a.page) ++shift;
+    a.page_magic = (uint32_t)((((unsigned __int128)1 << (31 + shift)) + a.page - 1) / a.page);
+    a.page_shift = shift - 1;
+    if (a.page == 1) a.page_magic = 0;
+    if (t == GS_F32) return a.vec ? launch_typed<float, true>(a, z, s) : launch_typed<float, false>(a, z, s);
+    return a.vec ? launch_typed<bf16_t, true>(a, z, s) : launch_typed<bf16_t, false>(a, z, s);
+}
+
+}  // namespace gs

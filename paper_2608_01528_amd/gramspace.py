@@ -7,7 +7,8 @@ Two layers with the C names:
 * `gs_compress`, `gs_compress_padded`, `gs_compress_partitioned`, `gs_compress_noalloc`, `gs_project`, `gs_prob2vec`, `gs_prob2vec_sparse`,
   `gs_similarity`,
   `gs_attention`, `gs_similarity_attention`, `gs_reconstruct`, `gs_bind_coords`, `gs_soft_select`, `gs_bind_restored`,
-  `gs_cross_attention`, `gs_cross_attention_grad` and `gs_sample`
+  `gs_cross_attention`, `gs_cross_attention_grad`, `gs_sample`,
+  `gs_paged_plan`, `gs_paged_store`, `gs_paged_attention` and `gs_verify`
   below take torch tensors on the current
   GPU, allocate the outputs with torch, and pass pointers, sizes and the
   current stream to the library.  They only marshal arguments: every step of
@@ -114,6 +115,18 @@ _SIGS["gs_cross_attention_grad"] = ([_vp, ctypes.c_int, _vp, ctypes.c_size_t, _v
 _SIGS["gs_sample_workspace"] = ([ctypes.c_int, _i64, _i64], ctypes.c_size_t)
 _SIGS["gs_sample"] = ([_vp, ctypes.c_int, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp],
                       ctypes.c_int)
+# gs_paged_step, gs_paged_rows, gs_paged_attn and gs_drafts likewise
+_SIGS["gs_paged_plan_workspace"] = ([_i64], ctypes.c_size_t)
+_SIGS["gs_paged_plan"] = ([_vp, _vp, ctypes.c_size_t, _vp], ctypes.c_int)
+_SIGS["gs_paged_store"] = ([_vp, ctypes.c_int, ctypes.c_int, _vp], ctypes.c_int)
+_SIGS["gs_paged_attention_workspace"] = ([_vp, ctypes.c_int], ctypes.c_size_t)
+_SIGS["gs_paged_attention"] = ([_vp, ctypes.c_int, _vp, ctypes.c_size_t, _vp], ctypes.c_int)
+_SIGS["gs_verify_workspace"] = ([_i64, _i64], ctypes.c_size_t)
+_SIGS["gs_verify"] = ([_vp, ctypes.c_int, _vp, ctypes.c_size_t, _vp], ctypes.c_int)
+_PAGED_STEP = struct.Struct("=3q4Q2qQq5Q")
+_PAGED_ROWS = struct.Struct("=5qQ" + "Q3q" * 4)
+_PAGED_ATTN = struct.Struct("=11q3Q2qd" + "Q3q" * 4 + "Q")
+_DRAFTS = struct.Struct("=3qQqQq7Q")
 _ATTN = struct.Struct("=6q3Qqd" + "Q3q" * 4 + "Q" + "Q3q" * 4)
 _SAMPLING = struct.Struct("=4Qfiff")
 
@@ -747,3 +760,169 @@ def gs_sample(S: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=
     if not (prob or kept):
         return idx
     return (idx,) + ((pr,) if prob else ()) + ((kp,) if kept else ())
+
+
+# ------------------------------------------------ serving out of a paged cache
+
+def _table(t, B: int):
+    """Address, columns and leading dimension of a page table."""
+    _here(t, "table", torch.int32)
+    if t.dim() != 2 or t.shape[0] != B:
+        raise ValueError("table must have %d rows, got %s" % (B, tuple(t.shape)))
+    width = t.shape[1]
+    if (width > 1 and t.stride(1) != 1) or (B > 1 and t.stride(0) < width):
+        raise ValueError("table must have rows of its own with unit column stride")
+    return t.data_ptr(), width, max(t.stride(0), width)
+
+
+def _rows3(t: torch.Tensor, name: str, shape, dtype):
+    """Address and strides of rows (N, heads, values), as a sequence's."""
+    if t.shape != shape:
+        raise ValueError("%s must be %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    _here(t, name, dtype)
+    s = t.stride()
+    if s[2] != 1 and shape[2] > 1:
+        raise ValueError("%s must have values of a head side by side (unit last stride)" % name)
+    return t.data_ptr(), 0, s[0], s[1]
+
+
+def _cache(Kc, Vc):
+    c = Kc.shape
+    if len(c) != 4:
+        raise ValueError("Kc and Vc must be (pages, page, Hkv, Dh)")
+    if c[1] < 1:
+        raise ValueError("pages of the cache have no positions")
+    t = _DT.get(Kc.dtype)
+    if t is None:
+        raise ValueError("Kc: unsupported dtype %s" % Kc.dtype)
+    return t, c, _seq(Kc, "Kc", c, Kc.dtype) + _seq(Vc, "Vc", c, Kc.dtype)
+
+
+def gs_paged_plan(length: torch.Tensor, add: torch.Tensor, table: torch.Tensor, free: torch.Tensor, nfree: torch.Tensor,
+                  page: int, rows: int, length_out: torch.Tensor | None = None, nfree_out: torch.Tensor | None = None,
+                  qoff_out: torch.Tensor | None = None, slots_out: torch.Tensor | None = None,
+                  added_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """Pages and slots of a step: `add` positions (int32, B; negative: taken
+    back) for requests that hold `length` (int32, B) in pages of `page`
+    positions.  `table` (int32, B x width) and the stack of free pages `free`
+    (int32) with its height `nfree` (int32, 1) are updated in place, the latter
+    only if nfree_out is nfree itself (and length if length_out is).  Returns
+    (length, nfree, qoff, slots, added): the new lengths and height, the
+    requests' first rows (int32, B + 1), the slots of `rows` rows (int64, -1
+    for none) and the positions each request got (int32, B)."""
+    i32, dev = torch.int32, table.device
+    B = length.numel()
+    length_out = length.new_empty(B) if length_out is None else length_out
+    nfree_out = nfree.new_empty(1) if nfree_out is None else nfree_out
+    qoff = torch.empty(B + 1, dtype=i32, device=dev) if qoff_out is None else qoff_out
+    slots = torch.empty(rows, dtype=torch.int64, device=dev) if slots_out is None else slots_out
+    added = torch.empty(B, dtype=i32, device=dev) if added_out is None else added_out
+    given = _PAGED_STEP.pack(B, page, rows, _per_row(length, "length", B, i32), _per_row(add, "add", B, i32),
+                             _per_row(length_out, "length_out", B, i32), *_table(table, B),
+                             _per_row(free, "free", free.numel(), i32), free.numel(),
+                             _per_row(nfree, "nfree", 1, i32), _per_row(nfree_out, "nfree_out", 1, i32),
+                             _per_row(qoff, "qoff_out", B + 1, i32), _per_row(slots, "slots_out", rows, torch.int64),
+                             _per_row(added, "added_out", B, i32))
+    L = lib()
+    ws, n, _keep = _workspace(L.gs_paged_plan_workspace(B), workspace, dev)
+    _check(L.gs_paged_plan(given, ws, n, _stream()))
+    return length_out, nfree_out, qoff, slots, added
+
+
+def gs_paged_store(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor):
+    """Rows of K and V (N, Hkv, Dh) into their slots (int64, N; negative: none)
+    of the cache Kc, Vc (pages, page, Hkv, Dh), rounded to its type."""
+    ct, c, at = _cache(Kc, Vc)
+    t = _DT.get(K.dtype)
+    if t is None:
+        raise ValueError("K: unsupported dtype %s" % K.dtype)
+    if K.dim() != 3:
+        raise ValueError("K and V must be (N, Hkv, Dh)")
+    n = K.shape[0]
+    shape = (n, c[2], c[3])
+    given = _PAGED_ROWS.pack(n, c[2], c[3], c[0], c[1], _per_row(slots, "slots", n, torch.int64),
+                             *_rows3(K, "K", shape, K.dtype), *_rows3(V, "V", shape, K.dtype), *at)
+    _check(lib().gs_paged_store(given, t, ct, _stream()))
+
+
+def gs_paged_attention(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, table: torch.Tensor, klen: torch.Tensor,
+                       qoff: torch.Tensor | None = None, max_new: int | None = None, max_len: int | None = None,
+                       window: int = 0, sinks: int = 0, scale: float | None = None, lse: bool = False,
+                       out: torch.Tensor | None = None, lse_out: torch.Tensor | None = None,
+                       workspace: torch.Tensor | None = None):
+    """Attention of the rows Q (N, Hq, Dh) to their requests' states in the
+    paged cache: request b has klen[b] (int32) states in the pages of
+    table[b], and the rows qoff[b] .. qoff[b + 1] - 1 (int32, B + 1; None: one
+    row each) at its last positions, of which each sees the states up to its
+    own (window > 0: the last `window` of them and the first `sinks`).
+    max_new, max_len: most rows and states of a request, as far as they are
+    known (N, and what the table has room for, otherwise).  scale 1 / sqrt(Dh)
+    by default.  Returns O, or (O, lse) with lse (N, Hq) fp32; rows of no
+    request are not written."""
+    t, c, at = _cache(Kc, Vc)
+    q = Q.shape
+    if len(q) != 3 or q[2] != c[3]:
+        raise ValueError("Q must be (N, Hq, %d), got %s" % (c[3], tuple(q)))
+    N, Hq, Dh = q
+    B = klen.numel()
+    tab, width, ldt = _table(table, B)
+    if max_new is None:
+        max_new = N if qoff is not None else 1
+    room = width * c[1]
+    max_len = min(room, 0x7fffffff - 256) if max_len is None else max_len
+    if out is None:
+        out = Q.new_empty(q)
+    if lse_out is None and lse:
+        lse_out = Q.new_empty((N, Hq), dtype=torch.float32)
+    lp = 0
+    if lse_out is not None:
+        lp = _per_row(lse_out, "lse", N * Hq, torch.float32)
+        if lse_out.shape != (N, Hq):
+            raise ValueError("lse must be (%d, %d)" % (N, Hq))
+    given = _PAGED_ATTN.pack(B, N, max_new, max_len, Hq, c[2], Dh, c[0], c[1], width, ldt, tab,
+                             _per_row(klen, "klen", B, torch.int32), _per_row(qoff, "qoff", B + 1, torch.int32),
+                             window, sinks, float(max(Dh, 1) ** -0.5 if scale is None else scale),
+                             *_rows3(Q, "Q", q, Kc.dtype), *at, *_rows3(out, "out", q, Kc.dtype), lp)
+    L = lib()
+    ws, n, _keep = _workspace(L.gs_paged_attention_workspace(given, t), workspace, Q.device)
+    _check(L.gs_paged_attention(given, t, ws, n, _stream()))
+    return (out, lse_out) if lse else out
+
+
+def gs_verify(P: torch.Tensor, drafted: torch.Tensor, u: torch.Tensor, v: torch.Tensor, qoff: torch.Tensor,
+              Q: torch.Tensor | None = None, entries: bool = False, accepted_out: torch.Tensor | None = None,
+              entry_out: torch.Tensor | None = None, entries_out: torch.Tensor | None = None,
+              workspace: torch.Tensor | None = None):
+    """Drafted entries taken or refused: the rows qoff[b] .. qoff[b + 1] - 1
+    (int32, B + 1) of the probabilities P (N x M) are request b's, drafted
+    (int32, N) the entry drafted to follow each row (the last row's is not
+    read), Q (N x M) the drafting model's probabilities (None: certain), u
+    (fp32, N) and v (fp32, B) random numbers in [0, 1).  Returns (accepted,
+    entry), int32 of B: the drafts taken and the entry drawn after them; with
+    `entries` also int32 of N, each request's new entries from its first row
+    on and -1 behind them (rows of no request are not written)."""
+    pt, ldp = _mat(P, "P")
+    _here(P, "P")
+    N, M = P.shape
+    qp, ldq = 0, M
+    if Q is not None:
+        _shape(Q, "Q", N, M)
+        _here(Q, "Q", P.dtype)
+        _, ldq = _mat(Q, "Q")
+        qp = Q.data_ptr()
+    for x, name in ((P, "P"), (Q, "Q")):
+        if x is not None and N > 1 and x.stride(0) < M:
+            raise ValueError("%s must have rows of its own" % name)
+    i32, dev = torch.int32, P.device
+    B = v.numel()
+    acc = torch.empty(B, dtype=i32, device=dev) if accepted_out is None else accepted_out
+    ent = torch.empty(B, dtype=i32, device=dev) if entry_out is None else entry_out
+    every = torch.empty(N, dtype=i32, device=dev) if entries and entries_out is None else entries_out
+    given = _DRAFTS.pack(B, N, M, P.data_ptr(), ldp, qp, ldq, _per_row(drafted, "drafted", N, i32),
+                         _per_row(u, "u", N, torch.float32), _per_row(v, "v", B, torch.float32),
+                         _per_row(qoff, "qoff", B + 1, i32), _per_row(acc, "accepted_out", B, i32),
+                         _per_row(ent, "entry_out", B, i32), _per_row(every, "entries_out", N, i32))
+    L = lib()
+    ws, n, _keep = _workspace(L.gs_verify_workspace(B, M), workspace, dev)
+    _check(L.gs_verify(given, pt, ws, n, _stream()))
+    return (acc, ent, every) if entries else (acc, ent)

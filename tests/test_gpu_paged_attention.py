@@ -1,0 +1,319 @@
+"""gs_paged_attention against 64 bits, row by row, within attn_util's bounds."""
+import random
+
+import numpy as np
+import pytest
+import torch
+
+import attn_util
+import paged_util
+from paper_2608_01528_amd import gramspace as gs
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+i32 = torch.int32
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def cache(seed, dtype, klen, page, Hkv, Dh, spare=3, fill=float("nan"), pad=0):
+    """A cache whose pages lie in any order; places that hold no state, and
+    pages of no request, hold `fill`.  Returns (Kc, Vc, table)."""
+    g = torch.Generator().manual_seed(seed)
+    held = [-(-max(k, 0) // page) for k in klen]
+    pages = sum(held) + spare
+    order = torch.randperm(pages, generator=g).tolist()
+    width = max(held + [1]) + 1
+    Kc, Vc = (torch.full((pages, page, Hkv, Dh + pad), fill, dtype=dtype) for _ in range(2))
+    table = torch.full((len(klen), width), -1, dtype=i32)
+    for b, k in enumerate(klen):
+        for i in range(held[b]):
+            p = order.pop()
+            table[b, i] = p
+            n = min(page, k - i * page)
+            for c in (Kc, Vc):
+                c[p, :n, :, :Dh] = torch.randn(n, Hkv, Dh, generator=g).to(dtype)
+    return Kc.to(DEV)[..., :Dh], Vc.to(DEV)[..., :Dh], table.to(DEV)
+
+
+def ints(x):
+    return torch.tensor(x, dtype=i32, device=DEV)
+
+
+def check(Q, Kc, Vc, table, klen, qoff=None, **kw):
+    # rows that are not written keep what they hold
+    out, lse = torch.full_like(Q, 7.0), torch.full(Q.shape[:2], 7.0, device=DEV)
+    gs.gs_paged_attention(Q, Kc, Vc, table, klen, qoff=qoff, out=out, lse_out=lse, **kw)
+    ref, written = paged_util.attention(Q, Kc, Vc, table, klen, qoff, **kw)
+    w = written.to(DEV)
+    attn_util.check(out[w], {"O": tuple(x[written] for x in ref["O"])}, "O")
+    attn_util.check(lse[w], {"lse": tuple(x[written] for x in ref["lse"])}, "lse")
+    assert (out[~w] == 7).all() and (lse[~w] == 7).all()
+    return out, lse
+
+
+def offsets(n, lead=0):
+    return ints([lead] + (lead + np.cumsum(n)).tolist())
+
+
+def problem(seed, dtype, n, klen, page, Hq, Hkv, Dh, lead=0, tail=0, **kw):
+    Kc, Vc, table = cache(seed, dtype, klen, page, Hkv, Dh, **kw)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed + 1)
+    Q = torch.randn(lead + sum(n) + tail, Hq, Dh, generator=g, device=DEV).to(dtype)
+    return Q, Kc, Vc, table, ints(klen), offsets(n, lead)
+
+
+# lengths around tiles of 32 and 64 and pages, from none on
+LENGTHS = [1, 0, 5, 31, 32, 33, 64, 65, 127, 200, 300]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("page", [1, 5, 16, 24, 32, 64, 100])
+def test_tokens(dtype, page):
+    """One row a request, without offsets."""
+    Q, Kc, Vc, table, klen, _ = problem(page, dtype, [1] * len(LENGTHS), LENGTHS, page, 8, 2, 64)
+    check(Q, Kc, Vc, table, klen)
+    check(Q, Kc, Vc, table, klen, max_len=max(LENGTHS))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("Hq,Hkv,Dh", [(1, 1, 1), (3, 3, 8), (8, 1, 32), (12, 4, 40), (5, 1, 65), (6, 2, 80), (4, 2, 96),
+                                       (8, 8, 100), (32, 8, 128), (16, 1, 128), (33, 1, 64), (40, 1, 24)])
+def test_heads(dtype, Hq, Hkv, Dh):
+    n, k = [1, 2, 0, 3, 1], [70, 33, 10, 130, 1]
+    check(*problem(Hq + Dh, dtype, n, k, 16, Hq, Hkv, Dh))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,k", [
+    ([2, 5, 8, 4], [2, 40, 8, 100]),                # drafts, some on an empty history
+    ([33, 1, 70, 0, 128, 129], [33, 90, 200, 10, 128, 400]),
+    ([300], [301]), ([65, 65], [65, 65]),
+])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (7, 3), (40, 4), (64, 70), (100, 1)])
+def test_windows(dtype, n, k, window, sinks):
+    check(*problem(sum(n), dtype, n, k, 24, 4, 2, 64, lead=2, tail=3), window=window, sinks=sinks)
+
+
+def test_many_requests():
+    """More requests than a wave looks over at once, and than 64 of its lanes' shares."""
+    for B in (65, 700, 4200):
+        rng = random.Random(B)
+        n = [rng.choice([0, 1, 1, 1, 2]) for _ in range(B)]
+        k = [rng.choice([0, 1, 9, 40, 70]) + a for a in n]
+        check(*problem(B, BF16, n, k, 16, 2, 1, 32))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_long_history_in_parts(dtype):
+    """One request's states shared out to many waves, and to many work-groups."""
+    Q, Kc, Vc, table, klen, qoff = problem(2, dtype, [1, 2], [40000, 17], 64, 4, 1, 64)
+    check(Q, Kc, Vc, table, klen, qoff)
+    check(Q, Kc, Vc, table, klen, qoff, window=20000, sinks=100)
+    Q, Kc, Vc, table, klen, qoff = problem(3, dtype, [20, 1], [9001, 5000], 32, 4, 2, 64)
+    check(Q, Kc, Vc, table, klen, qoff)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [[1, 1, 1], [4, 3, 5], [50, 1, 40]])
+def test_states_that_are_not_finite(dtype, n):
+    """NaN and infinities in states change the rows that see them and no others;
+    so do queries that are not finite."""
+    k = [100, 60, 90]
+    for window, sinks in ((0, 0), (30, 2)):
+        Q, Kc, Vc, table, klen, qoff = problem(11, dtype, n, k, 16, 4, 2, 64)
+        clean = gs.gs_paged_attention(Q, Kc, Vc, table, klen, qoff, window=window, sinks=sinks, lse=True)
+        for where in range(2):
+            for value in (float("nan"), float("inf"), -float("inf")):
+                C = [Kc.clone(), Vc.clone()]
+                spots = []
+                for b in range(3):
+                    for j in {k[b] - 1, max(k[b] - 3, 0), k[b] // 2, 1}:
+                        C[where][int(table[b, j // 16]), j % 16, 1, 5] = value
+                        spots.append((b, j))
+                O, lse = gs.gs_paged_attention(Q, *C, table, klen, qoff, window=window, sinks=sinks, lse=True)
+                off = qoff.tolist()
+                for b in range(3):
+                    for i in range(n[b]):
+                        p = k[b] - n[b] + i
+                        sees = set(paged_util.seen(p, k[b], window, sinks).tolist())
+                        hit = [j for bb, j in spots if bb == b and j in sees]
+                        r = off[b] + i
+                        assert torch.equal(O[r, :2], clean[0][r, :2]) and torch.equal(lse[r, :2], clean[1][r, :2])
+                        if not hit:
+                            assert torch.equal(O[r, 2:], clean[0][r, 2:]), (b, i, value)
+                            assert torch.equal(lse[r, 2:], clean[1][r, 2:])
+                        elif where == 1:        # a value: its own column alone
+                            rest = [d for d in range(64) if d != 5]
+                            assert torch.equal(O[r, 2:][:, rest], clean[0][r, 2:][:, rest])
+                            assert torch.equal(lse[r], clean[1][r])
+                            got = O[r, 2:, 5]
+                            assert got.isnan().all() if value != value else (got == value).all()
+                        elif value != value:
+                            assert O[r, 2:].isnan().all() and lse[r, 2:].isnan().all()
+        bad = Q.clone()
+        bad[0, 3, 7] = float("nan")
+        O, lse = gs.gs_paged_attention(bad, Kc, Vc, table, klen, qoff, window=window, sinks=sinks, lse=True)
+        assert O[0, 3].isnan().all()
+        same = torch.ones(O.shape[:2], dtype=torch.bool, device=DEV)
+        same[0, 3] = False
+        assert torch.equal(O[same], clean[0][same]) and torch.equal(lse[same], clean[1][same])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [[1, 1, 1], [40, 3, 30]])
+def test_pages_that_are_not_there(dtype, n):
+    """Page numbers out of range count as states that are not there; pages
+    behind a window are not looked at."""
+    Q, Kc, Vc, table, klen, qoff = problem(5, dtype, n, [100, 60, 90], 16, 4, 2, 40)
+    bad = table.clone()
+    bad[0, 1], bad[0, 3], bad[1, 0], bad[2, :] = -1, Kc.shape[0], 2**31 - 1, -2**31
+    out, lse = check(Q, Kc, Vc, bad, klen, qoff)
+    assert (out[qoff[2]:] == 0).all() and (lse[qoff[2]:] == -float("inf")).all()
+    evicted = table.clone()
+    for b, (k, a) in enumerate(zip([100, 60, 90], n)):
+        gone = (k - a - 20 + 1) // 16       # pages wholly before the first row's window, behind the sinks' page
+        evicted[b, 1: max(gone, 1)] = -5
+    x = gs.gs_paged_attention(Q, Kc, Vc, table, klen, qoff, window=20, sinks=3, lse=True)
+    y = gs.gs_paged_attention(Q, Kc, Vc, evicted, klen, qoff, window=20, sinks=3, lse=True)
+    assert torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
+    # a cache without pages
+    none = Kc[:0]
+    O, lse = gs.gs_paged_attention(Q, none, none, table, klen, qoff, lse=True)
+    assert (O == 0).all() and (lse == -float("inf")).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_numbers_out_of_range(dtype):
+    """Lengths below 0 and above max_len, offsets beyond the rows and falling,
+    more rows than max_new, more rows than states."""
+    Q, Kc, Vc, table, klen, _ = problem(6, dtype, [3, 9, 4], [50, 80, 33], 8, 4, 2, 64)
+    for lens, off, kw in (([-3, 80, 33], [0, 3, 12, 16], {}), ([50, 10**9, 33], [0, 3, 12, 16], {"max_len": 80}),
+                          ([50, 80, 33], [-7, 3, 2, 99], {}), ([50, 80, 33], [0, 3, 12, 16], {"max_new": 4}),
+                          ([2, 5, 0], [0, 3, 12, 16], {}), ([50, 80, 33], [1, 1, 1, 1], {}),
+                          ([50, 80, 33], [0, 3, 12, 16], {"max_new": 2, "window": 9, "sinks": 1})):
+        check(Q, Kc, Vc, table, ints(lens), ints(off), **kw)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [[1] * 4, [40, 2, 1, 33]])
+def test_strides(dtype, n):
+    """Rows inside wider ones, heads before places, tables inside wider ones,
+    and tensors whose rows lie on no boundary of 16 bytes."""
+    k = [77, 40, 10, 64]
+    for pad in (0, 1, 8):
+        Q, Kc, Vc, table, klen, qoff = problem(9, dtype, n, k, 16, 6, 2, 64, pad=pad)
+        Kt = Kc.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)
+        wide = torch.randn(Q.shape[0], 3, 6, 64 + pad, device=DEV).to(dtype)
+        T = torch.full((4, table.shape[1] + 5), 10**6, dtype=i32, device=DEV)
+        T[:, 2: 2 + table.shape[1]] = table
+        q = wide[:, 1, :, :64]
+        ref, _ = paged_util.attention(q, Kc, Vc, table, klen, qoff)
+        out = torch.full((Q.shape[0], 6, 130), 3.0, dtype=dtype, device=DEV)
+        for keys in (Kc, Kt):
+            gs.gs_paged_attention(q, keys, Vc, T[:, 2: 2 + table.shape[1]], klen, qoff, out=out[..., pad: pad + 64])
+            attn_util.check(out[..., pad: pad + 64], ref, "O")
+        assert (out[..., :pad] == 3).all() and (out[..., pad + 64:] == 3).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("scale", [-0.3, 1e-30, 3.0])
+def test_scales(dtype, scale):
+    check(*problem(4, dtype, [1, 2, 40], [90, 33, 70], 16, 4, 2, 64), scale=scale)
+
+
+def test_scores_that_rise_and_fall():
+    """The running maximum moves by hundreds, in both directions."""
+    for n in ([1, 3], [40, 36]):
+        Q, Kc, Vc, table, klen, qoff = problem(8, BF16, n, [700, 500], 32, 4, 2, 64)
+        Q = torch.ones_like(Q)
+        for b, k in enumerate([700, 500]):
+            for j in range(k):
+                Kc[int(table[b, j // 32]), j % 32] *= 0.02
+                Kc[int(table[b, j // 32]), j % 32] += 3.0 * (j if b else 350 - abs(j - 350)) / 100
+        check(Q, Kc, Vc, table, klen, qoff)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_empty_batches(dtype):
+    Q, Kc, Vc, table, klen, qoff = problem(1, dtype, [2, 1], [9, 4], 4, 2, 1, 32)
+    assert gs.gs_paged_attention(Q[:0], Kc, Vc, table, klen, ints([0, 0, 0])).shape == (0, 2, 32)
+    assert gs.gs_paged_attention(Q[:0], Kc, Vc, table[:0], klen[:0], ints([0])).shape == (0, 2, 32)
+    out = torch.full_like(Q, 5.0)
+    gs.gs_paged_attention(Q, Kc, Vc, table, klen, qoff, max_new=0, out=out)
+    assert (out == 5).all()
+    O, lse = gs.gs_paged_attention(Q, Kc, Vc, table, klen, qoff, max_len=0, lse=True)
+    assert (O == 0).all() and (lse == -float("inf")).all()
+
+
+def test_far_pages():
+    """Pages more than 2^32 values from the first."""
+    pages, page, Hkv, Dh = 150000, 32, 8, 128
+    if torch.cuda.mem_get_info()[0] < 5 * pages * page * Hkv * Dh:
+        pytest.skip("not enough memory")
+    Kc, Vc = (torch.empty(pages, page, Hkv, Dh, dtype=BF16, device=DEV) for _ in range(2))
+    assert Kc.numel() > 2**32
+    ids = [pages - 1, 7, 2**31 // (page * Hkv * Dh) + 1, pages // 2, pages - 2]
+    for c in (Kc, Vc):
+        c[ids] = torch.randn(len(ids), page, Hkv, Dh, device=DEV).to(BF16)
+    table, klen = ints([ids]), ints([page * len(ids) - 3])
+    small = [c[ids] for c in (Kc, Vc)]
+    for n in (1, 3, 50):
+        Q = torch.randn(n, 8, Dh, device=DEV).to(BF16)
+        q = ints([0, n])
+        x = gs.gs_paged_attention(Q, Kc, Vc, table, klen, q, lse=True)
+        y = gs.gs_paged_attention(Q, *small, ints([list(range(len(ids)))]), klen, q, lse=True)
+        assert torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
+
+
+@pytest.mark.parametrize("n", [[1] * 6, [5, 1, 0, 3, 2, 8], [200, 1, 90, 0, 33, 2]])
+def test_captured_with_other_lengths(n):
+    """A captured call replayed for other lengths, tables and rows gives what an
+    eager one gives, bit for bit; two at once on streams of their own as well."""
+    B, page = len(n), 16
+    sets = []
+    for s in range(3):
+        rng = random.Random(s)
+        k = [a + rng.choice([0, 40, 900]) for a in n]
+        m = list(n)
+        rng.shuffle(m)
+        k = [max(x, y) for x, y in zip(k, m)]
+        sets.append((m, k))
+    Kc, Vc, _ = cache(1, BF16, [1200] * B, page, 2, 64, fill=0.5)
+    table = torch.arange(B * 70, device=DEV, dtype=i32).view(B, 70) % Kc.shape[0]
+    Q = torch.randn(sum(n), 8, 64, device=DEV).to(BF16)
+    klen, qoff = ints(sets[0][1]), offsets(sets[0][0])
+    call = lambda **kw: gs.gs_paged_attention(Q, Kc, Vc, table, klen, qoff, max_new=max(n), max_len=1100, lse=True, **kw)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = call()
+    for m, k in sets + sets[::-1]:
+        klen.copy_(ints(k))
+        qoff.copy_(offsets(m))
+        Q.normal_()
+        g.replay()
+        eager = call()
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], eager[0]) and torch.equal(out[1], eager[1])
+    side = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(4):
+        got = []
+        for s in side:
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                got.append(call())
+        torch.cuda.synchronize()
+        for o in got:
+            assert torch.equal(o[0], eager[0]) and torch.equal(o[1], eager[1])
+
+
+def test_contents_of_the_workspace_do_not_matter():
+    for n in ([1, 1, 1], [60, 1, 40]):
+        p = problem(3, BF16, n, [5000, 100, 700], 16, 8, 2, 128)
+        want = gs.gs_paged_attention(*p, lse=True)
+        for fill in (0, 255):
+            ws = torch.full((1 << 28,), fill, dtype=torch.uint8, device=DEV)
+            got = gs.gs_paged_attention(*p, lse=True, workspace=ws)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

@@ -1,0 +1,201 @@
+"""gs_paged_plan and gs_paged_store against a list of pages and copies on the host."""
+import random
+
+import numpy as np
+import pytest
+import torch
+
+import paged_util
+from paper_2608_01528_amd import gramspace as gs
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+i32 = torch.int32
+
+
+class State:
+    """Requests that hold pages of a shuffled cache."""
+
+    def __init__(self, rng, B, page, width, free_share=0.5, length=None, spare=0):
+        self.page, self.width = page, width
+        self.length = [rng.randint(0, page * width) for _ in range(B)] if length is None else list(length)
+        held = [-(-min(max(x, 0), page * width) // page) for x in self.length]
+        pages = sum(held) + int(free_share * B * width) + 1
+        order = list(range(pages))
+        rng.shuffle(order)
+        self.table = np.full((B, width), -7, np.int32)
+        for b, h in enumerate(held):
+            for k in range(h):
+                self.table[b, k] = order.pop()
+        self.nfree = len(order)
+        self.free = np.array(order + [-9] * (sum(held) + spare), np.int32)
+
+    def tensors(self):
+        t = lambda x: torch.tensor(x, dtype=i32, device=DEV)  # noqa: E731
+        return t(self.length), torch.from_numpy(self.table).to(DEV), torch.from_numpy(self.free).to(DEV), t([self.nfree])
+
+
+def agree(got, want, table, free):
+    length, nfree, qoff, slots, added = got
+    assert length.tolist() == want[0]
+    assert nfree.tolist() == [want[1]]
+    assert qoff.tolist() == want[2]
+    assert np.array_equal(slots.cpu().numpy(), want[3])
+    assert added.tolist() == want[4]
+    assert np.array_equal(table.cpu().numpy(), want[5])
+    assert np.array_equal(free.cpu().numpy(), want[6])
+
+
+def adds(rng, B, kind, page):
+    if kind == "step":
+        return [rng.choice([1, 1, 1, 1, 0, 2, 5, -1, -3, -10**6]) for _ in range(B)]
+    if kind == "prompts":
+        return [rng.randint(0, 4 * page + 3) for _ in range(B)]
+    return [-rng.randint(0, 3 * page) for _ in range(B)]
+
+
+@pytest.mark.parametrize("kind", ["step", "prompts", "back"])
+@pytest.mark.parametrize("B,page,width", [(1, 16, 4), (5, 1, 9), (64, 16, 12), (200, 24, 3), (1024, 5, 6), (1025, 16, 3),
+                                          (2500, 3, 5), (3, 100, 50000)])
+def test_plan(B, page, width, kind):
+    rng = random.Random(B * 7 + page)
+    s = State(rng, B, page, width)
+    add = adds(rng, B, kind, page)
+    rows = max(0, sum(max(x, 0) for x in add) + rng.choice([-3, 0, 5]))
+    length, table, free, nfree = s.tensors()
+    got = gs.gs_paged_plan(length, torch.tensor(add, dtype=i32, device=DEV), table, free, nfree, page=page, rows=rows)
+    agree(got, paged_util.plan(s.length, add, s.table, s.free, s.nfree, page, rows), table, free)
+    assert length.tolist() == s.length and nfree.tolist() == [s.nfree]         # inputs as they were
+
+
+@pytest.mark.parametrize("B", [40, 1500])
+@pytest.mark.parametrize("share", [0.0, 0.05, 0.2])
+def test_too_few_pages(B, share):
+    rng = random.Random(B)
+    s = State(rng, B, 8, 6, free_share=share)
+    add = [rng.choice([1, 9, 20, -9, 0]) for _ in range(B)]
+    rows = sum(max(x, 0) for x in add)
+    length, table, free, nfree = s.tensors()
+    want = paged_util.plan(s.length, add, s.table, s.free, s.nfree, 8, rows)
+    if share < 0.1:
+        assert any(a > 0 and g == 0 for a, g in zip(add, want[4]))
+    got = gs.gs_paged_plan(length, torch.tensor(add, dtype=i32, device=DEV), table, free, nfree, page=8, rows=rows)
+    agree(got, want, table, free)
+
+
+def test_numbers_out_of_range():
+    """Lengths below 0 and beyond the table, heights beyond the list, amounts at
+    the ends of their type, a free list without room, negative pages."""
+    rng = random.Random(1)
+    big, low = 2**31 - 1, -2**31
+    for length, add in (([-5, 999, 10, 3, 0, 40], [3, 1, low, big, big, -2]), ([0, 40, 40, 1, 1, 1], [low, low, 0, big, 1, 1])):
+        for nfree in (-4, 0, 3, 10**9):
+            s = State(rng, 6, 4, 10, length=length)
+            s.table[5, 0] = -3
+            s.free = s.free[: s.nfree + 2]
+            ln, table, free, _ = s.tensors()
+            n = torch.tensor([nfree], dtype=i32, device=DEV)
+            got = gs.gs_paged_plan(ln, torch.tensor(add, dtype=i32, device=DEV), table, free, n, page=4, rows=25)
+            agree(got, paged_util.plan(length, add, s.table, s.free, nfree, 4, 25), table, free)
+
+
+def test_no_requests_and_no_rows():
+    e = lambda *n: torch.empty(*n, dtype=i32, device=DEV)  # noqa: E731
+    nfree = torch.tensor([2], dtype=i32, device=DEV)
+    free = torch.tensor([4, 5], dtype=i32, device=DEV)
+    out = gs.gs_paged_plan(e(0), e(0), e(0, 3), free, nfree, page=4, rows=5, nfree_out=nfree)
+    assert out[2].tolist() == [0] and out[3].tolist() == [-1] * 5 and nfree.tolist() == [2]
+    one = torch.tensor([1], dtype=i32, device=DEV)
+    table = torch.full((1, 3), -1, dtype=i32, device=DEV)
+    out = gs.gs_paged_plan(one, one, table, free, nfree, page=4, rows=0)
+    assert out[4].tolist() == [0] and out[2].tolist() == [0, 1] and out[0].tolist() == [1]
+    # a table without columns
+    out = gs.gs_paged_plan(one * 0, one, e(1, 0), free, nfree, page=4, rows=2)
+    assert out[4].tolist() == [0] and out[3].tolist() == [-1, -1]
+
+
+@pytest.mark.parametrize("B", [30, 1300])
+def test_captured_steps_in_place(B):
+    """Lengths, table and free list carried from replay to replay."""
+    rng = random.Random(3)
+    s = State(rng, B, 4, 8, length=[rng.randint(0, 6) for _ in range(B)])
+    length, table, free, nfree = s.tensors()
+    add = torch.zeros(B, dtype=i32, device=DEV)
+    rows = 4 * B
+    keep = [torch.empty(B + 1, dtype=i32, device=DEV), torch.empty(rows, dtype=torch.int64, device=DEV),
+            torch.empty(B, dtype=i32, device=DEV)]
+    ws = torch.empty(gs.lib().gs_paged_plan_workspace(B), dtype=torch.uint8, device=DEV)
+    step = lambda: gs.gs_paged_plan(length, add, table, free, nfree, page=4, rows=rows, length_out=length,  # noqa: E731
+                                    nfree_out=nfree, qoff_out=keep[0], slots_out=keep[1], added_out=keep[2], workspace=ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    lens, tab, fr, n = s.length, s.table, s.free, s.nfree
+    for i in range(5):
+        amounts = [rng.choice([1, 1, 3, 0, -2, -100]) for _ in range(B)]
+        add.copy_(torch.tensor(amounts, dtype=i32))
+        g.replay()
+        torch.cuda.synchronize()
+        want = paged_util.plan(lens, amounts, tab, fr, n, 4, rows)
+        agree((length, nfree, *keep), want, table, free)
+        lens, n, tab, fr = want[0], want[1], want[5], want[6]
+
+
+# ------------------------------------------------------------------ store
+
+@pytest.mark.parametrize("dt,ct", [(a, b) for a in (torch.float32, torch.bfloat16) for b in (torch.float32, torch.bfloat16)])
+@pytest.mark.parametrize("N,Hkv,Dh,page", [(1, 1, 1, 1), (37, 3, 40, 5), (200, 2, 128, 16), (65, 5, 7, 24), (9, 1, 200, 3)])
+def test_store(dt, ct, N, Hkv, Dh, page):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(N)
+    pages = N // page + 4
+    K, V = (torch.randn(N, Hkv, Dh, generator=g, device=DEV).to(dt) for _ in range(2))
+    Kc, Vc = (torch.randn(pages, page, Hkv, Dh, generator=g, device=DEV).to(ct) for _ in range(2))
+    slots = torch.randperm(pages * page, generator=g, device=DEV)[:N]
+    slots[::7] = torch.tensor([-1, pages * page, 2**62, -2**63], device=DEV).repeat(N)[: slots[::7].numel()]
+    want = []
+    for c, x in ((Kc, K), (Vc, V)):
+        w = c.clone().view(-1, Hkv, Dh)
+        ok = (slots >= 0) & (slots < pages * page)
+        w[slots[ok]] = x[ok].to(ct)
+        want.append(w.view_as(c))
+    gs.gs_paged_store(K, V, slots, Kc, Vc)
+    assert torch.equal(Kc, want[0]) and torch.equal(Vc, want[1])
+
+
+def test_store_strides_and_special_values():
+    """Rows inside wider ones, heads before places, values that are not finite
+    kept bit for bit."""
+    N, Hkv, Dh, page, pages = 50, 2, 24, 8, 9
+    wide = torch.randn(N, Hkv, 3 * Dh, device=DEV)
+    wide[3, 0, Dh], wide[4, 1, Dh + 1], wide[5, 0, Dh + 2] = float("inf"), -float("inf"), float("nan")
+    K, V = wide[:, :, Dh: 2 * Dh], wide.flip(0)[:, :, Dh: 2 * Dh]
+    both = torch.zeros(pages, Hkv, page, 2 * Dh + 3, device=DEV)
+    Kc = both[..., :Dh].permute(0, 2, 1, 3)
+    slots = torch.randperm(pages * page, device=DEV)[:N]
+    Vs = torch.zeros(pages, Hkv, page, Dh + 2, device=DEV)[..., 1: Dh + 1].permute(0, 2, 1, 3)
+    gs.gs_paged_store(K, V, slots, Kc, Vs)
+    at = lambda c: c[slots // page, slots % page]  # noqa: E731
+    assert torch.equal(at(Kc).view(torch.int32), K.contiguous().view(torch.int32))
+    assert torch.equal(at(Vs).view(torch.int32), V.contiguous().view(torch.int32))
+    assert both[..., Dh:].abs().sum() == 0
+
+
+def test_store_far_slots():
+    """A cache of more than 2^32 values."""
+    pages, page, Hkv, Dh = 1 << 13, 64, 8, 1040
+    assert pages * page * Hkv * Dh > 2**32
+    if torch.cuda.mem_get_info()[0] < 3 * pages * page * Hkv * Dh * 2:
+        pytest.skip("not enough memory")
+    Kc, Vc = (torch.zeros(pages, page, Hkv, Dh, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    K, V = (torch.randn(4, Hkv, Dh, device=DEV).to(torch.bfloat16) for _ in range(2))
+    slots = torch.tensor([0, pages * page - 1, 2**31 // (Hkv * Dh), pages * page // 2 + 3], device=DEV)
+    gs.gs_paged_store(K, V, slots, Kc, Vc)
+    for c, x in ((Kc, K), (Vc, V)):
+        assert torch.equal(c.view(-1, Hkv, Dh)[slots], x)
+        assert int((c.view(-1, Hkv * Dh)[:, 0] != 0).sum()) == 4
