@@ -118,10 +118,9 @@ template <typename T, int DP, int BN, int NT, bool VEC> struct PagedLoad {
         for (int q = 0; q < N; ++q)
             if (!((live >> (t / CPR + q * RPI)) & 1)) v[q] = u4v{0, 0, 0, 0};
     }
-    // zeros in place of values that are not finite; their rows marked in *rows (the
-    // wave's own, in LDS)
-    __device__ __forceinline__ void finite(unsigned long long *rows, int t) {
-        *rows = 0;
+    // Zeros in place of values that are not finite; says whether there were any.
+    __device__ __forceinline__ bool finite() {
+        bool any = false;
 #pragma unroll
         for (int q = 0; q < N; ++q) {
             bool bad = false;
@@ -138,8 +137,9 @@ template <typename T, int DP, int BN, int NT, bool VEC> struct PagedLoad {
                     bad |= lo || hi;
                 }
             }
-            if (bad) atomicOr(rows, 1ull << (t / CPR + q * RPI));
+            any |= bad;
         }
+        return any;
     }
 };
 
@@ -163,10 +163,13 @@ template <typename T, int NJ> __device__ __forceinline__ void add_not_finite(f16
 // tiles x0 .. x1 - 1.  Writes O and lse, or, with `part`, the rows' results of
 // these tiles there.
 template <typename T, int DC, int NW, int BN, bool VEC>
-__device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, unsigned long long *marks, int b, int hk, const Rows &r, int m0, int x0, int x1,
+__device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, int *marks, int b, int hk, const Rows &r, int m0, int x0, int x1,
                                      float *part, float *part_lse) {
     constexpr int DP = padded(DC), PER = Op<T>::PER, NS = DC / (2 * PER), NJ = DC / 32, NT = 64 * NW;
     constexpr int TILE = BN * DP * sizeof(T);
+    // A wave on its own has read its tile before it writes the next one there: its
+    // accesses to LDS take place in order.
+    constexpr int BUFFERS = NW == 1 ? 1 : 2;
     const int t = threadIdx.x % NT, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
     const int all = r.count * a.G, mw = m0 + 32 * w, m = mw + (l & 31);
     const bool on = m < all, wave_on = mw < all;
@@ -208,15 +211,17 @@ __device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, unsigned
         return on == ALL_LIVE<BN> && p >= j0 + BN - 1 && (!a.window || (int64_t)q - a.window < j0 || j0 + BN <= a.sinks);
     };
     // Rows of the block see different states of the tile: a product takes 0 inf and 0
-    // NaN for NaN, so that values which are not finite are kept out of it.
+    // NaN for NaN, so values that are not finite are kept out of it, and added at
+    // the end to the rows that see them.
     auto differ = [&](uint64_t on, int j0) { return i0 != i1 && !seen_by(on, j0, p0 + i0, p0 + i1); };
     auto stash = [&](char *kt, int buffer, uint64_t on, int j0) {
         if (on != ALL_LIVE<BN>) vr.clean(on, t);
-        if (differ(on, j0)) vr.finite(marks + NW * buffer + w, t);
+        if (differ(on, j0)) marks[NW * buffer + w] = __any(vr.finite());
         kr.stash(kt, t);
         vr.stash(kt + TILE, t);
     };
     int buffer = 0;             // the tile in use: K, then V
+    int left_out = 0;           // some tile held values that were kept out
     if (x0 < x1) {
         keys.ahead(a, view, view.start(x0));
         live = fetch();
@@ -285,24 +290,33 @@ __device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, unsigned
 #pragma unroll
                     for (int j = 0; j < NJ; ++j) o[j] = Op<T>::mma(col_frag<T, DP>(vt, 32 * n, s, j, l), pf, o[j]);
                 }
-            if (differ(live, j0)) {
-                unsigned long long rest = 0;
-#pragma unroll
-                for (int v = 0; v < NW; ++v) rest |= marks[NW * buffer + v];
-                for (; rest; rest &= rest - 1) {
-                    const int k = __ffsll(rest) - 1, j = j0 + k, g = j / a.page;
-                    const T *const from = V + keys.table[g] * a.v.b + (j - g * a.page) * a.v.l;
-                    if ((seen >> k) & 1) add_not_finite<T, NJ>(o, from, a.Dh, l);
-                }
-            }
         }
-        buffer ^= 1;
+        if (differ(live, j0)) {
+#pragma unroll
+            for (int v = 0; v < NW; ++v) left_out |= __builtin_amdgcn_readfirstlane(marks[NW * buffer + v]);
+        }
+        if (BUFFERS == 2) buffer ^= 1;
         live = next_live;
         if (x + 1 < x1) {
             stash(lds + buffer * 2 * TILE, buffer, live, view.start(x + 1));
             if (x + 2 < x1) {
                 next_live = fetch();
                 if (x + 3 < x1) keys.ahead(a, view, view.start(x + 3));
+            }
+        }
+    }
+    if (left_out) {             // they are added now, to the rows that see them
+        for (int x = x0; x < x1; ++x) {
+            const int j0 = view.start(x);
+            int32_t page, place;
+            keys.ahead(a, view, j0);
+            const uint64_t there = keys.take(a, &page, &place);
+            if (!differ(there, j0)) continue;
+            for (uint64_t rest = there; rest; rest &= rest - 1) {
+                const int k = __ffsll((unsigned long long)rest) - 1, j = j0 + k;
+                const int32_t g = __builtin_amdgcn_readlane(page, k), i = __builtin_amdgcn_readlane(place, k);
+                const bool sees = j <= pos && (!a.window || pos - j < a.window || j < a.sinks);
+                if (sees) add_not_finite<T, NJ>(o, V + g * a.v.b + i * a.v.l, a.Dh, l);
             }
         }
     }
@@ -339,6 +353,12 @@ __device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, unsigned
 
 // Waves a SIMD that registers are kept for (as gs_xattn.hip).
 template <typename T, int DC, int NW> constexpr int min_waves() { return sizeof(T) == 4 && (DC > 64 || NW == 1) ? 1 : 2; }
+
+// A number that all lanes hold, as a scalar.
+__device__ __forceinline__ int64_t scalar(int64_t x) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
 
 // ------------------------------------------------------------ few rows
 
@@ -402,8 +422,8 @@ __device__ __forceinline__ int64_t few_share(const PagedAttnArgs &a, int64_t tot
 template <typename T, int DC, int BN, bool VEC>
 __global__ void __launch_bounds__(64, (min_waves<T, DC, 1>())) few_kernel(PagedAttnArgs a) {
     constexpr int DP = padded(DC);
-    __shared__ __attribute__((aligned(16))) char lds[4 * BN * DP * sizeof(T)];
-    __shared__ unsigned long long marks[2];
+    __shared__ __attribute__((aligned(16))) char lds[2 * BN * DP * sizeof(T)];
+    __shared__ int marks[1];
     const int64_t wave = blockIdx.x;
     int64_t share = 0;
     Line<BN> line;
@@ -411,10 +431,11 @@ __global__ void __launch_bounds__(64, (min_waves<T, DC, 1>())) few_kernel(PagedA
         share = few_share(a, total);
         return wave * share;
     });
-    const int64_t begin = wave * share, units = line.total * a.Hkv;
+    share = scalar(share);
+    const int64_t begin = wave * share, units = scalar(line.total) * a.Hkv;
     const int64_t end = begin + share < units ? begin + share : units;
     int b = __builtin_amdgcn_readfirstlane(line.b);
-    int64_t u = begin, before = line.before;
+    int64_t u = begin, before = scalar(line.before);
     while (u < end && b < a.B) {
         const Rows r(a, b);
         const int tiles = few_tiles<BN>(a, b);
@@ -509,13 +530,16 @@ __device__ __forceinline__ int block_start(const PagedAttnArgs &a, int b) {
     return (a.qoff ? clamped(a.qoff, b, a.N) : b) * a.G / BLOCK + b;
 }
 
-// Lists the work: blocks from the last one down (later rows of a prompt see more),
-// those of more than a share of the tiles in equal parts.
+// Lists the work: blocks of more than a share of the tiles in equal parts, and the
+// longest first (in 64 steps), so that short ones fill the end.  Places within a
+// step, and of parts in the workspace, go by the order of atomics; no result does.
 template <int BN> __global__ void __launch_bounds__(1024) plan_kernel(PagedAttnArgs a) {
-    __shared__ int64_t room[4][16];
+    constexpr int STEPS = 64;
+    __shared__ int64_t room[16];
+    __shared__ int next[STEPS], longest, slots, joins;
     const int t = threadIdx.x;
-    auto tiles_of = [&](int i, int *b, int *tile) {
-        *b = 0, *tile = 0;
+    int b = 0, tile = 0;
+    auto tiles_of = [&](int i) {
         if (i >= a.blocks || a.B == 0) return 0;
         int lo = 0, hi = a.B;
         while (hi - lo > 1) {
@@ -526,41 +550,61 @@ template <int BN> __global__ void __launch_bounds__(1024) plan_kernel(PagedAttnA
         const Rows r(a, lo);
         const int k = i - block_start(a, lo), all = r.count * a.G;
         if (k < 0 || k * BLOCK >= all) return 0;
-        *b = lo, *tile = k;
+        b = lo, tile = k;
         const View<BN> v(a, r, k * BLOCK / a.G, ((k + 1) * BLOCK < all ? (k + 1) * BLOCK - 1 : all - 1) / a.G);
         return v.tiles > 1 ? v.tiles : 1;
     };
-    int b, tile;
+    if (t < STEPS) next[t] = 0;
+    if (t == 0) longest = 1, slots = 0, joins = 0;
     int64_t mine = 0, total;
-    for (int i = t; i < a.blocks; i += 1024) mine += tiles_of(i, &b, &tile);
-    (void)group_scan(mine, room[3], &total);
+    int n = 0, most = 0;
+    for (int i = t; i < a.blocks; i += 1024) {
+        n = tiles_of(i);
+        mine += n;
+        most = max(most, n);
+    }
+    (void)group_scan(mine, room, &total);
     total = (total * a.Hkv + a.waves - 1) / a.waves;
     const int share = total < a.least ? a.least : (int)(total < 0x40000000 ? total : 0x40000000);
-    int items = 0, slots = 0, joins = 0;
-    for (int i0 = 0; i0 < a.blocks; i0 += 1024) {
-        const int n = tiles_of(i0 + t < a.blocks ? a.blocks - 1 - (i0 + t) : a.blocks, &b, &tile);
-        const int parts = n > share ? (n - 1) / share + 1 : (n ? 1 : 0);
-        // (the next round's first scan waits for all to have read this one's last)
-        int64_t all;
-        const int item = items + (int)group_scan(parts, room[0], &all);
-        items += (int)all;
-        const int slot = slots + (int)group_scan(parts > 1 ? parts : 0, room[1], &all);
-        slots += (int)all;
-        const int join = joins + (int)group_scan(parts > 1, room[2], &all);
-        joins += (int)all;
+    atomicMax(&longest, min(most, share));
+    __syncthreads();
+    // parts of a block of n tiles, and their step by length
+    const int top = longest;
+    auto parts_of = [&](int n) { return n > share ? (n - 1) / share + 1 : (n ? 1 : 0); };
+    auto step_of = [&](int n, int parts) { return (int)((STEPS - 1) - (int64_t)(n / parts) * (STEPS - 1) / top); };
+    const bool again = a.blocks > 1024;         // more blocks than threads: looked up once more each time
+    for (int i = t; i < a.blocks; i += 1024) {
+        if (again) n = tiles_of(i);
+        const int parts = parts_of(n);
+        if (parts) atomicAdd(&next[step_of(n, parts)], parts);
+    }
+    __syncthreads();
+    if (t < STEPS) {
+        const int here = next[t], sum = (int)wave_scan(here, 64);
+        next[t] = sum - here;
+        if (t == STEPS - 1) a.head->items = sum;
+    }
+    __syncthreads();
+    for (int i = t; i < a.blocks; i += 1024) {
+        if (again) n = tiles_of(i);
+        const int parts = parts_of(n);
+        if (!parts) continue;
+        const int item = atomicAdd(&next[step_of(n, parts)], parts);
+        const int slot = parts > 1 ? atomicAdd(&slots, parts) : -1;
         for (int k = 0; k < parts; ++k)
             a.items[item + k] = PagedItem{b, tile, (int32_t)((int64_t)n * k / parts), (int32_t)((int64_t)n * (k + 1) / parts),
                                           parts > 1 ? slot + k : -1};
-        if (parts > 1) a.joins[join] = PagedJoin{b, tile, slot, parts};
+        if (parts > 1) a.joins[atomicAdd(&joins, 1)] = PagedJoin{b, tile, slot, parts};
     }
-    if (t == 0) *a.head = PagedAttnHead{items, joins};
+    __syncthreads();
+    if (t == 0) a.head->joins = joins;
 }
 
 template <typename T, int DC, int BN, bool VEC>
 __global__ void __launch_bounds__(256, (min_waves<T, DC, 4>())) many_kernel(PagedAttnArgs a) {
     constexpr int DP = padded(DC);
     __shared__ __attribute__((aligned(16))) char lds[4 * BN * DP * sizeof(T)];
-    __shared__ unsigned long long marks[8];
+    __shared__ int marks[8];
     const int item = blockIdx.x / a.Hkv, hk = blockIdx.x % a.Hkv;
     if (item >= a.head->items) return;
     const PagedItem p = a.items[item];
@@ -628,8 +672,8 @@ Layout layout(gs_dtype t, const PagedAttnArgs &a) {
     z.dp = padded(dc);
     z.few = rows <= FEW;
     if (z.few) {
-        // as many waves as the CUs hold at once, by their tiles' 160 KB
-        const int held = 163840 / (4 * tile_keys(t, true) * z.dp * (t == GS_F32 ? 4 : 2));
+        // as many waves as the CUs hold at once, by their registers
+        const int held = t == GS_F32 ? 4 : 8;
         z.rows = (int)rows;
         z.least = 4;
         const int64_t most = ((int64_t)(a.Lk + 31) / 32 + 1) * a.B * a.Hkv / z.least + 1;
