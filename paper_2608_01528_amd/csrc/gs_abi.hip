@@ -405,8 +405,7 @@ bool paged_sizes(const gs_paged_attn *a) {
     if (!counts({a->B, a->N, a->Lq, a->Lk, a->pages, a->page, a->width}) || a->page < 1) return false;
     if (a->Hq < 1 || a->Hq >= (1 << 16) || a->Hkv < 1 || a->Hq % a->Hkv || a->Dh < 1 || a->Dh > CROSS_ATTN_MAX_DH) return false;
     if (a->N * a->Hq >= ((int64_t)1 << 30) || a->B * a->Hkv >= ((int64_t)1 << 22)) return false;
-    const int64_t rows = a->Lq * (a->Hq / a->Hkv);
-    if (rows <= 32 && a->B * a->Hkv * rows >= ATTN_MAX_BLOCKS) return false;
+    if (a->B * (a->Lk / 32 + 3) >= SEQ_MAX) return false;       // tiles of a head, in all
     return a->Lk <= (__int128)a->width * a->page && a->window >= 0 && a->sinks >= 0;
 }
 

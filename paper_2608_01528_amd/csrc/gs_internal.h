@@ -341,7 +341,10 @@ struct PagedAttnArgs {
     bool vec;
     // set by launch_paged_attn
     uint32_t page_magic; int page_shift;    // j / page = (j page_magic) >> 32 >> page_shift
-    int rows, blocks, waves, least;         // packed rows of a part; blocks of rows; work-groups that share the work; fewest tiles of a part
+    int rows, least;                    // packed rows of a part; fewest tiles of a part
+    int ranges;                         // few rows: parts of the line of all tiles
+    int32_t *line;                      // tiles before each request; a range's tiles
+    int blocks, waves;                  // many rows: blocks of rows; work-groups that share the work
     PagedAttnHead *head;
     PagedItem *items;
     PagedJoin *joins;

@@ -354,12 +354,6 @@ __device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, int *mar
 // Waves a SIMD that registers are kept for (as gs_xattn.hip).
 template <typename T, int DC, int NW> constexpr int min_waves() { return sizeof(T) == 4 && (DC > 64 || NW == 1) ? 1 : 2; }
 
-// A number that all lanes hold, as a scalar.
-__device__ __forceinline__ int64_t scalar(int64_t x) {
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
-    return (int64_t)((uint64_t)hi << 32 | lo);
-}
-
 // ------------------------------------------------------------ few rows
 
 // Tiles of request b; one where there are rows, but no states.
@@ -370,154 +364,133 @@ template <int BN> __device__ __forceinline__ int few_tiles(const PagedAttnArgs &
     return v.tiles > 1 ? v.tiles : 1;
 }
 
-// A place in the line of all (request, head, tile): requests in order, each
-// request's heads one after the other.  Found by a wave: `total` tiles of a head
-// over all requests, the request that holds unit u, and the tiles of a head of
-// those before it.
-template <int BN> struct Line {
-    int64_t total, before;
-    int b;
-    template <typename F> __device__ __forceinline__ void find(const PagedAttnArgs &a, F unit) {
-        const int l = threadIdx.x & 63;
-        int s = 0, e = a.B;
-        before = 0;
-        bool first = true;
-        int64_t u = 0;
-        do {
-            const int per = (e - s + 63) / 64;
-            const int from = s + l * per, to = from + per < e ? from + per : e;
-            int64_t mine = 0;
-#pragma unroll 4
-            for (int i = from; i < to; ++i) mine += few_tiles<BN>(a, i);
-            int64_t sums = mine;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int64_t x = __shfl_up((long long)sums, d);
-                if (l >= d) sums += x;
-            }
-            if (first) {
-                total = __shfl((long long)sums, 63);
-                u = unit(total);
-                first = false;
-            }
-            const uint64_t past = __ballot((before + sums) * a.Hkv > u);
-            if (!past) {        // behind the end
-                b = a.B;
-                return;
-            }
-            const int at = __ffsll((unsigned long long)past) - 1;
-            before += __shfl((long long)(sums - mine), at);
-            s += at * per;
-            e = s + per < e ? s + per : e;
-        } while (e - s > 1);
-        b = s;
-    }
-};
-
-__device__ __forceinline__ int64_t few_share(const PagedAttnArgs &a, int64_t total) {
-    const int64_t per = (total * a.Hkv + a.waves - 1) / a.waves;
+__device__ __forceinline__ int few_share(const PagedAttnArgs &a, int total) {
+    const int per = (int)((uint32_t)(total - 1) / (uint32_t)a.ranges) + 1;
     return per < a.least ? a.least : per;
 }
 
+// All requests' tiles lie in a line, requests in order.  Found by a wave: the
+// share of the line that a range has, and for range i the request in which it
+// begins and the tiles of those before that; b = a.B behind the end.
+struct Line {
+    int total, share, before, b;
+    template <int BN> __device__ __forceinline__ void find(const PagedAttnArgs &a, int i) {
+        const int l = threadIdx.x & 63;
+        int s = 0, e = a.B;
+        int64_t u = 0;
+        before = 0;
+        for (bool first = true; first || e - s > 1; first = false) {
+            const int per = (e - s + 63) / 64;
+            const int from = s + l * per, to = from + per < e ? from + per : e;
+            int mine = 0;
+#pragma unroll 4
+            for (int k = from; k < to; ++k) mine += few_tiles<BN>(a, k);
+            const int sums = wave_upto(mine);
+            if (first) {
+                total = lane_value(sums, 63);
+                if (!total) break;
+                share = few_share(a, total);
+                u = (int64_t)i * share;
+            }
+            const uint64_t past = __ballot(before + sums > u);
+            if (!past) {
+                s = a.B;
+                break;
+            }
+            const int at = __ffsll((unsigned long long)past) - 1;
+            before += lane_value(sums - mine, at);
+            s += at * per;
+            e = s + per < e ? s + per : e;
+        }
+        b = total ? s : a.B;
+    }
+};
+
+// A range of the line, one head: a wave.  The heads of a range are read side by
+// side, as their states lie in the cache.
 template <typename T, int DC, int BN, bool VEC>
 __global__ void __launch_bounds__(64, (min_waves<T, DC, 1>())) few_kernel(PagedAttnArgs a) {
     constexpr int DP = padded(DC);
     __shared__ __attribute__((aligned(16))) char lds[2 * BN * DP * sizeof(T)];
     __shared__ int marks[1];
-    const int64_t wave = blockIdx.x;
-    int64_t share = 0;
-    Line<BN> line;
-    line.find(a, [&](int64_t total) {
-        share = few_share(a, total);
-        return wave * share;
-    });
-    share = scalar(share);
-    const int64_t begin = wave * share, units = scalar(line.total) * a.Hkv;
-    const int64_t end = begin + share < units ? begin + share : units;
-    int b = __builtin_amdgcn_readfirstlane(line.b);
-    int64_t u = begin, before = scalar(line.before);
-    while (u < end && b < a.B) {
+    const int range = blockIdx.x / a.Hkv, hk = blockIdx.x % a.Hkv;
+    Line line;
+    line.find<BN>(a, range);
+    int b = line.b, before = line.before;
+    if (b >= a.B) return;
+    const int begin = range * line.share, end = line.total - begin < line.share ? line.total : begin + line.share;
+    if (begin == 0 && hk == 0 && threadIdx.x == 0) a.line[a.B] = line.share;
+    for (int u = begin; u < end; ++b) {
         const Rows r(a, b);
         const int tiles = few_tiles<BN>(a, b);
-        if (tiles) {
-            const int64_t off = u - before * a.Hkv;
-            const int hk = (int)(off / tiles), x0 = (int)(off % tiles);
-            const int x1 = end - u < tiles - x0 ? x0 + (int)(end - u) : tiles;
-            const View<BN> v(a, r, 0, r.count - 1);
-            float *part = nullptr, *part_lse = nullptr;
-            if (x1 - x0 < tiles) {
-                const int64_t slot = 2 * wave + (u - x0 > begin);
-                part = a.part + slot * a.rows * DP;
-                part_lse = a.part_lse + slot * a.rows;
-            }
-            pass<T, DC, 1, BN, VEC>(a, lds, marks, b, hk, r, 0, x0, x1 < v.tiles ? x1 : v.tiles, part, part_lse);
-            u += x1 - x0;
-            if (hk + 1 < a.Hkv || x1 < tiles) continue;
+        if (!tiles) continue;
+        const int x0 = u - before, x1 = end - before < tiles ? end - before : tiles;
+        const View<BN> v(a, r, 0, r.count - 1);
+        float *part = nullptr, *part_lse = nullptr;
+        if (x1 - x0 < tiles) {
+            const int64_t slot = (int64_t)(2 * range + (before > begin)) * a.Hkv + hk;
+            part = a.part + slot * a.rows * DP;
+            part_lse = a.part_lse + slot * a.rows;
         }
+        if (x0 == 0 && hk == 0 && threadIdx.x == 0) a.line[b] = before;
+        pass<T, DC, 1, BN, VEC>(a, lds, marks, b, hk, r, 0, x0, x1 < v.tiles ? x1 : v.tiles, part, part_lse);
+        u += x1 - x0;
         before += tiles;
-        ++b;
     }
 }
 
-// Puts together a row of a request and head that part ends cut: a work-group a
+// Puts together rows of a request and head that range ends cut: a work-group a
 // row, parts shared out to its lanes' groups.
-template <typename T, int DP, int BN> __global__ void __launch_bounds__(256) few_join_kernel(PagedAttnArgs a) {
-    constexpr int LANES = DP / 4, GROUPS = 256 / LANES;
-    __shared__ int64_t counts[2][4];
+template <typename T, int DP, int BN, int NT> __global__ void __launch_bounds__(NT) few_join_kernel(PagedAttnArgs a) {
+    constexpr int LANES = DP / 4, GROUPS = NT / LANES, WAVES = NT / 64;
     __shared__ f4v sums[GROUPS][LANES];
-    __shared__ float weights[GROUPS], tops[4];
-    const int t = threadIdx.x, l = t & 63, w = t >> 6;
-    const int m = blockIdx.x % a.rows, hk = blockIdx.x / a.rows % a.Hkv, b = blockIdx.x / a.rows / a.Hkv;
+    __shared__ float weights[GROUPS], tops[WAVES];
+    const int t = threadIdx.x, l = t & 63, w = t >> 6, g = t / LANES, d = t % LANES;
+    const int hk = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv;
     const Rows r(a, b);
-    if (m >= r.count * a.G) return;
-    int64_t total = 0, before = 0;
-    for (int i = t; i < a.B; i += 256) {
-        const int n = few_tiles<BN>(a, i);
-        total += n;
-        if (i < b) before += n;
-    }
+    const int rows = r.count * a.G;
+    if (!rows) return;
+    const int before = a.line[b], share = a.line[a.B], tiles = few_tiles<BN>(a, b);
+    const int i0 = before / share, i1 = (before + tiles - 1) / share;
+    if (i0 == i1) return;
+    const int64_t step = 2 * (int64_t)a.Hkv * a.rows;
+    for (int m = blockIdx.y; m < rows; m += gridDim.y) {
+        // the first part may be its range's second one
+        const int64_t at0 = ((int64_t)(2 * i0 + (before > i0 * share)) * a.Hkv + hk) * a.rows + m;
+        const int64_t at1 = ((int64_t)(2 * i0) * a.Hkv + hk) * a.rows + m;
+        auto place = [&](int i) { return i == i0 ? at0 : at1 + (i - i0) * step; };
+        float top = -INFINITY;
+        for (int i = i0 + t; i <= i1; i += NT) top = fmaxf(top, a.part_lse[place(i)]);
 #pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        total += __shfl_xor((long long)total, d);
-        before += __shfl_xor((long long)before, d);
-    }
-    if (l == 0) counts[0][w] = total, counts[1][w] = before;
-    __syncthreads();
-    total = counts[0][0] + counts[0][1] + counts[0][2] + counts[0][3];
-    before = counts[1][0] + counts[1][1] + counts[1][2] + counts[1][3];
-    const int tiles = few_tiles<BN>(a, b);
-    const int64_t share = few_share(a, total), u0 = before * a.Hkv + (int64_t)hk * tiles;
-    const int64_t w0 = u0 / share, w1 = (u0 + tiles - 1) / share;
-    if (w0 == w1) return;
-    auto slot = [&](int64_t i) { return 2 * i + (u0 > i * share); };
-    float top = -INFINITY;
-    for (int64_t i = w0 + t; i <= w1; i += 256) top = fmaxf(top, a.part_lse[slot(i) * a.rows + m]);
+        for (int k = 32; k; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
+        if (l == 0) tops[w] = top;
+        __syncthreads();
 #pragma unroll
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    if (l == 0) tops[w] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    const float ref = top == -INFINITY ? 0.f : top;
-    const int g = t / LANES, d = t % LANES;
-    f4v o = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-#pragma unroll 4
-    for (int64_t i = w0 + g; i <= w1; i += GROUPS) {
-        const int64_t at = slot(i) * a.rows + m;
-        const float e = __builtin_amdgcn_exp2f((a.part_lse[at] - ref) * LOG2E);
-        sum += e;
-        o += e * *reinterpret_cast<const f4v *>(a.part + at * DP + 4 * d);
+        for (int k = 0; k < WAVES; ++k) top = fmaxf(top, tops[k]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        f4v o = {0.f, 0.f, 0.f, 0.f};
+        float sum = 0.f;
+#pragma unroll 8
+        for (int i = i0 + g; i <= i1; i += GROUPS) {
+            const int64_t at = place(i);
+            const float e = __builtin_amdgcn_exp2f((a.part_lse[at] - ref) * LOG2E);
+            sum += e;
+            o += e * *reinterpret_cast<const f4v *>(a.part + at * DP + 4 * d);
+        }
+        sums[g][d] = o;
+        if (d == 0) weights[g] = sum;
+        __syncthreads();
+        if (g == 0) {
+            const int all = i1 - i0 + 1 < GROUPS ? i1 - i0 + 1 : GROUPS;
+            for (int i = 1; i < all; ++i) o += sums[i][d], sum += weights[i];
+            const float inv = sum != 0.f ? 1.f / sum : 0.f;
+            const RowOf row(m, hk, a.G);
+            const int64_t at = r.first + row.i;
+            if (4 * d < a.Dh) store4<T>(static_cast<T *>(a.O) + at * a.o.l + row.h * a.o.h, 4 * d, a.Dh, a.vec, o * inv);
+            if (a.lse && d == 0) a.lse[at * a.Hq + row.h] = sum != 0.f ? ref + __builtin_amdgcn_logf(sum) * LN2 : -INFINITY;
+        }
+        __syncthreads();
     }
-    sums[g][d] = o;
-    if (d == 0) weights[g] = sum;
-    __syncthreads();
-    if (g) return;
-    for (int i = 1; i < GROUPS; ++i) o += sums[i][d], sum += weights[i];
-    const float inv = sum != 0.f ? 1.f / sum : 0.f;
-    const RowOf row(m, hk, a.G);
-    const int64_t at = r.first + row.i;
-    if (4 * d < a.Dh) store4<T>(static_cast<T *>(a.O) + at * a.o.l + row.h * a.o.h, 4 * d, a.Dh, a.vec, o * inv);
-    if (a.lse && d == 0) a.lse[at * a.Hq + row.h] = sum != 0.f ? ref + __builtin_amdgcn_logf(sum) * LN2 : -INFINITY;
 }
 
 // ------------------------------------------------------------ many rows
@@ -580,7 +553,7 @@ template <int BN> __global__ void __launch_bounds__(1024) plan_kernel(PagedAttnA
     }
     __syncthreads();
     if (t < STEPS) {
-        const int here = next[t], sum = (int)wave_scan(here, 64);
+        const int here = next[t], sum = wave_upto(here);
         next[t] = sum - here;
         if (t == STEPS - 1) a.head->items = sum;
     }
@@ -660,7 +633,7 @@ constexpr int tile_keys(gs_dtype t, bool few) { return t == GS_F32 || few ? 32 :
 // Sizes of the workspace's parts, by sizes that the host knows.
 struct Layout {
     bool few;
-    int waves, least, rows;
+    int ranges, waves, least, rows;
     int64_t blocks, items, joins, slots;
     int dp;
     size_t list, bytes;
@@ -676,9 +649,9 @@ Layout layout(gs_dtype t, const PagedAttnArgs &a) {
         const int held = t == GS_F32 ? 4 : 8;
         z.rows = (int)rows;
         z.least = 4;
-        const int64_t most = ((int64_t)(a.Lk + 31) / 32 + 1) * a.B * a.Hkv / z.least + 1;
-        z.waves = (int)(most < 256 * held ? most : 256 * held);
-        z.slots = 2 * (int64_t)z.waves;
+        const int64_t most = ((int64_t)(a.Lk + 31) / 32 + 1) * a.B / z.least + 1, full = 256 * held / a.Hkv;
+        z.ranges = (int)(most < full ? most : (full > 1 ? full : 1));
+        z.slots = 2 * (int64_t)z.ranges * a.Hkv;
     } else {
         const int64_t most = t == GS_F32 && dc > 64 ? 256 : 512;
         z.rows = BLOCK;
@@ -692,7 +665,7 @@ Layout layout(gs_dtype t, const PagedAttnArgs &a) {
         z.joins = z.slots / 2 + 1;
         z.slots *= a.Hkv;
     }
-    z.list = sizeof(PagedAttnHead) + (size_t)z.items * sizeof(PagedItem) + (size_t)z.joins * sizeof(PagedJoin);
+    z.list = z.few ? 4 * ((size_t)a.B + 1) : sizeof(PagedAttnHead) + (size_t)z.items * sizeof(PagedItem) + (size_t)z.joins * sizeof(PagedJoin);
     z.list = (z.list + 15) / 16 * 16;
     z.bytes = z.list + (size_t)z.slots * z.rows * (z.dp + 1) * 4;
     return z;
@@ -703,10 +676,12 @@ template <typename T, int DC, bool VEC> hipError_t launch_sized(const PagedAttnA
     constexpr gs_dtype t = sizeof(T) == 4 ? GS_F32 : GS_BF16;
     if (z.few) {
         constexpr int BN = tile_keys(t, true);
-        few_kernel<T, DC, BN, VEC><<<dim3((unsigned)z.waves), dim3(64), 0, s>>>(a);
+        few_kernel<T, DC, BN, VEC><<<dim3((unsigned)(z.ranges * a.Hkv)), dim3(64), 0, s>>>(a);
         hipError_t e = hipGetLastError();
-        if (e != hipSuccess || z.waves == 1) return e;
-        few_join_kernel<T, DP, BN><<<dim3((unsigned)(a.B * a.Hkv * a.rows)), dim3(256), 0, s>>>(a);
+        if (e != hipSuccess || z.ranges == 1) return e;
+        const dim3 rows((unsigned)(a.B * a.Hkv), (unsigned)(a.B * a.Hkv * a.rows <= 16384 ? a.rows : 1));
+        if (z.ranges / a.B >= 32) few_join_kernel<T, DP, BN, 1024><<<rows, dim3(1024), 0, s>>>(a);
+        else few_join_kernel<T, DP, BN, 256><<<rows, dim3(256), 0, s>>>(a);
         return hipGetLastError();
     }
     constexpr int BN = tile_keys(t, false);
@@ -734,7 +709,9 @@ hipError_t launch_paged_attn(gs_dtype t, PagedAttnArgs a, void *ws, hipStream_t 
     a.rows = z.rows;
     a.blocks = (int)z.blocks;
     a.waves = z.waves;
+    a.ranges = z.ranges;
     a.least = z.least;
+    a.line = static_cast<int32_t *>(ws);
     a.head = static_cast<PagedAttnHead *>(ws);
     a.items = reinterpret_cast<PagedItem *>(a.head + 1);
     a.joins = reinterpret_cast<PagedJoin *>(a.items + z.items);

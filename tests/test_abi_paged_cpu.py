@@ -127,7 +127,7 @@ def test_nothing_to_do(L, kind, change):
     (Attn, dict(Dh=0), gs.GS_ERR_SHAPE), (Attn, dict(page=0), gs.GS_ERR_SHAPE), (Attn, dict(pages=-1), gs.GS_ERR_SHAPE),
     (Attn, dict(window=-1), gs.GS_ERR_SHAPE), (Attn, dict(sinks=-1), gs.GS_ERR_SHAPE),
     (Attn, dict(N=2**28, Lq=1), gs.GS_ERR_SHAPE), (Attn, dict(B=2**21), gs.GS_ERR_SHAPE),
-    (Attn, dict(Hq=2**16, Hkv=2**16), gs.GS_ERR_SHAPE), (Attn, dict(B=2**20, Lq=4), gs.GS_ERR_SHAPE),
+    (Attn, dict(Hq=2**16, Hkv=2**16), gs.GS_ERR_SHAPE), (Attn, dict(B=2**9, Lk=2**27, page=2**25), gs.GS_ERR_SHAPE),
     (Attn, dict(qoff=0), gs.GS_ERR_SHAPE), (Attn, dict(ldt=4), gs.GS_ERR_SHAPE), (Attn, dict(ldt=2**45), gs.GS_ERR_SHAPE),
     (Attn, dict(scale=0.0), gs.GS_ERR_ARG), (Attn, dict(scale=float("nan")), gs.GS_ERR_ARG),
     (Attn, dict(scale=1e31), gs.GS_ERR_ARG), (Attn, dict(klen=0), gs.GS_ERR_ARG), (Attn, dict(table=0), gs.GS_ERR_ARG),
