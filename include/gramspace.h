@@ -739,7 +739,7 @@ gs_status gs_paged_store(const gs_paged_rows *p, gs_dtype t, gs_dtype ct, void *
  *   Lk         most states of a request, 0 <= Lk <= width page: klen counts as 0
  *              below 0 and as Lk above
  *   Hq, Hkv    heads; Hkv divides Hq        Dh   values a head, 1 <= Dh <= 128
- *   N Hq below 2^30, B Hkv below 2^22, Hq below 2^16, B (Lk / 32 + 3) below 2^31;
+ *   N Hq below 2^30, B Hkv below 2^22, Hq below 2^16, B (Lk / 16 + 3) below 2^31;
  *   Lq, Lk, pages, page, width below 2^31 - 256
  *   table      int32 B x width device, ldt >= width       klen int32[B] device
  *   qoff       int32[B + 1] device, clamped to 0 .. N; null: N = B, a row each

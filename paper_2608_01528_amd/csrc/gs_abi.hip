@@ -405,7 +405,7 @@ bool paged_sizes(const gs_paged_attn *a) {
     if (!counts({a->B, a->N, a->Lq, a->Lk, a->pages, a->page, a->width}) || a->page < 1) return false;
     if (a->Hq < 1 || a->Hq >= (1 << 16) || a->Hkv < 1 || a->Hq % a->Hkv || a->Dh < 1 || a->Dh > CROSS_ATTN_MAX_DH) return false;
     if (a->N * a->Hq >= ((int64_t)1 << 30) || a->B * a->Hkv >= ((int64_t)1 << 22)) return false;
-    if (a->B * (a->Lk / 32 + 3) >= SEQ_MAX) return false;       // tiles of a head, in all
+    if (a->B * (a->Lk / 16 + 3) >= SEQ_MAX) return false;       // tiles of a head, in all
     return a->Lk <= (__int128)a->width * a->page && a->window >= 0 && a->sinks >= 0;
 }
 

@@ -60,10 +60,26 @@ template <int BN> struct View {
     __device__ __forceinline__ bool holds(int j) const { return j < hi && (j < sink || j >= lo); }
 };
 
+// All keys of a tile at j0 are there (`on`), and seen by rows at positions from p to q.
+template <int BN> __device__ __forceinline__ bool seen_by(const PagedAttnArgs &a, uint64_t on, int j0, int p, int q) {
+    return on == ALL_LIVE<BN> && p >= j0 + BN - 1 && (!a.window || (int64_t)q - a.window < j0 || j0 + BN <= a.sinks);
+}
+
 // Bits 0 .. n - 1.
 __device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0 : (n >= 64 ? ~0ull : (1ull << n) - 1); }
 
+// Bit n: the row at position p sees key j0 + n.
+__device__ __forceinline__ uint64_t seen_bits(const PagedAttnArgs &a, int p, int j0) {
+    uint64_t seen = low_bits(p + 1 - j0);
+    if (a.window) seen &= ~low_bits((p >= a.window ? p - a.window + 1 : 0) - j0) | low_bits(a.sinks - j0);
+    return seen;
+}
+
 // ------------------------------------------------------------ tiles from pages
+
+// The loop over tiles holds no branch with a load in it: the compiler counts the
+// loads that are on their way, and behind such a branch it waits for all of them.
+// So a tile behind the last one is "read" too, from the cache's first place.
 
 // Where the keys of a tile lie: lane l knows key j0 + l.  Keys that are not
 // there stand for page 0, place 0, which is in memory, and do not take part.
@@ -74,14 +90,14 @@ template <int BN> struct Places {
     int j;
     bool there;
     __device__ __forceinline__ int page_of(const PagedAttnArgs &a) const {
-        return a.page_magic ? (int)(__umulhi((uint32_t)j, a.page_magic) >> a.page_shift) : j;
+        return (int)(__umulhi((uint32_t)j, a.page_magic) >> a.page_shift) + (a.page == 1 ? j : 0);
     }
-    // asks for the page of this lane's key of the tile at j0
-    __device__ __forceinline__ void ahead(const PagedAttnArgs &a, const View<BN> &v, int j0) {
-        j = j0 + l;
-        there = l < BN && v.holds(j);
-        id = -1;
-        if (there) id = table[page_of(a)];
+    // asks for the page of this lane's key of tile x (none from x1 on)
+    __device__ __forceinline__ void ahead(const PagedAttnArgs &a, const View<BN> &v, int x, int x1) {
+        j = v.start(x) + l;
+        there = x < x1 && l < BN && v.holds(j);
+        j = there ? j : 0;
+        id = table[page_of(a)];
     }
     // Lanes' pages and places in them, and the keys that are there (of the tile
     // last asked for).
@@ -93,32 +109,57 @@ template <int BN> struct Places {
     }
 };
 
-// A thread's part of a tile of K or V on its way to LDS (as TileLoad, rows from
-// pages).  Rows that are not live hold page 0's values until `clean`.
-template <typename T, int DP, int BN, int NT, bool VEC> struct PagedLoad {
+// A tile's place in LDS for blocks of 16 rows: as place() for bf16; in fp32 the
+// rows 4 g + e of four groups of lanes g, read 16 values each, lie in different
+// banks.
+template <typename T, int DP> __device__ __forceinline__ int place16(int r, int c) {
+    if constexpr (sizeof(T) == 2) return place<T, DP>(r, c);
+    else return (r * (DP / 4) + (c ^ (((r >> 2) & 3) << 2 | (r & 3)))) * 16;
+}
+
+// A thread's part of a tile of K and of V on its way to LDS (as TileLoad, rows from
+// pages).  Rows that are not there hold page 0's values until `clean`; pieces at
+// and past dh are never written (threads that would carry them carry piece 0 as
+// well), so what LDS holds there, zeros, stays.  ONCE: no other work-group reads the
+// tile, so it is not kept in the caches (reads of 2048 waves in such tiles: 5.5 TB/s,
+// with this 6.2).
+template <typename T, int DP, int BN, int NT, bool VEC, bool ONCE> struct PagedLoad {
     static constexpr int PER = Op<T>::PER, CPR = DP / PER, N = BN * CPR / NT, RPI = NT / CPR;
     static_assert(BN * CPR % NT == 0 && NT % CPR == 0, "whole chunks per thread");
-    u4v v[N];
-    __device__ __forceinline__ void fetch(const T *cache, const SeqStrides &s, int32_t page, int32_t at, bool any, int dh, int t) {
-        const int c = t % CPR, r0 = t / CPR;
+    u4v k[N], v[N];
+    static __device__ __forceinline__ int piece(int t, int dh) { return t % CPR * PER < dh ? t % CPR : 0; }
+    static __device__ __forceinline__ u4v load(const T *row, int c, int dh) {
+        if constexpr (VEC && ONCE) return __builtin_nontemporal_load(reinterpret_cast<const u4v *>(row + PER * c));
+        else if constexpr (VEC) return *reinterpret_cast<const u4v *>(row + PER * c);
+        else return load_chunk<T>(row, PER * c, dh, false);
+    }
+    __device__ __forceinline__ void fetch(const PagedAttnArgs &a, const T *K, const T *V, int32_t page, int32_t at, int t) {
+        const int c = piece(t, a.Dh), r0 = t / CPR;
+        int32_t g[N], i[N];
+#pragma unroll
+        for (int q = 0; q < N; ++q) g[q] = __shfl(page, r0 + q * RPI), i[q] = __shfl(at, r0 + q * RPI);
+#pragma unroll
+        for (int q = 0; q < N; ++q) k[q] = load(K + g[q] * a.k.b + i[q] * a.k.l, c, a.Dh);
+#pragma unroll
+        for (int q = 0; q < N; ++q) v[q] = load(V + g[q] * a.v.b + i[q] * a.v.l, c, a.Dh);
+    }
+    // K's tile, and V's behind it; BLOCK16: for blocks of 16 rows
+    template <bool BLOCK16> __device__ __forceinline__ void stash(char *tile, int dh, int t) const {
+        const int c = piece(t, dh);
 #pragma unroll
         for (int q = 0; q < N; ++q) {
-            const int32_t g = __shfl(page, r0 + q * RPI), i = __shfl(at, r0 + q * RPI);
-            v[q] = u4v{0, 0, 0, 0};
-            if (any && c * PER < dh) v[q] = load_chunk<T>(cache + g * s.b + i * s.l, PER * c, dh, VEC);
+            const int r = t / CPR + q * RPI, at = BLOCK16 ? place16<T, DP>(r, c) : place<T, DP>(r, c);
+            *reinterpret_cast<u4v *>(tile + at) = k[q];
+            *reinterpret_cast<u4v *>(tile + BN * DP * (int)sizeof(T) + at) = v[q];
         }
     }
-    __device__ __forceinline__ void stash(char *tile, int t) const {
-#pragma unroll
-        for (int q = 0; q < N; ++q) *reinterpret_cast<u4v *>(tile + place<T, DP>(t / CPR + q * RPI, t % CPR)) = v[q];
-    }
-    // zeros in the rows that are not live
+    // zeros in V's rows that are not there
     __device__ __forceinline__ void clean(uint64_t live, int t) {
 #pragma unroll
         for (int q = 0; q < N; ++q)
             if (!((live >> (t / CPR + q * RPI)) & 1)) v[q] = u4v{0, 0, 0, 0};
     }
-    // Zeros in place of values that are not finite; says whether there were any.
+    // Zeros in place of V's values that are not finite; says whether there were any.
     __device__ __forceinline__ bool finite() {
         bool any = false;
 #pragma unroll
@@ -197,40 +238,37 @@ __device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, int *mar
     for (int j = 0; j < NJ; ++j) o[j] = f16v{0};
     float mx = -INFINITY, sum = 0.f;
 
-    PagedLoad<T, DP, BN, NT, VEC> kr, vr;
+    PagedLoad<T, DP, BN, NT, VEC, NW == 1> way;
     uint64_t live = 0, next_live = 0;
     auto fetch = [&]() {
         int32_t page, place;
         const uint64_t on = keys.take(a, &page, &place);
-        kr.fetch(K, a.k, page, place, on != 0, a.Dh, t);
-        vr.fetch(V, a.v, page, place, on != 0, a.Dh, t);
+        way.fetch(a, K, V, page, place, t);
         return on;
-    };
-    // all keys of the tile at j0 are there, and seen by rows at positions from p to q
-    auto seen_by = [&](uint64_t on, int j0, int p, int q) {
-        return on == ALL_LIVE<BN> && p >= j0 + BN - 1 && (!a.window || (int64_t)q - a.window < j0 || j0 + BN <= a.sinks);
     };
     // Rows of the block see different states of the tile: a product takes 0 inf and 0
     // NaN for NaN, so values that are not finite are kept out of it, and added at
     // the end to the rows that see them.
-    auto differ = [&](uint64_t on, int j0) { return i0 != i1 && !seen_by(on, j0, p0 + i0, p0 + i1); };
-    auto stash = [&](char *kt, int buffer, uint64_t on, int j0) {
-        if (on != ALL_LIVE<BN>) vr.clean(on, t);
-        if (differ(on, j0)) marks[NW * buffer + w] = __any(vr.finite());
-        kr.stash(kt, t);
-        vr.stash(kt + TILE, t);
+    auto differ = [&](uint64_t on, int j0) { return i0 != i1 && !seen_by<BN>(a, on, j0, p0 + i0, p0 + i1); };
+    auto stash = [&](int buffer, uint64_t on, int j0) {
+        if (on != ALL_LIVE<BN>) way.clean(on, t);
+        if (differ(on, j0)) marks[NW * buffer + w] = __any(way.finite());
+        way.template stash<false>(lds + buffer * 2 * TILE, a.Dh, t);
     };
     int buffer = 0;             // the tile in use: K, then V
     int left_out = 0;           // some tile held values that were kept out
     if (x0 < x1) {
-        keys.ahead(a, view, view.start(x0));
-        live = fetch();
-        if (x0 + 1 < x1) keys.ahead(a, view, view.start(x0 + 1));
-        stash(lds, 0, live, view.start(x0));
-        if (x0 + 1 < x1) {
-            next_live = fetch();
-            if (x0 + 2 < x1) keys.ahead(a, view, view.start(x0 + 2));
+        if (a.Dh < DC) {
+            lds_barrier();      // (an earlier block's tiles have been read)
+            clear_lds<NT>(lds, BUFFERS * 2 * TILE, t);
+            lds_barrier();
         }
+        keys.ahead(a, view, x0, x1);
+        live = fetch();
+        keys.ahead(a, view, x0 + 1, x1);
+        stash(0, live, view.start(x0));
+        next_live = fetch();
+        keys.ahead(a, view, x0 + 2, x1);
     }
     for (int x = x0; x < x1; ++x) {
         const int j0 = view.start(x);
@@ -244,11 +282,8 @@ __device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, int *mar
 #pragma unroll
                 for (int s = 0; s < NS; ++s) p[n] = Op<T>::mma(row_frag<T, DP>(kt, 32 * n, s, l), q[s], p[n]);
             }
-            uint64_t seen = ~0ull;
-            if (!seen_by(live, j0, pmin, pmax)) {
-                seen = low_bits(pos + 1 - j0);
-                if (a.window) seen &= ~low_bits((pos >= a.window ? pos - a.window + 1 : 0) - j0) | low_bits(a.sinks - j0);
-                seen &= live;
+            if (!seen_by<BN>(a, live, j0, pmin, pmax)) {
+                const uint64_t seen = seen_bits(a, pos, j0) & live;
 #pragma unroll
                 for (int n = 0; n < BN / 32; ++n) {
                     const uint32_t bits = (uint32_t)(seen >> (32 * n)) >> (4 * (l >> 5));
@@ -297,19 +332,15 @@ __device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, int *mar
         }
         if (BUFFERS == 2) buffer ^= 1;
         live = next_live;
-        if (x + 1 < x1) {
-            stash(lds + buffer * 2 * TILE, buffer, live, view.start(x + 1));
-            if (x + 2 < x1) {
-                next_live = fetch();
-                if (x + 3 < x1) keys.ahead(a, view, view.start(x + 3));
-            }
-        }
+        stash(buffer, live, view.start(x + 1));
+        next_live = fetch();
+        keys.ahead(a, view, x + 3, x1);
     }
     if (left_out) {             // they are added now, to the rows that see them
         for (int x = x0; x < x1; ++x) {
             const int j0 = view.start(x);
             int32_t page, place;
-            keys.ahead(a, view, j0);
+            keys.ahead(a, view, x, x1);
             const uint64_t there = keys.take(a, &page, &place);
             if (!differ(there, j0)) continue;
             for (uint64_t rest = there; rest; rest &= rest - 1) {
@@ -353,6 +384,212 @@ __device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, int *mar
 
 // Waves a SIMD that registers are kept for (as gs_xattn.hip).
 template <typename T, int DC, int NW> constexpr int min_waves() { return sizeof(T) == 4 && (DC > 64 || NW == 1) ? 1 : 2; }
+
+// ------------------------------------------------------------ up to 16 rows
+
+// The same pass for one wave and up to 16 packed rows, with products of 16 x 16:
+// lane l holds row l % 16 and of a block of 16 keys 4 (l / 16) + e.  Half the
+// registers of 32 rows leave room for two tiles on their way from memory while a
+// third is used: the pass waits for memory alone, and what is in flight decides
+// its rate.
+template <typename T> struct Op16;
+template <> struct Op16<bf16_t> {
+    static constexpr int BN = 32;       // keys a tile: the 32 terms of a product
+    static __device__ __forceinline__ f4v mma(bf8v a, bf8v b, f4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    // (probabilities in bf16, as in Op::pack)
+    static __device__ __forceinline__ bf8v pack(const f4v (&p)[2]) {
+        bf8v r;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = (__bf16)p[e / 4][e % 4];
+        return r;
+    }
+    // values 16 j .. of the keys in pack's order
+    template <int DP> static __device__ __forceinline__ bf8v col(const char *tile, int j, int l) {
+        const int a = l & 15, k = 4 * (l >> 4) + (a >> 2), n = 16 * j + 4 * (a & 3);
+        const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GS_LDS s4v *)(tile + place16<bf16_t, DP>(k, n >> 3) + 2 * (n & 7)));
+        const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GS_LDS s4v *)(tile + place16<bf16_t, DP>(k + 16, n >> 3) + 2 * (n & 7)));
+        const s4v both[2] = {lo, hi};
+        return *reinterpret_cast<const bf8v *>(both);
+    }
+};
+template <> struct Op16<float> {
+    static constexpr int BN = 16;
+    static __device__ __forceinline__ f4v mma(f4v a, f4v b, f4v c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+    static __device__ __forceinline__ f4v pack(const f4v (&p)[1]) { return p[0]; }
+    template <int DP> static __device__ __forceinline__ f4v col(const char *tile, int j, int l) {
+        f4v r;
+        const int n = 16 * j + (l & 15), k = 4 * (l >> 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = *reinterpret_cast<const float *>(tile + place16<float, DP>(k + e, n >> 2) + 4 * (n & 3));
+        return r;
+    }
+};
+
+template <typename T, int DC, bool VEC>
+__device__ __forceinline__ void pass16(const PagedAttnArgs &a, char *lds, int b, int hk, const Rows &r, int x0, int x1,
+                                       float *part, float *part_lse) {
+    constexpr int BN = Op16<T>::BN, DP = padded(DC), PER = Op<T>::PER, NS = DC / (4 * PER), NJ = DC / 16, NB = BN / 16;
+    constexpr int TILE = BN * DP * sizeof(T);
+    const int l = threadIdx.x, m = l & 15;
+    const int all = r.count * a.G;
+    const bool on = m < all;
+    const RowOf row(on ? m : 0, hk, a.G);
+    const int64_t at = r.first + row.i;
+    const View<BN> view(a, r, 0, r.count - 1);
+    const int pmin = r.kl - r.n, pmax = pmin + r.count - 1, pos = pmin + row.i;
+
+    typename Op<T>::V q[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        u4v v = {0, 0, 0, 0};
+        if (on) v = load_chunk<T>(static_cast<const T *>(a.Q) + at * a.q.l + row.h * a.q.h, PER * (4 * s + (l >> 4)), a.Dh, VEC);
+        q[s] = *reinterpret_cast<const typename Op<T>::V *>(&v);
+    }
+    const float c = fabsf(a.scale) * LOG2E;
+    if (a.scale < 0) {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) q[s] = -q[s];
+    }
+    const T *const K = static_cast<const T *>(a.K) + hk * a.k.h;
+    const T *const V = static_cast<const T *>(a.V) + hk * a.v.h;
+
+    f4v o[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) o[j] = f4v{0};
+    float mx = -INFINITY, sum = 0.f;
+    int left_out = 0;
+
+    // Two tiles on their way, and which of their keys are there.  Page numbers are
+    // asked for before the values of the tile before: loads return in order, and a
+    // page number must not wait for values that are needed later than it.
+    PagedLoad<T, DP, BN, 64, VEC, true> way[2];
+    uint64_t live[2];
+    Places<BN> keys[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) keys[i] = Places<BN>{a.table + b * a.ldt, l, -1, 0, false};
+    auto differ = [&](uint64_t on, int j0) { return pmin != pmax && !seen_by<BN>(a, on, j0, pmin, pmax); };
+    auto fetch = [&](int i) {
+        int32_t page, place;
+        live[i] = keys[i].take(a, &page, &place);
+        way[i].fetch(a, K, V, page, place, l);
+    };
+    // tile x, on its way number i, which tile x + 2 takes next
+    auto step = [&](int x, int i) {
+        const int j0 = view.start(x);
+        const uint64_t on = live[i];
+        if (on != ALL_LIVE<BN>) way[i].clean(on, l);
+        if (differ(on, j0)) left_out |= __any(way[i].finite());
+        lds_barrier();          // (one wave: keeps the accesses in order)
+        way[i].template stash<true>(lds, a.Dh, l);
+        keys[i ^ 1].ahead(a, view, x + 3, x1);
+        fetch(i);
+        lds_barrier();
+        f4v p[NB];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            p[n] = f4v{0};
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const typename Op<T>::V k = *reinterpret_cast<const typename Op<T>::V *>(lds + place16<T, DP>(16 * n + m, 4 * s + (l >> 4)));
+                p[n] = Op16<T>::mma(k, q[s], p[n]);
+            }
+        }
+        if (!seen_by<BN>(a, on, j0, pmin, pmax)) {
+            const uint32_t bits = (uint32_t)(seen_bits(a, pos, j0) & on) >> (4 * (l >> 4));
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (!((bits >> (16 * n + e)) & 1)) p[n][e] = -INFINITY;
+        }
+        float top = p[0][0];
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, p[n][e]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32)) * c;
+        if (__any(top > mx + 8.f)) {        // (as in pass)
+            const float next = fmaxf(mx, top);
+            const float turn = __builtin_amdgcn_exp2f(mx - (next == -INFINITY ? 0.f : next));
+            mx = next;
+            sum *= turn;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) o[j] *= turn;
+        }
+        const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                p[n][e] = __builtin_amdgcn_exp2f(fmaf(p[n][e], c, -ref));
+                sum += p[n][e];
+            }
+        const typename Op<T>::V pf = Op16<T>::pack(p);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) o[j] = Op16<T>::mma(Op16<T>::template col<DP>(lds + TILE, j, l), pf, o[j]);
+    };
+    if (x0 < x1) {
+        if (a.Dh < DC) {
+            lds_barrier();
+            clear_lds<64>(lds, 2 * TILE, l);
+            lds_barrier();
+        }
+        keys[0].ahead(a, view, x0, x1);
+        keys[1].ahead(a, view, x0 + 1, x1);
+        fetch(0);
+        keys[0].ahead(a, view, x0 + 2, x1);
+        fetch(1);
+        for (int x = x0;;) {
+            step(x, 0);
+            if (++x == x1) break;
+            step(x, 1);
+            if (++x == x1) break;
+        }
+    }
+    if (left_out) {
+        for (int x = x0; x < x1; ++x) {
+            const int j0 = view.start(x);
+            int32_t page, place;
+            keys[0].ahead(a, view, x, x1);
+            const uint64_t there = keys[0].take(a, &page, &place);
+            if (!differ(there, j0)) continue;
+            for (uint64_t rest = there; rest; rest &= rest - 1) {
+                const int k = __ffsll((unsigned long long)rest) - 1;
+                const int32_t g = __builtin_amdgcn_readlane(page, k), i = __builtin_amdgcn_readlane(place, k);
+                const T *const from = V + g * a.v.b + i * a.v.l;
+                if (!((seen_bits(a, pos, j0) >> k) & 1)) continue;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int d = 16 * j + 4 * (l >> 4) + e;
+                        const float v = d < a.Dh ? ld_f32<T>(from, d) : 0.f;
+                        if (!(fabsf(v) < INFINITY)) o[j][e] += v;
+                    }
+            }
+        }
+    }
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (!on) return;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float lse = sum != 0.f ? (mx + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
+    if (part) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) *reinterpret_cast<f4v *>(part + (int64_t)m * DP + 16 * j + 4 * (l >> 4)) = o[j] * inv;
+        if (l < 16) part_lse[m] = lse;
+        return;
+    }
+    T *const out = static_cast<T *>(a.O) + at * a.o.l + row.h * a.o.h;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) store4<T>(out, 16 * j + 4 * (l >> 4), a.Dh, VEC, o[j] * inv);
+    if (a.lse && l < 16) a.lse[at * a.Hq + row.h] = lse;
+}
 
 // ------------------------------------------------------------ few rows
 
@@ -406,14 +643,20 @@ struct Line {
     }
 };
 
+// Keys of a tile for up to R rows.
+template <typename T> constexpr int few_keys(int R) { return R == 16 ? Op16<T>::BN : 32; }
+
 // A range of the line, one head: a wave.  The heads of a range are read side by
 // side, as their states lie in the cache.
-template <typename T, int DC, int BN, bool VEC>
-__global__ void __launch_bounds__(64, (min_waves<T, DC, 1>())) few_kernel(PagedAttnArgs a) {
+template <typename T, int DC, int R, bool VEC>
+__global__ void __launch_bounds__(64, (R == 16 ? 1 : min_waves<T, DC, 1>())) few_kernel(PagedAttnArgs a) {
+    constexpr int BN = few_keys<T>(R);
     constexpr int DP = padded(DC);
     __shared__ __attribute__((aligned(16))) char lds[2 * BN * DP * sizeof(T)];
-    __shared__ int marks[1];
-    const int range = blockIdx.x / a.Hkv, hk = blockIdx.x % a.Hkv;
+    __shared__ int marks[1];        // (32 rows)
+    const int64_t place = logical_group((int64_t)a.ranges * a.Hkv);
+    const int range = (int)(place / a.Hkv), hk = (int)(place % a.Hkv);
+    if (range >= a.ranges) return;
     Line line;
     line.find<BN>(a, range);
     int b = line.b, before = line.before;
@@ -433,7 +676,8 @@ __global__ void __launch_bounds__(64, (min_waves<T, DC, 1>())) few_kernel(PagedA
             part_lse = a.part_lse + slot * a.rows;
         }
         if (x0 == 0 && hk == 0 && threadIdx.x == 0) a.line[b] = before;
-        pass<T, DC, 1, BN, VEC>(a, lds, marks, b, hk, r, 0, x0, x1 < v.tiles ? x1 : v.tiles, part, part_lse);
+        if constexpr (R == 16) pass16<T, DC, VEC>(a, lds, b, hk, r, x0, x1 < v.tiles ? x1 : v.tiles, part, part_lse);
+        else pass<T, DC, 1, BN, VEC>(a, lds, marks, b, hk, r, 0, x0, x1 < v.tiles ? x1 : v.tiles, part, part_lse);
         u += x1 - x0;
         before += tiles;
     }
@@ -628,7 +872,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256) many_join_k
 
 constexpr int FEW = 32;         // packed rows up to which waves work alone
 
-constexpr int tile_keys(gs_dtype t, bool few) { return t == GS_F32 || few ? 32 : 64; }
+constexpr int tile_keys(gs_dtype t) { return t == GS_F32 ? 32 : 64; }
 
 // Sizes of the workspace's parts, by sizes that the host knows.
 struct Layout {
@@ -646,10 +890,10 @@ Layout layout(gs_dtype t, const PagedAttnArgs &a) {
     z.few = rows <= FEW;
     if (z.few) {
         // as many waves as the CUs hold at once, by their registers
-        const int held = t == GS_F32 ? 4 : 8;
+        const int held = t == GS_F32 || rows <= 16 ? 4 : 8;
         z.rows = (int)rows;
         z.least = 4;
-        const int64_t most = ((int64_t)(a.Lk + 31) / 32 + 1) * a.B / z.least + 1, full = 256 * held / a.Hkv;
+        const int64_t most = ((int64_t)a.Lk / 16 + 3) * a.B / z.least + 1, full = 256 * held / a.Hkv;
         z.ranges = (int)(most < full ? most : (full > 1 ? full : 1));
         z.slots = 2 * (int64_t)z.ranges * a.Hkv;
     } else {
@@ -671,20 +915,22 @@ Layout layout(gs_dtype t, const PagedAttnArgs &a) {
     return z;
 }
 
+template <typename T, int DC, int R, bool VEC> hipError_t launch_few(const PagedAttnArgs &a, const Layout &z, hipStream_t s) {
+    constexpr int DP = padded(DC), BN = few_keys<T>(R);
+    few_kernel<T, DC, R, VEC><<<dim3((unsigned)((z.ranges * a.Hkv + 7) / 8 * 8)), dim3(64), 0, s>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || z.ranges == 1) return e;
+    const dim3 rows((unsigned)(a.B * a.Hkv), (unsigned)(a.B * a.Hkv * a.rows <= 16384 ? a.rows : 1));
+    if (z.ranges / a.B >= 32) few_join_kernel<T, DP, BN, 1024><<<rows, dim3(1024), 0, s>>>(a);
+    else few_join_kernel<T, DP, BN, 256><<<rows, dim3(256), 0, s>>>(a);
+    return hipGetLastError();
+}
+
 template <typename T, int DC, bool VEC> hipError_t launch_sized(const PagedAttnArgs &a, const Layout &z, hipStream_t s) {
     constexpr int DP = padded(DC);
     constexpr gs_dtype t = sizeof(T) == 4 ? GS_F32 : GS_BF16;
-    if (z.few) {
-        constexpr int BN = tile_keys(t, true);
-        few_kernel<T, DC, BN, VEC><<<dim3((unsigned)(z.ranges * a.Hkv)), dim3(64), 0, s>>>(a);
-        hipError_t e = hipGetLastError();
-        if (e != hipSuccess || z.ranges == 1) return e;
-        const dim3 rows((unsigned)(a.B * a.Hkv), (unsigned)(a.B * a.Hkv * a.rows <= 16384 ? a.rows : 1));
-        if (z.ranges / a.B >= 32) few_join_kernel<T, DP, BN, 1024><<<rows, dim3(1024), 0, s>>>(a);
-        else few_join_kernel<T, DP, BN, 256><<<rows, dim3(256), 0, s>>>(a);
-        return hipGetLastError();
-    }
-    constexpr int BN = tile_keys(t, false);
+    if (z.few) return z.rows <= 16 ? launch_few<T, DC, 16, VEC>(a, z, s) : launch_few<T, DC, 32, VEC>(a, z, s);
+    constexpr int BN = tile_keys(t);
     plan_kernel<BN><<<dim3(1), dim3(1024), 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -723,7 +969,11 @@ hipError_t launch_paged_attn(gs_dtype t, PagedAttnArgs a, void *ws, hipStream_t 
     while (((int64_t)1 << shift) < a.page) ++shift;
     a.page_magic = (uint32_t)((((unsigned __int128)1 << (31 + shift)) + a.page - 1) / a.page);
     a.page_shift = shift - 1;
-    if (a.page == 1) a.page_magic = 0;
+    if (a.page == 1) a.page_magic = 0, a.page_shift = 0;
+    if (!a.pages) {             // what stands for the first place of a cache without pages
+        a.K = a.V = a.Q;
+        a.k = a.v = SeqStrides{0, 0, 0};
+    }
     if (t == GS_F32) return a.vec ? launch_typed<float, true>(a, z, s) : launch_typed<float, false>(a, z, s);
     return a.vec ? launch_typed<bf16_t, true>(a, z, s) : launch_typed<bf16_t, false>(a, z, s);
 }
