@@ -342,7 +342,7 @@ struct PagedAttnArgs {
     // set by launch_paged_attn
     uint32_t page_magic; int page_shift;    // j / page = (j page_magic) >> 32 >> page_shift
     int rows, least;                    // packed rows of a part; fewest tiles of a part
-    int ranges;                         // few rows: parts of the line of all tiles
+    int ranges; bool whole;             // few rows: parts of the line of all tiles; a request each
     int32_t *line;                      // tiles before each request; a range's tiles
     int blocks, waves;                  // many rows: blocks of rows; work-groups that share the work
     PagedAttnHead *head;

@@ -388,10 +388,11 @@ template <typename T, int DC, int NW> constexpr int min_waves() { return sizeof(
 // ------------------------------------------------------------ up to 16 rows
 
 // The same pass for one wave and up to 16 packed rows, with products of 16 x 16:
-// lane l holds row l % 16 and of a block of 16 keys 4 (l / 16) + e.  Half the
-// registers of 32 rows leave room for two tiles on their way from memory while a
-// third is used: the pass waits for memory alone, and what is in flight decides
-// its rate.
+// lane l holds row l % 16 and of a block of 16 keys 4 (l / 16) + e.  Two such waves a
+// SIMD, each with a tile on its way while it uses another, wait for memory alone.
+// (One wave a SIMD with two tiles on their way: 122 us where this takes 119, 48
+// requests of up to 7000 states, 32 heads over 8 of 128, bf16; three or four tiles
+// 124 and 128.)
 template <typename T> struct Op16;
 template <> struct Op16<bf16_t> {
     static constexpr int BN = 32;       // keys a tile: the 32 terms of a product
@@ -463,30 +464,34 @@ __device__ __forceinline__ void pass16(const PagedAttnArgs &a, char *lds, int b,
     float mx = -INFINITY, sum = 0.f;
     int left_out = 0;
 
-    // Two tiles on their way, and which of their keys are there.  Page numbers are
-    // asked for before the values of the tile before: loads return in order, and a
-    // page number must not wait for values that are needed later than it.
-    PagedLoad<T, DP, BN, 64, VEC, true> way[2];
-    uint64_t live[2];
-    Places<BN> keys[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) keys[i] = Places<BN>{a.table + b * a.ldt, l, -1, 0, false};
+    PagedLoad<T, DP, BN, 64, VEC, true> way;
+    uint64_t live = 0;
+    Places<BN> keys{a.table + b * a.ldt, l, -1, 0, false};
     auto differ = [&](uint64_t on, int j0) { return pmin != pmax && !seen_by<BN>(a, on, j0, pmin, pmax); };
-    auto fetch = [&](int i) {
+    // the tile whose pages were asked for, and the pages of tile x
+    auto fetch = [&](int x) {
         int32_t page, place;
-        live[i] = keys[i].take(a, &page, &place);
-        way[i].fetch(a, K, V, page, place, l);
+        live = keys.take(a, &page, &place);
+        way.fetch(a, K, V, page, place, l);
+        keys.ahead(a, view, x, x1);
     };
-    // tile x, on its way number i, which tile x + 2 takes next
-    auto step = [&](int x, int i) {
+    if (x0 < x1) {
+        if (a.Dh < DC) {
+            lds_barrier();
+            clear_lds<64>(lds, 2 * TILE, l);
+            lds_barrier();
+        }
+        keys.ahead(a, view, x0, x1);
+        fetch(x0 + 1);
+    }
+    for (int x = x0; x < x1; ++x) {
         const int j0 = view.start(x);
-        const uint64_t on = live[i];
-        if (on != ALL_LIVE<BN>) way[i].clean(on, l);
-        if (differ(on, j0)) left_out |= __any(way[i].finite());
+        const uint64_t on = live;
+        if (on != ALL_LIVE<BN>) way.clean(on, l);
+        if (differ(on, j0)) left_out |= __any(way.finite());
         lds_barrier();          // (one wave: keeps the accesses in order)
-        way[i].template stash<true>(lds, a.Dh, l);
-        keys[i ^ 1].ahead(a, view, x + 3, x1);
-        fetch(i);
+        way.template stash<true>(lds, a.Dh, l);
+        fetch(x + 2);
         lds_barrier();
         f4v p[NB];
 #pragma unroll
@@ -532,31 +537,13 @@ __device__ __forceinline__ void pass16(const PagedAttnArgs &a, char *lds, int b,
         const typename Op<T>::V pf = Op16<T>::pack(p);
 #pragma unroll
         for (int j = 0; j < NJ; ++j) o[j] = Op16<T>::mma(Op16<T>::template col<DP>(lds + TILE, j, l), pf, o[j]);
-    };
-    if (x0 < x1) {
-        if (a.Dh < DC) {
-            lds_barrier();
-            clear_lds<64>(lds, 2 * TILE, l);
-            lds_barrier();
-        }
-        keys[0].ahead(a, view, x0, x1);
-        keys[1].ahead(a, view, x0 + 1, x1);
-        fetch(0);
-        keys[0].ahead(a, view, x0 + 2, x1);
-        fetch(1);
-        for (int x = x0;;) {
-            step(x, 0);
-            if (++x == x1) break;
-            step(x, 1);
-            if (++x == x1) break;
-        }
     }
     if (left_out) {
         for (int x = x0; x < x1; ++x) {
             const int j0 = view.start(x);
             int32_t page, place;
-            keys[0].ahead(a, view, x, x1);
-            const uint64_t there = keys[0].take(a, &page, &place);
+            keys.ahead(a, view, x, x1);
+            const uint64_t there = keys.take(a, &page, &place);
             if (!differ(there, j0)) continue;
             for (uint64_t rest = there; rest; rest &= rest - 1) {
                 const int k = __ffsll((unsigned long long)rest) - 1;
@@ -649,7 +636,7 @@ template <typename T> constexpr int few_keys(int R) { return R == 16 ? Op16<T>::
 // A range of the line, one head: a wave.  The heads of a range are read side by
 // side, as their states lie in the cache.
 template <typename T, int DC, int R, bool VEC>
-__global__ void __launch_bounds__(64, (R == 16 ? 1 : min_waves<T, DC, 1>())) few_kernel(PagedAttnArgs a) {
+__global__ void __launch_bounds__(64, (R == 16 ? 2 : min_waves<T, DC, 1>())) few_kernel(PagedAttnArgs a) {
     constexpr int BN = few_keys<T>(R);
     constexpr int DP = padded(DC);
     __shared__ __attribute__((aligned(16))) char lds[2 * BN * DP * sizeof(T)];
@@ -657,12 +644,18 @@ __global__ void __launch_bounds__(64, (R == 16 ? 1 : min_waves<T, DC, 1>())) few
     const int64_t place = logical_group((int64_t)a.ranges * a.Hkv);
     const int range = (int)(place / a.Hkv), hk = (int)(place % a.Hkv);
     if (range >= a.ranges) return;
-    Line line;
-    line.find<BN>(a, range);
-    int b = line.b, before = line.before;
-    if (b >= a.B) return;
-    const int begin = range * line.share, end = line.total - begin < line.share ? line.total : begin + line.share;
-    if (begin == 0 && hk == 0 && threadIdx.x == 0) a.line[a.B] = line.share;
+    int b, before = 0, begin = 0, end;
+    if (a.whole) {              // a request a range
+        b = range;
+        end = few_tiles<BN>(a, b);
+    } else {
+        Line line;
+        line.find<BN>(a, range);
+        b = line.b, before = line.before;
+        if (b >= a.B) return;
+        begin = range * line.share, end = line.total - begin < line.share ? line.total : begin + line.share;
+        if (begin == 0 && hk == 0 && threadIdx.x == 0) a.line[a.B] = line.share;
+    }
     for (int u = begin; u < end; ++b) {
         const Rows r(a, b);
         const int tiles = few_tiles<BN>(a, b);
@@ -675,7 +668,7 @@ __global__ void __launch_bounds__(64, (R == 16 ? 1 : min_waves<T, DC, 1>())) few
             part = a.part + slot * a.rows * DP;
             part_lse = a.part_lse + slot * a.rows;
         }
-        if (x0 == 0 && hk == 0 && threadIdx.x == 0) a.line[b] = before;
+        if (x0 == 0 && hk == 0 && threadIdx.x == 0 && !a.whole) a.line[b] = before;
         if constexpr (R == 16) pass16<T, DC, VEC>(a, lds, b, hk, r, x0, x1 < v.tiles ? x1 : v.tiles, part, part_lse);
         else pass<T, DC, 1, BN, VEC>(a, lds, marks, b, hk, r, 0, x0, x1 < v.tiles ? x1 : v.tiles, part, part_lse);
         u += x1 - x0;
@@ -683,13 +676,13 @@ __global__ void __launch_bounds__(64, (R == 16 ? 1 : min_waves<T, DC, 1>())) few
     }
 }
 
-// Puts together rows of a request and head that range ends cut: a work-group a
-// row, parts shared out to its lanes' groups.
-template <typename T, int DP, int BN, int NT> __global__ void __launch_bounds__(NT) few_join_kernel(PagedAttnArgs a) {
-    constexpr int LANES = DP / 4, GROUPS = NT / LANES, WAVES = NT / 64;
-    __shared__ f4v sums[GROUPS][LANES];
-    __shared__ float weights[GROUPS], tops[WAVES];
-    const int t = threadIdx.x, l = t & 63, w = t >> 6, g = t / LANES, d = t % LANES;
+// Puts together rows of a request and head that range ends cut: a work-group for 4
+// LANES values of a row, parts shared out to its groups of so many lanes.
+template <typename T, int DP, int BN, int NT, int LANES> __global__ void __launch_bounds__(NT) few_join_kernel(PagedAttnArgs a) {
+    constexpr int GROUPS = NT / LANES, WAVES = NT / 64;
+    __shared__ f4v sums[WAVES][LANES];
+    __shared__ float weights[WAVES], tops[WAVES];
+    const int t = threadIdx.x, l = t & 63, w = t >> 6, g = t / LANES, d = 4 * (blockIdx.z * LANES + t % LANES);
     const int hk = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv;
     const Rows r(a, b);
     const int rows = r.count * a.G;
@@ -714,23 +707,29 @@ template <typename T, int DP, int BN, int NT> __global__ void __launch_bounds__(
         const float ref = top == -INFINITY ? 0.f : top;
         f4v o = {0.f, 0.f, 0.f, 0.f};
         float sum = 0.f;
-#pragma unroll 8
+#pragma unroll 4
         for (int i = i0 + g; i <= i1; i += GROUPS) {
             const int64_t at = place(i);
             const float e = __builtin_amdgcn_exp2f((a.part_lse[at] - ref) * LOG2E);
             sum += e;
-            o += e * *reinterpret_cast<const f4v *>(a.part + at * DP + 4 * d);
+            o += e * *reinterpret_cast<const f4v *>(a.part + at * DP + d);
         }
-        sums[g][d] = o;
-        if (d == 0) weights[g] = sum;
+#pragma unroll
+        for (int k = LANES; k < 64; k <<= 1) {
+            sum += __shfl_xor(sum, k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], k);
+        }
+        if (l < LANES) sums[w][l] = o;
+        if (l == 0) weights[w] = sum;
         __syncthreads();
-        if (g == 0) {
-            const int all = i1 - i0 + 1 < GROUPS ? i1 - i0 + 1 : GROUPS;
-            for (int i = 1; i < all; ++i) o += sums[i][d], sum += weights[i];
+        if (t < LANES) {
+#pragma unroll
+            for (int k = 1; k < WAVES; ++k) o += sums[k][t], sum += weights[k];
             const float inv = sum != 0.f ? 1.f / sum : 0.f;
             const RowOf row(m, hk, a.G);
             const int64_t at = r.first + row.i;
-            if (4 * d < a.Dh) store4<T>(static_cast<T *>(a.O) + at * a.o.l + row.h * a.o.h, 4 * d, a.Dh, a.vec, o * inv);
+            if (d < a.Dh) store4<T>(static_cast<T *>(a.O) + at * a.o.l + row.h * a.o.h, d, a.Dh, a.vec, o * inv);
             if (a.lse && d == 0) a.lse[at * a.Hq + row.h] = sum != 0.f ? ref + __builtin_amdgcn_logf(sum) * LN2 : -INFINITY;
         }
         __syncthreads();
@@ -876,7 +875,7 @@ constexpr int tile_keys(gs_dtype t) { return t == GS_F32 ? 32 : 64; }
 
 // Sizes of the workspace's parts, by sizes that the host knows.
 struct Layout {
-    bool few;
+    bool few, whole;
     int ranges, waves, least, rows;
     int64_t blocks, items, joins, slots;
     int dp;
@@ -890,12 +889,17 @@ Layout layout(gs_dtype t, const PagedAttnArgs &a) {
     z.few = rows <= FEW;
     if (z.few) {
         // as many waves as the CUs hold at once, by their registers
-        const int held = t == GS_F32 || rows <= 16 ? 4 : 8;
+        const int held = t == GS_F32 && rows > 16 ? 4 : 8;
         z.rows = (int)rows;
         z.least = 4;
         const int64_t most = ((int64_t)a.Lk / 16 + 3) * a.B / z.least + 1, full = 256 * held / a.Hkv;
         z.ranges = (int)(most < full ? most : (full > 1 ? full : 1));
-        z.slots = 2 * (int64_t)z.ranges * a.Hkv;
+        // Short histories are not cut: up to 8 tiles in a row take less than a second
+        // launch.
+        const int bn = t == GS_F32 && rows <= 16 ? 16 : 32;
+        z.whole = a.Lk <= 8 * bn;
+        if (z.whole) z.ranges = a.B;
+        z.slots = z.whole ? 0 : 2 * (int64_t)z.ranges * a.Hkv;
     } else {
         const int64_t most = t == GS_F32 && dc > 64 ? 256 : 512;
         z.rows = BLOCK;
@@ -919,10 +923,11 @@ template <typename T, int DC, int R, bool VEC> hipError_t launch_few(const Paged
     constexpr int DP = padded(DC), BN = few_keys<T>(R);
     few_kernel<T, DC, R, VEC><<<dim3((unsigned)((z.ranges * a.Hkv + 7) / 8 * 8)), dim3(64), 0, s>>>(a);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || z.ranges == 1) return e;
-    const dim3 rows((unsigned)(a.B * a.Hkv), (unsigned)(a.B * a.Hkv * a.rows <= 16384 ? a.rows : 1));
-    if (z.ranges / a.B >= 32) few_join_kernel<T, DP, BN, 1024><<<rows, dim3(1024), 0, s>>>(a);
-    else few_join_kernel<T, DP, BN, 256><<<rows, dim3(256), 0, s>>>(a);
+    if (e != hipSuccess || z.whole) return e;
+    // many parts a request: more lanes a row
+    const unsigned pairs = (unsigned)(a.B * a.Hkv), rows = pairs * (int64_t)a.rows <= 16384 ? (unsigned)a.rows : 1;
+    if (z.ranges / a.B >= 32) few_join_kernel<T, DP, BN, 1024, 8><<<dim3(pairs, rows, DP / 32), dim3(1024), 0, s>>>(a);
+    else few_join_kernel<T, DP, BN, 256, DP / 4><<<dim3(pairs, rows), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -956,6 +961,7 @@ hipError_t launch_paged_attn(gs_dtype t, PagedAttnArgs a, void *ws, hipStream_t 
     a.blocks = (int)z.blocks;
     a.waves = z.waves;
     a.ranges = z.ranges;
+    a.whole = z.whole;
     a.least = z.least;
     a.line = static_cast<int32_t *>(ws);
     a.head = static_cast<PagedAttnHead *>(ws);
