@@ -341,6 +341,7 @@ struct PagedAttnArgs {
     bool vec;
     // set by launch_paged_attn
     uint32_t page_magic; int page_shift;    // j / page = (j page_magic) >> 32 >> page_shift
+    bool alike;                         // K and V have the same strides
     int rows, least;                    // packed rows of a part; fewest tiles of a part
     int ranges; bool whole;             // few rows: parts of the line of all tiles; a request each
     int32_t *line;                      // tiles before each request; a range's tiles

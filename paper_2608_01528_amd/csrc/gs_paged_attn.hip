@@ -99,15 +99,20 @@ template <int BN> struct Places {
         j = there ? j : 0;
         id = table[page_of(a)];
     }
-    // Lanes' pages and places in them, and the keys that are there (of the tile
-    // last asked for).
-    __device__ __forceinline__ uint64_t take(const PagedAttnArgs &a, int32_t *page, int32_t *at) const {
+    // Where lanes' keys and values lie, in values from the cache's first, and the
+    // keys that are there (of the tile last asked for).
+    __device__ __forceinline__ uint64_t take(const PagedAttnArgs &a, int64_t *k, int64_t *v) const {
         const bool on = there && id >= 0 && id < a.pages;
-        *page = on ? id : 0;
-        *at = on ? j - page_of(a) * a.page : 0;
+        const int g = on ? id : 0, i = on ? j - page_of(a) * a.page : 0;
+        *k = g * a.k.b + i * a.k.l;
+        *v = g * a.v.b + i * a.v.l;
         return __ballot(on);
     }
 };
+__device__ __forceinline__ int64_t from_lane(int64_t x, int lane) {
+    const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)x, lane), hi = (uint32_t)__shfl((int)(x >> 32), lane);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
 
 // A tile's place in LDS for blocks of 16 rows: as place() for bf16; in fp32 the
 // rows 4 g + e of four groups of lanes g, read 16 values each, lie in different
@@ -133,15 +138,19 @@ template <typename T, int DP, int BN, int NT, bool VEC, bool ONCE> struct PagedL
         else if constexpr (VEC) return *reinterpret_cast<const u4v *>(row + PER * c);
         else return load_chunk<T>(row, PER * c, dh, false);
     }
-    __device__ __forceinline__ void fetch(const PagedAttnArgs &a, const T *K, const T *V, int32_t page, int32_t at, int t) {
+    // the rows at K + ks and V + vs of the lanes
+    __device__ __forceinline__ void fetch(const PagedAttnArgs &a, const T *K, const T *V, int64_t ks, int64_t vs, int t) {
         const int c = piece(t, a.Dh), r0 = t / CPR;
-        int32_t g[N], i[N];
+        int64_t at[N];
 #pragma unroll
-        for (int q = 0; q < N; ++q) g[q] = __shfl(page, r0 + q * RPI), i[q] = __shfl(at, r0 + q * RPI);
+        for (int q = 0; q < N; ++q) at[q] = from_lane(ks, r0 + q * RPI);
 #pragma unroll
-        for (int q = 0; q < N; ++q) k[q] = load(K + g[q] * a.k.b + i[q] * a.k.l, c, a.Dh);
+        for (int q = 0; q < N; ++q) k[q] = load(K + at[q], c, a.Dh);
+        if (!a.alike)
 #pragma unroll
-        for (int q = 0; q < N; ++q) v[q] = load(V + g[q] * a.v.b + i[q] * a.v.l, c, a.Dh);
+            for (int q = 0; q < N; ++q) at[q] = from_lane(vs, r0 + q * RPI);
+#pragma unroll
+        for (int q = 0; q < N; ++q) v[q] = load(V + at[q], c, a.Dh);
     }
     // K's tile, and V's behind it; BLOCK16: for blocks of 16 rows
     template <bool BLOCK16> __device__ __forceinline__ void stash(char *tile, int dh, int t) const {
@@ -241,9 +250,9 @@ __device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, int *mar
     PagedLoad<T, DP, BN, NT, VEC, NW == 1> way;
     uint64_t live = 0, next_live = 0;
     auto fetch = [&]() {
-        int32_t page, place;
-        const uint64_t on = keys.take(a, &page, &place);
-        way.fetch(a, K, V, page, place, t);
+        int64_t ks, vs;
+        const uint64_t on = keys.take(a, &ks, &vs);
+        way.fetch(a, K, V, ks, vs, t);
         return on;
     };
     // Rows of the block see different states of the tile: a product takes 0 inf and 0
@@ -339,15 +348,14 @@ __device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, int *mar
     if (left_out) {             // they are added now, to the rows that see them
         for (int x = x0; x < x1; ++x) {
             const int j0 = view.start(x);
-            int32_t page, place;
+            int64_t ks, vs;
             keys.ahead(a, view, x, x1);
-            const uint64_t there = keys.take(a, &page, &place);
+            const uint64_t there = keys.take(a, &ks, &vs);
             if (!differ(there, j0)) continue;
             for (uint64_t rest = there; rest; rest &= rest - 1) {
                 const int k = __ffsll((unsigned long long)rest) - 1, j = j0 + k;
-                const int32_t g = __builtin_amdgcn_readlane(page, k), i = __builtin_amdgcn_readlane(place, k);
                 const bool sees = j <= pos && (!a.window || pos - j < a.window || j < a.sinks);
-                if (sees) add_not_finite<T, NJ>(o, V + g * a.v.b + i * a.v.l, a.Dh, l);
+                if (sees) add_not_finite<T, NJ>(o, V + lane_value(vs, k), a.Dh, l);
             }
         }
     }
@@ -470,9 +478,9 @@ __device__ __forceinline__ void pass16(const PagedAttnArgs &a, char *lds, int b,
     auto differ = [&](uint64_t on, int j0) { return pmin != pmax && !seen_by<BN>(a, on, j0, pmin, pmax); };
     // the tile whose pages were asked for, and the pages of tile x
     auto fetch = [&](int x) {
-        int32_t page, place;
-        live = keys.take(a, &page, &place);
-        way.fetch(a, K, V, page, place, l);
+        int64_t ks, vs;
+        live = keys.take(a, &ks, &vs);
+        way.fetch(a, K, V, ks, vs, l);
         keys.ahead(a, view, x, x1);
     };
     if (x0 < x1) {
@@ -541,14 +549,13 @@ __device__ __forceinline__ void pass16(const PagedAttnArgs &a, char *lds, int b,
     if (left_out) {
         for (int x = x0; x < x1; ++x) {
             const int j0 = view.start(x);
-            int32_t page, place;
+            int64_t ks, vs;
             keys.ahead(a, view, x, x1);
-            const uint64_t there = keys.take(a, &page, &place);
+            const uint64_t there = keys.take(a, &ks, &vs);
             if (!differ(there, j0)) continue;
             for (uint64_t rest = there; rest; rest &= rest - 1) {
                 const int k = __ffsll((unsigned long long)rest) - 1;
-                const int32_t g = __builtin_amdgcn_readlane(page, k), i = __builtin_amdgcn_readlane(place, k);
-                const T *const from = V + g * a.v.b + i * a.v.l;
+                const T *const from = V + lane_value(vs, k);
                 if (!((seen_bits(a, pos, j0) >> k) & 1)) continue;
 #pragma unroll
                 for (int j = 0; j < NJ; ++j)
@@ -976,6 +983,7 @@ hipError_t launch_paged_attn(gs_dtype t, PagedAttnArgs a, void *ws, hipStream_t 
     a.page_magic = (uint32_t)((((unsigned __int128)1 << (31 + shift)) + a.page - 1) / a.page);
     a.page_shift = shift - 1;
     if (a.page == 1) a.page_magic = 0, a.page_shift = 0;
+    a.alike = a.k.b == a.v.b && a.k.l == a.v.l;
     if (!a.pages) {             // what stands for the first place of a cache without pages
         a.K = a.V = a.Q;
         a.k = a.v = SeqStrides{0, 0, 0};
