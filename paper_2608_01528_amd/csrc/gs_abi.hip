@@ -1167,9 +1167,6 @@ gs_status gs_verify(const gs_drafts *p, gs_dtype pt, void *ws, size_t ws_bytes, 
     a.B = p->B; a.N = p->N; a.M = p->M; a.P = p->P; a.ldp = p->ldp; a.Q = p->Q; a.ldq = p->ldq;
     a.drafted = p->drafted; a.u = p->u; a.v = p->v; a.qoff = p->qoff;
     a.accepted = p->accepted; a.entry = p->entry; a.entries = p->entries;
-    const int64_t per = 16 / (int64_t)es;
-    a.vec_p = reinterpret_cast<uintptr_t>(p->P) % 16 == 0 && (p->N <= 1 || p->ldp % per == 0);
-    a.vec_q = reinterpret_cast<uintptr_t>(p->Q) % 16 == 0 && (p->N <= 1 || p->ldq % per == 0);
     return launched(launch_verify(pt, a, ws, (hipStream_t)stream), fn);
 }
 

@@ -355,6 +355,7 @@ size_t paged_attn_workspace(gs_dtype t, const PagedAttnArgs &a);
 hipError_t launch_paged_attn(gs_dtype t, PagedAttnArgs a, void *ws, hipStream_t s);
 
 // Drafted entries (gs_verify.hip).
+struct VerifyRequest { int64_t first, n, taken; int32_t refused; };     // a request's rows, drafts taken, the one refused
 struct VerifyArgs {
     int64_t B, N, M;
     const void *P; int64_t ldp;
@@ -363,10 +364,10 @@ struct VerifyArgs {
     const float *u, *v;
     const int32_t *qoff;
     int32_t *accepted, *entry, *entries;
-    bool vec_p, vec_q;                  // rows start on 16-byte boundaries
     // set by launch_verify
     int64_t parts;
     double *sums;                       // B x parts x 2
+    VerifyRequest *requests;
 };
 int64_t verify_groups(int64_t B, int64_t M);
 size_t verify_workspace(int64_t B, int64_t M);

@@ -104,46 +104,63 @@ __device__ void plan_sums(const PagedPlanArgs &a, int32_t *left, int32_t *back, 
 }
 
 // The last b with sums[b] <= i (sums[0] = 0, sums[B] > i).
-__device__ __forceinline__ int64_t owner(const int32_t *sums, int64_t B, int64_t i) {
-    int64_t lo = 0, hi = B;
+__device__ __forceinline__ int owner(const int32_t *sums, int B, int i) {
+    int lo = 0, hi = B;
     while (hi - lo > 1) {
-        const int64_t mid = (lo + hi) >> 1;
+        const int mid = (int)((uint32_t)(lo + hi) >> 1);
         if (sums[mid] <= i) lo = mid;
         else hi = mid;
     }
     return lo;
 }
 
-// Pages and slots number `first`, first + step, ...
+// Pages given back, pages taken and slots lie in one line, of which this does
+// number `first`, first + step, ...: one copy of the code for all three, which a
+// launch reads from memory each time.
 __device__ void plan_fill(const PagedPlanArgs &a, const PlanSums &z, const PlanHead &head, int64_t first, int64_t step) {
-    const int64_t B = a.B, page = a.page;
-    auto returned = [&](int64_t i) {
-        const int64_t b = owner(z.back, B, i);
-        return a.table[b * a.ldt + up(z.left[b], page) + (i - z.back[b])];
-    };
-    // the i-th page taken comes from the end of the free ones and the returned
-    // ones behind them
-    auto fresh = [&](int64_t i) {
-        const int64_t at = (int64_t)head.avail - 1 - i;
-        return at < head.nfree ? a.free_pages[at] : returned(at - head.nfree);
-    };
-    for (int64_t i = first; i < head.back; i += step) a.free_pages[(int64_t)head.nfree + i] = returned(i);
-    for (int64_t i = first; i < head.taken; i += step) {
-        const int64_t b = owner(z.take, B, i);
-        a.table[b * a.ldt + up(z.left[b], page) + (i - z.take[b])] = fresh(i);
-    }
-    const int64_t rows = B ? z.qoff[B] : 0;
-    for (int64_t r = first; r < a.rows; r += step) {
-        int64_t slot = -1;
-        if (r < rows) {
-            const int64_t b = owner(z.qoff, B, r), left = z.left[b];
-            if (left >= 0) {
-                const int64_t at = left + (r - z.qoff[b]), held = up(left, page), g = (uint32_t)at / (uint32_t)page;
-                const int64_t id = g < held ? a.table[b * a.ldt + g] : fresh(z.take[b] + (g - held));
-                if (id >= 0) slot = id * page + (at - g * page);
-            }
+    const int B = (int)a.B;
+    const int64_t ends[2] = {head.back, (int64_t)head.back + head.taken}, total = ends[1] + a.rows;
+    const int rows = B ? z.qoff[B] : 0;
+    for (int64_t i = first; i < total; i += step) {
+        const int kind = (i >= ends[0]) + (i >= ends[1]);
+        const int k = (int)(i - (kind ? ends[kind - 1] : 0));
+        const int32_t *const sums = kind == 0 ? z.back : (kind == 1 ? z.take : z.qoff);
+        int32_t id = -1;
+        int64_t left = -1, held = 0, at = 0;
+        int b = 0;
+        if (kind < 2 || k < rows) {
+            b = owner(sums, B, k);
+            left = z.left[b];
         }
-        a.slots[r] = slot;
+        if (left >= 0) {
+            held = up(left, a.page);
+            const int off = k - sums[b];
+            int taken = -1;             // its number among the pages taken
+            const int32_t *from = a.table + b * a.ldt;
+            if (kind == 0) {
+                from += held + off;
+            } else if (kind == 1) {
+                taken = k;
+                at = held + off;
+            } else {
+                const int64_t p = left + off, g = (uint32_t)p / (uint32_t)a.page;
+                at = p - g * a.page;
+                if (g < held) from += g;
+                else taken = z.take[b] + (int)(g - held);
+            }
+            if (taken >= 0) {           // from the end of the free pages and the returned ones behind them
+                const int pos = head.avail - 1 - taken;
+                from = a.free_pages + pos;
+                if (pos >= head.nfree) {
+                    const int c = owner(z.back, B, pos - head.nfree);
+                    from = a.table + c * a.ldt + up(z.left[c], a.page) + (pos - head.nfree - z.back[c]);
+                }
+            }
+            id = *from;
+        }
+        if (kind == 0) a.free_pages[(int64_t)head.nfree + k] = id;
+        else if (kind == 1) a.table[b * a.ldt + at] = id;
+        else a.slots[k] = id < 0 ? -1 : id * a.page + at;
     }
 }
 

@@ -1,24 +1,25 @@
 // Drafted entries taken or refused, and the entry after them drawn (gs_verify).
 //
 // Which drafts are taken needs two gathered numbers a draft; then one row of P
-// (and of Q) is read for the draw.  Its weights are summed and searched in parts
-// of PART entries: a row of one part stays in registers, longer rows take a
-// launch for the parts' sums and one that searches them and reads the part that
-// the draw falls into once more.  Sums are fp64 in a fixed order (lanes, waves,
-// pieces, parts): a draw depends on their last bits alone.
-#include "gs_internal.h"
+// (and of Q) is read for the draw.  A thread holds a few consecutive entries of it;
+// one prefix sum over the threads gives the total and says which of them holds the
+// entry.  Rows of up to ONE entries are a work-group's; longer ones take a launch in
+// which each wave sums UNIT entries, and one that finds the unit and reads it once
+// more.  Sums are fp64 in a fixed order.  What bounds it is a chain of dependent
+// loads (offsets, drafts, their probabilities, the row) and, as each instruction
+// runs once, the reading of the code: a thread holds no more than the row needs.
+#include "gs_scan.h"
 
 namespace gs {
 namespace {
 
-constexpr int GROUP = 256, WAVES = GROUP / 64;
-constexpr int HELD = 16, PART = GROUP * HELD;       // entries a thread holds, a work-group holds
-
-typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+constexpr int WAVES = 4, GROUP = 64 * WAVES;
+constexpr int ONE = 16 * GROUP;         // entries of a row that a work-group holds
+constexpr int UNIT = 1024;              // entries that a wave sums, and a work-group searches
 
 // Negative numbers, infinities and NaN have no weight.
-__device__ __forceinline__ double weight(float x) { return x > 0.f && x < INFINITY ? (double)x : 0.; }
-template <typename T> __device__ __forceinline__ float widen(const T *p, int64_t i) { return ld_f32<T>(p, i); }
+__device__ __forceinline__ float weighed(float x) { return x > 0.f && x < INFINITY ? x : 0.f; }
+template <typename T> __device__ __forceinline__ double weight(const T *p, int64_t i) { return weighed(ld_f32<T>(p, i)); }
 
 __device__ __forceinline__ int64_t bounded(const int32_t *qoff, int64_t b, int64_t N) {
     const int64_t x = qoff[b];
@@ -48,8 +49,8 @@ template <typename T> __device__ __forceinline__ Request request(const VerifyArg
             const float u = a.u[row];
             double p = 0., q = 0.;
             if (x >= 0 && x < a.M) {
-                p = weight(widen(static_cast<const T *>(a.P), row * a.ldp + x));
-                q = a.Q ? weight(widen(static_cast<const T *>(a.Q), row * a.ldq + x)) : 1.;
+                p = weight(static_cast<const T *>(a.P), row * a.ldp + x);
+                q = a.Q ? weight(static_cast<const T *>(a.Q), row * a.ldq + x) : 1.;
             }
             ok = (u > 0.f ? (double)u : 0.) * q < p;
         }
@@ -65,110 +66,127 @@ template <typename T> __device__ __forceinline__ Request request(const VerifyArg
     return r;
 }
 
-// The weights of a part's entries that a thread holds: piece s, V consecutive
-// entries at base + s GROUP V + V t.
-template <typename T> struct Part {
-    static constexpr int V = 16 / sizeof(T), PIECES = HELD / V;
-    float p[HELD], q[HELD];
+// The weights of H consecutive entries.
+template <typename T, int H> struct Part {
+    float p[H], q[H];
     int64_t at;
     bool less;          // weights max(p - q, 0)
-    static __device__ __forceinline__ void fetch(float (&v)[HELD], const T *row, int64_t at, int64_t M, bool vec) {
+    // (rows start on any boundary: loads of 16 or 8 bytes need that of an entry)
+    static __device__ __forceinline__ void fetch(float (&v)[H], const T *row, int64_t at, int64_t M) {
+        constexpr int V = 4;
+        typedef uint32_t word __attribute__((ext_vector_type(V * sizeof(T) / 4), aligned(sizeof(T))));
+        if (at + H <= M) {
 #pragma unroll
-        for (int s = 0; s < PIECES; ++s) {
-            const int64_t j = at + (int64_t)s * GROUP * V;
-            if (vec && j + V <= M) {
-                const u4v x = *reinterpret_cast<const u4v *>(row + j);
+            for (int s = 0; s < H; s += V) {
+                const word x = *reinterpret_cast<const word *>(row + at + s);
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    if constexpr (sizeof(T) == 4) v[s * V + e] = __uint_as_float(x[e]);
-                    else v[s * V + e] = bf16_to_f32((uint16_t)(x[e / 2] >> (16 * (e & 1))));
+                    if constexpr (sizeof(T) == 4) v[s + e] = weighed(__uint_as_float(x[e]));
+                    else v[s + e] = weighed(__uint_as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16));
                 }
-            } else {
-#pragma unroll
-                for (int e = 0; e < V; ++e) v[s * V + e] = j + e < M ? widen(row, j + e) : 0.f;
             }
-        }
-    }
-    __device__ __forceinline__ void load(const VerifyArgs &a, const Request &r, int64_t part) {
-        const int64_t row = r.first + r.taken;
-        at = part * PART + (int64_t)V * threadIdx.x;
-        less = r.taken < r.n - 1;
-        fetch(p, static_cast<const T *>(a.P) + row * a.ldp, at, a.M, a.vec_p);
-        if (!less) return;
-        if (a.Q) {
-            fetch(q, static_cast<const T *>(a.Q) + row * a.ldq, at, a.M, a.vec_q);
         } else {
 #pragma unroll
-            for (int k = 0; k < HELD; ++k) q[k] = at + (int64_t)(k / V) * GROUP * V + k % V == r.refused ? 1.f : 0.f;
+            for (int e = 0; e < H; ++e) v[e] = 0.f;
+            if (at < M)
+#pragma unroll
+                for (int e = 0; e < H; ++e)
+                    if (at + e < M) v[e] = weighed(ld_f32<T>(row, at + e));
         }
     }
-    __device__ __forceinline__ double w(int k) const {
-        const double x = weight(p[k]);
-        return less ? fmax(x - weight(q[k]), 0.) : x;
+    __device__ __forceinline__ void load(const VerifyArgs &a, const Request &r, int64_t from) {
+        const int64_t row = r.first + r.taken;
+        at = from;
+        less = r.taken < r.n - 1;
+        fetch(p, static_cast<const T *>(a.P) + row * a.ldp, at, a.M);
+        if (less && a.Q) {
+            fetch(q, static_cast<const T *>(a.Q) + row * a.ldq, at, a.M);
+        } else {
+#pragma unroll
+            for (int k = 0; k < H; ++k) q[k] = less && at + k == r.refused ? 1.f : 0.f;
+        }
+    }
+    __device__ __forceinline__ double w(int k) const { return fmax((double)p[k] - (double)q[k], 0.); }
+    __device__ __forceinline__ double sum() const {
+        double x = 0.;
+#pragma unroll
+        for (int k = 0; k < H; ++k) x += w(k);
+        return x;
+    }
+    __device__ __forceinline__ double sum_p() const {
+        double x = 0.;
+#pragma unroll
+        for (int k = 0; k < H; ++k) x += (double)p[k];
+        return x;
+    }
+    __device__ __forceinline__ void forget_q() {
+        less = false;
+#pragma unroll
+        for (int k = 0; k < H; ++k) q[k] = 0.f;
     }
 };
 
-__device__ __forceinline__ double wave_sum(double x) {
+// Sums over the threads before this one and over all; room: NW values that are not
+// in use.
+template <int NW> __device__ __forceinline__ double sums_before(double mine, double *room, double *total) {
+    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const double upto = wave_upto(mine);
+    if constexpr (NW == 1) {
+        *total = lane_value(upto, 63);
+        return upto - mine;
+    }
+    if (l == 63) room[w] = upto;
+    __syncthreads();
+    double before = 0., all = 0.;
 #pragma unroll
-    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
-    return x;
+    for (int v = 0; v < NW; ++v) {
+        if (v < w) before += room[v];
+        all += room[v];
+    }
+    *total = all;
+    return before + (upto - mine);
 }
 
-// The entry at which the sum of the part's weights passes `target`, which is
-// below their total but for rounding (infinite: the last of any weight); -1 if
-// none has any.
-template <typename T> __device__ __forceinline__ int64_t search(const Part<T> &part, double target) {
-    constexpr int V = Part<T>::V, PIECES = Part<T>::PIECES;
-    __shared__ double sums[PIECES][WAVES];
-    __shared__ unsigned long long found, last;
-    const int t = threadIdx.x, l = t & 63, w = t >> 6;
-    if (t == 0) found = ~0ull, last = 0;
-    double mine[PIECES];
-    int64_t top = -1;
-#pragma unroll
-    for (int s = 0; s < PIECES; ++s) {
-        mine[s] = 0.;
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const double x = part.w(s * V + e);
-            mine[s] += x;
-            if (x > 0.) top = part.at + (int64_t)s * GROUP * V + e;
-        }
-        const double all = wave_sum(mine[s]);
-        if (l == 0) sums[s][w] = all;
-    }
+// The first number of a wave's lanes that have one, and the last.  (Lanes hold
+// rising numbers, so no atomics are needed.)
+struct Ends { int64_t first, last; };
+__device__ __forceinline__ Ends ends_of(bool hit, int64_t at, bool any, int64_t top) {
+    const uint64_t h = __ballot(hit), n = __ballot(any);
+    return Ends{h ? lane_value(at, __ffsll((unsigned long long)h) - 1) : -1, n ? lane_value(top, 63 - __clzll((long long)n)) : -1};
+}
+// The same over the waves of a work-group; room: NW values that are not in use.
+template <int NW> __device__ __forceinline__ Ends group_ends(Ends e, Ends *room) {
+    if constexpr (NW == 1) return e;
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = e;
     __syncthreads();
-    double before = 0.;         // of the pieces and waves before this one
+    e = Ends{-1, -1};
 #pragma unroll
-    for (int s = 0; s < PIECES; ++s) {
-        double here = before;
+    for (int v = 0; v < NW; ++v) {
+        const Ends x = room[v];
+        if (e.first < 0) e.first = x.first;
+        if (x.last >= 0) e.last = x.last;
+    }
+    return e;
+}
+
+// The entry at which the sum of the weights passes `target`, which is below their
+// total but for rounding (infinite: the last of any weight); -1 if none has any.
+// before: the sum over the threads before this one.
+template <int NW, typename T, int H>
+__device__ __forceinline__ int64_t search(const Part<T, H> &part, double before, double target, Ends *room) {
+    double c = before;
+    int top = -1, hit = H;
 #pragma unroll
-        for (int v = 0; v < WAVES; ++v) {
-            if (v < w) here += sums[s][v];
-            before += sums[s][v];
-        }
-        if (!(target < here + sums[s][w])) continue;       // (wave-uniform)
-        // exclusive sums of the lanes' weights
-        double c = mine[s];
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const double x = __shfl_up(c, d);
-            if (l >= d) c += x;
-        }
-        c = here + c - mine[s];
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const double x = part.w(s * V + e);
-            c += x;
-            if (x > 0. && c > target) {
-                atomicMin(&found, (unsigned long long)(part.at + (int64_t)s * GROUP * V + e));
-                break;
-            }
+    for (int k = 0; k < H; ++k) {
+        const double x = part.w(k);
+        c += x;
+        if (x > 0.) {
+            top = k;
+            if (c > target && hit == H) hit = k;
         }
     }
-    if (top >= 0) atomicMax(&last, (unsigned long long)(top + 1));
-    __syncthreads();
-    return found != ~0ull ? (int64_t)found : (int64_t)last - 1;
+    const Ends e = group_ends<NW>(ends_of(hit < H, part.at + hit, top >= 0, part.at + top), room);
+    return e.first >= 0 ? e.first : e.last;
 }
 
 // target of a draw: v of the total, from 1 on beyond every sum
@@ -182,156 +200,134 @@ __device__ __forceinline__ void write_out(const VerifyArgs &a, int64_t b, const 
         a.entry[b] = (int32_t)entry;
     }
     if (a.entries)
-        for (int64_t i = threadIdx.x; i < r.n; i += GROUP)
+        for (int64_t i = threadIdx.x; i < r.n; i += blockDim.x)
             a.entries[r.first + i] = i < r.taken ? a.drafted[r.first + i] : (i == r.taken ? (int32_t)entry : -1);
 }
 
-// Sum over the work-group; room: WAVES values that are not in use.
-__device__ __forceinline__ double group_sum(double x, double *room) {
-    const double s = wave_sum(x);
-    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = s;
-    __syncthreads();
-    double all = 0.;
-#pragma unroll
-    for (int v = 0; v < WAVES; ++v) all += room[v];
-    return all;
-}
-
-// Rows of one part: a work-group a request.
-template <typename T> __global__ void __launch_bounds__(GROUP) verify_kernel(VerifyArgs a) {
-    __shared__ double room[2][WAVES];
+// Rows of up to 64 NW H entries: a work-group of NW waves a request.
+template <typename T, int NW, int H> __global__ void __launch_bounds__(64 * NW) verify_kernel(VerifyArgs a) {
+    __shared__ double room[2][NW];
+    __shared__ Ends ends[NW];
     const int64_t b = blockIdx.x;
+    const float v = a.v[b];
     const Request r = request<T>(a, b);
     int64_t entry = -1;
     if (r.n) {
-        Part<T> part;
-        part.load(a, r, 0);
-        double mine = 0.;
-#pragma unroll
-        for (int k = 0; k < HELD; ++k) mine += part.w(k);
-        double total = group_sum(mine, room[0]);
+        Part<T, H> part;
+        part.load(a, r, H * threadIdx.x);
+        double mine = part.sum(), total;
+        double before = sums_before<NW>(mine, room[0], &total);
         if (total == 0. && part.less) {
-            part.less = false;
-            mine = 0.;
-#pragma unroll
-            for (int k = 0; k < HELD; ++k) mine += part.w(k);
-            total = group_sum(mine, room[1]);
+            part.forget_q();
+            mine = part.sum_p();
+            before = sums_before<NW>(mine, room[1], &total);
         }
-        entry = search<T>(part, target_of(a.v[b], total));
+        entry = search<NW>(part, before, target_of(v, total), ends);
     }
     write_out(a, b, r, entry);
 }
 
-// The sums of a part: of its weights, and of p.
+// The sums of a wave's unit: of its weights, and of p.
 template <typename T> __global__ void __launch_bounds__(GROUP) verify_sums_kernel(VerifyArgs a) {
-    __shared__ double room[2][WAVES];
-    const int64_t b = blockIdx.x / a.parts, k = blockIdx.x % a.parts;
+    const int64_t groups = (a.parts + WAVES - 1) / WAVES;
+    const int64_t b = blockIdx.x / groups, k = blockIdx.x % groups * WAVES + (threadIdx.x >> 6);
+    const int l = threadIdx.x & 63;
     const Request r = request<T>(a, b);
-    if (!r.n) return;
-    Part<T> part;
-    part.load(a, r, k);
-    double w = 0., p = 0.;
-#pragma unroll
-    for (int i = 0; i < HELD; ++i) w += part.w(i), p += weight(part.p[i]);
-    w = group_sum(w, room[0]);
-    p = group_sum(p, room[1]);
-    if (threadIdx.x == 0) {
+    if (k == 0 && l == 0) a.requests[b] = VerifyRequest{r.first, r.n, r.taken, r.refused};
+    if (!r.n || k >= a.parts) return;
+    constexpr int H = UNIT / 64;
+    Part<T, H> part;
+    part.load(a, r, k * UNIT + H * l);
+    const double w = wave_upto(part.sum()), p = wave_upto(part.sum_p());
+    if (l == 63) {
         a.sums[2 * (b * a.parts + k)] = w;
         a.sums[2 * (b * a.parts + k) + 1] = p;
     }
 }
 
 template <typename T> __global__ void __launch_bounds__(GROUP) verify_draw_kernel(VerifyArgs a) {
-    __shared__ double room[2][WAVES];
-    __shared__ unsigned long long found, last;
-    __shared__ double before;
-    const int t = threadIdx.x, l = t & 63, w = t >> 6;
+    __shared__ double room[4][WAVES], before;
+    __shared__ Ends ends[3][WAVES];
+    const int t = threadIdx.x;
     const int64_t b = blockIdx.x;
-    const Request r = request<T>(a, b);
+    const VerifyRequest given = a.requests[b];
+    const Request r{given.first, given.n, given.taken, given.refused};
     if (!r.n) {
         write_out(a, b, r, -1);
         return;
     }
+    const float v = a.v[b];
     const double *const sums = a.sums + 2 * b * a.parts;
     double wt = 0., pt = 0.;
     for (int64_t k = t; k < a.parts; k += GROUP) wt += sums[2 * k], pt += sums[2 * k + 1];
-    wt = group_sum(wt, room[0]);
-    pt = group_sum(pt, room[1]);
+    double mine = wt;
+    (void)sums_before<WAVES>(mine, room[0], &wt);
+    mine = pt;
+    (void)sums_before<WAVES>(mine, room[1], &pt);
     const int from = wt > 0. ? 0 : 1;
-    const double total = from ? pt : wt, target = target_of(a.v[b], total);
-    if (t == 0) found = ~0ull, last = 0;
-    // the part in which the sum passes the target, GROUP parts at a time
+    const double target = target_of(v, from ? pt : wt);
+    // the unit in which the sum passes the target, GROUP units at a time
     double carry = 0.;
-    int64_t top = -1;
-    for (int64_t k0 = 0; k0 < a.parts; k0 += GROUP) {
-        const int64_t k = k0 + t;
-        const double x = k < a.parts ? sums[2 * k + from] : 0.;
-        double c = x;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const double y = __shfl_up(c, d);
-            if (l >= d) c += y;
-        }
-        __syncthreads();
-        if (l == 63) room[0][w] = c;
-        __syncthreads();
-        double all = 0., here = carry;
-#pragma unroll
-        for (int v = 0; v < WAVES; ++v) {
-            if (v < w) here += room[0][v];
-            all += room[0][v];
-        }
+    int64_t k = -1, last = -1;
+    int turn = 0;
+    for (int64_t k0 = 0; k0 < a.parts && k < 0; k0 += GROUP, turn ^= 1) {
+        const int64_t i = k0 + t;
+        const double x = i < a.parts ? sums[2 * i + from] : 0.;
+        double all;
+        const double here = carry + sums_before<WAVES>(x, room[2 + turn], &all);
         carry += all;
-        if (x > 0.) {
-            top = k;
-            if (here + c > target) atomicMin(&found, (unsigned long long)k);
-        }
-        __syncthreads();
-        if (found != ~0ull) {
-            if (found == (unsigned long long)k) before = here + c - x;
-            break;
-        }
+        const bool hit = x > 0. && here + x > target;
+        const Ends e = group_ends<WAVES>(ends_of(hit, i, x > 0., i), ends[turn]);
+        k = e.first;
+        if (e.last >= 0) last = e.last;
+        if (k >= 0 && k == i) before = here;
     }
-    if (top >= 0) atomicMax(&last, (unsigned long long)(top + 1));
     __syncthreads();
-    const bool hit = found != ~0ull;
-    const int64_t k = hit ? (int64_t)found : (int64_t)last - 1;
+    const double rest = k >= 0 ? target - before : (double)INFINITY;
+    if (k < 0) k = last;
     int64_t entry = -1;
     if (k >= 0) {
-        Part<T> part;
-        part.load(a, r, k);
-        if (from) part.less = false;
-        entry = search<T>(part, hit ? target - before : (double)INFINITY);
+        Part<T, UNIT / GROUP> part;
+        part.load(a, r, k * UNIT + UNIT / GROUP * t);
+        if (from) part.forget_q();
+        double all;
+        const double at = sums_before<WAVES>(part.sum(), room[0], &all);
+        entry = search<WAVES>(part, at, rest, ends[2]);
     }
     write_out(a, b, r, entry);
 }
 
-int64_t parts_of(int64_t M) { return (M + PART - 1) / PART; }
+int64_t parts_of(int64_t M) { return M <= ONE ? 1 : (M + UNIT - 1) / UNIT; }
 
 template <typename T> hipError_t launch_typed(const VerifyArgs &a, hipStream_t s) {
+    const dim3 grid((unsigned)a.B);
     if (a.parts == 1) {
-        verify_kernel<T><<<dim3((unsigned)a.B), dim3(GROUP), 0, s>>>(a);
+        if (a.M <= 256) verify_kernel<T, 1, 4><<<grid, dim3(64), 0, s>>>(a);
+        else if (a.M <= GROUP * 4) verify_kernel<T, WAVES, 4><<<grid, dim3(GROUP), 0, s>>>(a);
+        else if (a.M <= GROUP * 8) verify_kernel<T, WAVES, 8><<<grid, dim3(GROUP), 0, s>>>(a);
+        else verify_kernel<T, WAVES, 16><<<grid, dim3(GROUP), 0, s>>>(a);
         return hipGetLastError();
     }
-    verify_sums_kernel<T><<<dim3((unsigned)(a.B * a.parts)), dim3(GROUP), 0, s>>>(a);
+    verify_sums_kernel<T><<<dim3((unsigned)(a.B * ((a.parts + WAVES - 1) / WAVES))), dim3(GROUP), 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    verify_draw_kernel<T><<<dim3((unsigned)a.B), dim3(GROUP), 0, s>>>(a);
+    verify_draw_kernel<T><<<grid, dim3(GROUP), 0, s>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t verify_groups(int64_t B, int64_t M) { return B * parts_of(M); }
+int64_t verify_groups(int64_t B, int64_t M) { return B * ((parts_of(M) + WAVES - 1) / WAVES); }
 
 size_t verify_workspace(int64_t B, int64_t M) {
     const int64_t parts = parts_of(M);
-    return parts == 1 ? 0 : (size_t)(B * parts) * 16;
+    return parts == 1 ? 0 : (size_t)(B * parts) * 16 + (size_t)B * sizeof(VerifyRequest);
 }
 
 hipError_t launch_verify(gs_dtype pt, VerifyArgs a, void *ws, hipStream_t s) {
     a.parts = parts_of(a.M);
     a.sums = static_cast<double *>(ws);
+    a.requests = reinterpret_cast<VerifyRequest *>(a.sums + 2 * a.B * a.parts);
     return pt == GS_F32 ? launch_typed<float>(a, s) : launch_typed<bf16_t>(a, s);
 }
 
