@@ -33,8 +33,8 @@ struct PlanSums {
 
 __device__ __forceinline__ int32_t below(int64_t x, int64_t most) { return (int32_t)(x < most ? x : most); }
 
-// The sums, written to `left`, `back`, `take`, `rows_at` (nullable, as qoff) and the
-// outputs qoff, length_out, added and nfree_out.
+// The sums, written to `left`, `back`, `take`, `rows_at` (as qoff) and the outputs
+// qoff, length_out, added and nfree_out.
 __device__ void plan_sums(const PagedPlanArgs &a, int32_t *left, int32_t *back, int32_t *take, int32_t *rows_at,
                           PlanHead *head) {
     __shared__ int64_t room[4][SCAN / 64];
@@ -78,7 +78,9 @@ __device__ void plan_sums(const PagedPlanArgs &a, int32_t *left, int32_t *back, 
         const int64_t want = wanted + group_scan(need, room[2 + turn], &want_total);
         turn ^= 1;
         const bool served = fits && (need == 0 || want + need <= avail);
-        if (fits && !served) atomicMin(&first_short, (unsigned long long)want);
+        // (`want` rises from lane to lane: a wave's first one is its least)
+        const uint64_t wanting = __ballot(fits && !served);
+        if (wanting && (t & 63) == __ffsll((unsigned long long)wanting) - 1) atomicMin(&first_short, (unsigned long long)want);
         rows += row_total;
         wanted += want_total;
         __syncthreads();
@@ -90,14 +92,14 @@ __device__ void plan_sums(const PagedPlanArgs &a, int32_t *left, int32_t *back, 
             a.length_out[b] = (int32_t)(served ? len + n : rest);
             a.added[b] = (int32_t)(served ? n : 0);
             a.qoff[b] = below(row, 0x7fffffff);
-            if (rows_at) rows_at[b] = below(row, 0x7fffffff);
+            rows_at[b] = below(row, 0x7fffffff);
         }
     }
     if (t == 0) {
         back[a.B] = (int32_t)returned;
         take[a.B] = (int32_t)taken;
         a.qoff[a.B] = below(rows, 0x7fffffff);
-        if (rows_at) rows_at[a.B] = below(rows, 0x7fffffff);
+        rows_at[a.B] = below(rows, 0x7fffffff);
         *a.nfree_out = (int32_t)(avail - taken);
         *head = PlanHead{(int32_t)nfree, (int32_t)returned, (int32_t)taken, (int32_t)avail};
     }
@@ -177,20 +179,25 @@ __global__ void __launch_bounds__(SCAN) plan_kernel(PagedPlanArgs a) {
 
 __global__ void __launch_bounds__(SCAN) plan_sums_kernel(PagedPlanArgs a) {
     int32_t *const at = a.sums;
-    plan_sums(a, at, at + a.B, at + 2 * a.B + 1, nullptr, a.head);
+    plan_sums(a, at, at + a.B, at + 2 * a.B + 1, at + 3 * a.B + 2, a.head);
 }
 
-__global__ void __launch_bounds__(256) plan_fill_kernel(PagedPlanArgs a) {
-    __shared__ int32_t staged[4 * STAGED + 3];
+template <bool LDS> __global__ void __launch_bounds__(256) plan_fill_kernel(PagedPlanArgs a) {
+    typedef int32_t i4v __attribute__((ext_vector_type(4)));
+    __shared__ i4v staged[LDS ? STAGED + 1 : 1];
     const int B = (int)a.B;
-    PlanSums z{a.sums, a.sums + a.B, a.sums + 2 * a.B + 1, a.qoff};
-    if (a.B <= STAGED) {
-        for (int i = threadIdx.x; i < 3 * B + 2; i += 256) staged[i] = a.sums[i];
-        for (int i = threadIdx.x; i < B + 1; i += 256) staged[3 * B + 2 + i] = a.qoff[i];
+    const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+    const PlanHead head = *a.head;
+    if constexpr (LDS) {        // (asked for together: each load takes about a microsecond)
+#pragma unroll 4
+        for (int i = threadIdx.x; i < (4 * B + 6) / 4; i += 256) staged[i] = reinterpret_cast<const i4v *>(a.sums)[i];
         __syncthreads();
-        z = PlanSums{staged, staged + B, staged + 2 * B + 1, staged + 3 * B + 2};
+        const int32_t *const at = reinterpret_cast<const int32_t *>(staged);
+        plan_fill(a, PlanSums{at, at + B, at + 2 * B + 1, at + 3 * B + 2}, head, first, step);
+    } else {
+        const int32_t *const at = a.sums;
+        plan_fill(a, PlanSums{at, at + B, at + 2 * B + 1, at + 3 * B + 2}, head, first, step);
     }
-    plan_fill(a, z, *a.head, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
 }
 
 // ---------------------------------------------------------------- rows
@@ -258,7 +265,7 @@ template <typename T, typename C> __global__ void __launch_bounds__(256) store_k
 
 }  // namespace
 
-size_t paged_plan_workspace(int64_t B) { return (sizeof(PlanHead) + 4 * (size_t)(3 * B + 2) + 15) / 16 * 16; }
+size_t paged_plan_workspace(int64_t B) { return (sizeof(PlanHead) + 4 * (size_t)(4 * B + 3) + 15) / 16 * 16; }
 
 hipError_t launch_paged_plan(PagedPlanArgs a, void *ws, hipStream_t s) {
     a.head = static_cast<PlanHead *>(ws);
@@ -271,7 +278,9 @@ hipError_t launch_paged_plan(PagedPlanArgs a, void *ws, hipStream_t s) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t groups = (a.rows + 1023) / 1024, most = 1024;
-    plan_fill_kernel<<<dim3((unsigned)(groups < 64 ? 64 : (groups < most ? groups : most))), dim3(256), 0, s>>>(a);
+    const dim3 grid((unsigned)(groups < 64 ? 64 : (groups < most ? groups : most)));
+    if (a.B <= STAGED) plan_fill_kernel<true><<<grid, dim3(256), 0, s>>>(a);
+    else plan_fill_kernel<false><<<grid, dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
 
