@@ -672,7 +672,7 @@ gs_status gs_sample(const void *S, gs_dtype st, int64_t B, int64_t M, int64_t ld
  *   nfree_out  int32[1] out; may be nfree
  *   qoff       int32[B + 1] out     slots int64[rows] out
  *   added      int32[B] out: positions added
- *   ws         device workspace of gs_paged_plan_workspace(B) bytes, 16-byte
+ *   ws         device workspace of gs_paged_plan_workspace(p) bytes (0: none), 16-byte
  *              aligned; calls that may run at the same time need one each
  * All integer arithmetic: results do not depend on the schedule.
  */
@@ -689,7 +689,8 @@ typedef struct {
     int32_t *added;
 } gs_paged_step;
 
-size_t gs_paged_plan_workspace(int64_t B);
+/* Bytes of workspace (0 also for sizes that the call rejects); by B, rows and width. */
+size_t gs_paged_plan_workspace(const gs_paged_step *p);
 
 gs_status gs_paged_plan(const gs_paged_step *p, void *ws, size_t ws_bytes, void *stream);
 
@@ -733,7 +734,8 @@ gs_status gs_paged_store(const gs_paged_rows *p, gs_dtype t, gs_dtype ct, void *
  * included; neither do states whose page number lies outside [0, pages) (they
  * count as not there).  Pages of which no row sees a state are not read, and may
  * have been given to others.  Rows of no request, and rows of a request behind
- * its first Lq, are left as they are.
+ * its first Lq, are left as they are; a row that two requests name (offsets that
+ * fall) holds values of either.
  *
  *   B, N       requests and rows >= 0       Lq   most rows of a request, >= 0
  *   Lk         most states of a request, 0 <= Lk <= width page: klen counts as 0
@@ -750,7 +752,7 @@ gs_status gs_paged_store(const gs_paged_rows *p, gs_dtype t, gs_dtype ct, void *
  *              in {F32, BF16}, strides as for gs_cross_attention.  Rows that start
  *              on 16-byte boundaries with Dh a multiple of 16 bytes are the fast case
  *   lse        float N x Hq out, nullable
- *   ws         device workspace of gs_paged_attention_workspace(p, t) bytes,
+ *   ws         device workspace of gs_paged_attention_workspace(p, t) bytes (0: none),
  *              16-byte aligned; calls that may run at the same time need one each
  * fp32 accumulation; probabilities enter the second product in type t.  Work is
  * shared out by the lengths that the device holds, in parts whose results are
@@ -796,7 +798,7 @@ gs_status gs_paged_attention(const gs_paged_attn *p, gs_dtype t, void *ws, size_
  *   drafted     int32[N], u float[N], v float[B], qoff int32[B + 1] device (clamped
  *               to 0 .. N)
  *   accepted, entry   int32[B] out;  entries int32[N] out, nullable (rows of no
- *               request are left as they are)
+ *               request are left as they are, rows that two name hold either's)
  *   ws          device workspace of gs_verify_workspace(B, M) bytes (0: none),
  *               16-byte aligned; calls that may run at the same time need one each
  * Comparisons, weights and sums are fp64, summed in a fixed order.

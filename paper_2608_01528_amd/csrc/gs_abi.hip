@@ -400,6 +400,8 @@ bool counts(std::initializer_list<int64_t> v) {
     return true;
 }
 
+bool step_sizes(const gs_paged_step *p) { return counts({p->B, p->page, p->rows, p->width, p->capacity}) && p->page >= 1; }
+
 // Sizes that the kernels of gs_paged_attention count in 32 bits.
 bool paged_sizes(const gs_paged_attn *a) {
     if (!counts({a->B, a->N, a->Lq, a->Lk, a->pages, a->page, a->width}) || a->page < 1) return false;
@@ -1018,12 +1020,15 @@ gs_status gs_sample(const void *S, gs_dtype st, int64_t B, int64_t M, int64_t ld
     return launched(launch_sample(st, a, ws, (hipStream_t)stream), fn);
 }
 
-size_t gs_paged_plan_workspace(int64_t B) { return counts({B}) ? paged_plan_workspace(B) : 0; }
+size_t gs_paged_plan_workspace(const gs_paged_step *p) {
+    if (!p || !step_sizes(p)) return 0;
+    return paged_plan_workspace(p->B, p->rows, p->width);
+}
 
 gs_status gs_paged_plan(const gs_paged_step *p, void *ws, size_t ws_bytes, void *stream) {
     const char *fn = "gs_paged_plan";
     if (!p) return fail(GS_ERR_ARG, "%s: the step is null", fn);
-    if (!counts({p->B, p->page, p->rows, p->width, p->capacity}) || p->page < 1)
+    if (!step_sizes(p))
         return fail(GS_ERR_SHAPE, "%s: need B, rows, width, capacity >= 0 and page >= 1, all below 2^31 - 256", fn);
     if (p->ldt < p->width || !within_reach(p->B, p->ldt, p->width))
         return fail(GS_ERR_SHAPE, "%s: leading dimension of the table out of range", fn);
@@ -1036,7 +1041,7 @@ gs_status gs_paged_plan(const gs_paged_step *p, void *ws, size_t ws_bytes, void 
         if (!e.p && e.needed) return fail(GS_ERR_ARG, "%s: %s is null", fn, e.name);
         GS_CHECK(check_aligned(e.p, e.es, e.name));
     }
-    const size_t need = paged_plan_workspace(p->B);
+    const size_t need = paged_plan_workspace(p->B, p->rows, p->width);
     GS_CHECK(check_ws(fn, ws, ws_bytes, need));
     // length_out and nfree_out may be the inputs themselves
     const bool same = p->length_out == p->length, same_n = p->nfree_out == p->nfree;

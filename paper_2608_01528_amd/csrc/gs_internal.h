@@ -295,7 +295,6 @@ hipError_t launch_sample(gs_dtype st, SampleArgs a, void *ws, hipStream_t s);
 
 // A paged cache: pages and slots of a step, its states (gs_paged.hip), its
 // attention (gs_paged_attn.hip).
-constexpr int64_t PLAN_ONE_PAGES = (int64_t)1 << 17;    // table entries up to which one work-group moves pages
 struct PagedPlanHead { int32_t nfree, back, taken, avail; };
 struct PagedPlanArgs {
     int64_t B, page, rows, width, ldt, capacity;
@@ -310,7 +309,7 @@ struct PagedPlanArgs {
     PagedPlanHead *head;
     int32_t *sums;
 };
-size_t paged_plan_workspace(int64_t B);
+size_t paged_plan_workspace(int64_t B, int64_t rows, int64_t width);
 hipError_t launch_paged_plan(PagedPlanArgs a, void *ws, hipStream_t s);
 struct PagedStoreArgs {
     const void *K, *V;

@@ -920,7 +920,7 @@ Layout layout(gs_dtype t, const PagedAttnArgs &a) {
         z.joins = z.slots / 2 + 1;
         z.slots *= a.Hkv;
     }
-    z.list = z.few ? 4 * ((size_t)a.B + 1) : sizeof(PagedAttnHead) + (size_t)z.items * sizeof(PagedItem) + (size_t)z.joins * sizeof(PagedJoin);
+    z.list = z.whole ? 0 : z.few ? 4 * ((size_t)a.B + 1) : sizeof(PagedAttnHead) + (size_t)z.items * sizeof(PagedItem) + (size_t)z.joins * sizeof(PagedJoin);
     z.list = (z.list + 15) / 16 * 16;
     z.bytes = z.list + (size_t)z.slots * z.rows * (z.dp + 1) * 4;
     return z;

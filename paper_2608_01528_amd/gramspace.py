@@ -116,7 +116,7 @@ _SIGS["gs_sample_workspace"] = ([ctypes.c_int, _i64, _i64], ctypes.c_size_t)
 _SIGS["gs_sample"] = ([_vp, ctypes.c_int, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp],
                       ctypes.c_int)
 # gs_paged_step, gs_paged_rows, gs_paged_attn and gs_drafts likewise
-_SIGS["gs_paged_plan_workspace"] = ([_i64], ctypes.c_size_t)
+_SIGS["gs_paged_plan_workspace"] = ([_vp], ctypes.c_size_t)
 _SIGS["gs_paged_plan"] = ([_vp, _vp, ctypes.c_size_t, _vp], ctypes.c_int)
 _SIGS["gs_paged_store"] = ([_vp, ctypes.c_int, ctypes.c_int, _vp], ctypes.c_int)
 _SIGS["gs_paged_attention_workspace"] = ([_vp, ctypes.c_int], ctypes.c_size_t)
@@ -619,7 +619,8 @@ def _per_row(t, name: str, n: int, dtype):
     """Address of a contiguous vector of n entries, 0 for None."""
     if t is None:
         return 0
-    _here(t, name, dtype)
+    if t.dtype is not dtype or not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+        _here(t, name, dtype)
     if t.numel() != n or not t.is_contiguous():
         raise ValueError("%s must be contiguous with %d entries" % (name, n))
     return t.data_ptr()
@@ -810,13 +811,15 @@ def gs_paged_plan(length: torch.Tensor, add: torch.Tensor, table: torch.Tensor, 
     (length, nfree, qoff, slots, added): the new lengths and height, the
     requests' first rows (int32, B + 1), the slots of `rows` rows (int64, -1
     for none) and the positions each request got (int32, B)."""
-    i32, dev = torch.int32, table.device
+    # (allocating the results is most of what a call costs on the host: like an
+    # input where there is one of their kind)
+    i32 = torch.int32
     B = length.numel()
-    length_out = length.new_empty(B) if length_out is None else length_out
-    nfree_out = nfree.new_empty(1) if nfree_out is None else nfree_out
-    qoff = torch.empty(B + 1, dtype=i32, device=dev) if qoff_out is None else qoff_out
-    slots = torch.empty(rows, dtype=torch.int64, device=dev) if slots_out is None else slots_out
-    added = torch.empty(B, dtype=i32, device=dev) if added_out is None else added_out
+    length_out = torch.empty_like(length) if length_out is None else length_out
+    nfree_out = torch.empty_like(nfree) if nfree_out is None else nfree_out
+    qoff = length.new_empty(B + 1) if qoff_out is None else qoff_out
+    slots = length.new_empty(rows, dtype=torch.int64) if slots_out is None else slots_out
+    added = torch.empty_like(length) if added_out is None else added_out
     given = _PAGED_STEP.pack(B, page, rows, _per_row(length, "length", B, i32), _per_row(add, "add", B, i32),
                              _per_row(length_out, "length_out", B, i32), *_table(table, B),
                              _per_row(free, "free", free.numel(), i32), free.numel(),
@@ -824,7 +827,7 @@ def gs_paged_plan(length: torch.Tensor, add: torch.Tensor, table: torch.Tensor, 
                              _per_row(qoff, "qoff_out", B + 1, i32), _per_row(slots, "slots_out", rows, torch.int64),
                              _per_row(added, "added_out", B, i32))
     L = lib()
-    ws, n, _keep = _workspace(L.gs_paged_plan_workspace(B), workspace, dev)
+    ws, n, _keep = _workspace(L.gs_paged_plan_workspace(given), workspace, table.device)
     _check(L.gs_paged_plan(given, ws, n, _stream()))
     return length_out, nfree_out, qoff, slots, added
 
@@ -871,7 +874,7 @@ def gs_paged_attention(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, tabl
     room = width * c[1]
     max_len = min(room, 0x7fffffff - 256) if max_len is None else max_len
     if out is None:
-        out = Q.new_empty(q)
+        out = torch.empty_like(Q)
     if lse_out is None and lse:
         lse_out = Q.new_empty((N, Hq), dtype=torch.float32)
     lp = 0
@@ -915,9 +918,9 @@ def gs_verify(P: torch.Tensor, drafted: torch.Tensor, u: torch.Tensor, v: torch.
             raise ValueError("%s must have rows of its own" % name)
     i32, dev = torch.int32, P.device
     B = v.numel()
-    acc = torch.empty(B, dtype=i32, device=dev) if accepted_out is None else accepted_out
-    ent = torch.empty(B, dtype=i32, device=dev) if entry_out is None else entry_out
-    every = torch.empty(N, dtype=i32, device=dev) if entries and entries_out is None else entries_out
+    acc = v.new_empty(B, dtype=i32) if accepted_out is None else accepted_out
+    ent = torch.empty_like(acc) if entry_out is None else entry_out
+    every = torch.empty_like(drafted) if entries and entries_out is None else entries_out
     given = _DRAFTS.pack(B, N, M, P.data_ptr(), ldp, qp, ldq, _per_row(drafted, "drafted", N, i32),
                          _per_row(u, "u", N, torch.float32), _per_row(v, "v", B, torch.float32),
                          _per_row(qoff, "qoff", B + 1, i32), _per_row(acc, "accepted_out", B, i32),

@@ -52,7 +52,8 @@ def seen(p, klen, window, sinks):
 
 
 def attention(Q, Kc, Vc, table, klen, qoff, max_new=None, max_len=None, window=0, sinks=0, scale=None):
-    """{name: (value, bound)} of O (N, Hq, Dh) and lse (N, Hq), and which rows are written."""
+    """{name: (value, bound)} of O (N, Hq, Dh) and lse (N, Hq), and how many
+    requests name each row (a row of two, where offsets fall, holds either's)."""
     Q, Kc, Vc = (t.detach().cpu() for t in (Q, Kc, Vc))
     table, klen = table.cpu().numpy().astype(np.int64), klen.cpu().tolist()
     pages, page = Kc.shape[:2]
@@ -62,13 +63,13 @@ def attention(Q, Kc, Vc, table, klen, qoff, max_new=None, max_len=None, window=0
     off = list(range(N + 1)) if qoff is None else [min(max(x, 0), N) for x in qoff.cpu().tolist()]
     O, lse = torch.zeros(N, Hq, Dh, dtype=torch.float64), torch.zeros(N, Hq, dtype=torch.float64)
     tO, tl = torch.zeros_like(O), torch.zeros_like(lse)
-    written = torch.zeros(N, dtype=torch.bool)
+    named = torch.zeros(N, dtype=torch.int32)
     for b, k in enumerate(klen):
         k = min(max(k, 0), max_len)
         n = max(off[b + 1] - off[b], 0)
         for i in range(n if max_new is None else min(n, max_new)):
             r = off[b] + i
-            written[r] = True
+            named[r] += 1
             j = seen(k - n + i, k, window, sinks)
             ids = table[b, j // page]
             ok = (ids >= 0) & (ids < pages)
@@ -76,7 +77,7 @@ def attention(Q, Kc, Vc, table, klen, qoff, max_new=None, max_len=None, window=0
             ref = attn_util.reference(Q[None, r: r + 1], Kc[g, at][None], Vc[g, at][None], scale=scale)
             O[r], tO[r] = ref["O"][0][0, 0], ref["O"][1][0, 0]
             lse[r], tl[r] = ref["lse"][0][0, :, 0], ref["lse"][1][0, :, 0]
-    return {"O": (O, tO), "lse": (lse, tl)}, written
+    return {"O": (O, tO), "lse": (lse, tl)}, named
 
 
 def weights(row):
@@ -85,7 +86,8 @@ def weights(row):
 
 
 def verify(P, Q, drafted, u, v, qoff, near=None):
-    """(accepted, entry, entries) on arrays; entries of rows of no request are None.
+    """(accepted, entry, entries) on arrays; entries of rows of no request, and of
+    rows that two requests name (offsets that fall), are None.
     `near`: a list that gets the relative distance of each draw's target from
     the next border between entries."""
     N, M = P.shape
@@ -130,4 +132,7 @@ def verify(P, Q, drafted, u, v, qoff, near=None):
             entries[off[b] + k] = -1
         accepted.append(a)
         entry.append(e)
-    return accepted, entry, entries
+    named = np.zeros(N, int)
+    for b in range(len(v)):
+        named[off[b]: max(off[b], off[b + 1])] += 1
+    return accepted, entry, [x if k < 2 else None for x, k in zip(entries, named)]

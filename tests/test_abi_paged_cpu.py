@@ -112,7 +112,7 @@ def test_nothing_to_do(L, kind, change):
     (Step, dict(length_out=0x10000004), gs.GS_ERR_ARG),         # not the lengths, but over them
     (Step, dict(add=0x12000000), gs.GS_ERR_ARG), (Step, dict(qoff=0x13000000), gs.GS_ERR_ARG),
     (Step, dict(nfree_out=0x14000000), gs.GS_ERR_ARG), (Step, dict(added=0x10000000), gs.GS_ERR_ARG),
-    (Step, dict(slots=WS), gs.GS_ERR_ARG),
+    (Step, dict(slots=WS, rows=5000), gs.GS_ERR_ARG),
     (Rows, dict(N=-1), gs.GS_ERR_SHAPE), (Rows, dict(Hkv=0), gs.GS_ERR_SHAPE), (Rows, dict(Dh=0), gs.GS_ERR_SHAPE),
     (Rows, dict(page=0), gs.GS_ERR_SHAPE), (Rows, dict(pages=-1), gs.GS_ERR_SHAPE),
     (Rows, dict(N=2**30, Dh=40), gs.GS_ERR_SHAPE), (Rows, dict(slots=0), gs.GS_ERR_ARG),
@@ -135,7 +135,7 @@ def test_nothing_to_do(L, kind, change):
     (Attn, dict(Q=(0, 0, 256, 64)), gs.GS_ERR_ARG), (Attn, dict(K=(0x14000001, 2048, 128, 64)), gs.GS_ERR_ALIGN),
     (Attn, dict(O=(0x16000000, 0, 255, 64)), gs.GS_ERR_SHAPE), (Attn, dict(O=(0x13000000, 0, 256, 64)), gs.GS_ERR_ARG),
     (Attn, dict(lse=0x16000000), gs.GS_ERR_ARG), (Attn, dict(O=(0x14001000, 0, 256, 64)), gs.GS_ERR_ARG),
-    (Attn, dict(O=(WS, 0, 256, 64)), gs.GS_ERR_ARG),
+    (Attn, dict(O=(WS, 0, 256, 64), Lk=300, width=20, ldt=20), gs.GS_ERR_ARG),
     (Drafts, dict(B=-1), gs.GS_ERR_SHAPE), (Drafts, dict(N=-1), gs.GS_ERR_SHAPE), (Drafts, dict(M=0), gs.GS_ERR_SHAPE),
     (Drafts, dict(M=BIG, ldp=BIG, ldq=BIG), gs.GS_ERR_SHAPE), (Drafts, dict(B=2**24), gs.GS_ERR_SHAPE),
     (Drafts, dict(B=2**14, M=2**22, ldp=2**22, ldq=2**22), gs.GS_ERR_SHAPE), (Drafts, dict(ldp=99), gs.GS_ERR_SHAPE),
@@ -168,8 +168,9 @@ def test_null_problems(L):
 def test_workspaces(L):
     """Sizes that are asked for are the sizes that are enough."""
     M = 50000
-    for kind, need, change in ((Step, L.gs_paged_plan_workspace(3), {}),
-                               (Attn, L.gs_paged_attention_workspace(Attn().bytes(), gs.GS_BF16), {}),
+    for kind, need, change in ((Step, L.gs_paged_plan_workspace(Step(rows=5000).bytes()), dict(rows=5000)),
+                               (Attn, L.gs_paged_attention_workspace(Attn(Lk=300, page=64).bytes(), gs.GS_BF16),
+                                dict(Lk=300, page=64, K=(0x14000000, 8192, 128, 64), V=(0x15000000, 8192, 128, 64))),
                                (Attn, L.gs_paged_attention_workspace(Attn(Lq=9, Hq=64).bytes(), gs.GS_BF16),
                                 dict(Lq=9, Hq=64, Q=(0x13000000, 0, 4096, 64), O=(0x16000000, 0, 4096, 64))),
                                (Drafts, L.gs_verify_workspace(3, M), dict(M=M, ldp=M, ldq=M, P=0x20000000, Q=0x30000000))):
@@ -180,7 +181,8 @@ def test_workspaces(L):
         if not torch.cuda.is_available():
             assert kind(**change).call(L, n=need) == gs.GS_ERR_DEVICE
     assert L.gs_verify_workspace(3, 4096) == 0 and L.gs_verify_workspace(0, M) == 0 and L.gs_verify_workspace(2**24, M) == 0
-    assert L.gs_paged_plan_workspace(-1) == 0
+    assert L.gs_paged_plan_workspace(Step(B=-1, rows=5000).bytes()) == 0 and L.gs_paged_plan_workspace(Step().bytes()) == 0
+    assert L.gs_paged_plan_workspace(None) == 0 and L.gs_paged_attention_workspace(Attn().bytes(), gs.GS_BF16) == 0
     for change in (dict(B=0), dict(N=0), dict(Lq=0), dict(Dh=129), dict(Lk=81)):
         assert L.gs_paged_attention_workspace(Attn(**change).bytes(), gs.GS_BF16) == 0
     assert L.gs_paged_attention_workspace(Attn().bytes(), gs.GS_F64) == 0

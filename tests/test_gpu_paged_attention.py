@@ -43,11 +43,11 @@ def check(Q, Kc, Vc, table, klen, qoff=None, **kw):
     # rows that are not written keep what they hold
     out, lse = torch.full_like(Q, 7.0), torch.full(Q.shape[:2], 7.0, device=DEV)
     gs.gs_paged_attention(Q, Kc, Vc, table, klen, qoff=qoff, out=out, lse_out=lse, **kw)
-    ref, written = paged_util.attention(Q, Kc, Vc, table, klen, qoff, **kw)
-    w = written.to(DEV)
+    ref, named = paged_util.attention(Q, Kc, Vc, table, klen, qoff, **kw)
+    written, w, none = named == 1, (named == 1).to(DEV), (named == 0).to(DEV)
     attn_util.check(out[w], {"O": tuple(x[written] for x in ref["O"])}, "O")
     attn_util.check(lse[w], {"lse": tuple(x[written] for x in ref["lse"])}, "lse")
-    assert (out[~w] == 7).all() and (lse[~w] == 7).all()
+    assert (out[none] == 7).all() and (lse[none] == 7).all()
     return out, lse
 
 
