@@ -14,6 +14,8 @@
 // More rows (prompts): a launch lists the blocks of 128 rows, longest first, cut
 // where they are longer than a work-group's share (plan_kernel), and what was cut
 // is put together by many_join_kernel.
+#include <algorithm>
+
 #include "gs_attn.h"
 #include "gs_scan.h"
 
@@ -757,21 +759,24 @@ __device__ __forceinline__ int block_start(const PagedAttnArgs &a, int b) {
 // longest first (in 64 steps), so that short ones fill the end.  Places within a
 // step, and of parts in the workspace, go by the order of atomics; no result does.
 template <int BN> __global__ void __launch_bounds__(1024) plan_kernel(PagedAttnArgs a) {
-    constexpr int STEPS = 64;
+    constexpr int STEPS = 64, STAGED = 1024;
     __shared__ int64_t room[16];
     __shared__ int next[STEPS], longest, slots, joins;
+    __shared__ int starts[STAGED];
     const int t = threadIdx.x;
     int b = 0, tile = 0;
+    const bool staged = a.B <= STAGED;
+    if (staged && t < a.B) starts[t] = block_start(a, t);
     auto tiles_of = [&](int i) {
         if (i >= a.blocks || a.B == 0) return 0;
         int lo = 0, hi = a.B;
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
-            if (block_start(a, mid) <= i) lo = mid;
+            if ((staged ? starts[mid] : block_start(a, mid)) <= i) lo = mid;
             else hi = mid;
         }
         const Rows r(a, lo);
-        const int k = i - block_start(a, lo), all = r.count * a.G;
+        const int k = i - (staged ? starts[lo] : block_start(a, lo)), all = r.count * a.G;
         if (k < 0 || k * BLOCK >= all) return 0;
         b = lo, tile = k;
         const View<BN> v(a, r, k * BLOCK / a.G, ((k + 1) * BLOCK < all ? (k + 1) * BLOCK - 1 : all - 1) / a.G);
@@ -779,6 +784,7 @@ template <int BN> __global__ void __launch_bounds__(1024) plan_kernel(PagedAttnA
     };
     if (t < STEPS) next[t] = 0;
     if (t == 0) longest = 1, slots = 0, joins = 0;
+    __syncthreads();
     int64_t mine = 0, total;
     int n = 0, most = 0;
     for (int i = t; i < a.blocks; i += 1024) {
@@ -789,7 +795,9 @@ template <int BN> __global__ void __launch_bounds__(1024) plan_kernel(PagedAttnA
     (void)group_scan(mine, room, &total);
     total = (total * a.Hkv + a.waves - 1) / a.waves;
     const int share = total < a.least ? a.least : (int)(total < 0x40000000 ? total : 0x40000000);
-    atomicMax(&longest, min(most, share));
+#pragma unroll
+    for (int d = 32; d; d >>= 1) most = max(most, __shfl_xor(most, d));
+    if ((t & 63) == 0) atomicMax(&longest, min(most, share));
     __syncthreads();
     // parts of a block of n tiles, and their step by length
     const int top = longest;
@@ -901,10 +909,12 @@ Layout layout(gs_dtype t, const PagedAttnArgs &a) {
         z.least = 4;
         const int64_t most = ((int64_t)a.Lk / 16 + 3) * a.B / z.least + 1, full = 256 * held / a.Hkv;
         z.ranges = (int)(most < full ? most : (full > 1 ? full : 1));
-        // Short histories are not cut: up to 8 tiles in a row take less than a second
-        // launch.
+        // Short histories and windows are not cut: up to 8 tiles in a row take less
+        // than a second launch.
         const int bn = t == GS_F32 && rows <= 16 ? 16 : 32;
-        z.whole = a.Lk <= 8 * bn;
+        int64_t most_tiles = ((int64_t)a.Lk + bn - 1) / bn;
+        if (a.window) most_tiles = std::min(most_tiles, ((int64_t)a.window + a.Lq - 2) / bn + 2 + ((int64_t)a.sinks + bn - 1) / bn);
+        z.whole = most_tiles <= 8;
         if (z.whole) z.ranges = a.B;
         z.slots = z.whole ? 0 : 2 * (int64_t)z.ranges * a.Hkv;
     } else {
