@@ -685,9 +685,60 @@ __global__ void __launch_bounds__(64, (R == 16 ? 2 : min_waves<T, DC, 1>())) few
     }
 }
 
-// Puts together rows of a request and head that range ends cut: a work-group for 4
-// LANES values of a row, parts shared out to its groups of so many lanes.
-template <typename T, int DP, int BN, int NT, int LANES> __global__ void __launch_bounds__(NT) few_join_kernel(PagedAttnArgs a) {
+// Where the parts of a request and head that range ends cut lie.
+struct Cut {
+    int i0, i1;         // its ranges
+    int64_t first, next, step;
+    template <int BN> __device__ __forceinline__ void find(const PagedAttnArgs &a, int b, int hk) {
+        const int before = a.line[b], share = a.line[a.B], tiles = few_tiles<BN>(a, b);
+        i0 = before / share, i1 = (before + tiles - 1) / share;
+        step = 2 * (int64_t)a.Hkv * a.rows;
+        // the first part may be its range's second one
+        first = ((int64_t)(2 * i0 + (before > i0 * share)) * a.Hkv + hk) * a.rows;
+        next = ((int64_t)(2 * i0) * a.Hkv + hk) * a.rows;
+    }
+    __device__ __forceinline__ int64_t place(int i, int m) const { return (i == i0 ? first : next + (i - i0) * step) + m; }
+};
+
+__device__ __forceinline__ float joined_lse(float ref, float sum) {
+    return sum != 0.f ? ref + __builtin_amdgcn_logf(sum) * LN2 : -INFINITY;
+}
+
+// Puts together rows of which there are a few parts: a thread for 4 values.
+template <typename T, int DP, int BN> __global__ void __launch_bounds__(256) few_join_kernel(PagedAttnArgs a) {
+    constexpr int LANES = DP / 4;
+    const int hk = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv, d = 4 * (threadIdx.x % LANES);
+    const Rows r(a, b);
+    const int rows = r.count * a.G, step = gridDim.y * (256 / LANES);
+    int m = blockIdx.y * (256 / LANES) + threadIdx.x / LANES;
+    if (m >= rows || d >= a.Dh) return;
+    Cut c;
+    c.find<BN>(a, b, hk);
+    if (c.i0 == c.i1) return;
+    for (; m < rows; m += step) {
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll 4
+        for (int i = c.i0; i <= c.i1; ++i) top = fmaxf(top, a.part_lse[c.place(i, m)]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        f4v o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int i = c.i0; i <= c.i1; ++i) {
+            const int64_t at = c.place(i, m);
+            const float e = __builtin_amdgcn_exp2f((a.part_lse[at] - ref) * LOG2E);
+            sum += e;
+            o += e * *reinterpret_cast<const f4v *>(a.part + at * DP + d);
+        }
+        const float inv = sum != 0.f ? 1.f / sum : 0.f;
+        const RowOf row(m, hk, a.G);
+        const int64_t at = r.first + row.i;
+        store4<T>(static_cast<T *>(a.O) + at * a.o.l + row.h * a.o.h, d, a.Dh, a.vec, o * inv);
+        if (a.lse && d == 0) a.lse[at * a.Hq + row.h] = joined_lse(ref, sum);
+    }
+}
+
+// The same for many parts: a work-group for 4 LANES values of a row, parts shared out
+// to its groups of so many lanes.
+template <typename T, int DP, int BN, int NT, int LANES> __global__ void __launch_bounds__(NT) few_join_many_kernel(PagedAttnArgs a) {
     constexpr int GROUPS = NT / LANES, WAVES = NT / 64;
     __shared__ f4v sums[WAVES][LANES];
     __shared__ float weights[WAVES], tops[WAVES];
@@ -696,15 +747,12 @@ template <typename T, int DP, int BN, int NT, int LANES> __global__ void __launc
     const Rows r(a, b);
     const int rows = r.count * a.G;
     if (!rows) return;
-    const int before = a.line[b], share = a.line[a.B], tiles = few_tiles<BN>(a, b);
-    const int i0 = before / share, i1 = (before + tiles - 1) / share;
+    Cut c;
+    c.find<BN>(a, b, hk);
+    const int i0 = c.i0, i1 = c.i1;
     if (i0 == i1) return;
-    const int64_t step = 2 * (int64_t)a.Hkv * a.rows;
     for (int m = blockIdx.y; m < rows; m += gridDim.y) {
-        // the first part may be its range's second one
-        const int64_t at0 = ((int64_t)(2 * i0 + (before > i0 * share)) * a.Hkv + hk) * a.rows + m;
-        const int64_t at1 = ((int64_t)(2 * i0) * a.Hkv + hk) * a.rows + m;
-        auto place = [&](int i) { return i == i0 ? at0 : at1 + (i - i0) * step; };
+        auto place = [&](int i) { return c.place(i, m); };
         float top = -INFINITY;
         for (int i = i0 + t; i <= i1; i += NT) top = fmaxf(top, a.part_lse[place(i)]);
 #pragma unroll
@@ -739,7 +787,7 @@ template <typename T, int DP, int BN, int NT, int LANES> __global__ void __launc
             const RowOf row(m, hk, a.G);
             const int64_t at = r.first + row.i;
             if (d < a.Dh) store4<T>(static_cast<T *>(a.O) + at * a.o.l + row.h * a.o.h, d, a.Dh, a.vec, o * inv);
-            if (a.lse && d == 0) a.lse[at * a.Hq + row.h] = sum != 0.f ? ref + __builtin_amdgcn_logf(sum) * LN2 : -INFINITY;
+            if (a.lse && d == 0) a.lse[at * a.Hq + row.h] = joined_lse(ref, sum);
         }
         __syncthreads();
     }
@@ -879,7 +927,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256) many_join_k
     const RowOf row(m, hk, a.G);
     const int64_t at = r.first + row.i;
     store4<T>(static_cast<T *>(a.O) + at * a.o.l + row.h * a.o.h, d, a.Dh, a.vec, o * inv);
-    if (a.lse && d == 0) a.lse[at * a.Hq + row.h] = sum != 0.f ? ref + __builtin_amdgcn_logf(sum) * LN2 : -INFINITY;
+    if (a.lse && d == 0) a.lse[at * a.Hq + row.h] = joined_lse(ref, sum);
 }
 
 // ------------------------------------------------------------ dispatch
@@ -941,10 +989,14 @@ template <typename T, int DC, int R, bool VEC> hipError_t launch_few(const Paged
     few_kernel<T, DC, R, VEC><<<dim3((unsigned)((z.ranges * a.Hkv + 7) / 8 * 8)), dim3(64), 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || z.whole) return e;
-    // many parts a request: more lanes a row
+    // 16 parts a request or more: more lanes a row
     const unsigned pairs = (unsigned)(a.B * a.Hkv), rows = pairs * (int64_t)a.rows <= 16384 ? (unsigned)a.rows : 1;
-    if (z.ranges / a.B >= 32) few_join_kernel<T, DP, BN, 1024, 8><<<dim3(pairs, rows, DP / 32), dim3(1024), 0, s>>>(a);
-    else few_join_kernel<T, DP, BN, 256, DP / 4><<<dim3(pairs, rows), dim3(256), 0, s>>>(a);
+    if (z.ranges / a.B >= 16) {
+        few_join_many_kernel<T, DP, BN, 1024, 8><<<dim3(pairs, rows, DP / 32), dim3(1024), 0, s>>>(a);
+    } else {
+        const unsigned pieces = (unsigned)((a.rows * (DP / 4) + 255) / 256);
+        few_join_kernel<T, DP, BN><<<dim3(pairs, pieces), dim3(256), 0, s>>>(a);
+    }
     return hipGetLastError();
 }
 
