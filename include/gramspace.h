@@ -709,7 +709,9 @@ gs_status gs_paged_plan(const gs_paged_step *p, void *ws, size_t ws_bytes, void 
  *   K, V    in   element (n, h, d) at p[n sl + h sh + d], type t in {F32, BF16}
  *                (sb is not used)
  *   Kc, Vc  out  element (page g, place i, h, d) at p[g sb + i sl + h sh + d],
- *                type ct in {F32, BF16}; elements at places of their own
+ *                type ct in {F32, BF16}; elements at places of their own (with the
+ *                same strides they may lie within one another: keys and values side
+ *                by side in each page)
  * Strides as for gs_cross_attention.  Nothing but the named slots is written.
  */
 typedef struct {
@@ -732,8 +734,8 @@ gs_status gs_paged_store(const gs_paged_rows *p, gs_dtype t, gs_dtype ct, void *
  * A row that sees no state gives O = 0 and lse = -inf.  States that a row does
  * not see contribute nothing to it whatever they hold, NaN and infinities
  * included; neither do states whose page number lies outside [0, pages) (they
- * count as not there).  Pages of which no row sees a state are not read, and may
- * have been given to others.  Rows of no request, and rows of a request behind
+ * count as not there).  Pages of which no row sees a state may have been given to
+ * others, and their places in the table may hold anything.  Rows of no request, and rows of a request behind
  * its first Lq, are left as they are; a row that two requests name (offsets that
  * fall) holds values of either.
  *

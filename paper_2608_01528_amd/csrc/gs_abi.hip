@@ -402,6 +402,25 @@ bool counts(std::initializer_list<int64_t> v) {
 
 bool step_sizes(const gs_paged_step *p) { return counts({p->B, p->page, p->rows, p->width, p->capacity}) && p->page >= 1; }
 
+// Two tensors of the same shape and strides that lie within one another (keys and
+// values side by side in each page, say) without sharing a place: one tensor with
+// a dimension of 2 more.
+bool side_by_side(const gs_seq &x, const gs_seq &y, const SeqShape &z, size_t es) {
+    if (x.sb != y.sb || x.sl != y.sl || x.sh != y.sh) return false;
+    const int64_t apart = std::abs(static_cast<const char *>(x.p) - static_cast<const char *>(y.p));
+    if (apart % (int64_t)es) return false;
+    int64_t s[4] = {x.sb, x.sl, x.sh, apart / (int64_t)es}, n[4] = {z.n[0], z.n[1], z.n[2], 2}, extent = z.dh;
+    for (int i = 0; i < 4; ++i)
+        for (int j = i + 1; j < 4; ++j)
+            if (s[j] < s[i]) std::swap(s[i], s[j]), std::swap(n[i], n[j]);
+    for (int i = 0; i < 4; ++i) {
+        if (n[i] <= 1) continue;
+        if (s[i] < extent) return false;
+        extent += (n[i] - 1) * s[i];
+    }
+    return true;
+}
+
 // Sizes that the kernels of gs_paged_attention count in 32 bits.
 bool paged_sizes(const gs_paged_attn *a) {
     if (!counts({a->B, a->N, a->Lq, a->Lk, a->pages, a->page, a->width}) || a->page < 1) return false;
@@ -1077,8 +1096,14 @@ gs_status gs_paged_store(const gs_paged_rows *p, gs_dtype t, gs_dtype ct, void *
     GS_CHECK(check_seq(fn, "Vc", p->Vc, c, ct, true));
     if (!p->slots && p->N) return fail(GS_ERR_ARG, "%s: slots is null", fn);
     GS_CHECK(check_aligned(p->slots, 8, "slots"));
-    GS_CHECK(check_overlaps({seq_span(K, x, esize(t), "K"), seq_span(V, x, esize(t), "V"), span(p->slots, 1, p->N, p->N, 8, "slots")},
-                            {seq_span(p->Kc, c, esize(ct), "Kc"), seq_span(p->Vc, c, esize(ct), "Vc")}));
+    const Span in[] = {seq_span(K, x, esize(t), "K"), seq_span(V, x, esize(t), "V"), span(p->slots, 1, p->N, p->N, 8, "slots")};
+    const Span out[] = {seq_span(p->Kc, c, esize(ct), "Kc"), seq_span(p->Vc, c, esize(ct), "Vc")};
+    if (side_by_side(p->Kc, p->Vc, c, esize(ct))) {
+        GS_CHECK(check_overlaps(in, 3, out, 1));
+        GS_CHECK(check_overlaps(in, 3, out + 1, 1));
+    } else {
+        GS_CHECK(check_overlaps(in, 3, out, 2));
+    }
     if (p->N == 0 || p->pages == 0) return ok();
     GS_CHECK(check_device());
     PagedStoreArgs a{};

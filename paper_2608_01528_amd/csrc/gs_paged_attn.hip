@@ -10,7 +10,8 @@
 // How the work is shared out follows the lengths in device memory.  Requests of
 // few rows (up to 32 a key and value head: tokens, drafts): all tiles of all
 // requests and heads lie in one line, of which every wave takes an equal part
-// (few_kernel); a request cut by part ends is put together by few_join_kernel.
+// (few_kernel); a request cut by part ends is put together by few_join_kernel or,
+// of many parts, few_join_many_kernel.
 // More rows (prompts): a launch lists the blocks of 128 rows, longest first, cut
 // where they are longer than a work-group's share (plan_kernel), and what was cut
 // is put together by many_join_kernel.
@@ -988,7 +989,7 @@ template <typename T, int DC, int R, bool VEC> hipError_t launch_few(const Paged
     constexpr int DP = padded(DC), BN = few_keys<T>(R);
     few_kernel<T, DC, R, VEC><<<dim3((unsigned)((z.ranges * a.Hkv + 7) / 8 * 8)), dim3(64), 0, s>>>(a);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || z.whole) return e;
+    if (e != hipSuccess || z.whole || z.ranges == 1) return e;
     // 16 parts a request or more: more lanes a row
     const unsigned pairs = (unsigned)(a.B * a.Hkv), rows = pairs * (int64_t)a.rows <= 16384 ? (unsigned)a.rows : 1;
     if (z.ranges / a.B >= 16) {

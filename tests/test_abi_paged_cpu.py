@@ -89,6 +89,8 @@ def test_valid_problems_end_with_the_missing_device(L, kind):
     (Step, dict(B=0, length=0, add=0, length_out=0, table=0, added=0)), (Step, dict(rows=0, slots=0)),
     (Step, dict(capacity=0, free=0)), (Step, dict(width=0, ldt=0, table=0)),
     (Step, dict(length_out=0x10000000)), (Step, dict(nfree_out=0x15000000)),
+    (Rows, dict(Kc=(0x13000000, 4096, 128, 64), Vc=(0x13001000, 4096, 128, 64))),
+    (Rows, dict(Kc=(0x13000000, 4096, 256, 128), Vc=(0x13000080, 4096, 256, 128))),
     (Attn, dict(qoff=0, N=3)), (Attn, dict(lse=0)), (Attn, dict(Lk=80)), (Attn, dict(window=2**62, sinks=2**62)),
     (Attn, dict(Lk=0, table=0)), (Attn, dict(pages=0, K=(0, 0, 0, 0), V=(0, 0, 0, 0))),
     (Drafts, dict(Q=0)), (Drafts, dict(entries=0)), (Drafts, dict(M=2**31 - 257, ldp=2**31, ldq=2**31, N=1, B=3, P=2**44, Q=2**45))])
@@ -120,7 +122,11 @@ def test_nothing_to_do(L, kind, change):
     (Rows, dict(K=(0, 0, 128, 64)), gs.GS_ERR_ARG), (Rows, dict(Kc=(0x13000000, 2048, 128, 63)), gs.GS_ERR_SHAPE),
     (Rows, dict(Kc=(0x13000000, 0, 128, 64)), gs.GS_ERR_SHAPE), (Rows, dict(Vc=(0x14000000, -1, 128, 64)), gs.GS_ERR_SHAPE),
     (Rows, dict(Vc=(0x14000000, 2**41, 128, 64)), gs.GS_ERR_SHAPE), (Rows, dict(Kc=(0x11000000, 2048, 128, 64)), gs.GS_ERR_ARG),
-    (Rows, dict(Vc=(0x13000100, 2048, 128, 64)), gs.GS_ERR_ARG),
+    (Rows, dict(Vc=(0x13000100, 2048, 128, 64)), gs.GS_ERR_ARG), (Rows, dict(Vc=(0x13000000, 2048, 128, 64)), gs.GS_ERR_ARG),
+    # side by side, but a value too near, of other strides, or over the rows that are read
+    (Rows, dict(Kc=(0x13000000, 4096, 128, 64), Vc=(0x13000ffe, 4096, 128, 64)), gs.GS_ERR_ARG),
+    (Rows, dict(Kc=(0x13000000, 4096, 128, 64), Vc=(0x13001000, 4096, 64, 1024)), gs.GS_ERR_ARG),
+    (Rows, dict(Kc=(0x13000000, 4096, 128, 64), Vc=(0x13001000, 4096, 128, 64), K=(0x13010000, 0, 128, 64)), gs.GS_ERR_ARG),
     (Attn, dict(B=-1), gs.GS_ERR_SHAPE), (Attn, dict(N=-1), gs.GS_ERR_SHAPE), (Attn, dict(Lq=-1), gs.GS_ERR_SHAPE),
     (Attn, dict(Lk=81), gs.GS_ERR_SHAPE), (Attn, dict(Lk=-1), gs.GS_ERR_SHAPE), (Attn, dict(Hkv=3), gs.GS_ERR_SHAPE),
     (Attn, dict(Hkv=0), gs.GS_ERR_SHAPE), (Attn, dict(Hq=0), gs.GS_ERR_SHAPE), (Attn, dict(Dh=129), gs.GS_ERR_SHAPE),

@@ -186,6 +186,23 @@ def test_store_strides_and_special_values():
     assert both[..., Dh:].abs().sum() == 0
 
 
+@pytest.mark.parametrize("ct", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("where", ["page", "place", "head"])
+def test_store_side_by_side(where, ct):
+    """Keys and values in one tensor: a page of each in turn, a place, a head."""
+    N, Hkv, Dh, page, pages = 40, 3, 16, 8, 7
+    both = {"page": lambda c: (c[:, 0], c[:, 1]), "place": lambda c: (c[:, :, 0], c[:, :, 1]),
+            "head": lambda c: (c[:, :, :, 0], c[:, :, :, 1])}[where]
+    shape = {"page": (pages, 2, page, Hkv, Dh), "place": (pages, page, 2, Hkv, Dh), "head": (pages, page, Hkv, 2, Dh)}[where]
+    c = torch.zeros(shape, dtype=ct, device=DEV)
+    Kc, Vc = both(c)
+    K, V = torch.randn(N, Hkv, Dh, device=DEV), torch.randn(N, Hkv, Dh, device=DEV)
+    slots = torch.randperm(pages * page, device=DEV)[:N]
+    gs.gs_paged_store(K, V, slots, Kc, Vc)
+    assert torch.equal(Kc[slots // page, slots % page], K.to(ct)) and torch.equal(Vc[slots // page, slots % page], V.to(ct))
+    assert int((c != 0).sum()) == 2 * N * Hkv * Dh
+
+
 def test_store_far_slots():
     """A cache of more than 2^32 values."""
     pages, page, Hkv, Dh = 1 << 13, 64, 8, 1040
