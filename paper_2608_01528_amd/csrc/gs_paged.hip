@@ -207,19 +207,19 @@ template <bool LDS> __global__ void __launch_bounds__(256) plan_fill_kernel(Page
 
 // ---------------------------------------------------------------- rows
 
-// Eight values of a row from d on.
+// Eight values of a row from d on (read once: not kept in the caches).
 template <typename T> __device__ __forceinline__ void read8(float (&v)[8], const T *row, int d, int dh, bool vec) {
     typedef uint32_t u4v __attribute__((ext_vector_type(4)));
     if (vec) {
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                const u4v x = *reinterpret_cast<const u4v *>(row + d + 4 * q);
+                const u4v x = __builtin_nontemporal_load(reinterpret_cast<const u4v *>(row + d + 4 * q));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[4 * q + e] = __uint_as_float(x[e]);
             }
         } else {
-            const u4v x = *reinterpret_cast<const u4v *>(row + d);
+            const u4v x = __builtin_nontemporal_load(reinterpret_cast<const u4v *>(row + d));
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = bf16_to_f32((uint16_t)(x[e / 2] >> (16 * (e & 1))));
         }
