@@ -8,6 +8,10 @@
 // more.  Sums are fp64 in a fixed order.  What bounds it is a chain of dependent
 // loads (offsets, drafts, their probabilities, the row) and, as each instruction
 // runs once, the reading of the code: a thread holds no more than the row needs.
+// One request, 131072 entries, fp32: 4.2 + 4.0 us; 120 of 50257, bf16, 23 MB: 9.8 +
+// 5.0; 2000 of 1843, fp32: 8.6.  (Which lane's entry is the first goes by ballots:
+// an atomic of many lanes on LDS, which the compiler runs lane by lane, cost 8 us a
+// kernel.)
 #include "gs_scan.h"
 
 namespace gs {
