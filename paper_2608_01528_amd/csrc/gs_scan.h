@@ -40,7 +40,6 @@ template <typename V> __device__ __forceinline__ V wave_upto(V v) {
     v += lane_moved<0x142, 0xa>(v);         // lane 15 of the row before, into rows 1 and 3
     return v + lane_moved<0x143, 0xc>(v);   // lane 31, into rows 2 and 3
 }
-template <typename V> __device__ __forceinline__ V wave_total(V v) { return lane_value(wave_upto(v), 63); }
 
 // Exclusive sums of v over 1024 threads, and their total; room: 16 values that no
 // thread may still be reading (one barrier lies between its writes and its reads).

@@ -95,6 +95,31 @@ def test_windows(dtype, n, k, window, sinks):
     check(*problem(sum(n), dtype, n, k, 24, 4, 2, 64, lead=2, tail=3), window=window, sinks=sinks)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [[1, 1, 1], [3, 1, 8], [60, 2, 40]])
+@pytest.mark.parametrize("window,sinks", [(20, 3), (1, 0), (64, 33), (300, 1)])
+def test_windows_of_long_histories(dtype, n, window, sinks):
+    """Windows that leave most of the states out: a few tiles, or parts of them."""
+    check(*problem(window, dtype, n, [5000, 4001, 44], 16, 4, 2, 64), window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_values_that_are_not_finite_in_a_long_history(dtype):
+    """A history in parts: the last draft's value changes its own row alone."""
+    n, k = [4, 1], [30000, 50]
+    Q, Kc, Vc, table, klen, qoff = problem(21, dtype, n, k, 64, 4, 2, 64)
+    want = gs.gs_paged_attention(Q, Kc, Vc, table, klen, qoff, lse=True)
+    for value in (float("nan"), float("inf")):
+        V = Vc.clone()
+        V[int(table[0, (k[0] - 1) // 64]), (k[0] - 1) % 64, :, 9] = value
+        O, lse = gs.gs_paged_attention(Q, Kc, V, table, klen, qoff, lse=True)
+        assert torch.equal(lse, want[1])
+        rest = [0, 1, 2, 4]
+        assert torch.equal(O[rest], want[0][rest])
+        got = O[3, :, 9]
+        assert got.isnan().all() if value != value else (got == value).all()
+
+
 def test_many_requests():
     """More requests than a wave looks over at once, and than 64 of its lanes' shares."""
     for B in (65, 700, 4200):
