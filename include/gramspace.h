@@ -756,7 +756,9 @@ gs_status gs_paged_store(const gs_paged_rows *p, gs_dtype t, gs_dtype ct, void *
  *   lse        float N x Hq out, nullable
  *   ws         device workspace of gs_paged_attention_workspace(p, t) bytes (0: none),
  *              16-byte aligned; calls that may run at the same time need one each
- * fp32 accumulation; probabilities enter the second product in type t.  Work is
+ * fp32 accumulation.  Probabilities enter the second product in fp32, or, of bf16
+ * tensors, as two bf16 terms (Lq Hq / Hkv up to 32: off by 2^-15 of each at most) or
+ * rounded to one (more: 2^-8).  Work is
  * shared out by the lengths that the device holds, in parts whose results are
  * added in a fixed order: the same call gives the same bits.
  */

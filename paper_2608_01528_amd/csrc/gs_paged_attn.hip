@@ -218,6 +218,19 @@ template <typename T, int NJ> __device__ __forceinline__ void add_not_finite(f16
     }
 }
 
+// Probabilities of bf16 tensors enter the second product as two bf16 terms where a
+// wave works alone: the first 8 bits of each, and the rest rounded (off by 2^-15 of
+// the probability at most).  Those kernels wait for memory, and a second product on
+// the tile that is there takes little: 48 requests of up to 7000 states, 32 heads
+// over 8 of 128, 121.5 -> 122.5 us, the error of O 0.0022 -> 0.0017 of its norm, which
+// is its own rounding.  Blocks of 128 rows are bound by the products among others and
+// keep one rounded term (Op::pack): 5 pieces of up to 1500 rows on up to 6000
+// states, 444 us, with two terms 625, error 0.0023 and 0.0017.
+template <typename T, int NW> constexpr bool TWO_TERMS = sizeof(T) == 2 && NW == 1;
+__device__ __forceinline__ float first_term(float p) { return __uint_as_float(__float_as_uint(p) & 0xffff0000u); }
+// (at least 2^-17 of p, so that an infinite value times both terms is infinite)
+__device__ __forceinline__ float second_term(float p) { return fmaxf(p - first_term(p), 0x1p-17f * p); }
+
 // ------------------------------------------------------------ the pass
 
 // A block of 32 NW packed rows from m0 on of request b's head group hk against its
@@ -341,9 +354,24 @@ __device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, int *mar
             for (int n = 0; n < BN / 32; ++n)
 #pragma unroll
                 for (int s = 0; s < 16 / PER; ++s) {
-                    const typename Op<T>::V pf = Op<T>::pack(p[n], s);
+                    if constexpr (TWO_TERMS<T, NW>) {
+                        typename Op<T>::V first, second;
 #pragma unroll
-                    for (int j = 0; j < NJ; ++j) o[j] = Op<T>::mma(col_frag<T, DP>(vt, 32 * n, s, j, l), pf, o[j]);
+                        for (int e = 0; e < PER; ++e) {
+                            first[e] = (__bf16)first_term(p[n][PER * s + e]);
+                            second[e] = (__bf16)second_term(p[n][PER * s + e]);
+                        }
+#pragma unroll
+                        for (int j = 0; j < NJ; ++j) {
+                            const typename Op<T>::V v = col_frag<T, DP>(vt, 32 * n, s, j, l);
+                            o[j] = Op<T>::mma(v, first, o[j]);
+                            o[j] = Op<T>::mma(v, second, o[j]);
+                        }
+                    } else {
+                        const typename Op<T>::V pf = Op<T>::pack(p[n], s);
+#pragma unroll
+                        for (int j = 0; j < NJ; ++j) o[j] = Op<T>::mma(col_frag<T, DP>(vt, 32 * n, s, j, l), pf, o[j]);
+                    }
                 }
         }
         if (differ(live, j0)) {
@@ -416,14 +444,19 @@ template <typename T> struct Op16;
 template <> struct Op16<bf16_t> {
     static constexpr int BN = 32;       // keys a tile: the 32 terms of a product
     static __device__ __forceinline__ f4v mma(bf8v a, bf8v b, f4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-    // (probabilities in bf16, as in Op::pack)
-    static __device__ __forceinline__ bf8v pack(const f4v (&p)[2]) {
-        bf8v r;
+    // o += v p, the probabilities in two terms
+    struct Terms {
+        bf8v first, second;
+        __device__ __forceinline__ explicit Terms(const f4v (&p)[2]) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r[e] = (__bf16)p[e / 4][e % 4];
-        return r;
-    }
-    // values 16 j .. of the keys in pack's order
+            for (int e = 0; e < 8; ++e) {
+                first[e] = (__bf16)first_term(p[e / 4][e % 4]);
+                second[e] = (__bf16)second_term(p[e / 4][e % 4]);
+            }
+        }
+        __device__ __forceinline__ f4v add(bf8v v, f4v o) const { return mma(v, second, mma(v, first, o)); }
+    };
+    // values 16 j .. of the keys in the terms' order
     template <int DP> static __device__ __forceinline__ bf8v col(const char *tile, int j, int l) {
         const int a = l & 15, k = 4 * (l >> 4) + (a >> 2), n = 16 * j + 4 * (a & 3);
         const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GS_LDS s4v *)(tile + place16<bf16_t, DP>(k, n >> 3) + 2 * (n & 7)));
@@ -439,7 +472,11 @@ template <> struct Op16<float> {
         for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
         return c;
     }
-    static __device__ __forceinline__ f4v pack(const f4v (&p)[1]) { return p[0]; }
+    struct Terms {
+        f4v p;
+        __device__ __forceinline__ explicit Terms(const f4v (&p)[1]) : p(p[0]) {}
+        __device__ __forceinline__ f4v add(f4v v, f4v o) const { return mma(v, p, o); }
+    };
     template <int DP> static __device__ __forceinline__ f4v col(const char *tile, int j, int l) {
         f4v r;
         const int n = 16 * j + (l & 15), k = 4 * (l >> 4);
@@ -553,9 +590,9 @@ __device__ __forceinline__ void pass16(const PagedAttnArgs &a, char *lds, int b,
                 p[n][e] = __builtin_amdgcn_exp2f(fmaf(p[n][e], c, -ref));
                 sum += p[n][e];
             }
-        const typename Op<T>::V pf = Op16<T>::pack(p);
+        const typename Op16<T>::Terms terms(p);
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) o[j] = Op16<T>::mma(Op16<T>::template col<DP>(lds + TILE, j, l), pf, o[j]);
+        for (int j = 0; j < NJ; ++j) o[j] = terms.add(Op16<T>::template col<DP>(lds + TILE, j, l), o[j]);
     }
     if (left_out) {
         for (int x = x0; x < x1; ++x) {
