@@ -637,9 +637,13 @@ gs_status gs_sample(const void *S, gs_dtype st, int64_t B, int64_t M, int64_t ld
  * table[b, j / page] page + j % page of the cache.  A step adds new positions to
  * requests: rows qoff[b] .. qoff[b + 1] - 1 of its tensors (qoff int32[B + 1],
  * nondecreasing) belong to request b.  One step is gs_paged_plan, gs_paged_store
- * of the new keys and values, gs_paged_attention, and, where entries were
- * drafted, gs_verify.  All lengths, tables and offsets stay in device memory, so
- * a captured step can be replayed.
+ * of the new keys and values, gs_paged_attention_added, and, where entries were
+ * drafted, gs_verify_added.  A plan may refuse a request its positions: its rows
+ * are there all the same, but stand for no position.  The plan's `added` tells the
+ * later calls; those without it take every request's rows for its last positions,
+ * so what they give for a refused request belongs to no position and is to be
+ * dropped.  All lengths, tables and offsets stay in device memory, so a captured
+ * step can be replayed.
  *
  * gs_paged_plan -- pages and slots of a step.  With len = length[b] and
  * up(x) = ceil(x / page):
@@ -653,7 +657,7 @@ gs_status gs_sample(const void *S, gs_dtype st, int64_t B, int64_t M, int64_t ld
  *      (up(len + add) <= width; len + add below 2^31), its rows end within `rows`,
  *      and it needs no page or no more are wanted up to and with it, by all that
  *      pass the first two conditions, than are free.  Others get nothing: length_out = len, added 0,
- *      slots -1.
+ *      slots -1 (their rows in qoff stand for no position).
  *   qoff[0] = 0, qoff[b + 1] = qoff[b] + max(add[b], 0), served or not (2^31 - 1
  *   where it would pass that)
  *   slots[qoff[b] + i] = slot of position len + i of a served request; -1 in the
@@ -776,6 +780,12 @@ size_t gs_paged_attention_workspace(const gs_paged_attn *p, gs_dtype t);
 
 gs_status gs_paged_attention(const gs_paged_attn *p, gs_dtype t, void *ws, size_t ws_bytes, void *stream);
 
+/* The same with the positions that each request got (added: int32[B] device, as
+   gs_paged_plan gives it; null: all got theirs).  Rows of a request with
+   added[b] <= 0 see no state: O = 0 and lse = -inf. */
+gs_status gs_paged_attention_added(const gs_paged_attn *p, const int32_t *added, gs_dtype t, void *ws, size_t ws_bytes,
+                                   void *stream);
+
 /*
  * gs_verify -- drafted entries taken or refused by the probabilities p that the
  * model gives at their places (speculative sampling: what is left has the
@@ -820,6 +830,12 @@ typedef struct {
 size_t gs_verify_workspace(int64_t B, int64_t M);
 
 gs_status gs_verify(const gs_drafts *p, gs_dtype pt, void *ws, size_t ws_bytes, void *stream);
+
+/* The same with the positions that each request got (added: int32[B] device, as
+   gs_paged_plan gives it; null: all got theirs).  A request with added[b] <= 0
+   gives accepted 0, entry -1 and -1 in its rows of entries, and none of its rows
+   of P and Q is read. */
+gs_status gs_verify_added(const gs_drafts *p, const int32_t *added, gs_dtype pt, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

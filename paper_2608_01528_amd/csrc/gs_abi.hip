@@ -1121,6 +1121,10 @@ size_t gs_paged_attention_workspace(const gs_paged_attn *p, gs_dtype t) {
 }
 
 gs_status gs_paged_attention(const gs_paged_attn *p, gs_dtype t, void *ws, size_t ws_bytes, void *stream) {
+    return gs_paged_attention_added(p, nullptr, t, ws, ws_bytes, stream);
+}
+
+gs_status gs_paged_attention_added(const gs_paged_attn *p, const int32_t *added, gs_dtype t, void *ws, size_t ws_bytes, void *stream) {
     const char *fn = "gs_paged_attention";
     if (!p) return fail(GS_ERR_ARG, "%s: the problem is null", fn);
     if (!is_batch_type(t)) return fail(GS_ERR_DTYPE, "%s: tensors must be f32 or bf16", fn);
@@ -1143,19 +1147,20 @@ gs_status gs_paged_attention(const gs_paged_attn *p, gs_dtype t, void *ws, size_
     GS_CHECK(check_aligned(p->table, 4, "table"));
     GS_CHECK(check_aligned(p->klen, 4, "klen"));
     GS_CHECK(check_aligned(p->qoff, 4, "qoff"));
+    GS_CHECK(check_aligned(added, 4, "added"));
     GS_CHECK(check_aligned(p->lse, 4, "lse"));
     const size_t es = esize(t), need = gs_paged_attention_workspace(p, t);
     GS_CHECK(check_ws(fn, ws, ws_bytes, need));
     GS_CHECK(check_overlaps({seq_span(Q, q, es, "Q"), seq_span(p->K, c, es, "K"), seq_span(p->V, c, es, "V"),
                              span(p->table, p->B, p->width, p->ldt, 4, "table"), span(p->klen, 1, p->B, p->B, 4, "klen"),
-                             span(p->qoff, 1, p->B + 1, p->B + 1, 4, "qoff")},
+                             span(p->qoff, 1, p->B + 1, p->B + 1, 4, "qoff"), span(added, 1, p->B, p->B, 4, "added")},
                             {seq_span(O, q, es, "O"), span(p->lse, 1, p->N * p->Hq, 1, 4, "lse"), bytes_span(ws, need, "workspace")}));
     if (!p->B || !p->N || !p->Lq) return ok();
     GS_CHECK(check_device());
     PagedAttnArgs a = paged_args(p);
     a.Q = Q.p; a.K = p->K.p; a.V = p->V.p; a.O = O.p; a.lse = p->lse;
     a.q = strides(Q); a.k = strides(p->K); a.v = strides(p->V); a.o = strides(O);
-    a.table = p->table; a.klen = p->klen; a.qoff = p->qoff;
+    a.table = p->table; a.klen = p->klen; a.qoff = p->qoff; a.added = added;
     a.scale = (float)p->scale;
     a.vec = vec_rows(Q, q, t) && vec_rows(p->K, c, t) && vec_rows(p->V, c, t) && vec_rows(O, q, t);
     return launched(launch_paged_attn(t, a, ws, (hipStream_t)stream), fn);
@@ -1167,6 +1172,10 @@ size_t gs_verify_workspace(int64_t B, int64_t M) {
 }
 
 gs_status gs_verify(const gs_drafts *p, gs_dtype pt, void *ws, size_t ws_bytes, void *stream) {
+    return gs_verify_added(p, nullptr, pt, ws, ws_bytes, stream);
+}
+
+gs_status gs_verify_added(const gs_drafts *p, const int32_t *added, gs_dtype pt, void *ws, size_t ws_bytes, void *stream) {
     const char *fn = "gs_verify";
     if (!p) return fail(GS_ERR_ARG, "%s: the drafts are null", fn);
     if (!is_batch_type(pt)) return fail(GS_ERR_DTYPE, "%s: probabilities must be f32 or bf16", fn);
@@ -1177,7 +1186,7 @@ gs_status gs_verify(const gs_drafts *p, gs_dtype pt, void *ws, size_t ws_bytes, 
     if ((p->P && !within_reach(p->N, p->ldp, p->M)) || (p->Q && !within_reach(p->N, p->ldq, p->M)))
         return fail(GS_ERR_SHAPE, "%s: leading dimension out of range", fn);
     const struct { const void *p; bool needed; const char *name; } each[] = {
-        {p->drafted, p->N > 0, "drafted"}, {p->u, p->N > 0, "u"}, {p->v, p->B > 0, "v"}, {p->qoff, p->B > 0, "qoff"},
+        {p->drafted, p->N > 0, "drafted"}, {p->u, p->N > 0, "u"}, {p->v, p->B > 0, "v"}, {p->qoff, p->B > 0, "qoff"}, {added, false, "added"},
         {p->accepted, p->B > 0, "accepted"}, {p->entry, p->B > 0, "entry"}, {p->entries, false, "entries"}};
     for (const auto &e : each) {
         if (!e.p && e.needed) return fail(GS_ERR_ARG, "%s: %s is null", fn, e.name);
@@ -1188,14 +1197,15 @@ gs_status gs_verify(const gs_drafts *p, gs_dtype pt, void *ws, size_t ws_bytes, 
     const size_t es = esize(pt);
     GS_CHECK(check_overlaps({span(p->P, p->N, p->M, p->ldp, es, "P"), span(p->Q, p->N, p->M, p->ldq, es, "Q"),
                              span(p->drafted, 1, p->N, p->N, 4, "drafted"), span(p->u, 1, p->N, p->N, 4, "u"),
-                             span(p->v, 1, p->B, p->B, 4, "v"), span(p->qoff, 1, p->B + 1, p->B + 1, 4, "qoff")},
+                             span(p->v, 1, p->B, p->B, 4, "v"), span(p->qoff, 1, p->B + 1, p->B + 1, 4, "qoff"),
+                             span(added, 1, p->B, p->B, 4, "added")},
                             {span(p->accepted, 1, p->B, p->B, 4, "accepted"), span(p->entry, 1, p->B, p->B, 4, "entry"),
                              span(p->entries, 1, p->N, p->N, 4, "entries"), bytes_span(ws, need, "workspace")}));
     if (p->B == 0) return ok();
     GS_CHECK(check_device());
     VerifyArgs a{};
     a.B = p->B; a.N = p->N; a.M = p->M; a.P = p->P; a.ldp = p->ldp; a.Q = p->Q; a.ldq = p->ldq;
-    a.drafted = p->drafted; a.u = p->u; a.v = p->v; a.qoff = p->qoff;
+    a.drafted = p->drafted; a.u = p->u; a.v = p->v; a.qoff = p->qoff; a.added = added;
     a.accepted = p->accepted; a.entry = p->entry; a.entries = p->entries;
     return launched(launch_verify(pt, a, ws, (hipStream_t)stream), fn);
 }

@@ -336,6 +336,7 @@ struct PagedAttnArgs {
     int pages, page, window, sinks;
     int64_t ldt;
     const int32_t *table, *klen, *qoff; // qoff nullable
+    const int32_t *added;               // nullable
     float scale;
     bool vec;
     // set by launch_paged_attn
@@ -354,7 +355,8 @@ size_t paged_attn_workspace(gs_dtype t, const PagedAttnArgs &a);
 hipError_t launch_paged_attn(gs_dtype t, PagedAttnArgs a, void *ws, hipStream_t s);
 
 // Drafted entries (gs_verify.hip).
-struct VerifyRequest { int64_t first, n, taken; int32_t refused; };     // a request's rows, drafts taken, the one refused
+// a request's rows, drafts taken, the one refused, whether there is something to draw from
+struct VerifyRequest { int64_t first, n, taken; int32_t refused, drawn; };
 struct VerifyArgs {
     int64_t B, N, M;
     const void *P; int64_t ldp;
@@ -362,6 +364,7 @@ struct VerifyArgs {
     const int32_t *drafted;
     const float *u, *v;
     const int32_t *qoff;
+    const int32_t *added;               // nullable
     int32_t *accepted, *entry, *entries;
     // set by launch_verify
     int64_t parts;

@@ -35,11 +35,14 @@ using namespace attn;
 // ------------------------------------------------------------ what is seen
 
 // Rows of request b: qoff clamped to the tensors' rows; `n` of them count for
-// positions, the first `count` are computed.
+// positions, the first `count` are computed.  A request that got no positions for
+// its rows has them see nothing: they stand before state 0 of none.
 struct Rows {
     int first, n, count, kl;
     __device__ __forceinline__ Rows(const PagedAttnArgs &a, int b) {
+        const int got = a.added ? a.added[b] : 1;
         kl = clamped(a.klen, b, a.Lk);
+        if (got <= 0) kl = 0;
         if (!a.qoff) {
             first = b;
             n = 1;

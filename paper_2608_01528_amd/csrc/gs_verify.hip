@@ -34,6 +34,7 @@ struct Request {
     int64_t first;      // its first row
     int64_t n, taken;   // its rows, drafts taken
     int32_t refused;    // the draft that was not, -1 if all were
+    int32_t drawn;      // its rows stand for positions: an entry is drawn
 };
 
 // Every wave finds this on its own, a draft a lane.
@@ -44,6 +45,8 @@ template <typename T> __device__ __forceinline__ Request request(const VerifyArg
     r.n = bounded(a.qoff, b + 1, a.N) - r.first;
     r.refused = -1;
     if (r.n < 0) r.n = 0;
+    r.drawn = r.n > 0 && (!a.added || a.added[b] > 0);
+    if (!r.drawn) return r;
     for (int64_t i0 = 0; i0 < r.n - 1; i0 += 64) {
         const int64_t i = i0 + l, row = r.first + i;
         bool ok = true;
@@ -66,7 +69,7 @@ template <typename T> __device__ __forceinline__ Request request(const VerifyArg
             return r;
         }
     }
-    r.taken = r.n ? r.n - 1 : 0;
+    r.taken = r.n - 1;
     return r;
 }
 
@@ -216,7 +219,7 @@ template <typename T, int NW, int H> __global__ void __launch_bounds__(64 * NW) 
     const float v = a.v[b];
     const Request r = request<T>(a, b);
     int64_t entry = -1;
-    if (r.n) {
+    if (r.drawn) {
         Part<T, H> part;
         part.load(a, r, H * threadIdx.x);
         double mine = part.sum(), total;
@@ -237,8 +240,8 @@ template <typename T> __global__ void __launch_bounds__(GROUP) verify_sums_kerne
     const int64_t b = blockIdx.x / groups, k = blockIdx.x % groups * WAVES + (threadIdx.x >> 6);
     const int l = threadIdx.x & 63;
     const Request r = request<T>(a, b);
-    if (k == 0 && l == 0) a.requests[b] = VerifyRequest{r.first, r.n, r.taken, r.refused};
-    if (!r.n || k >= a.parts) return;
+    if (k == 0 && l == 0) a.requests[b] = VerifyRequest{r.first, r.n, r.taken, r.refused, r.drawn};
+    if (!r.drawn || k >= a.parts) return;
     constexpr int H = UNIT / 64;
     Part<T, H> part;
     part.load(a, r, k * UNIT + H * l);
@@ -255,8 +258,8 @@ template <typename T> __global__ void __launch_bounds__(GROUP) verify_draw_kerne
     const int t = threadIdx.x;
     const int64_t b = blockIdx.x;
     const VerifyRequest given = a.requests[b];
-    const Request r{given.first, given.n, given.taken, given.refused};
-    if (!r.n) {
+    const Request r{given.first, given.n, given.taken, given.refused, given.drawn};
+    if (!r.drawn) {
         write_out(a, b, r, -1);
         return;
     }

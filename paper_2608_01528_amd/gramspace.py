@@ -121,8 +121,10 @@ _SIGS["gs_paged_plan"] = ([_vp, _vp, ctypes.c_size_t, _vp], ctypes.c_int)
 _SIGS["gs_paged_store"] = ([_vp, ctypes.c_int, ctypes.c_int, _vp], ctypes.c_int)
 _SIGS["gs_paged_attention_workspace"] = ([_vp, ctypes.c_int], ctypes.c_size_t)
 _SIGS["gs_paged_attention"] = ([_vp, ctypes.c_int, _vp, ctypes.c_size_t, _vp], ctypes.c_int)
+_SIGS["gs_paged_attention_added"] = ([_vp, _vp, ctypes.c_int, _vp, ctypes.c_size_t, _vp], ctypes.c_int)
 _SIGS["gs_verify_workspace"] = ([_i64, _i64], ctypes.c_size_t)
 _SIGS["gs_verify"] = ([_vp, ctypes.c_int, _vp, ctypes.c_size_t, _vp], ctypes.c_int)
+_SIGS["gs_verify_added"] = ([_vp, _vp, ctypes.c_int, _vp, ctypes.c_size_t, _vp], ctypes.c_int)
 _PAGED_STEP = struct.Struct("=3q4Q2qQq5Q")
 _PAGED_ROWS = struct.Struct("=5qQ" + "Q3q" * 4)
 _PAGED_ATTN = struct.Struct("=11q3Q2qd" + "Q3q" * 4 + "Q")
@@ -810,7 +812,9 @@ def gs_paged_plan(length: torch.Tensor, add: torch.Tensor, table: torch.Tensor, 
     only if nfree_out is nfree itself (and length if length_out is).  Returns
     (length, nfree, qoff, slots, added): the new lengths and height, the
     requests' first rows (int32, B + 1), the slots of `rows` rows (int64, -1
-    for none) and the positions each request got (int32, B)."""
+    for none) and the positions each request got (int32, B; 0 where pages, table
+    or rows had no room: hand it on to gs_paged_attention and gs_verify, as qoff
+    counts such a request's rows all the same)."""
     # (allocating the results is most of what a call costs on the host: like an
     # input where there is one of their kind)
     i32 = torch.int32
@@ -852,7 +856,7 @@ def gs_paged_attention(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, tabl
                        qoff: torch.Tensor | None = None, max_new: int | None = None, max_len: int | None = None,
                        window: int = 0, sinks: int = 0, scale: float | None = None, lse: bool = False,
                        out: torch.Tensor | None = None, lse_out: torch.Tensor | None = None,
-                       workspace: torch.Tensor | None = None):
+                       workspace: torch.Tensor | None = None, added: torch.Tensor | None = None):
     """Attention of the rows Q (N, Hq, Dh) to their requests' states in the
     paged cache: request b has klen[b] (int32) states in the pages of
     table[b], and the rows qoff[b] .. qoff[b + 1] - 1 (int32, B + 1; None: one
@@ -860,8 +864,10 @@ def gs_paged_attention(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, tabl
     own (window > 0: the last `window` of them and the first `sinks`).
     max_new, max_len: most rows and states of a request, as far as they are
     known (N, and what the table has room for, otherwise).  scale 1 / sqrt(Dh)
-    by default.  Returns O, or (O, lse) with lse (N, Hq) fp32; rows of no
-    request are not written."""
+    by default.  added (int32, B): the positions each request got from the
+    plan; the rows of one that got none see no state (O = 0, lse = -inf).
+    Returns O, or (O, lse) with lse (N, Hq) fp32; rows of no request are not
+    written."""
     t, c, at = _cache(Kc, Vc)
     q = Q.shape
     if len(q) != 3 or q[2] != c[3]:
@@ -888,14 +894,14 @@ def gs_paged_attention(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, tabl
                              *_rows3(Q, "Q", q, Kc.dtype), *at, *_rows3(out, "out", q, Kc.dtype), lp)
     L = lib()
     ws, n, _keep = _workspace(L.gs_paged_attention_workspace(given, t), workspace, Q.device)
-    _check(L.gs_paged_attention(given, t, ws, n, _stream()))
+    _check(L.gs_paged_attention_added(given, _per_row(added, "added", B, torch.int32) or None, t, ws, n, _stream()))
     return (out, lse_out) if lse else out
 
 
 def gs_verify(P: torch.Tensor, drafted: torch.Tensor, u: torch.Tensor, v: torch.Tensor, qoff: torch.Tensor,
               Q: torch.Tensor | None = None, entries: bool = False, accepted_out: torch.Tensor | None = None,
               entry_out: torch.Tensor | None = None, entries_out: torch.Tensor | None = None,
-              workspace: torch.Tensor | None = None):
+              workspace: torch.Tensor | None = None, added: torch.Tensor | None = None):
     """Drafted entries taken or refused: the rows qoff[b] .. qoff[b + 1] - 1
     (int32, B + 1) of the probabilities P (N x M) are request b's, drafted
     (int32, N) the entry drafted to follow each row (the last row's is not
@@ -903,7 +909,9 @@ def gs_verify(P: torch.Tensor, drafted: torch.Tensor, u: torch.Tensor, v: torch.
     (fp32, N) and v (fp32, B) random numbers in [0, 1).  Returns (accepted,
     entry), int32 of B: the drafts taken and the entry drawn after them; with
     `entries` also int32 of N, each request's new entries from its first row
-    on and -1 behind them (rows of no request are not written)."""
+    on and -1 behind them (rows of no request are not written).  added (int32,
+    B): the positions each request got from the plan; one that got none takes
+    and draws nothing (accepted 0, entry -1)."""
     pt, ldp = _mat(P, "P")
     _here(P, "P")
     N, M = P.shape
@@ -927,5 +935,5 @@ def gs_verify(P: torch.Tensor, drafted: torch.Tensor, u: torch.Tensor, v: torch.
                          _per_row(ent, "entry_out", B, i32), _per_row(every, "entries_out", N, i32))
     L = lib()
     ws, n, _keep = _workspace(L.gs_verify_workspace(B, M), workspace, dev)
-    _check(L.gs_verify(given, pt, ws, n, _stream()))
+    _check(L.gs_verify_added(given, _per_row(added, "added", B, i32) or None, pt, ws, n, _stream()))
     return (acc, ent, every) if entries else (acc, ent)
