@@ -762,48 +762,45 @@ template <typename T, int DP, int BN> __global__ void __launch_bounds__(256) few
     const int hk = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv, d = 4 * (threadIdx.x % LANES);
     Cut c(a, b);
     const Rows r(a, b);
-    const int rows = r.count * a.G, step = gridDim.y * (256 / LANES);
-    int m = blockIdx.y * (256 / LANES) + threadIdx.x / LANES;
-    if (m >= rows || d >= a.Dh) return;
+    const int m = blockIdx.y * (256 / LANES) + threadIdx.x / LANES;
+    if (m >= r.count * a.G || d >= a.Dh) return;
     c.find<BN>(a, b, hk);
     if (c.i0 == c.i1) return;
-    for (; m < rows; m += step) {
-        float top = -INFINITY, sum = 0.f;
-        f4v o = {0.f, 0.f, 0.f, 0.f};
-        // four parts at a time, their log-sums and values asked for together
-        for (int i = c.i0; i <= c.i1; i += 4) {
-            float lse[4];
-            f4v v[4];
+    float top = -INFINITY, sum = 0.f;
+    f4v o = {0.f, 0.f, 0.f, 0.f};
+    // four parts at a time, their log-sums and values asked for together
+    for (int i = c.i0; i <= c.i1; i += 4) {
+        float lse[4];
+        f4v v[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int64_t at = c.place(i + k <= c.i1 ? i + k : c.i1, m);
-                lse[k] = a.part_lse[at];
-                v[k] = *reinterpret_cast<const f4v *>(a.part + at * DP + d);
-            }
-            float next = top;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (i + k <= c.i1) next = fmaxf(next, lse[k]);
-            const float ref = next == -INFINITY ? 0.f : next;
-            const float turn = __builtin_amdgcn_exp2f((top - ref) * LOG2E);
-            top = next;
-            sum *= turn;
-            o *= turn;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (i + k > c.i1) continue;
-                const float e = __builtin_amdgcn_exp2f((lse[k] - ref) * LOG2E);
-                sum += e;
-                o += e * v[k];
-            }
+        for (int k = 0; k < 4; ++k) {
+            const int64_t at = c.place(i + k <= c.i1 ? i + k : c.i1, m);
+            lse[k] = a.part_lse[at];
+            v[k] = *reinterpret_cast<const f4v *>(a.part + at * DP + d);
         }
-        const float ref = top == -INFINITY ? 0.f : top;
-        const float inv = sum != 0.f ? 1.f / sum : 0.f;
-        const RowOf row(m, hk, a.G);
-        const int64_t at = r.first + row.i;
-        store4<T>(static_cast<T *>(a.O) + at * a.o.l + row.h * a.o.h, d, a.Dh, a.vec, o * inv);
-        if (a.lse && d == 0) a.lse[at * a.Hq + row.h] = joined_lse(ref, sum);
+        float next = top;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i + k <= c.i1) next = fmaxf(next, lse[k]);
+        const float ref = next == -INFINITY ? 0.f : next;
+        const float turn = __builtin_amdgcn_exp2f((top - ref) * LOG2E);
+        top = next;
+        sum *= turn;
+        o *= turn;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (i + k > c.i1) continue;
+            const float e = __builtin_amdgcn_exp2f((lse[k] - ref) * LOG2E);
+            sum += e;
+            o += e * v[k];
+        }
     }
+    const float ref = top == -INFINITY ? 0.f : top;
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    const RowOf row(m, hk, a.G);
+    const int64_t at = r.first + row.i;
+    store4<T>(static_cast<T *>(a.O) + at * a.o.l + row.h * a.o.h, d, a.Dh, a.vec, o * inv);
+    if (a.lse && d == 0) a.lse[at * a.Hq + row.h] = joined_lse(ref, sum);
 }
 
 // The same for many parts: a work-group for 4 LANES values of a row, parts shared out
@@ -816,50 +813,47 @@ template <typename T, int DP, int BN, int NT, int LANES> __global__ void __launc
     const int hk = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv;
     Cut c(a, b);
     const Rows r(a, b);
-    const int rows = r.count * a.G;
-    if (!rows) return;
+    const int m = blockIdx.y;
+    if (m >= r.count * a.G) return;
     c.find<BN>(a, b, hk);
     const int i0 = c.i0, i1 = c.i1;
     if (i0 == i1) return;
-    for (int m = blockIdx.y; m < rows; m += gridDim.y) {
-        auto place = [&](int i) { return c.place(i, m); };
-        float top = -INFINITY;
-        for (int i = i0 + t; i <= i1; i += NT) top = fmaxf(top, a.part_lse[place(i)]);
+    auto place = [&](int i) { return c.place(i, m); };
+    float top = -INFINITY;
+    for (int i = i0 + t; i <= i1; i += NT) top = fmaxf(top, a.part_lse[place(i)]);
 #pragma unroll
-        for (int k = 32; k; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
-        if (l == 0) tops[w] = top;
-        __syncthreads();
+    for (int k = 32; k; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
+    if (l == 0) tops[w] = top;
+    __syncthreads();
 #pragma unroll
-        for (int k = 0; k < WAVES; ++k) top = fmaxf(top, tops[k]);
-        const float ref = top == -INFINITY ? 0.f : top;
-        f4v o = {0.f, 0.f, 0.f, 0.f};
-        float sum = 0.f;
+    for (int k = 0; k < WAVES; ++k) top = fmaxf(top, tops[k]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    f4v o = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
 #pragma unroll 4
-        for (int i = i0 + g; i <= i1; i += GROUPS) {
-            const int64_t at = place(i);
-            const float e = __builtin_amdgcn_exp2f((a.part_lse[at] - ref) * LOG2E);
-            sum += e;
-            o += e * *reinterpret_cast<const f4v *>(a.part + at * DP + d);
-        }
+    for (int i = i0 + g; i <= i1; i += GROUPS) {
+        const int64_t at = place(i);
+        const float e = __builtin_amdgcn_exp2f((a.part_lse[at] - ref) * LOG2E);
+        sum += e;
+        o += e * *reinterpret_cast<const f4v *>(a.part + at * DP + d);
+    }
 #pragma unroll
-        for (int k = LANES; k < 64; k <<= 1) {
-            sum += __shfl_xor(sum, k);
+    for (int k = LANES; k < 64; k <<= 1) {
+        sum += __shfl_xor(sum, k);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], k);
-        }
-        if (l < LANES) sums[w][l] = o;
-        if (l == 0) weights[w] = sum;
-        __syncthreads();
-        if (t < LANES) {
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], k);
+    }
+    if (l < LANES) sums[w][l] = o;
+    if (l == 0) weights[w] = sum;
+    __syncthreads();
+    if (t < LANES) {
 #pragma unroll
-            for (int k = 1; k < WAVES; ++k) o += sums[k][t], sum += weights[k];
-            const float inv = sum != 0.f ? 1.f / sum : 0.f;
-            const RowOf row(m, hk, a.G);
-            const int64_t at = r.first + row.i;
-            if (d < a.Dh) store4<T>(static_cast<T *>(a.O) + at * a.o.l + row.h * a.o.h, d, a.Dh, a.vec, o * inv);
-            if (a.lse && d == 0) a.lse[at * a.Hq + row.h] = joined_lse(ref, sum);
-        }
-        __syncthreads();
+        for (int k = 1; k < WAVES; ++k) o += sums[k][t], sum += weights[k];
+        const float inv = sum != 0.f ? 1.f / sum : 0.f;
+        const RowOf row(m, hk, a.G);
+        const int64_t at = r.first + row.i;
+        if (d < a.Dh) store4<T>(static_cast<T *>(a.O) + at * a.o.l + row.h * a.o.h, d, a.Dh, a.vec, o * inv);
+        if (a.lse && d == 0) a.lse[at * a.Hq + row.h] = joined_lse(ref, sum);
     }
 }
 
@@ -1060,9 +1054,9 @@ template <typename T, int DC, int R, bool VEC> hipError_t launch_few(const Paged
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || z.whole || z.ranges == 1) return e;
     // 16 parts a request or more: more lanes a row
-    const unsigned pairs = (unsigned)(a.B * a.Hkv), rows = pairs * (int64_t)a.rows <= 16384 ? (unsigned)a.rows : 1;
+    const unsigned pairs = (unsigned)(a.B * a.Hkv);
     if (z.ranges / a.B >= 16) {
-        few_join_many_kernel<T, DP, BN, 1024, 8><<<dim3(pairs, rows, DP / 32), dim3(1024), 0, s>>>(a);
+        few_join_many_kernel<T, DP, BN, 1024, 8><<<dim3(pairs, (unsigned)a.rows, DP / 32), dim3(1024), 0, s>>>(a);
     } else {
         const unsigned pieces = (unsigned)((a.rows * (DP / 4) + 255) / 256);
         few_join_kernel<T, DP, BN><<<dim3(pairs, pieces), dim3(256), 0, s>>>(a);
