@@ -1053,10 +1053,19 @@ template <typename T, int DC, int R, bool VEC> hipError_t launch_few(const Paged
     few_kernel<T, DC, R, VEC><<<dim3((unsigned)((z.ranges * a.Hkv + 7) / 8 * 8)), dim3(64), 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || z.whole || z.ranges == 1) return e;
-    // 16 parts a request or more: more lanes a row
+    // Parts of a row are joined by a thread for 4 values, or shared out to a work-group:
+    // from 16 a request on (the mean; one long history among short ones has more) to one
+    // of 512 threads for a row, or, where they fit the CUs, to such of 1024 for 32 values.
+    // Heads of 128 values, us by thread, by 512 and by 1024: 12 parts of 21 requests, 32
+    // rows each 5.0, 5.5, 23; 16 of 16, 32 rows 5.5, 4.9, 17; 128 rows 6.4, 9.8, 61; 32 of
+    // 8, 32 rows 7.7, 4.7, 10; 512 parts of one, 32 rows over 4 heads -, 8.6, 7.1; 782
+    // parts, 8 rows -, 10.9, 7.4; 256 parts of one of 16 requests, 128 rows 42, 13, 47.
     const unsigned pairs = (unsigned)(a.B * a.Hkv);
-    if (z.ranges / a.B >= 16) {
+    const int64_t parts = z.ranges / a.B, groups = (int64_t)pairs * a.rows * (DP / 32);
+    if (parts >= 16 && groups <= 256) {
         few_join_many_kernel<T, DP, BN, 1024, 8><<<dim3(pairs, (unsigned)a.rows, DP / 32), dim3(1024), 0, s>>>(a);
+    } else if (parts >= 16) {
+        few_join_many_kernel<T, DP, BN, 512, DP / 4><<<dim3(pairs, (unsigned)a.rows, 1), dim3(512), 0, s>>>(a);
     } else {
         const unsigned pieces = (unsigned)((a.rows * (DP / 4) + 255) / 256);
         few_join_kernel<T, DP, BN><<<dim3(pairs, pieces), dim3(256), 0, s>>>(a);
