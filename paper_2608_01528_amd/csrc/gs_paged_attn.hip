@@ -236,6 +236,25 @@ __device__ __forceinline__ float second_term(float p) { return fmaxf(p - first_t
 
 // ------------------------------------------------------------ the pass
 
+// Waves a SIMD that registers are kept for.  (A wave on its own holds the whole tile
+// that is on its way.  A value that found no register is read back from memory, and
+// such a read waits for all loads before it, the next tile's too: 40 requests of up to
+// 6000 states, 32 rows over 4 heads of 128, bf16, 94 us with two waves and 44 such
+// values, 70 with one and none.)
+template <typename T, int DC, int NW> constexpr int min_waves() {
+    return NW == 1 ? (sizeof(T) == 4 || DC > 64 ? 1 : 2) : (sizeof(T) == 4 && DC > 64 ? 1 : 2);
+}
+
+// Heads whose values' places in LDS are too many (64 of four bytes) to be kept from
+// tile to tile: they are worked out anew from a lane number of which the compiler
+// does not know that it is the same.  (fp32 heads of 128, 32 rows: 167 -> 138 us,
+// 8 rows 111 -> 105.)
+template <typename T, int DC> constexpr bool MANY_PLACES = sizeof(T) == 4 && DC > 96;
+__device__ __forceinline__ int anew(int l) {
+    asm volatile("" : "+v"(l));
+    return l;
+}
+
 // A block of 32 NW packed rows from m0 on of request b's head group hk against its
 // tiles x0 .. x1 - 1.  Writes O and lse, or, with `part`, the rows' results of
 // these tiles there.
@@ -310,6 +329,7 @@ __device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, int *mar
         const int j0 = view.start(x);
         const char *const kt = lds + buffer * 2 * TILE, *const vt = kt + TILE;
         lds_barrier();
+        const int lane = NW == 1 && MANY_PLACES<T, DC> ? anew(l) : l;
         if (wave_on) {
             f16v p[BN / 32];
 #pragma unroll
@@ -366,14 +386,14 @@ __device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, int *mar
                         }
 #pragma unroll
                         for (int j = 0; j < NJ; ++j) {
-                            const typename Op<T>::V v = col_frag<T, DP>(vt, 32 * n, s, j, l);
+                            const typename Op<T>::V v = col_frag<T, DP>(vt, 32 * n, s, j, lane);
                             o[j] = Op<T>::mma(v, first, o[j]);
                             o[j] = Op<T>::mma(v, second, o[j]);
                         }
                     } else {
                         const typename Op<T>::V pf = Op<T>::pack(p[n], s);
 #pragma unroll
-                        for (int j = 0; j < NJ; ++j) o[j] = Op<T>::mma(col_frag<T, DP>(vt, 32 * n, s, j, l), pf, o[j]);
+                        for (int j = 0; j < NJ; ++j) o[j] = Op<T>::mma(col_frag<T, DP>(vt, 32 * n, s, j, lane), pf, o[j]);
                     }
                 }
         }
@@ -431,9 +451,6 @@ __device__ __forceinline__ void pass(const PagedAttnArgs &a, char *lds, int *mar
         }
     if (a.lse && l < 32) a.lse[at * a.Hq + row.h] = lse;
 }
-
-// Waves a SIMD that registers are kept for (as gs_xattn.hip).
-template <typename T, int DC, int NW> constexpr int min_waves() { return sizeof(T) == 4 && (DC > 64 || NW == 1) ? 1 : 2; }
 
 // ------------------------------------------------------------ up to 16 rows
 
@@ -549,6 +566,7 @@ __device__ __forceinline__ void pass16(const PagedAttnArgs &a, char *lds, int b,
         if (on != ALL_LIVE<BN>) way.clean(on, l);
         if (differ(on, j0)) left_out |= __any(way.finite());
         lds_barrier();          // (one wave: keeps the accesses in order)
+        const int lane = MANY_PLACES<T, DC> ? anew(l) : l;
         way.template stash<true>(lds, a.Dh, l);
         fetch(x + 2);
         lds_barrier();
@@ -595,7 +613,7 @@ __device__ __forceinline__ void pass16(const PagedAttnArgs &a, char *lds, int b,
             }
         const typename Op16<T>::Terms terms(p);
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) o[j] = terms.add(Op16<T>::template col<DP>(lds + TILE, j, l), o[j]);
+        for (int j = 0; j < NJ; ++j) o[j] = terms.add(Op16<T>::template col<DP>(lds + TILE, j, lane), o[j]);
     }
     if (left_out) {
         for (int x = x0; x < x1; ++x) {
@@ -1015,8 +1033,8 @@ Layout layout(gs_dtype t, const PagedAttnArgs &a) {
     z.dp = padded(dc);
     z.few = rows <= FEW;
     if (z.few) {
-        // as many waves as the CUs hold at once, by their registers
-        const int held = t == GS_F32 && rows > 16 ? 4 : 8;
+        // as many waves as the CUs hold at once, by their registers (min_waves; 8 in pass16)
+        const int held = rows > 16 && (t == GS_F32 || dc > 64) ? 4 : 8;
         z.rows = (int)rows;
         z.least = 4;
         const int64_t most = ((int64_t)a.Lk / 16 + 3) * a.B / z.least + 1, full = 256 * held / a.Hkv;
