@@ -8,9 +8,9 @@
 // given back in this step: it is then read from the table of the request that
 // gave it (which the step does not write), not from the free list, so that no
 // part waits for another.  Latency bounds it: 250 requests of one more position
-// each, some 3000 pages given back, 10 us in one work-group; 700 prompts of
-// 702350 slots 4.2 us of sums and 11 of slots (a search of ten steps and a load,
-// four times a thread).
+// each, some 3000 pages given back, 8.6 us in one work-group; 700 prompts of
+// 702350 slots 4.2 us of sums and 10.4 of slots (a search of ten steps and a load,
+// four times a thread, one after the other).
 #include "gs_scan.h"
 
 namespace gs {
@@ -21,7 +21,7 @@ constexpr int STAGED = 2048;        // requests whose sums are searched in LDS
 
 // One work-group does the whole step where requests, rows and the pages that may be
 // given back are few.  (250 requests of 504 rows and 125000 pages at most, some 3000
-// of them given back: 10.0 us, in two launches 4.2 + 6.5 and their gap.)
+// of them given back: 8.6 us, in two launches 4.2 + 4.0, their gap and 3 us of the host's.)
 constexpr int64_t ONE_ROWS = 4096, ONE_PAGES = (int64_t)1 << 17;
 bool in_one(int64_t B, int64_t rows, int64_t width) { return B <= SCAN && rows <= ONE_ROWS && B * width <= ONE_PAGES; }
 
@@ -32,19 +32,24 @@ __device__ __forceinline__ int64_t up(int64_t x, int64_t page) {
     return x ? (int64_t)(((uint32_t)x - 1u) / (uint32_t)page + 1u) : 0;
 }
 
-// Sums over the requests as a step leaves them (B + 1 entries where there is a
-// total).  left: positions before the new ones, or -1 - that where the request
-// asked and got nothing.
+// Sums over the requests as a step leaves them, side by side (B + 1 entries where
+// there is a total).  left: positions before the new ones, or -1 - that where the
+// request asked and got nothing.
 struct PlanSums {
-    const int32_t *left, *back, *take, *qoff;
+    int32_t *at;
+    int64_t B;
+    __device__ __forceinline__ int32_t *left() const { return at; }
+    __device__ __forceinline__ int32_t *back() const { return at + B; }
+    __device__ __forceinline__ int32_t *take() const { return at + 2 * B + 1; }
+    __device__ __forceinline__ int32_t *qoff() const { return at + 3 * B + 2; }
+    static constexpr int size(int B) { return 4 * B + 3; }
 };
 
 __device__ __forceinline__ int32_t below(int64_t x, int64_t most) { return (int32_t)(x < most ? x : most); }
 
-// The sums, written to `left`, `back`, `take`, `rows_at` (as qoff) and the outputs
-// qoff, length_out, added and nfree_out.
-__device__ void plan_sums(const PagedPlanArgs &a, int32_t *left, int32_t *back, int32_t *take, int32_t *rows_at,
-                          PlanHead *head) {
+// The sums, written to z and the outputs qoff, length_out, added and nfree_out.
+__device__ void plan_sums(const PagedPlanArgs &a, const PlanSums &z, PlanHead *head) {
+    int32_t *const left = z.left(), *const back = z.back(), *const take = z.take(), *const rows_at = z.qoff();
     __shared__ int64_t room[4][SCAN / 64];
     __shared__ unsigned long long first_short;
     const int t = threadIdx.x;
@@ -126,21 +131,23 @@ __device__ __forceinline__ int owner(const int32_t *sums, int B, int i) {
 
 // Pages given back, pages taken and slots lie in one line, of which this does
 // number `first`, first + step, ...: one copy of the code for all three, which a
-// launch reads from memory each time.
+// launch reads from memory each time.  (What differs is chosen among numbers, not
+// among places of numbers: such a choice lays them out in memory, which each thread
+// wrote and read back.)
 __device__ void plan_fill(const PagedPlanArgs &a, const PlanSums &z, const PlanHead &head, int64_t first, int64_t step) {
     const int B = (int)a.B;
-    const int64_t ends[2] = {head.back, (int64_t)head.back + head.taken}, total = ends[1] + a.rows;
-    const int rows = B ? z.qoff[B] : 0;
+    const int64_t end0 = head.back, end1 = end0 + head.taken, total = end1 + a.rows;
+    const int rows = B ? z.qoff()[B] : 0;
     for (int64_t i = first; i < total; i += step) {
-        const int kind = (i >= ends[0]) + (i >= ends[1]);
-        const int k = (int)(i - (kind ? ends[kind - 1] : 0));
-        const int32_t *const sums = kind == 0 ? z.back : (kind == 1 ? z.take : z.qoff);
+        const int kind = (i >= end0) + (i >= end1);
+        const int k = (int)(i - (kind == 0 ? 0 : kind == 1 ? end0 : end1));
+        const int32_t *const sums = z.at + (kind == 0 ? z.B : kind == 1 ? 2 * z.B + 1 : 3 * z.B + 2);   // back, take, qoff
         int32_t id = -1;
         int64_t left = -1, held = 0, at = 0;
         int b = 0;
         if (kind < 2 || k < rows) {
             b = owner(sums, B, k);
-            left = z.left[b];
+            left = z.left()[b];
         }
         if (left >= 0) {
             held = up(left, a.page);
@@ -156,14 +163,14 @@ __device__ void plan_fill(const PagedPlanArgs &a, const PlanSums &z, const PlanH
                 const int64_t p = left + off, g = (uint32_t)p / (uint32_t)a.page;
                 at = p - g * a.page;
                 if (g < held) from += g;
-                else taken = z.take[b] + (int)(g - held);
+                else taken = z.take()[b] + (int)(g - held);
             }
             if (taken >= 0) {           // from the end of the free pages and the returned ones behind them
                 const int pos = head.avail - 1 - taken;
                 from = a.free_pages + pos;
                 if (pos >= head.nfree) {
-                    const int c = owner(z.back, B, pos - head.nfree);
-                    from = a.table + c * a.ldt + up(z.left[c], a.page) + (pos - head.nfree - z.back[c]);
+                    const int c = owner(z.back(), B, pos - head.nfree);
+                    from = a.table + c * a.ldt + up(z.left()[c], a.page) + (pos - head.nfree - z.back()[c]);
                 }
             }
             id = *from;
@@ -178,16 +185,16 @@ __device__ void plan_fill(const PagedPlanArgs &a, const PlanSums &z, const PlanH
 // are not those that are written, but for the free list's returned part, which is
 // read from the tables.
 __global__ void __launch_bounds__(SCAN) plan_kernel(PagedPlanArgs a) {
-    __shared__ int32_t left[SCAN], back[SCAN + 1], take[SCAN + 1], rows_at[SCAN + 1];
+    __shared__ int32_t sums[PlanSums::size(SCAN)];
     __shared__ PlanHead head;
-    plan_sums(a, left, back, take, rows_at, &head);
+    const PlanSums z{sums, a.B};
+    plan_sums(a, z, &head);
     __syncthreads();
-    plan_fill(a, PlanSums{left, back, take, rows_at}, head, threadIdx.x, SCAN);
+    plan_fill(a, z, head, threadIdx.x, SCAN);
 }
 
 __global__ void __launch_bounds__(SCAN) plan_sums_kernel(PagedPlanArgs a) {
-    int32_t *const at = a.sums;
-    plan_sums(a, at, at + a.B, at + 2 * a.B + 1, at + 3 * a.B + 2, a.head);
+    plan_sums(a, PlanSums{a.sums, a.B}, a.head);
 }
 
 template <bool LDS> __global__ void __launch_bounds__(256) plan_fill_kernel(PagedPlanArgs a) {
@@ -198,13 +205,11 @@ template <bool LDS> __global__ void __launch_bounds__(256) plan_fill_kernel(Page
     const PlanHead head = *a.head;
     if constexpr (LDS) {        // (asked for together: each load takes about a microsecond)
 #pragma unroll 4
-        for (int i = threadIdx.x; i < (4 * B + 6) / 4; i += 256) staged[i] = reinterpret_cast<const i4v *>(a.sums)[i];
+        for (int i = threadIdx.x; i < (PlanSums::size(B) + 3) / 4; i += 256) staged[i] = reinterpret_cast<const i4v *>(a.sums)[i];
         __syncthreads();
-        const int32_t *const at = reinterpret_cast<const int32_t *>(staged);
-        plan_fill(a, PlanSums{at, at + B, at + 2 * B + 1, at + 3 * B + 2}, head, first, step);
+        plan_fill(a, PlanSums{reinterpret_cast<int32_t *>(staged), a.B}, head, first, step);
     } else {
-        const int32_t *const at = a.sums;
-        plan_fill(a, PlanSums{at, at + B, at + 2 * B + 1, at + 3 * B + 2}, head, first, step);
+        plan_fill(a, PlanSums{a.sums, a.B}, head, first, step);
     }
 }
 
@@ -256,7 +261,7 @@ template <typename T> __device__ __forceinline__ void write8(const float (&v)[8]
 }
 
 // A thread moves eight values of K and of V.  Bound by HBM: 16000 rows of 8 heads of
-// 128 values, fp32 to bf16, 197 MB in 34 us, 5.7 TB/s.
+// 128 values, fp32 to bf16, of which 15000 have a slot, 185 MB in 34 us, 5.4 TB/s.
 template <typename T, typename C> __global__ void __launch_bounds__(256) store_kernel(PagedStoreArgs a) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= a.N * a.pieces) return;

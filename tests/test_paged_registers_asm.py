@@ -33,3 +33,12 @@ def test_attention(tmp_path):
     assert sum("10few_kernel" in n for n in found) == 24 and sum("11many_kernel" in n for n in found) == 12
     for name, (memory, spilled, _) in found.items():
         assert memory == 0 and spilled == 0, name
+
+
+def test_pages_and_rows(tmp_path):
+    """The plan's sums are all that it keeps in LDS: 4 for each of 1024 requests in one
+    work-group, of 2048 in the launch that follows them."""
+    found = kernels("gs_paged.hip", tmp_path)
+    for name, (memory, spilled, lds) in found.items():
+        assert memory == 0 and spilled == 0, name
+        assert lds <= 4 * (4 * (2048 if "plan_fill" in name else 1024) + 4) + 1024, (name, lds)
