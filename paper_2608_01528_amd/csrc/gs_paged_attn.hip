@@ -17,12 +17,16 @@
 // is put together by many_join_kernel.
 //
 // Few rows are bound by HBM: 48 requests of up to 7000 states, 32 heads over 8 of
-// 128 values, bf16, 643 MB in 115 us, 5.6 TB/s (reads alone in such pages reach 6.2),
-// and 5 us to join; one of 200001 states, 4 heads of keys, 410 MB in 78 + 7 us.  Equal
+// 128 values, bf16, 643 MB in 118 us, 5.5 TB/s (reads alone in such pages reach 6.2),
+// and 5 us to join; one of 200001 states, 4 heads of keys, 410 MB in 79 + 7 us.  Equal
 // parts of one line (rather than parts of each request) and all heads of a part side
 // by side: 199 -> 161 us; neighbours on one XCD: 154.  Many rows are bound by the
 // matrix cores, the exponentials and LDS in turn, as gs_xattn.hip's: 5 pieces of up to
-// 1500 rows on up to 6000 states, 442 us, 830 TF/s.
+// 1500 rows on up to 6000 states, 435 us, 840 TF/s.
+//
+// The form goes by the most rows of a request that the host names: one piece of a
+// prompt in a step puts its tokens into blocks of 128 rows too.  (40 tokens over up to
+// 7000 states and two pieces of 500 rows: 157 us in one call, 107 + 76 in two.)
 #include <algorithm>
 
 #include "gs_attn.h"

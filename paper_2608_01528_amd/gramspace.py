@@ -863,11 +863,14 @@ def gs_paged_attention(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, tabl
     row each) at its last positions, of which each sees the states up to its
     own (window > 0: the last `window` of them and the first `sinks`).
     max_new, max_len: most rows and states of a request, as far as they are
-    known (N, and what the table has room for, otherwise).  scale 1 / sqrt(Dh)
-    by default.  added (int32, B): the positions each request got from the
-    plan; the rows of one that got none see no state (O = 0, lse = -inf).
-    Returns O, or (O, lse) with lse (N, Hq) fp32; rows of no request are not
-    written."""
+    known (N, and what the table has room for, otherwise).  They choose the
+    kernels: name max_new where it is below N (with max_new Hq / Hkv up to 32,
+    tokens and drafts, a request costs what its states do; beyond, each takes
+    blocks of 128 rows).  Q, out and the cache are of one type.  scale
+    1 / sqrt(Dh) by default.  added (int32, B): the positions each request got
+    from the plan; the rows of one that got none see no state (O = 0, lse =
+    -inf).  Returns O, or (O, lse) with lse (N, Hq) fp32, no part of torch's
+    graph; rows of no request are not written."""
     t, c, at = _cache(Kc, Vc)
     q = Q.shape
     if len(q) != 3 or q[2] != c[3]:
